@@ -12,6 +12,9 @@
  *       average of the m-b candidates with the highest scores.
  *   Section 6.1.1 baselines: Mean, and Definition 4 (marginal Median).
  *
+ * and, for models that answer with tokens, the operators of both sides of Algorithm 1 around it: log probabilities and layer norm
+ * with their gradients, activations in 8 bits, weight gradients per worker, and Definition 2 from log probabilities.
+ *
  * Conventions shared by every call
  * --------------------------------
  * Pointers.  Arguments marked DEVICE point to HIP device memory of the current
@@ -243,6 +246,129 @@ size_t zeno_krum_workspace_bytes(int32_t m);
 zeno_status_t zeno_krum(const float* G, int64_t ldg, int32_t m, int64_t d, int32_t b, float* out, int32_t* chosen,
                         float* krum_scores, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Models that answer with tokens -------------------------------------------------------------------------------------
+ * What a worker and the server of Algorithm 1 need where f is the mean of -log p(token) over the tokens of a batch: the loss with
+ * its gradient, layer norm with its gradient, activations kept in 8 bits for the backward pass, the gradient of a linear layer's
+ * weights, and Definition 2 from the log probabilities of the m+1 models.  Gradients of parameters are written as float32
+ * straight into rows of G, one row for each worker.
+ *
+ * Activations, logits and their gradients are matrices of `dtype`, rows a given number of elements apart (>= the row's length),
+ * aligned to their element; any row length and any pitch is accepted, and pitches that are a multiple of 16 bytes are fastest.
+ * Sums, statistics and parameters are float32.  A result in 16 bits is rounded once, from float32.
+ * Groups.  The rows of a batch belong to m workers: rows offsets[g] .. offsets[g+1]-1 to worker g.  `offsets` is DEVICE int32
+ *   [m+1], ascending, within 0..rows; NULL: all rows belong to one group (m = 1).  Groups may be empty: their gradients are zero.
+ *   Rows before offsets[0] and from offsets[m] on belong to nobody: they are not read, and their rows of dx are left as they were.
+ *   Offsets that break these rules give wrong gradients, but nothing outside the arguments is read or written.
+ * Sums over rows are taken in an order that depends on the sizes and offsets alone: equal calls give equal bits.
+ * Outputs must not overlap inputs or each other, except where a call says so.  No call waits, allocates or reads device
+ * memory on the host, so all of them may be captured into a graph; calls that may overlap in time need workspaces of their own. */
+typedef enum { ZENO_F32 = 0, ZENO_BF16 = 1, ZENO_F16 = 2 } zeno_dtype_t;
+
+#define ZENO_MAX_TOP 32           /* alternatives per token */
+#define ZENO_MAX_VOCAB (1 << 30)
+#define ZENO_MAX_WIDTH (1 << 24)  /* columns of activations */
+
+/* Log probabilities of given tokens, entropy and the most probable tokens of every row of logits z:
+ *   log p_j = z_j - log sum_i exp z_i,   H = - sum_j p_j log p_j   (natural logarithms).
+ *   logits     DEVICE [rows x vocab], rows ldz >= vocab elements apart, 1 <= vocab <= ZENO_MAX_VOCAB; rows >= 0
+ *   labels     DEVICE [rows] or NULL (then logp is NULL too).  -1: the token does not count, its log probability is written as 0;
+ *              any other label outside 0..vocab-1 gives NaN (nothing is read out of bounds)
+ *   logp       DEVICE [rows] out, or NULL
+ *   entropy    DEVICE [rows] out, or NULL
+ *   stats      DEVICE [rows x 2] out, or NULL: max z and log sum exp(z - max z), which zeno_logprobs_backward takes
+ *   top        0..min(ZENO_MAX_TOP, vocab); top_index DEVICE [rows x top] int32 and top_logp DEVICE [rows x top] out: the `top` largest
+ *              logits' indices, the largest first, ties to the lower index, and their log probabilities; both NULL if top is 0
+ * -inf is a token that cannot be drawn: probability 0, log probability -inf.  A row of nothing but -inf has no distribution: its log
+ * probabilities are -inf, its entropy 0, its stats (-inf, 0), its gradient 0.  A row with a NaN or +inf gives NaN; in the choice of the
+ * alternatives a NaN ranks as -inf.
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_logprobs_workspace_bytes(rows, vocab, top) */
+size_t zeno_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
+zeno_status_t zeno_logprobs(const void* logits, int64_t ldz, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* labels,
+                            float* logp, float* entropy, float* stats, int32_t top, int32_t* top_index, float* top_logp,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of the logits, for gradients g of logp, h of the entropy and q of the alternatives' log probabilities:
+ *   dz_j = g [j = label] + sum_k q_k [j = top_index_k] - p_j (g + sum_k q_k + h (log p_j + H)).
+ *   stats, entropy  as zeno_logprobs wrote them (entropy only if grad_entropy is given)
+ *   labels, grad_logp        DEVICE [rows] or both NULL; a row with label -1 takes no part in g
+ *   grad_entropy             DEVICE [rows] or NULL
+ *   top, top_index, grad_top DEVICE [rows x top]; top = 0 and grad_top NULL if not wanted.  An index that stands twice counts twice;
+ *                            one outside 0..vocab-1 makes the row NaN
+ *   dlogits    DEVICE [rows x vocab] of the same dtype out, rows ldd apart; may be the logits themselves with ldd = ldz
+ * At least one of the three gradients is given. */
+zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dtype, int32_t rows, int32_t vocab,
+                                     const float* stats, const int32_t* labels, const float* grad_logp, const float* entropy,
+                                     const float* grad_entropy, int32_t top, const int32_t* top_index, const float* grad_top,
+                                     void* dlogits, int64_t ldd, void* stream);
+
+/* A checkpoint holds activations in 8 bits: e4m3 values (OCP: 4 exponent and 3 mantissa bits, no infinities) in blocks of 32 columns
+ * that share a power-of-two scale, 33/32 bytes per value.
+ *   values  DEVICE [rows x 32 ceil(width/32)] bytes, 16-byte aligned, the columns behind the last zero
+ *   scales  DEVICE [rows x ceil(width/32)] bytes: the scale of a block is 2^(byte - 127), the smallest that brings its largest finite
+ *           magnitude to 448 or less
+ * A value is off by at most 2^-4 of itself or 2^-10 of its block's scale, whichever is larger.  Infinities and NaN are kept as NaN
+ * and do not enter the scale.  Rows can be taken out of a checkpoint by moving both pointers.
+ *   x  DEVICE [rows x width], rows ldx apart, 1 <= width <= ZENO_MAX_WIDTH */
+zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, uint8_t* values,
+                              uint8_t* scales, void* stream);
+/* The values of a checkpoint as a matrix of `dtype`, for a backward pass of the caller's own.  Exact in float32 and bf16, except that a
+ * value which was rounded up past the type's largest comes back as the largest. */
+zeno_status_t zeno_checkpoint_values(const uint8_t* values, const uint8_t* scales, int32_t rows, int32_t width, int32_t dtype,
+                                     void* out, int64_t ldo, void* stream);
+
+/* Layer norm: y = weight (x - mean) rstd + bias with rstd = 1 / sqrt(var + eps), mean and var (of the population) over a row.
+ *   x, y          DEVICE [rows x width] of the same dtype
+ *   weight, bias  DEVICE [width] float32, as they stand in a parameter vector (4-byte aligned); bias may be NULL
+ *   eps           finite, > 0
+ *   mean, rstd    DEVICE [rows] float32 out (zeno_layer_norm_backward takes them), or NULL
+ *   values, scales  a checkpoint of x to write in the same pass, bit for bit what zeno_checkpoint writes, or both NULL */
+zeno_status_t zeno_layer_norm(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, const float* weight,
+                              const float* bias, float eps, void* y, int64_t ldy, float* mean, float* rstd, uint8_t* values,
+                              uint8_t* scales, void* stream);
+
+/* Its backward pass.  With xh = (x - mean) rstd and a = weight dy:
+ *   dx = rstd (a - mean(a) - xh mean(a xh)),  dweight_g = sum of dy xh over the rows of group g,  dbias_g = sum of dy.
+ *   x  as in the forward pass, or NULL: then values and scales are a checkpoint of it, whose values stand for x
+ *   dx       DEVICE [rows x width], of dy's dtype, or NULL; may be dy itself with lddx = lddy
+ *   dweight, dbias  DEVICE, group g's at dweight + g ldw and dbias + g ldb (columns of rows of G; ldw, ldb >= width), or NULL
+ *   m, offsets      groups (above), 1 <= m <= ZENO_MAX_CANDIDATES
+ * At least one output is given.
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_layer_norm_workspace_bytes(rows, width, m) */
+size_t zeno_layer_norm_workspace_bytes(int32_t rows, int32_t width, int32_t m);
+zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t width, const void* x,
+                                       int64_t ldx, const uint8_t* values, const uint8_t* scales, const float* mean,
+                                       const float* rstd, const float* weight, int32_t m, const int32_t* offsets, void* dx,
+                                       int64_t lddx, float* dweight, int64_t ldw, float* dbias, int64_t ldb, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/* Gradient of a linear layer's weights, y = W a + bias, from a checkpoint of its input a:
+ *   dW_g[o][k] = sum over the rows t of group g of dy[t][o] a[t][k],   dbias_g[o] = sum of dy[t][o].
+ * The products are exact (dy enters as one bf16 piece, as two if it is fp16 and as three if it is float32; products of operands below
+ * about 1e-33 keep fewer bits) and are summed in float32.
+ *   dy       DEVICE [rows x out], rows lddy apart
+ *   values, scales  checkpoint of the input, [rows x width]
+ *   dweight  DEVICE, group g's [out x width] row-major matrix at dweight + g ldw, ldw >= out * width
+ *   dbias    DEVICE, group g's [out] at dbias + g ldb, ldb >= out, or NULL
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_weight_gradient_workspace_bytes(rows, out, width, m)
+ * UNSUPPORTED where out * width is too large for one launch (from about 2^37 on). */
+size_t zeno_weight_gradient_workspace_bytes(int32_t rows, int32_t out, int32_t width, int32_t m);
+zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t out, const uint8_t* values,
+                                   const uint8_t* scales, int32_t width, int32_t m, const int32_t* offsets, float* dweight,
+                                   int64_t ldw, float* dbias, int64_t ldb, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Definition 2 for models whose forward passes are the caller's: f_r is the mean of -log p over the n tokens of the server's batch, and
+ *   scores[i] = mean_t (logp[i][t] - logp_x[t]) - rho ||G[i]||^2.
+ *   G, ldg  as for zeno_score (d = the row length)
+ *   logp_x  DEVICE [n] log probabilities at x;  logp DEVICE [m x n], rows ldp >= n apart: at x - gamma G[i]
+ *   labels  DEVICE [n] or NULL: tokens with label -1 do not count.  Where none counts the loss difference is 0
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_score_logprobs_workspace_bytes(m, d)
+ * Differences, mean and norm are float64, rounded once; what the log probabilities themselves are rounded by (2^-24 of them) stays in
+ * the difference. */
+size_t zeno_score_logprobs_workspace_bytes(int32_t m, int64_t d);
+zeno_status_t zeno_score_logprobs(const float* G, int64_t ldg, int32_t m, int64_t d, const float* logp_x, const float* logp,
+                                  int64_t ldp, int32_t n, const int32_t* labels, float rho, float* scores, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* Text of a status code; any other value gives "unknown status". */
 const char* zeno_status_string(int32_t status);
 
@@ -284,7 +410,15 @@ typedef enum {
   ZENO_KERNEL_CONV_CAND = 11,     /* one convolution of the m candidate passes and the pass at x through the next one, in the last
                                      one mostly through a fully connected layer of at most 32 outputs (which then has no
                                      LAYER_BASE record); one or two launches */
-  ZENO_KERNEL_AUX = 12            /* fills of padded operands */
+  ZENO_KERNEL_AUX = 12,           /* fills of padded operands */
+  /* one record for all launches of a call: */
+  ZENO_KERNEL_LOGPROBS = 13,
+  ZENO_KERNEL_LOGPROBS_GRAD = 14,
+  ZENO_KERNEL_LAYER_NORM = 15,
+  ZENO_KERNEL_LAYER_NORM_GRAD = 16,
+  ZENO_KERNEL_CHECKPOINT = 17,    /* either direction */
+  ZENO_KERNEL_WEIGHT_GRAD = 18,
+  ZENO_KERNEL_SCORE_LOGPROBS = 19
 } zeno_kernel_t;
 
 typedef struct {

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -24,11 +25,17 @@ STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported size", 3: "workspace",
 EXPORTS = ["zeno_model_create", "zeno_cnn_model_create", "zeno_model_destroy", "zeno_model_num_params",
            "zeno_score_workspace_bytes", "zeno_score", "zeno_score_static", "zeno_aggregate", "zeno_aggregate_update", "zeno_mean",
            "zeno_median", "zeno_krum_workspace_bytes", "zeno_krum", "zeno_status_string", "zeno_profile_enable", "zeno_profile_collect",
-           "zeno_score_plan_check"]
+           "zeno_score_plan_check", "zeno_logprobs_workspace_bytes", "zeno_logprobs", "zeno_logprobs_backward", "zeno_checkpoint",
+           "zeno_checkpoint_values", "zeno_layer_norm", "zeno_layer_norm_workspace_bytes", "zeno_layer_norm_backward",
+           "zeno_weight_gradient_workspace_bytes", "zeno_weight_gradient", "zeno_score_logprobs_workspace_bytes",
+           "zeno_score_logprobs"]
 
 KERNEL_NAMES = ["pack", "layer_base", "layer_cand", "loss", "combine", "average", "mean", "median", "average_update",
-                "krum", "conv_base", "conv_cand", "aux"]
+                "krum", "conv_base", "conv_cand", "aux", "logprobs", "logprobs_grad", "layer_norm", "layer_norm_grad", "checkpoint",
+                "weight_grad", "score_logprobs"]
 ZENO_MAX_CONV = 8
+ZENO_MAX_TOP = 32
+DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class ZenoError(RuntimeError):
@@ -112,6 +119,22 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.zeno_krum.restype = ctypes.c_int
     lib.zeno_score_plan_check.argtypes = [vp, i32, i32]
     lib.zeno_score_plan_check.restype = ctypes.c_int
+    size = ctypes.c_size_t
+    for name, res, args in [
+            ("zeno_logprobs_workspace_bytes", size, [i32, i32, i32]),
+            ("zeno_logprobs", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, size, vp]),
+            ("zeno_logprobs_backward", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, i64, vp]),
+            ("zeno_checkpoint", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, vp]),
+            ("zeno_checkpoint_values", ctypes.c_int, [vp, vp, i32, i32, i32, vp, i64, vp]),
+            ("zeno_layer_norm", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp, vp, vp]),
+            ("zeno_layer_norm_workspace_bytes", size, [i32, i32, i32]),
+            ("zeno_layer_norm_backward", ctypes.c_int,
+             [vp, i64, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, i64, vp, size, vp]),
+            ("zeno_weight_gradient_workspace_bytes", size, [i32, i32, i32, i32]),
+            ("zeno_weight_gradient", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, i64, vp, i64, vp, size, vp]),
+            ("zeno_score_logprobs_workspace_bytes", size, [i32, i64]),
+            ("zeno_score_logprobs", ctypes.c_int, [vp, i64, i32, i64, vp, vp, i64, i32, vp, f32, vp, vp, size, vp])]:
+        getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
     lib.zeno_profile_enable.argtypes = [i32]
     lib.zeno_profile_enable.restype = ctypes.c_int
     lib.zeno_profile_collect.argtypes = [ctypes.POINTER(_ProfileRecord), i32]
@@ -401,6 +424,311 @@ def zeno_krum(G, b, *, out=None, want_scores=True, workspace=None):
     if st != 0:
         raise ZenoError(st, "zeno_krum")
     return out, chosen, ks
+
+
+# ---- models that answer with tokens
+
+class Checkpoint(NamedTuple):
+    """Activations [rows x width] in 8 bits: e4m3 values [rows x 32 ceil(width/32)] and, for every 32 columns, the byte of a scale
+    2^(byte - 127), both uint8 and contiguous."""
+    values: torch.Tensor
+    scales: torch.Tensor
+    width: int
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    """A tensor of the current device (a call runs on the current stream of that device)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA/HIP tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+
+
+def _vec(t, dtype, name: str, shape):
+    """Device pointer of a contiguous tensor of the given shape, or None."""
+    if t is None:
+        return None
+    _here(t, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev(t, dtype, name)
+
+
+def _matrix(t, name: str, shape=None, dtype=None):
+    """(pointer, pitch, dtype code, rows, columns) of a 2-D matrix whose rows are contiguous and do not overlap."""
+    _here(t, name)
+    if t.dtype not in DTYPE or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must have dtype {dtype or list(DTYPE)}, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be a matrix of shape {tuple(shape) if shape is not None else '(rows, columns)'}, "
+                         f"got {tuple(t.shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    pitch = int(t.stride(0)) if rows > 1 else int(cols)
+    if pitch < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.data_ptr(), pitch, DTYPE[t.dtype], int(rows), int(cols)
+
+
+def _grad_rows(t, name: str, m: int, n: int):
+    """(pointer, pitch) of m rows of n float32 gradients: columns of G, or a tensor of its own."""
+    if t is None:
+        return None, n
+    ptr, pitch, _, _, _ = _matrix(t, name, (m, n), torch.float32)
+    return ptr, pitch
+
+
+def _kept(ckpt: Checkpoint, rows: int):
+    if not isinstance(ckpt, Checkpoint):
+        raise ValueError("a Checkpoint is needed")
+    blocks = (int(ckpt.width) + 31) // 32
+    return (_vec(ckpt.values, torch.uint8, "values", (rows, 32 * blocks)), _vec(ckpt.scales, torch.uint8, "scales", (rows, blocks)))
+
+
+def _groups(groups, m_of):
+    """(m, device pointer) of a group offset tensor [m + 1]; None: one group."""
+    if groups is None:
+        return 1, None
+    if not isinstance(groups, torch.Tensor) or groups.dim() != 1 or groups.numel() < 2:
+        raise ValueError(f"groups must hold the m + 1 row offsets of the {m_of}")
+    return int(groups.numel()) - 1, _vec(groups, torch.int32, "groups", groups.shape)
+
+
+def _workspace(n: int, where: str, device=None) -> torch.Tensor:
+    if n == 0:
+        raise ZenoError(1, where)
+    return torch.empty(n, dtype=torch.uint8, device=device or torch.device("cuda", torch.cuda.current_device()))
+
+
+def alloc_logprobs_workspace(rows: int, vocab: int, top: int = 0, device=None) -> torch.Tensor:
+    return _workspace(int(load_library().zeno_logprobs_workspace_bytes(int(rows), int(vocab), int(top))),
+                      "zeno_logprobs_workspace_bytes", device)
+
+
+def zeno_logprobs(logits, labels=None, *, top=0, want_entropy=False, want_stats=False, logp=None, entropy=None, stats=None,
+                  top_index=None, top_logp=None, workspace=None):
+    """Log probabilities of the labels (int32 [rows]; -1: does not count, 0 is written), entropy and the `top` most probable
+    tokens of the rows of logits.  Returns (logp, entropy, stats, top_index, top_logp), None where not wanted; `stats`
+    [rows x 2] is what zeno_logprobs_backward takes."""
+    lib = load_library()
+    ptr, pitch, code, rows, vocab = _matrix(logits, "logits")
+    top, dev, f32 = int(top), logits.device, torch.float32
+    if labels is not None and logp is None:
+        logp = torch.empty(rows, dtype=f32, device=dev)
+    if want_entropy and entropy is None:
+        entropy = torch.empty(rows, dtype=f32, device=dev)
+    if want_stats and stats is None:
+        stats = torch.empty((rows, 2), dtype=f32, device=dev)
+    if top > 0 and top_index is None:
+        top_index = torch.empty((rows, top), dtype=torch.int32, device=dev)
+    if top > 0 and top_logp is None:
+        top_logp = torch.empty((rows, top), dtype=f32, device=dev)
+    if workspace is None:
+        workspace = alloc_logprobs_workspace(rows, vocab, top, dev)
+    _here(workspace, "workspace")
+    st = lib.zeno_logprobs(ptr, pitch, code, rows, vocab, _vec(labels, torch.int32, "labels", (rows,)),
+                           _vec(logp, f32, "logp", (rows,)), _vec(entropy, f32, "entropy", (rows,)),
+                           _vec(stats, f32, "stats", (rows, 2)), top,
+                           _vec(top_index, torch.int32, "top_index", (rows, top)) if top else None,
+                           _vec(top_logp, f32, "top_logp", (rows, top)) if top else None,
+                           _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_logprobs")
+    return logp, entropy, stats, top_index, top_logp
+
+
+def zeno_logprobs_backward(logits, stats, *, labels=None, grad_logp=None, entropy=None, grad_entropy=None, top_index=None,
+                           grad_top=None, out=None):
+    """Gradient of the logits from the gradients of logp [rows], of the entropy [rows] and of top_logp [rows x top], whichever
+    are given.  out=logits works in place."""
+    lib = load_library()
+    ptr, pitch, code, rows, vocab = _matrix(logits, "logits")
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    o_ptr, o_pitch, _, _, _ = _matrix(out, "out", (rows, vocab), logits.dtype)
+    f32 = torch.float32
+    top = 0
+    if grad_top is not None:
+        if not isinstance(grad_top, torch.Tensor) or grad_top.dim() != 2 or grad_top.shape[1] == 0:
+            raise ValueError("grad_top must have shape (rows, top)")
+        top = int(grad_top.shape[1])
+    st = lib.zeno_logprobs_backward(ptr, pitch, code, rows, vocab, _vec(stats, f32, "stats", (rows, 2)),
+                                    _vec(labels, torch.int32, "labels", (rows,)), _vec(grad_logp, f32, "grad_logp", (rows,)),
+                                    _vec(entropy, f32, "entropy", (rows,)), _vec(grad_entropy, f32, "grad_entropy", (rows,)), top,
+                                    _vec(top_index, torch.int32, "top_index", (rows, top)) if top else None,
+                                    _vec(grad_top, f32, "grad_top", (rows, top)), o_ptr, o_pitch, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_logprobs_backward")
+    return out
+
+
+def alloc_checkpoint(rows: int, width: int, device=None) -> Checkpoint:
+    device = device or torch.device("cuda", torch.cuda.current_device())
+    blocks = (int(width) + 31) // 32
+    return Checkpoint(torch.empty((int(rows), 32 * blocks), dtype=torch.uint8, device=device),
+                      torch.empty((int(rows), blocks), dtype=torch.uint8, device=device), int(width))
+
+
+def zeno_checkpoint(x, *, out=None) -> Checkpoint:
+    """The activations x [rows x width] in 8 bits."""
+    lib = load_library()
+    ptr, pitch, code, rows, width = _matrix(x, "x")
+    if out is None:
+        out = alloc_checkpoint(rows, width, x.device)
+    if not isinstance(out, Checkpoint) or out.width != width:
+        raise ValueError("out must be a Checkpoint of x's width")
+    v, s = _kept(out, rows)
+    st = lib.zeno_checkpoint(ptr, pitch, code, rows, width, v, s, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_checkpoint")
+    return out
+
+
+def zeno_checkpoint_values(ckpt: Checkpoint, dtype=torch.float32, *, out=None):
+    """The values that a checkpoint holds, [rows x width] of the given type."""
+    lib = load_library()
+    if not isinstance(ckpt, Checkpoint):
+        raise ValueError("a Checkpoint is needed")
+    rows = int(ckpt.values.shape[0])
+    if out is None:
+        out = torch.empty((rows, ckpt.width), dtype=dtype, device=ckpt.values.device)
+    ptr, pitch, code, _, width = _matrix(out, "out", (rows, ckpt.width))
+    v, s = _kept(ckpt, rows)
+    st = lib.zeno_checkpoint_values(v, s, rows, width, code, ptr, pitch, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_checkpoint_values")
+    return out
+
+
+def zeno_layer_norm(x, weight, bias=None, eps=1e-5, *, y=None, mean=None, rstd=None, want_checkpoint=False, checkpoint=None):
+    """Layer norm of the rows of x; weight and bias float32 [width].  Returns (y, mean, rstd, Checkpoint of x or None)."""
+    lib = load_library()
+    ptr, pitch, code, rows, width = _matrix(x, "x")
+    if y is None:
+        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+    y_ptr, y_pitch, _, _, _ = _matrix(y, "y", (rows, width), x.dtype)
+    if mean is None:
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if want_checkpoint and checkpoint is None:
+        checkpoint = alloc_checkpoint(rows, width, x.device)
+    v = s = None
+    if checkpoint is not None:
+        if not isinstance(checkpoint, Checkpoint) or checkpoint.width != width:
+            raise ValueError("checkpoint must be a Checkpoint of x's width")
+        v, s = _kept(checkpoint, rows)
+    st = lib.zeno_layer_norm(ptr, pitch, code, rows, width, _vec(weight, torch.float32, "weight", (width,)),
+                             _vec(bias, torch.float32, "bias", (width,)), float(eps), y_ptr, y_pitch,
+                             _vec(mean, torch.float32, "mean", (rows,)), _vec(rstd, torch.float32, "rstd", (rows,)), v, s, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_layer_norm")
+    return y, mean, rstd, checkpoint
+
+
+def alloc_layer_norm_workspace(rows: int, width: int, m: int = 1, device=None) -> torch.Tensor:
+    return _workspace(int(load_library().zeno_layer_norm_workspace_bytes(int(rows), int(width), int(m))),
+                      "zeno_layer_norm_workspace_bytes", device)
+
+
+def zeno_layer_norm_backward(dy, x, mean, rstd, weight, *, groups=None, want_dx=True, want_weight=True, want_bias=True, dx=None,
+                             dweight=None, dbias=None, workspace=None):
+    """Backward pass of zeno_layer_norm; x is its input or a Checkpoint of it.  groups: int32 row offsets [m + 1] of the m
+    workers (None: one group).  dweight and dbias are [m x width] float32, for instance column slices of G.  dx=dy works in
+    place; rows that belong to no group keep what dx held (zeros if dx is not given).  Returns (dx, dweight, dbias)."""
+    lib = load_library()
+    ptr, pitch, code, rows, width = _matrix(dy, "dy")
+    m, offsets = _groups(groups, "workers")
+    kept = isinstance(x, Checkpoint)
+    v = s = x_ptr = None
+    x_pitch = width
+    if kept:
+        if x.width != width:
+            raise ValueError("the checkpoint's width is not dy's")
+        v, s = _kept(x, rows)
+    else:
+        x_ptr, x_pitch, _, _, _ = _matrix(x, "x", (rows, width), dy.dtype)
+    if want_dx and dx is None:
+        dx = (torch.empty if groups is None else torch.zeros)((rows, width), dtype=dy.dtype, device=dy.device)
+    if want_weight and dweight is None:
+        dweight = torch.empty((m, width), dtype=torch.float32, device=dy.device)
+    if want_bias and dbias is None:
+        dbias = torch.empty((m, width), dtype=torch.float32, device=dy.device)
+    d_ptr, d_pitch = None, width
+    if dx is not None:
+        d_ptr, d_pitch, _, _, _ = _matrix(dx, "dx", (rows, width), dy.dtype)
+    w_ptr, ldw = _grad_rows(dweight, "dweight", m, width)
+    b_ptr, ldb = _grad_rows(dbias, "dbias", m, width)
+    if workspace is None:
+        workspace = alloc_layer_norm_workspace(rows, width, m, dy.device)
+    _here(workspace, "workspace")
+    st = lib.zeno_layer_norm_backward(ptr, pitch, code, rows, width, x_ptr, x_pitch, v, s,
+                                      _vec(mean, torch.float32, "mean", (rows,)), _vec(rstd, torch.float32, "rstd", (rows,)),
+                                      _vec(weight, torch.float32, "weight", (width,)), m, offsets, d_ptr, d_pitch, w_ptr, ldw, b_ptr,
+                                      ldb, _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def alloc_weight_gradient_workspace(rows: int, out: int, width: int, m: int = 1, device=None) -> torch.Tensor:
+    return _workspace(int(load_library().zeno_weight_gradient_workspace_bytes(int(rows), int(out), int(width), int(m))),
+                      "zeno_weight_gradient_workspace_bytes", device)
+
+
+def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, dweight=None, dbias=None, workspace=None):
+    """Gradient of a linear layer's weights (and bias) for each of the m workers, from dy [rows x out] and a Checkpoint of the
+    layer's input.  dweight [m x out * width] and dbias [m x out] are float32, for instance column slices of G."""
+    lib = load_library()
+    ptr, pitch, code, rows, out = _matrix(dy, "dy")
+    m, offsets = _groups(groups, "workers")
+    v, s = _kept(ckpt, rows)
+    width = int(ckpt.width)
+    if dweight is None:
+        dweight = torch.empty((m, out * width), dtype=torch.float32, device=dy.device)
+    if want_bias and dbias is None:
+        dbias = torch.empty((m, out), dtype=torch.float32, device=dy.device)
+    w_ptr, ldw = _grad_rows(dweight, "dweight", m, out * width)
+    b_ptr, ldb = _grad_rows(dbias, "dbias", m, out)
+    if workspace is None:
+        workspace = alloc_weight_gradient_workspace(rows, out, width, m, dy.device)
+    _here(workspace, "workspace")
+    st = lib.zeno_weight_gradient(ptr, pitch, code, rows, out, v, s, width, m, offsets, w_ptr, ldw, b_ptr, ldb,
+                                  _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_weight_gradient")
+    return dweight, dbias
+
+
+def alloc_score_logprobs_workspace(m: int, d: int, device=None) -> torch.Tensor:
+    return _workspace(int(load_library().zeno_score_logprobs_workspace_bytes(int(m), int(d))),
+                      "zeno_score_logprobs_workspace_bytes", device)
+
+
+def zeno_score_logprobs(G, logp_x, logp, rho, *, labels=None, scores=None, workspace=None):
+    """scores[i] = mean_t (logp[i][t] - logp_x[t]) - rho ||G[i]||^2  (Definition 2 for the mean of -log p); tokens with
+    label -1 do not count."""
+    lib = load_library()
+    _here(G, "G")
+    g_ptr, ldg = _rows(G)
+    m, d = int(G.shape[0]), int(G.shape[1])
+    if not isinstance(logp_x, torch.Tensor) or logp_x.dim() != 1:
+        raise ValueError("logp_x must be a vector")
+    n = int(logp_x.numel())
+    p_ptr, ldp, _, _, _ = _matrix(logp, "logp", (m, n), torch.float32)
+    if scores is None:
+        scores = torch.empty(m, dtype=torch.float32, device=G.device)
+    if workspace is None:
+        workspace = alloc_score_logprobs_workspace(m, d, G.device)
+    _here(workspace, "workspace")
+    st = lib.zeno_score_logprobs(g_ptr, ldg, m, d, _vec(logp_x, torch.float32, "logp_x", (n,)), p_ptr, ldp, n,
+                                 _vec(labels, torch.int32, "labels", (n,)), float(rho),
+                                 _vec(scores, torch.float32, "scores", (m,)), _dev(workspace, torch.uint8, "workspace"),
+                                 workspace.numel(), _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_score_logprobs")
+    return scores
 
 
 def profile_enable(on: bool = True):

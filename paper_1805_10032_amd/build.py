@@ -20,9 +20,11 @@ OBJ_DIR = os.path.join(HERE, "_build")
 # (source, object suffix, extra flags).  The streaming layer kernel's four instantiation files are compiled once per
 # number of row blocks (four of them in bf16 only), longest first, so that ten objects build in parallel.
 LAYER_UNITS = ["zeno_layer_bf16_delta.hip", "zeno_layer_bf16_first.hip", "zeno_layer_f32_delta.hip", "zeno_layer_f32_first.hip"]
+TOKEN_SOURCES = ("zeno_logprobs.hip", "zeno_norm.hip", "zeno_checkpoint.hip", "zeno_weight.hip", "zeno_score_tokens.hip")
 SOURCES = ([(u, f"_mb{mb}", [f"-DZENO_LAYER_MB={mb}"]) for mb in (4, 2, 1) for u in LAYER_UNITS if mb < 4 or "bf16" in u] +
            [(s, "", []) for s in ("zeno_median.hip", "zeno_krum.hip", "zeno_capi.hip", "zeno_layer.hip", "zeno_loss.hip",
-                                  "zeno_aggregate.hip", "zeno_median_select.hip", "zeno_conv.hip", "zeno_small.hip", "zeno_first.hip")])
+                                  "zeno_aggregate.hip", "zeno_median_select.hip", "zeno_conv.hip", "zeno_small.hip", "zeno_first.hip",
+                                  *TOKEN_SOURCES)])
 
 # Packed-fp32 instruction selection is switched off for all device code.
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -53,6 +55,8 @@ def _fresh(obj, src, stamp):
             deps.append(os.path.join(CSRC, "zeno_split.h"))
         if src == "zeno_conv.hip":
             deps.append(os.path.join(CSRC, "zeno_index.h"))
+        if src in TOKEN_SOURCES or src == "zeno_capi.hip":
+            deps.append(os.path.join(CSRC, "zeno_tokens.h"))
         return all(os.path.getmtime(d) < t for d in deps)
     except OSError:
         return False

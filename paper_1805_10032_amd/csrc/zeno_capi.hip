@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "zeno_internal.h"
+#include "zeno_tokens.h"
 
 // Scratch of zeno_score_static: a file-scope device array, one copy per GPU at that GPU's own
 // address, held until the process ends.  In host code this name is only a handle for
@@ -210,6 +211,20 @@ struct ProfScope {
     if (slot < (int)g_prof.size()) (void)hipEventRecord(g_prof[slot].stop, stream);
   }
 };
+
+int dtype_bytes(int dtype) { return dtype == ZENO_F32 ? 4 : 2; }
+
+// A matrix argument of the token operators; one without rows needs no memory.
+bool matrix_ok(const void* p, int64_t ld, int32_t dtype, int32_t rows, int32_t cols) {
+  if (dtype != ZENO_F32 && dtype != ZENO_BF16 && dtype != ZENO_F16) return false;
+  return rows >= 0 && cols >= 1 && ld >= cols && (rows == 0 || p != nullptr) && aligned(p, dtype_bytes(dtype));
+}
+bool checkpoint_ok(const uint8_t* values, const uint8_t* scales, int32_t rows) {
+  return (rows == 0 || (values != nullptr && scales != nullptr)) && aligned(values, 16);
+}
+bool groups_ok(int32_t m, const int32_t* offsets) {
+  return m >= 1 && m <= ZENO_MAX_CANDIDATES && (offsets != nullptr || m == 1) && aligned(offsets, 4);
+}
 
 zeno_status_t check_score_args(const zeno_model_t* model, const float* x, const float* G, int64_t ldg, int32_t m,
                                const zeno_batch_t* batch, float gamma, float rho, const float* scores) {
@@ -1093,6 +1108,173 @@ zeno_status_t zeno_krum(const float* G, int64_t ldg, int32_t m, int64_t d, int32
     return ZENO_ERR_WORKSPACE;
   ProfScope ps(ZENO_KERNEL_KRUM, 0, 4.0 * (double)d * (m + 2), reinterpret_cast<hipStream_t>(stream));
   ZENO_TRY(launch_krum(G, ldg, m, d, b, out, chosen, krum_scores, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+// ---- models that answer with tokens
+
+size_t zeno_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
+  if (rows < 0 || vocab < 1 || vocab > ZENO_MAX_VOCAB || top < 0 || top > ZENO_MAX_TOP || top > vocab) return 0;
+  return logprobs_workspace_bytes(rows, vocab, top);
+}
+
+zeno_status_t zeno_logprobs(const void* logits, int64_t ldz, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* labels,
+                            float* logp, float* entropy, float* stats, int32_t top, int32_t* top_index, float* top_logp,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(logits, ldz, dtype, rows, vocab) || top < 0 || top > vocab) return ZENO_ERR_INVALID_ARG;
+  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB) return ZENO_ERR_UNSUPPORTED;
+  if (logp == nullptr && entropy == nullptr && stats == nullptr && top == 0) return ZENO_ERR_INVALID_ARG;
+  if ((logp != nullptr && labels == nullptr && rows > 0) || (top > 0 && rows > 0 && (top_index == nullptr || top_logp == nullptr)))
+    return ZENO_ERR_INVALID_ARG;
+  if (!aligned(labels, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4) || !aligned(top_index, 4) ||
+      !aligned(top_logp, 4))
+    return ZENO_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < logprobs_workspace_bytes(rows, vocab, top))
+    return ZENO_ERR_WORKSPACE;
+  if (rows == 0) return ZENO_OK;
+  const LogprobsArgs a = {logits, ldz, dtype, rows, vocab, labels, logp, entropy, stats, top, top_index, top_logp};
+  ProfScope ps(ZENO_KERNEL_LOGPROBS, 0, (double)rows * ((double)vocab * dtype_bytes(dtype) + 8.0 * top + 20.0),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_logprobs(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dtype, int32_t rows, int32_t vocab,
+                                     const float* stats, const int32_t* labels, const float* grad_logp, const float* entropy,
+                                     const float* grad_entropy, int32_t top, const int32_t* top_index, const float* grad_top,
+                                     void* dlogits, int64_t ldd, void* stream) {
+  if (!matrix_ok(logits, ldz, dtype, rows, vocab) || !matrix_ok(dlogits, ldd, dtype, rows, vocab)) return ZENO_ERR_INVALID_ARG;
+  if (top < 0 || top > vocab) return ZENO_ERR_INVALID_ARG;
+  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB) return ZENO_ERR_UNSUPPORTED;
+  if (rows == 0) return ZENO_OK;
+  if (grad_logp == nullptr && grad_entropy == nullptr && grad_top == nullptr) return ZENO_ERR_INVALID_ARG;
+  if (stats == nullptr || (grad_logp != nullptr && labels == nullptr) || (grad_entropy != nullptr && entropy == nullptr))
+    return ZENO_ERR_INVALID_ARG;
+  if ((grad_top != nullptr) != (top > 0) || (top > 0 && top_index == nullptr)) return ZENO_ERR_INVALID_ARG;
+  if (dlogits == logits && ldd != ldz && rows > 1) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(stats, 4) || !aligned(labels, 4) || !aligned(grad_logp, 4) || !aligned(entropy, 4) || !aligned(grad_entropy, 4) ||
+      !aligned(top_index, 4) || !aligned(grad_top, 4))
+    return ZENO_ERR_INVALID_ARG;
+  const LogprobsGradArgs a = {logits, dlogits, ldz,     ldd,          dtype, rows,      vocab,
+                              stats,  labels,  grad_logp, grad_entropy, entropy, top, top_index, grad_top};
+  ProfScope ps(ZENO_KERNEL_LOGPROBS_GRAD, 0, (double)rows * (2.0 * vocab * dtype_bytes(dtype) + 8.0 * top + 24.0),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_logprobs_backward(a, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, uint8_t* values,
+                              uint8_t* scales, void* stream) {
+  if (!matrix_ok(x, ldx, dtype, rows, width) || !checkpoint_ok(values, scales, rows)) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (rows == 0) return ZENO_OK;
+  ProfScope ps(ZENO_KERNEL_CHECKPOINT, 0, (double)rows * width * (dtype_bytes(dtype) + 33.0 / 32), reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_checkpoint(x, ldx, dtype, rows, width, values, scales, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+zeno_status_t zeno_checkpoint_values(const uint8_t* values, const uint8_t* scales, int32_t rows, int32_t width, int32_t dtype,
+                                     void* out, int64_t ldo, void* stream) {
+  if (!matrix_ok(out, ldo, dtype, rows, width) || !checkpoint_ok(values, scales, rows)) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (rows == 0) return ZENO_OK;
+  ProfScope ps(ZENO_KERNEL_CHECKPOINT, 0, (double)rows * width * (dtype_bytes(dtype) + 33.0 / 32), reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_checkpoint_values(values, scales, rows, width, dtype, out, ldo, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+zeno_status_t zeno_layer_norm(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, const float* weight,
+                              const float* bias, float eps, void* y, int64_t ldy, float* mean, float* rstd, uint8_t* values,
+                              uint8_t* scales, void* stream) {
+  if (!matrix_ok(x, ldx, dtype, rows, width) || !matrix_ok(y, ldy, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;
+  if (weight == nullptr || !std::isfinite(eps) || !(eps > 0.f)) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return ZENO_ERR_INVALID_ARG;
+  if ((values != nullptr) != (scales != nullptr) || !aligned(values, 16)) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (rows == 0) return ZENO_OK;
+  const NormArgs a = {x, y, ldx, ldy, dtype, rows, width, weight, bias, eps, mean, rstd, values, scales};
+  ProfScope ps(ZENO_KERNEL_LAYER_NORM, 0,
+               (double)rows * width * (2.0 * dtype_bytes(dtype) + (values != nullptr ? 33.0 / 32 : 0.0)) + 8.0 * rows + 8.0 * width,
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_layer_norm(a, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+size_t zeno_layer_norm_workspace_bytes(int32_t rows, int32_t width, int32_t m) {
+  if (rows < 0 || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
+  return layer_norm_workspace_bytes(rows, width, m);
+}
+
+zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t width, const void* x,
+                                       int64_t ldx, const uint8_t* values, const uint8_t* scales, const float* mean,
+                                       const float* rstd, const float* weight, int32_t m, const int32_t* offsets, void* dx,
+                                       int64_t lddx, float* dweight, int64_t ldw, float* dbias, int64_t ldb, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(dy, lddy, dtype, rows, width) || !groups_ok(m, offsets)) return ZENO_ERR_INVALID_ARG;
+  if (x != nullptr ? (!matrix_ok(x, ldx, dtype, rows, width) || values != nullptr || scales != nullptr)
+                   : !checkpoint_ok(values, scales, rows))
+    return ZENO_ERR_INVALID_ARG;
+  if (weight == nullptr || (rows > 0 && (mean == nullptr || rstd == nullptr))) return ZENO_ERR_INVALID_ARG;
+  if (dx != nullptr && !matrix_ok(dx, lddx, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;
+  if (dx != nullptr && dx == dy && lddx != lddy && rows > 1) return ZENO_ERR_INVALID_ARG;
+  if (dx == nullptr && dweight == nullptr && dbias == nullptr) return ZENO_ERR_INVALID_ARG;
+  if ((dweight != nullptr && ldw < width) || (dbias != nullptr && ldb < width)) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
+    return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layer_norm_workspace_bytes(rows, width, m))
+    return ZENO_ERR_WORKSPACE;
+  const NormGradArgs a = {dy,    x,    values, scales, dx, lddy,    ldx,     lddx,  dtype, rows, width,
+                          mean, rstd, weight, m,      offsets, dweight, dbias, ldw,   ldb};
+  ProfScope ps(ZENO_KERNEL_LAYER_NORM_GRAD, 0,
+               (double)rows * width * ((dx != nullptr ? 2.0 : 1.0) * dtype_bytes(dtype) + (x != nullptr ? dtype_bytes(dtype) : 33.0 / 32)) +
+                   8.0 * m * width,
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_layer_norm_backward(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+size_t zeno_weight_gradient_workspace_bytes(int32_t rows, int32_t out, int32_t width, int32_t m) {
+  if (rows < 0 || out < 1 || out > ZENO_MAX_WIDTH || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
+  return weight_gradient_workspace_bytes(rows, out, width, m);
+}
+
+zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t out, const uint8_t* values,
+                                   const uint8_t* scales, int32_t width, int32_t m, const int32_t* offsets, float* dweight,
+                                   int64_t ldw, float* dbias, int64_t ldb, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(dy, lddy, dtype, rows, out) || width < 1 || !checkpoint_ok(values, scales, rows) || !groups_ok(m, offsets))
+    return ZENO_ERR_INVALID_ARG;
+  if (dweight == nullptr || ldw < (int64_t)out * width || (dbias != nullptr && ldb < out)) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(dweight, 4) || !aligned(dbias, 4)) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH || out > ZENO_MAX_WIDTH || !weight_gradient_fits(out, width)) return ZENO_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < weight_gradient_workspace_bytes(rows, out, width, m))
+    return ZENO_ERR_WORKSPACE;
+  const WeightGradArgs a = {dy, lddy, dtype, rows, out, width, values, scales, m, offsets, dweight, dbias, ldw, ldb};
+  ProfScope ps(ZENO_KERNEL_WEIGHT_GRAD, 0,
+               (double)rows * (out * (double)dtype_bytes(dtype) + width * 33.0 / 32) + 4.0 * m * ((double)out * width + out),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_weight_gradient(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+size_t zeno_score_logprobs_workspace_bytes(int32_t m, int64_t d) {
+  if (m < 1 || m > ZENO_MAX_CANDIDATES || d < 1) return 0;
+  return score_logprobs_workspace_bytes(m, d);
+}
+
+zeno_status_t zeno_score_logprobs(const float* G, int64_t ldg, int32_t m, int64_t d, const float* logp_x, const float* logp,
+                                  int64_t ldp, int32_t n, const int32_t* labels, float rho, float* scores, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  if (G == nullptr || logp_x == nullptr || logp == nullptr || scores == nullptr) return ZENO_ERR_INVALID_ARG;
+  if (m < 1 || m > ZENO_MAX_CANDIDATES || d < 1 || ldg < d || n < 1 || ldp < n) return ZENO_ERR_INVALID_ARG;
+  if (!std::isfinite(rho) || rho < 0.f) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(G, 4) || !aligned(logp_x, 4) || !aligned(logp, 4) || !aligned(labels, 4) || !aligned(scores, 4))
+    return ZENO_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < score_logprobs_workspace_bytes(m, d))
+    return ZENO_ERR_WORKSPACE;
+  ProfScope ps(ZENO_KERNEL_SCORE_LOGPROBS, 0, 4.0 * (double)d * m + 4.0 * (m + 1.0) * n, reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_score_logprobs(G, ldg, m, d, logp_x, logp, ldp, n, labels, rho, scores, workspace,
+                                 reinterpret_cast<hipStream_t>(stream)));
   return ZENO_OK;
 }
 

@@ -1,0 +1,656 @@
+// Log probabilities of given tokens, entropy and top alternatives of rows of logits, and their gradient.
+//
+// With M = max z and s = sum exp(z - M):   log p_j = (z_j - M) - log s,   H = log s - (1/s) sum exp(z - M) (z - M).
+// One pass over a row: every thread keeps a reference c (in units of log2, within one of its running maximum) and the sums of
+// 2^(L z - c) and of 2^(L z - c) (L z - c), L = log2 e, so a value costs one FMA and one exponential.
+#include "zeno_tokens.h"
+
+#include <float.h>
+
+namespace zeno {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kThreads = 256;
+constexpr int kGroups = 16;        // maxima that a thread keeps of its share of a row, for the search of the top values
+constexpr int kCandidates = 512;   // top values are chosen from at most so many
+constexpr int kMaxParts = 64;      // workgroups that share a row
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float finite(float x) { return fminf(fmaxf(x, -FLT_MAX), FLT_MAX); }
+
+// What a row, or a part of it, comes to: s and t relative to the largest logit M.
+struct RowSums {
+  float M, s, t;   // max, sum 2^(L(z-M)), sum 2^(L(z-M)) L(z-M)
+};
+
+// The sums of two parts relative to M >= part.M.
+__device__ inline void move_to(RowSums& p, float M) {
+  if (p.s != 0.f && p.M < M) {
+    const float delta = fmaxf((p.M - M) * kLog2e, -1e4f), r = exp2_fast(delta);
+    p.t = r * fmaf(p.s, delta, p.t);
+    p.s *= r;
+  }
+  p.M = M;
+}
+
+// A row whose logits are all -inf has no distribution: nothing can be drawn from it.
+__device__ inline bool is_empty(float M, float s) { return M == -__builtin_inff() && s == 0.f; }
+
+__device__ inline float log_prob(float z, float M, float log_s, bool empty) {
+  return empty ? -__builtin_inff() : (z - M) - log_s;
+}
+
+__device__ inline float clean(float z) { return z != z ? -__builtin_inff() : z; }   // a NaN ranks as -inf
+
+// Writes what a row gives, except its alternatives.  One thread.
+template <typename T>
+__device__ inline void finish_row(const LogprobsArgs& a, int row, RowSums r, float* log_s_out) {
+  if (r.M == __builtin_inff()) r.s = __builtin_nanf("");   // inf - inf
+  const bool empty = is_empty(r.M, r.s);
+  const float log_s = empty ? 0.f : logf(r.s);
+  if (a.stats) {
+    a.stats[2LL * row] = r.M;
+    a.stats[2LL * row + 1] = log_s;
+  }
+  if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - kLn2 * (r.t / r.s);
+  if (a.logp) {
+    const int y = a.labels[row];
+    float lp = 0.f;   // label -1: the token does not count
+    if (y != -1)
+      lp = y >= 0 && y < a.vocab
+               ? log_prob((float)reinterpret_cast<const T*>(a.logits)[(long long)row * a.ldz + y], r.M, log_s, empty)
+               : __builtin_nanf("");
+    a.logp[row] = lp;
+  }
+  *log_s_out = log_s;
+}
+
+// NW waves for a row (or a part of it); 4 / NW rows a workgroup.
+template <typename T, int NW, bool TOP>
+struct Shared {
+  static constexpr int TPR = 64 * NW;
+  float wave_max[4], wave_s[4], wave_t[4];
+  float log_s[4 / NW], M[4 / NW];
+  int empty[4 / NW];
+  float group_max[TOP ? 4 / NW : 1][TOP ? kGroups : 1][TOP ? TPR : 1];
+  float thread_max[TOP ? 4 / NW : 1][TOP ? TPR : 1];
+  float tau[4 / NW];
+  int count[4 / NW], more[4 / NW], ties[4];
+  float cand_val[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
+  int cand_idx[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
+  float best_val[4];
+  int best_idx[4];
+};
+
+template <typename T>
+__device__ inline void load_at(const T* row, int n, int i, float (&v)[Wide<T>::N]) {
+  if (i + Wide<T>::N <= n)
+    load_wide(row + i, v);
+  else
+    load_part(row + i, n - i, -__builtin_inff(), v);
+}
+
+// The k largest of row[0..n), ties to the lower index, in order, handed to put(rank, value, index).  k <= n, k <= TPR.
+// Every thread kept the maxima of kGroups groups of its values while it read the row.  The k-th largest of the threads' maxima
+// is no larger than the k-th largest value, so only groups that reach it are read again: about k of them.
+template <typename T, int NW, typename Put>
+__device__ inline void top_values(Shared<T, NW, true>& sh, int slot, const T* row, int n, int iters, int per_group, int k, int tid,
+                                  Put put) {
+  constexpr int N = Wide<T>::N, TPR = 64 * NW;
+  const int lane = tid & 63, wave = slot * NW + tid / 64;   // (tid counts from the row's first thread)
+  float mine = sh.thread_max[slot][tid];
+  int rank = 0;
+  for (int i = 0; i < TPR; ++i) {
+    const float o = sh.thread_max[slot][i];
+    rank += (o > mine || (o == mine && i < tid)) ? 1 : 0;
+  }
+  if (rank == k - 1) sh.tau[slot] = mine;
+  if (tid == 0) sh.count[slot] = 0;
+  row_sync<NW>();
+  const float tau = sh.tau[slot];
+  float v[N];
+  auto collect = [&](bool ties) {
+    for (int g = 0; g * per_group < iters; ++g) {
+      if (sh.group_max[slot][g][tid] < tau) continue;
+      for (int it = g * per_group; it < iters && it < (g + 1) * per_group; ++it) {
+        const int at = (it * TPR + tid) * N;
+        if (at >= n) break;
+        load_at(row, n, at, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float c = clean(v[j]);
+          if (at + j < n && (ties ? c >= tau : c > tau)) {
+            const int pos = atomicAdd(&sh.count[slot], 1);
+            if (pos < kCandidates) {
+              sh.cand_val[slot][pos] = c;
+              sh.cand_idx[slot][pos] = at + j;
+            }
+          }
+        }
+      }
+    }
+  };
+  collect(true);
+  row_sync<NW>();
+  int found = sh.count[slot];
+  if (found > kCandidates) {
+    // Many values equal to tau (masked rows, rows of few values): only the larger ones, then the first of the equal ones.
+    row_sync<NW>();
+    if (tid == 0) sh.count[slot] = 0;
+    row_sync<NW>();
+    collect(false);
+    row_sync<NW>();
+    found = sh.count[slot];
+    if (found > kCandidates) {
+      // The largest values crowd in the shares of few threads: one pass over the row for each of the k.
+      float last = __builtin_inff();
+      int last_idx = -1;
+      for (int r = 0; r < k; ++r) {
+        float bv = 0.f;
+        int bi = -1;
+        for (int it = 0; it < iters; ++it) {
+          const int at = (it * TPR + tid) * N;
+          if (at >= n) break;
+          load_at(row, n, at, v);
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const float c = clean(v[j]);
+            const bool after = c < last || (c == last && at + j > last_idx);
+            if (at + j < n && after && (bi < 0 || c > bv)) {
+              bv = c;
+              bi = at + j;
+            }
+          }
+        }
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+          const float ov = __shfl_xor(bv, off, 64);
+          const int oi = __shfl_xor(bi, off, 64);
+          if (oi >= 0 && (bi < 0 || ov > bv || (ov == bv && oi < bi))) {
+            bv = ov;
+            bi = oi;
+          }
+        }
+        if (NW > 1) {
+          if (lane == 0) {
+            sh.best_val[wave] = bv;
+            sh.best_idx[wave] = bi;
+          }
+          __syncthreads();
+          for (int w = 0; w < NW; ++w) {
+            const float ov = sh.best_val[w];
+            const int oi = sh.best_idx[w];
+            if (oi >= 0 && (bi < 0 || ov > bv || (ov == bv && oi < bi))) {
+              bv = ov;
+              bi = oi;
+            }
+          }
+          __syncthreads();
+        }
+        if (tid == 0) put(r, bv, bi);
+        last = bv;
+        last_idx = bi;
+      }
+      return;
+    }
+    if (found < k) {
+      // the first (k - found) values equal to tau, in order of their index
+      int have = found;
+      for (int it = 0; it < iters && have < k; ++it) {
+        const int at = (it * TPR + tid) * N;
+        int eq = 0;
+        if (at < n) {
+          load_at(row, n, at, v);
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (at + j < n && clean(v[j]) == tau) eq |= 1 << j;
+        }
+        const int cnt = __popc(eq);
+        int before = cnt;   // inclusive prefix over the lanes
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const int o = __shfl_up(before, off, 64);
+          if (lane >= off) before += o;
+        }
+        int total = __shfl(before, 63, 64);
+        before -= cnt;
+        if (NW > 1) {
+          if (lane == 0) sh.ties[wave] = total;
+          __syncthreads();
+          total = 0;
+          for (int w = 0; w < NW; ++w) {
+            if (w < wave) before += sh.ties[w];
+            total += sh.ties[w];
+          }
+          __syncthreads();
+        }
+        int pos = have + before;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (eq >> j & 1) {
+            if (pos < k) {
+              sh.cand_val[slot][pos] = tau;
+              sh.cand_idx[slot][pos] = at + j;
+            }
+            ++pos;
+          }
+        have += total;
+      }
+      found = have < k ? have : k;
+      row_sync<NW>();
+    }
+  }
+  for (int i = tid; i < found; i += TPR) {
+    const float c = sh.cand_val[slot][i];
+    const int ci = sh.cand_idx[slot][i];
+    int better = 0;
+    for (int j = 0; j < found; ++j) {
+      const float o = sh.cand_val[slot][j];
+      better += (o > c || (o == c && sh.cand_idx[slot][j] < ci)) ? 1 : 0;
+    }
+    if (better < k) put(better, c, ci);
+  }
+}
+
+// Partial results of a row that several workgroups share.
+struct Parts {
+  float* sums;   // [rows][parts][3]
+  float* val;    // [rows][parts][top]
+  int* idx;      // (-1: the part has fewer values)
+  int parts;     // 1: the kernel writes the results itself
+  int len;       // values of a part
+};
+
+template <typename T, int NW, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Parts w) {
+  constexpr int N = Wide<T>::N, TPR = 64 * NW, RPB = 4 / NW;
+  __shared__ Shared<T, NW, TOP> sh;
+  const int slot = threadIdx.x / TPR, tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const int part = blockIdx.y;
+  const int begin = part * w.len;
+  const int n = a.vocab - begin < w.len ? a.vocab - begin : w.len;
+  const int iters = (n + TPR * N - 1) / (TPR * N);
+  const int per_group = (iters + kGroups - 1) / kGroups;
+  const long long blocks = ((long long)a.rows + RPB - 1) / RPB;
+  for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const long long r64 = b * RPB + slot;
+    const bool live = r64 < a.rows;
+    const int rowi = live ? (int)r64 : a.rows - 1;   // (a wave behind the last row repeats it and writes nothing)
+    const T* row = reinterpret_cast<const T*>(a.logits) + (long long)rowi * a.ldz + begin;
+    const float inf = __builtin_inff();
+    float M = -inf, lim = -inf, c = 0.f, s = 0.f, t = 0.f, gm = -inf;
+    int in_group = 0, g = 0;
+    float v[N];
+    auto take = [&]() {
+      float cm = v[0];
+#pragma unroll
+      for (int j = 1; j < N; ++j) cm = fmaxf(cm, v[j]);
+      if (cm > lim) {
+        const float cn = finite(cm * kLog2e);
+        if (s != 0.f) {
+          const float delta = fmaxf(c - cn, -1e4f), r = exp2_fast(delta);
+          t = r * fmaf(s, delta, t);
+          s *= r;
+        }
+        c = cn;
+        lim = cm + 0.6875f;   // the reference follows when it is a factor of two behind
+      }
+      M = fmaxf(M, cm);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = fmaf(v[j], kLog2e, -c), e = exp2_fast(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, -1e30f), t);   // (0 * -inf would be NaN)
+      }
+      if (TOP) {
+        gm = fmaxf(gm, cm);
+        if (++in_group == per_group) {
+          sh.group_max[slot][g++][tid] = gm;
+          gm = -inf;
+          in_group = 0;
+        }
+      }
+    };
+    for (int it = 0; it < iters; ++it) {
+      const int at = (it * TPR + tid) * N;
+      if (at + N <= n)
+        load_wide(row + at, v);
+      else
+        load_part(row + at, n - at, -inf, v);
+      take();
+    }
+    if (TOP && in_group > 0) sh.group_max[slot][g][tid] = gm;
+    if (TOP) sh.thread_max[slot][tid] = M;
+    // the row's maximum, and every thread's sums relative to it
+    const float own_max = M;
+    M = wave_max_f(M);
+    if (NW > 1) {
+      if (lane == 0) sh.wave_max[wave] = M;
+      __syncthreads();
+      for (int i = 0; i < NW; ++i) M = fmaxf(M, sh.wave_max[i]);
+    }
+    if (fabsf(M) > 0x1p126f && fabsf(M) < inf) {
+      // L M is out of range (a row masked with the type's lowest value): once more with z - M first
+      s = t = 0.f;
+      for (int it = 0; it < iters; ++it) {
+        const int at = (it * TPR + tid) * N;
+        if (at + N <= n)
+          load_wide(row + at, v);
+        else
+          load_part(row + at, n - at, -inf, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float d = (v[j] - M) * kLog2e, e = exp2_fast(d);
+          s += e;
+          t = fmaf(e, fmaxf(d, -1e30f), t);
+        }
+      }
+    } else if (s != 0.f) {
+      // c is L times some logit, rounded: the exact product with M's is what the sums refer to from here on
+      const float delta = own_max == -inf ? 0.f : fmaxf(fmaf(-M, kLog2e, c), -1e4f), r = exp2_fast(delta);
+      t = r * fmaf(s, delta, t);
+      s *= r;
+    }
+    s = wave_sum_f(s);
+    t = wave_sum_f(t);
+    if (NW > 1) {
+      if (lane == 0) {
+        sh.wave_s[wave] = s;
+        sh.wave_t[wave] = t;
+      }
+      __syncthreads();
+      s = sh.wave_s[0];
+      t = sh.wave_t[0];
+      for (int i = 1; i < NW; ++i) {
+        s += sh.wave_s[i];
+        t += sh.wave_t[i];
+      }
+    }
+    if (w.parts > 1) {
+      const long long p = (long long)rowi * w.parts + part;
+      if (tid == 0 && live) {
+        w.sums[3 * p] = M;
+        w.sums[3 * p + 1] = s;
+        w.sums[3 * p + 2] = t;
+      }
+      if constexpr (TOP) {
+        const int k = a.top < n ? a.top : n;
+        if (tid >= k && tid < a.top && live) w.idx[p * a.top + tid] = -1;
+        row_sync<NW>();
+        top_values<T, NW>(sh, slot, row, n, iters, per_group, k, tid, [&](int rank, float val, int idx) {
+          if (!live) return;
+          w.val[p * a.top + rank] = val;
+          w.idx[p * a.top + rank] = begin + idx;
+        });
+      }
+    } else {
+      if (tid == 0) {
+        float log_s = 0.f;
+        const RowSums r = {M, s, t};
+        if (live) finish_row<T>(a, rowi, r, &log_s);
+        sh.log_s[slot] = log_s;
+      }
+      if constexpr (TOP) {
+        row_sync<NW>();
+        const float log_s = sh.log_s[slot];
+        const bool empty = is_empty(M, s);
+        top_values<T, NW>(sh, slot, row, n, iters, per_group, a.top, tid, [&](int rank, float val, int idx) {
+          if (!live) return;
+          a.top_index[(long long)rowi * a.top + rank] = idx;
+          const float z = (float)row[idx];   // (a NaN stays one)
+          a.top_logp[(long long)rowi * a.top + rank] = log_prob(z, M, log_s, empty);
+        });
+      }
+    }
+    row_sync<NW>();   // the next row uses the same shared memory
+  }
+}
+
+// Joins the parts of a row: one workgroup of one wave a row.
+template <typename T>
+__global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts w) {
+  __shared__ float cand_val[kMaxParts * 32];
+  __shared__ int cand_idx[kMaxParts * 32];
+  __shared__ int count;
+  __shared__ float tau_sh;
+  const int lane = threadIdx.x;
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    RowSums r = {-__builtin_inff(), 0.f, 0.f};
+    const long long p = row * w.parts + lane;
+    if (lane < w.parts) r = {w.sums[3 * p], w.sums[3 * p + 1], w.sums[3 * p + 2]};
+    move_to(r, wave_max_f(r.M));
+    r.s = wave_sum_f(r.s);
+    r.t = wave_sum_f(r.t);
+    float log_s = 0.f;
+    if (lane == 0) finish_row<T>(a, (int)row, r, &log_s);
+    log_s = __shfl(log_s, 0, 64);
+    if (r.M == __builtin_inff()) r.s = __builtin_nanf("");
+    const int k = a.top;
+    if (k > 0) {
+      const bool empty = is_empty(r.M, r.s);
+      // the k-th largest of the parts' largest values bounds the k-th largest from below
+      float head = lane < w.parts ? w.val[p * k] : -__builtin_inff();   // (every part has a first value)
+      if (lane == 0) {
+        count = 0;
+        tau_sh = -__builtin_inff();
+      }
+      row_sync<1>();
+      int rank = 0;
+      for (int i = 0; i < w.parts; ++i) {
+        const float o = __shfl(head, i, 64);
+        rank += (o > head || (o == head && i < lane)) ? 1 : 0;
+      }
+      if (lane < w.parts && rank == k - 1) tau_sh = head;
+      row_sync<1>();
+      const float tau = tau_sh;
+      for (int i = lane; i < w.parts * k; i += 64) {
+        const int idx = w.idx[row * w.parts * k + i];
+        if (idx < 0) continue;
+        const float val = w.val[row * w.parts * k + i];
+        if (val >= tau) {
+          const int pos = atomicAdd(&count, 1);
+          cand_val[pos] = val;
+          cand_idx[pos] = idx;
+        }
+      }
+      row_sync<1>();
+      const int found = count;
+      for (int i = lane; i < found; i += 64) {
+        const float c = cand_val[i];
+        const int ci = cand_idx[i];
+        int better = 0;
+        for (int j = 0; j < found; ++j) {
+          const float o = cand_val[j];
+          better += (o > c || (o == c && cand_idx[j] < ci)) ? 1 : 0;
+        }
+        if (better < k) {
+          a.top_index[row * k + better] = ci;
+          const float z = (float)reinterpret_cast<const T*>(a.logits)[row * a.ldz + ci];
+          a.top_logp[row * k + better] = log_prob(z, r.M, log_s, empty);
+        }
+      }
+      row_sync<1>();
+    }
+  }
+}
+
+// ---- gradient:  dz_j = g [j = y] + sum_k q_k [j = i_k] - p_j (g + sum_k q_k + h (log p_j + H))
+// with g, h, q the gradients of logp, H and the alternatives' log probabilities.
+template <typename T, bool ENT, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArgs a, int segs, int seg_len) {
+  constexpr int N = Wide<T>::N;
+  __shared__ int special_idx[33];
+  __shared__ float special_g[33];
+  const long long tiles = (long long)a.rows * segs;
+  const float inf = __builtin_inff();
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const long long row = tile / segs;
+    const int lo = (int)(tile % segs) * seg_len;
+    const int n = a.vocab - lo < seg_len ? a.vocab - lo : seg_len;
+    const T* z = reinterpret_cast<const T*>(a.logits) + row * a.ldz + lo;
+    T* out = reinterpret_cast<T*>(a.dlogits) + row * a.ldd + lo;
+    float M = a.stats[2 * row], log_s = a.stats[2 * row + 1];
+    const bool empty = M == -inf && log_s == 0.f;
+    int y = -1;
+    float g = 0.f;
+    if (a.grad_logp) {
+      y = a.labels[row];
+      if (y != -1) g = y >= 0 && y < a.vocab ? a.grad_logp[row] : __builtin_nanf("");
+      if (y < 0 || y >= a.vocab) y = -1;
+    }
+    float sum = g;
+    if (TOP) {
+      if (threadIdx.x < a.top) {
+        const int idx = a.top_index[row * a.top + threadIdx.x];
+        const bool valid = idx >= 0 && idx < a.vocab;
+        special_idx[threadIdx.x] = valid ? idx : -1;
+        special_g[threadIdx.x] = valid ? a.grad_top[row * a.top + threadIdx.x] : __builtin_nanf("");
+      }
+      __syncthreads();
+      for (int i = 0; i < a.top; ++i) sum += special_g[i];
+    }
+    const float h = ENT ? a.grad_entropy[row] : 0.f;
+    const float base = ENT ? fmaf(h, a.entropy[row], sum) : sum;
+    if (empty) {
+      M = 0.f;
+      log_s = inf;   // every probability is 0
+    }
+    // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
+    auto grad = [&](float v) {
+      const float lp = (v - M) - log_s, p = exp2_fast(lp * kLog2e);
+      return -p * (ENT ? fmaf(h, fmaxf(lp, -256.f), base) : base);
+    };
+    // the alternatives' columns of this segment, before anything is overwritten (dlogits may be the logits)
+    float kept = 0.f;
+    int mine = -1;
+    if (TOP && threadIdx.x < a.top) {
+      const int idx = special_idx[threadIdx.x] - lo;
+      if (idx >= 0 && idx < n) {
+        mine = idx;
+        kept = (float)z[idx];
+      }
+    }
+    if (TOP) __syncthreads();
+    for (int at = threadIdx.x * N; at < n; at += kThreads * N) {
+      float v[N];
+      if (at + N <= n)
+        load_wide(z + at, v);
+      else
+        load_part(z + at, n - at, -inf, v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = grad(v[j]);
+      const int hit = y - lo - at;
+      if (hit >= 0 && hit < N && !empty) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j == hit) v[j] += g;
+      }
+      if (at + N <= n)
+        store_wide(out + at, v);
+      else
+        store_part(out + at, n - at, v);
+    }
+    if (TOP) {
+      __syncthreads();   // the segment is written: its special columns once more, with all that falls on them
+      if (mine >= 0 && !empty) {
+        float d = grad(kept);
+        if (mine == y - lo) d += g;
+        for (int i = 0; i < a.top; ++i)
+          if (special_idx[i] - lo == mine) d += special_g[i];
+        out[mine] = (T)d;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// Rows of up to 2048 values take one wave, longer ones a workgroup of four.
+bool wave_rows(int vocab) { return vocab <= 2048; }
+
+// Workgroups that share a row: where the rows alone do not fill the chip.
+int row_parts(int rows, int vocab) {
+  if (wave_rows(vocab) || rows >= 512) return 1;
+  long long parts = (1024 + rows - 1) / rows;
+  const long long most = (vocab + 4095) / 4096;
+  if (parts > most) parts = most;
+  return (int)(parts < kMaxParts ? parts : kMaxParts);
+}
+
+Parts parts_for(int rows, int vocab, int top, void* workspace) {
+  Parts w;
+  w.parts = row_parts(rows, vocab);
+  const long long unit = kThreads * 8;   // whole 16-byte loads in every part, whatever the type
+  w.len = (int)(((vocab + w.parts - 1LL) / w.parts + unit - 1) / unit * unit);
+  if (w.parts == 1) w.len = vocab;
+  w.parts = w.parts == 1 ? 1 : (int)((vocab + (long long)w.len - 1) / w.len);   // (none of them empty)
+  const size_t n = (size_t)rows * w.parts;
+  unsigned char* base = reinterpret_cast<unsigned char*>(workspace);
+  w.sums = reinterpret_cast<float*>(base);
+  base += align_up(n * 3 * sizeof(float), 256);
+  w.val = reinterpret_cast<float*>(base);
+  base += align_up(n * top * sizeof(float), 256);
+  w.idx = reinterpret_cast<int*>(base);
+  return w;
+}
+
+template <typename T>
+hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream) {
+  const int rpb = wave_rows(a.vocab) ? 4 : 1;
+  const long long blocks = ((long long)a.rows + rpb - 1) / rpb;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), w.parts), block(kThreads);
+  if (wave_rows(a.vocab)) {
+    if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 1, true>), grid, block, 0, stream, a, w);
+    else hipLaunchKernelGGL((logprobs_kernel<T, 1, false>), grid, block, 0, stream, a, w);
+  } else {
+    if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 4, true>), grid, block, 0, stream, a, w);
+    else hipLaunchKernelGGL((logprobs_kernel<T, 4, false>), grid, block, 0, stream, a, w);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || w.parts == 1) return e;
+  hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.rows), dim3(64), 0, stream, a, w);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad_type(const LogprobsGradArgs& a, hipStream_t stream) {
+  const int seg_len = kThreads * Wide<T>::N * 4;
+  const int segs = ceil_div(a.vocab, seg_len);
+  const long long tiles = (long long)a.rows * segs;
+  const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : (1 << 20))), block(kThreads);
+  const bool ent = a.grad_entropy != nullptr, top = a.grad_top != nullptr && a.top > 0;
+  if (ent && top) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, true>), grid, block, 0, stream, a, segs, seg_len);
+  else if (ent) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, false>), grid, block, 0, stream, a, segs, seg_len);
+  else if (top) hipLaunchKernelGGL((logprobs_grad_kernel<T, false, true>), grid, block, 0, stream, a, segs, seg_len);
+  else hipLaunchKernelGGL((logprobs_grad_kernel<T, false, false>), grid, block, 0, stream, a, segs, seg_len);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprobs_workspace_bytes(int rows, int vocab, int top) {
+  const Parts w = parts_for(rows, vocab, top, nullptr);
+  if (w.parts == 1) return 256;
+  const size_t n = (size_t)rows * w.parts;
+  return align_up(n * 3 * sizeof(float), 256) + 2 * align_up(n * top * sizeof(float), 256);
+}
+
+hipError_t launch_logprobs(const LogprobsArgs& a, void* workspace, hipStream_t stream) {
+  const Parts w = parts_for(a.rows, a.vocab, a.top, workspace);
+  switch (a.dtype) {
+    case ZENO_F32: return launch_type<float>(a, w, stream);
+    case ZENO_BF16: return launch_type<__bf16>(a, w, stream);
+    default: return launch_type<_Float16>(a, w, stream);
+  }
+}
+
+hipError_t launch_logprobs_backward(const LogprobsGradArgs& a, hipStream_t stream) {
+  switch (a.dtype) {
+    case ZENO_F32: return launch_grad_type<float>(a, stream);
+    case ZENO_BF16: return launch_grad_type<__bf16>(a, stream);
+    default: return launch_grad_type<_Float16>(a, stream);
+  }
+}
+
+}  // namespace zeno

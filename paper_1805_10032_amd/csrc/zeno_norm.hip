@@ -1,0 +1,544 @@
+// Layer norm and its backward pass; the weights' gradients are summed per group of rows (a worker's tokens).
+//
+//   xh = (x - mean) rstd,  y = weight xh + bias,  rstd = 1 / sqrt(var + eps)
+//   a = weight dy,  dx = rstd (a - mean(a) - xh mean(a xh)),  dweight_g = sum_{rows of g} dy xh,  dbias_g = sum dy
+//
+// A row stays in registers between its statistics and its result: x is read once.  Threads own columns, so the weights stay in
+// registers from row to row, and so do the sums of their gradients.
+#include "zeno_tokens.h"
+
+namespace zeno {
+namespace {
+
+constexpr int kMaxGrid = 1 << 20;
+
+// NW waves for a row; a workgroup has four waves at least, of which one-wave rows use one each.
+template <int NW>
+struct Shape {
+  static constexpr int TPR = 64 * NW, THREADS = NW < 4 ? 256 : TPR, RPB = THREADS / TPR;
+};
+
+// Sums over the threads of a row.  The buffers alternate from row to row, so one barrier is enough: a buffer is written again
+// behind the barrier of the row between, which every wave reaches after it has read it.
+template <int NW>
+__device__ inline void row_sums2(float& a, float& b, float (*buf)[2], int wave) {
+  a = wave_sum_f(a);
+  b = wave_sum_f(b);
+  if (NW > 1) {
+    if ((threadIdx.x & 63) == 0) {
+      buf[wave][0] = a;
+      buf[wave][1] = b;
+    }
+    __syncthreads();
+    a = buf[0][0];
+    b = buf[0][1];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) {
+      a += buf[i][0];
+      b += buf[i][1];
+    }
+  }
+}
+template <int NW>
+__device__ inline float row_sum1(float a, float (*buf)[2], int wave) {
+  a = wave_sum_f(a);
+  if (NW > 1) {
+    if ((threadIdx.x & 63) == 0) buf[wave][0] = a;
+    __syncthreads();
+    a = buf[0][0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) a += buf[i][0];
+  }
+  return a;
+}
+
+template <typename T>
+__device__ inline void load_cols(const T* row, int col, int width, float (&v)[Wide<T>::N]) {
+  if (col + Wide<T>::N <= width)
+    load_wide(row + col, v);
+  else
+    load_part(row + col, width - col, 0.f, v);
+}
+template <typename T>
+__device__ inline void store_cols(T* row, int col, int width, const float (&v)[Wide<T>::N]) {
+  if (col + Wide<T>::N <= width)
+    store_wide(row + col, v);
+  else
+    store_part(row + col, width - col, v);
+}
+template <int N>
+__device__ inline void load_params(const float* p, int col, int width, float (&v)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = p != nullptr && col + j < width ? p[col + j] : 0.f;
+}
+
+// The 8-bit copy of N columns of a row (a block's columns lie in neighbouring lanes).  Every lane of the wave takes part.
+template <int N>
+__device__ inline void keep_cols(const float (&v)[N], int col, int width, int blocks, uint8_t* values, uint8_t* scales, long long row) {
+  float largest = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) largest = ckpt_larger(largest, v[j]);
+#pragma unroll
+  for (int off = 1; off < kCkptBlock / N; off <<= 1) largest = fmaxf(largest, __shfl_xor(largest, off, 64));
+  const int k = ckpt_exponent(largest);
+  float q[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) q[j] = ckpt_quotient(v[j], k);
+  if (col < blocks * kCkptBlock) {
+    uint8_t* p = values + row * ((long long)blocks * kCkptBlock) + col;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) *reinterpret_cast<unsigned*>(p + j) = ckpt_pack4(q[j], q[j + 1], q[j + 2], q[j + 3]);
+    if (col % kCkptBlock == 0) scales[row * blocks + col / kCkptBlock] = (uint8_t)(k + 127);
+  }
+}
+
+// CH 16-byte pieces of a row a thread.
+template <typename T, int NW, int CH>
+__global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
+  constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
+  __shared__ float buf[2][NW][2];
+  const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
+  const int blocks = ckpt_blocks(a.width);
+  const float inv = 1.f / (float)a.width;
+  float w[CH][N], b[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    load_params(a.weight, (c * TPR + tid) * N, a.width, w[c]);
+    load_params(a.bias, (c * TPR + tid) * N, a.width, b[c]);
+  }
+  for (long long row = (long long)blockIdx.x * RPB + slot; row < a.rows; row += (long long)gridDim.x * RPB) {
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
+    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy;
+    float v[CH][N], sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_cols(x, (c * TPR + tid) * N, a.width, v[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum += v[c][j];
+    const float mean = row_sum1<NW>(sum, buf[0], wave) * inv;
+    float sq = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = v[c][j] - mean;
+        if ((c * TPR + tid) * N + j < a.width) sq = fmaf(d, d, sq);
+      }
+    const float var = row_sum1<NW>(sq, buf[1], wave) * inv;
+    const float rstd = 1.f / sqrtf(var + a.eps);
+    if (a.values != nullptr) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) keep_cols<N>(v[c], (c * TPR + tid) * N, a.width, blocks, a.values, a.scales, row);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[c][j] = fmaf((v[c][j] - mean) * rstd, w[c][j], b[c][j]);
+      store_cols(y, (c * TPR + tid) * N, a.width, v[c]);
+    }
+    if (tid == 0) {
+      if (a.mean != nullptr) a.mean[row] = mean;
+      if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// Rows too wide for the registers: read once for the mean, once for the variance and once for the result, from the caches
+// where they hold the row.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+  constexpr int N = Wide<T>::N, TPR = 1024;
+  __shared__ float buf[2][16][2];
+  const int tid = threadIdx.x, wave = tid / 64;
+  const int blocks = ckpt_blocks(a.width), iters = (a.width + TPR * N - 1) / (TPR * N);
+  const float inv = 1.f / (float)a.width;
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
+    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy;
+    float v[N], w[N], b[N], sum = 0.f, sq = 0.f;
+    for (int c = 0; c < iters; ++c) {
+      load_cols(x, (c * TPR + tid) * N, a.width, v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum += v[j];
+    }
+    const float mean = row_sum1<16>(sum, buf[0], wave) * inv;
+    for (int c = 0; c < iters; ++c) {
+      load_cols(x, (c * TPR + tid) * N, a.width, v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = v[j] - mean;
+        if ((c * TPR + tid) * N + j < a.width) sq = fmaf(d, d, sq);
+      }
+    }
+    const float rstd = 1.f / sqrtf(row_sum1<16>(sq, buf[1], wave) * inv + a.eps);
+    for (int c = 0; c < iters; ++c) {
+      const int col = (c * TPR + tid) * N;
+      load_cols(x, col, a.width, v);
+      if (a.values != nullptr) keep_cols<N>(v, col, a.width, blocks, a.values, a.scales, row);
+      load_params(a.weight, col, a.width, w);
+      load_params(a.bias, col, a.width, b);
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = fmaf((v[j] - mean) * rstd, w[j], b[j]);
+      store_cols(y, col, a.width, v);
+    }
+    if (tid == 0) {
+      if (a.mean != nullptr) a.mean[row] = mean;
+      if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// ---- backward.  Workgroup c takes rows [c * chunk, (c + 1) * chunk), whatever groups they belong to: the work is even however ragged
+// the groups are.  Its sums for group g go to slot c + g: walking down the rows, every new piece raises c or g, so no two pieces share
+// a slot, and a group's slots are its chunks' numbers plus g.  Sums are added in that order: the same bits every time.
+struct Pieces {
+  float* partial;   // [chunks + m][2][width]
+  int chunk, chunks;
+};
+
+__device__ inline int first_group(const int32_t* offsets, int m, int row, int rows) {
+  int g = 0;
+  if (offsets == nullptr) return 0;
+  for (int i = 0; i < m; i += blockDim.x) {
+    const int at = i + (int)threadIdx.x;
+    g += __syncthreads_count(at < m && group_offset(offsets, at + 1, rows) <= row);
+  }
+  return g;
+}
+
+// xh of N columns, from the row itself or from its checkpoint
+template <typename T, bool KEPT>
+__device__ inline void load_xh(const NormGradArgs& a, long long row, int col, int blocks, float mean, float rstd, float (&v)[Wide<T>::N]) {
+  constexpr int N = Wide<T>::N;
+  if (KEPT) {
+    if (col < blocks * kCkptBlock) {
+      unsigned words[N / 4];
+      const uint8_t* p = a.values + row * ((long long)blocks * kCkptBlock) + col;
+#pragma unroll
+      for (int j = 0; j < N / 4; ++j) words[j] = reinterpret_cast<const unsigned*>(p)[j];
+      ckpt_unpack(words, ckpt_scale((int)a.scales[row * blocks + col / kCkptBlock] - 127), v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = 0.f;
+    }
+  } else {
+    load_cols(reinterpret_cast<const T*>(a.x) + row * a.ldx, col, a.width, v);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = (v[j] - mean) * rstd;
+}
+
+template <typename T, int NW, int CH, bool KEPT>
+__global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradArgs a, Pieces p) {
+  constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
+  __shared__ float buf[2][NW][2];
+  __shared__ float joined[RPB > 1 ? 2 * CH * N * 64 : 1];
+  const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
+  const int blocks = ckpt_blocks(a.width);
+  const float inv = 1.f / (float)a.width;
+  const int r0 = blockIdx.x * p.chunk, r1 = a.rows - r0 < p.chunk ? a.rows : r0 + p.chunk;
+  float w[CH][N];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) load_params(a.weight, (c * TPR + tid) * N, a.width, w[c]);
+  int parity = 0;
+  for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
+    const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
+    if (begin >= r1) break;
+    const int lo = begin > r0 ? begin : r0, hi = end < r1 ? end : r1;
+    if (lo >= hi) continue;
+    float dw[CH][N], db[CH][N];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < N; ++j) dw[c][j] = db[c][j] = 0.f;
+    for (long long row = lo + slot; row < hi; row += RPB) {
+      const float mean = a.mean[row], rstd = a.rstd[row];
+      const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.lddy;
+      float xh[CH][N], d[CH][N], c1 = 0.f, c2 = 0.f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        load_cols(dy, (c * TPR + tid) * N, a.width, d[c]);
+        load_xh<T, KEPT>(a, row, (c * TPR + tid) * N, blocks, mean, rstd, xh[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          db[c][j] += d[c][j];
+          dw[c][j] = fmaf(d[c][j], xh[c][j], dw[c][j]);
+          d[c][j] *= w[c][j];
+          c1 += d[c][j];
+          c2 = fmaf(d[c][j], xh[c][j], c2);
+        }
+      if (a.dx != nullptr) {
+        row_sums2<NW>(c1, c2, buf[parity], wave);
+        parity ^= 1;
+        c1 *= inv;
+        c2 *= inv;
+        T* dx = reinterpret_cast<T*>(a.dx) + row * a.lddx;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) d[c][j] = rstd * (d[c][j] - fmaf(xh[c][j], c2, c1));
+          store_cols(dx, (c * TPR + tid) * N, a.width, d[c]);
+        }
+      }
+    }
+    float* out = p.partial + (long long)(blockIdx.x + g) * 2 * a.width;
+    if (RPB > 1) {
+      // the waves' sums, one wave after the other
+      for (int s = 0; s < RPB; ++s) {
+        if (slot == s) {
+#pragma unroll
+          for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+              const int at = (c * N + j) * 64 + tid;
+              joined[at] = s == 0 ? dw[c][j] : joined[at] + dw[c][j];
+              joined[CH * N * 64 + at] = s == 0 ? db[c][j] : joined[CH * N * 64 + at] + db[c][j];
+            }
+        }
+        __syncthreads();
+      }
+      if (slot == 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            dw[c][j] = joined[(c * N + j) * 64 + tid];
+            db[c][j] = joined[CH * N * 64 + (c * N + j) * 64 + tid];
+          }
+      }
+      __syncthreads();
+    }
+    if (RPB == 1 || slot == 0) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * TPR + tid) * N;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (col + j < a.width) {
+            out[col + j] = dw[c][j];
+            out[a.width + col + j] = db[c][j];
+          }
+      }
+    }
+  }
+}
+
+// Rows too wide for the registers: dx from two reads of the row ...
+template <typename T, bool KEPT>
+__global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a) {
+  constexpr int N = Wide<T>::N, TPR = 1024;
+  __shared__ float buf[2][16][2];
+  const int tid = threadIdx.x, wave = tid / 64;
+  const int blocks = ckpt_blocks(a.width), iters = (a.width + TPR * N - 1) / (TPR * N);
+  const float inv = 1.f / (float)a.width;
+  const int first = group_offset(a.offsets, 0, a.rows), last = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
+  int parity = 0;
+  for (long long row = first + (long long)blockIdx.x; row < last; row += gridDim.x) {
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.lddy;
+    T* dx = reinterpret_cast<T*>(a.dx) + row * a.lddx;
+    float xh[N], d[N], w[N], c1 = 0.f, c2 = 0.f;
+    for (int c = 0; c < iters; ++c) {
+      const int col = (c * TPR + tid) * N;
+      load_cols(dy, col, a.width, d);
+      load_xh<T, KEPT>(a, row, col, blocks, mean, rstd, xh);
+      load_params(a.weight, col, a.width, w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        c1 = fmaf(d[j], w[j], c1);
+        c2 = fmaf(d[j] * w[j], xh[j], c2);
+      }
+    }
+    row_sums2<16>(c1, c2, buf[parity], wave);
+    parity ^= 1;
+    c1 *= inv;
+    c2 *= inv;
+    for (int c = 0; c < iters; ++c) {
+      const int col = (c * TPR + tid) * N;
+      load_cols(dy, col, a.width, d);
+      load_xh<T, KEPT>(a, row, col, blocks, mean, rstd, xh);
+      load_params(a.weight, col, a.width, w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) d[j] = rstd * (d[j] * w[j] - fmaf(xh[j], c2, c1));
+      store_cols(dx, col, a.width, d);
+    }
+  }
+}
+
+// ... and the weights' gradients by columns: 1024 threads' columns of the rows of a chunk.
+template <typename T, bool KEPT>
+__global__ __launch_bounds__(1024) void norm_grad_long_weights_kernel(NormGradArgs a, Pieces p) {
+  constexpr int N = Wide<T>::N;
+  const int blocks = ckpt_blocks(a.width);
+  const int col = (int)(blockIdx.y * 1024 + threadIdx.x) * N;
+  const int r0 = blockIdx.x * p.chunk, r1 = a.rows - r0 < p.chunk ? a.rows : r0 + p.chunk;
+  for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
+    const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
+    if (begin >= r1) break;
+    const int lo = begin > r0 ? begin : r0, hi = end < r1 ? end : r1;
+    if (lo >= hi) continue;
+    float dw[N], db[N], d[N], xh[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) dw[j] = db[j] = 0.f;
+    for (long long row = lo; row < hi; ++row) {
+      load_cols(reinterpret_cast<const T*>(a.dy) + row * a.lddy, col, a.width, d);
+      load_xh<T, KEPT>(a, row, col, blocks, a.mean[row], a.rstd[row], xh);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        db[j] += d[j];
+        dw[j] = fmaf(d[j], xh[j], dw[j]);
+      }
+    }
+    float* out = p.partial + (long long)(blockIdx.x + g) * 2 * a.width;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (col + j < a.width) {
+        out[col + j] = dw[j];
+        out[a.width + col + j] = db[j];
+      }
+  }
+}
+
+// A group's gradient: its slots in order.  64 columns (of weights and biases together) a workgroup, four waves over the slots.
+__global__ __launch_bounds__(256) void norm_grad_join_kernel(Pieces p, const int32_t* offsets, int rows, int width,
+                                                             float* __restrict__ dweight, float* __restrict__ dbias, long long ldw,
+                                                             long long ldb) {
+  __shared__ float shared[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, g = blockIdx.y;
+  const long long col = (long long)blockIdx.x * 64 + lane;
+  const int begin = group_offset(offsets, g, rows), end = group_offset(offsets, g + 1, rows);
+  float sum = 0.f;
+  if (begin < end && col < 2LL * width) {
+    const int c1 = (end - 1) / p.chunk;
+    for (int c = begin / p.chunk + wave; c <= c1; c += 4) sum += p.partial[(long long)(c + g) * 2 * width + col];
+  }
+  shared[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && col < 2LL * width) {
+    sum = (shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]);
+    if (col < width) {
+      if (dweight != nullptr) dweight[g * ldw + col] = sum;
+    } else if (dbias != nullptr) {
+      dbias[g * ldb + col - width] = sum;
+    }
+  }
+}
+
+// Rows of a chunk: about a thousand chunks of a large batch; at least 16 rows, where the partial sums (8 bytes a column and chunk)
+// are a tenth of what the rows themselves move, unless that leaves most of the chip without work.
+int chunk_rows(int rows) {
+  const int many = ceil_div(rows, 1024), few = ceil_div(rows, 256);
+  int c = few < 16 ? few : 16;
+  if (many > c) c = many;
+  return c < 1 ? 4 : (c + 3) / 4 * 4;
+}
+
+Pieces pieces_for(int rows, void* workspace) {
+  Pieces p;
+  p.partial = reinterpret_cast<float*>(workspace);
+  p.chunk = chunk_rows(rows);
+  p.chunks = ceil_div(rows, p.chunk);
+  return p;
+}
+
+// The narrowest launch that holds a row: waves a row and 16-byte pieces a thread.  0 waves: the kernels for long rows.
+void pick_shape(int width, int per_load, int* nw, int* ch) {
+  static const int shapes[][2] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}};
+  for (const auto& s : shapes)
+    if ((long long)width <= 64LL * s[0] * s[1] * per_load) {
+      *nw = s[0];
+      *ch = s[1];
+      return;
+    }
+  *nw = 0;
+  *ch = 0;
+}
+
+template <typename T, int NW, int CH>
+void start_norm(const NormArgs& a, hipStream_t stream) {
+  const long long need = ((long long)a.rows + Shape<NW>::RPB - 1) / Shape<NW>::RPB;
+  const long long most = 256LL * 2048 / Shape<NW>::THREADS;   // as many as the chip holds
+  hipLaunchKernelGGL((norm_kernel<T, NW, CH>), dim3((unsigned)(need < most ? need : most)), dim3(Shape<NW>::THREADS), 0, stream, a);
+}
+
+template <typename T>
+hipError_t launch_norm_type(const NormArgs& a, hipStream_t stream) {
+  int nw, ch;
+  pick_shape(a.width, Wide<T>::N, &nw, &ch);
+  if (nw == 1 && ch == 1) start_norm<T, 1, 1>(a, stream);
+  else if (nw == 1 && ch == 2) start_norm<T, 1, 2>(a, stream);
+  else if (nw == 1) start_norm<T, 1, 4>(a, stream);
+  else if (nw == 4 && ch == 2) start_norm<T, 4, 2>(a, stream);
+  else if (nw == 4) start_norm<T, 4, 4>(a, stream);
+  else if (nw == 16 && ch == 2) start_norm<T, 16, 2>(a, stream);
+  else if (nw == 16) start_norm<T, 16, 4>(a, stream);
+  else hipLaunchKernelGGL(norm_long_kernel<T>, dim3(a.rows < 512 ? a.rows : 512), dim3(1024), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <typename T, int NW, int CH, bool KEPT>
+void start_grad(const NormGradArgs& a, const Pieces& p, hipStream_t stream) {
+  hipLaunchKernelGGL((norm_grad_kernel<T, NW, CH, KEPT>), dim3(p.chunks), dim3(Shape<NW>::THREADS), 0, stream, a, p);
+}
+
+template <typename T, bool KEPT>
+hipError_t launch_grad_type(const NormGradArgs& a, const Pieces& p, hipStream_t stream) {
+  int nw, ch;
+  pick_shape(a.width, Wide<T>::N, &nw, &ch);
+  if (a.rows == 0) {
+    // (no rows: the groups' gradients are zero)
+  } else if (nw == 1 && ch == 1) start_grad<T, 1, 1, KEPT>(a, p, stream);
+  else if (nw == 1 && ch == 2) start_grad<T, 1, 2, KEPT>(a, p, stream);
+  else if (nw == 1) start_grad<T, 1, 4, KEPT>(a, p, stream);
+  else if (nw == 4 && ch == 2) start_grad<T, 4, 2, KEPT>(a, p, stream);
+  else if (nw == 4) start_grad<T, 4, 4, KEPT>(a, p, stream);
+  else if (nw == 16 && ch == 2) start_grad<T, 16, 2, KEPT>(a, p, stream);
+  else if (nw == 16) start_grad<T, 16, 4, KEPT>(a, p, stream);
+  else {
+    // (the weights' gradients first: dx may be dy)
+    if (a.dweight != nullptr || a.dbias != nullptr) {
+      hipLaunchKernelGGL((norm_grad_long_weights_kernel<T, KEPT>), dim3(p.chunks, ceil_div(a.width, 1024 * Wide<T>::N)), dim3(1024), 0,
+                         stream, a, p);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    if (a.dx != nullptr)
+      hipLaunchKernelGGL((norm_grad_long_dx_kernel<T, KEPT>), dim3(a.rows < 512 ? a.rows : 512), dim3(1024), 0, stream, a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (a.dweight == nullptr && a.dbias == nullptr)) return e;
+  hipLaunchKernelGGL(norm_grad_join_kernel, dim3(ceil_div(2LL * a.width, 64), a.m), dim3(256), 0, stream, p, a.offsets, a.rows, a.width,
+                     a.dweight, a.dbias, a.ldw, a.ldb);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(const NormArgs& a, hipStream_t stream) {
+  switch (a.dtype) {
+    case ZENO_F32: return launch_norm_type<float>(a, stream);
+    case ZENO_BF16: return launch_norm_type<__bf16>(a, stream);
+    default: return launch_norm_type<_Float16>(a, stream);
+  }
+}
+
+size_t layer_norm_workspace_bytes(int rows, int width, int m) {
+  const Pieces p = pieces_for(rows, nullptr);
+  return align_up((size_t)(p.chunks + m) * 2 * width * sizeof(float), 256);
+}
+
+hipError_t launch_layer_norm_backward(const NormGradArgs& a, void* workspace, hipStream_t stream) {
+  const Pieces p = pieces_for(a.rows, workspace);
+  const bool kept = a.x == nullptr;
+  switch (a.dtype) {
+    case ZENO_F32: return kept ? launch_grad_type<float, true>(a, p, stream) : launch_grad_type<float, false>(a, p, stream);
+    case ZENO_BF16: return kept ? launch_grad_type<__bf16, true>(a, p, stream) : launch_grad_type<__bf16, false>(a, p, stream);
+    default: return kept ? launch_grad_type<_Float16, true>(a, p, stream) : launch_grad_type<_Float16, false>(a, p, stream);
+  }
+}
+
+}  // namespace zeno

@@ -1,0 +1,111 @@
+"""Gradients of a linear layer's weights from 8-bit activations, per worker, against float64 sums of the same values."""
+import numpy as np
+import pytest
+import torch
+
+from tests import _tokens as T
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1805_10032_amd import binding
+    binding.load_library()
+    return binding
+
+
+def check(B, rows, out, width, ty, offsets=None, seed=1, pitch=None, shift=0, edit=None, G_extra=(0, 0)):
+    g = torch.Generator().manual_seed(seed)
+    a = torch.randn(rows, width, generator=g) * torch.exp(0.7 * torch.randn(width, generator=g))
+    dy = torch.randn(rows, out, generator=g)
+    if edit is not None:
+        edit(a, dy)
+    dy, _ = T.strided(dy, T.TYPES[ty], pitch or out, shift)
+    ck = B.zeno_checkpoint(a.cuda())
+    off = [0, rows] if offsets is None else offsets
+    m = len(off) - 1
+    groups = None if offsets is None else torch.tensor(off, dtype=torch.int32, device="cuda")
+    n = out * width
+    before, behind = G_extra
+    G = torch.full((m, before + n + out + behind), 7.0, device="cuda")
+    dw, db = B.zeno_weight_gradient(dy, ck, groups=groups, dweight=G[:, before:before + n], dbias=G[:, before + n:before + n + out])
+    torch.cuda.synchronize()
+    a64, d64 = B.zeno_checkpoint_values(ck).double().cpu().numpy(), dy.double().cpu().numpy()
+    for i, (p, q) in enumerate(zip(off, off[1:])):
+        with np.errstate(invalid="ignore"):
+            want, mag = d64[p:q].T @ a64[p:q], np.abs(d64[p:q]).T @ np.abs(a64[p:q])
+            # exact products (float32's three pieces leave at most 2^-24 of dy out); every addition rounds a sum by at most
+            # 2^-23 of it (the matrix instruction's own rounding included), and three pieces are three additions a token
+            pieces = {"fp32": 3, "bf16": 1, "fp16": 2}[ty]
+            tol = (pieces * (q - p) + 8) * 2 * T.EPS * mag + 1e-37
+            got = dw[i].double().cpu().numpy().reshape(out, width)
+            ok = (np.abs(got - want) <= tol) | (got == want) | (np.isnan(got) & np.isnan(want))
+            assert ok.all(), (i, np.argwhere(~ok)[:5], got[~ok][:5], want[~ok][:5])
+            wb, mb = d64[p:q].sum(0), np.abs(d64[p:q]).sum(0)
+            gb = db[i].double().cpu().numpy()
+            ok = (np.abs(gb - wb) <= (q - p + 8) * T.EPS * mb + 1e-37) | (gb == wb) | (np.isnan(gb) & np.isnan(wb))
+            assert ok.all(), ("bias", i, np.argwhere(~ok)[:5])
+    assert (G[:, :before] == 7).all() and (G[:, before + n + out:] == 7).all()
+    return G
+
+
+SHAPES = [(1, 1, 1), (2, 3, 5), (31, 10, 33), (33, 128, 128), (64, 129, 127), (100, 257, 300), (77, 64, 1001), (600, 10, 40), (40, 513, 96)]
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,out,width", SHAPES)
+def test_one_group(B, rows, out, width, ty):
+    check(B, rows, out, width, ty)
+    check(B, rows, out, width, ty, pitch=out + 3, shift=5, seed=2)
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,out,width", [(200, 40, 70), (900, 130, 260), (3000, 7, 33)])
+def test_groups(B, rows, out, width, ty):
+    off = [2, 2, 3, rows // 4, rows // 4 + 31, rows // 2, rows - 7, rows - 7]
+    G = check(B, rows, out, width, ty, off, G_extra=(3, 2))
+    n = out * width + out
+    assert not G[0, 3:3 + n].any() and not G[-1, 3:3 + n].any()
+    assert torch.equal(G, check(B, rows, out, width, ty, off, G_extra=(3, 2)))       # the same bits every time
+
+
+def test_long_sums(B):
+    """Tokens cut into pieces that several workgroups sum."""
+    check(B, 20000, 10, 100, "fp32")
+    check(B, 9001, 200, 140, "bf16", [0, 4000, 4000, 9001])
+    check(B, 5000, 10, 30, "fp16", [0, 5, 5000])
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+def test_values_that_are_not_finite(B, ty):
+    """An infinity in dy meets ordinary activations and zeros; a NaN among the activations; they reach their row or column only."""
+    def edit(a, dy):
+        dy[3, 2] = float("inf")
+        a[3, 4] = 0.0
+        a[5, 6] = float("nan")
+        dy[7, 1] = float("-inf")
+        a[7, :] = a[7, :].abs() + 0.5
+    check(B, 50, 40, 70, ty, edit=edit)
+
+
+def test_floats_at_the_ends_of_the_range(B):
+    def edit(a, dy):
+        dy[0, 0] = 3.4e38
+        a[0, :] = 0.25
+        dy[1:, 0] = 0.0
+        dy[:, 1] *= 1e-20
+        dy[:, 2] *= 1e30
+        a[:, 5] *= 1e-6
+    check(B, 40, 8, 40, "fp32", edit=edit)
+
+
+def test_no_rows_and_no_bias(B):
+    ck = B.zeno_checkpoint(torch.empty(0, 40, device="cuda"))
+    dw, db = B.zeno_weight_gradient(torch.empty(0, 9, device="cuda"), ck, groups=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    assert dw.shape == (2, 360) and not dw.any() and not db.any()
+    x, dy = torch.randn(30, 40, device="cuda"), torch.randn(30, 9, device="cuda")
+    ck = B.zeno_checkpoint(x)
+    dw, db = B.zeno_weight_gradient(dy, ck)
+    only, none = B.zeno_weight_gradient(dy, ck, want_bias=False)
+    assert none is None and torch.equal(only, dw)
