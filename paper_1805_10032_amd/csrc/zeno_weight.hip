@@ -161,6 +161,167 @@ __global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs a,
   }
 }
 
+// Wide tiles for long sums: 256 x 256 outputs a workgroup, 128 x 128 a wave, which halves what each matrix instruction reads from LDS
+// (64 x 64 a wave asks for all of its bandwidth).  One workgroup a compute unit; stages alternate between two buffers, so the next
+// one is fetched and converted while this one is multiplied.
+constexpr int kWide = 256;
+constexpr int kWidePitch = 288;   // bf16 of an LDS row, 64 bytes behind a multiple of 256
+
+__device__ inline bf16x8 read_wide(const __bf16* tile, int col, int token, int lane) {
+  const int at = (token + 8 * (lane / 32) + (lane % 16) / 4) * kWidePitch + col + 16 * ((lane / 16) % 2) + 4 * (lane % 4);
+  typedef __attribute__((address_space(3))) s16x4* lds;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * kWidePitch));
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, both);
+}
+
+// What a thread fetches of a stage: 8 columns of four tokens of dy, 16 of two tokens of the activations.
+template <typename T>
+struct Fetched {
+  typename Wide<T>::type dy[4][8 / Wide<T>::N];
+  uint4 a[2];
+  uint8_t scale[2];
+};
+
+template <typename T>
+__device__ inline void fetch(const WeightGradArgs& a, int t0, int end, int o0, int k0, int blocks, int tid, Fetched<T>& f) {
+  constexpr int N = Wide<T>::N;
+  const int last = end - 1;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int token = t0 + tid / 32 + 8 * h, col = o0 + 8 * (tid % 32);
+    const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < last ? token : last) * a.lddy + col;
+    if (token < end && col + 8 <= a.out) {
+#pragma unroll
+      for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 / N; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) f.dy[h][i][j] = token < end && col + i * N + j < a.out ? p[i * N + j] : (T)0.f;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int token = t0 + tid / 16 + 16 * h, col = k0 + 16 * (tid % 16);
+    f.a[h] = make_uint4(0, 0, 0, 0);
+    f.scale[h] = 127;
+    if (token < end && col < blocks * kCkptBlock) {
+      f.a[h] = *reinterpret_cast<const uint4*>(a.values + (long long)token * (blocks * kCkptBlock) + col);
+      f.scale[h] = a.scales[(long long)token * blocks + col / kCkptBlock];
+    }
+  }
+}
+
+__device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
+  const bf16x2 q0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false), q1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true);
+  const bf16x2 q2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, false), q3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, true);
+  return bf16x8{q0.x, q0.y, q1.x, q1.y, q2.x, q2.y, q3.x, q3.y};
+}
+
+template <typename T, int P>
+struct WideStage {
+  __bf16 y[P][kTokens * kWidePitch];
+  __bf16 a[kTokens * kWidePitch];
+};
+
+template <typename T, int P>
+__device__ inline void deposit(const Fetched<T>& f, WideStage<T, P>& st, int tid, float (&bias)[8]) {
+  constexpr int N = Wide<T>::N;
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    bf16x8 plane[P];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = (float)f.dy[h][j / N][j % N];
+      bias[j] += v;
+      __bf16 p[P];
+      split<P>(v, p);
+#pragma unroll
+      for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][(tid / 32 + 8 * h) * kWidePitch + 8 * (tid % 32)]) = plane[i];
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float s = ckpt_scale((int)f.scale[h] - 127);
+    __bf16* to = &st.a[(tid / 16 + 16 * h) * kWidePitch + 16 * (tid % 16)];
+    *reinterpret_cast<bf16x8*>(to) = widen8(f.a[h].x, f.a[h].y, s);
+    *reinterpret_cast<bf16x8*>(to + 8) = widen8(f.a[h].z, f.a[h].w, s);
+  }
+}
+
+template <typename T, int P>
+__global__ __launch_bounds__(kThreads, 1) void weight_grad_wide_kernel(WeightGradArgs a, int tiles_in) {
+  extern __shared__ __align__(16) unsigned char memory[];
+  WideStage<T, P>* stage = reinterpret_cast<WideStage<T, P>*>(memory);   // two of them
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  const int o0 = (int)(blockIdx.x / tiles_in) * kWide, k0 = (int)(blockIdx.x % tiles_in) * kWide;
+  const int g = blockIdx.y;
+  const Span span = piece_of(a, g, 0, 1);
+  const int blocks = ckpt_blocks(a.width);
+  const int wo = 128 * (wave / 2), wk = 128 * (wave % 2);
+  f32x16 acc[4][4] = {};
+  float bias[8] = {};
+  Fetched<T> f;
+  const int stages = (span.end - span.begin + kTokens - 1) / kTokens;
+  if (stages > 0) {
+    fetch<T>(a, span.begin, span.end, o0, k0, blocks, tid, f);
+    deposit<T, P>(f, stage[0], tid, bias);
+    if (stages > 1) fetch<T>(a, span.begin + kTokens, span.end, o0, k0, blocks, tid, f);
+  }
+  __syncthreads();
+  for (int i = 0; i < stages; ++i) {
+    const WideStage<T, P>& st = stage[i & 1];
+#pragma unroll
+    for (int t = 0; t < kTokens; t += 16) {
+      bf16x8 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = read_wide(st.a, wk + 32 * j, t, lane);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p) {
+          const bf16x8 y = read_wide(st.y[p], wo + 32 * r, t, lane);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x[j], acc[r][j], 0, 0, 0);
+        }
+      if (t == 0 && i + 1 < stages) {
+        deposit<T, P>(f, stage[(i + 1) & 1], tid, bias);
+        if (i + 2 < stages) fetch<T>(a, span.begin + (i + 2) * kTokens, span.end, o0, k0, blocks, tid, f);
+      }
+    }
+    __syncthreads();
+  }
+  float* dw = a.dweight + g * a.ldw;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = k0 + wk + 32 * j + lane % 32;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int o = o0 + wo + 32 * r + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
+        if (o < a.out && k < a.width) dw[(long long)o * a.width + k] = acc[r][j][e];
+      }
+    }
+  if (k0 == 0 && a.dbias != nullptr) {
+    float (*part)[kWide] = reinterpret_cast<float (*)[kWide]>(memory);   // [8][256]; behind the last barrier nobody reads a stage
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[tid / 32][8 * (tid % 32) + j] = bias[j];
+    __syncthreads();
+    if (o0 + tid < a.out) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += part[i][tid];
+      a.dbias[g * a.ldb + o0 + tid] = sum;
+    }
+  }
+}
+
 // The pieces of a group's tokens, in order.
 __global__ __launch_bounds__(kThreads) void weight_grad_join_kernel(WeightGradArgs a, int pieces, const float* __restrict__ partial) {
   const long long n = (long long)a.out * a.width, all = n + (a.dbias != nullptr ? a.out : 0), stride = n + a.out;
@@ -187,6 +348,21 @@ int pieces_of(int rows, int out, int width, int m) {
   return pieces < 1 ? 1 : (int)pieces;
 }
 
+bool wide_tiles(int rows, int out, int width, int m) {
+  return out > kTile && width > kTile && (long long)ceil_div(out, kWide) * ceil_div(width, kWide) * m >= 256 && rows / m >= 64;
+}
+
+template <typename T, int P>
+hipError_t start_wide(const WeightGradArgs& a, hipStream_t stream) {
+  const size_t lds = 2 * sizeof(WideStage<T, P>);
+  const auto kernel = weight_grad_wide_kernel<T, P>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  const int tiles_in = ceil_div(a.width, kWide);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_in * (long long)ceil_div(a.out, kWide)), a.m), dim3(kThreads), lds, stream, a, tiles_in);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 bool weight_gradient_fits(int out, int width) { return tiles_of(out, width) * kThreads < (1LL << 31); }
@@ -200,6 +376,11 @@ size_t weight_gradient_workspace_bytes(int rows, int out, int width, int m) {
 hipError_t launch_weight_gradient(const WeightGradArgs& a, void* workspace, hipStream_t stream) {
   const int pieces = pieces_of(a.rows, a.out, a.width, a.m);
   float* partial = reinterpret_cast<float*>(workspace);
+  if (wide_tiles(a.rows, a.out, a.width, a.m)) {
+    if (a.dtype == ZENO_F32) return start_wide<float, 3>(a, stream);
+    if (a.dtype == ZENO_BF16) return start_wide<__bf16, 1>(a, stream);
+    return start_wide<_Float16, 2>(a, stream);
+  }
   const dim3 grid((unsigned)tiles_of(a.out, a.width), a.m * pieces), block(kThreads);
   const int tiles_in = ceil_div(a.width, kTile);
   switch (a.dtype) {

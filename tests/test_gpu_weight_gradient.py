@@ -78,6 +78,19 @@ def test_long_sums(B):
 
 
 @pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("m,out,width", [(64, 300, 257), (256, 129, 200), (70, 264, 500)])
+def test_wide_tiles(B, m, out, width, ty):
+    """Enough output for the wide tiles: ragged groups, empty ones and ones of a single token, widths that end inside a tile."""
+    g = torch.Generator().manual_seed(m)
+    sizes = torch.randint(0, 180, (m,), generator=g)
+    sizes[:4] = torch.tensor([0, 1, 32, 33])
+    off = [0, *torch.cumsum(sizes, 0).tolist()]
+    rows = max(off[-1] + 3, 64 * m)
+    check(B, rows, out, width, ty, off, G_extra=(1, 2))
+    check(B, rows, out, width, ty, off, pitch=out + 1, shift=3)
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
 def test_values_that_are_not_finite(B, ty):
     """An infinity in dy meets ordinary activations and zeros; a NaN among the activations; they reach their row or column only."""
     def edit(a, dy):
