@@ -12,12 +12,27 @@ namespace zeno {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 128;      // outputs x inputs of a workgroup; each of its four waves 64 x 64
-constexpr int kTokens = 32;     // tokens of a stage
-constexpr int kPitch = 160;     // bf16 of an LDS row: 64 bytes behind a multiple of 256, so four rows lie on different banks
+constexpr int kTokens = 32;   // pieces of a group's tokens are multiples of it
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// A workgroup of four waves: WO of them along the outputs, 4 / WO along the inputs; a wave takes 32 FO x 32 FI of the product.
+// dy goes in as P pieces; a stage is KT tokens.
+template <int WO_, int FO_, int FI_, int P_>
+struct Tile {
+  static constexpr int WO = WO_, FO = FO_, FI = FI_, P = P_, KT = P == 1 ? 32 : 16;
+  static constexpr int OUT = 32 * FO * WO, IN = 32 * FI * (4 / WO);
+  // bf16 of an LDS row, 64 bytes behind a multiple of 256: the four rows of a transposing read lie on different banks
+  static constexpr int PITCH_O = OUT == 32 ? 32 : OUT + 32, PITCH_I = IN + 32;
+  // what a thread fetches of a stage: 8 outputs of CO tokens, 16 inputs of CI
+  static constexpr int CHUNKS_O = OUT / 8 * KT, CHUNKS_I = IN / 16 * KT;
+  static constexpr int CO = (CHUNKS_O + kThreads - 1) / kThreads, CI = (CHUNKS_I + kThreads - 1) / kThreads;
+};
+template <int P> using WideTile = Tile<2, 4, 4, P>;   // 256 x 256
+template <int P> using MidTile = Tile<2, 2, 2, P>;    // 128 x 128
+template <int P> using FlatTile = Tile<1, 1, 2, P>;   // 32 x 256
 
 struct Span {
   int begin, end;
@@ -25,7 +40,7 @@ struct Span {
 __device__ inline Span piece_of(const WeightGradArgs& a, int g, int piece, int pieces) {
   const int b = group_offset(a.offsets, g, a.rows), e = group_offset(a.offsets, g + 1, a.rows);
   const int n = e > b ? e - b : 0;
-  const int len = ((n + pieces - 1) / pieces + kTokens - 1) / kTokens * kTokens;
+  const int len = (int)(((n + pieces - 1LL) / pieces + kTokens - 1) / kTokens * kTokens);
   const long long lo = b + (long long)len * piece, hi = lo + len;
   Span s;
   s.begin = (int)(lo < b + n ? lo : b + n);
@@ -47,170 +62,62 @@ __device__ inline void split(float v, __bf16 (&piece)[P]) {
   }
 }
 
-// Eight columns of a row as floats, zeros behind its end.
-template <typename T>
-__device__ inline void load8(const T* row, int col, int width, float (&v)[8]) {
-  constexpr int N = Wide<T>::N;
-#pragma unroll
-  for (int h = 0; h < 8 / N; ++h) {
-    float part[N];
-    const int at = col + h * N;
-    if (at + N <= width)
-      load_wide(row + at, part);
-    else
-      load_part(row + at, width - at, 0.f, part);
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[h * N + j] = part[j];
-  }
-}
-
 // One operand of a matrix instruction: 32 columns from `col` on of 16 tokens, lane l column l % 32, tokens 8 (l / 32) + 0..7.
+template <int PITCH>
 __device__ inline bf16x8 read_columns(const __bf16* tile, int col, int token, int lane) {
-  const int at = (token + 8 * (lane / 32) + (lane % 16) / 4) * kPitch + col + 16 * ((lane / 16) % 2) + 4 * (lane % 4);
+  const int at = (token + 8 * (lane / 32) + (lane % 16) / 4) * PITCH + col + 16 * ((lane / 16) % 2) + 4 * (lane % 4);
   typedef __attribute__((address_space(3))) s16x4* lds;
   const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at));
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * kPitch));
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * PITCH));
   const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   return __builtin_bit_cast(bf16x8, both);
 }
 
-template <typename T, int P>
-__global__ __launch_bounds__(kThreads) void weight_grad_kernel(WeightGradArgs a, int tiles_in, int pieces, float* partial) {
-  __shared__ __align__(16) __bf16 ys[P][kTokens * kPitch];
-  __shared__ __align__(16) __bf16 as[kTokens * kPitch];
-  __shared__ float bias_part[16][kTile];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-  const int o0 = (int)(blockIdx.x / tiles_in) * kTile, k0 = (int)(blockIdx.x % tiles_in) * kTile;
-  const int g = blockIdx.y / pieces, piece = blockIdx.y % pieces;
-  const Span span = piece_of(a, g, piece, pieces);
-  const int blocks = ckpt_blocks(a.width);
-  const int wo = 64 * (wave / 2), wk = 64 * (wave % 2);
-  f32x16 acc[2][2] = {};
-  float bias[8] = {};
-  for (int t0 = span.begin; t0 < span.end; t0 += kTokens) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int token = tid / 16 + 16 * h, col = 8 * (tid % 16);
-      const bool live = t0 + token < span.end;
-      const long long row = live ? t0 + token : span.begin;
-      float v[8];
-      load8(reinterpret_cast<const T*>(a.dy) + row * a.lddy, o0 + col, live ? a.out : 0, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bias[j] += v[j];
-      bf16x8 plane[P];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        __bf16 p[P];
-        split<P>(v[j], p);
-#pragma unroll
-        for (int i = 0; i < P; ++i) plane[i][j] = p[i];
-      }
-#pragma unroll
-      for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&ys[i][token * kPitch + col]) = plane[i];
-      bf16x8 kept = {};
-      if (live && k0 + col < blocks * kCkptBlock) {
-        const uint2 w = *reinterpret_cast<const uint2*>(a.values + row * ((long long)blocks * kCkptBlock) + k0 + col);
-        const float s = ckpt_scale((int)a.scales[row * blocks + (k0 + col) / kCkptBlock] - 127);
-        const bf16x2 q0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, s, false), q1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.x, s, true);
-        const bf16x2 q2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, false), q3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w.y, s, true);
-        kept = {q0.x, q0.y, q1.x, q1.y, q2.x, q2.y, q3.x, q3.y};
-      }
-      *reinterpret_cast<bf16x8*>(&as[token * kPitch + col]) = kept;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int t = 0; t < kTokens; t += 16) {
-      bf16x8 x[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) x[j] = read_columns(as, wk + 32 * j, t, lane);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int p = P - 1; p >= 0; --p) {
-          const bf16x8 y = read_columns(ys[p], wo + 32 * i, t, lane);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x[j], acc[i][j], 0, 0, 0);
-        }
-    }
-    __syncthreads();
-  }
-  const long long n = (long long)a.out * a.width;
-  float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (n + a.out);
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int k = k0 + wk + 32 * j + lane % 32;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int o = o0 + wo + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-        if (o < a.out && k < a.width) dw[(long long)o * a.width + k] = acc[i][j][e];
-      }
-    }
-  if (k0 == 0 && a.dbias != nullptr) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) bias_part[tid / 16][8 * (tid % 16) + j] = bias[j];
-    __syncthreads();
-    if (tid < kTile && o0 + tid < a.out) {
-      float sum = 0.f;
-      for (int i = 0; i < 16; ++i) sum += bias_part[i][tid];
-      float* db = pieces == 1 ? a.dbias + g * a.ldb : dw + n;
-      db[o0 + tid] = sum;
-    }
-  }
-}
-
-// Wide tiles for long sums: 256 x 256 outputs a workgroup, 128 x 128 a wave, which halves what each matrix instruction reads from LDS
-// (64 x 64 a wave asks for all of its bandwidth).  One workgroup a compute unit; stages alternate between two buffers, so the next
-// one is fetched and converted while this one is multiplied.
-constexpr int kWide = 256;
-constexpr int kWidePitch = 288;   // bf16 of an LDS row, 64 bytes behind a multiple of 256
-
-__device__ inline bf16x8 read_wide(const __bf16* tile, int col, int token, int lane) {
-  const int at = (token + 8 * (lane / 32) + (lane % 16) / 4) * kWidePitch + col + 16 * ((lane / 16) % 2) + 4 * (lane % 4);
-  typedef __attribute__((address_space(3))) s16x4* lds;
-  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at));
-  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + at + 4 * kWidePitch));
-  typedef short s16x8 __attribute__((ext_vector_type(8)));
-  const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  return __builtin_bit_cast(bf16x8, both);
-}
-
-// What a thread fetches of a stage: 8 columns of four tokens of dy, 16 of two tokens of the activations.
-template <typename T>
+template <typename T, typename S>
 struct Fetched {
-  typename Wide<T>::type dy[4][8 / Wide<T>::N];
-  uint4 a[2];
-  uint8_t scale[2];
+  typename Wide<T>::type dy[S::CO][8 / Wide<T>::N];
+  uint4 a[S::CI];
+  uint8_t scale[S::CI];
 };
 
-template <typename T>
-__device__ inline void fetch(const WeightGradArgs& a, int t0, int end, int o0, int k0, int blocks, int tid, Fetched<T>& f) {
+// Tokens behind the span's end come as copies of its last one: deposit() puts zeros in the place of their dy, and the product with
+// the last token's activations is then NaN only where that token has made it NaN already.  No token is behind a branch, so all
+// loads of a stage are on their way together.
+template <typename T, typename S>
+__device__ inline void fetch(const WeightGradArgs& a, int t0, int end, int o0, int k0, int blocks, int tid, Fetched<T, S>& f) {
   constexpr int N = Wide<T>::N;
-  const int last = end - 1;
+  if (tid < S::CHUNKS_O) {
+    constexpr int PER = S::OUT / 8;
+    const int col = o0 + 8 * (tid % PER);
+    if (col + 8 <= a.out) {
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    const int token = t0 + tid / 32 + 8 * h, col = o0 + 8 * (tid % 32);
-    const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < last ? token : last) * a.lddy + col;
-    if (token < end && col + 8 <= a.out) {
+      for (int h = 0; h < S::CO; ++h) {
+        const int token = t0 + tid / PER + kThreads / PER * h;
+        const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < end ? token : end - 1) * a.lddy + col;
 #pragma unroll
-      for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
-    } else {
+        for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
+      }
+    } else if (col < a.out) {   // (columns behind the last: copies of it, which no output takes)
 #pragma unroll
-      for (int i = 0; i < 8 / N; ++i)
+      for (int h = 0; h < S::CO; ++h) {
+        const int token = t0 + tid / PER + kThreads / PER * h;
+        const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < end ? token : end - 1) * a.lddy;
 #pragma unroll
-        for (int j = 0; j < N; ++j) f.dy[h][i][j] = token < end && col + i * N + j < a.out ? p[i * N + j] : (T)0.f;
+        for (int i = 0; i < 8 / N; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) f.dy[h][i][j] = p[col + i * N + j < a.out ? col + i * N + j : a.out - 1];
+      }
     }
   }
+  constexpr int PER = S::IN / 16;
+  const int col = k0 + 16 * (tid % PER);
+  if (tid < S::CHUNKS_I && col < blocks * kCkptBlock) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int token = t0 + tid / 16 + 16 * h, col = k0 + 16 * (tid % 16);
-    f.a[h] = make_uint4(0, 0, 0, 0);
-    f.scale[h] = 127;
-    if (token < end && col < blocks * kCkptBlock) {
-      f.a[h] = *reinterpret_cast<const uint4*>(a.values + (long long)token * (blocks * kCkptBlock) + col);
-      f.scale[h] = a.scales[(long long)token * blocks + col / kCkptBlock];
+    for (int h = 0; h < S::CI; ++h) {
+      const int token = t0 + tid / PER + kThreads / PER * h;
+      const long long row = token < end ? token : end - 1;
+      f.a[h] = *reinterpret_cast<const uint4*>(a.values + row * (blocks * kCkptBlock) + col);
+      f.scale[h] = a.scales[row * blocks + col / kCkptBlock];
     }
   }
 }
@@ -221,103 +128,150 @@ __device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
   return bf16x8{q0.x, q0.y, q1.x, q1.y, q2.x, q2.y, q3.x, q3.y};
 }
 
-template <typename T, int P>
-struct WideStage {
-  __bf16 y[P][kTokens * kWidePitch];
-  __bf16 a[kTokens * kWidePitch];
+template <typename S>
+struct Stage {
+  __bf16 y[S::P][S::KT * S::PITCH_O];
+  __bf16 a[S::KT * S::PITCH_I];
 };
 
-template <typename T, int P>
-__device__ inline void deposit(const Fetched<T>& f, WideStage<T, P>& st, int tid, float (&bias)[8]) {
-  constexpr int N = Wide<T>::N;
+template <typename T, typename S>
+__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int tid, float (&bias)[8]) {
+  constexpr int N = Wide<T>::N, P = S::P;
+  if (tid < S::CHUNKS_O) {
+    constexpr int PER = S::OUT / 8;
 #pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    bf16x8 plane[P];
+    for (int h = 0; h < S::CO; ++h) {
+      const int token = tid / PER + kThreads / PER * h;
+      const bool live = token < left;
+      bf16x8 plane[P];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float v = (float)f.dy[h][j / N][j % N];
-      bias[j] += v;
-      __bf16 p[P];
-      split<P>(v, p);
+      for (int j = 0; j < 8; ++j) {
+        const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
+        bias[j] += v;
+        __bf16 p[P];
+        split<P>(v, p);
 #pragma unroll
-      for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+        for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+      }
+#pragma unroll
+      for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
     }
-#pragma unroll
-    for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][(tid / 32 + 8 * h) * kWidePitch + 8 * (tid % 32)]) = plane[i];
   }
+  if (tid < S::CHUNKS_I) {
+    constexpr int PER = S::IN / 16;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float s = ckpt_scale((int)f.scale[h] - 127);
-    __bf16* to = &st.a[(tid / 16 + 16 * h) * kWidePitch + 16 * (tid % 16)];
-    *reinterpret_cast<bf16x8*>(to) = widen8(f.a[h].x, f.a[h].y, s);
-    *reinterpret_cast<bf16x8*>(to + 8) = widen8(f.a[h].z, f.a[h].w, s);
+    for (int h = 0; h < S::CI; ++h) {
+      const float s = ckpt_scale((int)f.scale[h] - 127);
+      __bf16* to = &st.a[(tid / PER + kThreads / PER * h) * S::PITCH_I + 16 * (tid % PER)];
+      *reinterpret_cast<bf16x8*>(to) = widen8(f.a[h].x, f.a[h].y, s);
+      *reinterpret_cast<bf16x8*>(to + 8) = widen8(f.a[h].z, f.a[h].w, s);
+    }
   }
 }
 
-template <typename T, int P>
-__global__ __launch_bounds__(kThreads, 1) void weight_grad_wide_kernel(WeightGradArgs a, int tiles_in) {
+// The operands of 16 tokens.
+template <typename S>
+struct Operands {
+  bf16x8 x[S::FI], y[S::P][S::FO];
+};
+template <typename S>
+__device__ inline void read_operands(const Stage<S>& st, int t, int wo, int wk, int lane, Operands<S>& f) {
+#pragma unroll
+  for (int j = 0; j < S::FI; ++j) f.x[j] = read_columns<S::PITCH_I>(st.a, wk + 32 * j, t, lane);
+#pragma unroll
+  for (int r = 0; r < S::FO; ++r)
+#pragma unroll
+    for (int p = 0; p < S::P; ++p) f.y[p][r] = read_columns<S::PITCH_O>(st.y[p], wo + 32 * r, t, lane);
+}
+template <typename S>
+__device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI]) {
+#pragma unroll
+  for (int r = 0; r < S::FO; ++r)
+#pragma unroll
+    for (int p = S::P - 1; p >= 0; --p)   // the smallest piece first
+#pragma unroll
+      for (int j = 0; j < S::FI; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.y[p][r], f.x[j], acc[r][j], 0, 0, 0);
+}
+
+// Three stages in LDS: one that is multiplied, one that is whole, from which the first operands behind the barrier have been read
+// before it, and one that is being written; a fourth is on its way from memory.
+template <typename T, typename S>
+__global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kernel(WeightGradArgs a, int tiles_in, int pieces,
+                                                                                  float* partial) {
   extern __shared__ __align__(16) unsigned char memory[];
-  WideStage<T, P>* stage = reinterpret_cast<WideStage<T, P>*>(memory);   // two of them
+  Stage<S>* stage = reinterpret_cast<Stage<S>*>(memory);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-  const int o0 = (int)(blockIdx.x / tiles_in) * kWide, k0 = (int)(blockIdx.x % tiles_in) * kWide;
-  const int g = blockIdx.y;
-  const Span span = piece_of(a, g, 0, 1);
+  const int o0 = (int)(blockIdx.x / tiles_in) * S::OUT, k0 = (int)(blockIdx.x % tiles_in) * S::IN;
+  const int g = blockIdx.y / pieces, piece = blockIdx.y % pieces;
+  const Span span = piece_of(a, g, piece, pieces);
   const int blocks = ckpt_blocks(a.width);
-  const int wo = 128 * (wave / 2), wk = 128 * (wave % 2);
-  f32x16 acc[4][4] = {};
+  const int wo = 32 * S::FO * (wave % S::WO), wk = 32 * S::FI * (wave / S::WO);
+  f32x16 acc[S::FO][S::FI] = {};
   float bias[8] = {};
-  Fetched<T> f;
-  const int stages = (span.end - span.begin + kTokens - 1) / kTokens;
+  Fetched<T, S> f = {};
+  const int n = span.end - span.begin, stages = (n + S::KT - 1) / S::KT;
+  for (int i = 0; i < 2 && i < stages; ++i) {
+    fetch<T, S>(a, span.begin + i * S::KT, span.end, o0, k0, blocks, tid, f);
+    deposit<T, S>(f, stage[i], n - i * S::KT, tid, bias);
+  }
+  if (stages > 2) fetch<T, S>(a, span.begin + 2 * S::KT, span.end, o0, k0, blocks, tid, f);
+  __syncthreads();
   if (stages > 0) {
-    fetch<T>(a, span.begin, span.end, o0, k0, blocks, tid, f);
-    deposit<T, P>(f, stage[0], tid, bias);
-    if (stages > 1) fetch<T>(a, span.begin + kTokens, span.end, o0, k0, blocks, tid, f);
+    Operands<S> now, next;
+    read_operands<S>(stage[0], 0, wo, wk, lane, now);
+    int at = 0;   // i % 3
+    for (int i = 0; i < stages; ++i) {
+      const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
+      // (behind the last stage the buffers hold an older one, which is read and not used)
+      read_operands<S>(S::KT == 32 ? stage[at] : stage[after], S::KT == 32 ? 16 : 0, wo, wk, lane, next);
+      multiply<S>(now, acc);
+      if (i + 2 < stages) {
+        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, tid, bias);
+        if (i + 3 < stages) fetch<T, S>(a, span.begin + (i + 3) * S::KT, span.end, o0, k0, blocks, tid, f);
+      }
+      if (S::KT == 32) {
+        read_operands<S>(stage[after], 0, wo, wk, lane, now);
+        multiply<S>(next, acc);
+      } else {
+        now = next;
+      }
+      __syncthreads();
+      at = after;
+    }
   }
   __syncthreads();
-  for (int i = 0; i < stages; ++i) {
-    const WideStage<T, P>& st = stage[i & 1];
+  const long long size = (long long)a.out * a.width;
+  float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
+  const bool inside = o0 + S::OUT <= a.out && k0 + S::IN <= a.width;
 #pragma unroll
-    for (int t = 0; t < kTokens; t += 16) {
-      bf16x8 x[4];
+  for (int r = 0; r < S::FO; ++r)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = read_wide(st.a, wk + 32 * j, t, lane);
+    for (int j = 0; j < S::FI; ++j) {
+      const int k = k0 + wk + 32 * j + lane % 32, o = o0 + wo + 32 * r + 4 * (lane / 32);
+      float* to = dw + (long long)o * a.width + k;
+      if (inside) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int e = 0; e < 16; ++e) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
+      } else {
 #pragma unroll
-        for (int p = P - 1; p >= 0; --p) {
-          const bf16x8 y = read_wide(st.y[p], wo + 32 * r, t, lane);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x[j], acc[r][j], 0, 0, 0);
-        }
-      if (t == 0 && i + 1 < stages) {
-        deposit<T, P>(f, stage[(i + 1) & 1], tid, bias);
-        if (i + 2 < stages) fetch<T>(a, span.begin + (i + 2) * kTokens, span.end, o0, k0, blocks, tid, f);
-      }
-    }
-    __syncthreads();
-  }
-  float* dw = a.dweight + g * a.ldw;
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = k0 + wk + 32 * j + lane % 32;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int o = o0 + wo + 32 * r + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-        if (o < a.out && k < a.width) dw[(long long)o * a.width + k] = acc[r][j][e];
+        for (int e = 0; e < 16; ++e)
+          if (o + 8 * (e / 4) + e % 4 < a.out && k < a.width) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
       }
     }
   if (k0 == 0 && a.dbias != nullptr) {
-    float (*part)[kWide] = reinterpret_cast<float (*)[kWide]>(memory);   // [8][256]; behind the last barrier nobody reads a stage
+    constexpr int PER = S::OUT / 8, PARTS = (S::CHUNKS_O < kThreads ? S::CHUNKS_O : kThreads) / PER;
+    float (*part)[S::OUT] = reinterpret_cast<float (*)[S::OUT]>(memory);
+    if (tid < S::CHUNKS_O) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) part[tid / 32][8 * (tid % 32) + j] = bias[j];
+      for (int j = 0; j < 8; ++j) part[tid / PER][8 * (tid % PER) + j] = bias[j];
+    }
     __syncthreads();
-    if (o0 + tid < a.out) {
+    if (tid < S::OUT && o0 + tid < a.out) {
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += part[i][tid];
-      a.dbias[g * a.ldb + o0 + tid] = sum;
+      for (int i = 0; i < PARTS; ++i) sum += part[i][tid];
+      float* db = pieces == 1 ? a.dbias + g * a.ldb : dw + size;
+      db[o0 + tid] = sum;
     }
   }
 }
@@ -337,61 +291,70 @@ __global__ __launch_bounds__(kThreads) void weight_grad_join_kernel(WeightGradAr
   }
 }
 
-long long tiles_of(int out, int width) { return (long long)ceil_div(out, kTile) * ceil_div(width, kTile); }
+template <typename S>
+long long tiles_of(int out, int width) { return (long long)ceil_div(out, S::OUT) * ceil_div(width, S::IN); }
 
-// Pieces that a group's tokens are cut into: where the output tiles alone leave most of the chip idle.
-int pieces_of(int rows, int out, int width, int m) {
-  const long long tiles = tiles_of(out, width) * m;
-  long long pieces = 512 / tiles;
-  const long long most = rows / m / 256;
+enum Shape { kFlat, kMid, kWide };
+struct Plan {
+  Shape shape;
+  int pieces;   // that a group's tokens are cut into: where the output tiles alone leave most of the chip idle
+};
+Plan plan_for(int rows, int out, int width, int m) {
+  Plan p;
+  p.shape = out <= 32 ? kFlat : kMid;
+  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= 64) p.shape = kWide;
+  const long long tiles = (p.shape == kFlat ? tiles_of<FlatTile<1>>(out, width) : tiles_of<MidTile<1>>(out, width)) * m;
+  long long pieces = p.shape == kWide ? 1 : 768 / tiles;
+  const long long most = rows / m / 128;
   if (pieces > most) pieces = most;
-  return pieces < 1 ? 1 : (int)pieces;
+  p.pieces = pieces < 1 ? 1 : (int)pieces;
+  return p;
 }
 
-bool wide_tiles(int rows, int out, int width, int m) {
-  return out > kTile && width > kTile && (long long)ceil_div(out, kWide) * ceil_div(width, kWide) * m >= 256 && rows / m >= 64;
+template <typename T, typename S>
+hipError_t start(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
+  constexpr size_t lds = 3 * sizeof(Stage<S>);
+  static_assert(lds <= 160 * 1024 && sizeof(float) * 8 * (S::CHUNKS_O < kThreads ? S::CHUNKS_O : kThreads) <= lds, "LDS");
+  const auto kernel = weight_grad_kernel<T, S>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles_of<S>(a.out, a.width), a.m * pieces), dim3(kThreads), lds, stream, a,
+                     ceil_div(a.width, S::IN), pieces, partial);
+  return hipGetLastError();
 }
 
 template <typename T, int P>
-hipError_t start_wide(const WeightGradArgs& a, hipStream_t stream) {
-  const size_t lds = 2 * sizeof(WideStage<T, P>);
-  const auto kernel = weight_grad_wide_kernel<T, P>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (e != hipSuccess) return e;
-  const int tiles_in = ceil_div(a.width, kWide);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_in * (long long)ceil_div(a.out, kWide)), a.m), dim3(kThreads), lds, stream, a, tiles_in);
-  return hipGetLastError();
+hipError_t start_shape(const WeightGradArgs& a, const Plan& p, float* partial, hipStream_t stream) {
+  switch (p.shape) {
+    case kFlat: return start<T, FlatTile<P>>(a, p.pieces, partial, stream);
+    case kMid: return start<T, MidTile<P>>(a, p.pieces, partial, stream);
+    default: return start<T, WideTile<P>>(a, p.pieces, partial, stream);
+  }
 }
 
 }  // namespace
 
-bool weight_gradient_fits(int out, int width) { return tiles_of(out, width) * kThreads < (1LL << 31); }
+bool weight_gradient_fits(int out, int width) { return tiles_of<MidTile<1>>(out, width) * kThreads < (1LL << 31); }
 
 size_t weight_gradient_workspace_bytes(int rows, int out, int width, int m) {
-  const int pieces = pieces_of(rows, out, width, m);
-  if (pieces == 1) return 256;
-  return align_up((size_t)m * pieces * ((size_t)out * width + out) * sizeof(float), 256);
+  const Plan p = plan_for(rows, out, width, m);
+  if (p.pieces == 1) return 256;
+  return align_up((size_t)m * p.pieces * ((size_t)out * width + out) * sizeof(float), 256);
 }
 
 hipError_t launch_weight_gradient(const WeightGradArgs& a, void* workspace, hipStream_t stream) {
-  const int pieces = pieces_of(a.rows, a.out, a.width, a.m);
+  const Plan p = plan_for(a.rows, a.out, a.width, a.m);
   float* partial = reinterpret_cast<float*>(workspace);
-  if (wide_tiles(a.rows, a.out, a.width, a.m)) {
-    if (a.dtype == ZENO_F32) return start_wide<float, 3>(a, stream);
-    if (a.dtype == ZENO_BF16) return start_wide<__bf16, 1>(a, stream);
-    return start_wide<_Float16, 2>(a, stream);
-  }
-  const dim3 grid((unsigned)tiles_of(a.out, a.width), a.m * pieces), block(kThreads);
-  const int tiles_in = ceil_div(a.width, kTile);
+  hipError_t e;
   switch (a.dtype) {
-    case ZENO_F32: hipLaunchKernelGGL((weight_grad_kernel<float, 3>), grid, block, 0, stream, a, tiles_in, pieces, partial); break;
-    case ZENO_BF16: hipLaunchKernelGGL((weight_grad_kernel<__bf16, 1>), grid, block, 0, stream, a, tiles_in, pieces, partial); break;
-    default: hipLaunchKernelGGL((weight_grad_kernel<_Float16, 2>), grid, block, 0, stream, a, tiles_in, pieces, partial); break;
+    case ZENO_F32: e = start_shape<float, 3>(a, p, partial, stream); break;
+    case ZENO_BF16: e = start_shape<__bf16, 1>(a, p, partial, stream); break;
+    default: e = start_shape<_Float16, 2>(a, p, partial, stream); break;
   }
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || pieces == 1) return e;
+  if (e != hipSuccess || p.pieces == 1) return e;
   const long long n = (long long)a.out * a.width + a.out, blocks = (n + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096), a.m), block, 0, stream, a, pieces, partial);
+  hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096), a.m), dim3(kThreads), 0, stream, a,
+                     p.pieces, partial);
   return hipGetLastError();
 }
 
