@@ -7,6 +7,7 @@
 // Both operands have the tokens as their slow axis, and a lane of the matrix instruction wants eight tokens of one column: tiles
 // stay as they are in LDS and the transposing LDS read turns four tokens x sixteen columns at a time.
 #include "zeno_tokens.h"
+#include <cstdlib>
 
 namespace zeno {
 namespace {
@@ -80,46 +81,65 @@ struct Fetched {
   uint8_t scale[S::CI];
 };
 
-// Tokens behind the span's end come as copies of its last one: deposit() puts zeros in the place of their dy, and the product with
-// the last token's activations is then NaN only where that token has made it NaN already.  No token is behind a branch, so all
-// loads of a stage are on their way together.
+// Where a thread's part of a stage lies: its first token's, a stage further with every fetch.
 template <typename T, typename S>
-__device__ inline void fetch(const WeightGradArgs& a, int t0, int end, int o0, int k0, int blocks, int tid, Fetched<T, S>& f) {
-  constexpr int N = Wide<T>::N;
-  if (tid < S::CHUNKS_O) {
-    constexpr int PER = S::OUT / 8;
-    const int col = o0 + 8 * (tid % PER);
-    if (col + 8 <= a.out) {
+struct Source {
+  const T* dy;
+  const uint8_t *values, *scales;
+  int out_left, token;     // columns of dy from its first on (<= 0: none); tokens between the stage's first and its own (dy)
+  bool inputs;
+};
+template <typename T, typename S>
+__device__ inline Source<T, S> source_of(const WeightGradArgs& a, int first, int o0, int k0, int blocks, int tid) {
+  constexpr int PO = S::OUT / 8, PI = S::IN / 16;
+  Source<T, S> s;
+  const int o = o0 + 8 * (tid % PO), k = k0 + 16 * (tid % PI);
+  s.out_left = tid < S::CHUNKS_O ? a.out - o : 0;
+  s.token = tid / PO;
+  s.dy = reinterpret_cast<const T*>(a.dy) + (long long)(first + tid / PO) * a.lddy + o;
+  s.inputs = tid < S::CHUNKS_I && k < blocks * kCkptBlock;
+  s.values = a.values + (long long)(first + tid / PI) * (blocks * kCkptBlock) + k;
+  s.scales = a.scales + (long long)(first + tid / PI) * blocks + k / kCkptBlock;
+  return s;
+}
+
+// One stage, of which `left` tokens belong to the span.  In the last one, tokens behind the span's end come as copies of its last:
+// deposit() puts zeros in the place of their dy, and the product with the last token's activations is then NaN only where that token
+// has made it NaN already.  No load is behind a branch of its own, so all of a stage are on their way together.
+template <typename T, typename S>
+__device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid, Fetched<T, S>& f) {
+  constexpr int N = Wide<T>::N, PO = S::OUT / 8, PI = S::IN / 16, RO = kThreads / PO, RI = kThreads / PI;
+  const bool whole = left >= S::KT;
+  // tokens that a thread's h-th row is moved back by
+  auto back = [&](int token) { return whole || token < left ? 0 : token - left + 1; };
+  if (s.out_left >= 8) {
 #pragma unroll
-      for (int h = 0; h < S::CO; ++h) {
-        const int token = t0 + tid / PER + kThreads / PER * h;
-        const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < end ? token : end - 1) * a.lddy + col;
+    for (int h = 0; h < S::CO; ++h) {
+      const T* p = s.dy + (long long)(RO * h - back(s.token + RO * h)) * a.lddy;
 #pragma unroll
-        for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
-      }
-    } else if (col < a.out) {   // (columns behind the last: copies of it, which no output takes)
+      for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
+    }
+  } else if (s.out_left > 0) {   // (columns behind the last: copies of it, which no output takes)
 #pragma unroll
-      for (int h = 0; h < S::CO; ++h) {
-        const int token = t0 + tid / PER + kThreads / PER * h;
-        const T* p = reinterpret_cast<const T*>(a.dy) + (long long)(token < end ? token : end - 1) * a.lddy;
+    for (int h = 0; h < S::CO; ++h) {
+      const T* p = s.dy + (long long)(RO * h - back(s.token + RO * h)) * a.lddy;
 #pragma unroll
-        for (int i = 0; i < 8 / N; ++i)
+      for (int i = 0; i < 8 / N; ++i)
 #pragma unroll
-          for (int j = 0; j < N; ++j) f.dy[h][i][j] = p[col + i * N + j < a.out ? col + i * N + j : a.out - 1];
-      }
+        for (int j = 0; j < N; ++j) f.dy[h][i][j] = p[i * N + j < s.out_left ? i * N + j : s.out_left - 1];
     }
   }
-  constexpr int PER = S::IN / 16;
-  const int col = k0 + 16 * (tid % PER);
-  if (tid < S::CHUNKS_I && col < blocks * kCkptBlock) {
+  if (s.inputs) {
 #pragma unroll
     for (int h = 0; h < S::CI; ++h) {
-      const int token = t0 + tid / PER + kThreads / PER * h;
-      const long long row = token < end ? token : end - 1;
-      f.a[h] = *reinterpret_cast<const uint4*>(a.values + row * (blocks * kCkptBlock) + col);
-      f.scale[h] = a.scales[row * blocks + col / kCkptBlock];
+      const long long row = RI * h - back(tid / PI + RI * h);
+      f.a[h] = *reinterpret_cast<const uint4*>(s.values + row * (blocks * kCkptBlock));
+      f.scale[h] = s.scales[row * blocks];
     }
   }
+  s.dy += (long long)S::KT * a.lddy;
+  s.values += (long long)S::KT * (blocks * kCkptBlock);
+  s.scales += (long long)S::KT * blocks;
 }
 
 __device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
@@ -134,24 +154,37 @@ struct Stage {
   __bf16 a[S::KT * S::PITCH_I];
 };
 
+// Into LDS as bf16, and dy into the sums of the bias where the workgroup has these to take.
 template <typename T, typename S>
-__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int tid, float (&bias)[8]) {
+__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int tid, bool sums, float (&bias)[8]) {
   constexpr int N = Wide<T>::N, P = S::P;
   if (tid < S::CHUNKS_O) {
     constexpr int PER = S::OUT / 8;
+    const bool whole = left >= S::KT;
 #pragma unroll
     for (int h = 0; h < S::CO; ++h) {
       const int token = tid / PER + kThreads / PER * h;
-      const bool live = token < left;
+      const bool live = whole || token < left;
       bf16x8 plane[P];
+      if constexpr (P == 1) {
+        static_assert(P > 1 || sizeof(T) == 2, "one piece is dy itself");
+        uint4 raw = __builtin_bit_cast(uint4, f.dy[h][0]);
+        if (!whole) raw = live ? raw : make_uint4(0, 0, 0, 0);
+        plane[0] = __builtin_bit_cast(bf16x8, raw);
+        if (sums) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
-        bias[j] += v;
-        __bf16 p[P];
-        split<P>(v, p);
+          for (int j = 0; j < 8; ++j) bias[j] += (float)plane[0][j];
+        }
+      } else {
 #pragma unroll
-        for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+        for (int j = 0; j < 8; ++j) {
+          const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
+          if (sums) bias[j] += v;
+          __bf16 p[P];
+          split<P>(v, p);
+#pragma unroll
+          for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+        }
       }
 #pragma unroll
       for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
@@ -210,11 +243,16 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   float bias[8] = {};
   Fetched<T, S> f = {};
   const int n = span.end - span.begin, stages = (n + S::KT - 1) / S::KT;
-  for (int i = 0; i < 2 && i < stages; ++i) {
-    fetch<T, S>(a, span.begin + i * S::KT, span.end, o0, k0, blocks, tid, f);
-    deposit<T, S>(f, stage[i], n - i * S::KT, tid, bias);
+  const bool sums = k0 == 0 && a.dbias != nullptr;
+  Source<T, S> from = source_of<T, S>(a, span.begin, o0, k0, blocks, tid);
+  if (stages > 0) {
+    Fetched<T, S> first = {}, second = {};   // (all three on their way at once; tokens behind the span's end are copies)
+    fetch<T, S>(a, from, n, blocks, tid, first);
+    fetch<T, S>(a, from, n - S::KT, blocks, tid, second);
+    fetch<T, S>(a, from, n - 2 * S::KT, blocks, tid, f);
+    deposit<T, S>(first, stage[0], n, tid, sums, bias);
+    deposit<T, S>(second, stage[1], n - S::KT, tid, sums, bias);
   }
-  if (stages > 2) fetch<T, S>(a, span.begin + 2 * S::KT, span.end, o0, k0, blocks, tid, f);
   __syncthreads();
   if (stages > 0) {
     Operands<S> now, next;
@@ -226,8 +264,8 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       read_operands<S>(S::KT == 32 ? stage[at] : stage[after], S::KT == 32 ? 16 : 0, wo, wk, lane, next);
       multiply<S>(now, acc);
       if (i + 2 < stages) {
-        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, tid, bias);
-        if (i + 3 < stages) fetch<T, S>(a, span.begin + (i + 3) * S::KT, span.end, o0, k0, blocks, tid, f);
+        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, tid, sums, bias);
+        if (i + 3 < stages) fetch<T, S>(a, from, n - (i + 3) * S::KT, blocks, tid, f);
       }
       if (S::KT == 32) {
         read_operands<S>(stage[after], 0, wo, wk, lane, now);
@@ -258,7 +296,7 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
           if (o + 8 * (e / 4) + e % 4 < a.out && k < a.width) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
       }
     }
-  if (k0 == 0 && a.dbias != nullptr) {
+  if (sums) {
     constexpr int PER = S::OUT / 8, PARTS = (S::CHUNKS_O < kThreads ? S::CHUNKS_O : kThreads) / PER;
     float (*part)[S::OUT] = reinterpret_cast<float (*)[S::OUT]>(memory);
     if (tid < S::CHUNKS_O) {
@@ -302,7 +340,7 @@ struct Plan {
 Plan plan_for(int rows, int out, int width, int m) {
   Plan p;
   p.shape = out <= 32 ? kFlat : kMid;
-  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= 64) p.shape = kWide;
+  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= (getenv("WG") ? atoi(getenv("WG")) : 64)) p.shape = kWide;
   const long long tiles = (p.shape == kFlat ? tiles_of<FlatTile<1>>(out, width) : tiles_of<MidTile<1>>(out, width)) * m;
   long long pieces = p.shape == kWide ? 1 : 768 / tiles;
   const long long most = rows / m / 128;
