@@ -7,7 +7,7 @@
 // Both operands have the tokens as their slow axis, and a lane of the matrix instruction wants eight tokens of one column: tiles
 // stay as they are in LDS and the transposing LDS read turns four tokens x sixteen columns at a time.
 #include "zeno_tokens.h"
-#include <cstdlib>
+#include <type_traits>
 
 namespace zeno {
 namespace {
@@ -142,6 +142,31 @@ __device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int left,
   s.scales += (long long)S::KT * blocks;
 }
 
+// The same for a whole stage of a tile that lies inside the matrix, in CO + CI pieces, the last of which moves on.
+template <typename T, typename S>
+__device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T, S>& s, int blocks, int tid, Fetched<T, S>& f) {
+  constexpr int N = Wide<T>::N, RO = kThreads / (S::OUT / 8), RI = kThreads / (S::IN / 16);
+  if (piece < S::CO) {
+    const int h = piece;
+    if (S::CHUNKS_O >= kThreads || tid < S::CHUNKS_O) {
+      const T* p = s.dy + (long long)(RO * h) * a.lddy;
+#pragma unroll
+      for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
+    }
+  } else if (piece < S::CO + S::CI) {
+    const int h = piece - S::CO;
+    if (S::CHUNKS_I >= kThreads || tid < S::CHUNKS_I) {
+      f.a[h] = *reinterpret_cast<const uint4*>(s.values + (long long)(RI * h) * (blocks * kCkptBlock));
+      f.scale[h] = s.scales[(long long)(RI * h) * blocks];
+    }
+  }
+  if (piece == S::CO + S::CI - 1) {
+    s.dy += (long long)S::KT * a.lddy;
+    s.values += (long long)S::KT * (blocks * kCkptBlock);
+    s.scales += (long long)S::KT * blocks;
+  }
+}
+
 __device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
   const bf16x2 q0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false), q1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true);
   const bf16x2 q2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, false), q3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, true);
@@ -154,52 +179,53 @@ struct Stage {
   __bf16 a[S::KT * S::PITCH_I];
 };
 
-// Into LDS as bf16, and dy into the sums of the bias where the workgroup has these to take.
+// Piece h < CO: eight outputs' dy of one token into LDS as bf16, and into the sums of the bias where the workgroup has these to take;
+// piece CO + h: sixteen activations.
+template <typename T, typename S, bool INSIDE>
+__device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>& st, int left, int tid, bool sums, float (&bias)[8]) {
+  constexpr int N = Wide<T>::N, P = S::P;
+  if (piece < S::CO) {
+    if (S::CHUNKS_O < kThreads && tid >= S::CHUNKS_O) return;
+    constexpr int PER = S::OUT / 8;
+    const int h = piece, token = tid / PER + kThreads / PER * h;
+    const bool live = INSIDE || token < left;
+    bf16x8 plane[P];
+    if constexpr (P == 1) {
+      static_assert(P > 1 || sizeof(T) == 2, "one piece is dy itself");
+      uint4 raw = __builtin_bit_cast(uint4, f.dy[h][0]);
+      if (!live) raw = make_uint4(0, 0, 0, 0);
+      plane[0] = __builtin_bit_cast(bf16x8, raw);
+      if (sums) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bias[j] += (float)plane[0][j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
+        if (sums) bias[j] += v;
+        __bf16 p[P];
+        split<P>(v, p);
+#pragma unroll
+        for (int i = 0; i < P; ++i) plane[i][j] = p[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
+  } else if (piece < S::CO + S::CI) {
+    if (S::CHUNKS_I < kThreads && tid >= S::CHUNKS_I) return;
+    constexpr int PER = S::IN / 16;
+    const int h = piece - S::CO;
+    const float s = ckpt_scale((int)f.scale[h] - 127);
+    __bf16* to = &st.a[(tid / PER + kThreads / PER * h) * S::PITCH_I + 16 * (tid % PER)];
+    *reinterpret_cast<bf16x8*>(to) = widen8(f.a[h].x, f.a[h].y, s);
+    *reinterpret_cast<bf16x8*>(to + 8) = widen8(f.a[h].z, f.a[h].w, s);
+  }
+}
 template <typename T, typename S>
 __device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int tid, bool sums, float (&bias)[8]) {
-  constexpr int N = Wide<T>::N, P = S::P;
-  if (tid < S::CHUNKS_O) {
-    constexpr int PER = S::OUT / 8;
-    const bool whole = left >= S::KT;
 #pragma unroll
-    for (int h = 0; h < S::CO; ++h) {
-      const int token = tid / PER + kThreads / PER * h;
-      const bool live = whole || token < left;
-      bf16x8 plane[P];
-      if constexpr (P == 1) {
-        static_assert(P > 1 || sizeof(T) == 2, "one piece is dy itself");
-        uint4 raw = __builtin_bit_cast(uint4, f.dy[h][0]);
-        if (!whole) raw = live ? raw : make_uint4(0, 0, 0, 0);
-        plane[0] = __builtin_bit_cast(bf16x8, raw);
-        if (sums) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) bias[j] += (float)plane[0][j];
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
-          if (sums) bias[j] += v;
-          __bf16 p[P];
-          split<P>(v, p);
-#pragma unroll
-          for (int i = 0; i < P; ++i) plane[i][j] = p[i];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
-    }
-  }
-  if (tid < S::CHUNKS_I) {
-    constexpr int PER = S::IN / 16;
-#pragma unroll
-    for (int h = 0; h < S::CI; ++h) {
-      const float s = ckpt_scale((int)f.scale[h] - 127);
-      __bf16* to = &st.a[(tid / PER + kThreads / PER * h) * S::PITCH_I + 16 * (tid % PER)];
-      *reinterpret_cast<bf16x8*>(to) = widen8(f.a[h].x, f.a[h].y, s);
-      *reinterpret_cast<bf16x8*>(to + 8) = widen8(f.a[h].z, f.a[h].w, s);
-    }
-  }
+  for (int piece = 0; piece < S::CO + S::CI; ++piece) deposit_piece<T, S, false>(piece, f, st, left, tid, sums, bias);
 }
 
 // The operands of 16 tokens.
@@ -208,26 +234,40 @@ struct Operands {
   bf16x8 x[S::FI], y[S::P][S::FO];
 };
 template <typename S>
-__device__ inline void read_operands(const Stage<S>& st, int t, int wo, int wk, int lane, Operands<S>& f) {
-#pragma unroll
-  for (int j = 0; j < S::FI; ++j) f.x[j] = read_columns<S::PITCH_I>(st.a, wk + 32 * j, t, lane);
-#pragma unroll
-  for (int r = 0; r < S::FO; ++r)
-#pragma unroll
-    for (int p = 0; p < S::P; ++p) f.y[p][r] = read_columns<S::PITCH_O>(st.y[p], wo + 32 * r, t, lane);
+__device__ inline void read_operand(int which, const Stage<S>& st, int t, int wo, int wk, int lane, Operands<S>& f) {
+  if (which < S::FI) {
+    f.x[which] = read_columns<S::PITCH_I>(st.a, wk + 32 * which, t, lane);
+  } else {
+    const int r = (which - S::FI) / S::P, p = (which - S::FI) % S::P;
+    f.y[p][r] = read_columns<S::PITCH_O>(st.y[p], wo + 32 * r, t, lane);
+  }
 }
 template <typename S>
-__device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI]) {
+__device__ inline void read_operands(const Stage<S>& st, int t, int wo, int wk, int lane, Operands<S>& f) {
+#pragma unroll
+  for (int i = 0; i < S::FI + S::FO * S::P; ++i) read_operand<S>(i, st, t, wo, wk, lane, f);
+}
+// between(i) stands behind the i-th matrix instruction and stays there
+template <typename S, typename F>
+__device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI], F between) {
+  int i = 0;
 #pragma unroll
   for (int r = 0; r < S::FO; ++r)
 #pragma unroll
     for (int p = S::P - 1; p >= 0; --p)   // the smallest piece first
 #pragma unroll
-      for (int j = 0; j < S::FI; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.y[p][r], f.x[j], acc[r][j], 0, 0, 0);
+      for (int j = 0; j < S::FI; ++j) {
+        acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.y[p][r], f.x[j], acc[r][j], 0, 0, 0);
+        between(i++);
+      }
+}
+template <typename S>
+__device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI]) {
+  multiply<S>(f, acc, [](int) {});
 }
 
 // Three stages in LDS: one that is multiplied, one that is whole, from which the first operands behind the barrier have been read
-// before it, and one that is being written; a fourth is on its way from memory.
+// before it, and one that is being written; two more are on their way from memory.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kernel(WeightGradArgs a, int tiles_in, int pieces,
                                                                                   float* partial) {
@@ -241,31 +281,75 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   const int wo = 32 * S::FO * (wave % S::WO), wk = 32 * S::FI * (wave / S::WO);
   f32x16 acc[S::FO][S::FI] = {};
   float bias[8] = {};
-  Fetched<T, S> f = {};
   const int n = span.end - span.begin, stages = (n + S::KT - 1) / S::KT;
   const bool sums = k0 == 0 && a.dbias != nullptr;
   Source<T, S> from = source_of<T, S>(a, span.begin, o0, k0, blocks, tid);
   if (stages > 0) {
-    Fetched<T, S> first = {}, second = {};   // (all three on their way at once; tokens behind the span's end are copies)
-    fetch<T, S>(a, from, n, blocks, tid, first);
-    fetch<T, S>(a, from, n - S::KT, blocks, tid, second);
-    fetch<T, S>(a, from, n - 2 * S::KT, blocks, tid, f);
-    deposit<T, S>(first, stage[0], n, tid, sums, bias);
-    deposit<T, S>(second, stage[1], n - S::KT, tid, sums, bias);
-  }
-  __syncthreads();
-  if (stages > 0) {
+    Fetched<T, S> even = {}, odd = {};
+    {
+      Fetched<T, S> first = {}, second = {};   // (all four on their way at once; tokens behind the span's end are copies)
+      fetch<T, S>(a, from, n, blocks, tid, first);
+      fetch<T, S>(a, from, n - S::KT, blocks, tid, second);
+      fetch<T, S>(a, from, n - 2 * S::KT, blocks, tid, even);
+      fetch<T, S>(a, from, n - 3 * S::KT, blocks, tid, odd);
+      deposit<T, S>(first, stage[0], n, tid, sums, bias);
+      deposit<T, S>(second, stage[1], n - S::KT, tid, sums, bias);
+    }
+    __syncthreads();
     Operands<S> now, next;
     read_operands<S>(stage[0], 0, wo, wk, lane, now);
-    int at = 0;   // i % 3
-    for (int i = 0; i < stages; ++i) {
+    int at = 0, i = 0;   // at = i % 3
+    // One stage; `f` holds the one after next, and takes the second after that.
+    auto inside = [&](Fetched<T, S>& f, auto with_sums) {
+      constexpr bool SUMS = decltype(with_sums)::value;
+      const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
+      // Reads first, one a step; the conversions and LDS writes spread over the steps behind them; loads last.
+      constexpr int STEPS = S::FO * S::FI * S::P, READS = S::FI + S::FO * S::P, PIECES = S::CO + S::CI;
+      constexpr bool TWO = S::KT == 32;
+      constexpr int FROM = READS < STEPS ? READS : STEPS, ROOM = TWO ? STEPS - FROM : (STEPS - FROM) / 2;
+      constexpr int EVERY = ROOM / PIECES > 0 ? ROOM / PIECES : 1, LOADS_FROM = TWO ? (STEPS > PIECES ? STEPS - PIECES : 0) : FROM + EVERY * PIECES;
+      auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
+      auto read_next = [&](int i) { read_operand<S>(i, TWO ? stage[at] : stage[after], TWO ? 16 : 0, wo, wk, lane, next); };
+      auto read_now = [&](int i) { read_operand<S>(i, stage[after], 0, wo, wk, lane, now); };
+      auto write = [&](int i) { deposit_piece<T, S, true>(i, f, stage[last], S::KT, tid, SUMS, bias); };
+      auto load = [&](int i) { fetch_piece<T, S>(i, a, from, blocks, tid, f); };
+      int reads = 0, writes = 0, loads = 0;   // (constants once the steps are unrolled)
+      pin();
+      multiply<S>(now, acc, [&](int step) {
+        if (reads < READS) read_next(reads++);
+        if (step >= FROM && (step - FROM) % EVERY == 0 && writes < PIECES) write(writes++);
+        if (!TWO && step >= LOADS_FROM && loads < PIECES) load(loads++);
+        pin();
+      });
+#pragma unroll
+      for (int i = FROM < READS ? FROM : READS; i < READS; ++i) read_next(i);
+#pragma unroll
+      for (int i = STEPS > FROM ? (STEPS - FROM + EVERY - 1) / EVERY : 0; i < PIECES; ++i) write(i);
+      if (TWO) {
+        int again = 0;
+        multiply<S>(next, acc, [&](int step) {
+          if (again < READS) read_now(again++);
+          if (step >= LOADS_FROM && loads < PIECES) load(loads++);
+          pin();
+        });
+#pragma unroll
+        for (int i = FROM < READS ? FROM : READS; i < READS; ++i) read_now(i);
+      } else {
+        now = next;
+      }
+#pragma unroll
+      for (int i = STEPS > LOADS_FROM ? STEPS - LOADS_FROM : 0; i < PIECES; ++i) load(i);
+      __syncthreads();
+      at = after;
+    };
+    auto any = [&](Fetched<T, S>& f, int i) {
       const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
       // (behind the last stage the buffers hold an older one, which is read and not used)
       read_operands<S>(S::KT == 32 ? stage[at] : stage[after], S::KT == 32 ? 16 : 0, wo, wk, lane, next);
       multiply<S>(now, acc);
       if (i + 2 < stages) {
         deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, tid, sums, bias);
-        if (i + 3 < stages) fetch<T, S>(a, from, n - (i + 3) * S::KT, blocks, tid, f);
+        if (i + 4 < stages) fetch<T, S>(a, from, n - (i + 4) * S::KT, blocks, tid, f);
       }
       if (S::KT == 32) {
         read_operands<S>(stage[after], 0, wo, wk, lane, now);
@@ -275,6 +359,24 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       }
       __syncthreads();
       at = after;
+    };
+    if (o0 + S::OUT <= a.out && k0 + S::IN <= blocks * kCkptBlock) {
+      // One wave a SIMD issues in order: what is to run beside the matrix instructions has to stand between them.
+      if (S::P > 1 || sums) {   // (beside the splitting the additions do not matter)
+        for (; (i + 6) * S::KT <= n; i += 2) {
+          inside(even, std::true_type());
+          inside(odd, std::true_type());
+        }
+      } else {
+        for (; (i + 6) * S::KT <= n; i += 2) {
+          inside(even, std::false_type());
+          inside(odd, std::false_type());
+        }
+      }
+    }
+    for (; i < stages; i += 2) {
+      any(even, i);
+      if (i + 1 < stages) any(odd, i + 1);
     }
   }
   __syncthreads();
@@ -340,7 +442,7 @@ struct Plan {
 Plan plan_for(int rows, int out, int width, int m) {
   Plan p;
   p.shape = out <= 32 ? kFlat : kMid;
-  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= (getenv("WG") ? atoi(getenv("WG")) : 64)) p.shape = kWide;
+  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= 64) p.shape = kWide;
   const long long tiles = (p.shape == kFlat ? tiles_of<FlatTile<1>>(out, width) : tiles_of<MidTile<1>>(out, width)) * m;
   long long pieces = p.shape == kWide ? 1 : 768 / tiles;
   const long long most = rows / m / 128;
