@@ -7,6 +7,7 @@
 // Both operands have the tokens as their slow axis, and a lane of the matrix instruction wants eight tokens of one column: tiles
 // stay as they are in LDS and the transposing LDS read turns four tokens x sixteen columns at a time.
 #include "zeno_tokens.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace zeno {
@@ -21,19 +22,20 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // A workgroup of four waves: WO of them along the outputs, 4 / WO along the inputs; a wave takes 32 FO x 32 FI of the product.
 // dy goes in as P pieces; a stage is KT tokens.
-template <int WO_, int FO_, int FI_, int P_>
+// ODD: the outputs are not a multiple of eight.
+template <int WO_, int FO_, int FI_, int P_, bool ODD_>
 struct Tile {
+  static constexpr bool ODD = ODD_;
   static constexpr int WO = WO_, FO = FO_, FI = FI_, P = P_, KT = P == 1 ? 32 : 16;
   static constexpr int OUT = 32 * FO * WO, IN = 32 * FI * (4 / WO);
   // bf16 of an LDS row, 64 bytes behind a multiple of 256: the four rows of a transposing read lie on different banks
-  static constexpr int PITCH_O = OUT == 32 ? 32 : OUT + 32, PITCH_I = IN + 32;
+  static constexpr int PITCH_O = OUT + 32, PITCH_I = IN + 32;
   // what a thread fetches of a stage: 8 outputs of CO tokens, 16 inputs of CI
   static constexpr int CHUNKS_O = OUT / 8 * KT, CHUNKS_I = IN / 16 * KT;
   static constexpr int CO = (CHUNKS_O + kThreads - 1) / kThreads, CI = (CHUNKS_I + kThreads - 1) / kThreads;
 };
-template <int P> using WideTile = Tile<2, 4, 4, P>;   // 256 x 256
-template <int P> using MidTile = Tile<2, 2, 2, P>;    // 128 x 128
-template <int P> using FlatTile = Tile<1, 1, 2, P>;   // 32 x 256
+template <int P, bool ODD = false> using WideTile = Tile<2, 4, 4, P, ODD>;   // 256 x 256
+template <int P, bool ODD = false> using MidTile = Tile<2, 2, 2, P, ODD>;    // 128 x 128
 
 struct Span {
   int begin, end;
@@ -81,83 +83,51 @@ struct Fetched {
   uint8_t scale[S::CI];
 };
 
-// Where a thread's part of a stage lies: its first token's, a stage further with every fetch.
+// Where a thread's part of a stage lies: its first token's, a stage further with every fetch.  Columns behind a matrix's last one are
+// those before it once more: no load is behind a branch, and no output takes them.  Eight outputs of which only some are left are
+// fetched as the row's last eight, and moved down by `shift` on their way to LDS.
 template <typename T, typename S>
 struct Source {
   const T* dy;
   const uint8_t *values, *scales;
-  int out_left, token;     // columns of dy from its first on (<= 0: none); tokens between the stage's first and its own (dy)
-  bool inputs;
+  int shift;
 };
 template <typename T, typename S>
 __device__ inline Source<T, S> source_of(const WeightGradArgs& a, int first, int o0, int k0, int blocks, int tid) {
   constexpr int PO = S::OUT / 8, PI = S::IN / 16;
   Source<T, S> s;
   const int o = o0 + 8 * (tid % PO), k = k0 + 16 * (tid % PI);
-  s.out_left = tid < S::CHUNKS_O ? a.out - o : 0;
-  s.token = tid / PO;
-  s.dy = reinterpret_cast<const T*>(a.dy) + (long long)(first + tid / PO) * a.lddy + o;
-  s.inputs = tid < S::CHUNKS_I && k < blocks * kCkptBlock;
-  s.values = a.values + (long long)(first + tid / PI) * (blocks * kCkptBlock) + k;
-  s.scales = a.scales + (long long)(first + tid / PI) * blocks + k / kCkptBlock;
+  const int from = o + 8 <= a.out ? o : a.out - 8;
+  s.shift = o < a.out ? o - from : 0;
+  s.dy = reinterpret_cast<const T*>(a.dy) + (long long)(first + tid / PO) * a.lddy + from;
+  const int at = k < blocks * kCkptBlock ? k : 0;
+  s.values = a.values + (long long)(first + tid / PI) * (blocks * kCkptBlock) + at;
+  s.scales = a.scales + (long long)(first + tid / PI) * blocks + at / kCkptBlock;
   return s;
 }
 
-// One stage, of which `left` tokens belong to the span.  In the last one, tokens behind the span's end come as copies of its last:
-// deposit() puts zeros in the place of their dy, and the product with the last token's activations is then NaN only where that token
-// has made it NaN already.  No load is behind a branch of its own, so all of a stage are on their way together.
-template <typename T, typename S>
-__device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid, Fetched<T, S>& f) {
+// One stage in CO + CI pieces, the last of which moves on.  WHOLE: all its tokens belong to the span; otherwise `left` of them do, and
+// those behind them come as copies of the last: deposit_piece() puts zeros in the place of their dy, and the product with the last
+// token's activations is then NaN only where that token has made it NaN already.
+template <typename T, typename S, bool WHOLE>
+__device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid,
+                                   Fetched<T, S>& f) {
   constexpr int N = Wide<T>::N, PO = S::OUT / 8, PI = S::IN / 16, RO = kThreads / PO, RI = kThreads / PI;
-  const bool whole = left >= S::KT;
-  // tokens that a thread's h-th row is moved back by
-  auto back = [&](int token) { return whole || token < left ? 0 : token - left + 1; };
-  if (s.out_left >= 8) {
-#pragma unroll
-    for (int h = 0; h < S::CO; ++h) {
-      const T* p = s.dy + (long long)(RO * h - back(s.token + RO * h)) * a.lddy;
-#pragma unroll
-      for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
-    }
-  } else if (s.out_left > 0) {   // (columns behind the last: copies of it, which no output takes)
-#pragma unroll
-    for (int h = 0; h < S::CO; ++h) {
-      const T* p = s.dy + (long long)(RO * h - back(s.token + RO * h)) * a.lddy;
-#pragma unroll
-      for (int i = 0; i < 8 / N; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) f.dy[h][i][j] = p[i * N + j < s.out_left ? i * N + j : s.out_left - 1];
-    }
-  }
-  if (s.inputs) {
-#pragma unroll
-    for (int h = 0; h < S::CI; ++h) {
-      const long long row = RI * h - back(tid / PI + RI * h);
-      f.a[h] = *reinterpret_cast<const uint4*>(s.values + row * (blocks * kCkptBlock));
-      f.scale[h] = s.scales[row * blocks];
-    }
-  }
-  s.dy += (long long)S::KT * a.lddy;
-  s.values += (long long)S::KT * (blocks * kCkptBlock);
-  s.scales += (long long)S::KT * blocks;
-}
-
-// The same for a whole stage of a tile that lies inside the matrix, in CO + CI pieces, the last of which moves on.
-template <typename T, typename S>
-__device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T, S>& s, int blocks, int tid, Fetched<T, S>& f) {
-  constexpr int N = Wide<T>::N, RO = kThreads / (S::OUT / 8), RI = kThreads / (S::IN / 16);
+  // tokens that a row is moved back by
+  auto back = [&](int token) { return WHOLE || token < left ? 0 : token - left + 1; };
   if (piece < S::CO) {
     const int h = piece;
     if (S::CHUNKS_O >= kThreads || tid < S::CHUNKS_O) {
-      const T* p = s.dy + (long long)(RO * h) * a.lddy;
+      const T* p = s.dy + (long long)(RO * h - back(tid / PO + RO * h)) * a.lddy;
 #pragma unroll
       for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
     }
   } else if (piece < S::CO + S::CI) {
     const int h = piece - S::CO;
     if (S::CHUNKS_I >= kThreads || tid < S::CHUNKS_I) {
-      f.a[h] = *reinterpret_cast<const uint4*>(s.values + (long long)(RI * h) * (blocks * kCkptBlock));
-      f.scale[h] = s.scales[(long long)(RI * h) * blocks];
+      const long long row = RI * h - back(tid / PI + RI * h);
+      f.a[h] = *reinterpret_cast<const uint4*>(s.values + row * (blocks * kCkptBlock));
+      f.scale[h] = s.scales[row * blocks];
     }
   }
   if (piece == S::CO + S::CI - 1) {
@@ -165,6 +135,11 @@ __device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T,
     s.values += (long long)S::KT * (blocks * kCkptBlock);
     s.scales += (long long)S::KT * blocks;
   }
+}
+template <typename T, typename S>
+__device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid, Fetched<T, S>& f) {
+#pragma unroll
+  for (int piece = 0; piece < S::CO + S::CI; ++piece) fetch_piece<T, S, false>(piece, a, s, left, blocks, tid, f);
 }
 
 __device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
@@ -181,18 +156,26 @@ struct Stage {
 
 // Piece h < CO: eight outputs' dy of one token into LDS as bf16, and into the sums of the bias where the workgroup has these to take;
 // piece CO + h: sixteen activations.
-template <typename T, typename S, bool INSIDE>
-__device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>& st, int left, int tid, bool sums, float (&bias)[8]) {
+template <typename T, typename S, bool WHOLE>
+__device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>& st, int left, int shift, int tid, bool sums,
+                                     float (&bias)[8]) {
   constexpr int N = Wide<T>::N, P = S::P;
   if (piece < S::CO) {
     if (S::CHUNKS_O < kThreads && tid >= S::CHUNKS_O) return;
     constexpr int PER = S::OUT / 8;
     const int h = piece, token = tid / PER + kThreads / PER * h;
-    const bool live = INSIDE || token < left;
+    const bool live = WHOLE || token < left;
     bf16x8 plane[P];
     if constexpr (P == 1) {
       static_assert(P > 1 || sizeof(T) == 2, "one piece is dy itself");
       uint4 raw = __builtin_bit_cast(uint4, f.dy[h][0]);
+      if (S::ODD && shift != 0) {
+        if (shift & 4) raw = make_uint4(raw.z, raw.w, raw.w, raw.w);
+        if (shift & 2) raw = make_uint4(raw.y, raw.z, raw.w, raw.w);
+        if (shift & 1)
+          raw = make_uint4(__builtin_amdgcn_alignbit(raw.y, raw.x, 16), __builtin_amdgcn_alignbit(raw.z, raw.y, 16),
+                           __builtin_amdgcn_alignbit(raw.w, raw.z, 16), raw.w >> 16);
+      }
       if (!live) raw = make_uint4(0, 0, 0, 0);
       plane[0] = __builtin_bit_cast(bf16x8, raw);
       if (sums) {
@@ -200,12 +183,23 @@ __device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>
         for (int j = 0; j < 8; ++j) bias[j] += (float)plane[0][j];
       }
     } else {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (float)f.dy[h][j / N][j % N];
+      if (S::ODD && shift != 0) {
+#pragma unroll
+        for (int by = 4; by > 0; by /= 2)
+          if (shift & by) {
+#pragma unroll
+            for (int j = 0; j + by < 8; ++j) v[j] = v[j + by];
+          }
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float v = live ? (float)f.dy[h][j / N][j % N] : 0.f;
-        if (sums) bias[j] += v;
+        if (!live) v[j] = 0.f;
+        if (sums) bias[j] += v[j];
         __bf16 p[P];
-        split<P>(v, p);
+        split<P>(v[j], p);
 #pragma unroll
         for (int i = 0; i < P; ++i) plane[i][j] = p[i];
       }
@@ -223,9 +217,10 @@ __device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>
   }
 }
 template <typename T, typename S>
-__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int tid, bool sums, float (&bias)[8]) {
+__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int shift, int tid, bool sums,
+                               float (&bias)[8]) {
 #pragma unroll
-  for (int piece = 0; piece < S::CO + S::CI; ++piece) deposit_piece<T, S, false>(piece, f, st, left, tid, sums, bias);
+  for (int piece = 0; piece < S::CO + S::CI; ++piece) deposit_piece<T, S, false>(piece, f, st, left, shift, tid, sums, bias);
 }
 
 // The operands of 16 tokens.
@@ -292,15 +287,15 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       fetch<T, S>(a, from, n - S::KT, blocks, tid, second);
       fetch<T, S>(a, from, n - 2 * S::KT, blocks, tid, even);
       fetch<T, S>(a, from, n - 3 * S::KT, blocks, tid, odd);
-      deposit<T, S>(first, stage[0], n, tid, sums, bias);
-      deposit<T, S>(second, stage[1], n - S::KT, tid, sums, bias);
+      deposit<T, S>(first, stage[0], n, from.shift, tid, sums, bias);
+      deposit<T, S>(second, stage[1], n - S::KT, from.shift, tid, sums, bias);
     }
     __syncthreads();
     Operands<S> now, next;
     read_operands<S>(stage[0], 0, wo, wk, lane, now);
     int at = 0, i = 0;   // at = i % 3
     // One stage; `f` holds the one after next, and takes the second after that.
-    auto inside = [&](Fetched<T, S>& f, auto with_sums) {
+    auto whole = [&](Fetched<T, S>& f, auto with_sums) __attribute__((always_inline)) {
       constexpr bool SUMS = decltype(with_sums)::value;
       const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
       // Reads first, one a step; the conversions and LDS writes spread over the steps behind them; loads last.
@@ -311,8 +306,8 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
       auto read_next = [&](int i) { read_operand<S>(i, TWO ? stage[at] : stage[after], TWO ? 16 : 0, wo, wk, lane, next); };
       auto read_now = [&](int i) { read_operand<S>(i, stage[after], 0, wo, wk, lane, now); };
-      auto write = [&](int i) { deposit_piece<T, S, true>(i, f, stage[last], S::KT, tid, SUMS, bias); };
-      auto load = [&](int i) { fetch_piece<T, S>(i, a, from, blocks, tid, f); };
+      auto write = [&](int i) { deposit_piece<T, S, true>(i, f, stage[last], S::KT, from.shift, tid, SUMS, bias); };
+      auto load = [&](int i) { fetch_piece<T, S, true>(i, a, from, S::KT, blocks, tid, f); };
       int reads = 0, writes = 0, loads = 0;   // (constants once the steps are unrolled)
       pin();
       multiply<S>(now, acc, [&](int step) {
@@ -342,13 +337,13 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       __syncthreads();
       at = after;
     };
-    auto any = [&](Fetched<T, S>& f, int i) {
+    auto any = [&](Fetched<T, S>& f, int i) __attribute__((always_inline)) {
       const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
       // (behind the last stage the buffers hold an older one, which is read and not used)
       read_operands<S>(S::KT == 32 ? stage[at] : stage[after], S::KT == 32 ? 16 : 0, wo, wk, lane, next);
       multiply<S>(now, acc);
       if (i + 2 < stages) {
-        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, tid, sums, bias);
+        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, from.shift, tid, sums, bias);
         if (i + 4 < stages) fetch<T, S>(a, from, n - (i + 4) * S::KT, blocks, tid, f);
       }
       if (S::KT == 32) {
@@ -360,18 +355,16 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       __syncthreads();
       at = after;
     };
-    if (o0 + S::OUT <= a.out && k0 + S::IN <= blocks * kCkptBlock) {
-      // One wave a SIMD issues in order: what is to run beside the matrix instructions has to stand between them.
-      if (S::P > 1 || sums) {   // (beside the splitting the additions do not matter)
-        for (; (i + 6) * S::KT <= n; i += 2) {
-          inside(even, std::true_type());
-          inside(odd, std::true_type());
-        }
-      } else {
-        for (; (i + 6) * S::KT <= n; i += 2) {
-          inside(even, std::false_type());
-          inside(odd, std::false_type());
-        }
+    // One wave a SIMD issues in order: what is to run beside the matrix instructions has to stand between them.
+    if (S::P > 1 || sums) {   // (beside the splitting the additions do not matter)
+      for (; (i + 6) * S::KT <= n; i += 2) {
+        whole(even, std::true_type());
+        whole(odd, std::true_type());
+      }
+    } else {
+      for (; (i + 6) * S::KT <= n; i += 2) {
+        whole(even, std::integral_constant<bool, (S::P > 1)>());
+        whole(odd, std::integral_constant<bool, (S::P > 1)>());
       }
     }
     for (; i < stages; i += 2) {
@@ -416,39 +409,172 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   }
 }
 
-// The pieces of a group's tokens, in order.
-__global__ __launch_bounds__(kThreads) void weight_grad_join_kernel(WeightGradArgs a, int pieces, const float* __restrict__ partial) {
+// Few outputs: the sums are short of work for the matrix cores, and reading the activations is what counts.  A lane owns COLS columns and
+// all outputs of them; a wave goes down its tokens, whose dy it has put into LDS in float32 and reads back as broadcasts.  The eight
+// waves of a workgroup share the columns and add up at the end.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewTokens = 32;
+
+template <typename T, int OMAX, int COLS>
+__global__ __launch_bounds__(kFewThreads, OMAX * COLS <= 64 ? 4 : 2) void weight_grad_few_kernel(WeightGradArgs a, int pieces, float* partial) {
+  constexpr int kCols = 64 * COLS, kStaged = kFewWaves * kFewTokens * OMAX, kJoined = OMAX * kCols;
+  __shared__ __align__(16) float memory[kStaged > kJoined ? kStaged : kJoined];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  const int g = blockIdx.y / pieces, piece = blockIdx.y % pieces;
+  const Span span = piece_of(a, g, piece, pieces);
+  const int blocks = ckpt_blocks(a.width);
+  const int col = (int)blockIdx.x * kCols + COLS * lane;
+  const int at = col < blocks * kCkptBlock ? col : 0;   // (columns behind the last: the first ones, which nothing takes)
+  const bool sums = blockIdx.x == 0 && a.dbias != nullptr;
+  constexpr int SP = OMAX <= 4 ? 4 : (OMAX <= 8 ? 8 : (OMAX <= 16 ? 16 : 32));   // lanes that stage a token's dy
+  float acc[OMAX][COLS] = {}, bias = 0.f;                                       // (the bias: output lane % SP, tokens of the lane)
+  float (*staged)[OMAX] = reinterpret_cast<float (*)[OMAX]>(memory + wave * kFewTokens * OMAX);
+  const uint8_t* values = a.values + at;
+  const uint8_t* scales = a.scales + at / kCkptBlock;
+  const long long pitch = (long long)blocks * kCkptBlock;
+  for (int t0 = span.begin + kFewTokens * wave; t0 < span.end; t0 += kFewTokens * kFewWaves) {
+    const int n = span.end - t0 < kFewTokens ? span.end - t0 : kFewTokens;
+    row_sync<1>();
+#pragma unroll
+    for (int i = 0; i < kFewTokens * SP / 64; ++i) {
+      const int t = 64 / SP * i + lane / SP, o = lane % SP;
+      const float d = t < n && o < a.out ? (float)reinterpret_cast<const T*>(a.dy)[(long long)(t0 + t) * a.lddy + o] : 0.f;
+      bias += d;
+      if (o < OMAX) staged[t][o] = d;
+    }
+    row_sync<1>();
+    constexpr int STEP = 8;
+    for (int t = 0; t < n; t += STEP) {
+      unsigned words[STEP][COLS / 4];
+      uint8_t scale[STEP];
+#pragma unroll
+      for (int i = 0; i < STEP; ++i) {
+        const long long row = t0 + (t + i < n ? t + i : n - 1);   // (its dy is zero in LDS where it stands in for another)
+#pragma unroll
+        for (int j = 0; j < COLS / 4; ++j) words[i][j] = reinterpret_cast<const unsigned*>(values + row * pitch)[j];
+        scale[i] = scales[row * blocks];
+      }
+#pragma unroll
+      for (int i = 0; i < STEP; ++i) {
+        float v[COLS];
+        ckpt_unpack(words[i], ckpt_scale((int)scale[i] - 127), v);
+#pragma unroll
+        for (int o = 0; o < OMAX; o += 4) {
+          const float4 d = *reinterpret_cast<const float4*>(&staged[t + i][o]);
+          const float dd[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) acc[o + e][c] = fmaf(dd[e], v[c], acc[o + e][c]);
+          }
+        }
+      }
+    }
+  }
+  const long long size = (long long)a.out * a.width;
+  float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
+  float (*joined)[kCols] = reinterpret_cast<float (*)[kCols]>(memory);
+  for (int w = 0; w < kFewWaves; ++w) {
+    __syncthreads();
+    if (wave == w) {
+#pragma unroll
+      for (int o = 0; o < OMAX; ++o)
+#pragma unroll
+        for (int c = 0; c < COLS; c += 4) {
+          float4* to = reinterpret_cast<float4*>(&joined[o][COLS * lane + c]);
+          float4 v = make_float4(acc[o][c], acc[o][c + 1], acc[o][c + 2], acc[o][c + 3]);
+          if (w > 0) {
+            const float4 old = *to;
+            v = make_float4(v.x + old.x, v.y + old.y, v.z + old.z, v.w + old.w);
+          }
+          *to = v;
+        }
+    }
+  }
+  __syncthreads();
+  const int left = a.width - (int)blockIdx.x * kCols < kCols ? a.width - (int)blockIdx.x * kCols : kCols;
+  for (int o = 0; o < a.out; ++o)
+    for (int c = tid; c < left; c += kFewThreads) dw[(long long)o * a.width + (int)blockIdx.x * kCols + c] = joined[o][c];
+  if (sums) {
+#pragma unroll
+    for (int off = SP; off < 64; off <<= 1) bias += __shfl_xor(bias, off, 64);
+    for (int w = 0; w < kFewWaves; ++w) {
+      __syncthreads();
+      if (wave == w && lane < SP) memory[lane] = bias + (w > 0 ? memory[lane] : 0.f);
+    }
+    __syncthreads();
+    float* db = pieces == 1 ? a.dbias + g * a.ldb : dw + size;
+    if (tid < a.out) db[tid] = memory[tid];
+  }
+}
+
+// The pieces of a group's tokens.  A wave takes 64 gradients and every so-manieth piece; the waves' sums are added in their order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void weight_grad_join_kernel(WeightGradArgs a, int pieces, const float* __restrict__ partial) {
+  __shared__ float shared[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, waves = blockDim.x / 64, g = blockIdx.y;
   const long long n = (long long)a.out * a.width, all = n + (a.dbias != nullptr ? a.out : 0), stride = n + a.out;
-  const int g = blockIdx.y;
   const float* p = partial + (long long)g * pieces * stride;
-  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kThreads) {
+  for (long long base = 64LL * blockIdx.x; base < all; base += 64LL * gridDim.x) {
+    const long long i = base + lane;
     float sum = 0.f;
-    for (int s = 0; s < pieces; ++s) sum += p[s * stride + i];
-    if (i < n)
-      a.dweight[g * a.ldw + i] = sum;
-    else
-      a.dbias[g * a.ldb + i - n] = sum;
+    if (i < all) {
+#pragma unroll 4
+      for (int s = wave; s < pieces; s += waves) sum += p[s * stride + i];
+    }
+    shared[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && i < all) {
+      for (int w = 1; w < waves; ++w) sum += shared[w][lane];
+      if (i < n)
+        a.dweight[g * a.ldw + i] = sum;
+      else
+        a.dbias[g * a.ldb + i - n] = sum;
+    }
+    __syncthreads();
   }
 }
 
 template <typename S>
 long long tiles_of(int out, int width) { return (long long)ceil_div(out, S::OUT) * ceil_div(width, S::IN); }
 
-enum Shape { kFlat, kMid, kWide };
+constexpr int kFewOutputs = 32;   // at most so many: the kernel for few outputs
+inline int few_columns(int out) { return out <= 8 ? 512 : 256; }
+
+enum Shape { kFew, kMid, kWide };
 struct Plan {
   Shape shape;
-  int pieces;   // that a group's tokens are cut into: where the output tiles alone leave most of the chip idle
+  int pieces;   // that a group's tokens are cut into: where the output alone leaves most of the chip idle
 };
 Plan plan_for(int rows, int out, int width, int m) {
   Plan p;
-  p.shape = out <= 32 ? kFlat : kMid;
+  if (out <= kFewOutputs) {
+    p.shape = kFew;
+    const long long strips = (long long)ceil_div(width, few_columns(out)) * m;
+    const long long pieces = 512 / strips, most = rows / m / (kFewTokens * kFewWaves);
+    p.pieces = (int)std::max(1LL, std::min(pieces, most));
+    return p;
+  }
+  p.shape = kMid;
   if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= 64) p.shape = kWide;
-  const long long tiles = (p.shape == kFlat ? tiles_of<FlatTile<1>>(out, width) : tiles_of<MidTile<1>>(out, width)) * m;
-  long long pieces = p.shape == kWide ? 1 : 768 / tiles;
-  const long long most = rows / m / 128;
-  if (pieces > most) pieces = most;
-  p.pieces = pieces < 1 ? 1 : (int)pieces;
+  const long long pieces = p.shape == kWide ? 1 : 768 / (tiles_of<MidTile<1>>(out, width) * m), most = rows / m / 128;
+  p.pieces = (int)std::max(1LL, std::min(pieces, most));
   return p;
+}
+
+template <typename T, int OMAX, int COLS>
+hipError_t start_few(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
+  hipLaunchKernelGGL((weight_grad_few_kernel<T, OMAX, COLS>), dim3(ceil_div(a.width, 64 * COLS), a.m * pieces), dim3(kFewThreads), 0, stream,
+                     a, pieces, partial);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t start_few_type(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
+  if (a.out <= 4) return start_few<T, 4, 8>(a, pieces, partial, stream);
+  if (a.out <= 8) return start_few<T, 8, 8>(a, pieces, partial, stream);
+  if (a.out <= 12) return start_few<T, 12, 4>(a, pieces, partial, stream);
+  if (a.out <= 16) return start_few<T, 16, 4>(a, pieces, partial, stream);
+  if (a.out <= 24) return start_few<T, 24, 4>(a, pieces, partial, stream);
+  return start_few<T, 32, 4>(a, pieces, partial, stream);
 }
 
 template <typename T, typename S>
@@ -463,13 +589,17 @@ hipError_t start(const WeightGradArgs& a, int pieces, float* partial, hipStream_
   return hipGetLastError();
 }
 
-template <typename T, int P>
+template <typename T, int P, bool ODD>
 hipError_t start_shape(const WeightGradArgs& a, const Plan& p, float* partial, hipStream_t stream) {
   switch (p.shape) {
-    case kFlat: return start<T, FlatTile<P>>(a, p.pieces, partial, stream);
-    case kMid: return start<T, MidTile<P>>(a, p.pieces, partial, stream);
-    default: return start<T, WideTile<P>>(a, p.pieces, partial, stream);
+    case kFew: return start_few_type<T>(a, p.pieces, partial, stream);
+    case kMid: return start<T, MidTile<P, ODD>>(a, p.pieces, partial, stream);
+    default: return start<T, WideTile<P, ODD>>(a, p.pieces, partial, stream);
   }
+}
+template <typename T, int P>
+hipError_t start_type(const WeightGradArgs& a, const Plan& p, float* partial, hipStream_t stream) {
+  return a.out % 8 != 0 ? start_shape<T, P, true>(a, p, partial, stream) : start_shape<T, P, false>(a, p, partial, stream);
 }
 
 }  // namespace
@@ -487,14 +617,16 @@ hipError_t launch_weight_gradient(const WeightGradArgs& a, void* workspace, hipS
   float* partial = reinterpret_cast<float*>(workspace);
   hipError_t e;
   switch (a.dtype) {
-    case ZENO_F32: e = start_shape<float, 3>(a, p, partial, stream); break;
-    case ZENO_BF16: e = start_shape<__bf16, 1>(a, p, partial, stream); break;
-    default: e = start_shape<_Float16, 2>(a, p, partial, stream); break;
+    case ZENO_F32: e = start_type<float, 3>(a, p, partial, stream); break;
+    case ZENO_BF16: e = start_type<__bf16, 1>(a, p, partial, stream); break;
+    default: e = start_type<_Float16, 2>(a, p, partial, stream); break;
   }
   if (e != hipSuccess || p.pieces == 1) return e;
-  const long long n = (long long)a.out * a.width + a.out, blocks = (n + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096), a.m), dim3(kThreads), 0, stream, a,
-                     p.pieces, partial);
+  const long long n = (long long)a.out * a.width + a.out, blocks = (n + 63) / 64;
+  int waves = 1;
+  while (waves < kJoinWaves && 4 * waves < p.pieces) waves *= 2;   // four pieces a wave
+  hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)(blocks < 8192 ? blocks : 8192), a.m), dim3(64 * waves), 0, stream, a, p.pieces,
+                     partial);
   return hipGetLastError();
 }
 

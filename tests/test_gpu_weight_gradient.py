@@ -70,6 +70,16 @@ def test_groups(B, rows, out, width, ty):
     assert torch.equal(G, check(B, rows, out, width, ty, off, G_extra=(3, 2)))       # the same bits every time
 
 
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("out", [1, 4, 5, 8, 9, 12, 13, 16, 17, 24, 25, 32, 33])
+def test_few_outputs(B, out, ty):
+    """Every number of outputs that has a variant of its own, widths on both sides of a workgroup's columns, tokens of one wave, of
+    several, and of several workgroups."""
+    check(B, 700, out, 530, ty, [1, 1, 34, 300, 699], G_extra=(1, 1))
+    check(B, 3001, out, 255, ty, pitch=out + 1, shift=1)
+    check(B, 9, out, 4, ty)
+
+
 def test_long_sums(B):
     """Tokens cut into pieces that several workgroups sum."""
     check(B, 20000, 10, 100, "fp32")
