@@ -31,18 +31,12 @@ __global__ __launch_bounds__(kThreads) void checkpoint_kernel(const T* __restric
 #pragma unroll
       for (int j = 0; j < N; ++j) v[h * N + j] = part[j];
     }
-    float largest = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) largest = ckpt_larger(largest, v[j]);
-    largest = fmaxf(largest, __shfl_xor(largest, 1, 64));
-    largest = fmaxf(largest, __shfl_xor(largest, 2, 64));
-    const int k = ckpt_exponent(largest);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = ckpt_quotient(v[j], k);
+    float q[8];
+    const int k = ckpt_quotients<8>(v, q);
     if (live) {
       uint2 w;
-      w.x = ckpt_pack4(v[0], v[1], v[2], v[3]);
-      w.y = ckpt_pack4(v[4], v[5], v[6], v[7]);
+      w.x = ckpt_pack4(q[0], q[1], q[2], q[3]);
+      w.y = ckpt_pack4(q[4], q[5], q[6], q[7]);
       *reinterpret_cast<uint2*>(values + row * (blocks * 32LL) + col) = w;
       if ((threadIdx.x & 3) == 0) scales[row * blocks + col / 32] = (uint8_t)(k + 127);
     }

@@ -7,6 +7,8 @@
 // registers from row to row, and so do the sums of their gradients.
 #include "zeno_tokens.h"
 
+#include <type_traits>
+
 namespace zeno {
 namespace {
 
@@ -75,15 +77,8 @@ __device__ inline void load_params(const float* p, int col, int width, float (&v
 // The 8-bit copy of N columns of a row (a block's columns lie in neighbouring lanes).  Every lane of the wave takes part.
 template <int N>
 __device__ inline void keep_cols(const float (&v)[N], int col, int width, int blocks, uint8_t* values, uint8_t* scales, long long row) {
-  float largest = 0.f;
-#pragma unroll
-  for (int j = 0; j < N; ++j) largest = ckpt_larger(largest, v[j]);
-#pragma unroll
-  for (int off = 1; off < kCkptBlock / N; off <<= 1) largest = fmaxf(largest, __shfl_xor(largest, off, 64));
-  const int k = ckpt_exponent(largest);
   float q[N];
-#pragma unroll
-  for (int j = 0; j < N; ++j) q[j] = ckpt_quotient(v[j], k);
+  const int k = ckpt_quotients<N>(v, q);
   if (col < blocks * kCkptBlock) {
     uint8_t* p = values + row * ((long long)blocks * kCkptBlock) + col;
 #pragma unroll
@@ -92,55 +87,151 @@ __device__ inline void keep_cols(const float (&v)[N], int col, int width, int bl
   }
 }
 
-// CH 16-byte pieces of a row a thread.
+// Keeps the compiler from holding the unpacked values of a row from one pass over it to the next: unpacking again costs an instruction a
+// value, holding them costs the registers of a second workgroup.
+template <typename V>
+__device__ inline void unpack_again(V& v) {
+  asm volatile("" : "+v"(v));
+}
+
+// A thread's part of a row as it lies in memory: CH 16-byte pieces, the c-th at column (c * TPR + tid) * N.  Pieces behind the row's end
+// are its first columns once more, and one that the end cuts is the row's last N columns: so all of them are whole loads behind no
+// branch, and cut() puts the right values (and zeros) in their place when they are used.
+template <typename T, int TPR, int CH>
+struct RowPart {
+  typename Wide<T>::type raw[CH];
+  __device__ inline void load(const T* row, int tid, int width) {
+    constexpr int N = Wide<T>::N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * TPR + tid) * N;
+      if (width < N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) raw[c][j] = row[j < width ? j : 0];
+      } else {
+        const int at = col + N <= width ? col : (col < width ? width - N : 0);
+        raw[c] = *reinterpret_cast<const typename Wide<T>::unaligned*>(row + at);
+      }
+    }
+  }
+  __device__ inline void again() {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (CH * Wide<T>::N >= 32) unpack_again(raw[c]);
+  }
+  __device__ inline void get(int c, int tid, int width, float (&v)[Wide<T>::N]) const {
+    constexpr int N = Wide<T>::N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = (float)raw[c][j];
+    if ((c + 1) * TPR * N > width) cut<N>((c * TPR + tid) * N, width, v);
+  }
+  __device__ inline void normalised(int c, int tid, int width, float mean, float rstd, float (&v)[Wide<T>::N]) const {
+    get(c, tid, width, v);
+#pragma unroll
+    for (int j = 0; j < Wide<T>::N; ++j) v[j] = (v[j] - mean) * rstd;
+  }
+  template <int N>
+  static __device__ inline void cut(int col, int width, float (&v)[N]) {
+    const int have = width - col;   // columns of this piece
+    if (have >= N) return;
+    const int shift = width < N ? 0 : N - width % N;
+#pragma unroll
+    for (int by = N / 2; by > 0; by /= 2)
+      if (shift & by) {
+#pragma unroll
+        for (int j = 0; j + by < N; ++j) v[j] = v[j + by];
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j >= have) v[j] = 0.f;
+  }
+};
+
+// Weights in LDS, in the order in which the lanes read them: four floats a lane next to the neighbour's.
+template <int N, int TPR, int CH>
+struct Params {
+  static constexpr int SIZE = CH * N * TPR;
+  __device__ static inline void fill(float* to, const float* from, int width) {
+    for (int i = threadIdx.x; i < SIZE; i += blockDim.x) {
+      const int j = i % 4, lane = i / 4 % TPR, h = i / (4 * TPR) % (N / 4), c = i / (4 * TPR) / (N / 4);
+      const int col = (c * TPR + lane) * N + 4 * h + j;
+      to[i] = from != nullptr && col < width ? from[col] : 0.f;
+    }
+  }
+  __device__ static inline void get(const float* p, int c, int tid, float (&v)[N]) {
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h) {
+      const float4 q = *reinterpret_cast<const float4*>(p + ((c * (N / 4) + h) * TPR + tid) * 4);
+      v[4 * h] = q.x;
+      v[4 * h + 1] = q.y;
+      v[4 * h + 2] = q.z;
+      v[4 * h + 3] = q.w;
+    }
+  }
+};
+
+// The next row is on its way while a row is reduced.
 template <typename T, int NW, int CH>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
   constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
+  typedef Params<N, TPR, CH> P;
   __shared__ float buf[2][NW][2];
+  __shared__ __align__(16) float weight[P::SIZE], bias[P::SIZE];
   const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
   const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
-  float w[CH][N], b[CH][N];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    load_params(a.weight, (c * TPR + tid) * N, a.width, w[c]);
-    load_params(a.bias, (c * TPR + tid) * N, a.width, b[c]);
-  }
-  for (long long row = (long long)blockIdx.x * RPB + slot; row < a.rows; row += (long long)gridDim.x * RPB) {
-    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
-    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy;
-    float v[CH][N], sum = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) load_cols(x, (c * TPR + tid) * N, a.width, v[c]);
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int j = 0; j < N; ++j) sum += v[c][j];
-    const float mean = row_sum1<NW>(sum, buf[0], wave) * inv;
-    float sq = 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float d = v[c][j] - mean;
-        if ((c * TPR + tid) * N + j < a.width) sq = fmaf(d, d, sq);
-      }
-    const float var = row_sum1<NW>(sq, buf[1], wave) * inv;
-    const float rstd = 1.f / sqrtf(var + a.eps);
-    if (a.values != nullptr) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) keep_cols<N>(v[c], (c * TPR + tid) * N, a.width, blocks, a.values, a.scales, row);
-    }
+  P::fill(weight, a.weight, a.width);
+  P::fill(bias, a.bias, a.width);
+  __syncthreads();
+  const long long step = (long long)gridDim.x * RPB;
+  long long row = (long long)blockIdx.x * RPB + slot;
+  if (row >= a.rows) return;
+  const T* x = reinterpret_cast<const T*>(a.x);
+  RowPart<T, TPR, CH> now, next;
+  now.load(x + row * a.ldx, tid, a.width);
+  for (; row < a.rows; row += step) {
+    next.load(x + (row + step < a.rows ? row + step : row) * a.ldx, tid, a.width);
+    float sum = 0.f, v[N];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      now.get(c, tid, a.width, v);
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[c][j] = fmaf((v[c][j] - mean) * rstd, w[c][j], b[c][j]);
-      store_cols(y, (c * TPR + tid) * N, a.width, v[c]);
+      for (int j = 0; j < N; ++j) sum += v[j];
+    }
+    const float mean = row_sum1<NW>(sum, buf[0], wave) * inv;
+    float sq = 0.f;
+    now.again();
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      now.get(c, tid, a.width, v);
+      const int have = a.width - (c * TPR + tid) * N;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = v[j] - mean;
+        if ((c + 1) * TPR * N <= a.width || j < have) sq = fmaf(d, d, sq);
+      }
+    }
+    const float var = row_sum1<NW>(sq, buf[1], wave) * inv;
+    const float rstd = 1.f / sqrtf(var + a.eps);
+    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy;
+    now.again();
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * TPR + tid) * N;
+      now.get(c, tid, a.width, v);
+      if (a.values != nullptr) keep_cols<N>(v, col, a.width, blocks, a.values, a.scales, row);
+      float w[N], b[N];
+      P::get(weight, c, tid, w);
+      P::get(bias, c, tid, b);
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = fmaf((v[j] - mean) * rstd, w[j], b[j]);
+      store_cols(y, col, a.width, v);
     }
     if (tid == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
     }
+    now = next;
   }
 }
 
@@ -229,18 +320,71 @@ __device__ inline void load_xh(const NormGradArgs& a, long long row, int col, in
   for (int j = 0; j < N; ++j) v[j] = (v[j] - mean) * rstd;
 }
 
+// The same of a checkpoint, whose rows end with zeros in whole blocks.
+template <typename T, int TPR, int CH>
+struct KeptPart {
+  unsigned words[CH][Wide<T>::N / 4];
+  uint8_t scale[CH];
+  __device__ inline void load(const uint8_t* values, const uint8_t* scales, long long row, int blocks, int tid) {
+    constexpr int N = Wide<T>::N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * TPR + tid) * N, at = col < blocks * kCkptBlock ? col : 0;
+      const uint8_t* p = values + row * ((long long)blocks * kCkptBlock) + at;
+#pragma unroll
+      for (int j = 0; j < N / 4; ++j) words[c][j] = reinterpret_cast<const unsigned*>(p)[j];
+      scale[c] = scales[row * blocks + at / kCkptBlock];
+    }
+  }
+  __device__ inline void again() {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < Wide<T>::N / 4; ++j)
+        if (CH * Wide<T>::N >= 32) unpack_again(words[c][j]);
+  }
+  // (q scale is exact, and so is the difference where it cancels)
+  __device__ inline void normalised(int c, int, int, float mean, float rstd, float (&v)[Wide<T>::N]) const {
+    const float s = ckpt_scale((int)scale[c] - 127);
+#pragma unroll
+    for (int i = 0; i < Wide<T>::N; i += 4) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(words[c][i / 4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(words[c][i / 4], true);
+      v[i] = fmaf(lo.x, s, -mean) * rstd;
+      v[i + 1] = fmaf(lo.y, s, -mean) * rstd;
+      v[i + 2] = fmaf(hi.x, s, -mean) * rstd;
+      v[i + 3] = fmaf(hi.y, s, -mean) * rstd;
+    }
+  }
+};
+template <typename T, int TPR, int CH, bool KEPT>
+struct GradRow {
+  RowPart<T, TPR, CH> dy;
+  typename std::conditional<KEPT, KeptPart<T, TPR, CH>, RowPart<T, TPR, CH>>::type x;
+  float mean, rstd;
+  __device__ inline void load(const NormGradArgs& a, long long row, int blocks, int tid) {
+    dy.load(reinterpret_cast<const T*>(a.dy) + row * a.lddy, tid, a.width);
+    if constexpr (KEPT)
+      x.load(a.values, a.scales, row, blocks, tid);
+    else
+      x.load(reinterpret_cast<const T*>(a.x) + row * a.ldx, tid, a.width);
+    mean = a.mean[row];
+    rstd = a.rstd[row];
+  }
+};
+
 template <typename T, int NW, int CH, bool KEPT>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradArgs a, Pieces p) {
   constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
+  typedef Params<N, TPR, CH> P;
   __shared__ float buf[2][NW][2];
+  __shared__ __align__(16) float weight[P::SIZE];
   __shared__ float joined[RPB > 1 ? 2 * CH * N * 64 : 1];
   const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
   const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
   const int r0 = blockIdx.x * p.chunk, r1 = a.rows - r0 < p.chunk ? a.rows : r0 + p.chunk;
-  float w[CH][N];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) load_params(a.weight, (c * TPR + tid) * N, a.width, w[c]);
+  P::fill(weight, a.weight, a.width);
+  __syncthreads();
   int parity = 0;
   for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
     const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
@@ -252,38 +396,49 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int j = 0; j < N; ++j) dw[c][j] = db[c][j] = 0.f;
-    for (long long row = lo + slot; row < hi; row += RPB) {
-      const float mean = a.mean[row], rstd = a.rstd[row];
-      const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.lddy;
-      float xh[CH][N], d[CH][N], c1 = 0.f, c2 = 0.f;
+    GradRow<T, TPR, CH, KEPT> now, next, after;   // two rows are on their way while a third is reduced (one: 92 instead of 84 us)
+    if (lo + slot < hi) {
+      now.load(a, lo + slot, blocks, tid);
+      next.load(a, lo + slot + RPB < hi ? lo + slot + RPB : lo + slot, blocks, tid);
+    }
+    for (int row = lo + slot; row < hi; row += RPB) {
+      after.load(a, row + 2 * RPB < hi ? row + 2 * RPB : row, blocks, tid);
+      const float mean = now.mean, rstd = now.rstd;
+      float c1 = 0.f, c2 = 0.f, d[N], xh[N], w[N];
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        load_cols(dy, (c * TPR + tid) * N, a.width, d[c]);
-        load_xh<T, KEPT>(a, row, (c * TPR + tid) * N, blocks, mean, rstd, xh[c]);
-      }
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
+        now.dy.get(c, tid, a.width, d);
+        now.x.normalised(c, tid, a.width, mean, rstd, xh);
+        P::get(weight, c, tid, w);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          db[c][j] += d[c][j];
-          dw[c][j] = fmaf(d[c][j], xh[c][j], dw[c][j]);
-          d[c][j] *= w[c][j];
-          c1 += d[c][j];
-          c2 = fmaf(d[c][j], xh[c][j], c2);
+          db[c][j] += d[j];
+          dw[c][j] = fmaf(d[j], xh[j], dw[c][j]);
+          const float t = d[j] * w[j];
+          c1 += t;
+          c2 = fmaf(t, xh[j], c2);
         }
+      }
       if (a.dx != nullptr) {
         row_sums2<NW>(c1, c2, buf[parity], wave);
         parity ^= 1;
-        c1 *= inv;
-        c2 *= inv;
-        T* dx = reinterpret_cast<T*>(a.dx) + row * a.lddx;
+        c1 *= inv * -rstd;
+        c2 *= inv * -rstd;
+        T* dx = reinterpret_cast<T*>(a.dx) + (long long)row * a.lddx;
+        now.dy.again();
+        now.x.again();
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
+          now.dy.get(c, tid, a.width, d);
+          now.x.normalised(c, tid, a.width, mean, rstd, xh);
+          P::get(weight, c, tid, w);
 #pragma unroll
-          for (int j = 0; j < N; ++j) d[c][j] = rstd * (d[c][j] - fmaf(xh[c][j], c2, c1));
-          store_cols(dx, (c * TPR + tid) * N, a.width, d[c]);
+          for (int j = 0; j < N; ++j) d[j] = fmaf(d[j] * w[j], rstd, fmaf(xh[j], c2, c1));
+          store_cols(dx, (c * TPR + tid) * N, a.width, d);
         }
       }
+      now = next;
+      next = after;
     }
     float* out = p.partial + (long long)(blockIdx.x + g) * 2 * a.width;
     if (RPB > 1) {
@@ -301,18 +456,13 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
         }
         __syncthreads();
       }
-      if (slot == 0) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int j = 0; j < N; ++j) {
-            dw[c][j] = joined[(c * N + j) * 64 + tid];
-            db[c][j] = joined[CH * N * 64 + (c * N + j) * 64 + tid];
-          }
+      for (int i = threadIdx.x; i < a.width; i += Shape<NW>::THREADS) {
+        const int c = i / (64 * N), lane = i / N % 64, at = (c * N + i % N) * 64 + lane;
+        out[i] = joined[at];
+        out[a.width + i] = joined[CH * N * 64 + at];
       }
       __syncthreads();
-    }
-    if (RPB == 1 || slot == 0) {
+    } else {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int col = (c * TPR + tid) * N;
@@ -428,13 +578,14 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(Pieces p, const int
   }
 }
 
-// Rows of a chunk: about a thousand chunks of a large batch; at least 16 rows, where the partial sums (8 bytes a column and chunk)
-// are a tenth of what the rows themselves move, unless that leaves most of the chip without work.
+// Rows of a chunk: 512 chunks of a large batch, two workgroups a compute unit (16384 x 4096 bf16 from a checkpoint: 84 us; 256 chunks 93,
+// 768 105, because a third workgroup does not fit beside two); at least 16 rows, where the partial sums (8 bytes a column and chunk) are a
+// tenth of what the rows themselves move, unless that leaves most of the chip without work.
 int chunk_rows(int rows) {
-  const int many = ceil_div(rows, 1024), few = ceil_div(rows, 256);
+  const int many = ceil_div(rows, 512), few = ceil_div(rows, 256);
   int c = few < 16 ? few : 16;
   if (many > c) c = many;
-  return c < 1 ? 4 : (c + 3) / 4 * 4;
+  return c < 1 ? 1 : c;
 }
 
 Pieces pieces_for(int rows, void* workspace) {
@@ -445,11 +596,13 @@ Pieces pieces_for(int rows, void* workspace) {
   return p;
 }
 
-// The narrowest launch that holds a row: waves a row and 16-byte pieces a thread.  0 waves: the kernels for long rows.
-void pick_shape(int width, int per_load, int* nw, int* ch) {
-  static const int shapes[][2] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}};
+// The narrowest launch that holds a row: waves a row and 16-byte pieces a thread.  0 waves: the kernels for long rows, beyond 16384
+// columns, whose weights and biases no longer fit LDS.
+void pick_shape(int width, int per_load, bool backward, int* nw, int* ch) {
+  // (the backward pass holds two sums for every column: from four pieces a thread on, a row is shared by four waves)
+  const int shapes[][2] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 16 / per_load}};
   for (const auto& s : shapes)
-    if ((long long)width <= 64LL * s[0] * s[1] * per_load) {
+    if (64 * s[0] * s[1] * per_load <= 16384 && width <= 64 * s[0] * s[1] * per_load) {
       *nw = s[0];
       *ch = s[1];
       return;
@@ -461,21 +614,20 @@ void pick_shape(int width, int per_load, int* nw, int* ch) {
 template <typename T, int NW, int CH>
 void start_norm(const NormArgs& a, hipStream_t stream) {
   const long long need = ((long long)a.rows + Shape<NW>::RPB - 1) / Shape<NW>::RPB;
-  const long long most = 256LL * 2048 / Shape<NW>::THREADS;   // as many as the chip holds
+  const long long most = 256LL * 1024 / Shape<NW>::THREADS;   // what the chip holds with the weights in LDS: more workgroups would only fill it again
   hipLaunchKernelGGL((norm_kernel<T, NW, CH>), dim3((unsigned)(need < most ? need : most)), dim3(Shape<NW>::THREADS), 0, stream, a);
 }
 
 template <typename T>
 hipError_t launch_norm_type(const NormArgs& a, hipStream_t stream) {
   int nw, ch;
-  pick_shape(a.width, Wide<T>::N, &nw, &ch);
+  pick_shape(a.width, Wide<T>::N, false, &nw, &ch);
   if (nw == 1 && ch == 1) start_norm<T, 1, 1>(a, stream);
   else if (nw == 1 && ch == 2) start_norm<T, 1, 2>(a, stream);
-  else if (nw == 1) start_norm<T, 1, 4>(a, stream);
+  else if (nw == 1 && ch == 4) start_norm<T, 1, 4>(a, stream);
   else if (nw == 4 && ch == 2) start_norm<T, 4, 2>(a, stream);
   else if (nw == 4) start_norm<T, 4, 4>(a, stream);
-  else if (nw == 16 && ch == 2) start_norm<T, 16, 2>(a, stream);
-  else if (nw == 16) start_norm<T, 16, 4>(a, stream);
+  else if (nw == 16) start_norm<T, 16, 16 / Wide<T>::N>(a, stream);
   else hipLaunchKernelGGL(norm_long_kernel<T>, dim3(a.rows < 512 ? a.rows : 512), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
@@ -488,16 +640,15 @@ void start_grad(const NormGradArgs& a, const Pieces& p, hipStream_t stream) {
 template <typename T, bool KEPT>
 hipError_t launch_grad_type(const NormGradArgs& a, const Pieces& p, hipStream_t stream) {
   int nw, ch;
-  pick_shape(a.width, Wide<T>::N, &nw, &ch);
+  pick_shape(a.width, Wide<T>::N, true, &nw, &ch);
   if (a.rows == 0) {
     // (no rows: the groups' gradients are zero)
   } else if (nw == 1 && ch == 1) start_grad<T, 1, 1, KEPT>(a, p, stream);
   else if (nw == 1 && ch == 2) start_grad<T, 1, 2, KEPT>(a, p, stream);
-  else if (nw == 1) start_grad<T, 1, 4, KEPT>(a, p, stream);
+  else if (nw == 1 && ch == 4) start_grad<T, 1, 4, KEPT>(a, p, stream);
   else if (nw == 4 && ch == 2) start_grad<T, 4, 2, KEPT>(a, p, stream);
   else if (nw == 4) start_grad<T, 4, 4, KEPT>(a, p, stream);
-  else if (nw == 16 && ch == 2) start_grad<T, 16, 2, KEPT>(a, p, stream);
-  else if (nw == 16) start_grad<T, 16, 4, KEPT>(a, p, stream);
+  else if (nw == 16) start_grad<T, 16, 16 / Wide<T>::N, KEPT>(a, p, stream);
   else {
     // (the weights' gradients first: dx may be dy)
     if (a.dweight != nullptr || a.dbias != nullptr) {

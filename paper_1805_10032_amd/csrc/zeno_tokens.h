@@ -45,15 +45,31 @@ __device__ inline void store_part(T* p, int n, const float (&v)[Wide<T>::N]) {
     if (i < n) p[i] = (T)v[i];
 }
 
+// Reductions over the 64 lanes without LDS: neighbours by DPP inside rows of sixteen, rows by the lane swaps.  Every lane adds the same
+// pairs, so all of them get the same bits.
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+template <typename F>
+__device__ inline float wave_reduce(float v, F f) {
+  v = f(v, dpp<kDppXor1>(v));
+  v = f(v, dpp<kDppXor2>(v));
+  v = f(v, dpp<kDppHalfMirror>(v));
+  v = f(v, dpp<kDppMirror>(v));
+  const unsigned u = __float_as_uint(v);
+  const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = f(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+  const unsigned w = __float_as_uint(v);
+  const auto halves = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return f(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
 __device__ inline float wave_sum_f(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  return wave_reduce(v, [](float a, float b) { return a + b; });
 }
 __device__ inline float wave_max_f(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-  return v;
+  return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // Barrier of the NW waves that share a row.  One wave runs its LDS accesses in order, so only the compiler has to keep them so.
@@ -108,30 +124,53 @@ __device__ inline int ckpt_exponent(float largest) {
 }
 __device__ inline float ckpt_scale(int k) { return __uint_as_float(k > -127 ? (unsigned)(k + 127) << 23 : 1u << 22); }
 
-// v / 2^k on the e4m3 grid, rounded to nearest even; an infinity or a NaN becomes NaN.  With the largest k (floats above 448 * 2^119) the
-// grid's next step up may be beyond float32's range: values stop at the step below it.
-__device__ inline float ckpt_quotient(float v, int k) {
-  float q = v * ckpt_scale(-k);                        // -k lies in [-120, 127]: a normal scale, and the product is exact or tiny
-  if (k >= 120) q = fminf(fmaxf(q, -240.f), 240.f);
-  return fabsf(v) < __builtin_inff() ? q : __builtin_nanf("");
-}
 __device__ inline unsigned ckpt_pack4(float a, float b, float c, float d) {
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
-// the largest finite magnitude among |v|, `sofar`
-__device__ inline float ckpt_larger(float sofar, float v) {
-  const float a = fabsf(v);
-  return a < __builtin_inff() ? fmaxf(sofar, a) : sofar;
+// N of a block's 32 columns, whose others the next 32 / N - 1 lanes hold, divided by the block's scale; returns its exponent k.  An
+// infinity stays one and is packed as NaN; it does not enter the scale.  All lanes of a block take part.
+template <int N>
+__device__ inline int ckpt_quotients(const float (&v)[N], float (&q)[N]) {
+  auto block_max = [](float m) {
+    m = fmaxf(m, dpp<kDppXor1>(m));
+    m = fmaxf(m, dpp<kDppXor2>(m));
+    if (N == 4) m = fmaxf(m, dpp<kDppHalfMirror>(m));
+    return m;
+  };
+  float largest = fabsf(v[0]);
+#pragma unroll
+  for (int j = 1; j < N; ++j) largest = fmaxf(largest, fabsf(v[j]));
+  largest = block_max(largest);
+  const float inf = __builtin_inff();
+  if (!(largest < inf)) {   // (the lanes of a block agree)
+    largest = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) largest = fabsf(v[j]) < inf ? fmaxf(largest, fabsf(v[j])) : largest;
+    largest = block_max(largest);
+  }
+  const int k = ckpt_exponent(largest);
+  const float scale = ckpt_scale(-k);   // -k lies in [-120, 127]: a normal scale, and the quotient is exact or far below the grid's first step
+#pragma unroll
+  for (int j = 0; j < N; ++j) q[j] = v[j] * scale;
+  if (k >= 120) {
+    // floats above 448 * 2^119: the grid's next step up may lie beyond float32's range
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (fabsf(v[j]) < inf) q[j] = fminf(fmaxf(q[j], -240.f), 240.f);
+  }
+  return k;
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <int N>
 __device__ inline void ckpt_unpack(const unsigned* words, float scale, float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; i += 4) {
-    v[i] = __builtin_amdgcn_cvt_f32_fp8(words[i / 4], 0) * scale;
-    v[i + 1] = __builtin_amdgcn_cvt_f32_fp8(words[i / 4], 1) * scale;
-    v[i + 2] = __builtin_amdgcn_cvt_f32_fp8(words[i / 4], 2) * scale;
-    v[i + 3] = __builtin_amdgcn_cvt_f32_fp8(words[i / 4], 3) * scale;
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(words[i / 4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(words[i / 4], true);
+    v[i] = lo.x * scale;
+    v[i + 1] = lo.y * scale;
+    v[i + 2] = hi.x * scale;
+    v[i + 3] = hi.y * scale;
   }
 }
 
