@@ -18,6 +18,18 @@ constexpr int kCandidates = 512;   // top values are chosen from at most so many
 constexpr int kMaxParts = 64;      // workgroups that share a row
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// (written out: fmaxf would first quiet every operand that might be a signalling NaN, an instruction a value)
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+template <int N>
+__device__ inline float max_of(const float (&v)[N], float m) {
+#pragma unroll
+  for (int j = 0; j < N; j += 2) m = max3(v[j], v[j + 1], m);
+  return m;
+}
 __device__ inline float finite(float x) { return fminf(fmaxf(x, -FLT_MAX), FLT_MAX); }
 
 // What a row, or a part of it, comes to: s and t relative to the largest logit M.
@@ -75,8 +87,7 @@ struct Shared {
   float log_s[4 / NW], M[4 / NW];
   int empty[4 / NW];
   float group_max[TOP ? 4 / NW : 1][TOP ? kGroups : 1][TOP ? TPR : 1];
-  float thread_max[TOP ? 4 / NW : 1][TOP ? TPR : 1];
-  float tau[4 / NW];
+  __align__(16) float thread_max[TOP ? 4 / NW : 1][TOP ? TPR : 4];
   int count[4 / NW], more[4 / NW], ties[4];
   float cand_val[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
   int cand_idx[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
@@ -93,23 +104,27 @@ __device__ inline void load_at(const T* row, int n, int i, float (&v)[Wide<T>::N
 }
 
 // The k largest of row[0..n), ties to the lower index, in order, handed to put(rank, value, index).  k <= n, k <= TPR.
-// Every thread kept the maxima of kGroups groups of its values while it read the row.  The k-th largest of the threads' maxima
-// is no larger than the k-th largest value, so only groups that reach it are read again: about k of them.
+// Every thread kept the maxima of kGroups groups of its values while it read the row.  The k-th largest of 64 lanes' maxima is no larger
+// than the k-th largest value, so only groups that reach it are read again: about k of them.
 template <typename T, int NW, typename Put>
 __device__ inline void top_values(Shared<T, NW, true>& sh, int slot, const T* row, int n, int iters, int per_group, int k, int tid,
                                   Put put) {
   constexpr int N = Wide<T>::N, TPR = 64 * NW;
   const int lane = tid & 63, wave = slot * NW + tid / 64;   // (tid counts from the row's first thread)
-  float mine = sh.thread_max[slot][tid];
-  int rank = 0;
-  for (int i = 0; i < TPR; ++i) {
-    const float o = sh.thread_max[slot][i];
-    rank += (o > mine || (o == mine && i < tid)) ? 1 : 0;
-  }
-  if (rank == k - 1) sh.tau[slot] = mine;
   if (tid == 0) sh.count[slot] = 0;
+  float mine = sh.thread_max[slot][lane];   // of the lane's threads in all waves: 64 maxima bound the k-th value about as well as 256
+#pragma unroll
+  for (int w = 1; w < NW; ++w) mine = fmaxf(mine, sh.thread_max[slot][64 * w + lane]);
   row_sync<NW>();
-  const float tau = sh.tau[slot];
+  if (tid < 64) sh.thread_max[slot][lane] = mine;
+  row_sync<NW>();
+  int larger = 0;
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    const float4 o = *reinterpret_cast<const float4*>(&sh.thread_max[slot][i]);
+    larger += (o.x > mine ? 1 : 0) + (o.y > mine ? 1 : 0) + (o.z > mine ? 1 : 0) + (o.w > mine ? 1 : 0);
+  }
+  const float tau = -wave_max_f(larger < k ? -mine : -__builtin_inff());   // the smallest of those that fewer than k exceed: the k-th
   float v[N];
   auto collect = [&](bool ties) {
     for (int g = 0; g * per_group < iters; ++g) {
@@ -263,7 +278,7 @@ struct Parts {
   int len;       // values of a part
 };
 
-template <typename T, int NW, bool TOP>
+template <typename T, int NW, bool TOP, bool ENT>
 __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Parts w) {
   constexpr int N = Wide<T>::N, TPR = 64 * NW, RPB = 4 / NW;
   __shared__ Shared<T, NW, TOP> sh;
@@ -280,49 +295,67 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Part
     const int rowi = live ? (int)r64 : a.rows - 1;   // (a wave behind the last row repeats it and writes nothing)
     const T* row = reinterpret_cast<const T*>(a.logits) + (long long)rowi * a.ldz + begin;
     const float inf = __builtin_inff();
-    float M = -inf, lim = -inf, c = 0.f, s = 0.f, t = 0.f, gm = -inf;
-    int in_group = 0, g = 0;
+    float M = -inf, lim = -inf, c = 0.f, s = 0.f, t = 0.f;
     float v[N];
-    auto take = [&]() {
-      float cm = v[0];
-#pragma unroll
-      for (int j = 1; j < N; ++j) cm = fmaxf(cm, v[j]);
+    // one 16-byte piece
+    auto take = [&](const float (&v)[N]) __attribute__((always_inline)) {
+      const float cm = max_of<N>(v, -inf);
       if (cm > lim) {
         const float cn = finite(cm * kLog2e);
         if (s != 0.f) {
           const float delta = fmaxf(c - cn, -1e4f), r = exp2_fast(delta);
-          t = r * fmaf(s, delta, t);
+          if (ENT) t = r * fmaf(s, delta, t);
           s *= r;
         }
         c = cn;
         lim = cm + 0.6875f;   // the reference follows when it is a factor of two behind
       }
-      M = fmaxf(M, cm);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float d = fmaf(v[j], kLog2e, -c), e = exp2_fast(d);
         s += e;
-        t = fmaf(e, fmaxf(d, -1e30f), t);   // (0 * -inf would be NaN)
+        if (ENT) t = fmaf(e, fmaxf(d, -1e30f), t);   // (0 * -inf would be NaN)
       }
-      if (TOP) {
-        gm = fmaxf(gm, cm);
-        if (++in_group == per_group) {
-          sh.group_max[slot][g++][tid] = gm;
-          gm = -inf;
-          in_group = 0;
+      return cm;
+    };
+    // Four pieces on their way at a time; pieces [from, to) of the thread.
+    auto run = [&](int from, int to) __attribute__((always_inline)) {
+      constexpr int kAhead = 4;
+      float gm = -inf;
+      int it = from;
+      const int whole = n / N > tid ? (n / N - tid + TPR - 1) / TPR : 0;   // the thread's pieces that lie inside the row
+      for (; it + kAhead <= to && it + kAhead <= whole; it += kAhead) {
+        typename Wide<T>::type raw[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          raw[i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(row + ((it + i) * TPR + tid) * N);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) v[j] = (float)raw[i][j];
+          const float cm = take(v);
+          gm = max3(gm, cm, cm);
         }
       }
+      for (; it < to; ++it) {
+        const int at = (it * TPR + tid) * N;
+        if (at >= n) break;
+        load_at(row, n, at, v);
+        const float cm = take(v);
+        gm = max3(gm, cm, cm);
+      }
+      return gm;
     };
-    for (int it = 0; it < iters; ++it) {
-      const int at = (it * TPR + tid) * N;
-      if (at + N <= n)
-        load_wide(row + at, v);
-      else
-        load_part(row + at, n - at, -inf, v);
-      take();
+    if constexpr (TOP) {
+      for (int g = 0; g * per_group < iters; ++g) {
+        const float gm = clean(run(g * per_group, (g + 1) * per_group < iters ? (g + 1) * per_group : iters));
+        sh.group_max[slot][g][tid] = gm;
+        M = fmaxf(M, gm);
+      }
+      sh.thread_max[slot][tid] = M;
+    } else {
+      M = clean(run(0, iters));
     }
-    if (TOP && in_group > 0) sh.group_max[slot][g][tid] = gm;
-    if (TOP) sh.thread_max[slot][tid] = M;
     // the row's maximum, and every thread's sums relative to it
     const float own_max = M;
     M = wave_max_f(M);
@@ -336,25 +369,23 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Part
       s = t = 0.f;
       for (int it = 0; it < iters; ++it) {
         const int at = (it * TPR + tid) * N;
-        if (at + N <= n)
-          load_wide(row + at, v);
-        else
-          load_part(row + at, n - at, -inf, v);
+        if (at >= n) break;
+        load_at(row, n, at, v);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float d = (v[j] - M) * kLog2e, e = exp2_fast(d);
           s += e;
-          t = fmaf(e, fmaxf(d, -1e30f), t);
+          if (ENT) t = fmaf(e, fmaxf(d, -1e30f), t);
         }
       }
     } else if (s != 0.f) {
       // c is L times some logit, rounded: the exact product with M's is what the sums refer to from here on
       const float delta = own_max == -inf ? 0.f : fmaxf(fmaf(-M, kLog2e, c), -1e4f), r = exp2_fast(delta);
-      t = r * fmaf(s, delta, t);
+      if (ENT) t = r * fmaf(s, delta, t);
       s *= r;
     }
     s = wave_sum_f(s);
-    t = wave_sum_f(t);
+    if (ENT) t = wave_sum_f(t);
     if (NW > 1) {
       if (lane == 0) {
         sh.wave_s[wave] = s;
@@ -600,12 +631,17 @@ hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream
   const int rpb = wave_rows(a.vocab) ? 4 : 1;
   const long long blocks = ((long long)a.rows + rpb - 1) / rpb;
   const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), w.parts), block(kThreads);
+  const bool ent = a.entropy != nullptr;
   if (wave_rows(a.vocab)) {
-    if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 1, true>), grid, block, 0, stream, a, w);
-    else hipLaunchKernelGGL((logprobs_kernel<T, 1, false>), grid, block, 0, stream, a, w);
+    if (a.top > 0 && ent) hipLaunchKernelGGL((logprobs_kernel<T, 1, true, true>), grid, block, 0, stream, a, w);
+    else if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 1, true, false>), grid, block, 0, stream, a, w);
+    else if (ent) hipLaunchKernelGGL((logprobs_kernel<T, 1, false, true>), grid, block, 0, stream, a, w);
+    else hipLaunchKernelGGL((logprobs_kernel<T, 1, false, false>), grid, block, 0, stream, a, w);
   } else {
-    if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 4, true>), grid, block, 0, stream, a, w);
-    else hipLaunchKernelGGL((logprobs_kernel<T, 4, false>), grid, block, 0, stream, a, w);
+    if (a.top > 0 && ent) hipLaunchKernelGGL((logprobs_kernel<T, 4, true, true>), grid, block, 0, stream, a, w);
+    else if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 4, true, false>), grid, block, 0, stream, a, w);
+    else if (ent) hipLaunchKernelGGL((logprobs_kernel<T, 4, false, true>), grid, block, 0, stream, a, w);
+    else hipLaunchKernelGGL((logprobs_kernel<T, 4, false, false>), grid, block, 0, stream, a, w);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || w.parts == 1) return e;
