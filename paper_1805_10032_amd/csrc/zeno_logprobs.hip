@@ -329,6 +329,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Part
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
           raw[i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(row + ((it + i) * TPR + tid) * N);
+        __builtin_amdgcn_sched_barrier(0);   // (or the first one's values would be waited for before the last is sent)
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
 #pragma unroll
