@@ -436,63 +436,94 @@ class Checkpoint(NamedTuple):
     width: int
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    """A tensor of the current device (a call runs on the current stream of that device)."""
+# Small calls are bound by the host: the current device is asked for once a call, and only tensors that the caller handed over are
+# looked at.
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _elsewhere(t, name: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA/HIP tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    raise ValueError(f"{name} is on {t.device}, not on the current device")
 
 
-def _vec(t, dtype, name: str, shape):
-    """Device pointer of a contiguous tensor of the given shape, or None."""
+def _current(t, name: str) -> int:
+    """The current device's index, for the first tensor of a call; its others are compared with it."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _elsewhere(t, name)
+    dev = _device()
+    if t.get_device() != dev:
+        _elsewhere(t, name)
+    return dev
+
+
+def _vec(t, dtype, name: str, shape, dev: int):
+    """Device pointer of a contiguous tensor of the given shape on the current device, or None."""
     if t is None:
         return None
-    _here(t, name)
-    if tuple(t.shape) != tuple(shape):
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        _elsewhere(t, name)
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _dev(t, dtype, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _matrix(t, name: str, shape=None, dtype=None):
+def _matrix(t, name: str, dev: int, shape=None, dtype=None):
     """(pointer, pitch, dtype code, rows, columns) of a 2-D matrix whose rows are contiguous and do not overlap."""
-    _here(t, name)
-    if t.dtype not in DTYPE or (dtype is not None and t.dtype != dtype):
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        _elsewhere(t, name)
+    code = DTYPE.get(t.dtype)
+    if code is None or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name} must have dtype {dtype or list(DTYPE)}, got {t.dtype}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
         raise ValueError(f"{name} must be a matrix of shape {tuple(shape) if shape is not None else '(rows, columns)'}, "
-                         f"got {tuple(t.shape)}")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+                         f"got {tuple(size)}")
+    rows, cols = size
+    pitch, inner = t.stride()
+    if cols > 1 and inner != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    pitch = int(t.stride(0)) if rows > 1 else int(cols)
+    if rows <= 1:
+        pitch = cols
     if pitch < cols:
         raise ValueError(f"the rows of {name} overlap")
-    return t.data_ptr(), pitch, DTYPE[t.dtype], int(rows), int(cols)
+    return t.data_ptr(), pitch, code, rows, cols
 
 
-def _grad_rows(t, name: str, m: int, n: int):
+def _grad_rows(t, name: str, m: int, n: int, dev: int):
     """(pointer, pitch) of m rows of n float32 gradients: columns of G, or a tensor of its own."""
     if t is None:
         return None, n
-    ptr, pitch, _, _, _ = _matrix(t, name, (m, n), torch.float32)
+    ptr, pitch, _, _, _ = _matrix(t, name, dev, (m, n), torch.float32)
     return ptr, pitch
 
 
-def _kept(ckpt: Checkpoint, rows: int):
-    if not isinstance(ckpt, Checkpoint):
-        raise ValueError("a Checkpoint is needed")
-    blocks = (int(ckpt.width) + 31) // 32
-    return (_vec(ckpt.values, torch.uint8, "values", (rows, 32 * blocks)), _vec(ckpt.scales, torch.uint8, "scales", (rows, blocks)))
+def _kept(ckpt, rows: int, width: int, dev: int):
+    """Device pointers of a Checkpoint of [rows x width] activations."""
+    if not isinstance(ckpt, Checkpoint) or ckpt.width != width:
+        raise ValueError(f"a Checkpoint of {width} columns is needed")
+    blocks = (width + 31) // 32
+    return _vec(ckpt.values, torch.uint8, "values", (rows, 32 * blocks), dev), _vec(ckpt.scales, torch.uint8, "scales", (rows, blocks), dev)
 
 
-def _groups(groups, m_of):
-    """(m, device pointer) of a group offset tensor [m + 1]; None: one group."""
+def _groups(groups, dev: int):
+    """(m, device pointer) of the row offsets [m + 1] of m workers; None: one group."""
     if groups is None:
         return 1, None
     if not isinstance(groups, torch.Tensor) or groups.dim() != 1 or groups.numel() < 2:
-        raise ValueError(f"groups must hold the m + 1 row offsets of the {m_of}")
-    return int(groups.numel()) - 1, _vec(groups, torch.int32, "groups", groups.shape)
+        raise ValueError("groups must hold the m + 1 row offsets of the workers")
+    return groups.numel() - 1, _vec(groups, torch.int32, "groups", groups.shape, dev)
+
+
+def _scratch(workspace, dev: int):
+    """(pointer, bytes) of a workspace."""
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev:
+        _elsewhere(workspace, "workspace")
+    return _dev(workspace, torch.uint8, "workspace"), workspace.numel()
 
 
 def _workspace(n: int, where: str, device=None) -> torch.Tensor:
@@ -512,27 +543,31 @@ def zeno_logprobs(logits, labels=None, *, top=0, want_entropy=False, want_stats=
     tokens of the rows of logits.  Returns (logp, entropy, stats, top_index, top_logp), None where not wanted; `stats`
     [rows x 2] is what zeno_logprobs_backward takes."""
     lib = load_library()
-    ptr, pitch, code, rows, vocab = _matrix(logits, "logits")
-    top, dev, f32 = int(top), logits.device, torch.float32
-    if labels is not None and logp is None:
-        logp = torch.empty(rows, dtype=f32, device=dev)
-    if want_entropy and entropy is None:
-        entropy = torch.empty(rows, dtype=f32, device=dev)
-    if want_stats and stats is None:
-        stats = torch.empty((rows, 2), dtype=f32, device=dev)
-    if top > 0 and top_index is None:
-        top_index = torch.empty((rows, top), dtype=torch.int32, device=dev)
-    if top > 0 and top_logp is None:
-        top_logp = torch.empty((rows, top), dtype=f32, device=dev)
+    dev = _current(logits, "logits")
+    ptr, pitch, code, rows, vocab = _matrix(logits, "logits", dev)
+    top, f32, i32, new = int(top), torch.float32, torch.int32, logits.new_empty
+
+    def out(t, want, shape, dtype, name):
+        if t is not None:
+            return t, _vec(t, dtype, name, shape, dev)
+        if not want:
+            return None, None
+        t = new(shape, dtype=dtype)
+        return t, t.data_ptr()
+
+    logp, logp_p = out(logp, labels is not None, (rows,), f32, "logp")
+    entropy, entropy_p = out(entropy, want_entropy, (rows,), f32, "entropy")
+    stats, stats_p = out(stats, want_stats, (rows, 2), f32, "stats")
+    if top > 0:
+        top_index, index_p = out(top_index, True, (rows, top), i32, "top_index")
+        top_logp, top_p = out(top_logp, True, (rows, top), f32, "top_logp")
+    else:
+        top_index = top_logp = index_p = top_p = None
     if workspace is None:
-        workspace = alloc_logprobs_workspace(rows, vocab, top, dev)
-    _here(workspace, "workspace")
-    st = lib.zeno_logprobs(ptr, pitch, code, rows, vocab, _vec(labels, torch.int32, "labels", (rows,)),
-                           _vec(logp, f32, "logp", (rows,)), _vec(entropy, f32, "entropy", (rows,)),
-                           _vec(stats, f32, "stats", (rows, 2)), top,
-                           _vec(top_index, torch.int32, "top_index", (rows, top)) if top else None,
-                           _vec(top_logp, f32, "top_logp", (rows, top)) if top else None,
-                           _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+        workspace = alloc_logprobs_workspace(rows, vocab, top, logits.device)
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_logprobs(ptr, pitch, code, rows, vocab, _vec(labels, i32, "labels", (rows,), dev), logp_p, entropy_p, stats_p, top,
+                           index_p, top_p, ws, ws_bytes, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_logprobs")
     return logp, entropy, stats, top_index, top_logp
@@ -543,21 +578,22 @@ def zeno_logprobs_backward(logits, stats, *, labels=None, grad_logp=None, entrop
     """Gradient of the logits from the gradients of logp [rows], of the entropy [rows] and of top_logp [rows x top], whichever
     are given.  out=logits works in place."""
     lib = load_library()
-    ptr, pitch, code, rows, vocab = _matrix(logits, "logits")
+    dev = _current(logits, "logits")
+    ptr, pitch, code, rows, vocab = _matrix(logits, "logits", dev)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-    o_ptr, o_pitch, _, _, _ = _matrix(out, "out", (rows, vocab), logits.dtype)
-    f32 = torch.float32
-    top = 0
+        out = logits.new_empty((rows, vocab))
+    o_ptr, o_pitch, _, _, _ = _matrix(out, "out", dev, (rows, vocab), logits.dtype)
+    f32, i32, top = torch.float32, torch.int32, 0
     if grad_top is not None:
         if not isinstance(grad_top, torch.Tensor) or grad_top.dim() != 2 or grad_top.shape[1] == 0:
             raise ValueError("grad_top must have shape (rows, top)")
         top = int(grad_top.shape[1])
-    st = lib.zeno_logprobs_backward(ptr, pitch, code, rows, vocab, _vec(stats, f32, "stats", (rows, 2)),
-                                    _vec(labels, torch.int32, "labels", (rows,)), _vec(grad_logp, f32, "grad_logp", (rows,)),
-                                    _vec(entropy, f32, "entropy", (rows,)), _vec(grad_entropy, f32, "grad_entropy", (rows,)), top,
-                                    _vec(top_index, torch.int32, "top_index", (rows, top)) if top else None,
-                                    _vec(grad_top, f32, "grad_top", (rows, top)), o_ptr, o_pitch, _stream())
+    st = lib.zeno_logprobs_backward(ptr, pitch, code, rows, vocab, _vec(stats, f32, "stats", (rows, 2), dev),
+                                    _vec(labels, i32, "labels", (rows,), dev), _vec(grad_logp, f32, "grad_logp", (rows,), dev),
+                                    _vec(entropy, f32, "entropy", (rows,), dev),
+                                    _vec(grad_entropy, f32, "grad_entropy", (rows,), dev), top,
+                                    _vec(top_index, i32, "top_index", (rows, top), dev) if top else None,
+                                    _vec(grad_top, f32, "grad_top", (rows, top), dev), o_ptr, o_pitch, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_logprobs_backward")
     return out
@@ -570,15 +606,19 @@ def alloc_checkpoint(rows: int, width: int, device=None) -> Checkpoint:
                       torch.empty((int(rows), blocks), dtype=torch.uint8, device=device), int(width))
 
 
+def _new_checkpoint(x, rows: int, width: int) -> Checkpoint:
+    blocks = (width + 31) // 32
+    return Checkpoint(x.new_empty((rows, 32 * blocks), dtype=torch.uint8), x.new_empty((rows, blocks), dtype=torch.uint8), width)
+
+
 def zeno_checkpoint(x, *, out=None) -> Checkpoint:
     """The activations x [rows x width] in 8 bits."""
     lib = load_library()
-    ptr, pitch, code, rows, width = _matrix(x, "x")
+    dev = _current(x, "x")
+    ptr, pitch, code, rows, width = _matrix(x, "x", dev)
     if out is None:
-        out = alloc_checkpoint(rows, width, x.device)
-    if not isinstance(out, Checkpoint) or out.width != width:
-        raise ValueError("out must be a Checkpoint of x's width")
-    v, s = _kept(out, rows)
+        out = _new_checkpoint(x, rows, width)
+    v, s = _kept(out, rows, width, dev)
     st = lib.zeno_checkpoint(ptr, pitch, code, rows, width, v, s, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_checkpoint")
@@ -590,11 +630,12 @@ def zeno_checkpoint_values(ckpt: Checkpoint, dtype=torch.float32, *, out=None):
     lib = load_library()
     if not isinstance(ckpt, Checkpoint):
         raise ValueError("a Checkpoint is needed")
-    rows = int(ckpt.values.shape[0])
+    dev = _current(ckpt.values, "values")
+    rows, width = int(ckpt.values.shape[0]), int(ckpt.width)
     if out is None:
-        out = torch.empty((rows, ckpt.width), dtype=dtype, device=ckpt.values.device)
-    ptr, pitch, code, _, width = _matrix(out, "out", (rows, ckpt.width))
-    v, s = _kept(ckpt, rows)
+        out = ckpt.values.new_empty((rows, width), dtype=dtype)
+    ptr, pitch, code, _, _ = _matrix(out, "out", dev, (rows, width))
+    v, s = _kept(ckpt, rows, width, dev)
     st = lib.zeno_checkpoint_values(v, s, rows, width, code, ptr, pitch, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_checkpoint_values")
@@ -604,24 +645,22 @@ def zeno_checkpoint_values(ckpt: Checkpoint, dtype=torch.float32, *, out=None):
 def zeno_layer_norm(x, weight, bias=None, eps=1e-5, *, y=None, mean=None, rstd=None, want_checkpoint=False, checkpoint=None):
     """Layer norm of the rows of x; weight and bias float32 [width].  Returns (y, mean, rstd, Checkpoint of x or None)."""
     lib = load_library()
-    ptr, pitch, code, rows, width = _matrix(x, "x")
+    dev = _current(x, "x")
+    ptr, pitch, code, rows, width = _matrix(x, "x", dev)
+    f32 = torch.float32
     if y is None:
-        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-    y_ptr, y_pitch, _, _, _ = _matrix(y, "y", (rows, width), x.dtype)
+        y = x.new_empty((rows, width))
+    y_ptr, y_pitch, _, _, _ = _matrix(y, "y", dev, (rows, width), x.dtype)
     if mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+        mean = x.new_empty((rows,), dtype=f32)
     if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        rstd = x.new_empty((rows,), dtype=f32)
     if want_checkpoint and checkpoint is None:
-        checkpoint = alloc_checkpoint(rows, width, x.device)
-    v = s = None
-    if checkpoint is not None:
-        if not isinstance(checkpoint, Checkpoint) or checkpoint.width != width:
-            raise ValueError("checkpoint must be a Checkpoint of x's width")
-        v, s = _kept(checkpoint, rows)
-    st = lib.zeno_layer_norm(ptr, pitch, code, rows, width, _vec(weight, torch.float32, "weight", (width,)),
-                             _vec(bias, torch.float32, "bias", (width,)), float(eps), y_ptr, y_pitch,
-                             _vec(mean, torch.float32, "mean", (rows,)), _vec(rstd, torch.float32, "rstd", (rows,)), v, s, _stream())
+        checkpoint = _new_checkpoint(x, rows, width)
+    v, s = (None, None) if checkpoint is None else _kept(checkpoint, rows, width, dev)
+    st = lib.zeno_layer_norm(ptr, pitch, code, rows, width, _vec(weight, f32, "weight", (width,), dev), _vec(bias, f32, "bias", (width,), dev),
+                             float(eps), y_ptr, y_pitch, _vec(mean, f32, "mean", (rows,), dev), _vec(rstd, f32, "rstd", (rows,), dev), v, s,
+                             _stream())
     if st != 0:
         raise ZenoError(st, "zeno_layer_norm")
     return y, mean, rstd, checkpoint
@@ -638,35 +677,33 @@ def zeno_layer_norm_backward(dy, x, mean, rstd, weight, *, groups=None, want_dx=
     workers (None: one group).  dweight and dbias are [m x width] float32, for instance column slices of G.  dx=dy works in
     place; rows that belong to no group keep what dx held (zeros if dx is not given).  Returns (dx, dweight, dbias)."""
     lib = load_library()
-    ptr, pitch, code, rows, width = _matrix(dy, "dy")
-    m, offsets = _groups(groups, "workers")
-    kept = isinstance(x, Checkpoint)
+    dev = _current(dy, "dy")
+    ptr, pitch, code, rows, width = _matrix(dy, "dy", dev)
+    f32 = torch.float32
+    m, offsets = _groups(groups, dev)
     v = s = x_ptr = None
     x_pitch = width
-    if kept:
-        if x.width != width:
-            raise ValueError("the checkpoint's width is not dy's")
-        v, s = _kept(x, rows)
+    if isinstance(x, Checkpoint):
+        v, s = _kept(x, rows, width, dev)
     else:
-        x_ptr, x_pitch, _, _, _ = _matrix(x, "x", (rows, width), dy.dtype)
+        x_ptr, x_pitch, _, _, _ = _matrix(x, "x", dev, (rows, width), dy.dtype)
     if want_dx and dx is None:
-        dx = (torch.empty if groups is None else torch.zeros)((rows, width), dtype=dy.dtype, device=dy.device)
+        dx = dy.new_empty((rows, width)) if groups is None else dy.new_zeros((rows, width))
     if want_weight and dweight is None:
-        dweight = torch.empty((m, width), dtype=torch.float32, device=dy.device)
+        dweight = dy.new_empty((m, width), dtype=f32)
     if want_bias and dbias is None:
-        dbias = torch.empty((m, width), dtype=torch.float32, device=dy.device)
+        dbias = dy.new_empty((m, width), dtype=f32)
     d_ptr, d_pitch = None, width
     if dx is not None:
-        d_ptr, d_pitch, _, _, _ = _matrix(dx, "dx", (rows, width), dy.dtype)
-    w_ptr, ldw = _grad_rows(dweight, "dweight", m, width)
-    b_ptr, ldb = _grad_rows(dbias, "dbias", m, width)
+        d_ptr, d_pitch, _, _, _ = _matrix(dx, "dx", dev, (rows, width), dy.dtype)
+    w_ptr, ldw = _grad_rows(dweight, "dweight", m, width, dev)
+    b_ptr, ldb = _grad_rows(dbias, "dbias", m, width, dev)
     if workspace is None:
         workspace = alloc_layer_norm_workspace(rows, width, m, dy.device)
-    _here(workspace, "workspace")
-    st = lib.zeno_layer_norm_backward(ptr, pitch, code, rows, width, x_ptr, x_pitch, v, s,
-                                      _vec(mean, torch.float32, "mean", (rows,)), _vec(rstd, torch.float32, "rstd", (rows,)),
-                                      _vec(weight, torch.float32, "weight", (width,)), m, offsets, d_ptr, d_pitch, w_ptr, ldw, b_ptr,
-                                      ldb, _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_layer_norm_backward(ptr, pitch, code, rows, width, x_ptr, x_pitch, v, s, _vec(mean, f32, "mean", (rows,), dev),
+                                      _vec(rstd, f32, "rstd", (rows,), dev), _vec(weight, f32, "weight", (width,), dev), m, offsets, d_ptr,
+                                      d_pitch, w_ptr, ldw, b_ptr, ldb, ws, ws_bytes, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_layer_norm_backward")
     return dx, dweight, dbias
@@ -681,21 +718,23 @@ def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, d
     """Gradient of a linear layer's weights (and bias) for each of the m workers, from dy [rows x out] and a Checkpoint of the
     layer's input.  dweight [m x out * width] and dbias [m x out] are float32, for instance column slices of G."""
     lib = load_library()
-    ptr, pitch, code, rows, out = _matrix(dy, "dy")
-    m, offsets = _groups(groups, "workers")
-    v, s = _kept(ckpt, rows)
+    dev = _current(dy, "dy")
+    ptr, pitch, code, rows, out = _matrix(dy, "dy", dev)
+    m, offsets = _groups(groups, dev)
+    if not isinstance(ckpt, Checkpoint):
+        raise ValueError("a Checkpoint is needed")
     width = int(ckpt.width)
+    v, s = _kept(ckpt, rows, width, dev)
     if dweight is None:
-        dweight = torch.empty((m, out * width), dtype=torch.float32, device=dy.device)
+        dweight = dy.new_empty((m, out * width), dtype=torch.float32)
     if want_bias and dbias is None:
-        dbias = torch.empty((m, out), dtype=torch.float32, device=dy.device)
-    w_ptr, ldw = _grad_rows(dweight, "dweight", m, out * width)
-    b_ptr, ldb = _grad_rows(dbias, "dbias", m, out)
+        dbias = dy.new_empty((m, out), dtype=torch.float32)
+    w_ptr, ldw = _grad_rows(dweight, "dweight", m, out * width, dev)
+    b_ptr, ldb = _grad_rows(dbias, "dbias", m, out, dev)
     if workspace is None:
         workspace = alloc_weight_gradient_workspace(rows, out, width, m, dy.device)
-    _here(workspace, "workspace")
-    st = lib.zeno_weight_gradient(ptr, pitch, code, rows, out, v, s, width, m, offsets, w_ptr, ldw, b_ptr, ldb,
-                                  _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream())
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_weight_gradient(ptr, pitch, code, rows, out, v, s, width, m, offsets, w_ptr, ldw, b_ptr, ldb, ws, ws_bytes, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_weight_gradient")
     return dweight, dbias
@@ -710,22 +749,21 @@ def zeno_score_logprobs(G, logp_x, logp, rho, *, labels=None, scores=None, works
     """scores[i] = mean_t (logp[i][t] - logp_x[t]) - rho ||G[i]||^2  (Definition 2 for the mean of -log p); tokens with
     label -1 do not count."""
     lib = load_library()
-    _here(G, "G")
+    dev = _current(G, "G")
     g_ptr, ldg = _rows(G)
-    m, d = int(G.shape[0]), int(G.shape[1])
+    m, d = G.shape
     if not isinstance(logp_x, torch.Tensor) or logp_x.dim() != 1:
         raise ValueError("logp_x must be a vector")
-    n = int(logp_x.numel())
-    p_ptr, ldp, _, _, _ = _matrix(logp, "logp", (m, n), torch.float32)
+    n, f32 = int(logp_x.numel()), torch.float32
+    p_ptr, ldp, _, _, _ = _matrix(logp, "logp", dev, (m, n), f32)
     if scores is None:
-        scores = torch.empty(m, dtype=torch.float32, device=G.device)
+        scores = G.new_empty((m,))
     if workspace is None:
         workspace = alloc_score_logprobs_workspace(m, d, G.device)
-    _here(workspace, "workspace")
-    st = lib.zeno_score_logprobs(g_ptr, ldg, m, d, _vec(logp_x, torch.float32, "logp_x", (n,)), p_ptr, ldp, n,
-                                 _vec(labels, torch.int32, "labels", (n,)), float(rho),
-                                 _vec(scores, torch.float32, "scores", (m,)), _dev(workspace, torch.uint8, "workspace"),
-                                 workspace.numel(), _stream())
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_score_logprobs(g_ptr, ldg, m, d, _vec(logp_x, f32, "logp_x", (n,), dev), p_ptr, ldp, n,
+                                 _vec(labels, torch.int32, "labels", (n,), dev), float(rho), _vec(scores, f32, "scores", (m,), dev), ws,
+                                 ws_bytes, _stream())
     if st != 0:
         raise ZenoError(st, "zeno_score_logprobs")
     return scores

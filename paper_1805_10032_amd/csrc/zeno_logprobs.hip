@@ -7,13 +7,14 @@
 
 #include <float.h>
 
+#include <algorithm>
+
 namespace zeno {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256;
-constexpr int kGroups = 16;        // maxima that a thread keeps of its share of a row, for the search of the top values
 constexpr int kCandidates = 512;   // top values are chosen from at most so many
 constexpr int kMaxParts = 64;      // workgroups that share a row
 
@@ -79,20 +80,25 @@ __device__ inline void finish_row(const LogprobsArgs& a, int row, RowSums r, flo
   *log_s_out = log_s;
 }
 
-// NW waves for a row (or a part of it); 4 / NW rows a workgroup.
+// NW waves for a row (or a part of it): a workgroup is four rows of one wave each, or one row of four or sixteen.
+template <int NW>
+struct Shape {
+  static constexpr int TPR = 64 * NW, ROWS = NW == 1 ? 4 : 1, THREADS = TPR * ROWS, WAVES = THREADS / 64;
+  // maxima that a thread keeps of its share of the row, for the search of the top values
+  static constexpr int GROUPS = NW == 16 ? 4 : 16;
+};
 template <typename T, int NW, bool TOP>
 struct Shared {
-  static constexpr int TPR = 64 * NW;
-  float wave_max[4], wave_s[4], wave_t[4];
-  float log_s[4 / NW], M[4 / NW];
-  int empty[4 / NW];
-  float group_max[TOP ? 4 / NW : 1][TOP ? kGroups : 1][TOP ? TPR : 1];
-  __align__(16) float thread_max[TOP ? 4 / NW : 1][TOP ? TPR : 4];
-  int count[4 / NW], more[4 / NW], ties[4];
-  float cand_val[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
-  int cand_idx[TOP ? 4 / NW : 1][TOP ? kCandidates : 1];
-  float best_val[4];
-  int best_idx[4];
+  static constexpr int TPR = 64 * NW, ROWS = Shape<NW>::ROWS, WAVES = Shape<NW>::WAVES, GROUPS = Shape<NW>::GROUPS;
+  float wave_max[WAVES], wave_s[WAVES], wave_t[WAVES];
+  float log_s[ROWS];
+  float group_max[TOP ? ROWS : 1][TOP ? GROUPS : 1][TOP ? TPR : 1];
+  __align__(16) float thread_max[TOP ? ROWS : 1][TOP ? TPR : 4];
+  int count[ROWS], ties[WAVES];
+  float cand_val[TOP ? ROWS : 1][TOP ? kCandidates : 1];
+  int cand_idx[TOP ? ROWS : 1][TOP ? kCandidates : 1];
+  float best_val[WAVES];
+  int best_idx[WAVES];
 };
 
 template <typename T>
@@ -279,15 +285,15 @@ struct Parts {
 };
 
 template <typename T, int NW, bool TOP, bool ENT>
-__global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Parts w) {
-  constexpr int N = Wide<T>::N, TPR = 64 * NW, RPB = 4 / NW;
+__global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsArgs a, Parts w) {
+  constexpr int N = Wide<T>::N, TPR = 64 * NW, RPB = Shape<NW>::ROWS;
   __shared__ Shared<T, NW, TOP> sh;
   const int slot = threadIdx.x / TPR, tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   const int part = blockIdx.y;
   const int begin = part * w.len;
   const int n = a.vocab - begin < w.len ? a.vocab - begin : w.len;
   const int iters = (n + TPR * N - 1) / (TPR * N);
-  const int per_group = (iters + kGroups - 1) / kGroups;
+  const int per_group = (iters + Shape<NW>::GROUPS - 1) / Shape<NW>::GROUPS;
   const long long blocks = ((long long)a.rows + RPB - 1) / RPB;
   for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
     const long long r64 = b * RPB + slot;
@@ -431,8 +437,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Part
         top_values<T, NW>(sh, slot, row, n, iters, per_group, a.top, tid, [&](int rank, float val, int idx) {
           if (!live) return;
           a.top_index[(long long)rowi * a.top + rank] = idx;
-          const float z = (float)row[idx];   // (a NaN stays one)
-          a.top_logp[(long long)rowi * a.top + rank] = log_prob(z, M, log_s, empty);
+          a.top_logp[(long long)rowi * a.top + rank] = log_prob(val, M, log_s, empty);   // (next to a NaN or +inf, log_s is NaN)
         });
       }
     }
@@ -440,48 +445,48 @@ __global__ __launch_bounds__(kThreads) void logprobs_kernel(LogprobsArgs a, Part
   }
 }
 
-// Joins the parts of a row: one workgroup of one wave a row.
+// Joins the parts of a row: one workgroup of one wave a row.  What does not depend on each other is read at once.
 template <typename T>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts w) {
-  __shared__ float cand_val[kMaxParts * 32];
+  __shared__ __align__(16) float cand_val[kMaxParts * 32];
   __shared__ int cand_idx[kMaxParts * 32];
   __shared__ int count;
-  __shared__ float tau_sh;
   const int lane = threadIdx.x;
+  const float inf = __builtin_inff();
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    RowSums r = {-__builtin_inff(), 0.f, 0.f};
+    const int k = a.top, all = w.parts * k;
     const long long p = row * w.parts + lane;
-    if (lane < w.parts) r = {w.sums[3 * p], w.sums[3 * p + 1], w.sums[3 * p + 2]};
+    RowSums r = {-inf, 0.f, 0.f};
+    float head = -inf, first_val = 0.f;
+    int first_idx = -1;
+    if (lane < w.parts) {
+      r = {w.sums[3 * p], w.sums[3 * p + 1], w.sums[3 * p + 2]};
+      if (k > 0) head = w.val[p * k];   // (every part has a first value)
+    }
+    if (lane < all) {
+      first_val = w.val[row * all + lane];
+      first_idx = w.idx[row * all + lane];
+    }
+    if (lane == 0) count = 0;
     move_to(r, wave_max_f(r.M));
     r.s = wave_sum_f(r.s);
     r.t = wave_sum_f(r.t);
     float log_s = 0.f;
     if (lane == 0) finish_row<T>(a, (int)row, r, &log_s);
-    log_s = __shfl(log_s, 0, 64);
-    if (r.M == __builtin_inff()) r.s = __builtin_nanf("");
-    const int k = a.top;
+    log_s = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(log_s)));
+    if (r.M == inf) r.s = __builtin_nanf("");
     if (k > 0) {
       const bool empty = is_empty(r.M, r.s);
       // the k-th largest of the parts' largest values bounds the k-th largest from below
-      float head = lane < w.parts ? w.val[p * k] : -__builtin_inff();   // (every part has a first value)
-      if (lane == 0) {
-        count = 0;
-        tau_sh = -__builtin_inff();
-      }
+      int larger = 0;
+      for (int i = 0; i < w.parts; ++i) larger += __shfl(head, i, 64) > head ? 1 : 0;
+      float tau = -inf;
+      if (w.parts >= k) tau = -wave_max_f(lane < w.parts && larger < k ? -head : -inf);
       row_sync<1>();
-      int rank = 0;
-      for (int i = 0; i < w.parts; ++i) {
-        const float o = __shfl(head, i, 64);
-        rank += (o > head || (o == head && i < lane)) ? 1 : 0;
-      }
-      if (lane < w.parts && rank == k - 1) tau_sh = head;
-      row_sync<1>();
-      const float tau = tau_sh;
-      for (int i = lane; i < w.parts * k; i += 64) {
-        const int idx = w.idx[row * w.parts * k + i];
-        if (idx < 0) continue;
-        const float val = w.val[row * w.parts * k + i];
-        if (val >= tau) {
+      for (int i = lane; i < all; i += 64) {
+        const float val = i < 64 ? first_val : w.val[row * all + i];
+        const int idx = i < 64 ? first_idx : w.idx[row * all + i];
+        if (idx >= 0 && val >= tau) {
           const int pos = atomicAdd(&count, 1);
           cand_val[pos] = val;
           cand_idx[pos] = idx;
@@ -499,8 +504,7 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts
         }
         if (better < k) {
           a.top_index[row * k + better] = ci;
-          const float z = (float)reinterpret_cast<const T*>(a.logits)[row * a.ldz + ci];
-          a.top_logp[row * k + better] = log_prob(z, r.M, log_s, empty);
+          a.top_logp[row * k + better] = log_prob(c, r.M, log_s, empty);
         }
       }
       row_sync<1>();
@@ -598,22 +602,24 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
   }
 }
 
-// Rows of up to 2048 values take one wave, longer ones a workgroup of four.
+// Rows of up to 2048 values take one wave; longer ones four, and sixteen where there are too few rows to fill the chip with four
+// (bf16, eight alternatives, us with sixteen waves / with four, which share a row of more than 8192 values between them: 1 x 32000
+// 12.4 / 17.0, 256 x 32000 14.3 / 19.0, 400 x 50257 29.4 / 29.8).
 bool wave_rows(int vocab) { return vocab <= 2048; }
+bool few_rows(int rows) { return rows < 512; }
 
-// Workgroups that share a row: where the rows alone do not fill the chip.
+// Workgroups that share a row, at most one for each compute unit in all.  The join costs a launch, which rows of up to 65536 values do
+// not bring in again (shared / whole: 1 x 65536 15.8 / 15.7, 1 x 131072 16.1 / 21.7, 64 x 131072 21.1 / 24.0).
 int row_parts(int rows, int vocab) {
-  if (wave_rows(vocab) || rows >= 512) return 1;
-  long long parts = (1024 + rows - 1) / rows;
-  const long long most = (vocab + 4095) / 4096;
-  if (parts > most) parts = most;
-  return (int)(parts < kMaxParts ? parts : kMaxParts);
+  if (vocab <= 65536 || rows > 128 || rows < 1) return 1;
+  const int parts = 256 / rows, most = vocab / 8192;
+  return std::min(std::min(parts, most), kMaxParts);
 }
 
 Parts parts_for(int rows, int vocab, int top, void* workspace) {
   Parts w;
   w.parts = row_parts(rows, vocab);
-  const long long unit = kThreads * 8;   // whole 16-byte loads in every part, whatever the type
+  const long long unit = 1024 * 8;   // whole 16-byte loads in every part, whatever the type
   w.len = (int)(((vocab + w.parts - 1LL) / w.parts + unit - 1) / unit * unit);
   if (w.parts == 1) w.len = vocab;
   w.parts = w.parts == 1 ? 1 : (int)((vocab + (long long)w.len - 1) / w.len);   // (none of them empty)
@@ -627,23 +633,24 @@ Parts parts_for(int rows, int vocab, int top, void* workspace) {
   return w;
 }
 
+template <typename T, int NW>
+void start(const LogprobsArgs& a, const Parts& w, dim3 grid, hipStream_t stream) {
+  const dim3 block(Shape<NW>::THREADS);
+  const bool ent = a.entropy != nullptr;
+  if (a.top > 0 && ent) hipLaunchKernelGGL((logprobs_kernel<T, NW, true, true>), grid, block, 0, stream, a, w);
+  else if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, NW, true, false>), grid, block, 0, stream, a, w);
+  else if (ent) hipLaunchKernelGGL((logprobs_kernel<T, NW, false, true>), grid, block, 0, stream, a, w);
+  else hipLaunchKernelGGL((logprobs_kernel<T, NW, false, false>), grid, block, 0, stream, a, w);
+}
+
 template <typename T>
 hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream) {
-  const int rpb = wave_rows(a.vocab) ? 4 : 1;
+  const int rpb = wave_rows(a.vocab) ? Shape<1>::ROWS : 1;
   const long long blocks = ((long long)a.rows + rpb - 1) / rpb;
-  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), w.parts), block(kThreads);
-  const bool ent = a.entropy != nullptr;
-  if (wave_rows(a.vocab)) {
-    if (a.top > 0 && ent) hipLaunchKernelGGL((logprobs_kernel<T, 1, true, true>), grid, block, 0, stream, a, w);
-    else if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 1, true, false>), grid, block, 0, stream, a, w);
-    else if (ent) hipLaunchKernelGGL((logprobs_kernel<T, 1, false, true>), grid, block, 0, stream, a, w);
-    else hipLaunchKernelGGL((logprobs_kernel<T, 1, false, false>), grid, block, 0, stream, a, w);
-  } else {
-    if (a.top > 0 && ent) hipLaunchKernelGGL((logprobs_kernel<T, 4, true, true>), grid, block, 0, stream, a, w);
-    else if (a.top > 0) hipLaunchKernelGGL((logprobs_kernel<T, 4, true, false>), grid, block, 0, stream, a, w);
-    else if (ent) hipLaunchKernelGGL((logprobs_kernel<T, 4, false, true>), grid, block, 0, stream, a, w);
-    else hipLaunchKernelGGL((logprobs_kernel<T, 4, false, false>), grid, block, 0, stream, a, w);
-  }
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), w.parts);
+  if (wave_rows(a.vocab)) start<T, 1>(a, w, grid, stream);
+  else if (few_rows(a.rows)) start<T, 16>(a, w, grid, stream);
+  else start<T, 4>(a, w, grid, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || w.parts == 1) return e;
   hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3(a.rows), dim3(64), 0, stream, a, w);

@@ -100,7 +100,8 @@ def test_workspace_queries(B):
         assert lib.zeno_weight_gradient_workspace_bytes(*args) == 0
     for args in ((0, 5), (1025, 5), (4, 0)):
         assert lib.zeno_score_logprobs_workspace_bytes(*args) == 0
-    for n in (lib.zeno_logprobs_workspace_bytes(0, 1, 0), lib.zeno_logprobs_workspace_bytes(3, 100000, 32),
+    for n in (lib.zeno_logprobs_workspace_bytes(0, 1, 0), lib.zeno_logprobs_workspace_bytes(0, 200000, 8),
+              lib.zeno_logprobs_workspace_bytes(3, 100000, 32),
               lib.zeno_layer_norm_workspace_bytes(0, 1, 1), lib.zeno_layer_norm_workspace_bytes(100, 77, 1024),
               lib.zeno_weight_gradient_workspace_bytes(0, 1, 1, 1), lib.zeno_weight_gradient_workspace_bytes(100000, 10, 10, 3),
               lib.zeno_score_logprobs_workspace_bytes(1, 1), lib.zeno_score_logprobs_workspace_bytes(1024, 1 << 33)):
