@@ -51,17 +51,34 @@ __device__ inline Span piece_of(const WeightGradArgs& a, int g, int piece, int p
   return s;
 }
 
-// v as the sum of P bf16 pieces.
+// Eight values as sums of P bf16 pieces, each the leading eight bits of what the pieces before it leave: two take fp16's 11 bits and three
+// float32's 24, nothing is rounded, and no finite value becomes infinite.
 template <int P>
-__device__ inline void split(float v, __bf16 (&piece)[P]) {
-  const bool fin = fabsf(v) < __builtin_inff();
-  // (a float above bf16's range leaves its rest to the second piece instead of rounding to infinity)
-  piece[0] = (__bf16)(P > 1 && fin ? fminf(fmaxf(v, -3.38953139e38f), 3.38953139e38f) : v);
-  float rest = v;
+__device__ inline void split(const float (&v)[8], uint4 (&piece)[P]) {
+  float rest[8], largest = 0.f;
 #pragma unroll
-  for (int i = 1; i < P; ++i) {
-    rest = fin ? rest - (float)piece[i - 1] : 0.f;
-    piece[i] = (__bf16)rest;
+  for (int j = 0; j < 8; ++j) {
+    rest[j] = v[j];
+    largest = fmaxf(largest, fabsf(v[j]));
+  }
+  const bool finite = largest < __builtin_inff();   // (a NaN hides from it and stays one: what it leaves is NaN)
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    unsigned bits[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bits[j] = __float_as_uint(rest[j]);
+    // the upper halves of two words
+    piece[p] = make_uint4(__builtin_amdgcn_perm(bits[1], bits[0], 0x07060302), __builtin_amdgcn_perm(bits[3], bits[2], 0x07060302),
+                          __builtin_amdgcn_perm(bits[5], bits[4], 0x07060302), __builtin_amdgcn_perm(bits[7], bits[6], 0x07060302));
+    if (p + 1 < P) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rest[j] -= __uint_as_float(bits[j] & 0xffff0000u);
+      if (!finite) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (fabsf(v[j]) == __builtin_inff()) rest[j] = 0.f;   // (infinity less itself is NaN)
+      }
+    }
   }
 }
 
@@ -106,40 +123,39 @@ __device__ inline Source<T, S> source_of(const WeightGradArgs& a, int first, int
   return s;
 }
 
-// One stage in CO + CI pieces, the last of which moves on.  WHOLE: all its tokens belong to the span; otherwise `left` of them do, and
-// those behind them come as copies of the last: deposit_piece() puts zeros in the place of their dy, and the product with the last
-// token's activations is then NaN only where that token has made it NaN already.
+// One stage in CO + CI pieces, the last of which moves on by `advance` tokens.  The last stage of a span ends where the span ends and
+// begins among tokens that the stage before has had already: deposit_piece() puts zeros in the place of their dy (their activations are
+// finite or have made the sums NaN already), and no load needs a test.  WHOLE: the span holds a stage; otherwise the stage begins at
+// token `base` < 0, and what lies before the span's first token comes as copies of it.
 template <typename T, typename S, bool WHOLE>
-__device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid,
+__device__ inline void fetch_piece(int piece, const WeightGradArgs& a, Source<T, S>& s, int base, int advance, int blocks, int tid,
                                    Fetched<T, S>& f) {
   constexpr int N = Wide<T>::N, PO = S::OUT / 8, PI = S::IN / 16, RO = kThreads / PO, RI = kThreads / PI;
-  // tokens that a row is moved back by
-  auto back = [&](int token) { return WHOLE || token < left ? 0 : token - left + 1; };
   if (piece < S::CO) {
-    const int h = piece;
+    const int h = piece, token = tid / PO + RO * h;
     if (S::CHUNKS_O >= kThreads || tid < S::CHUNKS_O) {
-      const T* p = s.dy + (long long)(RO * h - back(tid / PO + RO * h)) * a.lddy;
+      const T* p = s.dy + (long long)(WHOLE ? RO * h : (base + token > 0 ? base + token : 0) - tid / PO) * a.lddy;
 #pragma unroll
       for (int i = 0; i < 8 / N; ++i) f.dy[h][i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * N);
     }
   } else if (piece < S::CO + S::CI) {
-    const int h = piece - S::CO;
+    const int h = piece - S::CO, token = tid / PI + RI * h;
     if (S::CHUNKS_I >= kThreads || tid < S::CHUNKS_I) {
-      const long long row = RI * h - back(tid / PI + RI * h);
+      const long long row = WHOLE ? RI * h : (base + token > 0 ? base + token : 0) - tid / PI;
       f.a[h] = *reinterpret_cast<const uint4*>(s.values + row * (blocks * kCkptBlock));
       f.scale[h] = s.scales[row * blocks];
     }
   }
-  if (piece == S::CO + S::CI - 1) {
-    s.dy += (long long)S::KT * a.lddy;
-    s.values += (long long)S::KT * (blocks * kCkptBlock);
-    s.scales += (long long)S::KT * blocks;
+  if (WHOLE && piece == S::CO + S::CI - 1) {
+    s.dy += (long long)advance * a.lddy;
+    s.values += (long long)advance * (blocks * kCkptBlock);
+    s.scales += (long long)advance * blocks;
   }
 }
-template <typename T, typename S>
-__device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int left, int blocks, int tid, Fetched<T, S>& f) {
+template <typename T, typename S, bool WHOLE>
+__device__ inline void fetch(const WeightGradArgs& a, Source<T, S>& s, int base, int advance, int blocks, int tid, Fetched<T, S>& f) {
 #pragma unroll
-  for (int piece = 0; piece < S::CO + S::CI; ++piece) fetch_piece<T, S, false>(piece, a, s, left, blocks, tid, f);
+  for (int piece = 0; piece < S::CO + S::CI; ++piece) fetch_piece<T, S, WHOLE>(piece, a, s, base, advance, blocks, tid, f);
 }
 
 __device__ inline bf16x8 widen8(unsigned x, unsigned y, float s) {
@@ -155,17 +171,17 @@ struct Stage {
 };
 
 // Piece h < CO: eight outputs' dy of one token into LDS as bf16, and into the sums of the bias where the workgroup has these to take;
-// piece CO + h: sixteen activations.
+// piece CO + h: sixteen activations.  The stage's first `skip` tokens do not count.
 template <typename T, typename S, bool WHOLE>
-__device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>& st, int left, int shift, int tid, bool sums,
+__device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>& st, int skip, int shift, int tid, bool sums,
                                      float (&bias)[8]) {
   constexpr int N = Wide<T>::N, P = S::P;
   if (piece < S::CO) {
     if (S::CHUNKS_O < kThreads && tid >= S::CHUNKS_O) return;
     constexpr int PER = S::OUT / 8;
     const int h = piece, token = tid / PER + kThreads / PER * h;
-    const bool live = WHOLE || token < left;
-    bf16x8 plane[P];
+    const bool live = WHOLE || token >= skip;
+    uint4 plane[P];
     if constexpr (P == 1) {
       static_assert(P > 1 || sizeof(T) == 2, "one piece is dy itself");
       uint4 raw = __builtin_bit_cast(uint4, f.dy[h][0]);
@@ -176,11 +192,11 @@ __device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>
           raw = make_uint4(__builtin_amdgcn_alignbit(raw.y, raw.x, 16), __builtin_amdgcn_alignbit(raw.z, raw.y, 16),
                            __builtin_amdgcn_alignbit(raw.w, raw.z, 16), raw.w >> 16);
       }
-      if (!live) raw = make_uint4(0, 0, 0, 0);
-      plane[0] = __builtin_bit_cast(bf16x8, raw);
+      plane[0] = make_uint4(live ? raw.x : 0, live ? raw.y : 0, live ? raw.z : 0, live ? raw.w : 0);
       if (sums) {
+        const bf16x8 v = __builtin_bit_cast(bf16x8, plane[0]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bias[j] += (float)plane[0][j];
+        for (int j = 0; j < 8; ++j) bias[j] += (float)v[j];
       }
     } else {
       float v[8];
@@ -198,14 +214,11 @@ __device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>
       for (int j = 0; j < 8; ++j) {
         if (!live) v[j] = 0.f;
         if (sums) bias[j] += v[j];
-        __bf16 p[P];
-        split<P>(v[j], p);
-#pragma unroll
-        for (int i = 0; i < P; ++i) plane[i][j] = p[i];
       }
+      split<P>(v, plane);
     }
 #pragma unroll
-    for (int i = 0; i < P; ++i) *reinterpret_cast<bf16x8*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
+    for (int i = 0; i < P; ++i) *reinterpret_cast<uint4*>(&st.y[i][token * S::PITCH_O + 8 * (tid % PER)]) = plane[i];
   } else if (piece < S::CO + S::CI) {
     if (S::CHUNKS_I < kThreads && tid >= S::CHUNKS_I) return;
     constexpr int PER = S::IN / 16;
@@ -217,10 +230,9 @@ __device__ inline void deposit_piece(int piece, const Fetched<T, S>& f, Stage<S>
   }
 }
 template <typename T, typename S>
-__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int left, int shift, int tid, bool sums,
-                               float (&bias)[8]) {
+__device__ inline void deposit(const Fetched<T, S>& f, Stage<S>& st, int skip, int shift, int tid, bool sums, float (&bias)[8]) {
 #pragma unroll
-  for (int piece = 0; piece < S::CO + S::CI; ++piece) deposit_piece<T, S, false>(piece, f, st, left, shift, tid, sums, bias);
+  for (int piece = 0; piece < S::CO + S::CI; ++piece) deposit_piece<T, S, false>(piece, f, st, skip, shift, tid, sums, bias);
 }
 
 // The operands of 16 tokens.
@@ -279,41 +291,49 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   const int n = span.end - span.begin, stages = (n + S::KT - 1) / S::KT;
   const bool sums = k0 == 0 && a.dbias != nullptr;
   Source<T, S> from = source_of<T, S>(a, span.begin, o0, k0, blocks, tid);
+  // where stage s begins, and how many of its tokens the stages before have had (all of them behind the last stage)
+  auto base = [&](int s) { return s * S::KT < n - S::KT ? s * S::KT : n - S::KT; };
+  auto skip = [&](int s) { return s < stages ? s * S::KT - base(s) : S::KT; };
   if (stages > 0) {
     Fetched<T, S> even = {}, odd = {};
     {
-      Fetched<T, S> first = {}, second = {};   // (all four on their way at once; tokens behind the span's end are copies)
-      fetch<T, S>(a, from, n, blocks, tid, first);
-      fetch<T, S>(a, from, n - S::KT, blocks, tid, second);
-      fetch<T, S>(a, from, n - 2 * S::KT, blocks, tid, even);
-      fetch<T, S>(a, from, n - 3 * S::KT, blocks, tid, odd);
-      deposit<T, S>(first, stage[0], n, from.shift, tid, sums, bias);
-      deposit<T, S>(second, stage[1], n - S::KT, from.shift, tid, sums, bias);
+      Fetched<T, S> first = {}, second = {};   // (all four on their way at once)
+      if (n >= S::KT) {
+        fetch<T, S, true>(a, from, 0, base(1), blocks, tid, first);
+        fetch<T, S, true>(a, from, 0, base(2) - base(1), blocks, tid, second);
+        fetch<T, S, true>(a, from, 0, base(3) - base(2), blocks, tid, even);
+        fetch<T, S, true>(a, from, 0, base(4) - base(3), blocks, tid, odd);
+      } else {
+        fetch<T, S, false>(a, from, n - S::KT, 0, blocks, tid, first);
+      }
+      deposit<T, S>(first, stage[0], skip(0), from.shift, tid, sums, bias);
+      deposit<T, S>(second, stage[1], skip(1), from.shift, tid, sums, bias);
     }
     __syncthreads();
     Operands<S> now, next;
     read_operands<S>(stage[0], 0, wo, wk, lane, now);
     int at = 0, i = 0;   // at = i % 3
     // One stage; `f` holds the one after next, and takes the second after that.
-    auto whole = [&](Fetched<T, S>& f, auto with_sums) __attribute__((always_inline)) {
-      constexpr bool SUMS = decltype(with_sums)::value;
+    auto step = [&](Fetched<T, S>& f, int i, auto with_sums, auto whole) __attribute__((always_inline)) {
+      constexpr bool SUMS = decltype(with_sums)::value, WHOLE = decltype(whole)::value;
       const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
       // Reads first, one a step; the conversions and LDS writes spread over the steps behind them; loads last.
       constexpr int STEPS = S::FO * S::FI * S::P, READS = S::FI + S::FO * S::P, PIECES = S::CO + S::CI;
       constexpr bool TWO = S::KT == 32;
       constexpr int FROM = READS < STEPS ? READS : STEPS, ROOM = TWO ? STEPS - FROM : (STEPS - FROM) / 2;
       constexpr int EVERY = ROOM / PIECES > 0 ? ROOM / PIECES : 1, LOADS_FROM = TWO ? (STEPS > PIECES ? STEPS - PIECES : 0) : FROM + EVERY * PIECES;
+      const int skipped = skip(i + 2), advance = base(i + 5) - base(i + 4);
       auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
       auto read_next = [&](int i) { read_operand<S>(i, TWO ? stage[at] : stage[after], TWO ? 16 : 0, wo, wk, lane, next); };
       auto read_now = [&](int i) { read_operand<S>(i, stage[after], 0, wo, wk, lane, now); };
-      auto write = [&](int i) { deposit_piece<T, S, true>(i, f, stage[last], S::KT, from.shift, tid, SUMS, bias); };
-      auto load = [&](int i) { fetch_piece<T, S, true>(i, a, from, S::KT, blocks, tid, f); };
+      auto write = [&](int piece) { deposit_piece<T, S, WHOLE>(piece, f, stage[last], skipped, from.shift, tid, SUMS, bias); };
+      auto load = [&](int piece) { fetch_piece<T, S, true>(piece, a, from, 0, advance, blocks, tid, f); };
       int reads = 0, writes = 0, loads = 0;   // (constants once the steps are unrolled)
       pin();
-      multiply<S>(now, acc, [&](int step) {
+      multiply<S>(now, acc, [&](int m) {
         if (reads < READS) read_next(reads++);
-        if (step >= FROM && (step - FROM) % EVERY == 0 && writes < PIECES) write(writes++);
-        if (!TWO && step >= LOADS_FROM && loads < PIECES) load(loads++);
+        if (m >= FROM && (m - FROM) % EVERY == 0 && writes < PIECES) write(writes++);
+        if (!TWO && m >= LOADS_FROM && loads < PIECES) load(loads++);
         pin();
       });
 #pragma unroll
@@ -322,9 +342,9 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       for (int i = STEPS > FROM ? (STEPS - FROM + EVERY - 1) / EVERY : 0; i < PIECES; ++i) write(i);
       if (TWO) {
         int again = 0;
-        multiply<S>(next, acc, [&](int step) {
+        multiply<S>(next, acc, [&](int m) {
           if (again < READS) read_now(again++);
-          if (step >= LOADS_FROM && loads < PIECES) load(loads++);
+          if (m >= LOADS_FROM && loads < PIECES) load(loads++);
           pin();
         });
 #pragma unroll
@@ -337,39 +357,27 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       __syncthreads();
       at = after;
     };
-    auto any = [&](Fetched<T, S>& f, int i) __attribute__((always_inline)) {
-      const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
-      // (behind the last stage the buffers hold an older one, which is read and not used)
-      read_operands<S>(S::KT == 32 ? stage[at] : stage[after], S::KT == 32 ? 16 : 0, wo, wk, lane, next);
-      multiply<S>(now, acc);
-      if (i + 2 < stages) {
-        deposit<T, S>(f, stage[last], n - (i + 2) * S::KT, from.shift, tid, sums, bias);
-        if (i + 4 < stages) fetch<T, S>(a, from, n - (i + 4) * S::KT, blocks, tid, f);
-      }
-      if (S::KT == 32) {
-        read_operands<S>(stage[after], 0, wo, wk, lane, now);
-        multiply<S>(next, acc);
-      } else {
-        now = next;
-      }
-      __syncthreads();
-      at = after;
-    };
     // One wave a SIMD issues in order: what is to run beside the matrix instructions has to stand between them.
-    if (S::P > 1 || sums) {   // (beside the splitting the additions do not matter)
-      for (; (i + 6) * S::KT <= n; i += 2) {
-        whole(even, std::true_type());
-        whole(odd, std::true_type());
+    auto run = [&](auto with_sums) __attribute__((always_inline)) {
+      for (; (i + 4) * S::KT <= n; i += 2) {   // (the stages that are written, the one after next and the one behind it, are whole)
+        step(even, i, with_sums, std::true_type());
+        step(odd, i + 1, with_sums, std::true_type());
       }
+      for (; i < stages; i += 2) {
+        step(even, i, with_sums, std::false_type());
+        if (i + 1 < stages) step(odd, i + 1, with_sums, std::false_type());
+      }
+    };
+    if (n < S::KT) {
+      multiply<S>(now, acc);
+      if (S::KT == 32) {
+        read_operands<S>(stage[0], 16, wo, wk, lane, next);
+        multiply<S>(next, acc);
+      }
+    } else if (S::P > 1 || sums) {   // (beside the splitting the additions do not matter)
+      run(std::true_type());
     } else {
-      for (; (i + 6) * S::KT <= n; i += 2) {
-        whole(even, std::integral_constant<bool, (S::P > 1)>());
-        whole(odd, std::integral_constant<bool, (S::P > 1)>());
-      }
-    }
-    for (; i < stages; i += 2) {
-      any(even, i);
-      if (i + 1 < stages) any(odd, i + 1);
+      run(std::integral_constant<bool, (S::P > 1)>());
     }
   }
   __syncthreads();
