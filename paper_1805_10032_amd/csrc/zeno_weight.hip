@@ -273,6 +273,13 @@ __device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI
   multiply<S>(f, acc, [](int) {});
 }
 
+// Several pieces: a stage has P times the matrix instructions, and holding all its operands twice would take more registers than there
+// are.  The inputs' operands are held for this stage and the next, the outputs' three ahead in a ring of four.
+template <typename S>
+__device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf16x8 (&y)[4], int slot) {
+  y[slot] = read_columns<S::PITCH_O>(st.y[S::P - 1 - q % S::P], wo + 32 * (q / S::P), 0, lane);   // the smallest piece first
+}
+
 // Three stages in LDS: one that is multiplied, one that is whole, from which the first operands behind the barrier have been read
 // before it, and one that is being written; two more are on their way from memory.
 template <typename T, typename S>
@@ -310,8 +317,17 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       deposit<T, S>(second, stage[1], skip(1), from.shift, tid, sums, bias);
     }
     __syncthreads();
+    constexpr bool RING = S::FO == 4 && S::P > 1;
     Operands<S> now, next;
-    read_operands<S>(stage[0], 0, wo, wk, lane, now);
+    bf16x8 xa[S::FI], xb[S::FI], ring[4];
+    if constexpr (RING) {
+#pragma unroll
+      for (int j = 0; j < S::FI; ++j) xa[j] = read_columns<S::PITCH_I>(stage[0].a, wk + 32 * j, 0, lane);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) read_ring<S>(q, stage[0], wo, lane, ring, q);
+    } else {
+      read_operands<S>(stage[0], 0, wo, wk, lane, now);
+    }
     int at = 0, i = 0;   // at = i % 3
     // One stage; `f` holds the one after next, and takes the second after that.
     auto step = [&](Fetched<T, S>& f, int i, auto with_sums, auto whole) __attribute__((always_inline)) {
@@ -357,6 +373,35 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       __syncthreads();
       at = after;
     };
+    auto ring_step = [&](Fetched<T, S>& f, int i, bf16x8 (&x)[S::FI], bf16x8 (&x_next)[S::FI], auto whole) __attribute__((always_inline)) {
+      constexpr bool WHOLE = decltype(whole)::value;
+      constexpr int GROUPS = S::FO * S::P;
+      static_assert(!RING || GROUPS % 4 == 0, "the ring is where it was at the end of a stage");
+      const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
+      const int skipped = skip(i + 2), advance = base(i + 5) - base(i + 4);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q) {
+        const int r = q / S::P;
+#pragma unroll
+        for (int j = 0; j < S::FI; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[q % 4], x[j], acc[r][j], 0, 0, 0);
+        if (q + 3 < GROUPS) read_ring<S>(q + 3, stage[at], wo, lane, ring, (q + 3) % 4);
+        else read_ring<S>(q + 3 - GROUPS, stage[after], wo, lane, ring, (q + 3) % 4);
+        if (q < S::FI) x_next[q] = read_columns<S::PITCH_I>(stage[after].a, wk + 32 * q, 0, lane);
+        constexpr int PIECES = S::CO + S::CI;
+        if (q >= 1 && q - 1 < PIECES) deposit_piece<T, S, WHOLE>(q - 1, f, stage[last], skipped, from.shift, tid, true, bias);
+        if (q >= 1 + PIECES && q - 1 - PIECES < PIECES) fetch_piece<T, S, true>(q - 1 - PIECES, a, from, 0, advance, blocks, tid, f);
+      }
+#pragma unroll
+      for (int m = 0; m < GROUPS * S::FI; ++m) {
+        constexpr int kValu = 0x2, kMfma = 0x8, kRead = 0x100;
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kValu, 5, 0);
+        if (m % 2 == 0) __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+      }
+      __syncthreads();
+      at = after;
+    };
     // One wave a SIMD issues in order: what is to run beside the matrix instructions has to stand between them.
     auto run = [&](auto with_sums) __attribute__((always_inline)) {
       for (; (i + 4) * S::KT <= n; i += 2) {   // (the stages that are written, the one after next and the one behind it, are whole)
@@ -368,7 +413,21 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
         if (i + 1 < stages) step(odd, i + 1, with_sums, std::false_type());
       }
     };
-    if (n < S::KT) {
+    if constexpr (RING) {
+      if (n < S::KT) {
+        read_operands<S>(stage[0], 0, wo, wk, lane, now);
+        multiply<S>(now, acc);
+      } else {
+        for (; (i + 4) * S::KT <= n; i += 2) {
+          ring_step(even, i, xa, xb, std::true_type());
+          ring_step(odd, i + 1, xb, xa, std::true_type());
+        }
+        for (; i < stages; i += 2) {
+          ring_step(even, i, xa, xb, std::false_type());
+          if (i + 1 < stages) ring_step(odd, i + 1, xb, xa, std::false_type());
+        }
+      }
+    } else if (n < S::KT) {
       multiply<S>(now, acc);
       if (S::KT == 32) {
         read_operands<S>(stage[0], 16, wo, wk, lane, next);
