@@ -476,102 +476,169 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   }
 }
 
-// Few outputs: the sums are short of work for the matrix cores, and reading the activations is what counts.  A lane owns COLS columns and
-// all outputs of them; a wave goes down its tokens, whose dy it has put into LDS in float32 and reads back as broadcasts.  The eight
-// waves of a workgroup share the columns and add up at the end.
-constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewTokens = 32;
+// At most 32 outputs: reading the activations is what counts.  Each of a workgroup's four waves goes down its own tokens, 32 at a time, with
+// LDS of its own and no barrier; the waves share 128 inputs and add up at the end.  The bias is the product with a column of ones.
+constexpr int kFewOutputs = 32, kFewInputs = 128, kFewTokens = 32;
+constexpr int kFewPitchI = kFewInputs + 32, kFewPitchO = kFewOutputs;   // rows of 320 and 64 bytes: four lie on different banks
 
-template <typename T, int OMAX, int COLS>
-__global__ __launch_bounds__(kFewThreads, OMAX * COLS <= 64 ? 4 : 2) void weight_grad_few_kernel(WeightGradArgs a, int pieces, float* partial) {
-  constexpr int kCols = 64 * COLS, kStaged = kFewWaves * kFewTokens * OMAX, kJoined = OMAX * kCols;
-  __shared__ __align__(16) float memory[kStaged > kJoined ? kStaged : kJoined];
+// (16-bit values in words of their own: packing them in pairs would wait for the loads)
+template <typename T>
+__device__ inline unsigned raw_bits(const T* p) {
+  if constexpr (sizeof(T) == 2) return *reinterpret_cast<const uint16_t*>(p);
+  else return *reinterpret_cast<const unsigned*>(p);
+}
+template <typename T>
+__device__ inline float from_bits(unsigned bits) {
+  if constexpr (sizeof(T) == 2) return (float)__builtin_bit_cast(T, (uint16_t)bits);
+  else return __uint_as_float(bits);
+}
+
+template <int P>
+struct FewStage {
+  __bf16 a[16 * kFewPitchI];             // half a batch
+  __bf16 y[P][kFewTokens * kFewPitchO];
+};
+
+// EACH: dy of a batch for a lane, at least kFewTokens * a.out / 64.
+template <typename T, int P, int EACH>
+__global__ __launch_bounds__(kThreads, EACH > 8 ? 1 : 2) void weight_grad_few_kernel(WeightGradArgs a, int pieces, float* partial) {
+  constexpr int kWaves = kThreads / 64, FI = kFewInputs / 32;
+  __shared__ union {
+    FewStage<P> stage[kWaves];
+    float joined[kFewOutputs][kFewInputs + 1];   // (the last column: the bias)
+  } memory;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
   const int g = blockIdx.y / pieces, piece = blockIdx.y % pieces;
   const Span span = piece_of(a, g, piece, pieces);
   const int blocks = ckpt_blocks(a.width);
-  const int col = (int)blockIdx.x * kCols + COLS * lane;
-  const int at = col < blocks * kCkptBlock ? col : 0;   // (columns behind the last: the first ones, which nothing takes)
+  const int k0 = (int)blockIdx.x * kFewInputs;
   const bool sums = blockIdx.x == 0 && a.dbias != nullptr;
-  constexpr int SP = OMAX <= 4 ? 4 : (OMAX <= 8 ? 8 : (OMAX <= 16 ? 16 : 32));   // lanes that stage a token's dy
-  float acc[OMAX][COLS] = {}, bias = 0.f;                                       // (the bias: output lane % SP, tokens of the lane)
-  float (*staged)[OMAX] = reinterpret_cast<float (*)[OMAX]>(memory + wave * kFewTokens * OMAX);
-  const uint8_t* values = a.values + at;
-  const uint8_t* scales = a.scales + at / kCkptBlock;
-  const long long pitch = (long long)blocks * kCkptBlock;
-  for (int t0 = span.begin + kFewTokens * wave; t0 < span.end; t0 += kFewTokens * kFewWaves) {
-    const int n = span.end - t0 < kFewTokens ? span.end - t0 : kFewTokens;
-    row_sync<1>();
+  FewStage<P>& st = memory.stage[wave];
+  // outputs behind the last are zeros for good
+  for (int i = lane; i < P * kFewTokens * kFewPitchO; i += 64) (&st.y[0][0])[i] = (__bf16)0.f;
+  f32x16 acc[FI] = {}, acc_bias = {};
+  bf16x8 ones;
 #pragma unroll
-    for (int i = 0; i < kFewTokens * SP / 64; ++i) {
-      const int t = 64 / SP * i + lane / SP, o = lane % SP;
-      const float d = t < n && o < a.out ? (float)reinterpret_cast<const T*>(a.dy)[(long long)(t0 + t) * a.lddy + o] : 0.f;
-      bias += d;
-      if (o < OMAX) staged[t][o] = d;
-    }
-    row_sync<1>();
-    constexpr int STEP = 8;
-    for (int t = 0; t < n; t += STEP) {
-      unsigned words[STEP][COLS / 4];
-      uint8_t scale[STEP];
+  for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.f;
+  // a lane's part of a batch: sixteen activations of four tokens, and every 64th of the batch's dy
+  const int col = k0 + 16 * (lane % 8), at = col < blocks * kCkptBlock ? col : 0;   // (columns behind the last: the first ones)
+  const unsigned pitch = (unsigned)blocks * kCkptBlock;
+  const int elements = kFewTokens * a.out, magic = (65536 + a.out - 1) / a.out;
+  auto token_of = [&](int i) { return (64 * i + lane) * magic >> 16; };   // (of 64 i + lane < 1024, a.out <= 32: the quotient is exact)
+  // from the batch's first token on; beyond 32 bits only if lddy is, which the slow way below takes
+  unsigned dy_at[EACH];
 #pragma unroll
-      for (int i = 0; i < STEP; ++i) {
-        const long long row = t0 + (t + i < n ? t + i : n - 1);   // (its dy is zero in LDS where it stands in for another)
+  for (int i = 0; i < EACH; ++i) {
+    const int e = 64 * i + lane < elements ? 64 * i + lane : 0, t = e * magic >> 16;
+    dy_at[i] = (unsigned)t * (unsigned)a.lddy + (unsigned)(e - t * a.out);
+  }
+  const bool near = a.lddy < (1 << 24);
+  struct Batch {
+    uint4 words[4];
+    uint8_t scale[4];
+    unsigned dy[EACH];
+  };
+  auto load = [&](int t0, Batch& b) __attribute__((always_inline)) {
+    if (t0 + kFewTokens <= span.end && near) {
+      const uint8_t* values = a.values + (long long)t0 * pitch;
+      const uint8_t* scales = a.scales + (long long)t0 * blocks;
+      const T* dy = reinterpret_cast<const T*>(a.dy) + (long long)t0 * a.lddy;
 #pragma unroll
-        for (int j = 0; j < COLS / 4; ++j) words[i][j] = reinterpret_cast<const unsigned*>(values + row * pitch)[j];
-        scale[i] = scales[row * blocks];
+      for (int q = 0; q < 4; ++q) {
+        b.words[q] = *reinterpret_cast<const uint4*>(values + ((unsigned)(8 * q + lane / 8) * pitch + (unsigned)at));
+        b.scale[q] = scales[(unsigned)(8 * q + lane / 8) * (unsigned)blocks + (unsigned)(at / kCkptBlock)];
       }
 #pragma unroll
-      for (int i = 0; i < STEP; ++i) {
-        float v[COLS];
-        ckpt_unpack(words[i], ckpt_scale((int)scale[i] - 127), v);
+      for (int i = 0; i < EACH; ++i) b.dy[i] = raw_bits(dy + dy_at[i]);
+    } else {
+      const int last = span.end - 1;
 #pragma unroll
-        for (int o = 0; o < OMAX; o += 4) {
-          const float4 d = *reinterpret_cast<const float4*>(&staged[t + i][o]);
-          const float dd[4] = {d.x, d.y, d.z, d.w};
+      for (int q = 0; q < 4; ++q) {
+        const long long row = t0 + 8 * q + lane / 8 < last ? t0 + 8 * q + lane / 8 : last;   // (a copy of the last token has no dy)
+        b.words[q] = *reinterpret_cast<const uint4*>(a.values + row * pitch + at);
+        b.scale[q] = a.scales[row * blocks + at / kCkptBlock];
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+      for (int i = 0; i < EACH; ++i) {
+        const int e = 64 * i + lane < elements ? 64 * i + lane : 0, t = e * magic >> 16;
+        const long long row = t0 + t < last ? t0 + t : last;
+        b.dy[i] = raw_bits(reinterpret_cast<const T*>(a.dy) + row * a.lddy + (e - t * a.out));
+      }
+    }
+  };
+  Batch now, next;
+  const int step = kFewTokens * kWaves;
+  int t0 = span.begin + kFewTokens * wave;
+  if (t0 < span.end) load(t0, now);
+  for (; t0 < span.end; t0 += step) {
+    const int n = span.end - t0;
+    load(t0 + step < span.end ? t0 + step : t0, next);   // (always: loads that may not have been sent are waited for as if they were the last)
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) acc[o + e][c] = fmaf(dd[e], v[c], acc[o + e][c]);
-          }
+    for (int i = 0; i < EACH; ++i) {
+      const int e = 64 * i + lane, t = token_of(i), o = e - t * a.out;
+      float rest = t < n ? from_bits<T>(now.dy[i]) : 0.f;
+      const bool finite = fabsf(rest) < __builtin_inff();
+      if (e < elements) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const unsigned bits = __float_as_uint(rest);
+          *reinterpret_cast<uint16_t*>(&st.y[p][t * kFewPitchO + o]) = (uint16_t)(bits >> 16);
+          rest = finite ? rest - __uint_as_float(bits & 0xffff0000u) : (rest != rest ? rest : 0.f);
         }
       }
     }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      row_sync<1>();
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const float s = ckpt_scale((int)now.scale[2 * half + q] - 127);
+        const uint4 w = now.words[2 * half + q];
+        __bf16* to = &st.a[(8 * q + lane / 8) * kFewPitchI + 16 * (lane % 8)];
+        *reinterpret_cast<bf16x8*>(to) = widen8(w.x, w.y, s);
+        *reinterpret_cast<bf16x8*>(to + 8) = widen8(w.z, w.w, s);
+      }
+      row_sync<1>();
+      bf16x8 x[FI];
+#pragma unroll
+      for (int j = 0; j < FI; ++j) x[j] = read_columns<kFewPitchI>(st.a, 32 * j, 0, lane);
+#pragma unroll
+      for (int p = P - 1; p >= 0; --p) {
+        const bf16x8 y = read_columns<kFewPitchO>(st.y[p], 0, 16 * half, lane);
+#pragma unroll
+        for (int j = 0; j < FI; ++j) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, x[j], acc[j], 0, 0, 0);
+        if (sums) acc_bias = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y, ones, acc_bias, 0, 0, 0);
+      }
+    }
+    row_sync<1>();
+    now = next;
   }
-  const long long size = (long long)a.out * a.width;
-  float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
-  float (*joined)[kCols] = reinterpret_cast<float (*)[kCols]>(memory);
-  for (int w = 0; w < kFewWaves; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     __syncthreads();
     if (wave == w) {
 #pragma unroll
-      for (int o = 0; o < OMAX; ++o)
+      for (int e = 0; e < 16; ++e) {
+        const int o = 8 * (e / 4) + 4 * (lane / 32) + e % 4;
 #pragma unroll
-        for (int c = 0; c < COLS; c += 4) {
-          float4* to = reinterpret_cast<float4*>(&joined[o][COLS * lane + c]);
-          float4 v = make_float4(acc[o][c], acc[o][c + 1], acc[o][c + 2], acc[o][c + 3]);
-          if (w > 0) {
-            const float4 old = *to;
-            v = make_float4(v.x + old.x, v.y + old.y, v.z + old.z, v.w + old.w);
-          }
-          *to = v;
+        for (int j = 0; j < FI; ++j) {
+          float& sum = memory.joined[o][32 * j + lane % 32];
+          sum = w == 0 ? acc[j][e] : sum + acc[j][e];
         }
+        if (lane % 32 == 0) {
+          float& sum = memory.joined[o][kFewInputs];
+          sum = w == 0 ? acc_bias[e] : sum + acc_bias[e];
+        }
+      }
     }
   }
   __syncthreads();
-  const int left = a.width - (int)blockIdx.x * kCols < kCols ? a.width - (int)blockIdx.x * kCols : kCols;
-  for (int o = 0; o < a.out; ++o)
-    for (int c = tid; c < left; c += kFewThreads) dw[(long long)o * a.width + (int)blockIdx.x * kCols + c] = joined[o][c];
-  if (sums) {
-#pragma unroll
-    for (int off = SP; off < 64; off <<= 1) bias += __shfl_xor(bias, off, 64);
-    for (int w = 0; w < kFewWaves; ++w) {
-      __syncthreads();
-      if (wave == w && lane < SP) memory[lane] = bias + (w > 0 ? memory[lane] : 0.f);
-    }
-    __syncthreads();
-    float* db = pieces == 1 ? a.dbias + g * a.ldb : dw + size;
-    if (tid < a.out) db[tid] = memory[tid];
+  const long long size = (long long)a.out * a.width;
+  float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
+  for (int i = tid; i < a.out * kFewInputs; i += kThreads) {
+    const int o = i / kFewInputs, k = k0 + i % kFewInputs;
+    if (k < a.width) dw[(long long)o * a.width + k] = memory.joined[o][i % kFewInputs];
   }
+  if (sums && tid < a.out) (pieces == 1 ? a.dbias + g * a.ldb : dw + size)[tid] = memory.joined[tid][kFewInputs];
 }
 
 // The pieces of a group's tokens.  A wave takes 64 gradients and every so-manieth piece; the waves' sums are added in their order.
@@ -604,9 +671,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void weight_grad_join_kernel(Weigh
 template <typename S>
 long long tiles_of(int out, int width) { return (long long)ceil_div(out, S::OUT) * ceil_div(width, S::IN); }
 
-constexpr int kFewOutputs = 32;   // at most so many: the kernel for few outputs
-inline int few_columns(int out) { return out <= 8 ? 512 : 256; }
-
 enum Shape { kFew, kMid, kWide };
 struct Plan {
   Shape shape;
@@ -616,8 +680,8 @@ Plan plan_for(int rows, int out, int width, int m) {
   Plan p;
   if (out <= kFewOutputs) {
     p.shape = kFew;
-    const long long strips = (long long)ceil_div(width, few_columns(out)) * m;
-    const long long pieces = 512 / strips, most = rows / m / (kFewTokens * kFewWaves);
+    const long long strips = (long long)ceil_div(width, kFewInputs) * m;
+    const long long pieces = 512 / strips, most = rows / m / (kFewTokens * 4);
     p.pieces = (int)std::max(1LL, std::min(pieces, most));
     return p;
   }
@@ -628,20 +692,18 @@ Plan plan_for(int rows, int out, int width, int m) {
   return p;
 }
 
-template <typename T, int OMAX, int COLS>
+template <typename T, int P, int EACH>
 hipError_t start_few(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
-  hipLaunchKernelGGL((weight_grad_few_kernel<T, OMAX, COLS>), dim3(ceil_div(a.width, 64 * COLS), a.m * pieces), dim3(kFewThreads), 0, stream,
-                     a, pieces, partial);
+  hipLaunchKernelGGL((weight_grad_few_kernel<T, P, EACH>), dim3(ceil_div(a.width, kFewInputs), a.m * pieces), dim3(kThreads), 0, stream, a,
+                     pieces, partial);
   return hipGetLastError();
 }
-template <typename T>
-hipError_t start_few_type(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
-  if (a.out <= 4) return start_few<T, 4, 8>(a, pieces, partial, stream);
-  if (a.out <= 8) return start_few<T, 8, 8>(a, pieces, partial, stream);
-  if (a.out <= 12) return start_few<T, 12, 4>(a, pieces, partial, stream);
-  if (a.out <= 16) return start_few<T, 16, 4>(a, pieces, partial, stream);
-  if (a.out <= 24) return start_few<T, 24, 4>(a, pieces, partial, stream);
-  return start_few<T, 32, 4>(a, pieces, partial, stream);
+template <typename T, int P>
+hipError_t start_few(const WeightGradArgs& a, int pieces, float* partial, hipStream_t stream) {
+  if (a.out <= 4) return start_few<T, P, 2>(a, pieces, partial, stream);
+  if (a.out <= 12) return start_few<T, P, 6>(a, pieces, partial, stream);
+  if (a.out <= 16) return start_few<T, P, 8>(a, pieces, partial, stream);
+  return start_few<T, P, 16>(a, pieces, partial, stream);
 }
 
 template <typename T, typename S>
@@ -659,7 +721,7 @@ hipError_t start(const WeightGradArgs& a, int pieces, float* partial, hipStream_
 template <typename T, int P, bool ODD>
 hipError_t start_shape(const WeightGradArgs& a, const Plan& p, float* partial, hipStream_t stream) {
   switch (p.shape) {
-    case kFew: return start_few_type<T>(a, p.pieces, partial, stream);
+    case kFew: return start_few<T, P>(a, p.pieces, partial, stream);
     case kMid: return start<T, MidTile<P, ODD>>(a, p.pieces, partial, stream);
     default: return start<T, WideTile<P, ODD>>(a, p.pieces, partial, stream);
   }
