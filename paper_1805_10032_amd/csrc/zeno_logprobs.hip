@@ -15,6 +15,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256;
+constexpr int kNarrow = 256;       // values of a row that sixteen lanes hold
 constexpr int kCandidates = 512;   // top values are chosen from at most so many
 constexpr int kMaxParts = 64;      // workgroups that share a row
 
@@ -445,6 +446,82 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
   }
 }
 
+// Rows of a few values: sixteen lanes a row, which stays in registers; its alternatives are found one after the other.
+template <typename T, bool ENT>
+__global__ __launch_bounds__(kThreads) void logprobs_narrow_kernel(LogprobsArgs a) {
+  constexpr int N = Wide<T>::N, PIECES = kNarrow / (16 * N);
+  const int lane = threadIdx.x % 16;
+  const float inf = __builtin_inff();
+  auto reduce = [](float v, auto f) {
+    v = f(v, dpp<kDppXor1>(v));
+    v = f(v, dpp<kDppXor2>(v));
+    v = f(v, dpp<kDppHalfMirror>(v));
+    return f(v, dpp<kDppMirror>(v));
+  };
+  auto add = [](float x, float y) { return x + y; };
+  const long long rows_up = ((long long)a.rows + 15) / 16 * 16;   // (whole workgroups: the lanes of a row stay together)
+  for (long long r64 = (long long)blockIdx.x * (kThreads / 16) + threadIdx.x / 16; r64 < rows_up; r64 += (long long)gridDim.x * (kThreads / 16)) {
+    const bool live = r64 < a.rows;
+    const int rowi = live ? (int)r64 : a.rows - 1;
+    const T* row = reinterpret_cast<const T*>(a.logits) + (long long)rowi * a.ldz;
+    float v[PIECES][N], M = -inf, s = 0.f, t = 0.f;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int at = (16 * p + lane) * N;
+      load_at(row, a.vocab, at, v[p]);   // (-inf behind the row's end)
+      M = max_of<N>(v[p], M);
+    }
+    M = reduce(clean(M), [](float x, float y) { return fmaxf(x, y); });
+    const float ref = M > -inf ? M : 0.f;   // (a row of nothing but -inf)
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = (v[p][j] - ref) * kLog2e, e = exp2_fast(d);
+        s += e;
+        if (ENT) t = fmaf(e, fmaxf(d, -1e30f), t);
+      }
+    s = reduce(s, add);
+    if (ENT) t = reduce(t, add);
+    float log_s = 0.f;
+    const RowSums r = {M, s, t};
+    if (live && lane == 0) finish_row<T>(a, rowi, r, &log_s);
+    if (a.top > 0) {
+      if (M == inf) s = __builtin_nanf("");
+      const bool empty = is_empty(M, s);
+      log_s = __shfl(log_s, threadIdx.x % 64 - lane, 64);
+      float last = inf;
+      int last_idx = -1;
+      for (int k = 0; k < a.top; ++k) {
+        float best = -inf;
+        int best_idx = 0x7fffffff;   // (behind the row's end are -inf of higher indices than the row's own: top <= vocab, they are not reached)
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const float c = clean(v[p][j]);
+            const int idx = (16 * p + lane) * N + j;
+            const bool after = c < last || (c == last && idx > last_idx);
+            if (after && (c > best || (c == best && idx < best_idx))) {
+              best = c;
+              best_idx = idx;
+            }
+          }
+        last = reduce(best, [](float x, float y) { return fmaxf(x, y); });
+        int idx = best == last ? best_idx : 0x7fffffff;
+        idx = min(idx, dpp_int<kDppXor1>(idx));
+        idx = min(idx, dpp_int<kDppXor2>(idx));
+        idx = min(idx, dpp_int<kDppHalfMirror>(idx));
+        last_idx = min(idx, dpp_int<kDppMirror>(idx));
+        if (live && lane == 0) {
+          a.top_index[(long long)rowi * a.top + k] = last_idx;
+          a.top_logp[(long long)rowi * a.top + k] = log_prob(last, M, log_s, empty);
+        }
+      }
+    }
+  }
+}
+
 // Joins the parts of a row: one workgroup of one wave a row.  What does not depend on each other is read at once.
 template <typename T>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts w) {
@@ -514,16 +591,24 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts
 
 // ---- gradient:  dz_j = g [j = y] + sum_k q_k [j = i_k] - p_j (g + sum_k q_k + h (log p_j + H))
 // with g, h, q the gradients of logp, H and the alternatives' log probabilities.
-template <typename T, bool ENT, bool TOP>
+// L threads a segment of a row (16, 64 or 256): 256 / L segments a workgroup.
+template <typename T, bool ENT, bool TOP, int L>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArgs a, int segs, int seg_len) {
-  constexpr int N = Wide<T>::N;
-  __shared__ int special_idx[33];
-  __shared__ float special_g[33];
+  constexpr int N = Wide<T>::N, EACH = kThreads / L;
+  static_assert(!TOP || L >= 64, "every alternative has a thread");
+  __shared__ int all_idx[EACH][32];
+  __shared__ float all_g[EACH][32];
+  const int slot = threadIdx.x / L, tid = threadIdx.x % L;
+  int (&special_idx)[32] = all_idx[slot];
+  float (&special_g)[32] = all_g[slot];
   const long long tiles = (long long)a.rows * segs;
   const float inf = __builtin_inff();
-  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const long long row = tile / segs;
-    const int lo = (int)(tile % segs) * seg_len;
+  // (whole workgroups go through the loop: a segment behind the last repeats it and writes nothing)
+  for (long long first = (long long)blockIdx.x * EACH; first < tiles; first += (long long)gridDim.x * EACH) {
+    const bool live = first + slot < tiles;
+    const long long tile = live ? first + slot : tiles - 1;
+    const long long row = segs == 1 ? tile : tile / segs;
+    const int lo = (int)(tile - row * segs) * seg_len;
     const int n = a.vocab - lo < seg_len ? a.vocab - lo : seg_len;
     const T* z = reinterpret_cast<const T*>(a.logits) + row * a.ldz + lo;
     T* out = reinterpret_cast<T*>(a.dlogits) + row * a.ldd + lo;
@@ -538,11 +623,11 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
     }
     float sum = g;
     if (TOP) {
-      if (threadIdx.x < a.top) {
-        const int idx = a.top_index[row * a.top + threadIdx.x];
+      if (tid < a.top) {
+        const int idx = a.top_index[row * a.top + tid];
         const bool valid = idx >= 0 && idx < a.vocab;
-        special_idx[threadIdx.x] = valid ? idx : -1;
-        special_g[threadIdx.x] = valid ? a.grad_top[row * a.top + threadIdx.x] : __builtin_nanf("");
+        special_idx[tid] = valid ? idx : -1;
+        special_g[tid] = valid ? a.grad_top[row * a.top + tid] : __builtin_nanf("");
       }
       __syncthreads();
       for (int i = 0; i < a.top; ++i) sum += special_g[i];
@@ -561,15 +646,16 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
     // the alternatives' columns of this segment, before anything is overwritten (dlogits may be the logits)
     float kept = 0.f;
     int mine = -1;
-    if (TOP && threadIdx.x < a.top) {
-      const int idx = special_idx[threadIdx.x] - lo;
+    if (TOP && tid < a.top) {
+      const int idx = special_idx[tid] - lo;
       if (idx >= 0 && idx < n) {
         mine = idx;
         kept = (float)z[idx];
       }
     }
     if (TOP) __syncthreads();
-    for (int at = threadIdx.x * N; at < n; at += kThreads * N) {
+    if (live)
+    for (int at = tid * N; at < n; at += L * N) {
       float v[N];
       if (at + N <= n)
         load_wide(z + at, v);
@@ -590,7 +676,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
     }
     if (TOP) {
       __syncthreads();   // the segment is written: its special columns once more, with all that falls on them
-      if (mine >= 0 && !empty) {
+      if (mine >= 0 && !empty && live) {
         float d = grad(kept);
         if (mine == y - lo) d += g;
         for (int i = 0; i < a.top; ++i)
@@ -645,6 +731,13 @@ void start(const LogprobsArgs& a, const Parts& w, dim3 grid, hipStream_t stream)
 
 template <typename T>
 hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream) {
+  if (a.vocab <= kNarrow) {
+    const int blocks = ceil_div(a.rows, kThreads / 16);
+    const dim3 grid(blocks < 8192 ? blocks : 8192);
+    if (a.entropy != nullptr) hipLaunchKernelGGL((logprobs_narrow_kernel<T, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((logprobs_narrow_kernel<T, false>), grid, dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   const int rpb = wave_rows(a.vocab) ? Shape<1>::ROWS : 1;
   const long long blocks = ((long long)a.rows + rpb - 1) / rpb;
   const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)), w.parts);
@@ -657,18 +750,28 @@ hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream
   return hipGetLastError();
 }
 
+template <typename T, int L>
+hipError_t start_grad(const LogprobsGradArgs& a, hipStream_t stream) {
+  const int seg_len = L * Wide<T>::N * 4;
+  const int segs = ceil_div(a.vocab, seg_len), each = kThreads / L;
+  const long long blocks = ((long long)a.rows * segs + each - 1) / each;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))), block(kThreads);
+  const bool ent = a.grad_entropy != nullptr, top = a.grad_top != nullptr && a.top > 0;
+  if constexpr (L >= 64) {
+    if (ent && top) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, true, L>), grid, block, 0, stream, a, segs, seg_len);
+    else if (top) hipLaunchKernelGGL((logprobs_grad_kernel<T, false, true, L>), grid, block, 0, stream, a, segs, seg_len);
+  }
+  if (ent && !top) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, false, L>), grid, block, 0, stream, a, segs, seg_len);
+  else if (!top) hipLaunchKernelGGL((logprobs_grad_kernel<T, false, false, L>), grid, block, 0, stream, a, segs, seg_len);
+  return hipGetLastError();
+}
+
+// Short rows share a workgroup.
 template <typename T>
 hipError_t launch_grad_type(const LogprobsGradArgs& a, hipStream_t stream) {
-  const int seg_len = kThreads * Wide<T>::N * 4;
-  const int segs = ceil_div(a.vocab, seg_len);
-  const long long tiles = (long long)a.rows * segs;
-  const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : (1 << 20))), block(kThreads);
-  const bool ent = a.grad_entropy != nullptr, top = a.grad_top != nullptr && a.top > 0;
-  if (ent && top) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, true>), grid, block, 0, stream, a, segs, seg_len);
-  else if (ent) hipLaunchKernelGGL((logprobs_grad_kernel<T, true, false>), grid, block, 0, stream, a, segs, seg_len);
-  else if (top) hipLaunchKernelGGL((logprobs_grad_kernel<T, false, true>), grid, block, 0, stream, a, segs, seg_len);
-  else hipLaunchKernelGGL((logprobs_grad_kernel<T, false, false>), grid, block, 0, stream, a, segs, seg_len);
-  return hipGetLastError();
+  if (a.vocab <= kNarrow && a.grad_top == nullptr) return start_grad<T, 16>(a, stream);
+  if (a.vocab <= 64 * Wide<T>::N * 4) return start_grad<T, 64>(a, stream);
+  return start_grad<T, 256>(a, stream);
 }
 
 }  // namespace
