@@ -18,6 +18,8 @@ constexpr int kMaxGrid = 1 << 20;
 template <int NW>
 struct Shape {
   static constexpr int TPR = 64 * NW, THREADS = NW < 4 ? 256 : TPR, RPB = THREADS / TPR;
+  // Which of the workgroup's rows is a thread's (the same for a wave, so that a row's address needs no registers of the lanes).
+  static __device__ inline int slot() { return RPB > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0; }
 };
 
 // Sums over the threads of a row.  The buffers alternate from row to row, so one barrier is enough: a buffer is written again
@@ -105,12 +107,12 @@ struct RowPart {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (c * TPR + tid) * N;
-      if (width < N) {
+      if (TPR * CH == 64 && width < N) {   // (wider launches have wider rows)
 #pragma unroll
         for (int j = 0; j < N; ++j) raw[c][j] = row[j < width ? j : 0];
       } else {
-        const int at = col + N <= width ? col : (col < width ? width - N : 0);
-        raw[c] = *reinterpret_cast<const typename Wide<T>::unaligned*>(row + at);
+        const unsigned at = col + N <= width ? col : (col < width ? width - N : 0);
+        raw[c] = *reinterpret_cast<const typename Wide<T>::unaligned*>(reinterpret_cast<const char*>(row) + at * (unsigned)sizeof(T));
       }
     }
   }
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
   typedef Params<N, TPR, CH> P;
   __shared__ float buf[2][NW][2];
   __shared__ __align__(16) float weight[P::SIZE], bias[P::SIZE];
-  const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
+  const int tid = threadIdx.x % TPR, slot = Shape<NW>::slot(), wave = tid / 64;
   const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
   P::fill(weight, a.weight, a.width);
@@ -295,7 +297,7 @@ __device__ inline int first_group(const int32_t* offsets, int m, int row, int ro
     const int at = i + (int)threadIdx.x;
     g += __syncthreads_count(at < m && group_offset(offsets, at + 1, rows) <= row);
   }
-  return g;
+  return __builtin_amdgcn_readfirstlane(g);
 }
 
 // xh of N columns, from the row itself or from its checkpoint
@@ -327,13 +329,15 @@ struct KeptPart {
   uint8_t scale[CH];
   __device__ inline void load(const uint8_t* values, const uint8_t* scales, long long row, int blocks, int tid) {
     constexpr int N = Wide<T>::N;
+    const uint8_t* v = values + row * ((long long)blocks * kCkptBlock);
+    const uint8_t* s = scales + row * blocks;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int col = (c * TPR + tid) * N, at = col < blocks * kCkptBlock ? col : 0;
-      const uint8_t* p = values + row * ((long long)blocks * kCkptBlock) + at;
+      const int col = (c * TPR + tid) * N;
+      const unsigned at = col < blocks * kCkptBlock ? col : 0;
 #pragma unroll
-      for (int j = 0; j < N / 4; ++j) words[c][j] = reinterpret_cast<const unsigned*>(p)[j];
-      scale[c] = scales[row * blocks + at / kCkptBlock];
+      for (int j = 0; j < N / 4; ++j) words[c][j] = reinterpret_cast<const unsigned*>(v + at)[j];
+      scale[c] = s[at / kCkptBlock];
     }
   }
   __device__ inline void again() {
@@ -379,12 +383,12 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
   __shared__ float buf[2][NW][2];
   __shared__ __align__(16) float weight[P::SIZE];
   __shared__ float joined[RPB > 1 ? 2 * CH * N * 64 : 1];
-  const int tid = threadIdx.x % TPR, slot = threadIdx.x / TPR, wave = tid / 64;
+  const int tid = threadIdx.x % TPR, slot = Shape<NW>::slot(), wave = tid / 64;
   const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
   const int r0 = blockIdx.x * p.chunk, r1 = a.rows - r0 < p.chunk ? a.rows : r0 + p.chunk;
   P::fill(weight, a.weight, a.width);
-  __syncthreads();
+  if (a.offsets == nullptr) __syncthreads();   // (or the search for the first group has one)
   int parity = 0;
   for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
     const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
@@ -396,13 +400,19 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int j = 0; j < N; ++j) dw[c][j] = db[c][j] = 0.f;
-    GradRow<T, TPR, CH, KEPT> now, next, after;   // two rows are on their way while a third is reduced (one: 92 instead of 84 us)
+    // Two rows are on their way while a third is reduced (one: 92 instead of 84 us at 4096 bf16 columns).  With more values a thread there
+    // are registers for one, and with 32 values and eight waves for none, where a row that is on its way would be spilled (2000 x 12000
+    // fp32: 89 us, 189 with one).
+    constexpr int AHEAD = CH * N <= 16 ? 2 : NW == 8 && CH * N >= 32 ? 0 : 1;
+    GradRow<T, TPR, CH, KEPT> now, next, after;
     if (lo + slot < hi) {
-      now.load(a, lo + slot, blocks, tid);
-      next.load(a, lo + slot + RPB < hi ? lo + slot + RPB : lo + slot, blocks, tid);
+      if (AHEAD > 0) now.load(a, lo + slot, blocks, tid);
+      if (AHEAD == 2) next.load(a, lo + slot + RPB < hi ? lo + slot + RPB : lo + slot, blocks, tid);
     }
     for (int row = lo + slot; row < hi; row += RPB) {
-      after.load(a, row + 2 * RPB < hi ? row + 2 * RPB : row, blocks, tid);
+      if (AHEAD == 2) after.load(a, row + 2 * RPB < hi ? row + 2 * RPB : row, blocks, tid);
+      if (AHEAD == 0) now.load(a, row, blocks, tid);
+      if (AHEAD == 1) next.load(a, row + RPB < hi ? row + RPB : row, blocks, tid);
       const float mean = now.mean, rstd = now.rstd;
       float c1 = 0.f, c2 = 0.f, d[N], xh[N], w[N];
 #pragma unroll
@@ -437,8 +447,8 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
           store_cols(dx, (c * TPR + tid) * N, a.width, d);
         }
       }
-      now = next;
-      next = after;
+      if (AHEAD > 0) now = next;
+      if (AHEAD == 2) next = after;
     }
     float* out = p.partial + (long long)(blockIdx.x + g) * 2 * a.width;
     if (RPB > 1) {
@@ -553,23 +563,26 @@ __global__ __launch_bounds__(1024) void norm_grad_long_weights_kernel(NormGradAr
   }
 }
 
-// A group's gradient: its slots in order.  64 columns (of weights and biases together) a workgroup, four waves over the slots.
-__global__ __launch_bounds__(256) void norm_grad_join_kernel(Pieces p, const int32_t* offsets, int rows, int width,
-                                                             float* __restrict__ dweight, float* __restrict__ dbias, long long ldw,
-                                                             long long ldb) {
-  __shared__ float shared[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, g = blockIdx.y;
+// A group's gradient: its slots.  64 columns (of weights and biases together) a workgroup; a wave takes every so-manieth slot, and the waves'
+// sums are added in their order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void norm_grad_join_kernel(Pieces p, const int32_t* offsets, int rows, int width,
+                                                                         float* __restrict__ dweight, float* __restrict__ dbias,
+                                                                         long long ldw, long long ldb) {
+  __shared__ float shared[kJoinWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, waves = blockDim.x / 64, g = blockIdx.y;
   const long long col = (long long)blockIdx.x * 64 + lane;
   const int begin = group_offset(offsets, g, rows), end = group_offset(offsets, g + 1, rows);
   float sum = 0.f;
   if (begin < end && col < 2LL * width) {
     const int c1 = (end - 1) / p.chunk;
-    for (int c = begin / p.chunk + wave; c <= c1; c += 4) sum += p.partial[(long long)(c + g) * 2 * width + col];
+#pragma unroll 4
+    for (int c = begin / p.chunk + wave; c <= c1; c += waves) sum += p.partial[(long long)(c + g) * 2 * width + col];
   }
   shared[wave][lane] = sum;
   __syncthreads();
   if (wave == 0 && col < 2LL * width) {
-    sum = (shared[0][lane] + shared[1][lane]) + (shared[2][lane] + shared[3][lane]);
+    for (int w = 1; w < waves; ++w) sum += shared[w][lane];
     if (col < width) {
       if (dweight != nullptr) dweight[g * ldw + col] = sum;
     } else if (dbias != nullptr) {
@@ -579,8 +592,8 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(Pieces p, const int
 }
 
 // Rows of a chunk: 512 chunks of a large batch, two workgroups a compute unit (16384 x 4096 bf16 from a checkpoint: 84 us; 256 chunks 93,
-// 768 105, because a third workgroup does not fit beside two); at least 16 rows, where the partial sums (8 bytes a column and chunk) are a
-// tenth of what the rows themselves move, unless that leaves most of the chip without work.
+// 768 105, because a third workgroup does not fit beside two); at least 16 rows, where the
+// partial sums (8 bytes a column and chunk) are a tenth of what the rows themselves move, unless that leaves most of the chip without work.
 int chunk_rows(int rows) {
   const int many = ceil_div(rows, 512), few = ceil_div(rows, 256);
   int c = few < 16 ? few : 16;
@@ -597,14 +610,15 @@ Pieces pieces_for(int rows, void* workspace) {
 }
 
 // The narrowest launch that holds a row: waves a row and 16-byte pieces a thread.  0 waves: the kernels for long rows, beyond 16384
-// columns, whose weights and biases no longer fit LDS.
+// columns, whose weights and biases no longer fit LDS.  Beyond 512 threads' rows the backward pass takes more pieces a thread where the
+// forward pass takes more threads: its sums stay in registers, of which 1024 threads have 128 each (4000 x 12000 bf16: 410 us).
 void pick_shape(int width, int per_load, bool backward, int* nw, int* ch) {
-  // (the backward pass holds two sums for every column: from four pieces a thread on, a row is shared by four waves)
-  const int shapes[][2] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 16 / per_load}};
+  static const int shapes[][2] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {8, 2}, {8, 4}, {8, 8}};
   for (const auto& s : shapes)
     if (64 * s[0] * s[1] * per_load <= 16384 && width <= 64 * s[0] * s[1] * per_load) {
-      *nw = s[0];
-      *ch = s[1];
+      const bool spread = !backward && s[1] > 2 && s[0] > 1;
+      *nw = spread ? 16 : s[0];
+      *ch = spread ? s[1] / 2 : s[1];
       return;
     }
   *nw = 0;
@@ -626,8 +640,9 @@ hipError_t launch_norm_type(const NormArgs& a, hipStream_t stream) {
   else if (nw == 1 && ch == 2) start_norm<T, 1, 2>(a, stream);
   else if (nw == 1 && ch == 4) start_norm<T, 1, 4>(a, stream);
   else if (nw == 4 && ch == 2) start_norm<T, 4, 2>(a, stream);
-  else if (nw == 4) start_norm<T, 4, 4>(a, stream);
-  else if (nw == 16) start_norm<T, 16, 16 / Wide<T>::N>(a, stream);
+  else if (nw == 8) start_norm<T, 8, 2>(a, stream);
+  else if (nw == 16 && ch == 2) start_norm<T, 16, 2>(a, stream);
+  else if (nw == 16) start_norm<T, 16, 16 / Wide<T>::N>(a, stream);   // (four pieces: float32 alone)
   else hipLaunchKernelGGL(norm_long_kernel<T>, dim3(a.rows < 512 ? a.rows : 512), dim3(1024), 0, stream, a);
   return hipGetLastError();
 }
@@ -647,8 +662,9 @@ hipError_t launch_grad_type(const NormGradArgs& a, const Pieces& p, hipStream_t 
   else if (nw == 1 && ch == 2) start_grad<T, 1, 2, KEPT>(a, p, stream);
   else if (nw == 1 && ch == 4) start_grad<T, 1, 4, KEPT>(a, p, stream);
   else if (nw == 4 && ch == 2) start_grad<T, 4, 2, KEPT>(a, p, stream);
-  else if (nw == 4) start_grad<T, 4, 4, KEPT>(a, p, stream);
-  else if (nw == 16) start_grad<T, 16, 16 / Wide<T>::N, KEPT>(a, p, stream);
+  else if (nw == 8 && ch == 2) start_grad<T, 8, 2, KEPT>(a, p, stream);
+  else if (nw == 8 && ch == 4) start_grad<T, 8, 4, KEPT>(a, p, stream);
+  else if (nw == 8) start_grad<T, 8, 32 / Wide<T>::N, KEPT>(a, p, stream);   // (eight pieces: float32 alone)
   else {
     // (the weights' gradients first: dx may be dy)
     if (a.dweight != nullptr || a.dbias != nullptr) {
@@ -662,8 +678,9 @@ hipError_t launch_grad_type(const NormGradArgs& a, const Pieces& p, hipStream_t 
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || (a.dweight == nullptr && a.dbias == nullptr)) return e;
-  hipLaunchKernelGGL(norm_grad_join_kernel, dim3(ceil_div(2LL * a.width, 64), a.m), dim3(256), 0, stream, p, a.offsets, a.rows, a.width,
-                     a.dweight, a.dbias, a.ldw, a.ldb);
+  const int waves = p.chunks / a.m > 32 ? kJoinWaves : 4;   // (170 slots for four waves: 20 us)
+  hipLaunchKernelGGL(norm_grad_join_kernel, dim3(ceil_div(2LL * a.width, 64), a.m), dim3(64 * waves), 0, stream, p, a.offsets, a.rows,
+                     a.width, a.dweight, a.dbias, a.ldw, a.ldb);
   return hipGetLastError();
 }
 
