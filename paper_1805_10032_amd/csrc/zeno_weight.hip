@@ -686,8 +686,19 @@ Plan plan_for(int rows, int out, int width, int m) {
     return p;
   }
   p.shape = kMid;
-  if (out > MidTile<1>::OUT && width > MidTile<1>::IN && tiles_of<WideTile<1>>(out, width) * m >= 256 && rows / m >= 64) p.shape = kWide;
-  const long long pieces = p.shape == kWide ? 1 : 768 / (tiles_of<MidTile<1>>(out, width) * m), most = rows / m / 128;
+  if (out > MidTile<1>::OUT && width > MidTile<1>::IN) {
+    // wide tiles, one for every compute unit at least: as they are, or the tokens cut where they are many (bf16, 16384 tokens,
+    // 4096 x 1024: 154 us with four pieces of wide tiles, 197 with two of 128 x 128)
+    const long long wide = tiles_of<WideTile<1>>(out, width) * m, pieces = (255 + wide) / wide;
+    if (rows / m >= (wide >= 256 ? 64 : 1024 * pieces)) {
+      p.shape = kWide;
+      p.pieces = (int)pieces;
+      return p;
+    }
+  }
+  // two workgroups a compute unit, or one where the output is so small that joining the pieces counts (bf16, 6292 tokens, 64 x 2112: 20.5 us
+  // with 256 workgroups, 24.4 with 512; 8192 tokens, 1000 x 1024: 44.0 and 42.5)
+  const long long tiles = tiles_of<MidTile<1>>(out, width) * m, pieces = (tiles < 64 ? 256 : 512) / tiles, most = rows / m / 128;
   p.pieces = (int)std::max(1LL, std::min(pieces, most));
   return p;
 }
