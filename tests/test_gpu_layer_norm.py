@@ -17,9 +17,9 @@ def B():
 
 
 def chain(width, per_load):
-    """Longest chain of additions over a row: a thread's pieces (four at most, or the long kernel's share of 1024 threads), the wave's
+    """Longest chain of additions over a row: a thread's values (32 at most, or the long kernel's share of 1024 threads), the wave's
     six steps, sixteen waves."""
-    return max(4 * per_load, int(np.ceil(width / (1024 * per_load))) * per_load) + 6 + 16
+    return max(32, int(np.ceil(width / (1024 * per_load))) * per_load) + 6 + 16
 
 
 def make(rows, width, ty, seed, pitch=None, offset=0, shift=0.1):
@@ -160,6 +160,22 @@ def test_groups(B, rows, width, ty, ckpt):
     assert (dx[:3] == 5).all() and (dx[rows - 5:] == 5).all()
     again = check_backward(B, x, weight, off, ckpt)
     assert torch.equal(again[1], dw) and torch.equal(again[2], db)      # the same bits every time
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("rows,width,ty,extra,offset", [
+    (1100, 4100, "fp32", 0, 0), (1500, 4099, "bf16", 1, 1), (1030, 6144, "bf16", 0, 0), (530, 8192, "fp32", 0, 0),
+    (600, 8200, "bf16", 0, 0), (580, 12001, "fp16", 0, 3), (300, 16384, "bf16", 8, 0), (520, 12288, "fp32", 0, 0),
+    (270, 16383, "fp32", 2, 1)])
+def test_wide_rows(B, rows, width, ty, extra, offset, ckpt):
+    """Several rows a workgroup at every number of waves and pieces a row, with groups that end inside a chunk, also in place."""
+    x, _, weight, bias, g = make(rows, width, ty, rows + width, width + extra, offset)
+    check_forward(B, x, weight, bias, ckpt=ckpt)
+    off = [1, rows // 2, rows // 2, rows // 2 + 2, rows]
+    dy = torch.randn(rows, width, generator=g).to(x.dtype).cuda()
+    dx, dw, db = check_backward(B, x, weight, off, ckpt, dy=dy)
+    inplace = check_backward(B, x, weight, off, ckpt, dy=dy, dx=dy)
+    assert inplace[0] is dy and torch.equal(dy[1:], dx[1:]) and torch.equal(inplace[1], dw) and torch.equal(inplace[2], db)
 
 
 def test_many_groups(B):
