@@ -254,6 +254,7 @@ zeno_status_t zeno_krum(const float* G, int64_t ldg, int32_t m, int64_t d, int32
  *
  * Activations, logits and their gradients are matrices of `dtype`, rows a given number of elements apart (>= the row's length),
  * aligned to their element; any row length and any pitch is accepted, and pitches that are a multiple of 16 bytes are fastest.
+ * More than ZENO_MAX_ROWS rows are UNSUPPORTED.
  * Sums, statistics and parameters are float32.  A result in 16 bits is rounded once, from float32.
  * Groups.  The rows of a batch belong to m workers: rows offsets[g] .. offsets[g+1]-1 to worker g.  `offsets` is DEVICE int32
  *   [m+1], ascending, within 0..rows; NULL: all rows belong to one group (m = 1).  Groups may be empty: their gradients are zero.
@@ -266,6 +267,7 @@ typedef enum { ZENO_F32 = 0, ZENO_BF16 = 1, ZENO_F16 = 2 } zeno_dtype_t;
 
 #define ZENO_MAX_TOP 32           /* alternatives per token */
 #define ZENO_MAX_VOCAB (1 << 30)
+#define ZENO_MAX_ROWS (1 << 30)   /* tokens of a call */
 #define ZENO_MAX_WIDTH (1 << 24)  /* columns of activations */
 
 /* Log probabilities of given tokens, entropy and the most probable tokens of every row of logits z:

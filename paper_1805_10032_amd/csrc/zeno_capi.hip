@@ -1114,7 +1114,7 @@ zeno_status_t zeno_krum(const float* G, int64_t ldg, int32_t m, int64_t d, int32
 // ---- models that answer with tokens
 
 size_t zeno_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
-  if (rows < 0 || vocab < 1 || vocab > ZENO_MAX_VOCAB || top < 0 || top > ZENO_MAX_TOP || top > vocab) return 0;
+  if (rows < 0 || rows > ZENO_MAX_ROWS || vocab < 1 || vocab > ZENO_MAX_VOCAB || top < 0 || top > ZENO_MAX_TOP || top > vocab) return 0;
   return logprobs_workspace_bytes(rows, vocab, top);
 }
 
@@ -1122,7 +1122,7 @@ zeno_status_t zeno_logprobs(const void* logits, int64_t ldz, int32_t dtype, int3
                             float* logp, float* entropy, float* stats, int32_t top, int32_t* top_index, float* top_logp,
                             void* workspace, size_t workspace_bytes, void* stream) {
   if (!matrix_ok(logits, ldz, dtype, rows, vocab) || top < 0 || top > vocab) return ZENO_ERR_INVALID_ARG;
-  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB) return ZENO_ERR_UNSUPPORTED;
+  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (logp == nullptr && entropy == nullptr && stats == nullptr && top == 0) return ZENO_ERR_INVALID_ARG;
   if ((logp != nullptr && labels == nullptr && rows > 0) || (top > 0 && rows > 0 && (top_index == nullptr || top_logp == nullptr)))
     return ZENO_ERR_INVALID_ARG;
@@ -1145,7 +1145,7 @@ zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dt
                                      void* dlogits, int64_t ldd, void* stream) {
   if (!matrix_ok(logits, ldz, dtype, rows, vocab) || !matrix_ok(dlogits, ldd, dtype, rows, vocab)) return ZENO_ERR_INVALID_ARG;
   if (top < 0 || top > vocab) return ZENO_ERR_INVALID_ARG;
-  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB) return ZENO_ERR_UNSUPPORTED;
+  if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (rows == 0) return ZENO_OK;
   if (grad_logp == nullptr && grad_entropy == nullptr && grad_top == nullptr) return ZENO_ERR_INVALID_ARG;
   if (stats == nullptr || (grad_logp != nullptr && labels == nullptr) || (grad_entropy != nullptr && entropy == nullptr))
@@ -1166,7 +1166,7 @@ zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dt
 zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, uint8_t* values,
                               uint8_t* scales, void* stream) {
   if (!matrix_ok(x, ldx, dtype, rows, width) || !checkpoint_ok(values, scales, rows)) return ZENO_ERR_INVALID_ARG;
-  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (width > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (rows == 0) return ZENO_OK;
   ProfScope ps(ZENO_KERNEL_CHECKPOINT, 0, (double)rows * width * (dtype_bytes(dtype) + 33.0 / 32), reinterpret_cast<hipStream_t>(stream));
   ZENO_TRY(launch_checkpoint(x, ldx, dtype, rows, width, values, scales, reinterpret_cast<hipStream_t>(stream)));
@@ -1176,7 +1176,7 @@ zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t
 zeno_status_t zeno_checkpoint_values(const uint8_t* values, const uint8_t* scales, int32_t rows, int32_t width, int32_t dtype,
                                      void* out, int64_t ldo, void* stream) {
   if (!matrix_ok(out, ldo, dtype, rows, width) || !checkpoint_ok(values, scales, rows)) return ZENO_ERR_INVALID_ARG;
-  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (width > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (rows == 0) return ZENO_OK;
   ProfScope ps(ZENO_KERNEL_CHECKPOINT, 0, (double)rows * width * (dtype_bytes(dtype) + 33.0 / 32), reinterpret_cast<hipStream_t>(stream));
   ZENO_TRY(launch_checkpoint_values(values, scales, rows, width, dtype, out, ldo, reinterpret_cast<hipStream_t>(stream)));
@@ -1190,7 +1190,7 @@ zeno_status_t zeno_layer_norm(const void* x, int64_t ldx, int32_t dtype, int32_t
   if (weight == nullptr || !std::isfinite(eps) || !(eps > 0.f)) return ZENO_ERR_INVALID_ARG;
   if (!aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return ZENO_ERR_INVALID_ARG;
   if ((values != nullptr) != (scales != nullptr) || !aligned(values, 16)) return ZENO_ERR_INVALID_ARG;
-  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (width > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (rows == 0) return ZENO_OK;
   const NormArgs a = {x, y, ldx, ldy, dtype, rows, width, weight, bias, eps, mean, rstd, values, scales};
   ProfScope ps(ZENO_KERNEL_LAYER_NORM, 0,
@@ -1201,7 +1201,7 @@ zeno_status_t zeno_layer_norm(const void* x, int64_t ldx, int32_t dtype, int32_t
 }
 
 size_t zeno_layer_norm_workspace_bytes(int32_t rows, int32_t width, int32_t m) {
-  if (rows < 0 || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
+  if (rows < 0 || rows > ZENO_MAX_ROWS || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
   return layer_norm_workspace_bytes(rows, width, m);
 }
 
@@ -1221,7 +1221,7 @@ zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dty
   if ((dweight != nullptr && ldw < width) || (dbias != nullptr && ldb < width)) return ZENO_ERR_INVALID_ARG;
   if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
     return ZENO_ERR_INVALID_ARG;
-  if (width > ZENO_MAX_WIDTH) return ZENO_ERR_UNSUPPORTED;
+  if (width > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layer_norm_workspace_bytes(rows, width, m))
     return ZENO_ERR_WORKSPACE;
   const NormGradArgs a = {dy,    x,    values, scales, dx, lddy,    ldx,     lddx,  dtype, rows, width,
@@ -1235,7 +1235,7 @@ zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dty
 }
 
 size_t zeno_weight_gradient_workspace_bytes(int32_t rows, int32_t out, int32_t width, int32_t m) {
-  if (rows < 0 || out < 1 || out > ZENO_MAX_WIDTH || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
+  if (rows < 0 || rows > ZENO_MAX_ROWS || out < 1 || out > ZENO_MAX_WIDTH || width < 1 || width > ZENO_MAX_WIDTH || m < 1 || m > ZENO_MAX_CANDIDATES) return 0;
   return weight_gradient_workspace_bytes(rows, out, width, m);
 }
 
@@ -1246,7 +1246,7 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
     return ZENO_ERR_INVALID_ARG;
   if (dweight == nullptr || ldw < (int64_t)out * width || (dbias != nullptr && ldb < out)) return ZENO_ERR_INVALID_ARG;
   if (!aligned(dweight, 4) || !aligned(dbias, 4)) return ZENO_ERR_INVALID_ARG;
-  if (width > ZENO_MAX_WIDTH || out > ZENO_MAX_WIDTH || !weight_gradient_fits(out, width)) return ZENO_ERR_UNSUPPORTED;
+  if (width > ZENO_MAX_WIDTH || out > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS || !weight_gradient_fits(out, width)) return ZENO_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < weight_gradient_workspace_bytes(rows, out, width, m))
     return ZENO_ERR_WORKSPACE;
   const WeightGradArgs a = {dy, lddy, dtype, rows, out, width, values, scales, m, offsets, dweight, dbias, ldw, ldb};

@@ -1,0 +1,145 @@
+"""The operators for models that answer with tokens at the ends of their ranges: rows far apart, offsets past 2^31, more rows than a
+launch has workgroups, the most groups.  What such a call gives has to be, bit for bit, what the same rows give close together, or sums
+of small whole numbers, which float32 holds exactly."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1805_10032_amd import binding
+    binding.load_library()
+    return binding
+
+
+def far(x, pitch):
+    """The same rows `pitch` elements apart, in memory that is not cleared."""
+    buf = torch.empty((x.shape[0] - 1) * pitch + x.shape[1], dtype=x.dtype, device="cuda")
+    out = buf.as_strided(x.shape, (pitch, 1))
+    out.copy_(x)
+    return out
+
+
+def whole(shape, gen, most=2):
+    return torch.randint(-most, most + 1, shape, generator=gen).float()
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("vocab", [10, 300, 9000])
+def test_logits_far_apart(B, vocab, ty):
+    g = torch.Generator().manual_seed(vocab)
+    z = torch.randn(7, vocab, generator=g).to(TYPES[ty]).cuda()
+    lab = torch.randint(0, vocab, (7,), generator=g, dtype=torch.int32).cuda()
+    z2 = far(z, (1 << 29) + 1)
+    one, two = (B.zeno_logprobs(q, lab, top=3, want_entropy=True, want_stats=True) for q in (z, z2))
+    for a, b in zip(one, two):
+        assert torch.equal(a, b)
+    h = torch.randn(7, generator=g).cuda()
+    d = B.zeno_logprobs_backward(z, one[2], labels=lab, grad_logp=h, entropy=one[1], grad_entropy=h)
+    d2 = B.zeno_logprobs_backward(z2, one[2], labels=lab, grad_logp=h, entropy=one[1], grad_entropy=h, out=z2)
+    assert torch.equal(d, d2)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("width", [33, 4100, 17000])
+def test_activations_far_apart(B, width, ty):
+    g = torch.Generator().manual_seed(width)
+    x, dy = (torch.randn(7, width, generator=g).to(TYPES[ty]).cuda() for _ in range(2))
+    w, b = torch.randn(width, generator=g).cuda(), torch.randn(width, generator=g).cuda()
+    x2, dy2 = far(x, (1 << 29) + 3), far(dy, (1 << 29) + 5)
+    y, mean, rstd, ck = B.zeno_layer_norm(x, w, b, want_checkpoint=True)
+    y2, mean2, rstd2, ck2 = B.zeno_layer_norm(x2, w, b, want_checkpoint=True, y=far(x, (1 << 29) + 7))
+    assert torch.equal(y, y2) and torch.equal(mean, mean2) and torch.equal(rstd, rstd2)
+    assert torch.equal(ck.values, ck2.values) and torch.equal(ck.scales, ck2.scales)
+    alone = B.zeno_checkpoint(x2)
+    assert torch.equal(ck.values, alone.values) and torch.equal(ck.scales, alone.scales)
+    assert torch.equal(B.zeno_checkpoint_values(ck, x.dtype), B.zeno_checkpoint_values(ck, x.dtype, out=y2))
+    off = torch.tensor([0, 2, 7], dtype=torch.int32, device="cuda")
+    one, two = (B.zeno_layer_norm_backward(d, q, mean, rstd, w, groups=off, dx=o)
+                for d, q, o in ((dy, x, None), (dy2, x2, dy2)))
+    for p, q in zip(one, two):
+        assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("out,width", [(10, 100), (130, 300)])
+def test_gradients_far_apart(B, out, width, ty):
+    g = torch.Generator().manual_seed(out)
+    rows = 40
+    dy, a = whole((rows, out), g).to(TYPES[ty]).cuda(), whole((rows, width), g).cuda()
+    ck = B.zeno_checkpoint(a)
+    off = torch.tensor([1, 33, 40], dtype=torch.int32, device="cuda")
+    dw, db = B.zeno_weight_gradient(far(dy, (1 << 27) + 1), ck, groups=off)
+    for i, (p, q) in enumerate(((1, 33), (33, 40))):
+        assert torch.equal(dw[i].double().cpu(), (dy[p:q].double().cpu().T @ a[p:q].double().cpu()).reshape(-1))
+        assert torch.equal(db[i].double().cpu(), dy[p:q].double().cpu().sum(0))
+
+
+def test_a_checkpoint_past_32_bits(B):
+    rows, width, last = 70001, 32768, 90
+    g = torch.Generator().manual_seed(1)
+    ck = B.alloc_checkpoint(rows, width)
+    x = whole((last, width), g).bfloat16().cuda()
+    end = B.zeno_checkpoint(x, out=B.Checkpoint(ck.values[-last:], ck.scales[-last:], width))
+    everything = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(B.zeno_checkpoint_values(ck, torch.bfloat16, out=everything)[-last:], x)
+    dy = torch.zeros(rows, 40, dtype=torch.bfloat16, device="cuda")
+    dy[-last:] = whole((last, 40), g).bfloat16().cuda()
+    off = torch.tensor([rows - last, rows], dtype=torch.int32, device="cuda")
+    want = dy[-last:].double().cpu().T @ x.double().cpu()
+    for out in (3, 40):
+        dw, _ = B.zeno_weight_gradient(dy[:, :out], ck, groups=off)
+        assert torch.equal(dw[0].double().cpu().reshape(out, width), want[:out])
+    ck.values[-last:] = 0
+    ck.scales[-last:] = 0
+    again = B.zeno_checkpoint(everything, out=ck)
+    assert torch.equal(again.values[-last:], B.zeno_checkpoint(x).values) and torch.equal(again.scales[-last:], B.zeno_checkpoint(x).scales)
+    w = torch.ones(width, device="cuda")
+    _, mean, rstd, _ = B.zeno_layer_norm(x, w)
+    allmean, allrstd = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    allmean[-last:], allrstd[-last:] = mean, rstd
+    d = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    d[-last:] = x.flip(1)
+    got, gw, gb = B.zeno_layer_norm_backward(d, ck, allmean, allrstd, w, groups=off, dx=everything)
+    one, ow, ob = B.zeno_layer_norm_backward(x.flip(1).contiguous(), end, mean, rstd, w)
+    assert torch.equal(got[-last:], one) and torch.equal(gb, ob)
+    # (the rows are cut into other chunks: as many additions of the same products, in another order)
+    assert ((gw - ow).abs() <= 2 * last * 2.0 ** -24 * 4 * last * 10).all()
+
+
+def test_more_rows_than_workgroups(B):
+    """A launch has 2^20 workgroups at most and goes over the rows in steps."""
+    rows = (1 << 22) + 5000
+    g = torch.Generator().manual_seed(2)
+    for vocab in (3, 260):
+        z = torch.zeros(rows, vocab, dtype=torch.bfloat16, device="cuda")
+        lab = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+        tail = torch.randn(4999, vocab, generator=g).bfloat16().cuda()
+        z[-4999:] = tail
+        lab[-4999:] = 2
+        got = B.zeno_logprobs(z, lab, top=2, want_entropy=True, want_stats=True)
+        want = B.zeno_logprobs(tail, lab[-4999:], top=2, want_entropy=True, want_stats=True)
+        for p, q in zip(got, want):
+            assert torch.equal(p[-4999:], q)
+        assert not got[0][:-4999].any() and (got[3][:-4999, 1] == 1).all()
+        h = torch.ones(rows, device="cuda")
+        d = B.zeno_logprobs_backward(z, got[2], labels=lab, grad_logp=h, out=z)
+        assert torch.equal(d[-4999:], B.zeno_logprobs_backward(tail, want[2], labels=lab[-4999:], grad_logp=h[-4999:]))
+        assert not d[:-4999].any()
+
+
+@pytest.mark.parametrize("out,width", [(10, 64), (70, 96)])
+def test_the_most_groups(B, out, width):
+    g = torch.Generator().manual_seed(3)
+    rows, m = 700, 1024
+    dy, a = whole((rows, out), g).cuda(), whole((rows, width), g).cuda()
+    cuts = torch.sort(torch.randint(0, rows + 1, (m + 1,), generator=g)).values
+    G = torch.full((m, out * width + out), 7.0, device="cuda")
+    B.zeno_weight_gradient(dy, B.zeno_checkpoint(a), groups=cuts.int().cuda(), dweight=G[:, :out * width], dbias=G[:, out * width:])
+    for i in range(m):
+        p, q = int(cuts[i]), int(cuts[i + 1])
+        assert torch.equal(G[i, :out * width].reshape(out, width), dy[p:q].T @ a[p:q] if q > p else torch.zeros(out, width, device="cuda"))
+        assert torch.equal(G[i, out * width:], dy[p:q].sum(0))

@@ -79,6 +79,18 @@ def test_refused(B, name, status, changes):
     assert getattr(B.load_library(), name)(*args.values()) == status
 
 
+@pytest.mark.parametrize("name", [n for n in CALLS if "rows" in CALLS[n]])
+def test_rows_beyond_the_most(B, name):
+    """Row numbers keep room for a kernel's step in 32 bits."""
+    for rows in ((1 << 30) + 1, (1 << 31) - 1):
+        assert getattr(B.load_library(), name)(*dict(CALLS[name], rows=rows).values()) == UNSUPPORTED
+    lib = B.load_library()
+    rows = (1 << 30) + 1
+    assert lib.zeno_logprobs_workspace_bytes(rows, 10, 0) == 0 and lib.zeno_layer_norm_workspace_bytes(rows, 4, 1) == 0
+    assert lib.zeno_weight_gradient_workspace_bytes(rows, 4, 4, 1) == 0
+    assert lib.zeno_logprobs_workspace_bytes(rows - 1, 10, 0) > 0 and lib.zeno_layer_norm_workspace_bytes(rows - 1, 4, 1) > 0
+
+
 def test_calls_without_rows_need_no_memory(B):
     lib = B.load_library()
     none = {"zeno_logprobs": dict(rows=0, logits=None, labels=None, logp=None, top_index=None, top_logp=None, workspace_bytes=1 << 20),
