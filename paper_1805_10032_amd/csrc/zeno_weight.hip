@@ -577,13 +577,14 @@ __global__ __launch_bounds__(kThreads, EACH > 8 ? 1 : 2) void weight_grad_few_ke
     for (int i = 0; i < EACH; ++i) {
       const int e = 64 * i + lane, t = token_of(i), o = e - t * a.out;
       float rest = t < n ? from_bits<T>(now.dy[i]) : 0.f;
-      const bool finite = fabsf(rest) < __builtin_inff();
+      const bool infinite = fabsf(rest) == __builtin_inff();
       if (e < elements) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const unsigned bits = __float_as_uint(rest);
           *reinterpret_cast<uint16_t*>(&st.y[p][t * kFewPitchO + o]) = (uint16_t)(bits >> 16);
-          rest = finite ? rest - __uint_as_float(bits & 0xffff0000u) : (rest != rest ? rest : 0.f);
+          // (infinity less itself would be NaN; a NaN whose bits the first piece loses is one in the next)
+          rest = infinite ? 0.f : rest - __uint_as_float(bits & 0xffff0000u);
         }
       }
     }

@@ -132,3 +132,16 @@ def test_no_rows_and_no_bias(B):
     dw, db = B.zeno_weight_gradient(dy, ck)
     only, none = B.zeno_weight_gradient(dy, ck, want_bias=False)
     assert none is None and torch.equal(only, dw)
+
+
+@pytest.mark.parametrize("out", [3, 40, 300])
+def test_every_nan_stays_one(B, out):
+    """A float32 NaN whose payload lies in the lower half: its leading bits alone are those of an infinity."""
+    dy = torch.ones(70, out)
+    dy[5, 2] = torch.tensor([0x7f800001], dtype=torch.int32).view(torch.float32)
+    dy = dy.cuda()
+    dw, db = B.zeno_weight_gradient(dy, B.zeno_checkpoint(torch.ones(70, 300, device="cuda")))
+    dw = dw.reshape(out, 300)
+    assert torch.isnan(dw[2]).all() and torch.isnan(db[0, 2])
+    keep = [o for o in range(out) if o != 2]
+    assert (dw[keep] == 70).all() and (db[0, keep] == 70).all()
