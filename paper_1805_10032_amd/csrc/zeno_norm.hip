@@ -12,8 +12,6 @@
 namespace zeno {
 namespace {
 
-constexpr int kMaxGrid = 1 << 20;
-
 // NW waves for a row; a workgroup has four waves at least, of which one-wave rows use one each.
 template <int NW>
 struct Shape {
@@ -72,8 +70,20 @@ __device__ inline void store_cols(T* row, int col, int width, const float (&v)[W
 }
 template <int N>
 __device__ inline void load_params(const float* p, int col, int width, float (&v)[N]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+  if (p != nullptr && col + N <= width) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = p != nullptr && col + j < width ? p[col + j] : 0.f;
+    for (int j = 0; j < N; j += 4) {
+      const f4 q = *reinterpret_cast<const f4*>(p + col + j);
+      v[j] = q.x;
+      v[j + 1] = q.y;
+      v[j + 2] = q.z;
+      v[j + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = p != nullptr && col + j < width ? p[col + j] : 0.f;
+  }
 }
 
 // The 8-bit copy of N columns of a row (a block's columns lie in neighbouring lanes).  Every lane of the wave takes part.
@@ -237,44 +247,64 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
   }
 }
 
+// The pieces of a row that 1024 threads go over: f(column, whole), whole pieces four at a time so that their loads are on their way
+// together, then the one that the row's end cuts.
+template <int N, typename F>
+__device__ inline void over_row(int width, int tid, F f) {
+  constexpr int TPR = 1024;
+  const int whole = width / (TPR * N);
+#pragma unroll 4
+  for (int c = 0; c < whole; ++c) f((c * TPR + tid) * N, std::true_type());
+  if (whole * TPR * N < width) f((whole * TPR + tid) * N, std::false_type());
+}
+template <bool WHOLE, typename T>
+__device__ inline void load_cols(const T* row, int col, int width, float (&v)[Wide<T>::N]) {
+  if (WHOLE)
+    load_wide(row + col, v);
+  else
+    load_cols(row, col, width, v);
+}
+
 // Rows too wide for the registers: read once for the mean, once for the variance and once for the result, from the caches
 // where they hold the row.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
-  constexpr int N = Wide<T>::N, TPR = 1024;
+  constexpr int N = Wide<T>::N;
   __shared__ float buf[2][16][2];
   const int tid = threadIdx.x, wave = tid / 64;
-  const int blocks = ckpt_blocks(a.width), iters = (a.width + TPR * N - 1) / (TPR * N);
+  const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
-    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy;
-    float v[N], w[N], b[N], sum = 0.f, sq = 0.f;
-    for (int c = 0; c < iters; ++c) {
-      load_cols(x, (c * TPR + tid) * N, a.width, v);
+    const T* __restrict__ x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
+    T* __restrict__ y = reinterpret_cast<T*>(a.y) + row * a.ldy;
+    float sum = 0.f, sq = 0.f;
+    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+      float v[N];
+      load_cols<decltype(whole)::value>(x, col, a.width, v);
 #pragma unroll
       for (int j = 0; j < N; ++j) sum += v[j];
-    }
+    });
     const float mean = row_sum1<16>(sum, buf[0], wave) * inv;
-    for (int c = 0; c < iters; ++c) {
-      load_cols(x, (c * TPR + tid) * N, a.width, v);
+    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+      float v[N];
+      load_cols<decltype(whole)::value>(x, col, a.width, v);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const float d = v[j] - mean;
-        if ((c * TPR + tid) * N + j < a.width) sq = fmaf(d, d, sq);
+        if (decltype(whole)::value || col + j < a.width) sq = fmaf(d, d, sq);
       }
-    }
+    });
     const float rstd = 1.f / sqrtf(row_sum1<16>(sq, buf[1], wave) * inv + a.eps);
-    for (int c = 0; c < iters; ++c) {
-      const int col = (c * TPR + tid) * N;
-      load_cols(x, col, a.width, v);
+    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+      float v[N], w[N], b[N];
+      load_cols<decltype(whole)::value>(x, col, a.width, v);
       if (a.values != nullptr) keep_cols<N>(v, col, a.width, blocks, a.values, a.scales, row);
       load_params(a.weight, col, a.width, w);
       load_params(a.bias, col, a.width, b);
 #pragma unroll
       for (int j = 0; j < N; ++j) v[j] = fmaf((v[j] - mean) * rstd, w[j], b[j]);
       store_cols(y, col, a.width, v);
-    }
+    });
     if (tid == 0) {
       if (a.mean != nullptr) a.mean[row] = mean;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -301,11 +331,11 @@ __device__ inline int first_group(const int32_t* offsets, int m, int row, int ro
 }
 
 // xh of N columns, from the row itself or from its checkpoint
-template <typename T, bool KEPT>
+template <typename T, bool KEPT, bool WHOLE>
 __device__ inline void load_xh(const NormGradArgs& a, long long row, int col, int blocks, float mean, float rstd, float (&v)[Wide<T>::N]) {
   constexpr int N = Wide<T>::N;
   if (KEPT) {
-    if (col < blocks * kCkptBlock) {
+    if (WHOLE || col < blocks * kCkptBlock) {
       unsigned words[N / 4];
       const uint8_t* p = a.values + row * ((long long)blocks * kCkptBlock) + col;
 #pragma unroll
@@ -316,7 +346,7 @@ __device__ inline void load_xh(const NormGradArgs& a, long long row, int col, in
       for (int j = 0; j < N; ++j) v[j] = 0.f;
     }
   } else {
-    load_cols(reinterpret_cast<const T*>(a.x) + row * a.ldx, col, a.width, v);
+    load_cols<WHOLE>(reinterpret_cast<const T*>(a.x) + row * a.ldx, col, a.width, v);
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) v[j] = (v[j] - mean) * rstd;
@@ -490,10 +520,10 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
 // Rows too wide for the registers: dx from two reads of the row ...
 template <typename T, bool KEPT>
 __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a) {
-  constexpr int N = Wide<T>::N, TPR = 1024;
+  constexpr int N = Wide<T>::N;
   __shared__ float buf[2][16][2];
   const int tid = threadIdx.x, wave = tid / 64;
-  const int blocks = ckpt_blocks(a.width), iters = (a.width + TPR * N - 1) / (TPR * N);
+  const int blocks = ckpt_blocks(a.width);
   const float inv = 1.f / (float)a.width;
   const int first = group_offset(a.offsets, 0, a.rows), last = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
   int parity = 0;
@@ -501,35 +531,51 @@ __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a)
     const float mean = a.mean[row], rstd = a.rstd[row];
     const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.lddy;
     T* dx = reinterpret_cast<T*>(a.dx) + row * a.lddx;
-    float xh[N], d[N], w[N], c1 = 0.f, c2 = 0.f;
-    for (int c = 0; c < iters; ++c) {
-      const int col = (c * TPR + tid) * N;
-      load_cols(dy, col, a.width, d);
-      load_xh<T, KEPT>(a, row, col, blocks, mean, rstd, xh);
+    float c1 = 0.f, c2 = 0.f;
+    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+      float xh[N], d[N], w[N];
+      load_cols<decltype(whole)::value>(dy, col, a.width, d);
+      load_xh<T, KEPT, decltype(whole)::value>(a, row, col, blocks, mean, rstd, xh);
       load_params(a.weight, col, a.width, w);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         c1 = fmaf(d[j], w[j], c1);
         c2 = fmaf(d[j] * w[j], xh[j], c2);
       }
-    }
+    });
     row_sums2<16>(c1, c2, buf[parity], wave);
     parity ^= 1;
     c1 *= inv;
     c2 *= inv;
-    for (int c = 0; c < iters; ++c) {
-      const int col = (c * TPR + tid) * N;
-      load_cols(dy, col, a.width, d);
-      load_xh<T, KEPT>(a, row, col, blocks, mean, rstd, xh);
+    // (dx may be dy: a piece's loads come before its store)
+    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+      float xh[N], d[N], w[N];
+      load_cols<decltype(whole)::value>(dy, col, a.width, d);
+      load_xh<T, KEPT, decltype(whole)::value>(a, row, col, blocks, mean, rstd, xh);
       load_params(a.weight, col, a.width, w);
 #pragma unroll
       for (int j = 0; j < N; ++j) d[j] = rstd * (d[j] * w[j] - fmaf(xh[j], c2, c1));
       store_cols(dx, col, a.width, d);
-    }
+    });
   }
 }
 
-// ... and the weights' gradients by columns: 1024 threads' columns of the rows of a chunk.
+// ... and the weights' gradients by columns: 1024 threads' columns of the rows of a chunk, four rows on their way together.
+template <typename T, bool KEPT, bool WHOLE>
+__device__ inline void long_weights(const NormGradArgs& a, int lo, int hi, int col, int blocks, float (&dw)[Wide<T>::N], float (&db)[Wide<T>::N]) {
+  constexpr int N = Wide<T>::N;
+#pragma unroll 4
+  for (int row = lo; row < hi; ++row) {
+    float d[N], xh[N];
+    load_cols<WHOLE>(reinterpret_cast<const T*>(a.dy) + (long long)row * a.lddy, col, a.width, d);
+    load_xh<T, KEPT, WHOLE>(a, row, col, blocks, a.mean[row], a.rstd[row], xh);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      db[j] += d[j];
+      dw[j] = fmaf(d[j], xh[j], dw[j]);
+    }
+  }
+}
 template <typename T, bool KEPT>
 __global__ __launch_bounds__(1024) void norm_grad_long_weights_kernel(NormGradArgs a, Pieces p) {
   constexpr int N = Wide<T>::N;
@@ -541,18 +587,13 @@ __global__ __launch_bounds__(1024) void norm_grad_long_weights_kernel(NormGradAr
     if (begin >= r1) break;
     const int lo = begin > r0 ? begin : r0, hi = end < r1 ? end : r1;
     if (lo >= hi) continue;
-    float dw[N], db[N], d[N], xh[N];
+    float dw[N], db[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) dw[j] = db[j] = 0.f;
-    for (long long row = lo; row < hi; ++row) {
-      load_cols(reinterpret_cast<const T*>(a.dy) + row * a.lddy, col, a.width, d);
-      load_xh<T, KEPT>(a, row, col, blocks, a.mean[row], a.rstd[row], xh);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        db[j] += d[j];
-        dw[j] = fmaf(d[j], xh[j], dw[j]);
-      }
-    }
+    if (col + N <= a.width)
+      long_weights<T, KEPT, true>(a, lo, hi, col, blocks, dw, db);
+    else
+      long_weights<T, KEPT, false>(a, lo, hi, col, blocks, dw, db);
     float* out = p.partial + (long long)(blockIdx.x + g) * 2 * a.width;
 #pragma unroll
     for (int j = 0; j < N; ++j)
