@@ -3,8 +3,9 @@
 //   xh = (x - mean) rstd,  y = weight xh + bias,  rstd = 1 / sqrt(var + eps)
 //   a = weight dy,  dx = rstd (a - mean(a) - xh mean(a xh)),  dweight_g = sum_{rows of g} dy xh,  dbias_g = sum dy
 //
-// A row stays in registers between its statistics and its result: x is read once.  Threads own columns, so the weights stay in
-// registers from row to row, and so do the sums of their gradients.
+// A row stays in registers between its statistics and its result: x is read once.  Threads own columns: the weights are read once into LDS,
+// and the sums of their gradients stay in registers from row to row.  The variance is the mean of squared differences from the mean, not
+// the difference of two large sums.
 #include "zeno_tokens.h"
 
 #include <type_traits>
@@ -182,7 +183,9 @@ struct Params {
   }
 };
 
-// The next row is on its way while a row is reduced.
+// The next row is on its way while a row is reduced (the one after it as well: 72 -> 75 us).  Bound by memory and by what a row's two
+// reductions leave idle.  16384 x 4096 bf16 with a checkpoint 68 us (4.9 TB/s; a large copy moves 4.8), without one 51 us (5.3 TB/s);
+// 5003 x 1001 float32 11.5 us (3.5 TB/s), a launch and two round trips; 7634 x 6144 bf16 49 us, with a quarter of the threads idle.
 template <typename T, int NW, int CH>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
   constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
@@ -247,13 +250,13 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
   }
 }
 
-// The pieces of a row that 1024 threads go over: f(column, whole), whole pieces four at a time so that their loads are on their way
+// The pieces of a row that 1024 threads go over: f(column, whole), whole pieces AT_ONCE at a time so that their loads are on their way
 // together, then the one that the row's end cuts.
-template <int N, typename F>
+template <int N, int AT_ONCE, typename F>
 __device__ inline void over_row(int width, int tid, F f) {
   constexpr int TPR = 1024;
   const int whole = width / (TPR * N);
-#pragma unroll 4
+#pragma unroll AT_ONCE
   for (int c = 0; c < whole; ++c) f((c * TPR + tid) * N, std::true_type());
   if (whole * TPR * N < width) f((whole * TPR + tid) * N, std::false_type());
 }
@@ -266,7 +269,7 @@ __device__ inline void load_cols(const T* row, int col, int width, float (&v)[Wi
 }
 
 // Rows too wide for the registers: read once for the mean, once for the variance and once for the result, from the caches
-// where they hold the row.
+// where they hold the row.  2000 x 40000 bf16: 100 us (3.2 TB/s of one read and one write; piece after piece 333 us).
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   constexpr int N = Wide<T>::N;
@@ -278,14 +281,14 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     const T* __restrict__ x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
     T* __restrict__ y = reinterpret_cast<T*>(a.y) + row * a.ldy;
     float sum = 0.f, sq = 0.f;
-    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+    over_row<N, 4>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
       float v[N];
       load_cols<decltype(whole)::value>(x, col, a.width, v);
 #pragma unroll
       for (int j = 0; j < N; ++j) sum += v[j];
     });
     const float mean = row_sum1<16>(sum, buf[0], wave) * inv;
-    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+    over_row<N, 4>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
       float v[N];
       load_cols<decltype(whole)::value>(x, col, a.width, v);
 #pragma unroll
@@ -295,7 +298,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
       }
     });
     const float rstd = 1.f / sqrtf(row_sum1<16>(sq, buf[1], wave) * inv + a.eps);
-    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+    // (one: a checkpoint's blocks are found by exchanges between lanes, which keep their order)
+    over_row<N, 1>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
       float v[N], w[N], b[N];
       load_cols<decltype(whole)::value>(x, col, a.width, v);
       if (a.values != nullptr) keep_cols<N>(v, col, a.width, blocks, a.values, a.scales, row);
@@ -406,6 +410,11 @@ struct GradRow {
   }
 };
 
+//
+// A row's two sums and its result take two passes over its registers, which hold it as it lies in memory: unpacking it twice costs less than
+// the registers of the values.  16384 x 4096 bf16: 78 us from x (5.2 TB/s), 85 us from a checkpoint (4.0 TB/s: fewer bytes, the
+// same work; the vector pipes are busy for 37 %, waves wait for 44 % of their time, at one barrier a row and for the memory); 5003 x 1001 float32
+// 20 us (3.0 TB/s), 313 chunks that each add up four waves' sums.
 template <typename T, int NW, int CH, bool KEPT>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradArgs a, Pieces p) {
   constexpr int N = Wide<T>::N, TPR = Shape<NW>::TPR, RPB = Shape<NW>::RPB;
@@ -517,7 +526,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
   }
 }
 
-// Rows too wide for the registers: dx from two reads of the row ...
+// Rows too wide for the registers: dx from two reads of the row (2000 x 40000 bf16, both kernels and the join: 250 us) ...
 template <typename T, bool KEPT>
 __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a) {
   constexpr int N = Wide<T>::N;
@@ -532,7 +541,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a)
     const T* dy = reinterpret_cast<const T*>(a.dy) + row * a.lddy;
     T* dx = reinterpret_cast<T*>(a.dx) + row * a.lddx;
     float c1 = 0.f, c2 = 0.f;
-    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+    over_row<N, 4>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
       float xh[N], d[N], w[N];
       load_cols<decltype(whole)::value>(dy, col, a.width, d);
       load_xh<T, KEPT, decltype(whole)::value>(a, row, col, blocks, mean, rstd, xh);
@@ -548,7 +557,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a)
     c1 *= inv;
     c2 *= inv;
     // (dx may be dy: a piece's loads come before its store)
-    over_row<N>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
+    over_row<N, 4>(a.width, tid, [&](int col, auto whole) __attribute__((always_inline)) {
       float xh[N], d[N], w[N];
       load_cols<decltype(whole)::value>(dy, col, a.width, d);
       load_xh<T, KEPT, decltype(whole)::value>(a, row, col, blocks, mean, rstd, xh);
@@ -605,7 +614,8 @@ __global__ __launch_bounds__(1024) void norm_grad_long_weights_kernel(NormGradAr
 }
 
 // A group's gradient: its slots.  64 columns (of weights and biases together) a workgroup; a wave takes every so-manieth slot, and the waves'
-// sums are added in their order.
+// sums are added in their order.  33 groups of 1001 columns 4 us, 64 of 4096 (19 MB) 10 us; eight loads a thread on their way instead of four
+// change neither.
 constexpr int kJoinWaves = 16;
 __global__ __launch_bounds__(64 * kJoinWaves) void norm_grad_join_kernel(Pieces p, const int32_t* offsets, int rows, int width,
                                                                          float* __restrict__ dweight, float* __restrict__ dbias,
