@@ -451,11 +451,11 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
 }
 
 // Rows of a few values: sixteen lanes a row, which stays in registers; its alternatives are found one after the other.  65536 rows: 10 float32
-// values 8.5 us, 200 bf16 values 9.7 us (2.7 TB/s), a launch and one round trip to memory; three alternatives of 200 cost 20 us more, two
-// comparisons a value and alternative.
-template <typename T, bool ENT>
+// values 8.4 us, 200 bf16 values 8.8 us (3.0 TB/s), a launch and one round trip to memory; three alternatives of 200 cost 20 us more, a few
+// instructions a value and alternative.
+template <typename T, bool ENT, int PIECES>
 __global__ __launch_bounds__(kThreads) void logprobs_narrow_kernel(LogprobsArgs a) {
-  constexpr int N = Wide<T>::N, PIECES = kNarrow / (16 * N);
+  constexpr int N = Wide<T>::N;
   const int lane = threadIdx.x % 16;
   const float inf = __builtin_inff();
   auto reduce = [](float v, auto f) {
@@ -742,8 +742,12 @@ hipError_t launch_type(const LogprobsArgs& a, const Parts& w, hipStream_t stream
   if (a.vocab <= kNarrow) {
     const int blocks = ceil_div(a.rows, kThreads / 16);
     const dim3 grid(blocks < 8192 ? blocks : 8192);
-    if (a.entropy != nullptr) hipLaunchKernelGGL((logprobs_narrow_kernel<T, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((logprobs_narrow_kernel<T, false>), grid, dim3(kThreads), 0, stream, a);
+    constexpr int MOST = kNarrow / (16 * Wide<T>::N);
+    const bool one = a.vocab <= 16 * Wide<T>::N;   // a piece a lane is all of the row (65536 x 16 float32, sixteen alternatives: 132 -> 42 us)
+    if (one && a.entropy != nullptr) hipLaunchKernelGGL((logprobs_narrow_kernel<T, true, 1>), grid, dim3(kThreads), 0, stream, a);
+    else if (one) hipLaunchKernelGGL((logprobs_narrow_kernel<T, false, 1>), grid, dim3(kThreads), 0, stream, a);
+    else if (a.entropy != nullptr) hipLaunchKernelGGL((logprobs_narrow_kernel<T, true, MOST>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((logprobs_narrow_kernel<T, false, MOST>), grid, dim3(kThreads), 0, stream, a);
     return hipGetLastError();
   }
   const int rpb = wave_rows(a.vocab) ? Shape<1>::ROWS : 1;

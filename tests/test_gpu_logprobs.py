@@ -343,3 +343,19 @@ def test_no_rows(B):
                                                        want_stats=True)
     assert logp.shape == (0,) and index.shape == (0, 3)
     assert B.zeno_logprobs_backward(z, stats, labels=torch.empty(0, dtype=torch.int32, device="cuda"), grad_logp=logp).shape == (0, 50)
+
+
+@pytest.mark.parametrize("vocab,ty", [(15, "fp32"), (64, "fp32"), (65, "fp32"), (127, "bf16"), (128, "fp16"), (129, "bf16"), (255, "fp16"),
+                                      (256, "fp32"), (256, "bf16")])
+def test_few_values(B, vocab, ty):
+    """Rows that sixteen lanes hold, in one piece a lane and in several: masked, tied and broken rows, all the alternatives there are."""
+    z, _, labels, _ = make(70, vocab, ty, 40 + vocab, pitch=vocab + 1, offset=1)
+    z[0, 2:] = float("-inf")
+    z[1, :] = float("-inf")
+    z[2, :] = torch.finfo(z.dtype).min
+    z[3, :] = 0.5
+    z[4, vocab // 2] = float("nan")
+    z[5, vocab - 1] = float("inf")
+    z[6, vocab - 1] = z[6, 0]
+    check_forward(B, z, labels, min(vocab, 32))
+    check_forward(B, z, labels, 1)
