@@ -34,7 +34,10 @@ struct Tile {
   static constexpr int CHUNKS_O = OUT / 8 * KT, CHUNKS_I = IN / 16 * KT;
   static constexpr int CO = (CHUNKS_O + kThreads - 1) / kThreads, CI = (CHUNKS_I + kThreads - 1) / kThreads;
 };
-template <int P, bool ODD = false> using WideTile = Tile<2, 4, 4, P, ODD>;   // 256 x 256
+// 256 x 256, or 128 x 256 with several pieces of dy: half the sums, so that two workgroups share a compute unit and one's first loads and
+// stores run beside the other's products (20 x 100 tokens, 2048 x 2048: float32 129 -> 113 us, fp16 107 -> 98, with events around
+// each launch; 4 x 4096 tokens 377 -> 360 and 254 -> 247).  In bf16 the narrower tile spills and is slower (8 x 2048 tokens, 4096 x 4096: 660 -> 705 us).
+template <int P, bool ODD = false> using WideTile = Tile<2, (P > 1 ? 2 : 4), 4, P, ODD>;
 template <int P, bool ODD = false> using MidTile = Tile<2, 2, 2, P, ODD>;    // 128 x 128
 
 struct Span {
@@ -274,9 +277,9 @@ __device__ inline void multiply(const Operands<S>& f, f32x16 (&acc)[S::FO][S::FI
 }
 
 // Several pieces: a stage has P times the matrix instructions, and holding all its operands twice would take more registers than there
-// are.  The inputs' operands are held for this stage and the next, the outputs' three ahead in a ring of four.
-template <typename S>
-__device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf16x8 (&y)[4], int slot) {
+// are.  The inputs' operands are held for this stage and the next, the outputs' RN - 1 ahead in a ring of RN.
+template <typename S, int RN>
+__device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf16x8 (&y)[RN], int slot) {
   y[slot] = read_columns<S::PITCH_O>(st.y[S::P - 1 - q % S::P], wo + 32 * (q / S::P), 0, lane);   // the smallest piece first
 }
 
@@ -287,9 +290,8 @@ __device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf
 // 8 x 2048 tokens, 4096 x 4096, bf16: 550-590 us (930-1000 TFLOP/s; a large bf16 product of the library with its operands stored this way
 // 1187, stored the other way 1369).  The matrix pipes are busy for 48 % of the time and the clock gives way under them (the same code without
 // memory traffic runs the stream of matrix instructions at 1770-1900 TFLOP/s); waves stand ready but unissued for 39 %.
-// 20 x 100 tokens, 2048 x 2048, float32: 112 us, 2.9 TB/s of gradients written: a tile has seven stages, and its first loads (5 us) and its
-// 256 KB of stores (5 us) run beside nothing, since there is one workgroup a compute unit.  128 x 128 tiles, two workgroups a compute unit:
-// 134 us.
+// 20 x 100 tokens, 2048 x 2048, float32: 102 us, 3.3 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
+// 128 KB of stores where both workgroups of a compute unit are in them.  128 x 128 tiles: 134 us.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kernel(WeightGradArgs a, int tiles_in, int pieces,
                                                                                   float* partial) {
@@ -325,14 +327,15 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       deposit<T, S>(second, stage[1], skip(1), from.shift, tid, sums, bias);
     }
     __syncthreads();
-    constexpr bool RING = S::FO == 4 && S::P > 1;
+    constexpr bool RING = S::FI == 4 && S::P > 1;
+    constexpr int RN = S::FO * S::P % 4 == 0 ? 4 : 3;
     Operands<S> now, next;
-    bf16x8 xa[S::FI], xb[S::FI], ring[4];
+    bf16x8 xa[S::FI], xb[S::FI], ring[RN];
     if constexpr (RING) {
 #pragma unroll
       for (int j = 0; j < S::FI; ++j) xa[j] = read_columns<S::PITCH_I>(stage[0].a, wk + 32 * j, 0, lane);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) read_ring<S>(q, stage[0], wo, lane, ring, q);
+      for (int q = 0; q < RN - 1; ++q) read_ring<S, RN>(q, stage[0], wo, lane, ring, q);
     } else {
       read_operands<S>(stage[0], 0, wo, wk, lane, now);
     }
@@ -384,7 +387,7 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
     auto ring_step = [&](Fetched<T, S>& f, int i, bf16x8 (&x)[S::FI], bf16x8 (&x_next)[S::FI], auto whole) __attribute__((always_inline)) {
       constexpr bool WHOLE = decltype(whole)::value;
       constexpr int GROUPS = S::FO * S::P;
-      static_assert(!RING || GROUPS % 4 == 0, "the ring is where it was at the end of a stage");
+      static_assert(!RING || GROUPS % RN == 0, "the ring is where it was at the end of a stage");
       const int after = at == 2 ? 0 : at + 1, last = after == 2 ? 0 : after + 1;
       const int skipped = skip(i + 2), advance = base(i + 5) - base(i + 4);
       __builtin_amdgcn_sched_barrier(0);
@@ -392,13 +395,14 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
       for (int q = 0; q < GROUPS; ++q) {
         const int r = q / S::P;
 #pragma unroll
-        for (int j = 0; j < S::FI; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[q % 4], x[j], acc[r][j], 0, 0, 0);
-        if (q + 3 < GROUPS) read_ring<S>(q + 3, stage[at], wo, lane, ring, (q + 3) % 4);
-        else read_ring<S>(q + 3 - GROUPS, stage[after], wo, lane, ring, (q + 3) % 4);
+        for (int j = 0; j < S::FI; ++j) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[q % RN], x[j], acc[r][j], 0, 0, 0);
+        if (q + RN - 1 < GROUPS) read_ring<S, RN>(q + RN - 1, stage[at], wo, lane, ring, (q + RN - 1) % RN);
+        else read_ring<S, RN>(q + RN - 1 - GROUPS, stage[after], wo, lane, ring, (q + RN - 1) % RN);
         if (q < S::FI) x_next[q] = read_columns<S::PITCH_I>(stage[after].a, wk + 32 * q, 0, lane);
-        constexpr int PIECES = S::CO + S::CI;
-        if (q >= 1 && q - 1 < PIECES) deposit_piece<T, S, WHOLE>(q - 1, f, stage[last], skipped, from.shift, tid, true, bias);
-        if (q >= 1 + PIECES && q - 1 - PIECES < PIECES) fetch_piece<T, S, true>(q - 1 - PIECES, a, from, 0, advance, blocks, tid, f);
+        constexpr int PIECES = S::CO + S::CI, FIRST = GROUPS > 2 * PIECES ? 1 : 0;
+        static_assert(!RING || GROUPS >= FIRST + 2 * PIECES, "every piece has its place");
+        if (q >= FIRST && q - FIRST < PIECES) deposit_piece<T, S, WHOLE>(q - FIRST, f, stage[last], skipped, from.shift, tid, true, bias);
+        if (q >= FIRST + PIECES && q - FIRST - PIECES < PIECES) fetch_piece<T, S, true>(q - FIRST - PIECES, a, from, 0, advance, blocks, tid, f);
       }
 #pragma unroll
       for (int m = 0; m < GROUPS * S::FI; ++m) {
