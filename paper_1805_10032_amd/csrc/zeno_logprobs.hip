@@ -286,7 +286,7 @@ struct Parts {
 };
 
 // Reads every logit once; the alternatives are found in a second look at the few pieces whose maximum is large enough.  8192 x 32768 bf16 with
-// entropy: 120 us (4.5 TB/s): the vector pipes are busy for 60 % of it, an FMA and an exponential at a quarter of the rate for every value
+// entropy: 95 us (5.6 TB/s): the vector pipes are busy for 75 % of it, an FMA and an exponential at a quarter of the rate for every value
 // and two more for the entropy.  2047 x 50257 float32 with five alternatives and entropy: 80 us (5.1 TB/s).  One row of 32000 with eight: 10 us,
 // the round trips of the row's loads, two reductions over sixteen waves, the candidates and their ranks, one behind the other.
 template <typename T, int NW, bool TOP, bool ENT>
@@ -598,8 +598,9 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts
 // ---- gradient:  dz_j = g [j = y] + sum_k q_k [j = i_k] - p_j (g + sum_k q_k + h (log p_j + H))
 // with g, h, q the gradients of logp, H and the alternatives' log probabilities.
 // L threads a segment of a row (16, 64 or 256): 256 / L segments a workgroup.  Each logit is read and each gradient written once, with no
-// reduction, so short segments and many workgroups keep the memory busy.  8192 x 32768 bf16: 167 us (6.4 TB/s), bound by memory; the vector
-// pipes are busy for 55 %.
+// reduction, so short segments and many workgroups keep the memory busy.  8192 x 32768 bf16: 187 us (5.7 TB/s), bound by memory.  With
+// ordinary stores 167, but what they leave in the caches is written while the next kernel runs: the forward pass of the next batch takes 120 us
+// instead of 95, a product that reads the gradient 10 more.
 template <typename T, bool ENT, bool TOP, int L>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArgs a, int segs, int seg_len) {
   constexpr int N = Wide<T>::N, EACH = kThreads / L;
@@ -621,7 +622,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
     const T* z = reinterpret_cast<const T*>(a.logits) + row * a.ldz + lo;
     T* out = reinterpret_cast<T*>(a.dlogits) + row * a.ldd + lo;
     float M = a.stats[2 * row], log_s = a.stats[2 * row + 1];
-    const bool empty = M == -inf && log_s == 0.f;
+    const bool empty = M == -inf && log_s == 0.f, past = on_line(out);
     int y = -1;
     float g = 0.f;
     if (a.grad_logp) {
@@ -677,7 +678,9 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
         for (int j = 0; j < N; ++j)
           if (j == hit) v[j] += g;
       }
-      if (at + N <= n)
+      if (at + N <= n && past)
+        store_wide_past(out + at, v);
+      else if (at + N <= n)
         store_wide(out + at, v);
       else
         store_part(out + at, n - at, v);

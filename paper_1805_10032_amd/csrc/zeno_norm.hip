@@ -87,6 +87,13 @@ __device__ inline void load_params(const float* p, int col, int width, float (&v
   }
 }
 
+template <typename T>
+__device__ inline void store_cols_past(bool past, T* row, int col, int width, const float (&v)[Wide<T>::N]) {
+  if (past && col + Wide<T>::N <= width)
+    store_wide_past(row + col, v);
+  else
+    store_cols(row, col, width, v);
+}
 // The 8-bit copy of N columns of a row (a block's columns lie in neighbouring lanes).  Every lane of the wave takes part.
 template <int N>
 __device__ inline void keep_cols(const float (&v)[N], int col, int width, int blocks, uint8_t* values, uint8_t* scales, long long row) {
@@ -184,7 +191,7 @@ struct Params {
 };
 
 // The next row is on its way while a row is reduced (the one after it as well: 72 -> 75 us).  Bound by memory and by what a row's two
-// reductions leave idle.  16384 x 4096 bf16 with a checkpoint 68 us (4.9 TB/s; a large copy moves 4.8), without one 51 us (5.3 TB/s);
+// reductions leave idle.  16384 x 4096 bf16 with a checkpoint 63 us (5.3 TB/s; a large copy moves 4.8), without one 51 us (5.3 TB/s);
 // 5003 x 1001 float32 11.5 us (3.5 TB/s), a launch and two round trips; 7634 x 6144 bf16 49 us, with a quarter of the threads idle.
 template <typename T, int NW, int CH>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
@@ -412,8 +419,8 @@ struct GradRow {
 
 //
 // A row's two sums and its result take two passes over its registers, which hold it as it lies in memory: unpacking it twice costs less than
-// the registers of the values.  16384 x 4096 bf16: 78 us from x (5.2 TB/s), 85 us from a checkpoint (4.0 TB/s: fewer bytes, the
-// same work; the vector pipes are busy for 37 %, waves wait for 44 % of their time, at one barrier a row and for the memory); 5003 x 1001 float32
+// the registers of the values.  16384 x 4096 bf16: 82 us from a checkpoint (4.1 TB/s; the
+// vector pipes are busy for 39 %, waves wait for 44 % of their time, at one barrier a row and for the memory); 5003 x 1001 float32
 // 20 us (3.0 TB/s), 313 chunks that each add up four waves' sums.
 template <typename T, int NW, int CH, bool KEPT>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradArgs a, Pieces p) {
@@ -428,6 +435,8 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
   const int r0 = blockIdx.x * p.chunk, r1 = a.rows - r0 < p.chunk ? a.rows : r0 + p.chunk;
   P::fill(weight, a.weight, a.width);
   if (a.offsets == nullptr) __syncthreads();   // (or the search for the first group has one)
+  // (16384 x 4096 bf16 85 -> 82 us, the next forward pass 68 -> 63; for rows of one wave the test costs what it may bring)
+  const bool past = NW >= 4 && on_line(a.dx) && a.lddx * (long long)sizeof(T) % 128 == 0;
   int parity = 0;
   for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
     const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
@@ -483,7 +492,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
           P::get(weight, c, tid, w);
 #pragma unroll
           for (int j = 0; j < N; ++j) d[j] = fmaf(d[j] * w[j], rstd, fmaf(xh[j], c2, c1));
-          store_cols(dx, (c * TPR + tid) * N, a.width, d);
+          store_cols_past(past, dx, (c * TPR + tid) * N, a.width, d);
         }
       }
       if (AHEAD > 0) now = next;

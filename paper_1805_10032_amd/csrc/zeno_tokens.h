@@ -38,6 +38,20 @@ __device__ inline void store_wide(T* p, const float (&v)[Wide<T>::N]) {
   *reinterpret_cast<typename Wide<T>::unaligned*>(p) = raw;
 }
 
+// Rows that start on a memory line may be written past the caches, where they would only displace what the next operators read: whole lines
+// leave at once.  Rows that do not would be written in parts (a weight gradient 1000 columns wide 41 -> 45 us).
+__device__ inline bool on_line(const void* p) { return (reinterpret_cast<unsigned long long>(p) & 127) == 0; }
+// (or the compiler joins such a store with the ordinary one of the other branch)
+__device__ inline void keep_apart() { asm volatile("" ::: "memory"); }
+template <typename T>
+__device__ inline void store_wide_past(T* p, const float (&v)[Wide<T>::N]) {
+  typename Wide<T>::type raw;
+#pragma unroll
+  for (int i = 0; i < Wide<T>::N; ++i) raw[i] = (T)v[i];
+  __builtin_nontemporal_store(raw, reinterpret_cast<typename Wide<T>::unaligned*>(p));
+  keep_apart();
+}
+
 template <typename T>
 __device__ inline void store_part(T* p, int n, const float (&v)[Wide<T>::N]) {
 #pragma unroll

@@ -35,8 +35,8 @@ struct Tile {
   static constexpr int CO = (CHUNKS_O + kThreads - 1) / kThreads, CI = (CHUNKS_I + kThreads - 1) / kThreads;
 };
 // 256 x 256, or 128 x 256 with several pieces of dy: half the sums, so that two workgroups share a compute unit and one's first loads and
-// stores run beside the other's products (20 x 100 tokens, 2048 x 2048: float32 129 -> 113 us, fp16 107 -> 98, with events around
-// each launch; 4 x 4096 tokens 377 -> 360 and 254 -> 247).  In bf16 the narrower tile spills and is slower (8 x 2048 tokens, 4096 x 4096: 660 -> 705 us).
+// stores run beside the other's products (20 x 100 tokens, 2048 x 2048: float32 129 -> 113 us, fp16 107 -> 98, with events around each
+// launch; 4 x 4096 tokens 377 -> 360 and 254 -> 247).  In bf16 the narrower tile spills and is slower (8 x 2048 tokens, 4096 x 4096: 660 -> 705 us).
 template <int P, bool ODD = false> using WideTile = Tile<2, (P > 1 ? 2 : 4), 4, P, ODD>;
 template <int P, bool ODD = false> using MidTile = Tile<2, 2, 2, P, ODD>;    // 128 x 128
 
@@ -290,8 +290,9 @@ __device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf
 // 8 x 2048 tokens, 4096 x 4096, bf16: 550-590 us (930-1000 TFLOP/s; a large bf16 product of the library with its operands stored this way
 // 1187, stored the other way 1369).  The matrix pipes are busy for 48 % of the time and the clock gives way under them (the same code without
 // memory traffic runs the stream of matrix instructions at 1770-1900 TFLOP/s); waves stand ready but unissued for 39 %.
-// 20 x 100 tokens, 2048 x 2048, float32: 102 us, 3.3 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
-// 128 KB of stores where both workgroups of a compute unit are in them.  128 x 128 tiles: 134 us.
+// 20 x 100 tokens, 2048 x 2048, float32: 86 us, 3.9 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
+// 128 KB of stores where both workgroups of a compute unit are in them.  128 x 128 tiles: 134 us (102 with these before the stores went past
+// the caches).
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kernel(WeightGradArgs a, int tiles_in, int pieces,
                                                                                   float* partial) {
@@ -455,21 +456,36 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   const long long size = (long long)a.out * a.width;
   float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
   const bool inside = o0 + S::OUT <= a.out && k0 + S::IN <= a.width;
+  // Gradients are read when all layers have theirs, so they go past the caches (20 x 100 tokens, 2048 x 2048 float32: 101 -> 86 us; two such
+  // layers, one of 8192 outputs and the scores together 2610 -> 2384 us, 1024 wide 812 -> 757); pieces are joined at once.
+  const bool past = inside && pieces == 1 && a.width % 32 == 0 && on_line(dw);
+  if (past) {
 #pragma unroll
-  for (int r = 0; r < S::FO; ++r)
+    for (int r = 0; r < S::FO; ++r)
 #pragma unroll
-    for (int j = 0; j < S::FI; ++j) {
-      const int k = k0 + wk + 32 * j + lane % 32, o = o0 + wo + 32 * r + 4 * (lane / 32);
-      float* to = dw + (long long)o * a.width + k;
-      if (inside) {
+      for (int j = 0; j < S::FI; ++j) {
+        float* to = dw + (long long)(o0 + wo + 32 * r + 4 * (lane / 32)) * a.width + k0 + wk + 32 * j + lane % 32;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (o + 8 * (e / 4) + e % 4 < a.out && k < a.width) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
+        for (int e = 0; e < 16; ++e) __builtin_nontemporal_store(acc[r][j][e], &to[(long long)(8 * (e / 4) + e % 4) * a.width]);
       }
-    }
+    keep_apart();
+  } else {
+#pragma unroll
+    for (int r = 0; r < S::FO; ++r)
+#pragma unroll
+      for (int j = 0; j < S::FI; ++j) {
+        const int k = k0 + wk + 32 * j + lane % 32, o = o0 + wo + 32 * r + 4 * (lane / 32);
+        float* to = dw + (long long)o * a.width + k;
+        if (inside) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (o + 8 * (e / 4) + e % 4 < a.out && k < a.width) to[(long long)(8 * (e / 4) + e % 4) * a.width] = acc[r][j][e];
+        }
+      }
+  }
   if (sums) {
     constexpr int PER = S::OUT / 8, PARTS = (S::CHUNKS_O < kThreads ? S::CHUNKS_O : kThreads) / PER;
     float (*part)[S::OUT] = reinterpret_cast<float (*)[S::OUT]>(memory);
