@@ -143,3 +143,48 @@ def test_the_most_groups(B, out, width):
         p, q = int(cuts[i]), int(cuts[i + 1])
         assert torch.equal(G[i, :out * width].reshape(out, width), dy[p:q].T @ a[p:q] if q > p else torch.zeros(out, width, device="cuda"))
         assert torch.equal(G[i, out * width:], dy[p:q].sum(0))
+
+
+def off_line(shape, dtype):
+    """A matrix whose rows do not start on memory lines."""
+    return torch.empty(shape[0] * (shape[1] + 1) + 1, dtype=dtype, device="cuda").as_strided(shape, (shape[1] + 1, 1), 1)
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+def test_gradients_on_memory_lines_and_off_them(B, ty):
+    """Rows on memory lines are written another way: the same bits."""
+    g = torch.Generator().manual_seed(4)
+    dt = TYPES[ty]
+    for vocab in (128, 300 * 64, 40):
+        z = torch.randn(9, vocab, generator=g).to(dt).cuda()
+        lab = torch.randint(0, vocab, (9,), generator=g, dtype=torch.int32).cuda()
+        _, _, stats, index, _ = B.zeno_logprobs(z, lab, want_stats=True, top=2)
+        h, q = torch.randn(9, generator=g).cuda(), torch.randn(9, 2, generator=g).cuda()
+        for kw in (dict(), dict(top_index=index, grad_top=q)):
+            on, off = (B.zeno_logprobs_backward(z, stats, labels=lab, grad_logp=h, out=o, **kw) for o in (torch.empty_like(z), off_line(z.shape, dt)))
+            assert torch.equal(on, off) and not torch.isnan(on).any()
+    for width in (1024, 4096, 8192, 12032):
+        x, dy = (torch.randn(40, width, generator=g).to(dt).cuda() for _ in range(2))
+        w = torch.randn(width, generator=g).cuda()
+        _, mean, rstd, _ = B.zeno_layer_norm(x, w)
+        on, off = (B.zeno_layer_norm_backward(dy, x, mean, rstd, w, dx=o)[0] for o in (torch.empty_like(x), off_line(x.shape, dt)))
+        assert torch.equal(on, off) and not torch.isnan(on).any()
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+@pytest.mark.parametrize("m,out,width,rows", [(256, 256, 256, 16700), (70, 300, 544, 4600), (40, 128, 128, 900), (256, 264, 288, 17000)])
+def test_weight_gradients_on_memory_lines_and_off_them(B, m, out, width, rows, ty):
+    """All shapes of tiles, inside the output and across its end; sums of small whole numbers."""
+    g = torch.Generator().manual_seed(5)
+    dy, a = whole((rows, out), g).to(TYPES[ty]).cuda(), whole((rows, width), g).cuda()
+    cuts = torch.tensor([rows * i // m for i in range(m)] + [rows - 3])
+    ck = B.zeno_checkpoint(a)
+    off = cuts.int().cuda()
+    one, one_b = B.zeno_weight_gradient(dy, ck, groups=off)
+    G = off_line((m, out * width), torch.float32)
+    two, two_b = B.zeno_weight_gradient(dy, ck, groups=off, dweight=G)
+    assert torch.equal(one, two) and torch.equal(one_b, two_b)
+    d32 = dy.float()
+    for i in list(range(0, m, 37)) + [m - 1]:
+        p, q = int(cuts[i]), int(cuts[i + 1])
+        assert torch.equal(one[i].reshape(out, width), d32[p:q].T @ a[p:q]) and torch.equal(one_b[i], d32[p:q].sum(0))
