@@ -287,10 +287,10 @@ __device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf
 // before it, and one that is being written; two more are on their way from memory.
 // Tiles: a wave's 128 x 128 of the product reads the fewest operands from LDS that the registers allow, at one wave a SIMD, which issues in
 // order: what runs beside the matrix instructions stands between them.
-// 8 x 2048 tokens, 4096 x 4096, bf16: 550-590 us (930-1000 TFLOP/s; a large bf16 product of the library with its operands stored this way
+// 8 x 2048 tokens, 4096 x 4096, bf16: 550-605 us (910-1000 TFLOP/s; a large bf16 product of the library with its operands stored this way
 // 1187, stored the other way 1369).  The matrix pipes are busy for 48 % of the time and the clock gives way under them (the same code without
 // memory traffic runs the stream of matrix instructions at 1770-1900 TFLOP/s); waves stand ready but unissued for 39 %.
-// 20 x 100 tokens, 2048 x 2048, float32: 86 us, 3.9 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
+// 20 x 100 tokens, 2048 x 2048, float32: 86-92 us, 3.9 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
 // 128 KB of stores where both workgroups of a compute unit are in them.  128 x 128 tiles: 134 us (102 with these before the stores went past
 // the caches).
 template <typename T, typename S>
