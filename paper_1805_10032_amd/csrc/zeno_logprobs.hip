@@ -39,6 +39,23 @@ struct RowSums {
   float M, s, t;   // max, sum 2^(L(z-M)), sum 2^(L(z-M)) L(z-M)
 };
 
+// A thread's sums relative to a reference that is `delta` lower (delta = old reference - new one).  What lies 2^-100 below the new
+// reference adds nothing to it, and is left out rather than scaled: a thread that has met nothing but masks of a size where the reference
+// L z has no fraction left holds 2^(its rounding) there, up to infinity, which 0 would make NaN.  (Infinity would last through steps of
+// less than 100, but from 2^31, where the rounding reaches 128, down to ordinary logits there are more of them than a thread has pieces.  The
+// sums are NaN only next to a NaN.)
+template <bool ENT>
+__device__ inline void move_by(float& s, float& t, float delta) {
+  if (delta > -100.f) {
+    const float r = exp2_fast(delta);
+    if (ENT) t = r * fmaf(s, delta, t);
+    s *= r;
+  } else {
+    s = s == s ? 0.f : s;
+    if (ENT) t = s;
+  }
+}
+
 // The sums of two parts relative to M >= part.M.
 __device__ inline void move_to(RowSums& p, float M) {
   if (p.s != 0.f && p.M < M) {
@@ -313,11 +330,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
       const float cm = max_of<N>(v, -inf);
       if (cm > lim) {
         const float cn = finite(cm * kLog2e);
-        if (s != 0.f) {
-          const float delta = fmaxf(c - cn, -1e4f), r = exp2_fast(delta);
-          if (ENT) t = r * fmaf(s, delta, t);
-          s *= r;
-        }
+        if (s != 0.f) move_by<ENT>(s, t, c - cn);
         c = cn;
         lim = cm + 0.6875f;   // the reference follows when it is a factor of two behind
       }
@@ -376,8 +389,9 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
       __syncthreads();
       for (int i = 0; i < NW; ++i) M = fmaxf(M, sh.wave_max[i]);
     }
-    if (fabsf(M) > 0x1p126f && fabsf(M) < inf) {
-      // L M is out of range (a row masked with the type's lowest value): once more with z - M first
+    if (fabsf(M) > 0x1p24f && fabsf(M) < inf) {
+      // L M is rounded by more than 1, which all of the row's values would carry in their exponents, or out of range (a row masked
+      // throughout, whatever the mask's value): once more with z - M first
       s = t = 0.f;
       for (int it = 0; it < iters; ++it) {
         const int at = (it * TPR + tid) * N;
@@ -392,9 +406,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
       }
     } else if (s != 0.f) {
       // c is L times some logit, rounded: the exact product with M's is what the sums refer to from here on
-      const float delta = own_max == -inf ? 0.f : fmaxf(fmaf(-M, kLog2e, c), -1e4f), r = exp2_fast(delta);
-      if (ENT) t = r * fmaf(s, delta, t);
-      s *= r;
+      move_by<ENT>(s, t, own_max == -inf ? 0.f : fmaf(-M, kLog2e, c));
     }
     s = wave_sum_f(s);
     if (ENT) t = wave_sum_f(t);

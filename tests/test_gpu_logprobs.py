@@ -359,3 +359,39 @@ def test_few_values(B, vocab, ty):
     z[6, vocab - 1] = z[6, 0]
     check_forward(B, z, labels, min(vocab, 32))
     check_forward(B, z, labels, 1)
+
+
+def far_rows(vocab, fill, seed):
+    """Rows with masks and logits of the size of `fill`, whole and in part: log2(e) times them has no fraction left in float32."""
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn(10, vocab, generator=g) * 3
+    z[0, :] = fill
+    z[1, :vocab // 2] = fill                                  # every thread's first pieces, none of its last
+    z[2, torch.rand(vocab, generator=g) < 0.5] = fill
+    z[3, 1:] = fill
+    z[4, :] = fill
+    z[4, 3 * vocab // 4:] = fill / 2                          # two sizes, both large
+    z[5, vocab // 3] = -fill
+    z[6, :] = -fill
+    z[7, :] = torch.linspace(1, 0, vocab) * fill              # rises step by step
+    z[8, vocab // 2:] = fill
+    z[9, :] = fill + torch.linspace(0, 1, vocab) * 4000       # (the same value again where fill is that much larger)
+    return z
+
+
+@pytest.mark.parametrize("rows,vocab", [(10, 40), (10, 250), (10, 700), (10, 2600), (10, 20000), (520, 2600), (10, 70000)])
+@pytest.mark.parametrize("ty", ["fp32", "bf16"])
+@pytest.mark.parametrize("fill", [-3e4, -1.7e7, -1e8, -6e8, -1e9, -2e9, -1e10, -1e12, -1e20, -1e30, -1e38, 1e10, 1e30])
+def test_large_finite_logits(B, rows, vocab, ty, fill):
+    """Masks and logits of any finite size, in rows of one wave, of four, of sixteen and in rows shared by workgroups."""
+    z = far_rows(vocab, fill, 51)
+    g = torch.Generator().manual_seed(53)
+    if rows > 10:
+        z = torch.cat([torch.randn(rows - 10, vocab, generator=g), z])
+    view, _ = T.strided(z, T.TYPES[ty])
+    labels = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    labels[-3] = 0
+    _, ref = check_forward(B, view, labels, 6)
+    assert np.isfinite(ref["log_s"]).all()
+    if fill in (-1e10, -1e30, 1e10):
+        check_backward(B, view, labels, top=6)
