@@ -20,7 +20,8 @@ constexpr int kCandidates = 512;   // top values are chosen from at most so many
 constexpr int kMaxParts = 64;      // workgroups that share a row
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-// (written out: fmaxf would first quiet every operand that might be a signalling NaN, an instruction a value)
+// (written out: fmaxf would first quiet every operand that might be a signalling NaN, an instruction a value; such a NaN takes the value
+// beside it out of the maximum, so a thread that has met a NaN, as its sum shows, looks for its maxima again)
 __device__ inline float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
@@ -74,6 +75,12 @@ __device__ inline float log_prob(float z, float M, float log_s, bool empty) {
 }
 
 __device__ inline float clean(float z) { return z != z ? -__builtin_inff() : z; }   // a NaN ranks as -inf
+template <int N>
+__device__ inline float clean_max_of(const float (&v)[N], float m) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) m = fmaxf(m, clean(v[j]));
+  return m;
+}
 
 // Writes what a row gives, except its alternatives.  One thread.
 template <typename T>
@@ -381,6 +388,22 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void logprobs_kernel(LogprobsAr
     } else {
       M = clean(run(0, iters));
     }
+    if (s != s) {
+      M = -inf;
+      for (int it = 0, g = 0, end = per_group; it < iters; end += per_group, ++g) {
+        float gm = -inf;
+        for (; it < end && it < iters; ++it) {
+          const int at = (it * TPR + tid) * N;
+          if (at < n) {
+            load_at(row, n, at, v);
+            gm = clean_max_of<N>(v, gm);
+          }
+        }
+        if constexpr (TOP) sh.group_max[slot][g][tid] = gm;
+        M = fmaxf(M, gm);
+      }
+      if constexpr (TOP) sh.thread_max[slot][tid] = M;
+    }
     // the row's maximum, and every thread's sums relative to it
     const float own_max = M;
     M = wave_max_f(M);
@@ -501,6 +524,12 @@ __global__ __launch_bounds__(kThreads) void logprobs_narrow_kernel(LogprobsArgs 
       }
     s = reduce(s, add);
     if (ENT) t = reduce(t, add);
+    if (s != s) {   // (the lanes of a row agree)
+      M = -inf;
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) M = clean_max_of<N>(v[p], M);
+      M = reduce(M, [](float x, float y) { return fmaxf(x, y); });
+    }
     float log_s = 0.f;
     const RowSums r = {M, s, t};
     if (live && lane == 0) finish_row<T>(a, rowi, r, &log_s);

@@ -395,3 +395,18 @@ def test_large_finite_logits(B, rows, vocab, ty, fill):
     assert np.isfinite(ref["log_s"]).all()
     if fill in (-1e10, -1e30, 1e10):
         check_backward(B, view, labels, top=6)
+
+
+SIGNALLING = {"fp32": (torch.int32, 0x7f800001), "bf16": (torch.int16, 0x7f81), "fp16": (torch.int16, 0x7c01)}
+
+
+@pytest.mark.parametrize("ty", list(SIGNALLING))
+@pytest.mark.parametrize("rows,vocab", [(16, 40), (16, 300), (16, 2600), (16, 20000), (530, 2600), (16, 70000)])
+def test_signalling_nan_beside_the_largest(B, rows, vocab, ty):
+    """A NaN that has not been quieted takes nothing with it: the others keep their ranks and the maximum is theirs."""
+    z, _, labels, _ = make(rows, vocab, ty, 57)
+    bits, code = SIGNALLING[ty]
+    for r in range(16):
+        z[rows - 16 + r, 16 + r] = 60.0
+        z.view(bits)[rows - 16 + r, 16 + (r ^ 1)] = code
+    check_forward(B, z, labels, 5)
