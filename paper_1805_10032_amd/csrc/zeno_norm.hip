@@ -145,10 +145,10 @@ struct RowPart {
     for (int j = 0; j < N; ++j) v[j] = (float)raw[c][j];
     if ((c + 1) * TPR * N > width) cut<N>((c * TPR + tid) * N, width, v);
   }
-  __device__ inline void normalised(int c, int tid, int width, float mean, float rstd, float (&v)[Wide<T>::N]) const {
+  __device__ inline void centred(int c, int tid, int width, float mean, float (&v)[Wide<T>::N]) const {
     get(c, tid, width, v);
 #pragma unroll
-    for (int j = 0; j < Wide<T>::N; ++j) v[j] = (v[j] - mean) * rstd;
+    for (int j = 0; j < Wide<T>::N; ++j) v[j] -= mean;
   }
   template <int N>
   static __device__ inline void cut(int col, int width, float (&v)[N]) {
@@ -359,8 +359,9 @@ __device__ inline void load_xh(const NormGradArgs& a, long long row, int col, in
   } else {
     load_cols<WHOLE>(reinterpret_cast<const T*>(a.x) + row * a.ldx, col, a.width, v);
   }
+  // (0 behind the row's end, also where mean rstd is out of range: infinity times dy's 0 would be NaN)
 #pragma unroll
-  for (int j = 0; j < N; ++j) v[j] = (v[j] - mean) * rstd;
+  for (int j = 0; j < N; ++j) v[j] = WHOLE || col + j < a.width ? (v[j] - mean) * rstd : 0.f;
 }
 
 // The same of a checkpoint, whose rows end with zeros in whole blocks.
@@ -389,15 +390,15 @@ struct KeptPart {
         if (CH * Wide<T>::N >= 32) unpack_again(words[c][j]);
   }
   // (q scale is exact, and so is the difference where it cancels)
-  __device__ inline void normalised(int c, int, int, float mean, float rstd, float (&v)[Wide<T>::N]) const {
+  __device__ inline void centred(int c, int, int, float mean, float (&v)[Wide<T>::N]) const {
     const float s = ckpt_scale((int)scale[c] - 127);
 #pragma unroll
     for (int i = 0; i < Wide<T>::N; i += 4) {
       const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(words[c][i / 4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(words[c][i / 4], true);
-      v[i] = fmaf(lo.x, s, -mean) * rstd;
-      v[i + 1] = fmaf(lo.y, s, -mean) * rstd;
-      v[i + 2] = fmaf(hi.x, s, -mean) * rstd;
-      v[i + 3] = fmaf(hi.y, s, -mean) * rstd;
+      v[i] = fmaf(lo.x, s, -mean);
+      v[i + 1] = fmaf(lo.y, s, -mean);
+      v[i + 2] = fmaf(hi.x, s, -mean);
+      v[i + 3] = fmaf(hi.y, s, -mean);
     }
   }
 };
@@ -462,36 +463,38 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
       if (AHEAD == 0) now.load(a, row, blocks, tid);
       if (AHEAD == 1) next.load(a, row + RPB < hi ? row + RPB : row, blocks, tid);
       const float mean = now.mean, rstd = now.rstd;
-      float c1 = 0.f, c2 = 0.f, d[N], xh[N], w[N];
+      // x - mean in the row's sum, and rstd behind it: columns behind the row's end, where dy is 0, hold -mean, which is finite where
+      // mean rstd need not be
+      float c1 = 0.f, c2 = 0.f, d[N], u[N], w[N];
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         now.dy.get(c, tid, a.width, d);
-        now.x.normalised(c, tid, a.width, mean, rstd, xh);
+        now.x.centred(c, tid, a.width, mean, u);
         P::get(weight, c, tid, w);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           db[c][j] += d[j];
-          dw[c][j] = fmaf(d[j], xh[j], dw[c][j]);
+          dw[c][j] = fmaf(d[j], u[j] * rstd, dw[c][j]);
           const float t = d[j] * w[j];
           c1 += t;
-          c2 = fmaf(t, xh[j], c2);
+          c2 = fmaf(t, u[j], c2);
         }
       }
       if (a.dx != nullptr) {
         row_sums2<NW>(c1, c2, buf[parity], wave);
         parity ^= 1;
         c1 *= inv * -rstd;
-        c2 *= inv * -rstd;
+        c2 = rstd == 0.f ? 0.f : c2 * rstd * (inv * -rstd);   // (a variance out of range: the sum may be, too)
         T* dx = reinterpret_cast<T*>(a.dx) + (long long)row * a.lddx;
         now.dy.again();
         now.x.again();
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           now.dy.get(c, tid, a.width, d);
-          now.x.normalised(c, tid, a.width, mean, rstd, xh);
+          now.x.centred(c, tid, a.width, mean, u);
           P::get(weight, c, tid, w);
 #pragma unroll
-          for (int j = 0; j < N; ++j) d[j] = fmaf(d[j] * w[j], rstd, fmaf(xh[j], c2, c1));
+          for (int j = 0; j < N; ++j) d[j] = fmaf(d[j] * w[j], rstd, fmaf(u[j] * rstd, c2, c1));
           store_cols_past(past, dx, (c * TPR + tid) * N, a.width, d);
         }
       }

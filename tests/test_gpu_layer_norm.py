@@ -236,3 +236,40 @@ def test_gradient_against_differences(B):
             assert abs(slope(args, 0, (r, j)) - float(dx[r, j])) <= tol
     for j in range(9):
         assert abs(slope(args, 1, j) - float(dw[0, j])) <= tol and abs(slope(args, 2, j) - float(db[0, j])) <= tol
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("width,ty", [(1, "fp32"), (32, "fp32"), (100, "bf16"), (1001, "fp32"), (2050, "bf16"), (6144, "bf16"), (9001, "fp32"),
+                                      (20000, "fp32"), (40001, "bf16")])
+def test_what_lies_behind_a_row_has_no_weight(B, width, ty, ckpt):
+    """Equal values of a size whose product with rstd is out of range: xh is 0 in every column, so dx = rstd (a - mean(a)).  Lanes
+    behind the row's end must not bring in an infinity."""
+    rows, big, r = 3, 2.0 ** 110, 2.0 ** 20
+    g = torch.Generator().manual_seed(width)
+    x = torch.full((rows, width), big, dtype=T.TYPES[ty], device="cuda")
+    dy = torch.randn(rows, width, generator=g).to(T.TYPES[ty]).cuda()
+    w = (1 + 0.2 * torch.randn(width, generator=g)).cuda()
+    mean, rstd = torch.full((rows,), big, device="cuda"), torch.full((rows,), r, device="cuda")
+    dx, dw, db = B.zeno_layer_norm_backward(dy, B.zeno_checkpoint(x) if ckpt else x, mean, rstd, w)
+    d64 = dy.double().cpu().numpy()
+    a = d64 * w.double().cpu().numpy()
+    want = r * (a - a.mean(1, keepdims=True))
+    tol = r * ((chain(width, 16 // x.element_size()) + 3) * T.EPS * np.abs(a).mean(1, keepdims=True) + 5 * T.EPS * np.abs(a))
+    tol = tol + (np.abs(want) + tol) * T.half_step(x.dtype)
+    assert (np.abs(dx.double().cpu().numpy() - want) <= tol).all()
+    assert not dw.any()
+    assert (np.abs(db[0].double().cpu().numpy() - d64.sum(0)) <= (rows + 8) * T.EPS * np.abs(d64).sum(0)).all()
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("width", [100, 3000, 9001, 20000])
+def test_variance_out_of_range(B, width, ckpt):
+    """One value of 1e38: rstd is 0 in float32, so xh and dx are 0, whatever dy is."""
+    x, _, weight, _, g = make(3, width, "fp32", 14)
+    x[1, 5] = 1e38
+    dy = torch.randn(3, width, generator=g).cuda()
+    dy[1] *= 1000
+    _, mean, rstd, kept = B.zeno_layer_norm(x, weight, None, EPS_NORM, want_checkpoint=True)
+    assert float(rstd[1]) == 0
+    dx, dw, _ = B.zeno_layer_norm_backward(dy, kept if ckpt else x, mean, rstd, weight, groups=torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda"))
+    assert not dx[1].any() and not dw[1].any() and torch.isfinite(dx).all() and dx[0].any() and dx[2].any()
