@@ -472,7 +472,17 @@ def _vec(t, dtype, name: str, shape, dev: int):
     return t.data_ptr()
 
 
-def _matrix(t, name: str, dev: int, shape=None, dtype=None):
+# The C calls take sizes in 32 bits: a larger one would arrive there as another size.
+_MOST = (1 << 31) - 1
+
+
+def _size32(where: str, *sizes):
+    if any(abs(n) > _MOST for n in sizes):
+        raise ZenoError(2, where)
+    return sizes
+
+
+def _matrix(t, name: str, dev: int, shape=None, dtype=None, most=_MOST):
     """(pointer, pitch, dtype code, rows, columns) of a 2-D matrix whose rows are contiguous and do not overlap."""
     if not isinstance(t, torch.Tensor) or t.get_device() != dev:
         _elsewhere(t, name)
@@ -484,6 +494,8 @@ def _matrix(t, name: str, dev: int, shape=None, dtype=None):
         raise ValueError(f"{name} must be a matrix of shape {tuple(shape) if shape is not None else '(rows, columns)'}, "
                          f"got {tuple(size)}")
     rows, cols = size
+    if rows > _MOST or cols > most:
+        raise ZenoError(2, name)
     pitch, inner = t.stride()
     if cols > 1 and inner != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
@@ -495,10 +507,11 @@ def _matrix(t, name: str, dev: int, shape=None, dtype=None):
 
 
 def _grad_rows(t, name: str, m: int, n: int, dev: int):
-    """(pointer, pitch) of m rows of n float32 gradients: columns of G, or a tensor of its own."""
+    """(pointer, pitch) of m rows of n float32 gradients: columns of G, or a tensor of its own.  (n does not go to the call: a layer may
+    have more weights than 32 bits count.)"""
     if t is None:
         return None, n
-    ptr, pitch, _, _, _ = _matrix(t, name, dev, (m, n), torch.float32)
+    ptr, pitch, _, _, _ = _matrix(t, name, dev, (m, n), torch.float32, n)
     return ptr, pitch
 
 
@@ -506,6 +519,8 @@ def _kept(ckpt, rows: int, width: int, dev: int):
     """Device pointers of a Checkpoint of [rows x width] activations."""
     if not isinstance(ckpt, Checkpoint) or ckpt.width != width:
         raise ValueError(f"a Checkpoint of {width} columns is needed")
+    if width > _MOST:
+        raise ZenoError(2, "Checkpoint")
     blocks = (width + 31) // 32
     return _vec(ckpt.values, torch.uint8, "values", (rows, 32 * blocks), dev), _vec(ckpt.scales, torch.uint8, "scales", (rows, blocks), dev)
 
@@ -516,6 +531,8 @@ def _groups(groups, dev: int):
         return 1, None
     if not isinstance(groups, torch.Tensor) or groups.dim() != 1 or groups.numel() < 2:
         raise ValueError("groups must hold the m + 1 row offsets of the workers")
+    if groups.numel() > _MOST:
+        raise ZenoError(2, "groups")
     return groups.numel() - 1, _vec(groups, torch.int32, "groups", groups.shape, dev)
 
 
@@ -533,8 +550,8 @@ def _workspace(n: int, where: str, device=None) -> torch.Tensor:
 
 
 def alloc_logprobs_workspace(rows: int, vocab: int, top: int = 0, device=None) -> torch.Tensor:
-    return _workspace(int(load_library().zeno_logprobs_workspace_bytes(int(rows), int(vocab), int(top))),
-                      "zeno_logprobs_workspace_bytes", device)
+    sizes = _size32("zeno_logprobs_workspace_bytes", int(rows), int(vocab), int(top))
+    return _workspace(int(load_library().zeno_logprobs_workspace_bytes(*sizes)), "zeno_logprobs_workspace_bytes", device)
 
 
 def zeno_logprobs(logits, labels=None, *, top=0, want_entropy=False, want_stats=False, logp=None, entropy=None, stats=None,
@@ -546,6 +563,8 @@ def zeno_logprobs(logits, labels=None, *, top=0, want_entropy=False, want_stats=
     dev = _current(logits, "logits")
     ptr, pitch, code, rows, vocab = _matrix(logits, "logits", dev)
     top, f32, i32, new = int(top), torch.float32, torch.int32, logits.new_empty
+    if abs(top) > _MOST:
+        raise ZenoError(2, "zeno_logprobs")
 
     def out(t, want, shape, dtype, name):
         if t is not None:
@@ -667,8 +686,8 @@ def zeno_layer_norm(x, weight, bias=None, eps=1e-5, *, y=None, mean=None, rstd=N
 
 
 def alloc_layer_norm_workspace(rows: int, width: int, m: int = 1, device=None) -> torch.Tensor:
-    return _workspace(int(load_library().zeno_layer_norm_workspace_bytes(int(rows), int(width), int(m))),
-                      "zeno_layer_norm_workspace_bytes", device)
+    sizes = _size32("zeno_layer_norm_workspace_bytes", int(rows), int(width), int(m))
+    return _workspace(int(load_library().zeno_layer_norm_workspace_bytes(*sizes)), "zeno_layer_norm_workspace_bytes", device)
 
 
 def zeno_layer_norm_backward(dy, x, mean, rstd, weight, *, groups=None, want_dx=True, want_weight=True, want_bias=True, dx=None,
@@ -710,8 +729,8 @@ def zeno_layer_norm_backward(dy, x, mean, rstd, weight, *, groups=None, want_dx=
 
 
 def alloc_weight_gradient_workspace(rows: int, out: int, width: int, m: int = 1, device=None) -> torch.Tensor:
-    return _workspace(int(load_library().zeno_weight_gradient_workspace_bytes(int(rows), int(out), int(width), int(m))),
-                      "zeno_weight_gradient_workspace_bytes", device)
+    sizes = _size32("zeno_weight_gradient_workspace_bytes", int(rows), int(out), int(width), int(m))
+    return _workspace(int(load_library().zeno_weight_gradient_workspace_bytes(*sizes)), "zeno_weight_gradient_workspace_bytes", device)
 
 
 def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, dweight=None, dbias=None, workspace=None):
@@ -741,8 +760,8 @@ def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, d
 
 
 def alloc_score_logprobs_workspace(m: int, d: int, device=None) -> torch.Tensor:
-    return _workspace(int(load_library().zeno_score_logprobs_workspace_bytes(int(m), int(d))),
-                      "zeno_score_logprobs_workspace_bytes", device)
+    _size32("zeno_score_logprobs_workspace_bytes", int(m))
+    return _workspace(int(load_library().zeno_score_logprobs_workspace_bytes(int(m), int(d))), "zeno_score_logprobs_workspace_bytes", device)
 
 
 def zeno_score_logprobs(G, logp_x, logp, rho, *, labels=None, scores=None, workspace=None):

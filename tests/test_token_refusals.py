@@ -129,3 +129,27 @@ def test_the_binding_refuses_tensors_elsewhere(B):
                  lambda: B.zeno_checkpoint_values(ck)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_the_binding_refuses_sizes_beyond_32_bits(B):
+    """A size that the C call takes in 32 bits would otherwise arrive as another one.  The memory is never touched."""
+    long = (1 << 32) + 5
+    column = torch.empty(long, 1, dtype=torch.float16)
+    for t in (column, column.t()):
+        with pytest.raises(B.ZenoError) as e:
+            B._matrix(t, "x", t.get_device())
+        assert e.value.status == UNSUPPORTED
+    offsets = torch.empty(long, dtype=torch.int32)
+    with pytest.raises(B.ZenoError) as e:
+        B._groups(offsets, offsets.get_device())
+    assert e.value.status == UNSUPPORTED
+    for call in (lambda: B.alloc_logprobs_workspace(long, 10, 0), lambda: B.alloc_logprobs_workspace(4, long, 0),
+                 lambda: B.alloc_logprobs_workspace(4, 10, (1 << 32) + 1), lambda: B.alloc_layer_norm_workspace(long, 10, 1),
+                 lambda: B.alloc_layer_norm_workspace(10, long, 1), lambda: B.alloc_layer_norm_workspace(10, 10, long),
+                 lambda: B.alloc_weight_gradient_workspace(long, 10, 10, 1), lambda: B.alloc_weight_gradient_workspace(10, long, 10, 1),
+                 lambda: B.alloc_weight_gradient_workspace(10, 10, long, 1), lambda: B.alloc_weight_gradient_workspace(10, 10, 10, long),
+                 lambda: B.alloc_score_logprobs_workspace(long, 10)):
+        with pytest.raises(B.ZenoError):
+            call()
+    weights = torch.empty(1, (1 << 31) + 5)        # (one layer's weights; the rows of such gradients are counted in 64 bits)
+    assert B._grad_rows(weights, "dweight", 1, weights.shape[1], weights.get_device()) == (weights.data_ptr(), weights.shape[1])
