@@ -1,6 +1,8 @@
 """The operators for models that answer with tokens at the ends of their ranges: rows far apart, offsets past 2^31, more rows than a
 launch has workgroups, the most groups.  What such a call gives has to be, bit for bit, what the same rows give close together, or sums
 of small whole numbers, which float32 holds exactly."""
+import math
+
 import pytest
 import torch
 
@@ -188,3 +190,75 @@ def test_weight_gradients_on_memory_lines_and_off_them(B, m, out, width, rows, t
     for i in list(range(0, m, 37)) + [m - 1]:
         p, q = int(cuts[i]), int(cuts[i + 1])
         assert torch.equal(one[i].reshape(out, width), d32[p:q].T @ a[p:q]) and torch.equal(one_b[i], d32[p:q].sum(0))
+
+
+def test_the_largest_vocabulary(B):
+    """2^30 logits a row, shared by workgroups, and 2^23 in one workgroup each: s = sum exp(z - M) is known in closed form."""
+    for rows, vocab, ty in ((1, 1 << 30, torch.bfloat16), (1, (1 << 30) - 3, torch.float32), (200, 1 << 23, torch.bfloat16)):
+        z = torch.zeros(rows, vocab, dtype=ty, device="cuda")
+        z[:, vocab - 1], z[:, vocab // 2 + 1] = 20.0, 10.0
+        lab = torch.full((rows,), vocab // 2 + 1, dtype=torch.int32, device="cuda")
+        logp, entropy, stats, index, top = B.zeno_logprobs(z, lab, top=4, want_entropy=True, want_stats=True)
+        s = 1 + math.exp(-10) + (vocab - 2) * math.exp(-20)
+        t = -10 * math.exp(-10) - 20 * (vocab - 2) * math.exp(-20)
+        # at most 16384 values a thread and 22 joins; an exponential off by 4 EPS and its argument by EPS |20|
+        tol = (16384 + 64) * 2.0 ** -24
+        assert (logp.double() - (-10 - math.log(s))).abs().max() <= tol + 16 * 2.0 ** -24
+        assert (entropy.double() - (math.log(s) - t / s)).abs().max() <= 40 * tol
+        assert (index == torch.tensor([vocab - 1, vocab // 2 + 1, 0, 1], dtype=torch.int32, device="cuda")).all()
+        g = torch.ones(rows, device="cuda")
+        dz = B.zeno_logprobs_backward(z, stats, labels=lab, grad_logp=g, out=z)
+        half = torch.finfo(ty).eps
+        for at, want in ((vocab - 1, -1 / s), (vocab // 2 + 1, 1 - math.exp(-10) / s), (vocab - 2, -math.exp(-20) / s), (0, -math.exp(-20) / s)):
+            assert (dz[:, at].double() - want).abs().max() <= (half + 2 * tol + 64 * 2.0 ** -24) * abs(want)
+        del z, dz
+
+
+def test_the_widest_rows(B):
+    """2^24 columns of layer norm and of a checkpoint, and more weights than 32 bits count."""
+    rows, width = 3, 1 << 24
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.randn(rows, width, device="cuda", generator=g) for _ in range(2))
+    w = torch.ones(width, device="cuda")
+    y, mean, rstd, ck = B.zeno_layer_norm(x, w, want_checkpoint=True)
+    alone = B.zeno_checkpoint(x)
+    assert torch.equal(ck.values, alone.values) and torch.equal(ck.scales, alone.scales)
+    x64 = x.double()
+    m64, v64 = x64.mean(1), x64.var(1, unbiased=False)
+    k = (16384 + 64) * 2.0 ** -24                    # additions of a thread and its joins, times half a step
+    assert ((mean.double() - m64).abs() <= k * x64.abs().mean(1)).all()
+    assert ((rstd.double() * (v64 + 1e-5).sqrt() - 1).abs() <= k).all()
+    dx, dw, db = B.zeno_layer_norm_backward(dy, x, mean, rstd, w)
+    xh = (x64 - mean.double()[:, None]) * rstd.double()[:, None]
+    a = dy.double()
+    c1, c2 = a.mean(1, keepdim=True), (a * xh).mean(1, keepdim=True)
+    tol = rstd.double()[:, None] * (k * (a.abs().mean(1, keepdim=True) + xh.abs() * (a * xh).abs().mean(1, keepdim=True)) + 6 * 2.0 ** -24 * (a.abs() + (xh * c2).abs() + c1.abs()))
+    assert ((dx.double() - rstd.double()[:, None] * (a - c1 - xh * c2)).abs() <= tol).all()
+    assert ((dw[0].double() - (a * xh).sum(0)).abs() <= 8 * 2.0 ** -24 * (a * xh).abs().sum(0)).all()
+    assert ((db[0].double() - a.sum(0)).abs() <= 4 * 2.0 ** -24 * a.abs().sum(0)).all()
+    del x64, xh, a, tol, x, dy, y, dx, dw, db
+    for rows, out in ((40, 130), (70, 130), (70, 3)):
+        gen = torch.Generator().manual_seed(rows)
+        a = whole((rows, 1 << 12), gen).cuda().repeat(1, 1 << 12)
+        a[:, -5000:] = whole((rows, 5000), gen).cuda()
+        dy = whole((rows, out), gen).bfloat16().cuda()
+        dw, db = B.zeno_weight_gradient(dy, B.zeno_checkpoint(a))
+        dw = dw.view(out, width)
+        assert torch.equal(db[0], dy.float().sum(0))
+        for o in (0, 1, out // 2, out - 1):
+            assert torch.equal(dw[o], dy[:, o].float() @ a)
+        del a, dw
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+def test_a_layer_into_a_large_vocabulary(B, ty):
+    """The last layer of a token model: 50257 outputs, whole and in groups."""
+    g = torch.Generator().manual_seed(7)
+    rows, out, width = 300, 50257, 96
+    dy, a = whole((rows, out), g).to(TYPES[ty]).cuda(), whole((rows, width), g).cuda()
+    ck = B.zeno_checkpoint(a)
+    for cuts in ([0, rows], [3, 100, 100, 101, 290]):
+        dw, db = B.zeno_weight_gradient(dy, ck, groups=torch.tensor(cuts, dtype=torch.int32, device="cuda"))
+        for i, (p, q) in enumerate(zip(cuts, cuts[1:])):
+            d = dy[p:q].float()
+            assert torch.equal(dw[i].view(out, width), d.t().contiguous() @ a[p:q]) and torch.equal(db[i], d.sum(0))

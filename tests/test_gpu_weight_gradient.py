@@ -145,3 +145,43 @@ def test_every_nan_stays_one(B, out):
     assert torch.isnan(dw[2]).all() and torch.isnan(db[0, 2])
     keep = [o for o in range(out) if o != 2]
     assert (dw[keep] == 70).all() and (db[0, keep] == 70).all()
+
+
+def whole_sums(B, rows, out, width, ty, off, pitch=None, before=0):
+    """Small whole numbers, whose sums float32 holds exactly, and a workspace that held NaN."""
+    g = torch.Generator().manual_seed(rows + out + width)
+    dy, a = (torch.randint(-2, 3, (rows, n), generator=g).float() for n in (out, width))
+    dy, _ = T.strided(dy, T.TYPES[ty], pitch or out, before)
+    a = a.cuda()
+    m, n = len(off) - 1, out * width
+    G = torch.full((m, before + n + out + 1), 7.0, device="cuda")
+    ws = B.alloc_weight_gradient_workspace(rows, out, width, m).fill_(255)
+    B.zeno_weight_gradient(dy, B.zeno_checkpoint(a), groups=torch.tensor(off, dtype=torch.int32, device="cuda"), dweight=G[:, before:before + n],
+                           dbias=G[:, before + n:before + n + out], workspace=ws)
+    for i, (p, q) in enumerate(zip(off, off[1:])):
+        d = dy[p:q].float()
+        assert torch.equal(G[i, before:before + n].view(out, width), d.t().contiguous() @ a[p:q]), i
+        assert torch.equal(G[i, before + n:before + n + out], d.sum(0)), i
+    assert (G[:, :before] == 7).all() and (G[:, -1] == 7).all()
+    return ws.numel()
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,out,width,off", [
+    (16500, 4096, 1024, [3, 16490]), (16500, 4096, 1024, [0, 16500]), (9000, 2048, 2048, [0, 4000, 9000]),
+    (8300, 4093, 1025, [1, 8299]), (16400, 1000, 1000, [0, 5, 16400]), (17000, 521, 2050, [0, 0, 16993]), (17000, 300, 4095, [2, 35, 17000])])
+def test_wide_tiles_of_cut_tokens(B, rows, out, width, off, ty):
+    """Wide tiles whose tokens several workgroups share: ragged and empty groups, groups shorter than a piece, outputs that are no
+    multiple of eight and widths that end inside a tile."""
+    m = len(off) - 1
+    wide = -(-out // 256) * -(-width // 256) * m
+    assert out > 128 and width > 128 and wide < 256 and rows // m >= 1024 * ((255 + wide) // wide)      # what leads to this plan
+    used = whole_sums(B, rows, out, width, ty, off, pitch=out + 3 if out % 8 else out, before=1 if out % 8 else 0)
+    assert used >= 4 * m * ((255 + wide) // wide) * (out * width + out)
+
+
+@pytest.mark.parametrize("ty", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,out,width,off", [(9000, 200, 140, [0, 9000]), (5000, 129, 1000, [0, 8, 4990]), (12000, 12, 600, [5, 5, 12000])])
+def test_other_plans_of_cut_tokens(B, rows, out, width, off, ty):
+    used = whole_sums(B, rows, out, width, ty, off)
+    assert used > 256
