@@ -25,6 +25,10 @@ class TokenModel:
         if dtype not in B.DTYPE:
             raise ValueError(f"dtype must be one of {list(B.DTYPE)}")
         self.widths, self.dtype, self.eps = [int(w) for w in widths], dtype, float(eps)
+        # What fp16's backward pass multiplies a token's gradient by.  Its steps end at 2^-24: the mean's 1/n would push the probabilities of a
+        # large vocabulary below them (32000 values, 2500 tokens a worker: nine tenths of dlogits are 0), while 64 keeps 2^-30 of a token's
+        # loss, and 65504 / 64 = 1023 times it before a gradient is infinite.  The other types have float32's range and need none.
+        self.loss_scale = 64.0 if dtype == torch.float16 else 1.0
         self.offsets, at = [], 0
         for width, out in zip(self.widths, self.widths[1:]):
             parts = []
@@ -76,7 +80,9 @@ class TokenModel:
         bounds = groups.long()
         per_worker = (counted[bounds[1:]] - counted[bounds[:-1]]).clamp(min=1)
         worker = torch.bucketize(torch.arange(tokens, device=hidden.device), bounds[1:], right=True).clamp(max=m - 1)
-        dz = B.zeno_logprobs_backward(logits, stats, labels=labels, grad_logp=(-1.0 / per_worker[worker]).float(), out=logits)
+        unit = self.dtype == torch.float16    # the tokens' gradients are those of loss_scale times their own loss, not of the mean
+        grad = torch.full((tokens,), -self.loss_scale, device=hidden.device) if unit else (-1.0 / per_worker[worker]).float()
+        dz = B.zeno_logprobs_backward(logits, stats, labels=labels, grad_logp=grad, out=logits)
         for layer in reversed(range(len(kept))):
             norm_w, norm_b, w, b = [G[:, at:at + n] for at, n in self.offsets[layer]]
             ckpt_h, mean, rstd, ckpt_y, weights = kept[layer]
@@ -85,6 +91,8 @@ class TokenModel:
             scale = x[self.offsets[layer][0][0]:self.offsets[layer][0][0] + self.offsets[layer][0][1]]
             dz, _, _ = B.zeno_layer_norm_backward(dy, ckpt_h, mean, rstd, scale, groups=groups, want_dx=layer > 0,
                                                   dx=dy if layer > 0 else None, dweight=norm_w, dbias=norm_b)
+        if unit:
+            G *= (1.0 / (self.loss_scale * per_worker)).float()[:, None]
         return logp
 
     def scores(self, x, G, hidden, labels, gamma, rho):
