@@ -97,6 +97,8 @@ class TokenModel:
 
     def scores(self, x, G, hidden, labels, gamma, rho):
         """Definition 2 for every row of G on the server's tokens."""
+        if G.shape[1] != self.num_params:
+            raise ValueError("G needs rows of num_params")
         logp_x = self.logprobs(x, hidden, labels)
         logp = torch.empty((G.shape[0], hidden.shape[0]), dtype=torch.float32, device=hidden.device)
         for i in range(G.shape[0]):

@@ -161,3 +161,11 @@ def test_a_large_vocabulary_and_many_tokens(B, dtype):
         got, want, tol = G[i, at:at + size].double(), dz.sum(0), err.sum(0) + sums * dz.abs().sum(0)
         assert ((got - want).abs() <= tol).all(), ("bias", i, float(((got - want).abs() / tol).max()))
         assert not (want.abs() <= tol).any()
+
+
+def test_candidates_of_another_size_are_refused(B):
+    """A single column would otherwise be added to every parameter."""
+    model, x, hidden, labels, _ = setup([16, 9], 30, 2, torch.float32)
+    for d in (1, model.num_params - 1):
+        with pytest.raises(ValueError):
+            model.scores(x, torch.zeros(3, d, device="cuda"), hidden, labels, 0.1, 1e-3)
