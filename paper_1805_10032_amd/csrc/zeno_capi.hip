@@ -1156,7 +1156,8 @@ zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dt
       !aligned(top_index, 4) || !aligned(grad_top, 4))
     return ZENO_ERR_INVALID_ARG;
   const LogprobsGradArgs a = {logits, dlogits, ldz,     ldd,          dtype, rows,      vocab,
-                              stats,  labels,  grad_logp, grad_entropy, entropy, top, top_index, grad_top};
+                              stats,  labels,  grad_logp, grad_entropy, entropy, top, top_index, grad_top,
+                              (long long)rows * vocab * dtype_bytes(dtype) >= kPastBytes};
   ProfScope ps(ZENO_KERNEL_LOGPROBS_GRAD, 0, (double)rows * (2.0 * vocab * dtype_bytes(dtype) + 8.0 * top + 24.0),
                reinterpret_cast<hipStream_t>(stream));
   ZENO_TRY(launch_logprobs_backward(a, reinterpret_cast<hipStream_t>(stream)));
@@ -1225,7 +1226,7 @@ zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dty
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layer_norm_workspace_bytes(rows, width, m))
     return ZENO_ERR_WORKSPACE;
   const NormGradArgs a = {dy,    x,    values, scales, dx, lddy,    ldx,     lddx,  dtype, rows, width,
-                          mean, rstd, weight, m,      offsets, dweight, dbias, ldw,   ldb};
+                          mean, rstd, weight, m,      offsets, dweight, dbias, ldw,   ldb,   (long long)rows * width * dtype_bytes(dtype) >= kPastBytes};
   ProfScope ps(ZENO_KERNEL_LAYER_NORM_GRAD, 0,
                (double)rows * width * ((dx != nullptr ? 2.0 : 1.0) * dtype_bytes(dtype) + (x != nullptr ? dtype_bytes(dtype) : 33.0 / 32)) +
                    8.0 * m * width,

@@ -639,9 +639,8 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(LogprobsArgs a, Parts
 // ---- gradient:  dz_j = g [j = y] + sum_k q_k [j = i_k] - p_j (g + sum_k q_k + h (log p_j + H))
 // with g, h, q the gradients of logp, H and the alternatives' log probabilities.
 // L threads a segment of a row (16, 64 or 256): 256 / L segments a workgroup.  Each logit is read and each gradient written once, with no
-// reduction, so short segments and many workgroups keep the memory busy.  8192 x 32768 bf16: 187 us (5.7 TB/s), bound by memory.  With
-// ordinary stores 167, but what they leave in the caches is written while the next kernel runs: the forward pass of the next batch takes 120 us
-// instead of 95, a product that reads the gradient 10 more.
+// reduction, so short segments and many workgroups keep the memory busy.  8192 x 32768 bf16: 187 us (5.7 TB/s), bound by memory.  (With
+// ordinary stores 167 after a forward pass, which then takes 120 us instead of 95.)
 template <typename T, bool ENT, bool TOP, int L>
 __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArgs a, int segs, int seg_len) {
   constexpr int N = Wide<T>::N, EACH = kThreads / L;
@@ -663,7 +662,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogprobsGradArg
     const T* z = reinterpret_cast<const T*>(a.logits) + row * a.ldz + lo;
     T* out = reinterpret_cast<T*>(a.dlogits) + row * a.ldd + lo;
     float M = a.stats[2 * row], log_s = a.stats[2 * row + 1];
-    const bool empty = M == -inf && log_s == 0.f, past = on_line(out);
+    const bool empty = M == -inf && log_s == 0.f, past = a.large && on_line(out);
     int y = -1;
     float g = 0.f;
     if (a.grad_logp) {

@@ -437,7 +437,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
   P::fill(weight, a.weight, a.width);
   if (a.offsets == nullptr) __syncthreads();   // (or the search for the first group has one)
   // (16384 x 4096 bf16 85 -> 82 us, the next forward pass 68 -> 63; for rows of one wave the test costs what it may bring)
-  const bool past = NW >= 4 && on_line(a.dx) && a.lddx * (long long)sizeof(T) % 128 == 0;
+  const bool past = NW >= 4 && a.large && on_line(a.dx) && a.lddx * (long long)sizeof(T) % 128 == 0;
   int parity = 0;
   for (int g = first_group(a.offsets, a.m, r0, a.rows); g < a.m; ++g) {
     const int begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);

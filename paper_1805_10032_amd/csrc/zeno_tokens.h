@@ -38,9 +38,15 @@ __device__ inline void store_wide(T* p, const float (&v)[Wide<T>::N]) {
   *reinterpret_cast<typename Wide<T>::unaligned*>(p) = raw;
 }
 
-// Rows that start on a memory line may be written past the caches, where they would only displace what the next operators read: whole lines
-// leave at once.  Rows that do not would be written in parts (a weight gradient 1000 columns wide 41 -> 45 us).
+// Rows that start on a memory line may be written past the caches, whole lines at once, where the caches would keep them only to displace what
+// the next operators read and to write them then.  Rows that do not start on one would be written in parts (a weight gradient 1000 columns wide 41 ->
+// 45 us).
 __device__ inline bool on_line(const void* p) { return (reinterpret_cast<unsigned long long>(p) & 127) == 0; }
+// What the next launch reads back, gradients of activations and of logits, goes past the caches only where half of the 256 MB behind them would
+// not hold it.  Gradient, weight gradient from it and product with the weights, ordinary / past, us: dlogits in bf16 17 MB 90 / 92, 34 MB 141 /
+// 143, 134 MB 427 / 422, 537 MB 1149 / 1154; dx in bf16 17 MB 103 / 103, 134 MB 347 / 358.  The kernel again and again, with nothing that reads what
+// it wrote: dx 134 MB 90 / 74, dlogits in float32 268 MB 100 / 82.  A whole iteration takes the same time either way.
+constexpr long long kPastBytes = 128LL << 20;
 // (or the compiler joins such a store with the ordinary one of the other branch)
 __device__ inline void keep_apart() { asm volatile("" ::: "memory"); }
 template <typename T>
@@ -126,6 +132,7 @@ struct LogprobsGradArgs {
   int top;
   const int32_t* top_index;
   const float* grad_top;
+  bool large;   // dlogits: kPastBytes or more
 };
 hipError_t launch_logprobs_backward(const LogprobsGradArgs& a, hipStream_t stream);
 
@@ -221,6 +228,7 @@ struct NormGradArgs {
   const int32_t* offsets;           // nullptr: all rows are one group's
   float *dweight, *dbias;           // may be nullptr
   long long ldw, ldb;
+  bool large;                       // dx: kPastBytes or more
 };
 size_t layer_norm_workspace_bytes(int rows, int width, int m);
 hipError_t launch_layer_norm_backward(const NormGradArgs& a, void* workspace, hipStream_t stream);

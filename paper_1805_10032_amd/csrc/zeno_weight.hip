@@ -456,8 +456,10 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
   const long long size = (long long)a.out * a.width;
   float* dw = pieces == 1 ? a.dweight + g * a.ldw : partial + (long long)blockIdx.y * (size + a.out);
   const bool inside = o0 + S::OUT <= a.out && k0 + S::IN <= a.width;
-  // Gradients are read when all layers have theirs, so they go past the caches (20 x 100 tokens, 2048 x 2048 float32: 101 -> 86 us; two such
-  // layers, one of 8192 outputs and the scores together 2610 -> 2384 us, 1024 wide 812 -> 757); pieces are joined at once.
+  // Gradients are read when all layers have theirs, so they go past the caches, whatever their size: G as a whole is what the caches would have to
+  // hold.  Ordinary / past, us: 20 x 100 tokens, 2048 x 2048 float32 alone 108 / 92, with the scores and the update behind it 211 / 205 (bf16 204 /
+  // 206; 84 MB of G 71 / 73; 8 x 400 tokens, 4096 x 4096 424 / 381); whole iterations with 20 workers, three layers: 2048 wide and 8192 outputs
+  // float32 2935 / 2730, bf16 1757 / 1575, 1024 wide and 4096 outputs float32 924 / 876.  Pieces are joined at once.
   const bool past = inside && pieces == 1 && a.width % 32 == 0 && on_line(dw);
   if (past) {
 #pragma unroll

@@ -262,3 +262,31 @@ def test_a_layer_into_a_large_vocabulary(B, ty):
         for i, (p, q) in enumerate(zip(cuts, cuts[1:])):
             d = dy[p:q].float()
             assert torch.equal(dw[i].view(out, width), d.t().contiguous() @ a[p:q]) and torch.equal(db[i], d.sum(0))
+
+
+@pytest.mark.parametrize("ty", list(TYPES))
+def test_large_gradients_on_memory_lines_and_off_them(B, ty):
+    """From 128 MiB on, gradients of logits and of activations are written past the caches where their rows start on memory lines."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    dt = TYPES[ty]
+    size = torch.finfo(dt).bits // 8
+
+    def both(shape, call):
+        one, two = call(torch.full(shape, 7.0, dtype=dt, device="cuda")), call(off_line(shape, dt).fill_(7.0))
+        assert torch.equal(one, two) and not torch.isnan(one).any()
+
+    for vocab in (128, 192, 4096, 33000 // 64 * 64):
+        rows = (1 << 27) // (size * vocab) + 3
+        z = torch.randn(rows, vocab, generator=g, device="cuda").to(dt)
+        lab = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+        _, entropy, stats, index, _ = B.zeno_logprobs(z, lab, want_stats=True, want_entropy=True, top=2)
+        h, q = torch.randn(rows, generator=g, device="cuda"), torch.randn(rows, 2, generator=g, device="cuda")
+        for kw in (dict(), dict(top_index=index, grad_top=q), dict(entropy=entropy, grad_entropy=h)):
+            both(z.shape, lambda out: B.zeno_logprobs_backward(z, stats, labels=lab, grad_logp=h, out=out, **kw))
+    for width in (512, 1024, 2048, 4096, 8192, 12032, 16384):
+        rows = (1 << 27) // (size * width) + 3
+        x, dy = (torch.randn(rows, width, generator=g, device="cuda").to(dt) for _ in range(2))
+        w = torch.randn(width, generator=g, device="cuda")
+        _, mean, rstd, ck = B.zeno_layer_norm(x, w, want_checkpoint=True)
+        for src in (x, ck):
+            both(x.shape, lambda out: B.zeno_layer_norm_backward(dy, src, mean, rstd, w, dx=out)[0])
