@@ -81,7 +81,7 @@ class TokenModel:
         per_worker = (counted[bounds[1:]] - counted[bounds[:-1]]).clamp(min=1)
         worker = torch.bucketize(torch.arange(tokens, device=hidden.device), bounds[1:], right=True).clamp(max=m - 1)
         unit = self.dtype == torch.float16    # the tokens' gradients are those of loss_scale times their own loss, not of the mean
-        grad = torch.full((tokens,), -self.loss_scale, device=hidden.device) if unit else (-1.0 / per_worker[worker]).float()
+        grad = torch.full((tokens,), -self.loss_scale, dtype=torch.float32, device=hidden.device) if unit else (-1.0 / per_worker[worker]).float()
         dz = B.zeno_logprobs_backward(logits, stats, labels=labels, grad_logp=grad, out=logits)
         for layer in reversed(range(len(kept))):
             norm_w, norm_b, w, b = [G[:, at:at + n] for at, n in self.offsets[layer]]

@@ -169,3 +169,18 @@ def test_candidates_of_another_size_are_refused(B):
     for d in (1, model.num_params - 1):
         with pytest.raises(ValueError):
             model.scores(x, torch.zeros(3, d, device="cuda"), hidden, labels, 0.1, 1e-3)
+
+
+@pytest.mark.parametrize("dtype", list(T.TYPES.values()))
+def test_another_default_type(B, dtype):
+    model, x, hidden, labels, off = setup([16, 9], 30, 2, dtype)
+    groups = torch.tensor(off, dtype=torch.int32, device="cuda")
+    G, again = torch.empty(2, model.num_params, device="cuda"), torch.empty(2, model.num_params, device="cuda")
+    model.gradients(x, hidden, labels, groups, G)
+    scores = model.scores(x, G, hidden, labels, 0.1, 1e-3)
+    torch.set_default_dtype(torch.float64)
+    try:
+        model.gradients(x, hidden, labels, groups, again)
+        assert torch.equal(G, again) and torch.equal(scores, model.scores(x, G, hidden, labels, 0.1, 1e-3))
+    finally:
+        torch.set_default_dtype(torch.float32)
