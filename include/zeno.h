@@ -313,8 +313,9 @@ zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dt
  *   x  DEVICE [rows x width], rows ldx apart, 1 <= width <= ZENO_MAX_WIDTH */
 zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, uint8_t* values,
                               uint8_t* scales, void* stream);
-/* The values of a checkpoint as a matrix of `dtype`, for a backward pass of the caller's own.  Exact in float32 and bf16, except that a
- * value which was rounded up past the type's largest comes back as the largest. */
+/* The values of a checkpoint as a matrix of `dtype`, for a backward pass of the caller's own.  Exact in float32, and in bf16 where the scale is 2^-124
+ * (byte 3) or more: below, values under bf16's smallest step, 2^-133, are rounded to it.  In fp16 a value is rounded once.  One that the checkpoint
+ * rounded up past the type's largest comes back as the largest. */
 zeno_status_t zeno_checkpoint_values(const uint8_t* values, const uint8_t* scales, int32_t rows, int32_t width, int32_t dtype,
                                      void* out, int64_t ldo, void* stream);
 

@@ -100,3 +100,20 @@ def test_no_rows_and_what_lies_around(B):
     out, buf = T.strided(torch.zeros(4, 45), torch.bfloat16, 47, 3)
     B.zeno_checkpoint_values(ck, out=out)
     assert torch.equal(out, B.zeno_checkpoint_values(ck, torch.bfloat16)) and torch.isnan(T.around(out, buf)).all()
+
+
+def test_every_code_and_scale(B):
+    """The way back of all 256 codes at all 248 scales: exact in float32, and in bf16 but for what lies below its smallest steps (2^-133)."""
+    codes = np.tile(np.arange(256, dtype=np.uint8), (248, 1))
+    scales = np.tile(np.arange(248, dtype=np.uint8)[:, None], (1, 8))
+    ck = B.Checkpoint(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), 256)
+    want = T.checkpoint_values(codes, scales, 256)
+    for ty in (torch.float32, torch.bfloat16):
+        top = torch.finfo(ty).max
+        exact = np.clip(want, -top, top)
+        got = B.zeno_checkpoint_values(ck, ty).double().cpu().numpy()
+        same = (got == exact) | (np.isnan(got) & np.isnan(exact))
+        if ty == torch.bfloat16:
+            assert (np.abs(got - exact)[:3][~same[:3]] <= 2.0 ** -134).all()
+            same = same[3:]
+        assert same.all(), (ty, np.argwhere(~same)[:5])
