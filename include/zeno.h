@@ -280,9 +280,9 @@ typedef enum { ZENO_F32 = 0, ZENO_BF16 = 1, ZENO_F16 = 2 } zeno_dtype_t;
  *   stats      DEVICE [rows x 2] out, or NULL: max z and log sum exp(z - max z), which zeno_logprobs_backward takes
  *   top        0..min(ZENO_MAX_TOP, vocab); top_index DEVICE [rows x top] int32 and top_logp DEVICE [rows x top] out: the `top` largest
  *              logits' indices, the largest first, ties to the lower index, and their log probabilities; both NULL if top is 0
- * -inf is a token that cannot be drawn: probability 0, log probability -inf.  A row of nothing but -inf has no distribution: its log
- * probabilities are -inf, its entropy 0, its stats (-inf, 0), its gradient 0.  A row with a NaN or +inf gives NaN; in the choice of the
- * alternatives a NaN ranks as -inf.
+ * Finite logits of any size are taken (masks of -1e30 as well as of -1e9).  -inf is a token that cannot be drawn: probability 0, log
+ * probability -inf.  A row of nothing but -inf has no distribution: its log probabilities are -inf, its entropy 0, its stats (-inf, 0),
+ * its gradient 0.  A row with a NaN or +inf gives NaN; in the choice of the alternatives a NaN ranks as -inf.
  *   workspace  DEVICE, 256-byte aligned, >= zeno_logprobs_workspace_bytes(rows, vocab, top) */
 size_t zeno_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 zeno_status_t zeno_logprobs(const void* logits, int64_t ldz, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* labels,
@@ -313,9 +313,9 @@ zeno_status_t zeno_logprobs_backward(const void* logits, int64_t ldz, int32_t dt
  *   x  DEVICE [rows x width], rows ldx apart, 1 <= width <= ZENO_MAX_WIDTH */
 zeno_status_t zeno_checkpoint(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t width, uint8_t* values,
                               uint8_t* scales, void* stream);
-/* The values of a checkpoint as a matrix of `dtype`, for a backward pass of the caller's own.  Exact in float32, and in bf16 where the scale is 2^-124
- * (byte 3) or more: below, values under bf16's smallest step, 2^-133, are rounded to it.  In fp16 a value is rounded once.  One that the checkpoint
- * rounded up past the type's largest comes back as the largest. */
+/* The values of a checkpoint as a matrix of `dtype`, for a backward pass of the caller's own.  Exact in float32, and in bf16 where the
+ * scale is 2^-124 (byte 3) or more: below, values are rounded to multiples of bf16's smallest step, 2^-133.  In fp16 a value is rounded
+ * once.  One that the checkpoint rounded up past the type's largest comes back as the largest. */
 zeno_status_t zeno_checkpoint_values(const uint8_t* values, const uint8_t* scales, int32_t rows, int32_t width, int32_t dtype,
                                      void* out, int64_t ldo, void* stream);
 

@@ -191,7 +191,7 @@ struct Params {
 };
 
 // The next row is on its way while a row is reduced (the one after it as well: 72 -> 75 us).  Bound by memory and by what a row's two
-// reductions leave idle.  16384 x 4096 bf16 with a checkpoint 63 us (5.3 TB/s; a large copy moves 4.8), without one 51 us (5.3 TB/s);
+// reductions leave idle.  16384 x 4096 bf16 with a checkpoint 63 us (5.3 TB/s; plain streams of this mix reach 6.2), without one 51 us (5.3 TB/s);
 // 5003 x 1001 float32 11.5 us (3.5 TB/s), a launch and two round trips; 7634 x 6144 bf16 49 us, with a quarter of the threads idle.
 template <typename T, int NW, int CH>
 __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_kernel(NormArgs a) {
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(Shape<NW>::THREADS) void norm_grad_kernel(NormGradA
   }
 }
 
-// Rows too wide for the registers: dx from two reads of the row (2000 x 40000 bf16, both kernels and the join: 250 us) ...
+// Rows too wide for the registers: dx from two reads of the row (2000 x 40000 bf16, both kernels and the join: 299 us, from a checkpoint 254) ...
 template <typename T, bool KEPT>
 __global__ __launch_bounds__(1024) void norm_grad_long_dx_kernel(NormGradArgs a) {
   constexpr int N = Wide<T>::N;

@@ -28,7 +28,7 @@ struct Tile {
   static constexpr bool ODD = ODD_;
   static constexpr int WO = WO_, FO = FO_, FI = FI_, P = P_, KT = P == 1 ? 32 : 16;
   static constexpr int OUT = 32 * FO * WO, IN = 32 * FI * (4 / WO);
-  // bf16 of an LDS row, 64 bytes behind a multiple of 256: the four rows of a transposing read lie on different banks
+  // bf16 of an LDS row, 64 bytes behind a multiple of 256: the four rows of a transposing read lie on different banks (writes are not free of conflicts)
   static constexpr int PITCH_O = OUT + 32, PITCH_I = IN + 32;
   // what a thread fetches of a stage: 8 outputs of CO tokens, 16 inputs of CI
   static constexpr int CHUNKS_O = OUT / 8 * KT, CHUNKS_I = IN / 16 * KT;
@@ -288,8 +288,8 @@ __device__ inline void read_ring(int q, const Stage<S>& st, int wo, int lane, bf
 // Tiles: a wave's 128 x 128 of the product reads the fewest operands from LDS that the registers allow, at one wave a SIMD, which issues in
 // order: what runs beside the matrix instructions stands between them.
 // 8 x 2048 tokens, 4096 x 4096, bf16: 550-605 us (910-1000 TFLOP/s; a large bf16 product of the library with its operands stored this way
-// 1187, stored the other way 1369).  The matrix pipes are busy for 48 % of the time and the clock gives way under them (the same code without
-// memory traffic runs the stream of matrix instructions at 1770-1900 TFLOP/s); waves stand ready but unissued for 39 %.
+// 1187, stored the other way 1369).  The matrix pipes are busy for 52 % of the time and the clock gives way under them; waves stand ready but
+// unissued for 40 %.  LDS is active for 29 % of the cycles, a fifth of that conflicts.
 // 20 x 100 tokens, 2048 x 2048, float32: 86-92 us, 3.9 TB/s of gradients written; a tile has seven stages, and what is left is its first loads and its
 // 128 KB of stores where both workgroups of a compute unit are in them.  128 x 128 tiles: 134 us (102 with these before the stores went past
 // the caches).
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(kThreads, S::FO == 4 ? 1 : 2) void weight_grad_kern
 // thousand cycles of some 50 (widening the activations, splitting dy) and matrix instructions for 8; its two waves wait for half of their time,
 // each at its own LDS writes and reads.  A second batch on its way: 29.9 instead of 28.5 us for both launches; twice the pieces: 37.5.
 constexpr int kFewOutputs = 32, kFewInputs = 128, kFewTokens = 32;
-constexpr int kFewPitchI = kFewInputs + 32, kFewPitchO = kFewOutputs;   // rows of 320 and 64 bytes: four lie on different banks
+constexpr int kFewPitchI = kFewInputs + 32, kFewPitchO = kFewOutputs;   // rows of 320 and 64 bytes: four lie on different banks when read
 
 // (16-bit values in words of their own: packing them in pairs would wait for the loads)
 template <typename T>

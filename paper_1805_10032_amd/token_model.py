@@ -7,6 +7,10 @@ probabilities of the m + 1 models (TokenModel.scores, Definition 2); zeno_aggreg
 
 A parameter vector holds, layer by layer: the norm's weight and bias [width], the linear layer's weights [out x width] row-major
 and its bias [out], all float32.
+
+The operators' inputs and outputs are of the model's dtype, and so is what they cost in precision: activations are kept in 8 bits whatever the dtype
+(a term of a weight's gradient is off by up to 2^-4 of itself), and scores are differences of log probabilities whose logits are half a step off.  A
+server that needs them finer scores with a float32 model: the parameter vector is the same.
 """
 from __future__ import annotations
 
