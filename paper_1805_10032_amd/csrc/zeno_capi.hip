@@ -1123,7 +1123,7 @@ zeno_status_t zeno_logprobs(const void* logits, int64_t ldz, int32_t dtype, int3
                             void* workspace, size_t workspace_bytes, void* stream) {
   if (!matrix_ok(logits, ldz, dtype, rows, vocab) || top < 0 || top > vocab) return ZENO_ERR_INVALID_ARG;
   if (top > ZENO_MAX_TOP || vocab > ZENO_MAX_VOCAB || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
-  if (logp == nullptr && entropy == nullptr && stats == nullptr && top == 0) return ZENO_ERR_INVALID_ARG;
+  if (rows > 0 && logp == nullptr && entropy == nullptr && stats == nullptr && top == 0) return ZENO_ERR_INVALID_ARG;   // (outputs without rows have no address)
   if ((logp != nullptr && labels == nullptr && rows > 0) || (top > 0 && rows > 0 && (top_index == nullptr || top_logp == nullptr)))
     return ZENO_ERR_INVALID_ARG;
   if (!aligned(labels, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4) || !aligned(top_index, 4) ||
@@ -1218,13 +1218,14 @@ zeno_status_t zeno_layer_norm_backward(const void* dy, int64_t lddy, int32_t dty
   if (weight == nullptr || (rows > 0 && (mean == nullptr || rstd == nullptr))) return ZENO_ERR_INVALID_ARG;
   if (dx != nullptr && !matrix_ok(dx, lddx, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;
   if (dx != nullptr && dx == dy && lddx != lddy && rows > 1) return ZENO_ERR_INVALID_ARG;
-  if (dx == nullptr && dweight == nullptr && dbias == nullptr) return ZENO_ERR_INVALID_ARG;
+  if (rows > 0 && dx == nullptr && dweight == nullptr && dbias == nullptr) return ZENO_ERR_INVALID_ARG;
   if ((dweight != nullptr && ldw < width) || (dbias != nullptr && ldb < width)) return ZENO_ERR_INVALID_ARG;
   if (!aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
     return ZENO_ERR_INVALID_ARG;
   if (width > ZENO_MAX_WIDTH || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < layer_norm_workspace_bytes(rows, width, m))
     return ZENO_ERR_WORKSPACE;
+  if (rows == 0 && dweight == nullptr && dbias == nullptr) return ZENO_OK;
   const NormGradArgs a = {dy,    x,    values, scales, dx, lddy,    ldx,     lddx,  dtype, rows, width,
                           mean, rstd, weight, m,      offsets, dweight, dbias, ldw,   ldb,   (long long)rows * width * dtype_bytes(dtype) >= kPastBytes};
   ProfScope ps(ZENO_KERNEL_LAYER_NORM_GRAD, 0,

@@ -184,3 +184,57 @@ def test_another_default_type(B, dtype):
         assert torch.equal(G, again) and torch.equal(scores, model.scores(x, G, hidden, labels, 0.1, 1e-3))
     finally:
         torch.set_default_dtype(torch.float32)
+
+
+@pytest.mark.parametrize("dtype", list(T.TYPES.values()))
+def test_no_tokens(B, dtype):
+    """A batch without tokens: every worker sends zeros; each output by itself is empty."""
+    model, x, _, _, _ = setup([16, 9], 30, 2, dtype)
+    hidden, labels = torch.empty(0, 16, dtype=dtype, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    G = torch.full((3, model.num_params), 7.0, device="cuda")
+    logp = model.gradients(x, hidden, labels, torch.zeros(4, dtype=torch.int32, device="cuda"), G)
+    assert logp.shape == (0,) and not G.any()
+    assert B.zeno_logprobs(hidden, labels)[0].shape == (0,)
+    assert B.zeno_logprobs(hidden, want_entropy=True)[1].shape == (0,) and B.zeno_logprobs(hidden, want_stats=True)[2].shape == (0, 2)
+    w = torch.ones(16, device="cuda")
+    y, mean, rstd, ck = B.zeno_layer_norm(hidden, w, want_checkpoint=True)
+    for src in (hidden, ck):
+        dx, dw, db = B.zeno_layer_norm_backward(hidden, src, mean, rstd, w, want_weight=False, want_bias=False)
+        assert dx.shape == (0, 16) and dw is None and db is None
+
+
+@pytest.mark.parametrize("dtype", list(T.TYPES.values()))
+def test_captured_and_replayed(B, dtype):
+    """An iteration's gradients and scores in a graph, replayed on other tokens with eager work between."""
+    n, m = 700, 5
+    model, x, _, _, _ = setup([96, 160, 1000], 30, 2, dtype)
+    hidden, labels = torch.randn(n, 96, device="cuda").to(dtype), torch.zeros(n, dtype=torch.int32, device="cuda")
+    groups = torch.tensor([0, 100, 100, 300, 600, 690], dtype=torch.int32, device="cuda")
+    G, out = torch.empty(m, model.num_params, device="cuda"), {}
+
+    def run():
+        out["logp"] = model.gradients(x, hidden, labels, groups, G)
+        out["scores"] = model.scores(x, G, hidden[:64], labels[:64], 0.1, 1e-3)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    captured = dict(out)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for _ in range(4):
+        hidden.copy_(torch.randn(n, 96, generator=gen, device="cuda"))
+        labels.copy_(torch.randint(-1, 1000, (n,), generator=gen, device="cuda"))
+        run()
+        torch.cuda.synchronize()
+        want = G.clone(), out["logp"].clone(), out["scores"].clone()
+        G.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (G, captured["logp"], captured["scores"])))
+        assert all(torch.isfinite(t).all() for t in want) and G[0].any() and not G[1].any()

@@ -153,3 +153,16 @@ def test_the_binding_refuses_sizes_beyond_32_bits(B):
             call()
     weights = torch.empty(1, (1 << 31) + 5)        # (one layer's weights; the rows of such gradients are counted in 64 bits)
     assert B._grad_rows(weights, "dweight", 1, weights.shape[1], weights.get_device()) == (weights.data_ptr(), weights.shape[1])
+
+
+def test_outputs_without_rows_have_no_address(B):
+    """An empty tensor's pointer is NULL, whatever was asked for: no rows is no error."""
+    lib = B.load_library()
+    call = dict(CALLS["zeno_logprobs"], rows=0, logits=None, labels=None, logp=None, entropy=None, stats=None, top=0, top_index=None, top_logp=None,
+                workspace_bytes=1 << 20)
+    assert lib.zeno_logprobs(*call.values()) == 0
+    assert lib.zeno_logprobs(*dict(call, rows=1, logits=P).values()) == INVALID
+    call = dict(CALLS["zeno_layer_norm_backward"], rows=0, dy=None, x=None, mean=None, rstd=None, m=1, offsets=None, dx=None, dweight=None, dbias=None,
+                workspace_bytes=1 << 20)
+    assert lib.zeno_layer_norm_backward(*call.values()) == 0
+    assert lib.zeno_layer_norm_backward(*dict(call, rows=1, dy=P, x=P, mean=P, rstd=P).values()) == INVALID
