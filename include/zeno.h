@@ -362,7 +362,7 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
 /* Definition 2 for models whose forward passes are the caller's: f_r is the mean of -log p over the n tokens of the server's batch, and
  *   scores[i] = mean_t (logp[i][t] - logp_x[t]) - rho ||G[i]||^2.
  *   G, ldg  as for zeno_score (d = the row length)
- *   logp_x  DEVICE [n] log probabilities at x;  logp DEVICE [m x n], rows ldp >= n apart: at x - gamma G[i]
+ *   logp_x  DEVICE [n], n >= 1, log probabilities at x;  logp DEVICE [m x n], rows ldp >= n apart: at x - gamma G[i]
  *   labels  DEVICE [n] or NULL: tokens with label -1 do not count.  Where none counts the loss difference is 0
  *   workspace  DEVICE, 256-byte aligned, >= zeno_score_logprobs_workspace_bytes(m, d)
  * Differences, mean and norm are float64, rounded once; what the log probabilities themselves are rounded by (2^-24 of them) stays in
