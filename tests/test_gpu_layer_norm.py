@@ -273,3 +273,17 @@ def test_variance_out_of_range(B, width, ckpt):
     assert float(rstd[1]) == 0
     dx, dw, _ = B.zeno_layer_norm_backward(dy, kept if ckpt else x, mean, rstd, weight, groups=torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda"))
     assert not dx[1].any() and not dw[1].any() and torch.isfinite(dx).all() and dx[0].any() and dx[2].any()
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("rows,width,ty", [(1300, 257, "fp32"), (700, 512, "fp32"), (900, 513, "fp32"), (1100, 1025, "fp32"), (600, 2048, "fp32"),
+                                           (530, 2051, "fp32"), (520, 4096, "fp32"), (1200, 513, "bf16"), (800, 1025, "fp16"), (520, 8193, "bf16")])
+def test_every_shape_of_rows(B, rows, width, ty, ckpt):
+    """Both ends of every number of waves and pieces that a row may take, several rows a workgroup, ragged groups, also in place."""
+    x, _, weight, bias, g = make(rows, width, ty, rows + width)
+    check_forward(B, x, weight, bias, ckpt=ckpt)
+    off = [0, 7, 7, rows // 2 + 1, rows - 1]
+    dy = torch.randn(rows, width, generator=g).to(x.dtype).cuda()
+    dx, dw, db = check_backward(B, x, weight, off, ckpt, dy=dy)
+    inplace = check_backward(B, x, weight, off, ckpt, dy=dy, dx=dy)
+    assert inplace[0] is dy and torch.equal(dy[:-1], dx[:-1]) and torch.equal(inplace[1], dw) and torch.equal(inplace[2], db)

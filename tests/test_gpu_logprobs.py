@@ -410,3 +410,28 @@ def test_signalling_nan_beside_the_largest(B, rows, vocab, ty):
         z[rows - 16 + r, 16 + r] = 60.0
         z.view(bits)[rows - 16 + r, 16 + (r ^ 1)] = code
     check_forward(B, z, labels, 5)
+
+
+@pytest.mark.parametrize("rows,vocab,ty,lanes", [(3, 60000, "fp32", 1), (3, 60000, "bf16", 31), (514, 40000, "fp32", 1), (514, 9000, "bf16", 31),
+                                                 (5, 2048, "fp32", 31), (5, 2047, "fp16", 31), (1, 1 << 20, "bf16", 31), (2, 300000, "fp32", 20)])
+def test_more_of_the_largest_in_few_lanes_than_the_list_holds(B, rows, vocab, ty, lanes):
+    """The bound of the k-th value comes from 64 lanes' maxima: with the largest values in fewer than k of them it lies below more values
+    than are kept, which may be all different, in a few groups of equal ones, or equal with one of them infinite."""
+    n = 16 // torch.tensor([], dtype=T.TYPES[ty]).element_size()
+    g = torch.Generator().manual_seed(61)
+    lane = torch.arange(vocab) // n % 64
+    held = lane < lanes
+    assert int(held.sum()) > 512
+    z = torch.rand(rows, vocab, generator=g)
+    z[:, held] = 10 + torch.randint(0, 3000, (rows, int(held.sum())), generator=g).float() / 8
+    z[rows - 1, held] = 20.0
+    if rows > 1:
+        z[0, held] = 10 + torch.randint(0, 3, (int(held.sum()),), generator=g).float()
+    view, _ = T.strided(z, T.TYPES[ty])
+    for top in (lanes + 1, 32):
+        check_forward(B, view, None, top)
+    if ty == "fp32":
+        z[0, 4 * 64 + 1] = float("-inf")
+        z[rows - 1, 4 * 64 + 2] = float("inf")
+        view, _ = T.strided(z, T.TYPES[ty])
+        check_forward(B, view, None, 32)
