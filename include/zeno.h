@@ -359,6 +359,29 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
                                    const uint8_t* scales, int32_t width, int32_t m, const int32_t* offsets, float* dweight,
                                    int64_t ldw, float* dbias, int64_t ldb, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Embedding: out[t] = scale * table[ids[t]], the first operator of a model whose inputs are tokens.
+ *   table  DEVICE [vocab x width] of `table_dtype`, rows ldt elements apart: a block of a float32 parameter vector, or a copy in 16 bits
+ *   ids    DEVICE [rows].  -1: padding, a row of zeros; any other id outside 0..vocab-1 gives a row of NaN (nothing is read out of bounds)
+ *   scale  finite; the product is taken in float32
+ *   out    DEVICE [rows x width] of `dtype`, rows ldo apart
+ * 1 <= vocab <= ZENO_MAX_VOCAB, 1 <= width <= ZENO_MAX_WIDTH. */
+zeno_status_t zeno_embedding(const void* table, int64_t ldt, int32_t table_dtype, int32_t vocab, int32_t width, const int32_t* ids,
+                             int32_t rows, float scale, void* out, int64_t ldo, int32_t dtype, void* stream);
+
+/* Its gradient for each of m groups of rows: dtable_g[v] = scale * sum of dy[t] over the rows t of group g with ids[t] = v, summed in
+ * float32 in the order of the rows (pieces of equal length first) and multiplied by scale behind the sum.  Ids outside 0..vocab-1 take no part.
+ *   dy       DEVICE [rows x width] of `dtype`, rows lddy apart
+ *   dtable   DEVICE, group g's [vocab x width] row-major matrix at dtable + g ldg, ldg >= vocab * width (columns of rows of G)
+ *   accumulate  0: every row of every group's table is written, those of tokens that do not occur with zeros.  1: the gradients are added to what
+ *            dtable holds, and only rows of tokens that occur are touched (a table that is also the last layer's weights)
+ *   m, offsets  groups (above), 1 <= m <= ZENO_MAX_CANDIDATES
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_embedding_workspace_bytes(rows, vocab, width, m)
+ * UNSUPPORTED where m * vocab reaches 2^31. */
+size_t zeno_embedding_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t m);
+zeno_status_t zeno_embedding_backward(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t width, const int32_t* ids,
+                                      int32_t vocab, float scale, int32_t m, const int32_t* offsets, int32_t accumulate, float* dtable,
+                                      int64_t ldg, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Definition 2 for models whose forward passes are the caller's: f_r is the mean of -log p over the n tokens of the server's batch, and
  *   scores[i] = mean_t (logp[i][t] - logp_x[t]) - rho ||G[i]||^2.
  *   G, ldg  as for zeno_score (d = the row length)
@@ -421,7 +444,9 @@ typedef enum {
   ZENO_KERNEL_LAYER_NORM_GRAD = 16,
   ZENO_KERNEL_CHECKPOINT = 17,    /* either direction */
   ZENO_KERNEL_WEIGHT_GRAD = 18,
-  ZENO_KERNEL_SCORE_LOGPROBS = 19
+  ZENO_KERNEL_SCORE_LOGPROBS = 19,
+  ZENO_KERNEL_EMBEDDING = 20,
+  ZENO_KERNEL_EMBEDDING_GRAD = 21
 } zeno_kernel_t;
 
 typedef struct {

@@ -28,11 +28,11 @@ EXPORTS = ["zeno_model_create", "zeno_cnn_model_create", "zeno_model_destroy", "
            "zeno_score_plan_check", "zeno_logprobs_workspace_bytes", "zeno_logprobs", "zeno_logprobs_backward", "zeno_checkpoint",
            "zeno_checkpoint_values", "zeno_layer_norm", "zeno_layer_norm_workspace_bytes", "zeno_layer_norm_backward",
            "zeno_weight_gradient_workspace_bytes", "zeno_weight_gradient", "zeno_score_logprobs_workspace_bytes",
-           "zeno_score_logprobs"]
+           "zeno_score_logprobs", "zeno_embedding", "zeno_embedding_workspace_bytes", "zeno_embedding_backward"]
 
 KERNEL_NAMES = ["pack", "layer_base", "layer_cand", "loss", "combine", "average", "mean", "median", "average_update",
                 "krum", "conv_base", "conv_cand", "aux", "logprobs", "logprobs_grad", "layer_norm", "layer_norm_grad", "checkpoint",
-                "weight_grad", "score_logprobs"]
+                "weight_grad", "score_logprobs", "embedding", "embedding_grad"]
 ZENO_MAX_CONV = 8
 ZENO_MAX_TOP = 32
 DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -133,7 +133,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             ("zeno_weight_gradient_workspace_bytes", size, [i32, i32, i32, i32]),
             ("zeno_weight_gradient", ctypes.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, i64, vp, i64, vp, size, vp]),
             ("zeno_score_logprobs_workspace_bytes", size, [i32, i64]),
-            ("zeno_score_logprobs", ctypes.c_int, [vp, i64, i32, i64, vp, vp, i64, i32, vp, f32, vp, vp, size, vp])]:
+            ("zeno_score_logprobs", ctypes.c_int, [vp, i64, i32, i64, vp, vp, i64, i32, vp, f32, vp, vp, size, vp]),
+            ("zeno_embedding", ctypes.c_int, [vp, i64, i32, i32, i32, vp, i32, f32, vp, i64, i32, vp]),
+            ("zeno_embedding_workspace_bytes", size, [i32, i32, i32, i32]),
+            ("zeno_embedding_backward", ctypes.c_int, [vp, i64, i32, i32, i32, vp, i32, f32, i32, vp, i32, vp, i64, vp, size, vp])]:
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
     lib.zeno_profile_enable.argtypes = [i32]
     lib.zeno_profile_enable.restype = ctypes.c_int
@@ -757,6 +760,54 @@ def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, d
     if st != 0:
         raise ZenoError(st, "zeno_weight_gradient")
     return dweight, dbias
+
+
+def zeno_embedding(ids, table, dtype=None, *, scale=1.0, out=None):
+    """scale * table[ids] as `dtype` (default: the table's).  ids int32 [rows] (-1: a row of zeros), table [vocab x width], for instance
+    a block of a parameter vector."""
+    lib = load_library()
+    dev = _current(ids, "ids")
+    if ids.dim() != 1 or ids.numel() > _MOST:
+        raise ValueError("ids must be a vector")
+    rows = int(ids.numel())
+    ptr, pitch, code, vocab, width = _matrix(table, "table", dev)
+    if out is None:
+        out = table.new_empty((rows, width), dtype=dtype or table.dtype)
+    o_ptr, o_pitch, o_code, _, _ = _matrix(out, "out", dev, (rows, width), dtype)
+    st = lib.zeno_embedding(ptr, pitch, code, vocab, width, _vec(ids, torch.int32, "ids", (rows,), dev), rows, float(scale), o_ptr, o_pitch,
+                            o_code, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_embedding")
+    return out
+
+
+def alloc_embedding_workspace(rows: int, vocab: int, width: int, m: int = 1, device=None) -> torch.Tensor:
+    sizes = _size32("zeno_embedding_workspace_bytes", int(rows), int(vocab), int(width), int(m))
+    return _workspace(int(load_library().zeno_embedding_workspace_bytes(*sizes)), "zeno_embedding_workspace_bytes", device)
+
+
+def zeno_embedding_backward(dy, ids, vocab: int, *, scale=1.0, groups=None, dtable=None, accumulate=False, workspace=None):
+    """Gradient of the table of zeno_embedding for each of the m workers: dtable [m x vocab * width] float32, for instance column slices
+    of G.  accumulate=True adds to what dtable holds."""
+    lib = load_library()
+    dev = _current(dy, "dy")
+    ptr, pitch, code, rows, width = _matrix(dy, "dy", dev)
+    m, offsets = _groups(groups, dev)
+    vocab = int(vocab)
+    _size32("zeno_embedding_backward", vocab)
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs a dtable to add to")
+        dtable = dy.new_empty((m, max(vocab, 0) * width), dtype=torch.float32)
+    g_ptr, ldg = _grad_rows(dtable, "dtable", m, vocab * width, dev)
+    if workspace is None:
+        workspace = alloc_embedding_workspace(rows, vocab, width, m, dy.device)
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_embedding_backward(ptr, pitch, code, rows, width, _vec(ids, torch.int32, "ids", (rows,), dev), vocab, float(scale), m,
+                                     offsets, 1 if accumulate else 0, g_ptr, ldg, ws, ws_bytes, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_embedding_backward")
+    return dtable
 
 
 def alloc_score_logprobs_workspace(m: int, d: int, device=None) -> torch.Tensor:

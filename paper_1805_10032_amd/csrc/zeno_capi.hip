@@ -1259,6 +1259,47 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
   return ZENO_OK;
 }
 
+zeno_status_t zeno_embedding(const void* table, int64_t ldt, int32_t table_dtype, int32_t vocab, int32_t width, const int32_t* ids,
+                             int32_t rows, float scale, void* out, int64_t ldo, int32_t dtype, void* stream) {
+  if (!matrix_ok(table, ldt, table_dtype, vocab, width) || vocab < 1 || !matrix_ok(out, ldo, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;
+  if ((rows > 0 && ids == nullptr) || !aligned(ids, 4) || !std::isfinite(scale)) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH || vocab > ZENO_MAX_VOCAB || rows > ZENO_MAX_ROWS) return ZENO_ERR_UNSUPPORTED;
+  if (rows == 0) return ZENO_OK;
+  const EmbedArgs a = {table, out, ldt, ldo, table_dtype, dtype, vocab, width, rows, ids, scale};
+  ProfScope ps(ZENO_KERNEL_EMBEDDING, 0,
+               (double)rows * (4.0 + (double)width * dtype_bytes(dtype)) + (double)std::min(rows, vocab) * width * dtype_bytes(table_dtype),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_embedding(a, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+size_t zeno_embedding_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t m) {
+  if (rows < 0 || rows > ZENO_MAX_ROWS || vocab < 1 || vocab > ZENO_MAX_VOCAB || width < 1 || width > ZENO_MAX_WIDTH || m < 1 ||
+      m > ZENO_MAX_CANDIDATES || (int64_t)m * vocab >= (int64_t)1 << 31)
+    return 0;
+  return embedding_workspace_bytes(rows, vocab, width, m);
+}
+
+zeno_status_t zeno_embedding_backward(const void* dy, int64_t lddy, int32_t dtype, int32_t rows, int32_t width, const int32_t* ids,
+                                      int32_t vocab, float scale, int32_t m, const int32_t* offsets, int32_t accumulate, float* dtable,
+                                      int64_t ldg, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(dy, lddy, dtype, rows, width) || vocab < 1 || !groups_ok(m, offsets)) return ZENO_ERR_INVALID_ARG;
+  if (dtable == nullptr || ldg < (int64_t)vocab * width || !aligned(dtable, 4)) return ZENO_ERR_INVALID_ARG;
+  if ((rows > 0 && ids == nullptr) || !aligned(ids, 4) || !std::isfinite(scale) || accumulate < 0 || accumulate > 1) return ZENO_ERR_INVALID_ARG;
+  if (width > ZENO_MAX_WIDTH || vocab > ZENO_MAX_VOCAB || rows > ZENO_MAX_ROWS || (int64_t)m * vocab >= (int64_t)1 << 31) return ZENO_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < embedding_workspace_bytes(rows, vocab, width, m))
+    return ZENO_ERR_WORKSPACE;
+  EmbedGradArgs a = {};
+  a.dy = dy, a.lddy = lddy, a.dtype = dtype, a.rows = rows, a.width = width, a.ids = ids, a.vocab = vocab, a.scale = scale, a.m = m;
+  a.offsets = offsets, a.accumulate = accumulate != 0, a.dtable = dtable, a.ldg = ldg;
+  ProfScope ps(ZENO_KERNEL_EMBEDDING_GRAD, 0,
+               (double)rows * (4.0 + (double)width * dtype_bytes(dtype)) +
+                   4.0 * width * (accumulate ? 2.0 * std::min<double>(rows, (double)m * vocab) : (double)m * vocab),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_embedding_backward(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
 size_t zeno_score_logprobs_workspace_bytes(int32_t m, int64_t d) {
   if (m < 1 || m > ZENO_MAX_CANDIDATES || d < 1) return 0;
   return score_logprobs_workspace_bytes(m, d);

@@ -1,5 +1,5 @@
 // Shared by the operators for models that answer with tokens (log probabilities, layer norm, activations in 8 bits, weight
-// gradients, the score from log probabilities): element types, 128-bit access to rows at any element alignment, reductions.
+// gradients, embedding, the score from log probabilities): element types, 128-bit access to rows at any element alignment, reductions.
 #ifndef ZENO_TOKENS_H_
 #define ZENO_TOKENS_H_
 
@@ -254,6 +254,39 @@ struct WeightGradArgs {
 bool weight_gradient_fits(int out, int width);   // one launch
 size_t weight_gradient_workspace_bytes(int rows, int out, int width, int m);
 hipError_t launch_weight_gradient(const WeightGradArgs& a, void* workspace, hipStream_t stream);
+
+// ---- embedding (zeno_embedding.hip)
+struct EmbedArgs {
+  const void* table;
+  void* out;
+  long long ldt, ldo;
+  int table_dtype, dtype, vocab, width, rows;
+  const int32_t* ids;
+  float scale;
+};
+hipError_t launch_embedding(const EmbedArgs& a, hipStream_t stream);
+
+struct EmbedGradArgs {
+  const void* dy;
+  long long lddy;
+  int dtype, rows, width;
+  const int32_t* ids;
+  int vocab;
+  float scale;
+  int m;
+  const int32_t* offsets;   // nullptr: all rows are one group's
+  bool accumulate;
+  float* dtable;
+  long long ldg;
+  // set by the launch: the workspace's parts and how the work is cut
+  unsigned* key[2];
+  int* index[2];
+  unsigned *count, *total;
+  float* slots;
+  long long pieces, per_piece, fill_pieces;
+};
+size_t embedding_workspace_bytes(int rows, int vocab, int width, int m);
+hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream_t stream);
 
 // ---- the score from log probabilities (zeno_score_tokens.hip)
 size_t score_logprobs_workspace_bytes(int m, long long d);
