@@ -359,6 +359,47 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
                                    const uint8_t* scales, int32_t width, int32_t m, const int32_t* offsets, float* dweight,
                                    int64_t ldw, float* dbias, int64_t ldb, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Log probabilities of a linear layer's outputs, z = hidden weight^T + bias, without the logits: what zeno_logprobs makes of them, formed
+ * tile by tile and never stored.  The logits stay float32 (a product of 16-bit operands is exact and only the sums round; float32 operands
+ * enter as three bf16 pieces, six piece products: float32 accuracy).
+ *   hidden  DEVICE [rows x width] of `dtype`, rows ldh apart
+ *   weight  DEVICE [vocab x width] of `dtype`, rows ldw apart
+ *   bias    DEVICE [vocab] float32 or NULL.  -inf (or any low value) is a token that cannot be drawn
+ *   labels, logp, entropy, stats  as for zeno_logprobs (labels and logp both NULL if not wanted), with its rules for tokens without a distribution
+ * Masks belong into the bias: a hidden state or a weight that is not finite makes NaN of the logits it enters, or infinities.
+ * Operands whose rows start on 16 bytes and hold a multiple of eight values are read as they are, others are copied first (weights in
+ * pieces of the vocabulary).  1 <= width <= ZENO_MAX_HIDDEN, 1 <= vocab <= ZENO_MAX_OUTPUTS, rows <= ZENO_MAX_TOKENS, vocab * width <= 2^36.
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_linear_logprobs_workspace_bytes(rows, vocab, width, dtype) */
+#define ZENO_MAX_HIDDEN (1 << 16)
+#define ZENO_MAX_OUTPUTS (1 << 24)
+#define ZENO_MAX_TOKENS (1 << 22)
+size_t zeno_linear_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t dtype);
+zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* weight, int64_t ldw, int32_t dtype, const float* bias,
+                                   int32_t rows, int32_t vocab, int32_t width, const int32_t* labels, float* logp, float* entropy,
+                                   float* stats, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients for gradients g of logp and q of the entropy, the vocabulary in pieces whose logits are formed again:
+ *   dz_j = g [j = label] - p_j (g + q (log p_j + H)),   dhidden = dz weight,   dweight_g = sum of dz[t] hidden[t]^T over the rows of group g,
+ *   dbias_g = sum of dz[t].
+ * In 16-bit types dweight and dbias are taken from dz in two pieces of the type (off by at most 2^-16 of it in bf16, in fp16 2^-22 or
+ * 2^-38 of the largest gradient of the call), dhidden, which is rounded itself, from the first; in float32 from three bf16 pieces.
+ *   stats, entropy  as zeno_linear_logprobs wrote them (entropy only if grad_entropy is given)
+ *   labels, grad_logp        DEVICE [rows] or both NULL; a row with label -1 takes no part in g, another label outside 0..vocab-1 gives NaN
+ *   grad_entropy             DEVICE [rows] or NULL
+ *   dhidden  DEVICE [rows x width] of `dtype`, rows lddh apart, or NULL; may be hidden itself with lddh = ldh
+ *   dweight  DEVICE, group g's [vocab x width] row-major matrix at dweight + g ldg, ldg >= vocab * width, or NULL
+ *   dbias    DEVICE, group g's [vocab] at dbias + g ldb, ldb >= vocab, or NULL
+ *   m, offsets  groups (above); rows of no group take no part
+ * At least one of the gradients and one of the outputs is given.
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, m) */
+size_t zeno_linear_logprobs_backward_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t dtype, int32_t m);
+zeno_status_t zeno_linear_logprobs_backward(const void* hidden, int64_t ldh, const void* weight, int64_t ldw, int32_t dtype,
+                                            const float* bias, int32_t rows, int32_t vocab, int32_t width, const float* stats,
+                                            const int32_t* labels, const float* grad_logp, const float* entropy,
+                                            const float* grad_entropy, int32_t m, const int32_t* offsets, void* dhidden, int64_t lddh,
+                                            float* dweight, int64_t ldg, float* dbias, int64_t ldb, void* workspace,
+                                            size_t workspace_bytes, void* stream);
+
 /* Embedding: out[t] = scale * table[ids[t]], the first operator of a model whose inputs are tokens.
  *   table  DEVICE [vocab x width] of `table_dtype`, rows ldt elements apart: a block of a float32 parameter vector, or a copy in 16 bits
  *   ids    DEVICE [rows].  -1: padding, a row of zeros; any other id outside 0..vocab-1 gives a row of NaN (nothing is read out of bounds)
@@ -446,7 +487,9 @@ typedef enum {
   ZENO_KERNEL_WEIGHT_GRAD = 18,
   ZENO_KERNEL_SCORE_LOGPROBS = 19,
   ZENO_KERNEL_EMBEDDING = 20,
-  ZENO_KERNEL_EMBEDDING_GRAD = 21
+  ZENO_KERNEL_EMBEDDING_GRAD = 21,
+  ZENO_KERNEL_LINEAR_LOGPROBS = 22,
+  ZENO_KERNEL_LINEAR_LOGPROBS_GRAD = 23
 } zeno_kernel_t;
 
 typedef struct {

@@ -28,11 +28,14 @@ EXPORTS = ["zeno_model_create", "zeno_cnn_model_create", "zeno_model_destroy", "
            "zeno_score_plan_check", "zeno_logprobs_workspace_bytes", "zeno_logprobs", "zeno_logprobs_backward", "zeno_checkpoint",
            "zeno_checkpoint_values", "zeno_layer_norm", "zeno_layer_norm_workspace_bytes", "zeno_layer_norm_backward",
            "zeno_weight_gradient_workspace_bytes", "zeno_weight_gradient", "zeno_score_logprobs_workspace_bytes",
-           "zeno_score_logprobs", "zeno_embedding", "zeno_embedding_workspace_bytes", "zeno_embedding_backward"]
+           "zeno_score_logprobs", "zeno_embedding", "zeno_embedding_workspace_bytes", "zeno_embedding_backward",
+           "zeno_linear_logprobs_workspace_bytes", "zeno_linear_logprobs", "zeno_linear_logprobs_backward_workspace_bytes",
+           "zeno_linear_logprobs_backward"]
 
 KERNEL_NAMES = ["pack", "layer_base", "layer_cand", "loss", "combine", "average", "mean", "median", "average_update",
                 "krum", "conv_base", "conv_cand", "aux", "logprobs", "logprobs_grad", "layer_norm", "layer_norm_grad", "checkpoint",
-                "weight_grad", "score_logprobs", "embedding", "embedding_grad"]
+                "weight_grad", "score_logprobs", "embedding", "embedding_grad", "linear_logprobs",
+                "linear_logprobs_grad"]
 ZENO_MAX_CONV = 8
 ZENO_MAX_TOP = 32
 DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -136,7 +139,12 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
             ("zeno_score_logprobs", ctypes.c_int, [vp, i64, i32, i64, vp, vp, i64, i32, vp, f32, vp, vp, size, vp]),
             ("zeno_embedding", ctypes.c_int, [vp, i64, i32, i32, i32, vp, i32, f32, vp, i64, i32, vp]),
             ("zeno_embedding_workspace_bytes", size, [i32, i32, i32, i32]),
-            ("zeno_embedding_backward", ctypes.c_int, [vp, i64, i32, i32, i32, vp, i32, f32, i32, vp, i32, vp, i64, vp, size, vp])]:
+            ("zeno_embedding_backward", ctypes.c_int, [vp, i64, i32, i32, i32, vp, i32, f32, i32, vp, i32, vp, i64, vp, size, vp]),
+            ("zeno_linear_logprobs_workspace_bytes", size, [i32, i32, i32, i32]),
+            ("zeno_linear_logprobs", ctypes.c_int, [vp, i64, vp, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, size, vp]),
+            ("zeno_linear_logprobs_backward_workspace_bytes", size, [i32, i32, i32, i32, i32]),
+            ("zeno_linear_logprobs_backward", ctypes.c_int, [vp, i64, vp, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, i64,
+                                                             vp, i64, vp, i64, vp, size, vp])]:
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
     lib.zeno_profile_enable.argtypes = [i32]
     lib.zeno_profile_enable.restype = ctypes.c_int
@@ -760,6 +768,93 @@ def zeno_weight_gradient(dy, ckpt: Checkpoint, *, groups=None, want_bias=True, d
     if st != 0:
         raise ZenoError(st, "zeno_weight_gradient")
     return dweight, dbias
+
+
+def _linear_workspace(where: str, dtype, device, *sizes):
+    if dtype not in DTYPE:
+        raise ValueError(f"dtype must be one of {list(DTYPE)}")
+    rows, vocab, width, *m = _size32(where, *(int(n) for n in sizes))
+    return _workspace(int(getattr(load_library(), where)(rows, vocab, width, DTYPE[dtype], *m)), where, device)
+
+
+def alloc_linear_logprobs_workspace(rows: int, vocab: int, width: int, dtype=torch.bfloat16, device=None) -> torch.Tensor:
+    return _linear_workspace("zeno_linear_logprobs_workspace_bytes", dtype, device, rows, vocab, width)
+
+
+def alloc_linear_logprobs_backward_workspace(rows: int, vocab: int, width: int, dtype=torch.bfloat16, m: int = 1, device=None) -> torch.Tensor:
+    return _linear_workspace("zeno_linear_logprobs_backward_workspace_bytes", dtype, device, rows, vocab, width, m)
+
+
+def zeno_linear_logprobs(hidden, weight, bias=None, labels=None, *, want_entropy=False, want_stats=False, logp=None, entropy=None,
+                         stats=None, workspace=None):
+    """zeno_logprobs of the logits hidden weight^T + bias, which are never stored.  hidden [rows x width] and weight [vocab x width] of one
+    dtype, bias float32 [vocab].  Returns (logp, entropy, stats), None where not wanted; `stats` [rows x 2] is what
+    zeno_linear_logprobs_backward takes."""
+    lib = load_library()
+    dev = _current(hidden, "hidden")
+    ptr, pitch, code, rows, width = _matrix(hidden, "hidden", dev)
+    w_ptr, w_pitch, _, vocab, w_width = _matrix(weight, "weight", dev, None, hidden.dtype)
+    if w_width != width:
+        raise ValueError(f"weight must have {width} columns, got {w_width}")
+    f32, new = torch.float32, hidden.new_empty
+
+    def out(t, want, shape, name):
+        if t is not None:
+            return t, _vec(t, f32, name, shape, dev)
+        if not want:
+            return None, None
+        t = new(shape, dtype=f32)
+        return t, t.data_ptr()
+
+    logp, logp_p = out(logp, labels is not None, (rows,), "logp")
+    entropy, entropy_p = out(entropy, want_entropy, (rows,), "entropy")
+    stats, stats_p = out(stats, want_stats, (rows, 2), "stats")
+    if workspace is None:
+        workspace = alloc_linear_logprobs_workspace(rows, vocab, width, hidden.dtype, hidden.device)
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_linear_logprobs(ptr, pitch, w_ptr, w_pitch, code, _vec(bias, f32, "bias", (vocab,), dev), rows, vocab, width,
+                                  _vec(labels, torch.int32, "labels", (rows,), dev), logp_p, entropy_p, stats_p, ws, ws_bytes, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_linear_logprobs")
+    return logp, entropy, stats
+
+
+def zeno_linear_logprobs_backward(hidden, weight, bias, stats, *, labels=None, grad_logp=None, entropy=None, grad_entropy=None, groups=None,
+                                  want_hidden=True, want_weight=True, want_bias=True, dhidden=None, dweight=None, dbias=None,
+                                  workspace=None):
+    """Gradients of the hidden states and, for each of the m workers, of the weights and the bias, from the gradients of logp [rows] and of
+    the entropy [rows].  dweight [m x vocab * width] and dbias [m x vocab] are float32, for instance column slices of G; dhidden=hidden
+    works in place; rows that belong to no group keep what dhidden held (zeros if it is not given).  Returns (dhidden, dweight, dbias)."""
+    lib = load_library()
+    dev = _current(hidden, "hidden")
+    ptr, pitch, code, rows, width = _matrix(hidden, "hidden", dev)
+    w_ptr, w_pitch, _, vocab, w_width = _matrix(weight, "weight", dev, None, hidden.dtype)
+    if w_width != width:
+        raise ValueError(f"weight must have {width} columns, got {w_width}")
+    m, offsets = _groups(groups, dev)
+    f32 = torch.float32
+    if want_hidden and dhidden is None:
+        dhidden = hidden.new_empty((rows, width)) if groups is None else hidden.new_zeros((rows, width))
+    if want_weight and dweight is None:
+        dweight = hidden.new_empty((m, vocab * width), dtype=f32)
+    if want_bias and dbias is None:
+        dbias = hidden.new_empty((m, vocab), dtype=f32)
+    d_ptr, d_pitch = None, width
+    if dhidden is not None:
+        d_ptr, d_pitch, _, _, _ = _matrix(dhidden, "dhidden", dev, (rows, width), hidden.dtype)
+    g_ptr, ldg = _grad_rows(dweight, "dweight", m, vocab * width, dev)
+    b_ptr, ldb = _grad_rows(dbias, "dbias", m, vocab, dev)
+    if workspace is None:
+        workspace = alloc_linear_logprobs_backward_workspace(rows, vocab, width, hidden.dtype, m, hidden.device)
+    ws, ws_bytes = _scratch(workspace, dev)
+    st = lib.zeno_linear_logprobs_backward(ptr, pitch, w_ptr, w_pitch, code, _vec(bias, f32, "bias", (vocab,), dev), rows, vocab, width,
+                                           _vec(stats, f32, "stats", (rows, 2), dev), _vec(labels, torch.int32, "labels", (rows,), dev),
+                                           _vec(grad_logp, f32, "grad_logp", (rows,), dev), _vec(entropy, f32, "entropy", (rows,), dev),
+                                           _vec(grad_entropy, f32, "grad_entropy", (rows,), dev), m, offsets, d_ptr, d_pitch, g_ptr, ldg,
+                                           b_ptr, ldb, ws, ws_bytes, _stream())
+    if st != 0:
+        raise ZenoError(st, "zeno_linear_logprobs_backward")
+    return dhidden, dweight, dbias
 
 
 def zeno_embedding(ids, table, dtype=None, *, scale=1.0, out=None):

@@ -21,7 +21,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 # number of row blocks (four of them in bf16 only), longest first, so that ten objects build in parallel.
 LAYER_UNITS = ["zeno_layer_bf16_delta.hip", "zeno_layer_bf16_first.hip", "zeno_layer_f32_delta.hip", "zeno_layer_f32_first.hip"]
 TOKEN_SOURCES = ("zeno_logprobs.hip", "zeno_norm.hip", "zeno_checkpoint.hip", "zeno_weight.hip", "zeno_score_tokens.hip",
-                 "zeno_embedding.hip")
+                 "zeno_embedding.hip", "zeno_linear_logprobs.hip")
 SOURCES = ([(u, f"_mb{mb}", [f"-DZENO_LAYER_MB={mb}"]) for mb in (4, 2, 1) for u in LAYER_UNITS if mb < 4 or "bf16" in u] +
            [(s, "", []) for s in ("zeno_median.hip", "zeno_krum.hip", "zeno_capi.hip", "zeno_layer.hip", "zeno_loss.hip",
                                   "zeno_aggregate.hip", "zeno_median_select.hip", "zeno_conv.hip", "zeno_small.hip", "zeno_first.hip",

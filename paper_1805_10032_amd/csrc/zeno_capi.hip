@@ -1259,6 +1259,73 @@ zeno_status_t zeno_weight_gradient(const void* dy, int64_t lddy, int32_t dtype, 
   return ZENO_OK;
 }
 
+static bool linear_sizes_ok(int32_t rows, int32_t vocab, int32_t width) {
+  return rows <= ZENO_MAX_TOKENS && vocab <= ZENO_MAX_OUTPUTS && width <= ZENO_MAX_HIDDEN && (int64_t)vocab * width <= (int64_t)1 << 36;
+}
+static bool linear_query_ok(int32_t rows, int32_t vocab, int32_t width, int32_t dtype) {
+  return rows >= 0 && vocab >= 1 && width >= 1 && linear_sizes_ok(rows, vocab, width) &&
+         (dtype == ZENO_F32 || dtype == ZENO_BF16 || dtype == ZENO_F16);
+}
+
+size_t zeno_linear_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t dtype) {
+  return linear_query_ok(rows, vocab, width, dtype) ? linear_logprobs_workspace_bytes(rows, vocab, width, dtype) : 0;
+}
+
+zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* weight, int64_t ldw, int32_t dtype, const float* bias,
+                                   int32_t rows, int32_t vocab, int32_t width, const int32_t* labels, float* logp, float* entropy,
+                                   float* stats, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(hidden, ldh, dtype, rows, width) || vocab < 1 || !matrix_ok(weight, ldw, dtype, vocab, width)) return ZENO_ERR_INVALID_ARG;
+  if (!linear_sizes_ok(rows, vocab, width)) return ZENO_ERR_UNSUPPORTED;
+  if (rows > 0 && logp == nullptr && entropy == nullptr && stats == nullptr) return ZENO_ERR_INVALID_ARG;   // (outputs without rows have no address)
+  if (logp != nullptr && labels == nullptr && rows > 0) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(bias, 4) || !aligned(labels, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 4)) return ZENO_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < linear_logprobs_workspace_bytes(rows, vocab, width, dtype))
+    return ZENO_ERR_WORKSPACE;
+  if (rows == 0) return ZENO_OK;
+  const LinearLogprobsArgs a = {hidden, weight, ldh, ldw, dtype, rows, vocab, width, bias, labels, logp, entropy, stats};
+  ProfScope ps(ZENO_KERNEL_LINEAR_LOGPROBS, 0, ((double)rows + vocab) * width * dtype_bytes(dtype) + 4.0 * vocab + 20.0 * rows,
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_linear_logprobs(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
+size_t zeno_linear_logprobs_backward_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t dtype, int32_t m) {
+  if (m < 1 || m > ZENO_MAX_CANDIDATES || !linear_query_ok(rows, vocab, width, dtype)) return 0;
+  return linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, m);
+}
+
+zeno_status_t zeno_linear_logprobs_backward(const void* hidden, int64_t ldh, const void* weight, int64_t ldw, int32_t dtype,
+                                            const float* bias, int32_t rows, int32_t vocab, int32_t width, const float* stats,
+                                            const int32_t* labels, const float* grad_logp, const float* entropy,
+                                            const float* grad_entropy, int32_t m, const int32_t* offsets, void* dhidden, int64_t lddh,
+                                            float* dweight, int64_t ldg, float* dbias, int64_t ldb, void* workspace,
+                                            size_t workspace_bytes, void* stream) {
+  if (!matrix_ok(hidden, ldh, dtype, rows, width) || vocab < 1 || !matrix_ok(weight, ldw, dtype, vocab, width) || !groups_ok(m, offsets))
+    return ZENO_ERR_INVALID_ARG;
+  if (rows > 0 && (stats == nullptr || (grad_logp == nullptr && grad_entropy == nullptr))) return ZENO_ERR_INVALID_ARG;
+  if (rows > 0 && ((grad_logp != nullptr && labels == nullptr) || (grad_entropy != nullptr && entropy == nullptr))) return ZENO_ERR_INVALID_ARG;
+  if (rows > 0 && dhidden == nullptr && dweight == nullptr && dbias == nullptr) return ZENO_ERR_INVALID_ARG;
+  if (dhidden != nullptr && !matrix_ok(dhidden, lddh, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;
+  if (dhidden != nullptr && dhidden == hidden && lddh != ldh && rows > 1) return ZENO_ERR_INVALID_ARG;
+  if ((dweight != nullptr && ldg < (int64_t)vocab * width) || (dbias != nullptr && ldb < vocab)) return ZENO_ERR_INVALID_ARG;
+  if (!aligned(bias, 4) || !aligned(stats, 4) || !aligned(labels, 4) || !aligned(grad_logp, 4) || !aligned(entropy, 4) ||
+      !aligned(grad_entropy, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
+    return ZENO_ERR_INVALID_ARG;
+  if (!linear_sizes_ok(rows, vocab, width)) return ZENO_ERR_UNSUPPORTED;
+  if (workspace == nullptr || !aligned(workspace, 256) ||
+      workspace_bytes < linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, m))
+    return ZENO_ERR_WORKSPACE;
+  if (rows == 0 && dweight == nullptr && dbias == nullptr) return ZENO_OK;
+  const LinearLogprobsGradArgs a = {hidden, weight,    ldh,     ldw,          dtype, rows,    vocab,   width, bias,    stats, labels,
+                                    grad_logp, entropy, grad_entropy, m,     offsets, dhidden, lddh,  dweight, ldg,   dbias, ldb};
+  ProfScope ps(ZENO_KERNEL_LINEAR_LOGPROBS_GRAD, 0,
+               (((dhidden != nullptr ? 2.0 : 1.0) * rows + vocab) * width) * dtype_bytes(dtype) + 4.0 * vocab + 24.0 * rows +
+                   4.0 * m * vocab * ((dweight != nullptr ? width : 0.0) + (dbias != nullptr ? 1.0 : 0.0)),
+               reinterpret_cast<hipStream_t>(stream));
+  ZENO_TRY(launch_linear_logprobs_backward(a, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return ZENO_OK;
+}
+
 zeno_status_t zeno_embedding(const void* table, int64_t ldt, int32_t table_dtype, int32_t vocab, int32_t width, const int32_t* ids,
                              int32_t rows, float scale, void* out, int64_t ldo, int32_t dtype, void* stream) {
   if (!matrix_ok(table, ldt, table_dtype, vocab, width) || vocab < 1 || !matrix_ok(out, ldo, dtype, rows, width)) return ZENO_ERR_INVALID_ARG;

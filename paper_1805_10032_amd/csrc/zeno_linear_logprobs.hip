@@ -1,0 +1,973 @@
+// Log probabilities of a linear layer's outputs, z = h W^T + bias, without keeping the logits, and their gradients:
+//   log p_y = z_y - M - log s,  M = max z,  s = sum exp(z - M),  H = log s - (sum exp(z - M) (z - M)) / s,
+//   dz_j = g [j = y] - p_j (g + q (log p_j + H)),  dh = dz W,  dW_g = dz_g^T h_g,  db_g = sum dz.
+//
+// Forward: tiles of h W^T on the matrix cores; a tile leaves (max, sum of exponentials) for each of its tokens, which are joined behind.  The
+// logits stay float32 and never leave the registers.
+// Backward: the vocabulary in pieces.  A piece's logits are formed again, their dz goes to the workspace as 16-bit planes (a sum of
+// two or three of them where float32 gradients are taken from it), and two products read it: with W for dh, with h for dW.
+// Operands are planes of 16 bits: bf16 and fp16 as they are; float32 is a sum of three bf16 pieces, of whose nine products six are taken, those
+// that are left out lie below 2^-24 of the product.
+#include "zeno_tokens.h"
+#include <algorithm>
+
+namespace zeno {
+namespace {
+
+typedef unsigned short u16;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
+
+constexpr int kStep = 32;      // of the contraction in a stage
+constexpr int kStages = 4;     // in LDS: one that is multiplied, three on their way
+
+// BM x BN of the product for a workgroup of WM x WN waves.
+template <int BM_, int BN_, int WM_, int WN_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
+  static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;   // 32 x 32 blocks of a wave
+  static constexpr int A_BYTES = BM * kStep * 2, STAGE = (BM + BN) * kStep * 2;
+  static constexpr int LOADS_A = A_BYTES / 1024 / WAVES, LOADS_B = BN * kStep * 2 / 1024 / WAVES, LOADS = LOADS_A + LOADS_B;
+  static constexpr int PITCH = BM + 8;                         // of a plane of dz on its way out, [token][vocabulary]
+  static constexpr int LDS = kStages * STAGE > BN * PITCH * 2 ? kStages * STAGE : BN * PITCH * 2;
+};
+using WideTile = Tile<256, 256, 2, 4>;
+using MidTile = Tile<128, 128, 2, 2>;
+
+// An operand: planes of 16-bit values, `plane` elements apart, rows ld apart and on 16 bytes.
+struct Side {
+  const u16* p;
+  long long ld, plane;
+  int extent;   // rows along the contraction: how many there are; across it: columns, a multiple of eight
+};
+// Which planes are multiplied, the smallest products first.
+struct Pairs {
+  int count;
+  unsigned char a[6], b[6];
+};
+
+__device__ __attribute__((aligned(16))) unsigned zero_chunk[4];
+
+// 64 lanes x 16 bytes to consecutive bytes of LDS from `to` on, in no register and unseen by the compiler's wait counts (which would drain all
+// loads before every read of LDS); begin_stage() waits for it.  m0 is saved because it cannot be declared as written.
+__device__ inline void copy_to_lds(const u16* from, unsigned to) {
+  unsigned saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(saved)
+               : "v"(from), "s"(to)
+               : "memory");
+}
+// All but the `pending` copies issued last have arrived, for every wave, and every wave has read what the stage before held.
+template <int PENDING>
+__device__ inline void begin_stage() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(PENDING) : "memory");
+}
+
+// A side's part of a stage.  ACROSS false: rows of the side along the contraction, 64 bytes a row; chunk c of row r stands at c ^ (r / 4 % 4),
+// so that sixteen rows' chunks lie on all banks.  ACROSS true: the contraction's rows, B columns each; blocks of 32 columns are
+// exchanged by a row's number for the same reason.
+template <int B>
+__device__ inline int block_of(int k) { return B >= 256 ? (k & 3) | ((k >> 1) & 4) : (k & 3); }
+
+template <bool ACROSS, int B, int WAVES>
+struct Loader {
+  static constexpr int N = B * kStep * 2 / 1024 / WAVES, PER = 512 / B;   // copies a wave; rows of a copy, if ACROSS
+  static_assert(N >= 1, "every wave copies");
+  static_assert(!ACROSS || PER * WAVES % 16 == 0, "a lane's copies exchange the same blocks");
+  const u16* at[N];
+  int k;        // of the lane's first value, in its first copy
+  bool inside;  // its columns exist
+  unsigned to;
+  __device__ inline void start(const Side& s, int plane, long long first, long long x0, int wave, int lane, unsigned lds) {
+    to = lds + 1024 * wave;
+    inside = true;
+    const u16* p = s.p + plane * s.plane;
+    if (!ACROSS) {
+      k = 8 * ((lane % 4) ^ (lane / 16));
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const long long row = x0 + 16 * (wave + WAVES * n) + lane / 4;
+        at[n] = p + (row < s.extent ? row : s.extent - 1) * s.ld + first + k;
+      }
+    } else {
+      const int slot = lane % (64 / PER);
+      k = PER * wave + lane / (64 / PER);
+      const long long col = x0 + 32 * ((slot / 4) ^ block_of<B>(k)) + 8 * (slot % 4);
+      inside = col < s.extent;
+#pragma unroll
+      for (int n = 0; n < N; ++n) at[n] = p + (first + k + PER * WAVES * n) * s.ld + (inside ? col : 0);
+    }
+  }
+  // `left`: what of the contraction is left from this stage on
+  __device__ inline void issue(const Side& s, int stage_offset, int left) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const bool live = inside && k + (ACROSS ? PER * WAVES * n : 0) < left;
+      copy_to_lds(live ? at[n] : reinterpret_cast<const u16*>(zero_chunk), to + stage_offset + 1024 * WAVES * n);
+      at[n] += ACROSS ? kStep * s.ld : kStep;
+    }
+  }
+  __device__ inline void move(long long by) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) at[n] += by;
+  }
+};
+
+// Operand of 32 rows (columns) from r on and sixteen of the contraction from k on: lane l has row l % 32, values 8 (l / 32) + 0..7.
+template <bool ACROSS, int B>
+__device__ inline s16x8 read_operand(const unsigned char* part, int r, int k, int lane) {
+  if (!ACROSS) {
+    const int chunk = (k / 8 + lane / 32) ^ (lane % 32 / 4 % 4);
+    return *reinterpret_cast<const s16x8*>(part + (r + lane % 32) * (2 * kStep) + 16 * chunk);
+  } else {
+    const int row = k + 8 * (lane / 32) + lane % 16 / 4;
+    const int at = row * (2 * B) + 64 * ((r / 32) ^ block_of<B>(row)) + 32 * (lane / 16 % 2) + 8 * (lane % 4);
+    typedef __attribute__((address_space(3))) s16x4* p;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(part + at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(part + at + 4 * (2 * B)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+template <bool HALF>
+__device__ inline f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (HALF)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// acc += the product of BM rows (columns) of A from m0 on and BN of B from n0 on over `length` of the contraction, which begins at `first`.
+template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS>
+__device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
+                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN]) {
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN);
+  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)memory;
+  const int steps = (length + kStep - 1) / kStep, total = steps * pairs.count;
+  if (total == 0) return;
+  Loader<A_ACROSS, S::BM, S::WAVES> la;
+  Loader<B_ACROSS, S::BN, S::WAVES> lb;
+  la.start(a, pairs.a[0], first, m0, wave, lane, lds);
+  lb.start(b, pairs.b[0], first, n0, wave, lane, lds + S::A_BYTES);
+  int pair = 0, left = length;   // of the next stage to fetch
+  auto fetch = [&](int stage) __attribute__((always_inline)) {
+    la.issue(a, stage * S::STAGE, left);
+    lb.issue(b, stage * S::STAGE, left);
+    left -= kStep;
+    if (left <= 0 && pair + 1 < pairs.count) {
+      const long long back = (long long)steps * kStep;
+      la.move((pairs.a[pair + 1] - pairs.a[pair]) * a.plane - back * (A_ACROSS ? a.ld : 1));
+      lb.move((pairs.b[pair + 1] - pairs.b[pair]) * b.plane - back * (B_ACROSS ? b.ld : 1));
+      left = length;
+      ++pair;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i)
+    if (i < total) fetch(i);
+  for (int i = 0; i < total; ++i) {
+    if (i + 2 < total) begin_stage<2 * S::LOADS>();
+    else if (i + 1 < total) begin_stage<S::LOADS>();
+    else begin_stage<0>();
+    if (i + kStages - 1 < total) fetch((i + kStages - 1) % kStages);
+    const unsigned char* part = memory + (i % kStages) * S::STAGE;
+#pragma unroll
+    for (int k = 0; k < kStep; k += 16) {
+      s16x8 x[S::FM], y[S::FN];
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r) x[r] = read_operand<A_ACROSS, S::BM>(part, wm + 32 * r, k, lane);
+#pragma unroll
+      for (int j = 0; j < S::FN; ++j) y[j] = read_operand<B_ACROSS, S::BN>(part + S::A_BYTES, wn + 32 * j, k, lane);
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) acc[r][j] = multiply<HALF>(x[r], y[j], acc[r][j]);
+    }
+  }
+  begin_stage<0>();   // (the stages are free for what follows)
+}
+
+// Where a workgroup's tile lies: each of the eight dies, to which workgroups go in turn, takes a run of tiles, in patches of eight rows of tiles.
+struct Place {
+  int m, n;
+};
+__device__ inline Place place_of(unsigned id, unsigned tiles_m, unsigned tiles_n) {
+  const unsigned total = tiles_m * tiles_n, die = id % 8, q = total / 8, r = total % 8;
+  const unsigned at = die * q + (die < r ? die : r) + id / 8;
+  constexpr unsigned ROWS = 8;
+  const unsigned patch = ROWS * tiles_n, first = at / patch * ROWS, rows = tiles_m - first < ROWS ? tiles_m - first : ROWS;
+  Place p;
+  p.m = (int)(first + at % patch % rows);
+  p.n = (int)(at % patch / rows);
+  return p;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// What the logits' kernels share: A = rows of W from the vocabulary's `v0` on, B = h.
+struct LogitArgs {
+  Side w, h;
+  Pairs pairs;
+  int tiles_m, tiles_n, width;
+  int v0, vocab, rows;     // first value of this launch's vocabulary; the whole one; tokens
+  const float* bias;
+  const int32_t* labels;
+};
+// Row of a wave's 32 x 32 block that element e of a lane holds.
+__device__ inline int row_of(int e, int lane) { return 8 * (e / 4) + 4 * (lane / 32) + e % 4; }
+
+// Adds the bias; what lies behind the vocabulary becomes -inf.
+template <typename S>
+__device__ inline void add_bias(const LogitArgs& a, int v, int lane, f32x16 (&acc)[S::FM][S::FN]) {
+#pragma unroll
+  for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = v + 32 * r + row_of(4 * q, lane);
+      float b[4] = {0.f, 0.f, 0.f, 0.f};
+      if (at + 4 <= a.vocab) {
+        if (a.bias != nullptr) {
+          const f32x4 raw = *reinterpret_cast<const f32x4_a4*>(a.bias + at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) b[i] = raw[i];
+        }
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[r][j][4 * q + i] += b[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = at + i < a.vocab && a.bias != nullptr ? a.bias[at + i] : 0.f;
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[r][j][4 * q + i] = at + i < a.vocab ? acc[r][j][4 * q + i] + b[i] : -__builtin_inff();
+      }
+    }
+}
+
+// ---- forward: for each token and each slice of 32 FM values (max, sum of exp(z - max)) and, for the entropy, the sum of exp(z - max) (z - max)
+struct StatArgs {
+  LogitArgs l;
+  int slice0;            // of this launch's vocabulary
+  float2* part;          // [slices][rows]
+  float* part_u;         // [slices][rows] or nullptr
+  float* label_logit;    // [rows]
+};
+template <typename S, bool HALF>
+__global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(StatArgs a) {
+  extern __shared__ __align__(1024) unsigned char memory[];
+  const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
+  f32x16 acc[S::FM][S::FN] = {};
+  product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int v = a.l.v0 + t.m * S::BM + (wave % S::WM) * (32 * S::FM);
+  add_bias<S>(a.l, v, lane, acc);
+  const int slice = a.slice0 + t.m * S::WM + wave % S::WM;
+#pragma unroll
+  for (int j = 0; j < S::FN; ++j) {
+    const int token = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + 32 * j + lane % 32;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[r][j][e]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float from = top == -__builtin_inff() ? 0.f : top;
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float d = acc[r][j][e] - from, x = exp_fast(d);
+        s += x;
+        u += x > 0.f ? x * d : 0.f;
+      }
+    s += __shfl_xor(s, 32);
+    u += __shfl_xor(u, 32);
+    if (token < a.l.rows) {
+      const long long at = (long long)slice * a.l.rows + token;
+      if (lane < 32) {
+        a.part[at] = make_float2(top, s);
+        if (a.part_u != nullptr) a.part_u[at] = u;
+      }
+      const int hit = a.l.labels != nullptr ? a.l.labels[token] - v : -1;
+      if (hit >= 0 && hit < 32 * S::FM && hit + v < a.l.vocab) {
+#pragma unroll
+        for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (hit == 32 * r + row_of(e, lane)) a.label_logit[token] = acc[r][j][e];
+      }
+    }
+  }
+}
+
+// Slices joined: 64 tokens a workgroup, every wave some of the slices.
+constexpr int kJoinWaves = 16;
+struct JoinArgs {
+  const float2* part;
+  const float* part_u;
+  const float* label_logit;
+  const int32_t* labels;
+  int slices, rows, vocab;
+  float *logp, *entropy, *stats;
+};
+struct Sums {
+  float top, s, u;
+  __device__ inline void add(float t, float x, float y) {   // (exp(-inf) of nothing yet: a top of -inf adds nothing)
+    if (t == -__builtin_inff()) {
+      s += x;                                               // (0, or a NaN that has no place else)
+      return;
+    }
+    if (t > top) {
+      const float d = top - t, f = top == -__builtin_inff() ? 0.f : exp_fast(d);
+      u = f > 0.f ? f * (u + s * d) : 0.f;
+      s = s * f;                                            // (a NaN stays one)
+      top = t;
+      s += x;
+      u += y;
+    } else {
+      const float d = t - top, f = exp_fast(d);
+      s += f * x;
+      u += f > 0.f ? f * (y + x * d) : 0.f;
+    }
+  }
+};
+__global__ __launch_bounds__(64 * kJoinWaves) void logit_join_kernel(JoinArgs a) {
+  __shared__ float shared[3][kJoinWaves][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const long long token = (long long)blockIdx.x * 64 + lane;
+  const bool live = token < a.rows;
+  Sums m = {-__builtin_inff(), 0.f, 0.f};
+  if (live) {
+#pragma unroll 4
+    for (int i = wave; i < a.slices; i += kJoinWaves) {
+      const float2 p = a.part[(long long)i * a.rows + token];
+      m.add(p.x, p.y, a.part_u != nullptr ? a.part_u[(long long)i * a.rows + token] : 0.f);
+    }
+  }
+  shared[0][wave][lane] = m.top;
+  shared[1][wave][lane] = m.s;
+  shared[2][wave][lane] = m.u;
+  __syncthreads();
+  if (wave != 0 || !live) return;
+  for (int w = 1; w < kJoinWaves; ++w) m.add(shared[0][w][lane], shared[1][w][lane], shared[2][w][lane]);
+  const bool empty = m.top == -__builtin_inff() && m.s == 0.f;
+  const float log_s = empty ? 0.f : logf(m.s);
+  if (a.stats != nullptr) {
+    a.stats[2 * token] = m.top;
+    a.stats[2 * token + 1] = log_s;
+  }
+  if (a.entropy != nullptr) a.entropy[token] = empty ? 0.f : log_s - m.u / m.s;
+  if (a.logp != nullptr) {
+    const int y = a.labels[token];
+    float lp = 0.f;
+    if (y != -1) {
+      if (y < 0 || y >= a.vocab) lp = __builtin_nanf("");
+      else if (empty) lp = -__builtin_inff();
+      else lp = (a.label_logit[token] - m.top) - log_s;
+    }
+    a.logp[token] = lp;
+  }
+}
+
+// ---- operands
+
+// bf16 pieces of a float32, x = h + m + l up to 2^-25 of it.  No finite value becomes infinite; what is not finite has no remainder.
+__device__ inline void pieces_of(float x, u16 (&p)[3]) {
+  const bool finite = fabsf(x) < __builtin_inff();
+  float h = (float)(__bf16)x;
+  if (finite && !(fabsf(h) < __builtin_inff())) h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  const float r = finite ? x - h : 0.f, m = (float)(__bf16)r;
+  p[0] = (u16)(__float_as_uint(h) >> 16);
+  p[1] = (u16)(__float_as_uint(m) >> 16);
+  p[2] = __builtin_bit_cast(u16, (__bf16)(r - m));
+}
+// Rows on 16 bytes, a multiple of eight columns, zeros behind the last: a copy of 16-bit values or a float32's pieces, eight a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T* x, long long ldx, int rows, int width, int padded, u16* out, long long plane) {
+  const long long chunks = padded / 8, all = chunks * rows;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    const long long row = i / chunks;
+    const int col = (int)(i % chunks) * 8;
+    const T* from = x + row * ldx + col;
+    u16* to = out + row * padded + col;
+    if constexpr (sizeof(T) == 2) {
+      u16 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = col + j < width ? from[j] : (u16)0;
+      s16x8 raw;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) raw[j] = (short)v[j];
+      *reinterpret_cast<s16x8*>(to) = raw;
+    } else {
+      s16x8 raw[3];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        u16 p[3];
+        pieces_of(col + j < width ? (float)from[j] : 0.f, p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) raw[q][j] = (short)p[q];
+      }
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<s16x8*>(to + q * plane) = raw[q];
+    }
+  }
+}
+
+int padded_width(int width) { return (width + 7) / 8 * 8; }
+int planes_of(int dtype) { return dtype == ZENO_F32 ? 3 : 1; }
+// Whether a matrix can be read as it stands: 16-byte pieces of 16-bit values.
+bool as_it_is(const void* p, long long ld, int dtype, int width) {
+  return dtype != ZENO_F32 && width % 8 == 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+hipError_t pack(const void* x, long long ldx, int dtype, int rows, int width, u16* out, hipStream_t stream) {
+  const int padded = padded_width(width);
+  const long long plane = (long long)rows * padded, threads = plane / 8;
+  const unsigned blocks = (unsigned)std::min<long long>((threads + 255) / 256, 16384);
+  if (dtype == ZENO_F32)
+    pack_kernel<float><<<blocks, 256, 0, stream>>>(reinterpret_cast<const float*>(x), ldx, rows, width, padded, out, plane);
+  else
+    pack_kernel<u16><<<blocks, 256, 0, stream>>>(reinterpret_cast<const u16*>(x), ldx, rows, width, padded, out, plane);
+  return hipGetLastError();
+}
+Pairs pairs_of(int a, int b) {   // planes of the two sides
+  if (a == 3) return {6, {2, 0, 1, 1, 0, 0}, {0, 2, 1, 0, 1, 0}};
+  if (a == 2) return {2, {1, 0}, {0, 0}};
+  (void)b;
+  return {1, {0}, {0}};
+}
+
+// ---- backward
+
+struct GradScale {
+  float up, down;   // what dz is multiplied by on its way into 16 bits, and the products by on their way out
+};
+// fp16 keeps dz within 2^14: a power of two of the largest gradient that a token brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e, p H <= ln V < 21).
+// The others have float32's range.
+__global__ __launch_bounds__(1024) void grad_scale_kernel(const float* g, const float* q, const int32_t* labels, int rows, int half, GradScale* out) {
+  __shared__ float shared[16];
+  float largest = 0.f;
+  if (half)
+    for (int t = threadIdx.x; t < rows; t += 1024) {
+      float b = g != nullptr && labels[t] != -1 ? fabsf(g[t]) : 0.f;
+      if (q != nullptr) b += 22.f * fabsf(q[t]);
+      if (b < __builtin_inff()) largest = fmaxf(largest, b);
+    }
+  largest = wave_max_f(largest);
+  if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = largest;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 16; ++w) largest = fmaxf(largest, shared[w]);
+  int up = 0;
+  if (largest > 0.f) {
+    const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126;   // largest < 2^e
+    up = 14 - e;
+    up = up > 100 ? 100 : (up < -100 ? -100 : up);
+  }
+  out->up = __uint_as_float((unsigned)(127 + up) << 23);
+  out->down = __uint_as_float((unsigned)(127 - up) << 23);
+}
+
+struct DzArgs {
+  LogitArgs l;
+  const float *stats, *grad_logp, *entropy, *grad_entropy;
+  const GradScale* scale;
+  u16* dz;               // [planes][rows][ldz]
+  long long ldz, plane;
+};
+template <typename S, bool HALF, int P>
+__global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
+  extern __shared__ __align__(1024) unsigned char memory[];
+  const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
+  f32x16 acc[S::FM][S::FN] = {};
+  product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN), v = a.l.v0 + t.m * S::BM + wm;
+  add_bias<S>(a.l, v, lane, acc);
+  const float up = HALF ? a.scale->up : 1.f;
+#pragma unroll
+  for (int j = 0; j < S::FN; ++j) {
+    const int token = t.n * S::BN + wn + 32 * j + lane % 32;
+    const bool live = token < a.l.rows;
+    float M = 0.f, log_s = __builtin_inff(), g = 0.f, q = 0.f, H = 0.f;
+    int y = -1;
+    bool empty = true;
+    if (live) {
+      M = a.stats[2 * token];
+      log_s = a.stats[2 * token + 1];
+      empty = M == -__builtin_inff() && log_s == 0.f;
+      if (a.grad_logp != nullptr) {
+        y = a.l.labels[token];
+        if (y != -1) g = y >= 0 && y < a.l.vocab ? a.grad_logp[token] : __builtin_nanf("");
+      }
+      if (a.grad_entropy != nullptr) {
+        q = a.grad_entropy[token];
+        H = a.entropy[token];
+      }
+    }
+    if (empty) {
+      M = 0.f;
+      log_s = __builtin_inff();
+    }
+    const float base = a.grad_entropy != nullptr ? fmaf(q, H, g) : g;
+    const int hit = empty ? -1 : y - v;
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float lp = (acc[r][j][e] - M) - log_s, p = exp_fast(lp);
+        // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
+        float d = -p * (a.grad_entropy != nullptr ? fmaf(q, fmaxf(lp, -256.f), base) : base);
+        if (hit == 32 * r + row_of(e, lane)) d += g;
+        if (v + 32 * r + row_of(e, lane) >= a.l.vocab) d = 0.f;
+        acc[r][j][e] = d * up;
+      }
+  }
+  // a plane at a time through LDS, so that rows leave in whole lines
+  u16* tile = reinterpret_cast<u16*>(memory);
+#pragma unroll
+  for (int plane = 0; plane < P; ++plane) {
+    if (plane > 0) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s16x4 out;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float d = acc[r][j][4 * c + i];
+            if constexpr (HALF) {
+              const _Float16 x = (_Float16)d;
+              out[i] = __builtin_bit_cast(short, x);
+              acc[r][j][4 * c + i] = d - (float)x;
+            } else {
+              const __bf16 x = (__bf16)d;
+              out[i] = __builtin_bit_cast(short, x);
+              acc[r][j][4 * c + i] = d - (float)x;
+            }
+          }
+          *reinterpret_cast<s16x4*>(tile + (wn + 32 * j + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane)) = out;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BN * (S::BM / 8); i += S::THREADS) {
+      const int row = i / (S::BM / 8), col = i % (S::BM / 8) * 8;
+      const long long token = (long long)t.n * S::BN + row;
+      if (token < a.l.rows)
+        *reinterpret_cast<s16x8*>(a.dz + plane * a.plane + token * a.ldz + t.m * S::BM + col) =
+            *reinterpret_cast<const s16x8*>(tile + row * S::PITCH + col);
+    }
+  }
+}
+
+// dh: a piece of the vocabulary, cut into `splits` of `per` values that different workgroups sum, each into its own slot.
+struct HiddenArgs {
+  Side dz, w;
+  Pairs pairs;
+  int tiles_m, tiles_n, rows, width, length, per;
+  int first;             // the slots hold nothing yet
+  float* slots;          // [splits][rows][width]
+};
+template <typename S, bool HALF>
+__global__ __launch_bounds__(S::THREADS) void hidden_grad_kernel(HiddenArgs a) {
+  extern __shared__ __align__(1024) unsigned char memory[];
+  const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
+  const int begin = blockIdx.y * a.per, length = a.length - begin < a.per ? a.length - begin : a.per;
+  f32x16 acc[S::FM][S::FN] = {};
+  product<S, HALF, false, true>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0, memory, acc);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
+  float* slot = a.slots + (long long)blockIdx.y * a.rows * a.width;
+#pragma unroll
+  for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
+        if (row < a.rows && col < a.width) {
+          float& to = slot[(long long)row * a.width + col];
+          to = a.first ? acc[r][j][e] : to + acc[r][j][e];
+        }
+      }
+}
+// Slots in their order, for the rows that belong to somebody.
+template <typename T>
+__global__ __launch_bounds__(256) void hidden_join_kernel(const float* slots, int splits, int rows, int width, int m, const int32_t* offsets,
+                                                         const GradScale* scale, T* out, long long ldo) {
+  const int lo = group_offset(offsets, 0, rows), hi = group_offset(offsets, offsets == nullptr ? 1 : m, rows);
+  const long long stride = (long long)rows * width;
+  const float down = scale->down;
+  const long long all = stride;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    const long long row = i / width;
+    if (row < lo || row >= hi) continue;
+    float sum = slots[i];
+    for (int s = 1; s < splits; ++s) sum += slots[s * stride + i];
+    out[row * ldo + (i - row * width)] = (T)(sum * down);
+  }
+}
+
+// dW of a piece of the vocabulary, a group's tokens from its offset on.
+struct WeightArgs {
+  Side dz, h;
+  Pairs pairs;
+  int tiles_m, tiles_n, rows, width, values;   // values: of the vocabulary in this piece
+  const int32_t* offsets;
+  const GradScale* scale;
+  float* dweight;        // at the piece's first value
+  long long ldw;
+};
+template <typename S, bool HALF>
+__global__ __launch_bounds__(S::THREADS) void head_weight_grad_kernel(WeightArgs a) {
+  extern __shared__ __align__(1024) unsigned char memory[];
+  const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
+  const int g = blockIdx.y, begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
+  f32x16 acc[S::FM][S::FN] = {};
+  product<S, HALF, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, end > begin ? end - begin : 0, memory, acc);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
+  const float down = HALF ? a.scale->down : 1.f;
+  float* dw = a.dweight + g * a.ldw;
+#pragma unroll
+  for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
+        if (row < a.values && col < a.width) dw[(long long)row * a.width + col] = acc[r][j][e] * down;
+      }
+}
+
+// db of a piece: 512 values a workgroup, every wave some of the group's tokens.
+constexpr int kBiasWaves = 8;
+template <bool HALF, int P>
+__global__ __launch_bounds__(64 * kBiasWaves) void head_bias_grad_kernel(const u16* dz, long long ldz, long long plane, int rows, int values,
+                                                                        const int32_t* offsets, const GradScale* scale, float* dbias, long long ldb) {
+  __shared__ float shared[kBiasWaves][512];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = blockIdx.y;
+  const int begin = group_offset(offsets, g, rows), end = group_offset(offsets, g + 1, rows);
+  const int col = blockIdx.x * 512 + 8 * lane;
+  float sum[8] = {};
+  if (col < ldz) {
+    for (long long t = begin + wave; t < end; t += kBiasWaves) {
+#pragma unroll
+      for (int p = P - 1; p >= 0; --p) {
+        const s16x8 raw = *reinterpret_cast<const s16x8*>(dz + p * plane + t * ldz + col);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const short bits = raw[j];
+          sum[j] += HALF ? (float)__builtin_bit_cast(_Float16, bits) : __uint_as_float((unsigned)(u16)bits << 16);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) shared[wave][8 * lane + j] = sum[j];
+  __syncthreads();
+  const float down = HALF ? scale->down : 1.f;
+  const int at = blockIdx.x * 512 + threadIdx.x;
+  if (at < values) {
+    float s = shared[0][threadIdx.x];
+    for (int w = 1; w < kBiasWaves; ++w) s += shared[w][threadIdx.x];
+    dbias[g * ldb + at] = s * down;
+  }
+}
+
+// ---- plans
+
+template <typename S>
+hipError_t allow(const void* kernel) {
+  return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+}
+
+constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
+constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
+
+// Wide tiles where they give every compute unit one.
+bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
+
+struct Layout {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t here = at;
+    at += align_up(bytes, 256);
+    return here;
+  }
+};
+
+struct ForwardPlan {
+  bool wide;
+  int slice;          // values of the vocabulary in a slice
+  int piece;          // values that are packed at a time
+  int block;          // tokens at a time
+  size_t hidden, weight, part, part_u, label, bytes;
+};
+ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
+  ForwardPlan p;
+  p.block = std::min(rows, kRowBlock);
+  p.wide = wide_tiles(vocab, p.block);
+  p.slice = p.wide ? 32 * WideTile::FM : 32 * MidTile::FM;
+  const long long padded = padded_width(width);
+  p.piece = (int)std::min<long long>((vocab + 255) / 256 * 256LL, std::max<long long>(256, kPackElements / padded / 256 * 256));
+  Layout l;
+  p.hidden = l.take((size_t)planes_of(dtype) * p.block * padded * 2);
+  p.weight = l.take((size_t)planes_of(dtype) * std::min(p.piece, vocab) * padded * 2);
+  const size_t slices = (size_t)ceil_div(vocab, p.slice) + 4;
+  p.part = l.take(slices * p.block * 8);
+  p.part_u = l.take(slices * p.block * 4);
+  p.label = l.take((size_t)p.block * 4);
+  p.bytes = l.at + 256;
+  return p;
+}
+
+struct BackwardPlan {
+  bool wide_logits, wide_hidden, wide_weight;
+  int piece;          // values of the vocabulary at a time
+  int planes;         // of dz
+  int splits;
+  size_t hidden, weight, dz, slots, scale, bytes;
+};
+BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
+  BackwardPlan p;
+  const long long padded = padded_width(width), n = std::max(rows, 1);
+  p.planes = dtype == ZENO_F32 ? 3 : 2;
+  // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles
+  const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
+  const long long pieces = (vocab + most - 1) / most;
+  p.piece = (int)(((vocab + pieces - 1) / pieces + 255) / 256 * 256);
+  p.wide_logits = wide_tiles(p.piece, n);
+  p.wide_hidden = wide_tiles(n, width);
+  p.wide_weight = wide_tiles((long long)p.piece * m, width) && n / m >= 64;
+  const int side = p.wide_hidden ? 256 : 128;
+  const long long tiles = (long long)ceil_div(n, side) * ceil_div(width, side);
+  p.splits = (int)std::max<long long>(1, std::min<long long>(p.piece / 512, (p.wide_hidden ? 256 : 512) / tiles));
+  Layout l;
+  p.hidden = l.take((size_t)planes_of(dtype) * n * padded * 2);
+  p.weight = l.take((size_t)planes_of(dtype) * p.piece * padded * 2);
+  p.dz = l.take((size_t)p.planes * n * p.piece * 2);
+  p.slots = l.take((size_t)p.splits * n * width * 4);
+  p.scale = l.take(256);
+  p.bytes = l.at + 256;
+  return p;
+}
+
+template <typename S, bool HALF>
+hipError_t start_stats(const StatArgs& a, hipStream_t stream) {
+  const auto kernel = logit_stats_kernel<S, HALF>;
+  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <typename S, bool HALF, int P>
+hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
+  const auto kernel = logit_grad_kernel<S, HALF, P>;
+  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <typename S>
+hipError_t start_dz(const DzArgs& a, int dtype, hipStream_t stream) {
+  if (dtype == ZENO_F32) return start_dz<S, false, 3>(a, stream);
+  return dtype == ZENO_F16 ? start_dz<S, true, 2>(a, stream) : start_dz<S, false, 2>(a, stream);
+}
+template <typename S, bool HALF>
+hipError_t start_hidden(const HiddenArgs& a, int splits, hipStream_t stream) {
+  const auto kernel = hidden_grad_kernel<S, HALF>;
+  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+template <typename S, bool HALF>
+hipError_t start_weight(const WeightArgs& a, int m, hipStream_t stream) {
+  const auto kernel = head_weight_grad_kernel<S, HALF>;
+  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, m), S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+
+#define ZENO_STEP(expr)                          \
+  do {                                           \
+    const hipError_t zeno_step_error = (expr);   \
+    if (zeno_step_error != hipSuccess) return zeno_step_error; \
+  } while (0)
+
+// The side of a matrix of `rows` rows: as it stands, or packed into `space`.
+hipError_t side_of(const void* x, long long ld, int dtype, int rows, int width, u16* space, Side& s, hipStream_t stream) {
+  s.extent = rows;
+  if (as_it_is(x, ld, dtype, width)) {
+    s.p = reinterpret_cast<const u16*>(x);
+    s.ld = ld;
+    s.plane = 0;
+    return hipSuccess;
+  }
+  s.p = space;
+  s.ld = padded_width(width);
+  s.plane = (long long)rows * s.ld;
+  return pack(x, ld, dtype, rows, width, space, stream);
+}
+
+}  // namespace
+
+size_t linear_logprobs_workspace_bytes(int rows, int vocab, int width, int dtype) { return forward_plan(std::max(rows, 1), vocab, width, dtype).bytes; }
+
+hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, hipStream_t stream) {
+  const ForwardPlan p = forward_plan(a.rows, a.vocab, a.width, a.dtype);
+  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+  const size_t bytes = a.dtype == ZENO_F32 ? 4 : 2;
+  const bool half = a.dtype == ZENO_F16, direct = as_it_is(a.weight, a.ldw, a.dtype, a.width);
+  const int piece = direct ? a.vocab : p.piece;
+  for (int t0 = 0; t0 < a.rows; t0 += p.block) {
+    const int rows = std::min(p.block, a.rows - t0);
+    StatArgs s = {};
+    LogitArgs& l = s.l;
+    ZENO_STEP(side_of(reinterpret_cast<const unsigned char*>(a.hidden) + (size_t)t0 * a.ldh * bytes, a.ldh, a.dtype, rows, a.width,
+                      reinterpret_cast<u16*>(ws + p.hidden), l.h, stream));
+    l.pairs = pairs_of(planes_of(a.dtype), planes_of(a.dtype));
+    l.width = padded_width(a.width);
+    l.vocab = a.vocab;
+    l.rows = rows;
+    l.bias = a.bias;
+    l.labels = a.labels == nullptr ? nullptr : a.labels + t0;
+    s.part = reinterpret_cast<float2*>(ws + p.part);
+    s.part_u = a.entropy != nullptr ? reinterpret_cast<float*>(ws + p.part_u) : nullptr;
+    s.label_logit = reinterpret_cast<float*>(ws + p.label);
+    int slices = 0;
+    for (int v0 = 0; v0 < a.vocab; v0 += piece) {
+      const int values = std::min(piece, a.vocab - v0);
+      ZENO_STEP(side_of(reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v0 * a.ldw * bytes, a.ldw, a.dtype, values, a.width,
+                        reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
+      l.v0 = v0;
+      s.slice0 = v0 / p.slice;
+      const int side = p.wide ? 256 : 128;
+      l.tiles_m = ceil_div(values, side);
+      l.tiles_n = ceil_div(rows, side);
+      if (p.wide) ZENO_STEP(half ? (start_stats<WideTile, true>(s, stream)) : (start_stats<WideTile, false>(s, stream)));
+      else ZENO_STEP(half ? (start_stats<MidTile, true>(s, stream)) : (start_stats<MidTile, false>(s, stream)));
+      slices = s.slice0 + l.tiles_m * 2;
+    }
+    const JoinArgs j = {s.part, s.part_u, s.label_logit, l.labels, slices, rows, a.vocab, a.logp == nullptr ? nullptr : a.logp + t0,
+                        a.entropy == nullptr ? nullptr : a.entropy + t0, a.stats == nullptr ? nullptr : a.stats + 2 * (size_t)t0};
+    logit_join_kernel<<<(unsigned)ceil_div(rows, 64), 64 * kJoinWaves, 0, stream>>>(j);
+    ZENO_STEP(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+size_t linear_logprobs_backward_workspace_bytes(int rows, int vocab, int width, int dtype, int m) {
+  return backward_plan(rows, vocab, width, dtype, m).bytes;
+}
+
+hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void* workspace, hipStream_t stream) {
+  const BackwardPlan p = backward_plan(a.rows, a.vocab, a.width, a.dtype, a.m);
+  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+  const size_t bytes = a.dtype == ZENO_F32 ? 4 : 2;
+  const bool half = a.dtype == ZENO_F16;
+  const int planes = planes_of(a.dtype);
+  GradScale* scale = reinterpret_cast<GradScale*>(ws + p.scale);
+  grad_scale_kernel<<<1, 1024, 0, stream>>>(a.grad_logp, a.grad_entropy, a.labels, a.rows, half ? 1 : 0, scale);
+  ZENO_STEP(hipGetLastError());
+  DzArgs d = {};
+  LogitArgs& l = d.l;
+  if (a.rows > 0)
+    ZENO_STEP(side_of(a.hidden, a.ldh, a.dtype, a.rows, a.width, reinterpret_cast<u16*>(ws + p.hidden), l.h, stream));
+  l.pairs = pairs_of(planes, planes);
+  l.width = padded_width(a.width);
+  l.vocab = a.vocab;
+  l.rows = a.rows;
+  l.bias = a.bias;
+  l.labels = a.labels;
+  d.stats = a.stats;
+  d.grad_logp = a.grad_logp;
+  d.entropy = a.entropy;
+  d.grad_entropy = a.grad_entropy;
+  d.scale = scale;
+  d.dz = reinterpret_cast<u16*>(ws + p.dz);
+  d.ldz = p.piece;
+  d.plane = (long long)a.rows * p.piece;
+  float* slots = reinterpret_cast<float*>(ws + p.slots);
+  for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
+    const int values = std::min(p.piece, a.vocab - v0);
+    if (a.rows > 0) {
+      ZENO_STEP(side_of(reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v0 * a.ldw * bytes, a.ldw, a.dtype, values, a.width,
+                        reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
+      l.v0 = v0;
+      const int side = p.wide_logits ? 256 : 128;
+      l.tiles_m = ceil_div(values, side);
+      l.tiles_n = ceil_div(a.rows, side);
+      ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<MidTile>(d, a.dtype, stream));
+      if (a.dhidden != nullptr) {
+        HiddenArgs h = {};
+        h.dz = {d.dz, d.ldz, d.plane, a.rows};
+        h.w = l.w;
+        h.w.extent = l.width;   // (across the contraction: columns)
+        h.pairs = planes == 3 ? pairs_of(3, 3) : pairs_of(1, 1);
+        const int tile = p.wide_hidden ? 256 : 128;
+        h.tiles_m = ceil_div(a.rows, tile);
+        h.tiles_n = ceil_div(a.width, tile);
+        h.rows = a.rows;
+        h.width = a.width;
+        h.length = values;
+        h.per = ceil_div(ceil_div(values, p.splits), kStep) * kStep;
+        h.first = v0 == 0;
+        h.slots = slots;
+        if (p.wide_hidden) ZENO_STEP(half ? (start_hidden<WideTile, true>(h, p.splits, stream)) : (start_hidden<WideTile, false>(h, p.splits, stream)));
+        else ZENO_STEP(half ? (start_hidden<MidTile, true>(h, p.splits, stream)) : (start_hidden<MidTile, false>(h, p.splits, stream)));
+      }
+    }
+    if (a.dweight != nullptr) {
+      WeightArgs w = {};
+      w.dz = {d.dz, d.ldz, d.plane, p.piece};
+      w.h = l.h;
+      w.h.extent = l.width;
+      w.pairs = pairs_of(p.planes, planes);
+      const int tile = p.wide_weight ? 256 : 128;
+      w.tiles_m = ceil_div(values, tile);
+      w.tiles_n = ceil_div(a.width, tile);
+      w.rows = a.rows;
+      w.width = a.width;
+      w.values = values;
+      w.offsets = a.offsets;
+      w.scale = scale;
+      w.dweight = a.dweight + (long long)v0 * a.width;
+      w.ldw = a.ldg;
+      if (p.wide_weight) ZENO_STEP(half ? (start_weight<WideTile, true>(w, a.m, stream)) : (start_weight<WideTile, false>(w, a.m, stream)));
+      else ZENO_STEP(half ? (start_weight<MidTile, true>(w, a.m, stream)) : (start_weight<MidTile, false>(w, a.m, stream)));
+    }
+    if (a.dbias != nullptr) {
+      const dim3 grid((unsigned)ceil_div(values, 512), a.m);
+      float* db = a.dbias + v0;
+      if (a.dtype == ZENO_F32)
+        head_bias_grad_kernel<false, 3><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
+      else if (half)
+        head_bias_grad_kernel<true, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
+      else
+        head_bias_grad_kernel<false, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
+      ZENO_STEP(hipGetLastError());
+    }
+  }
+  if (a.dhidden != nullptr && a.rows > 0) {
+    const unsigned blocks = (unsigned)std::min<long long>(((long long)a.rows * a.width + 255) / 256, 16384);
+    if (a.dtype == ZENO_F32)
+      hidden_join_kernel<float><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<float*>(a.dhidden), a.lddh);
+    else if (half)
+      hidden_join_kernel<_Float16><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<_Float16*>(a.dhidden), a.lddh);
+    else
+      hidden_join_kernel<__bf16><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<__bf16*>(a.dhidden), a.lddh);
+    ZENO_STEP(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+}  // namespace zeno

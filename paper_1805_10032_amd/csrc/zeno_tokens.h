@@ -288,6 +288,37 @@ struct EmbedGradArgs {
 size_t embedding_workspace_bytes(int rows, int vocab, int width, int m);
 hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream_t stream);
 
+// ---- log probabilities of a linear layer's outputs (zeno_linear_logprobs.hip)
+struct LinearLogprobsArgs {
+  const void *hidden, *weight;
+  long long ldh, ldw;
+  int dtype, rows, vocab, width;
+  const float* bias;          // may be nullptr
+  const int32_t* labels;
+  float *logp, *entropy, *stats;
+};
+size_t linear_logprobs_workspace_bytes(int rows, int vocab, int width, int dtype);
+hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, hipStream_t stream);
+
+struct LinearLogprobsGradArgs {
+  const void *hidden, *weight;
+  long long ldh, ldw;
+  int dtype, rows, vocab, width;
+  const float *bias, *stats;
+  const int32_t* labels;
+  const float *grad_logp, *entropy, *grad_entropy;
+  int m;
+  const int32_t* offsets;     // nullptr: all rows are one group's
+  void* dhidden;              // each may be nullptr
+  long long lddh;
+  float* dweight;
+  long long ldg;
+  float* dbias;
+  long long ldb;
+};
+size_t linear_logprobs_backward_workspace_bytes(int rows, int vocab, int width, int dtype, int m);
+hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void* workspace, hipStream_t stream);
+
 // ---- the score from log probabilities (zeno_score_tokens.hip)
 size_t score_logprobs_workspace_bytes(int m, long long d);
 hipError_t launch_score_logprobs(const float* G, long long ldg, int m, long long d, const float* logp_x, const float* logp,
