@@ -4,10 +4,14 @@
 //
 // Forward: tiles of h W^T on the matrix cores; a tile leaves (max, sum of exponentials) for each of its tokens, which are joined behind.  The
 // logits stay float32 and never leave the registers.
-// Backward: the vocabulary in pieces.  A piece's logits are formed again, their dz goes to the workspace as 16-bit planes (a sum of
-// two or three of them where float32 gradients are taken from it), and two products read it: with W for dh, with h for dW.
+// Backward: the vocabulary in pieces.  A piece's logits are formed again, their dz goes to the workspace as 16-bit planes, and two products read
+// it: with W for dh, with h for dW.
 // Operands are planes of 16 bits: bf16 and fp16 as they are; float32 is a sum of three bf16 pieces, of whose nine products six are taken, those
 // that are left out lie below 2^-24 of the product.
+// dz in 16-bit types.  dh is rounded to the type itself, and takes dz in one plane of it; what the label's value, the largest as a rule, loses there
+// is added behind in float32.  dW and db are float32 and take dz as two fp16 planes, 22 bits, scaled so that the largest gradient comes
+// near fp16's largest: the sum of two bf16 planes has 16 bits, and its error (4e-6 of dW) would be several times that of the float32 sums.  fp16 planes need h in
+// fp16 too: bf16's eight bits fit, once a power of two for each column has brought its range there.
 #include "zeno_tokens.h"
 #include <algorithm>
 
@@ -447,12 +451,14 @@ Pairs pairs_of(int a, int b) {   // planes of the two sides
 struct GradScale {
   float up, down;   // what dz is multiplied by on its way into 16 bits, and the products by on their way out
 };
-// fp16 keeps dz within 2^14: a power of two of the largest gradient that a token brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e, p H <= ln V < 21).
-// The others have float32's range.
-__global__ __launch_bounds__(1024) void grad_scale_kernel(const float* g, const float* q, const int32_t* labels, int rows, int half, GradScale* out) {
+// 16-bit types keep dz within 2^14: a power of two of the largest gradient that a token brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
+// p H <= ln V < 21).  float32's pieces have its range.  `clear`: `n` words to set to zero on the way.
+__global__ __launch_bounds__(1024) void grad_scale_kernel(const float* g, const float* q, const int32_t* labels, int rows, int scaled, GradScale* out,
+                                                         unsigned* clear, int n) {
   __shared__ float shared[16];
   float largest = 0.f;
-  if (half)
+  for (int i = threadIdx.x; i < n; i += 1024) clear[i] = 0;
+  if (scaled)
     for (int t = threadIdx.x; t < rows; t += 1024) {
       float b = g != nullptr && labels[t] != -1 ? fabsf(g[t]) : 0.f;
       if (q != nullptr) b += 22.f * fabsf(q[t]);
@@ -473,14 +479,64 @@ __global__ __launch_bounds__(1024) void grad_scale_kernel(const float* g, const 
   out->down = __uint_as_float((unsigned)(127 - up) << 23);
 }
 
+// bf16 hidden states as fp16, each column times the power of two that brings its largest finite value to 2^14 .. 2^15: exact down to 2^-32
+// of that value.
+__device__ inline int column_power(unsigned largest) {   // largest magnitude, as float32 bits
+  if (largest == 0) return 0;
+  const int up = 14 + 127 - (int)(largest >> 23);
+  return up > 126 ? 126 : up;                            // (not below 14 + 127 - 254)
+}
+__host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
+__device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
+constexpr int kColumnRows = 256;   // that a workgroup looks at
+__global__ __launch_bounds__(256) void column_max_kernel(Side h, int width, unsigned* largest) {
+  const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
+  if (col >= width) return;
+  unsigned m[8] = {};
+  const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+  for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
+    const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned v = (unsigned)raw[j] & 0x7fff;
+      if (v < 0x7f80 && v > m[j]) m[j] = v;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (m[j] != 0 && col + j < width) atomicMax(&largest[col + j], m[j] << 16);
+}
+__global__ __launch_bounds__(256) void column_half_kernel(Side h, int width, const unsigned* largest, u16* out) {
+  const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
+  if (col >= width) return;
+  float up[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) up[j] = power_of_two(column_power(col + j < width ? largest[col + j] : 0));
+  const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+  for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
+    const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
+    s16x8 half;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const short bits = raw[j];
+      half[j] = __builtin_bit_cast(short, (_Float16)(__uint_as_float((unsigned)(u16)bits << 16) * up[j]));
+    }
+    *reinterpret_cast<s16x8*>(out + (long long)row * padded_stride(width) + col) = half;
+  }
+}
+
 struct DzArgs {
   LogitArgs l;
   const float *stats, *grad_logp, *entropy, *grad_entropy;
   const GradScale* scale;
   u16* dz;               // [planes][rows][ldz]
   long long ldz, plane;
+  float* rest;           // [rows] what the label's value loses in the first plane, or nullptr
 };
-template <typename S, bool HALF, int P>
+// Planes of dz.
+enum Planes { kBf16Three, kBf16AndHalf, kHalfTwo };   // three bf16 pieces; one bf16, and two fp16 pieces; two fp16 pieces
+__host__ __device__ constexpr int count_of(Planes p) { return p == kHalfTwo ? 2 : 3; }
+template <typename S, bool HALF, Planes P>
 __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
@@ -489,7 +545,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN), v = a.l.v0 + t.m * S::BM + wm;
   add_bias<S>(a.l, v, lane, acc);
-  const float up = HALF ? a.scale->up : 1.f;
+  const float up = P == kBf16Three ? 1.f : a.scale->up;
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     const int token = t.n * S::BN + wn + 32 * j + lane % 32;
@@ -515,7 +571,8 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
       log_s = __builtin_inff();
     }
     const float base = a.grad_entropy != nullptr ? fmaf(q, H, g) : g;
-    const int hit = empty ? -1 : y - v;
+    const int hit = y - v;
+    const float add = empty ? 0.f : g;
 #pragma unroll
     for (int r = 0; r < S::FM; ++r)
 #pragma unroll
@@ -523,7 +580,13 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
         const float lp = (acc[r][j][e] - M) - log_s, p = exp_fast(lp);
         // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
         float d = -p * (a.grad_entropy != nullptr ? fmaf(q, fmaxf(lp, -256.f), base) : base);
-        if (hit == 32 * r + row_of(e, lane)) d += g;
+        if (hit == 32 * r + row_of(e, lane)) {
+          d += add;
+          if (P != kBf16Three) {
+            const float scaled = d * up;
+            a.rest[token] = scaled - (P == kHalfTwo ? (float)(_Float16)scaled : (float)(__bf16)scaled);
+          }
+        }
         if (v + 32 * r + row_of(e, lane) >= a.l.vocab) d = 0.f;
         acc[r][j][e] = d * up;
       }
@@ -531,7 +594,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
   // a plane at a time through LDS, so that rows leave in whole lines
   u16* tile = reinterpret_cast<u16*>(memory);
 #pragma unroll
-  for (int plane = 0; plane < P; ++plane) {
+  for (int plane = 0; plane < count_of(P); ++plane) {
     if (plane > 0) __syncthreads();
 #pragma unroll
     for (int j = 0; j < S::FN; ++j)
@@ -543,14 +606,14 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float d = acc[r][j][4 * c + i];
-            if constexpr (HALF) {
+            if (P == kHalfTwo || (P == kBf16AndHalf && plane > 0)) {
               const _Float16 x = (_Float16)d;
               out[i] = __builtin_bit_cast(short, x);
               acc[r][j][4 * c + i] = d - (float)x;
             } else {
               const __bf16 x = (__bf16)d;
               out[i] = __builtin_bit_cast(short, x);
-              acc[r][j][4 * c + i] = d - (float)x;
+              if (P == kBf16Three) acc[r][j][4 * c + i] = d - (float)x;
             }
           }
           *reinterpret_cast<s16x4*>(tile + (wn + 32 * j + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane)) = out;
@@ -597,20 +660,36 @@ __global__ __launch_bounds__(S::THREADS) void hidden_grad_kernel(HiddenArgs a) {
         }
       }
 }
-// Slots in their order, for the rows that belong to somebody.
+// Slots in their order, and what the label's value lost, for the rows that belong to somebody.
+struct HiddenJoinArgs {
+  const float* slots;
+  int splits, rows, width, vocab, m;
+  const int32_t *offsets, *labels;
+  const GradScale* scale;
+  const float* rest;     // or nullptr
+  const void* weight;
+  long long ldw;
+  void* out;
+  long long ldo;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void hidden_join_kernel(const float* slots, int splits, int rows, int width, int m, const int32_t* offsets,
-                                                         const GradScale* scale, T* out, long long ldo) {
-  const int lo = group_offset(offsets, 0, rows), hi = group_offset(offsets, offsets == nullptr ? 1 : m, rows);
-  const long long stride = (long long)rows * width;
-  const float down = scale->down;
-  const long long all = stride;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-    const long long row = i / width;
-    if (row < lo || row >= hi) continue;
-    float sum = slots[i];
-    for (int s = 1; s < splits; ++s) sum += slots[s * stride + i];
-    out[row * ldo + (i - row * width)] = (T)(sum * down);
+__global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
+  const int lo = group_offset(a.offsets, 0, a.rows), hi = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
+  const long long stride = (long long)a.rows * a.width;
+  const float down = a.scale->down;
+  for (int row = lo + blockIdx.y; row < hi; row += gridDim.y) {
+    const int y = a.rest != nullptr ? a.labels[row] : -1;
+    const bool has = y >= 0 && y < a.vocab;
+    const float rest = has ? a.rest[row] : 0.f;
+    const float* from = a.slots + (long long)row * a.width;
+    const T* w = reinterpret_cast<const T*>(a.weight) + (has ? y : 0) * a.ldw;
+    T* to = reinterpret_cast<T*>(a.out) + row * a.ldo;
+    for (int col = blockIdx.x * 256 + threadIdx.x; col < a.width; col += gridDim.x * 256) {
+      float sum = from[col];
+      for (int s = 1; s < a.splits; ++s) sum += from[s * stride + col];
+      if (has) sum = fmaf(rest, (float)w[col], sum);
+      to[col] = (T)(sum * down);
+    }
   }
 }
 
@@ -621,6 +700,7 @@ struct WeightArgs {
   int tiles_m, tiles_n, rows, width, values;   // values: of the vocabulary in this piece
   const int32_t* offsets;
   const GradScale* scale;
+  const unsigned* columns;   // largest values of the columns of h that have been scaled by column_power(), or nullptr
   float* dweight;        // at the piece's first value
   long long ldw;
 };
@@ -636,14 +716,18 @@ __global__ __launch_bounds__(S::THREADS) void head_weight_grad_kernel(WeightArgs
   const float down = HALF ? a.scale->down : 1.f;
   float* dw = a.dweight + g * a.ldw;
 #pragma unroll
-  for (int r = 0; r < S::FM; ++r)
+  for (int j = 0; j < S::FN; ++j) {
+    const int col = col0 + 32 * j;
+    if (col >= a.width) continue;
+    const float back = HALF && a.columns != nullptr ? power_of_two(-column_power(a.columns[col])) : 1.f;
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j)
+    for (int r = 0; r < S::FM; ++r)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
-        if (row < a.values && col < a.width) dw[(long long)row * a.width + col] = acc[r][j][e] * down;
+        const int row = row0 + 32 * r + row_of(e, lane);
+        if (row < a.values) dw[(long long)row * a.width + col] = acc[r][j][e] * down * back;
       }
+  }
 }
 
 // db of a piece: 512 values a workgroup, every wave some of the group's tokens.
@@ -733,12 +817,12 @@ struct BackwardPlan {
   int piece;          // values of the vocabulary at a time
   int planes;         // of dz
   int splits;
-  size_t hidden, weight, dz, slots, scale, bytes;
+  size_t hidden, weight, dz, slots, scale, rest, half, columns, bytes;
 };
 BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   BackwardPlan p;
   const long long padded = padded_width(width), n = std::max(rows, 1);
-  p.planes = dtype == ZENO_F32 ? 3 : 2;
+  p.planes = dtype == ZENO_F16 ? 2 : 3;
   // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles
   const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
   const long long pieces = (vocab + most - 1) / most;
@@ -755,6 +839,9 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   p.dz = l.take((size_t)p.planes * n * p.piece * 2);
   p.slots = l.take((size_t)p.splits * n * width * 4);
   p.scale = l.take(256);
+  p.rest = l.take((size_t)n * 4);
+  p.half = l.take(dtype == ZENO_BF16 ? (size_t)n * padded * 2 : 0);
+  p.columns = l.take((size_t)width * 4);
   p.bytes = l.at + 256;
   return p;
 }
@@ -767,7 +854,7 @@ hipError_t start_stats(const StatArgs& a, hipStream_t stream) {
   kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::LDS, stream>>>(a);
   return hipGetLastError();
 }
-template <typename S, bool HALF, int P>
+template <typename S, bool HALF, Planes P>
 hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
   const auto kernel = logit_grad_kernel<S, HALF, P>;
   const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
@@ -777,8 +864,8 @@ hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
 }
 template <typename S>
 hipError_t start_dz(const DzArgs& a, int dtype, hipStream_t stream) {
-  if (dtype == ZENO_F32) return start_dz<S, false, 3>(a, stream);
-  return dtype == ZENO_F16 ? start_dz<S, true, 2>(a, stream) : start_dz<S, false, 2>(a, stream);
+  if (dtype == ZENO_F32) return start_dz<S, false, kBf16Three>(a, stream);
+  return dtype == ZENO_F16 ? start_dz<S, true, kHalfTwo>(a, stream) : start_dz<S, false, kBf16AndHalf>(a, stream);
 }
 template <typename S, bool HALF>
 hipError_t start_hidden(const HiddenArgs& a, int splits, hipStream_t stream) {
@@ -876,7 +963,9 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const bool half = a.dtype == ZENO_F16;
   const int planes = planes_of(a.dtype);
   GradScale* scale = reinterpret_cast<GradScale*>(ws + p.scale);
-  grad_scale_kernel<<<1, 1024, 0, stream>>>(a.grad_logp, a.grad_entropy, a.labels, a.rows, half ? 1 : 0, scale);
+  const bool convert = a.dtype == ZENO_BF16 && a.dweight != nullptr && a.rows > 0;
+  unsigned* columns = reinterpret_cast<unsigned*>(ws + p.columns);
+  grad_scale_kernel<<<1, 1024, 0, stream>>>(a.grad_logp, a.grad_entropy, a.labels, a.rows, planes == 1 ? 1 : 0, scale, columns, convert ? a.width : 0);
   ZENO_STEP(hipGetLastError());
   DzArgs d = {};
   LogitArgs& l = d.l;
@@ -888,6 +977,15 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   l.rows = a.rows;
   l.bias = a.bias;
   l.labels = a.labels;
+  Side hidden = l.h;   // as the weights' gradients take it
+  if (convert) {
+    const dim3 grid((unsigned)ceil_div(a.width, 512), (unsigned)ceil_div(a.rows, kColumnRows));
+    hidden = {reinterpret_cast<const u16*>(ws + p.half), l.width, 0, a.rows};
+    column_max_kernel<<<grid, 256, 0, stream>>>(l.h, a.width, columns);
+    column_half_kernel<<<grid, 256, 0, stream>>>(l.h, a.width, columns, reinterpret_cast<u16*>(ws + p.half));
+    ZENO_STEP(hipGetLastError());
+  }
+  d.rest = planes == 1 ? reinterpret_cast<float*>(ws + p.rest) : nullptr;
   d.stats = a.stats;
   d.grad_logp = a.grad_logp;
   d.entropy = a.entropy;
@@ -897,6 +995,8 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   d.ldz = p.piece;
   d.plane = (long long)a.rows * p.piece;
   float* slots = reinterpret_cast<float*>(ws + p.slots);
+  const int fine = a.dtype == ZENO_BF16 ? 1 : 0;   // the first plane that the float32 gradients take
+  const u16* fine_dz = d.dz + fine * d.plane;
   for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const int values = std::min(p.piece, a.vocab - v0);
     if (a.rows > 0) {
@@ -928,10 +1028,11 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
     }
     if (a.dweight != nullptr) {
       WeightArgs w = {};
-      w.dz = {d.dz, d.ldz, d.plane, p.piece};
-      w.h = l.h;
+      w.dz = {fine_dz, d.ldz, d.plane, p.piece};
+      w.h = hidden;
       w.h.extent = l.width;
-      w.pairs = pairs_of(p.planes, planes);
+      w.pairs = pairs_of(p.planes - fine, planes);
+      w.columns = convert ? columns : nullptr;
       const int tile = p.wide_weight ? 256 : 128;
       w.tiles_m = ceil_div(values, tile);
       w.tiles_n = ceil_div(a.width, tile);
@@ -942,29 +1043,26 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       w.scale = scale;
       w.dweight = a.dweight + (long long)v0 * a.width;
       w.ldw = a.ldg;
-      if (p.wide_weight) ZENO_STEP(half ? (start_weight<WideTile, true>(w, a.m, stream)) : (start_weight<WideTile, false>(w, a.m, stream)));
-      else ZENO_STEP(half ? (start_weight<MidTile, true>(w, a.m, stream)) : (start_weight<MidTile, false>(w, a.m, stream)));
+      if (p.wide_weight) ZENO_STEP(planes == 1 ? (start_weight<WideTile, true>(w, a.m, stream)) : (start_weight<WideTile, false>(w, a.m, stream)));
+      else ZENO_STEP(planes == 1 ? (start_weight<MidTile, true>(w, a.m, stream)) : (start_weight<MidTile, false>(w, a.m, stream)));
     }
     if (a.dbias != nullptr) {
       const dim3 grid((unsigned)ceil_div(values, 512), a.m);
       float* db = a.dbias + v0;
-      if (a.dtype == ZENO_F32)
+      if (planes == 3)
         head_bias_grad_kernel<false, 3><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
-      else if (half)
-        head_bias_grad_kernel<true, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
       else
-        head_bias_grad_kernel<false, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
+        head_bias_grad_kernel<true, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(fine_dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
       ZENO_STEP(hipGetLastError());
     }
   }
   if (a.dhidden != nullptr && a.rows > 0) {
-    const unsigned blocks = (unsigned)std::min<long long>(((long long)a.rows * a.width + 255) / 256, 16384);
-    if (a.dtype == ZENO_F32)
-      hidden_join_kernel<float><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<float*>(a.dhidden), a.lddh);
-    else if (half)
-      hidden_join_kernel<_Float16><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<_Float16*>(a.dhidden), a.lddh);
-    else
-      hidden_join_kernel<__bf16><<<blocks, 256, 0, stream>>>(slots, p.splits, a.rows, a.width, a.m, a.offsets, scale, reinterpret_cast<__bf16*>(a.dhidden), a.lddh);
+    const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.vocab, a.m, a.offsets, a.labels, scale,
+                              a.grad_logp != nullptr ? d.rest : nullptr, a.weight, a.ldw, a.dhidden, a.lddh};
+    const dim3 grid((unsigned)std::min(ceil_div(a.width, 256), 64), (unsigned)std::min(a.rows, 16384));
+    if (a.dtype == ZENO_F32) hidden_join_kernel<float><<<grid, 256, 0, stream>>>(j);
+    else if (half) hidden_join_kernel<_Float16><<<grid, 256, 0, stream>>>(j);
+    else hidden_join_kernel<__bf16><<<grid, 256, 0, stream>>>(j);
     ZENO_STEP(hipGetLastError());
   }
   return hipSuccess;

@@ -145,10 +145,10 @@ def backward(B, rows, vocab, width, ty, offsets, entropy_too, *, pad_h=0, pad_w=
     B.zeno_linear_logprobs_backward(h, w, b, stats, labels=labels if grad else None, grad_logp=g, entropy=entropy if entropy_too else None,
                                     grad_entropy=q, groups=groups, dhidden=dh, dweight=G[:, :n], dbias=G[:, n:])
     dz, e = ref.grad(g, q)
-    planes = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -16, "fp16": 2.0 ** -22}[ty]
+    planes = 2.0 ** -24 if ty == "fp32" else 2.0 ** -22
     first = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}[ty]
     least = 0.0
-    if ty == "fp16":
+    if ty != "fp32":
         least = 2.0 ** -38 * float(((g.abs() if grad else 0) + (22 * q.abs() if q is not None else 0)).max())
     lo, hi = off[0], off[-1]
     W, H = ref.W, ref.H
@@ -162,7 +162,8 @@ def backward(B, rows, vocab, width, ty, offsets, entropy_too, *, pad_h=0, pad_w=
         tokens = off[i + 1] - off[i]
         d, de = dz[part], e[part] + planes * dz[part].abs() + least
         want = d.t() @ H[part]
-        bound = de.t() @ H[part].abs() + (2 * tokens + 12) * EPS * (d.abs().t() @ H[part].abs())
+        inexact = 2.0 ** -39 * H.abs().amax(0) if ty == "bf16" and rows else 0.0   # hidden states in fp16, columns scaled
+        bound = de.t() @ H[part].abs() + d.abs().sum(0)[:, None] * inexact + (2 * tokens + 12) * EPS * (d.abs().t() @ H[part].abs())
         inside(G[i, :n].view(vocab, width), want, bound * 1.01 + EPS * want.abs() + 2.0 ** -120, f"dweight {i}")
         inside(G[i, n:], d.sum(0), (de.sum(0) + (3 * tokens + 16) * EPS * d.abs().sum(0)) * 1.01 + 2.0 ** -120, f"dbias {i}")
     assert torch.equal(before.isnan(), around(G, buf).isnan()) and torch.equal(dh_before.isnan(), around(dh, dh_buf).isnan())
