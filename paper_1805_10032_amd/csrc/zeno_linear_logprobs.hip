@@ -14,6 +14,7 @@
 // fp16 too: bf16's eight bits fit, once a power of two for each column has brought its range there.
 #include "zeno_tokens.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace zeno {
 namespace {
@@ -34,10 +35,11 @@ struct Tile {
   static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;   // 32 x 32 blocks of a wave
   static constexpr int A_BYTES = BM * kStep * 2, STAGE = (BM + BN) * kStep * 2;
   static constexpr int LOADS_A = A_BYTES / 1024 / WAVES, LOADS_B = BN * kStep * 2 / 1024 / WAVES, LOADS = LOADS_A + LOADS_B;
-  static constexpr int PITCH = BM + 8;                         // of a plane of dz on its way out, [token][vocabulary]
-  static constexpr int LDS = kStages * STAGE > BN * PITCH * 2 ? kStages * STAGE : BN * PITCH * 2;
+  static constexpr int PITCH = BM + 8;                         // of planes of dz on their way out, [32 WN tokens][vocabulary]
+  static constexpr int LDS = kStages * STAGE;
+  static_assert(3 * 32 * WN * PITCH * 2 <= LDS, "dz on its way out");
 };
-using WideTile = Tile<256, 256, 2, 4>;
+using WideTile = Tile<256, 256, 2, 2>;
 using MidTile = Tile<128, 128, 2, 2>;
 
 // An operand: planes of 16-bit values, `plane` elements apart, rows ld apart and on 16 bytes.
@@ -79,13 +81,16 @@ template <bool ACROSS, int B, int WAVES>
 struct Loader {
   static constexpr int N = B * kStep * 2 / 1024 / WAVES, PER = 512 / B;   // copies a wave; rows of a copy, if ACROSS
   static_assert(N >= 1, "every wave copies");
-  static_assert(!ACROSS || PER * WAVES % 16 == 0, "a lane's copies exchange the same blocks");
+  // ACROSS: the rows of a wave's copies differ in bits that block_of() does not look at, so that a lane has the same columns in all of them
+  static_assert(!ACROSS || (B == 256 && WAVES == 4) || (B == 128 && PER * WAVES == 16), "rows of a copy");
+  static __device__ inline int row_of_wave(int wave) { return B == 256 ? 2 * (wave & 1) + 8 * (wave >> 1) : PER * wave; }
+  static __device__ inline constexpr int row_of_copy(int n) { return B == 256 ? 4 * (n & 1) + 16 * (n >> 1) : 16 * n; }
   const u16* at[N];
   int k;        // of the lane's first value, in its first copy
   bool inside;  // its columns exist
   unsigned to;
   __device__ inline void start(const Side& s, int plane, long long first, long long x0, int wave, int lane, unsigned lds) {
-    to = lds + 1024 * wave;
+    to = lds + (ACROSS ? 2 * B * row_of_wave(wave) : 1024 * wave);
     inside = true;
     const u16* p = s.p + plane * s.plane;
     if (!ACROSS) {
@@ -97,21 +102,18 @@ struct Loader {
       }
     } else {
       const int slot = lane % (64 / PER);
-      k = PER * wave + lane / (64 / PER);
+      k = row_of_wave(wave) + lane / (64 / PER);
       const long long col = x0 + 32 * ((slot / 4) ^ block_of<B>(k)) + 8 * (slot % 4);
       inside = col < s.extent;
 #pragma unroll
-      for (int n = 0; n < N; ++n) at[n] = p + (first + k + PER * WAVES * n) * s.ld + (inside ? col : 0);
+      for (int n = 0; n < N; ++n) at[n] = p + (first + k + row_of_copy(n)) * s.ld + (inside ? col : 0);
     }
   }
   // `left`: what of the contraction is left from this stage on
-  __device__ inline void issue(const Side& s, int stage_offset, int left) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const bool live = inside && k + (ACROSS ? PER * WAVES * n : 0) < left;
-      copy_to_lds(live ? at[n] : reinterpret_cast<const u16*>(zero_chunk), to + stage_offset + 1024 * WAVES * n);
-      at[n] += ACROSS ? kStep * s.ld : kStep;
-    }
+  __device__ inline void issue(const Side& s, int n, int stage_offset, int left) {
+    const bool live = inside && k + (ACROSS ? row_of_copy(n) : 0) < left;
+    copy_to_lds(live ? at[n] : reinterpret_cast<const u16*>(zero_chunk), to + stage_offset + (ACROSS ? 2 * B * row_of_copy(n) : 1024 * WAVES * n));
+    at[n] += ACROSS ? kStep * s.ld : kStep;
   }
   __device__ inline void move(long long by) {
 #pragma unroll
@@ -142,10 +144,25 @@ __device__ inline f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// The operands of sixteen of the contraction, in the order in which they are needed.
+template <typename S>
+struct Operands {
+  s16x8 x[S::FM], y[S::FN];
+};
+template <typename S, bool A_ACROSS, bool B_ACROSS>
+__device__ inline void read_one(int i, const unsigned char* part, int k, int wm, int wn, int lane, Operands<S>& o) {
+  if (i >= 1 && i <= S::FN) o.y[i - 1] = read_operand<B_ACROSS, S::BN>(part + S::A_BYTES, wn + 32 * (i - 1), k, lane);
+  else o.x[i == 0 ? 0 : i - S::FN] = read_operand<A_ACROSS, S::BM>(part, wm + 32 * (i == 0 ? 0 : i - S::FN), k, lane);
+}
+
 // acc += the product of BM rows (columns) of A from m0 on and BN of B from n0 on over `length` of the contraction, which begins at `first`.
-template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS>
+// While a stage is multiplied the next is whole, so that its first operands are read before the barrier, the one behind it is on its way,
+// and the fourth is requested.  A wave of a wide tile has its SIMD to itself and issues in order: what runs beside the matrix
+// instructions stands between them.
+// SUMS: also the sums of A's rows over the contraction, as products with ones; the WN waves that have the same rows take FM / WN blocks of them each.
+template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS, bool SUMS = false>
 __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
-                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN]) {
+                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN], f32x16 (&sums)[S::FM / S::WN]) {
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN);
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)memory;
@@ -156,9 +173,10 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
   la.start(a, pairs.a[0], first, m0, wave, lane, lds);
   lb.start(b, pairs.b[0], first, n0, wave, lane, lds + S::A_BYTES);
   int pair = 0, left = length;   // of the next stage to fetch
-  auto fetch = [&](int stage) __attribute__((always_inline)) {
-    la.issue(a, stage * S::STAGE, left);
-    lb.issue(b, stage * S::STAGE, left);
+  auto fetch_one = [&](int i, int stage) __attribute__((always_inline)) {
+    if (i < S::LOADS_A) la.issue(a, i, stage * S::STAGE, left);
+    else lb.issue(b, i - S::LOADS_A, stage * S::STAGE, left);
+    if (i + 1 < S::LOADS) return;
     left -= kStep;
     if (left <= 0 && pair + 1 < pairs.count) {
       const long long back = (long long)steps * kStep;
@@ -170,27 +188,64 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
   };
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i)
-    if (i < total) fetch(i);
-  for (int i = 0; i < total; ++i) {
-    if (i + 2 < total) begin_stage<2 * S::LOADS>();
-    else if (i + 1 < total) begin_stage<S::LOADS>();
-    else begin_stage<0>();
-    if (i + kStages - 1 < total) fetch((i + kStages - 1) % kStages);
-    const unsigned char* part = memory + (i % kStages) * S::STAGE;
+    if (i < total) {
 #pragma unroll
-    for (int k = 0; k < kStep; k += 16) {
-      s16x8 x[S::FM], y[S::FN];
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r) x[r] = read_operand<A_ACROSS, S::BM>(part, wm + 32 * r, k, lane);
-#pragma unroll
-      for (int j = 0; j < S::FN; ++j) y[j] = read_operand<B_ACROSS, S::BN>(part + S::A_BYTES, wn + 32 * j, k, lane);
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j) acc[r][j] = multiply<HALF>(x[r], y[j], acc[r][j]);
+      for (int n = 0; n < S::LOADS; ++n) fetch_one(n, i);
     }
+  if (total > 2) begin_stage<S::LOADS>();   // the first two are whole
+  else begin_stage<0>();
+  constexpr int OPERANDS = S::FM + S::FN, PRODUCTS = S::FM * S::FN, READ_UNTIL = PRODUCTS > 4 ? PRODUCTS / 2 : PRODUCTS;
+  Operands<S> now, next;
+  s16x8 ones;                    // of B's first plane: each plane of A counts once
+  int its = 0, until = 0;        // pair that is multiplied, and the step where the next begins
+  auto set_ones = [&](int i) __attribute__((always_inline)) {
+    if (!SUMS || i < until) return;
+    its = i == 0 ? 0 : its + 1;
+    until += steps;
+    const short one = pairs.b[its] != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
+    ones = s16x8{one, one, one, one, one, one, one, one};
+  };
+#pragma unroll
+  for (int n = 0; n < OPERANDS; ++n) read_one<S, A_ACROSS, B_ACROSS>(n, memory, 0, wm, wn, lane, now);
+  // Sixteen of the contraction; the next sixteen's operands are read behind the first products, copies are sent behind the last.
+  auto half = [&](const Operands<S>& use, Operands<S>& fill, const unsigned char* part, int k, int from, int to, int stage,
+                  auto fetching) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < PRODUCTS; ++q) {
+      const int r = q / S::FN, j = q % S::FN;
+      acc[r][j] = multiply<HALF>(use.x[r], use.y[j], acc[r][j]);
+      if (SUMS && j == S::FN - 1 && r % S::WN == S::WN - 1) {
+        static_assert(S::WN == 2, "two waves have the same rows");
+        sums[r / 2] = multiply<HALF>(wave / S::WM == 0 ? use.x[r - 1] : use.x[r], ones, sums[r / 2]);
+      }
+#pragma unroll
+      for (int n = 0; n < OPERANDS; ++n)
+        if (n * READ_UNTIL / OPERANDS == q)
+          read_one<S, A_ACROSS, B_ACROSS>(n, part, k, wm, wn, lane, fill);
+      if constexpr (decltype(fetching)::value) {
+#pragma unroll
+        for (int n = from; n < to; ++n)
+          if (PRODUCTS / 2 + (n - from) * (PRODUCTS / 2) / (to - from) == q) fetch_one(n, stage);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto step = [&](int i, auto fetching) __attribute__((always_inline)) {
+    const int stage = (i + kStages - 1) % kStages;
+    set_ones(i);
+    half(now, next, memory + (i % kStages) * S::STAGE, 16, 0, S::LOADS / 2, stage, fetching);
+    // (behind the last stage: what stands in LDS, for no one)
+    half(next, now, memory + ((i + 1) % kStages) * S::STAGE, 0, S::LOADS / 2, S::LOADS, stage, fetching);
+  };
+  int i = 0;
+  for (; i + kStages - 1 < total; ++i) {
+    step(i, std::true_type());
+    begin_stage<S::LOADS>();   // the stage after next is whole
   }
-  begin_stage<0>();   // (the stages are free for what follows)
+  for (; i < total; ++i) {
+    step(i, std::false_type());
+    begin_stage<0>();
+  }
 }
 
 // Where a workgroup's tile lies: each of the eight dies, to which workgroups go in turn, takes a run of tiles, in patches of eight rows of tiles.
@@ -208,6 +263,13 @@ __device__ inline Place place_of(unsigned id, unsigned tiles_m, unsigned tiles_n
   return p;
 }
 
+template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS>
+__device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
+                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN]) {
+  f32x16 none[S::FM / S::WN];
+  product<S, HALF, A_ACROSS, B_ACROSS, false>(a, b, pairs, m0, n0, first, length, memory, acc, none);
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -223,34 +285,48 @@ struct LogitArgs {
 // Row of a wave's 32 x 32 block that element e of a lane holds.
 __device__ inline int row_of(int e, int lane) { return 8 * (e / 4) + 4 * (lane / 32) + e % 4; }
 
-// Adds the bias; what lies behind the vocabulary becomes -inf.
+// The bias of a wave's rows from v on; what lies behind the vocabulary gets -inf, whatever its logit (a copy of the last row's, or finite).
 template <typename S>
-__device__ inline void add_bias(const LogitArgs& a, int v, int lane, f32x16 (&acc)[S::FM][S::FN]) {
+struct Bias {
+  float b[S::FM][16];
+  bool whole;
+};
+template <typename S>
+__device__ inline void load_bias(const LogitArgs& a, int v, int lane, Bias<S>& o) {
+  o.whole = v + 32 * S::FM <= a.vocab;
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int at = v + 32 * r + row_of(4 * q, lane);
-      float b[4] = {0.f, 0.f, 0.f, 0.f};
-      if (at + 4 <= a.vocab) {
-        if (a.bias != nullptr) {
-          const f32x4 raw = *reinterpret_cast<const f32x4_a4*>(a.bias + at);
+      f32x4 raw = {0.f, 0.f, 0.f, 0.f};
+      if (a.bias != nullptr) {
+        if (o.whole) {
+          raw = *reinterpret_cast<const f32x4_a4*>(a.bias + at);
+        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) b[i] = raw[i];
+          for (int i = 0; i < 4; ++i) raw[i] = at + i < a.vocab ? a.bias[at + i] : 0.f;
         }
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[r][j][4 * q + i] += b[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = at + i < a.vocab && a.bias != nullptr ? a.bias[at + i] : 0.f;
-#pragma unroll
-        for (int j = 0; j < S::FN; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[r][j][4 * q + i] = at + i < a.vocab ? acc[r][j][4 * q + i] + b[i] : -__builtin_inff();
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o.b[r][4 * q + i] = raw[i];
     }
+}
+// A block of 32 tokens' logits.
+template <typename S>
+__device__ inline void logits_of(const LogitArgs& a, int v, int lane, const Bias<S>& bias, const f32x16 (&acc)[S::FM][S::FN], int j,
+                                 float (&z)[S::FM][16]) {
+#pragma unroll
+  for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[r][e] = acc[r][j][e] + bias.b[r][e];
+  if (!bias.whole) {
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (v + 32 * r + row_of(e, lane) >= a.vocab) z[r][e] = -__builtin_inff();
+  }
 }
 
 // ---- forward: for each token and each slice of 32 FM values (max, sum of exp(z - max)) and, for the entropy, the sum of exp(z - max) (z - max)
@@ -262,56 +338,73 @@ struct StatArgs {
   float* label_logit;    // [rows]
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(StatArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_kernel(StatArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
   f32x16 acc[S::FM][S::FN] = {};
   product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int v = a.l.v0 + t.m * S::BM + (wave % S::WM) * (32 * S::FM);
-  add_bias<S>(a.l, v, lane, acc);
+  Bias<S> bias;
+  load_bias<S>(a.l, v, lane, bias);
   const int slice = a.slice0 + t.m * S::WM + wave % S::WM;
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
+    __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
     const int token = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + 32 * j + lane % 32;
+    const bool live = token < a.l.rows;
+    const int hit = live && a.l.labels != nullptr ? a.l.labels[token] - v : -1;
+    float z[S::FM][16];
+    logits_of<S>(a.l, v, lane, bias, acc, j, z);
     float top = -__builtin_inff();
 #pragma unroll
     for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[r][j][e]);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, z[r][e]);
     top = fmaxf(top, __shfl_xor(top, 32));
     const float from = top == -__builtin_inff() ? 0.f : top;
     float s = 0.f, u = 0.f;
+    if (a.part_u == nullptr) {
 #pragma unroll
-    for (int r = 0; r < S::FM; ++r)
+      for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float d = acc[r][j][e] - from, x = exp_fast(d);
-        s += x;
-        u += x > 0.f ? x * d : 0.f;
-      }
+        for (int e = 0; e < 16; ++e) s += exp_fast(z[r][e] - from);
+    } else {
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float d = z[r][e] - from, x = exp_fast(d);
+          s += x;
+          u += x > 0.f ? x * d : 0.f;
+        }
+      u += __shfl_xor(u, 32);
+    }
     s += __shfl_xor(s, 32);
-    u += __shfl_xor(u, 32);
-    if (token < a.l.rows) {
+    if (live && lane < 32) {
       const long long at = (long long)slice * a.l.rows + token;
-      if (lane < 32) {
-        a.part[at] = make_float2(top, s);
-        if (a.part_u != nullptr) a.part_u[at] = u;
-      }
-      const int hit = a.l.labels != nullptr ? a.l.labels[token] - v : -1;
-      if (hit >= 0 && hit < 32 * S::FM && hit + v < a.l.vocab) {
+      a.part[at] = make_float2(top, s);
+      if (a.part_u != nullptr) a.part_u[at] = u;
+    }
+    const bool here = hit >= 0 && hit < 32 * S::FM && hit + v < a.l.vocab;
+    if (__any(here)) {
+      float mine_z = 0.f;
+      bool mine = false;
 #pragma unroll
-        for (int r = 0; r < S::FM; ++r)
+      for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (hit == 32 * r + row_of(e, lane)) a.label_logit[token] = acc[r][j][e];
-      }
+        for (int e = 0; e < 16; ++e)
+          if (hit == 32 * r + row_of(e, lane)) {
+            mine_z = z[r][e];
+            mine = true;
+          }
+      if (here && mine) a.label_logit[token] = mine_z;
     }
   }
 }
 
-// Slices joined: 64 tokens a workgroup, every wave some of the slices.
-constexpr int kJoinWaves = 16;
+// Slices joined: `tokens` of them a workgroup, the other threads along the slices.
+constexpr int kJoinThreads = 1024;
 struct JoinArgs {
   const float2* part;
   const float* part_u;
@@ -341,25 +434,28 @@ struct Sums {
     }
   }
 };
-__global__ __launch_bounds__(64 * kJoinWaves) void logit_join_kernel(JoinArgs a) {
-  __shared__ float shared[3][kJoinWaves][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const long long token = (long long)blockIdx.x * 64 + lane;
+__global__ __launch_bounds__(kJoinThreads) void logit_join_kernel(JoinArgs a, int tokens) {
+  __shared__ float shared[3][kJoinThreads];
+  const int tid = threadIdx.x, lines = kJoinThreads / tokens, line = tid / tokens;
+  const long long token = (long long)blockIdx.x * tokens + tid % tokens;
   const bool live = token < a.rows;
   Sums m = {-__builtin_inff(), 0.f, 0.f};
   if (live) {
 #pragma unroll 4
-    for (int i = wave; i < a.slices; i += kJoinWaves) {
+    for (int i = line; i < a.slices; i += lines) {
       const float2 p = a.part[(long long)i * a.rows + token];
       m.add(p.x, p.y, a.part_u != nullptr ? a.part_u[(long long)i * a.rows + token] : 0.f);
     }
   }
-  shared[0][wave][lane] = m.top;
-  shared[1][wave][lane] = m.s;
-  shared[2][wave][lane] = m.u;
-  __syncthreads();
-  if (wave != 0 || !live) return;
-  for (int w = 1; w < kJoinWaves; ++w) m.add(shared[0][w][lane], shared[1][w][lane], shared[2][w][lane]);
+  for (int half = lines / 2; half > 0; half /= 2) {
+    shared[0][tid] = m.top;
+    shared[1][tid] = m.s;
+    shared[2][tid] = m.u;
+    __syncthreads();
+    if (line < half) m.add(shared[0][tid + half * tokens], shared[1][tid + half * tokens], shared[2][tid + half * tokens]);
+    __syncthreads();
+  }
+  if (line != 0 || !live) return;
   const bool empty = m.top == -__builtin_inff() && m.s == 0.f;
   const float log_s = empty ? 0.f : logf(m.s);
   if (a.stats != nullptr) {
@@ -488,12 +584,13 @@ __device__ inline int column_power(unsigned largest) {   // largest magnitude, a
 }
 __host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
 __device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
-constexpr int kColumnRows = 256;   // that a workgroup looks at
+constexpr int kColumnRows = 64;   // that a workgroup looks at
 __global__ __launch_bounds__(256) void column_max_kernel(Side h, int width, unsigned* largest) {
   const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
   if (col >= width) return;
   unsigned m[8] = {};
   const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+#pragma unroll 4
   for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
     const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
 #pragma unroll
@@ -513,6 +610,7 @@ __global__ __launch_bounds__(256) void column_half_kernel(Side h, int width, con
 #pragma unroll
   for (int j = 0; j < 8; ++j) up[j] = power_of_two(column_power(col + j < width ? largest[col + j] : 0));
   const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+#pragma unroll 4
   for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
     const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
     s16x8 half;
@@ -537,23 +635,24 @@ struct DzArgs {
 enum Planes { kBf16Three, kBf16AndHalf, kHalfTwo };   // three bf16 pieces; one bf16, and two fp16 pieces; two fp16 pieces
 __host__ __device__ constexpr int count_of(Planes p) { return p == kHalfTwo ? 2 : 3; }
 template <typename S, bool HALF, Planes P>
-__global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_kernel(DzArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
   f32x16 acc[S::FM][S::FN] = {};
   product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN), v = a.l.v0 + t.m * S::BM + wm;
-  add_bias<S>(a.l, v, lane, acc);
+  Bias<S> bias;
+  load_bias<S>(a.l, v, lane, bias);
   const float up = P == kBf16Three ? 1.f : a.scale->up;
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
+    __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
     const int token = t.n * S::BN + wn + 32 * j + lane % 32;
-    const bool live = token < a.l.rows;
     float M = 0.f, log_s = __builtin_inff(), g = 0.f, q = 0.f, H = 0.f;
     int y = -1;
     bool empty = true;
-    if (live) {
+    if (token < a.l.rows) {
       M = a.stats[2 * token];
       log_s = a.stats[2 * token + 1];
       empty = M == -__builtin_inff() && log_s == 0.f;
@@ -568,63 +667,85 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(DzArgs a) {
     }
     if (empty) {
       M = 0.f;
-      log_s = __builtin_inff();
+      log_s = __builtin_inff();   // every probability is 0
     }
-    const float base = a.grad_entropy != nullptr ? fmaf(q, H, g) : g;
-    const int hit = y - v;
-    const float add = empty ? 0.f : g;
-#pragma unroll
-    for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float lp = (acc[r][j][e] - M) - log_s, p = exp_fast(lp);
-        // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
-        float d = -p * (a.grad_entropy != nullptr ? fmaf(q, fmaxf(lp, -256.f), base) : base);
-        if (hit == 32 * r + row_of(e, lane)) {
-          d += add;
-          if (P != kBf16Three) {
-            const float scaled = d * up;
-            a.rest[token] = scaled - (P == kHalfTwo ? (float)(_Float16)scaled : (float)(__bf16)scaled);
-          }
-        }
-        if (v + 32 * r + row_of(e, lane) >= a.l.vocab) d = 0.f;
-        acc[r][j][e] = d * up;
-      }
-  }
-  // a plane at a time through LDS, so that rows leave in whole lines
-  u16* tile = reinterpret_cast<u16*>(memory);
-#pragma unroll
-  for (int plane = 0; plane < count_of(P); ++plane) {
-    if (plane > 0) __syncthreads();
-#pragma unroll
-    for (int j = 0; j < S::FN; ++j)
+    float z[S::FM][16];
+    logits_of<S>(a.l, v, lane, bias, acc, j, z);
+    if (a.grad_entropy != nullptr) {
+      const float base = fmaf(q, H, g);
 #pragma unroll
       for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          s16x4 out;
+        for (int e = 0; e < 16; ++e) {
+          // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
+          const float lp = (z[r][e] - M) - log_s;
+          z[r][e] = -exp_fast(lp) * fmaf(q, fmaxf(lp, -256.f), base) * up;
+        }
+    } else {
+      const float base = -g * up;   // (a power of two)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float d = acc[r][j][4 * c + i];
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[r][e] = exp_fast((z[r][e] - M) - log_s) * base;
+    }
+    if (!bias.whole) {
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (v + 32 * r + row_of(e, lane) >= a.l.vocab) z[r][e] = 0.f;   // (NaN, where g is)
+    }
+    const int hit = y < a.l.vocab ? y - v : -1;
+    if (__any(hit >= 0 && hit < 32 * S::FM)) {
+      const float add = empty ? 0.f : g * up;
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (hit == 32 * r + row_of(e, lane)) {
+            const float d = z[r][e] + add;
+            z[r][e] = d;
+            if (P != kBf16Three) a.rest[token] = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
+          }
+    }
+    // this block of every wave's tokens through LDS, so that rows leave in whole lines
+    u16* tile = reinterpret_cast<u16*>(memory);
+    constexpr int TOKENS = 32 * S::WN, PLANE = TOKENS * S::PITCH;
+    if (j > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s16x4 out[count_of(P)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float d = z[r][4 * c + i];
+#pragma unroll
+          for (int plane = 0; plane < count_of(P); ++plane) {
             if (P == kHalfTwo || (P == kBf16AndHalf && plane > 0)) {
               const _Float16 x = (_Float16)d;
-              out[i] = __builtin_bit_cast(short, x);
-              acc[r][j][4 * c + i] = d - (float)x;
+              out[plane][i] = __builtin_bit_cast(short, x);
+              d -= (float)x;
             } else {
               const __bf16 x = (__bf16)d;
-              out[i] = __builtin_bit_cast(short, x);
-              if (P == kBf16Three) acc[r][j][4 * c + i] = d - (float)x;
+              out[plane][i] = __builtin_bit_cast(short, x);
+              if (P == kBf16Three) d -= (float)x;
             }
           }
-          *reinterpret_cast<s16x4*>(tile + (wn + 32 * j + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane)) = out;
         }
+        u16* to = tile + (32 * (wave / S::WM) + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane);
+#pragma unroll
+        for (int plane = 0; plane < count_of(P); ++plane) *reinterpret_cast<s16x4*>(to + plane * PLANE) = out[plane];
+      }
     __syncthreads();
-    for (int i = threadIdx.x; i < S::BN * (S::BM / 8); i += S::THREADS) {
-      const int row = i / (S::BM / 8), col = i % (S::BM / 8) * 8;
-      const long long token = (long long)t.n * S::BN + row;
-      if (token < a.l.rows)
-        *reinterpret_cast<s16x8*>(a.dz + plane * a.plane + token * a.ldz + t.m * S::BM + col) =
-            *reinterpret_cast<const s16x8*>(tile + row * S::PITCH + col);
+    constexpr int CHUNKS = S::BM / 8;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < count_of(P) * TOKENS * CHUNKS; i += S::THREADS) {
+      const int plane = i / (TOKENS * CHUNKS), row = i / CHUNKS % TOKENS, col = i % CHUNKS * 8;
+      const long long to = (long long)t.n * S::BN + row / 32 * (32 * S::FN) + 32 * j + row % 32;
+      if (to < a.l.rows)
+        *reinterpret_cast<s16x8*>(a.dz + plane * a.plane + to * a.ldz + t.m * S::BM + col) =
+            *reinterpret_cast<const s16x8*>(tile + plane * PLANE + row * S::PITCH + col);
     }
   }
 }
@@ -638,15 +759,26 @@ struct HiddenArgs {
   float* slots;          // [splits][rows][width]
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS) void hidden_grad_kernel(HiddenArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void hidden_grad_kernel(HiddenArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
   const int begin = blockIdx.y * a.per, length = a.length - begin < a.per ? a.length - begin : a.per;
-  f32x16 acc[S::FM][S::FN] = {};
-  product<S, HALF, false, true>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0, memory, acc);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
   float* slot = a.slots + (long long)blockIdx.y * a.rows * a.width;
+  f32x16 acc[S::FM][S::FN] = {};
+  if (!a.first) {   // the sums go on from what the slot holds, which arrives beside the first operands (behind the products: 684 us, 454 without)
+#pragma unroll
+    for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+      for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
+          if (row < a.rows && col < a.width) acc[r][j][e] = slot[(long long)row * a.width + col];
+        }
+  }
+  product<S, HALF, false, true>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0, memory, acc);
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
 #pragma unroll
@@ -654,10 +786,7 @@ __global__ __launch_bounds__(S::THREADS) void hidden_grad_kernel(HiddenArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
-        if (row < a.rows && col < a.width) {
-          float& to = slot[(long long)row * a.width + col];
-          to = a.first ? acc[r][j][e] : to + acc[r][j][e];
-        }
+        if (row < a.rows && col < a.width) slot[(long long)row * a.width + col] = acc[r][j][e];
       }
 }
 // Slots in their order, and what the label's value lost, for the rows that belong to somebody.
@@ -701,19 +830,34 @@ struct WeightArgs {
   const int32_t* offsets;
   const GradScale* scale;
   const unsigned* columns;   // largest values of the columns of h that have been scaled by column_power(), or nullptr
-  float* dweight;        // at the piece's first value
-  long long ldw;
+  float *dweight, *dbias;   // at the piece's first value; each may be nullptr
+  long long ldw, ldb;
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS) void head_weight_grad_kernel(WeightArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_grad_kernel(WeightArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
   const int g = blockIdx.y, begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
   f32x16 acc[S::FM][S::FN] = {};
-  product<S, HALF, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, end > begin ? end - begin : 0, memory, acc);
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, length = end > begin ? end - begin : 0;
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
   const float down = HALF ? a.scale->down : 1.f;
+  if (a.dbias != nullptr && t.n == 0) {
+    f32x16 sums[S::FM / S::WN] = {};
+    product<S, HALF, true, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, 0, begin, length, memory, acc, sums);
+    if (lane % 32 == 0) {
+#pragma unroll
+      for (int r = 0; r < S::FM / S::WN; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int row = row0 + 32 * (S::WN * r + wave / S::WM) + row_of(e, lane);
+          if (row < a.values) a.dbias[g * a.ldb + row] = sums[r][e] * down;
+        }
+    }
+  } else {
+    product<S, HALF, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length, memory, acc);
+  }
+  if (a.dweight == nullptr) return;
   float* dw = a.dweight + g * a.ldw;
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
@@ -727,41 +871,6 @@ __global__ __launch_bounds__(S::THREADS) void head_weight_grad_kernel(WeightArgs
         const int row = row0 + 32 * r + row_of(e, lane);
         if (row < a.values) dw[(long long)row * a.width + col] = acc[r][j][e] * down * back;
       }
-  }
-}
-
-// db of a piece: 512 values a workgroup, every wave some of the group's tokens.
-constexpr int kBiasWaves = 8;
-template <bool HALF, int P>
-__global__ __launch_bounds__(64 * kBiasWaves) void head_bias_grad_kernel(const u16* dz, long long ldz, long long plane, int rows, int values,
-                                                                        const int32_t* offsets, const GradScale* scale, float* dbias, long long ldb) {
-  __shared__ float shared[kBiasWaves][512];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, g = blockIdx.y;
-  const int begin = group_offset(offsets, g, rows), end = group_offset(offsets, g + 1, rows);
-  const int col = blockIdx.x * 512 + 8 * lane;
-  float sum[8] = {};
-  if (col < ldz) {
-    for (long long t = begin + wave; t < end; t += kBiasWaves) {
-#pragma unroll
-      for (int p = P - 1; p >= 0; --p) {
-        const s16x8 raw = *reinterpret_cast<const s16x8*>(dz + p * plane + t * ldz + col);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const short bits = raw[j];
-          sum[j] += HALF ? (float)__builtin_bit_cast(_Float16, bits) : __uint_as_float((unsigned)(u16)bits << 16);
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) shared[wave][8 * lane + j] = sum[j];
-  __syncthreads();
-  const float down = HALF ? scale->down : 1.f;
-  const int at = blockIdx.x * 512 + threadIdx.x;
-  if (at < values) {
-    float s = shared[0][threadIdx.x];
-    for (int w = 1; w < kBiasWaves; ++w) s += shared[w][threadIdx.x];
-    dbias[g * ldb + at] = s * down;
   }
 }
 
@@ -946,7 +1055,9 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
     }
     const JoinArgs j = {s.part, s.part_u, s.label_logit, l.labels, slices, rows, a.vocab, a.logp == nullptr ? nullptr : a.logp + t0,
                         a.entropy == nullptr ? nullptr : a.entropy + t0, a.stats == nullptr ? nullptr : a.stats + 2 * (size_t)t0};
-    logit_join_kernel<<<(unsigned)ceil_div(rows, 64), 64 * kJoinWaves, 0, stream>>>(j);
+    int tokens = 1;   // a workgroup for every compute unit, up to whole memory lines
+    while (tokens < 64 && rows / (2 * tokens) >= 256) tokens *= 2;
+    logit_join_kernel<<<(unsigned)ceil_div(rows, tokens), kJoinThreads, 0, stream>>>(j, tokens);
     ZENO_STEP(hipGetLastError());
   }
   return hipSuccess;
@@ -963,7 +1074,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const bool half = a.dtype == ZENO_F16;
   const int planes = planes_of(a.dtype);
   GradScale* scale = reinterpret_cast<GradScale*>(ws + p.scale);
-  const bool convert = a.dtype == ZENO_BF16 && a.dweight != nullptr && a.rows > 0;
+  const bool convert = a.dtype == ZENO_BF16 && (a.dweight != nullptr || a.dbias != nullptr) && a.rows > 0;
   unsigned* columns = reinterpret_cast<unsigned*>(ws + p.columns);
   grad_scale_kernel<<<1, 1024, 0, stream>>>(a.grad_logp, a.grad_entropy, a.labels, a.rows, planes == 1 ? 1 : 0, scale, columns, convert ? a.width : 0);
   ZENO_STEP(hipGetLastError());
@@ -1026,7 +1137,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         else ZENO_STEP(half ? (start_hidden<MidTile, true>(h, p.splits, stream)) : (start_hidden<MidTile, false>(h, p.splits, stream)));
       }
     }
-    if (a.dweight != nullptr) {
+    if (a.dweight != nullptr || a.dbias != nullptr) {
       WeightArgs w = {};
       w.dz = {fine_dz, d.ldz, d.plane, p.piece};
       w.h = hidden;
@@ -1035,25 +1146,18 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       w.columns = convert ? columns : nullptr;
       const int tile = p.wide_weight ? 256 : 128;
       w.tiles_m = ceil_div(values, tile);
-      w.tiles_n = ceil_div(a.width, tile);
+      w.tiles_n = a.dweight != nullptr ? ceil_div(a.width, tile) : 1;   // (the first ones take the bias's along)
       w.rows = a.rows;
       w.width = a.width;
       w.values = values;
       w.offsets = a.offsets;
       w.scale = scale;
-      w.dweight = a.dweight + (long long)v0 * a.width;
+      w.dweight = a.dweight != nullptr ? a.dweight + (long long)v0 * a.width : nullptr;
+      w.dbias = a.dbias != nullptr ? a.dbias + v0 : nullptr;
       w.ldw = a.ldg;
+      w.ldb = a.ldb;
       if (p.wide_weight) ZENO_STEP(planes == 1 ? (start_weight<WideTile, true>(w, a.m, stream)) : (start_weight<WideTile, false>(w, a.m, stream)));
       else ZENO_STEP(planes == 1 ? (start_weight<MidTile, true>(w, a.m, stream)) : (start_weight<MidTile, false>(w, a.m, stream)));
-    }
-    if (a.dbias != nullptr) {
-      const dim3 grid((unsigned)ceil_div(values, 512), a.m);
-      float* db = a.dbias + v0;
-      if (planes == 3)
-        head_bias_grad_kernel<false, 3><<<grid, 64 * kBiasWaves, 0, stream>>>(d.dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
-      else
-        head_bias_grad_kernel<true, 2><<<grid, 64 * kBiasWaves, 0, stream>>>(fine_dz, d.ldz, d.plane, a.rows, values, a.offsets, scale, db, a.ldb);
-      ZENO_STEP(hipGetLastError());
     }
   }
   if (a.dhidden != nullptr && a.rows > 0) {
