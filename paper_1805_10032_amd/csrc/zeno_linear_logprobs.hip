@@ -270,7 +270,7 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
   product<S, HALF, A_ACROSS, B_ACROSS, false>(a, b, pairs, m0, n0, first, length, memory, acc, none);
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // What the logits' kernels share: A = rows of W from the vocabulary's `v0` on, B = h.
@@ -285,27 +285,28 @@ struct LogitArgs {
 // Row of a wave's 32 x 32 block that element e of a lane holds.
 __device__ inline int row_of(int e, int lane) { return 8 * (e / 4) + 4 * (lane / 32) + e % 4; }
 
-// The bias of a wave's rows from v on; what lies behind the vocabulary gets -inf, whatever its logit (a copy of the last row's, or finite).
+// The bias of a wave's rows from v on.  What lies behind the vocabulary gets -inf: its products are copies of the last row's, so this makes a NaN of
+// none that is not there.
 template <typename S>
 struct Bias {
   float b[S::FM][16];
-  bool whole;
 };
 template <typename S>
 __device__ inline void load_bias(const LogitArgs& a, int v, int lane, Bias<S>& o) {
-  o.whole = v + 32 * S::FM <= a.vocab;
+  const bool whole = v + 32 * S::FM <= a.vocab;
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int at = v + 32 * r + row_of(4 * q, lane);
       f32x4 raw = {0.f, 0.f, 0.f, 0.f};
-      if (a.bias != nullptr) {
-        if (o.whole) {
-          raw = *reinterpret_cast<const f32x4_a4*>(a.bias + at);
-        } else {
+      if (whole) {
+        if (a.bias != nullptr) raw = *reinterpret_cast<const f32x4_a4*>(a.bias + at);
+      } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) raw[i] = at + i < a.vocab ? a.bias[at + i] : 0.f;
+        for (int i = 0; i < 4; ++i) {
+          if (at + i >= a.vocab) raw[i] = -__builtin_inff();
+          else if (a.bias != nullptr) raw[i] = a.bias[at + i];
         }
       }
 #pragma unroll
@@ -314,20 +315,14 @@ __device__ inline void load_bias(const LogitArgs& a, int v, int lane, Bias<S>& o
 }
 // A block of 32 tokens' logits.
 template <typename S>
-__device__ inline void logits_of(const LogitArgs& a, int v, int lane, const Bias<S>& bias, const f32x16 (&acc)[S::FM][S::FN], int j,
-                                 float (&z)[S::FM][16]) {
+__device__ inline void logits_of(const Bias<S>& bias, const f32x16 (&acc)[S::FM][S::FN], int j, float (&z)[S::FM][16]) {
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
 #pragma unroll
     for (int e = 0; e < 16; ++e) z[r][e] = acc[r][j][e] + bias.b[r][e];
-  if (!bias.whole) {
-#pragma unroll
-    for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (v + 32 * r + row_of(e, lane) >= a.vocab) z[r][e] = -__builtin_inff();
-  }
 }
+// exp(z - x) as 2^(L z - c) 2^(c - L x), c = L x rounded: one FMA a value, and the second factor once.  Beyond kNear that factor says nothing.
+constexpr float kNear = 0x1p20f;
 
 // ---- forward: for each token and each slice of 32 FM values (max, sum of exp(z - max)) and, for the entropy, the sum of exp(z - max) (z - max)
 struct StatArgs {
@@ -341,21 +336,24 @@ template <typename S, bool HALF>
 __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_kernel(StatArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int v = a.l.v0 + t.m * S::BM + (wave % S::WM) * (32 * S::FM), token0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
+  Bias<S> bias;   // (these arrive beside the operands)
+  load_bias<S>(a.l, v, lane, bias);
+  int label[S::FN];
+#pragma unroll
+  for (int j = 0; j < S::FN; ++j) label[j] = a.l.labels != nullptr && token0 + 32 * j < a.l.rows ? a.l.labels[token0 + 32 * j] : -1;
   f32x16 acc[S::FM][S::FN] = {};
   product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int v = a.l.v0 + t.m * S::BM + (wave % S::WM) * (32 * S::FM);
-  Bias<S> bias;
-  load_bias<S>(a.l, v, lane, bias);
   const int slice = a.slice0 + t.m * S::WM + wave % S::WM;
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
-    const int token = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + 32 * j + lane % 32;
+    const int token = token0 + 32 * j;
     const bool live = token < a.l.rows;
-    const int hit = live && a.l.labels != nullptr ? a.l.labels[token] - v : -1;
+    const int hit = label[j] - v;
     float z[S::FM][16];
-    logits_of<S>(a.l, v, lane, bias, acc, j, z);
+    logits_of<S>(bias, acc, j, z);
     float top = -__builtin_inff();
 #pragma unroll
     for (int r = 0; r < S::FM; ++r)
@@ -363,24 +361,44 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_
       for (int e = 0; e < 16; ++e) top = fmaxf(top, z[r][e]);
     top = fmaxf(top, __shfl_xor(top, 32));
     const float from = top == -__builtin_inff() ? 0.f : top;
-    float s = 0.f, u = 0.f;
-    if (a.part_u == nullptr) {
+    float s, u = 0.f;
+    {
+      const float c = from * kLog2e, off = -fmaf(from, kLog2e, -c), scale = __builtin_amdgcn_exp2f(off);
+      float part[2] = {};
+      if (a.part_u == nullptr) {
 #pragma unroll
-      for (int r = 0; r < S::FM; ++r)
+        for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s += exp_fast(z[r][e] - from);
-    } else {
+          for (int e = 0; e < 16; ++e) part[e % 2] += __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c));
+      } else {
+#pragma unroll
+        for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {   // (where the exponential is 0, its argument is cut off: 0 * -inf would be NaN)
+            const float d = fmaf(z[r][e], kLog2e, -c), x = __builtin_amdgcn_exp2f(d);
+            part[e % 2] += x;
+            u = fmaf(x, fmaxf(d, -256.f), u);
+          }
+        u = fmaf(off, part[0] + part[1], u) * (scale * kLn2);
+      }
+      s = (part[0] + part[1]) * scale;
+    }
+    const bool far = !(fabsf(from) <= kNear);
+    if (__any(far)) {   // (for these tokens alone: another token's logits do not show)
+      float far_s = 0.f, far_u = 0.f;
 #pragma unroll
       for (int r = 0; r < S::FM; ++r)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float d = z[r][e] - from, x = exp_fast(d);
-          s += x;
-          u += x > 0.f ? x * d : 0.f;
+          far_s += x;
+          far_u += x > 0.f ? x * d : 0.f;
         }
-      u += __shfl_xor(u, 32);
+      s = far ? far_s : s;
+      u = far ? far_u : u;
     }
     s += __shfl_xor(s, 32);
+    if (a.part_u != nullptr) u += __shfl_xor(u, 32);
     if (live && lane < 32) {
       const long long at = (long long)slice * a.l.rows + token;
       a.part[at] = make_float2(top, s);
@@ -398,7 +416,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_
             mine_z = z[r][e];
             mine = true;
           }
-      if (here && mine) a.label_logit[token] = mine_z;
+      if (here && mine && live) a.label_logit[token] = mine_z;
     }
   }
 }
@@ -638,41 +656,49 @@ template <typename S, bool HALF, Planes P>
 __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_kernel(DzArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
-  f32x16 acc[S::FM][S::FN] = {};
-  product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN), v = a.l.v0 + t.m * S::BM + wm;
-  Bias<S> bias;
+  Bias<S> bias;   // (these arrive beside the operands)
   load_bias<S>(a.l, v, lane, bias);
+  float stat[S::FN][2], grad[S::FN][3];   // max and logarithm of the sum; gradients of logp and entropy, entropy
+  int label[S::FN];
+#pragma unroll
+  for (int j = 0; j < S::FN; ++j) {
+    const int token = t.n * S::BN + wn + 32 * j + lane % 32;
+    stat[j][0] = -__builtin_inff();
+    stat[j][1] = grad[j][0] = grad[j][1] = grad[j][2] = 0.f;
+    label[j] = -1;
+    if (token < a.l.rows) {
+      stat[j][0] = a.stats[2 * token];
+      stat[j][1] = a.stats[2 * token + 1];
+      if (a.grad_logp != nullptr) {
+        label[j] = a.l.labels[token];
+        grad[j][0] = a.grad_logp[token];
+      }
+      if (a.grad_entropy != nullptr) {
+        grad[j][1] = a.grad_entropy[token];
+        grad[j][2] = a.entropy[token];
+      }
+    }
+  }
   const float up = P == kBf16Three ? 1.f : a.scale->up;
+  f32x16 acc[S::FM][S::FN] = {};
+  product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
-    const int token = t.n * S::BN + wn + 32 * j + lane % 32;
-    float M = 0.f, log_s = __builtin_inff(), g = 0.f, q = 0.f, H = 0.f;
-    int y = -1;
-    bool empty = true;
-    if (token < a.l.rows) {
-      M = a.stats[2 * token];
-      log_s = a.stats[2 * token + 1];
-      empty = M == -__builtin_inff() && log_s == 0.f;
-      if (a.grad_logp != nullptr) {
-        y = a.l.labels[token];
-        if (y != -1) g = y >= 0 && y < a.l.vocab ? a.grad_logp[token] : __builtin_nanf("");
-      }
-      if (a.grad_entropy != nullptr) {
-        q = a.grad_entropy[token];
-        H = a.entropy[token];
-      }
-    }
+    const int token = t.n * S::BN + wn + 32 * j + lane % 32, y = label[j];
+    float M = stat[j][0], log_s = stat[j][1];
+    const bool empty = M == -__builtin_inff() && log_s == 0.f;
+    const float g = y == -1 ? 0.f : (y >= 0 && y < a.l.vocab ? grad[j][0] : __builtin_nanf(""));
     if (empty) {
       M = 0.f;
       log_s = __builtin_inff();   // every probability is 0
     }
     float z[S::FM][16];
-    logits_of<S>(a.l, v, lane, bias, acc, j, z);
+    logits_of<S>(bias, acc, j, z);
     if (a.grad_entropy != nullptr) {
-      const float base = fmaf(q, H, g);
+      const float q = grad[j][1], base = fmaf(q, grad[j][2], g);
 #pragma unroll
       for (int r = 0; r < S::FM; ++r)
 #pragma unroll
@@ -682,18 +708,21 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
           z[r][e] = -exp_fast(lp) * fmaf(q, fmaxf(lp, -256.f), base) * up;
         }
     } else {
-      const float base = -g * up;   // (a power of two)
+      const bool far = empty || !(fabsf(M) <= kNear);
+      const float c = fmaf(log_s, kLog2e, M * kLog2e), plain = -g * up;   // (up: a power of two)
+      const float base = plain * __builtin_amdgcn_exp2f(-fmaf(log_s, kLog2e, fmaf(M, kLog2e, -c)));
+      if (!__any(far)) {
 #pragma unroll
-      for (int r = 0; r < S::FM; ++r)
+        for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[r][e] = exp_fast((z[r][e] - M) - log_s) * base;
-    }
-    if (!bias.whole) {
+          for (int e = 0; e < 16; ++e) z[r][e] = __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c)) * base;
+      } else {   // (for these tokens alone: another token's logits do not show)
 #pragma unroll
-      for (int r = 0; r < S::FM; ++r)
+        for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (v + 32 * r + row_of(e, lane) >= a.l.vocab) z[r][e] = 0.f;   // (NaN, where g is)
+          for (int e = 0; e < 16; ++e)
+            z[r][e] = far ? exp_fast((z[r][e] - M) - log_s) * plain : __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c)) * base;
+      }
     }
     const int hit = y < a.l.vocab ? y - v : -1;
     if (__any(hit >= 0 && hit < 32 * S::FM)) {
