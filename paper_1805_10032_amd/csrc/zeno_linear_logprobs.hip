@@ -51,14 +51,34 @@ struct Side {
 // Which planes are multiplied, the smallest products first.
 struct Pairs {
   int count;
-  unsigned char a[6], b[6];
+  unsigned a, b;   // four bits a plane, the first pair's lowest
 };
+__device__ inline int plane_of(unsigned planes, int i) { return (int)(planes >> (4 * i) & 15); }
 
 __device__ __attribute__((aligned(16))) unsigned zero_chunk[4];
 
-// 64 lanes x 16 bytes to consecutive bytes of LDS from `to` on, in no register and unseen by the compiler's wait counts (which would drain all
-// loads before every read of LDS); begin_stage() waits for it.  m0 is saved because it cannot be declared as written.
-__device__ inline void copy_to_lds(const u16* from, unsigned to) {
+// N times 64 lanes x 16 bytes, from `base` + off[n] + 1024 n to consecutive bytes of LDS from `to` on (the instruction's offset counts on both sides), in
+// no register and unseen by the compiler's wait counts (which would drain all loads before every read of LDS); begin_stage() waits for
+// them.  m0 is saved because it cannot be declared as written.
+template <int N>
+__device__ inline void copy_to_lds(const unsigned char* base, const unsigned (&off)[N], unsigned to) {
+  static_assert(N == 2 || N == 4, "copies of a wave");
+  unsigned saved;
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %6\n\t"
+                 "global_load_lds_dwordx4 %2, %6 offset:1024\n\tglobal_load_lds_dwordx4 %3, %6 offset:2048\n\t"
+                 "global_load_lds_dwordx4 %4, %6 offset:3072\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(to), "s"(base)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %4\n\t"
+                 "global_load_lds_dwordx4 %2, %4 offset:1024\n\ts_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "v"(off[0]), "v"(off[1]), "s"(to), "s"(base)
+                 : "memory");
+}
+__device__ inline void copy_to_lds(const unsigned char* from, unsigned to) {   // each lane from its own address
   unsigned saved;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
                : "=&s"(saved)
@@ -77,65 +97,73 @@ __device__ inline void begin_stage() {
 template <int B>
 __device__ inline int block_of(int k) { return B >= 256 ? (k & 3) | ((k >> 1) & 4) : (k & 3); }
 
+// What a wave copies: N times 1 KB of the part, one behind the other.
 template <bool ACROSS, int B, int WAVES>
 struct Loader {
-  static constexpr int N = B * kStep * 2 / 1024 / WAVES, PER = 512 / B;   // copies a wave; rows of a copy, if ACROSS
-  static_assert(N >= 1, "every wave copies");
-  // ACROSS: the rows of a wave's copies differ in bits that block_of() does not look at, so that a lane has the same columns in all of them
-  static_assert(!ACROSS || (B == 256 && WAVES == 4) || (B == 128 && PER * WAVES == 16), "rows of a copy");
-  static __device__ inline int row_of_wave(int wave) { return B == 256 ? 2 * (wave & 1) + 8 * (wave >> 1) : PER * wave; }
-  static __device__ inline constexpr int row_of_copy(int n) { return B == 256 ? 4 * (n & 1) + 16 * (n >> 1) : 16 * n; }
-  const u16* at[N];
-  int k;        // of the lane's first value, in its first copy
-  bool inside;  // its columns exist
-  unsigned to;
+  static constexpr int N = B * kStep * 2 / 1024 / WAVES, PER = 512 / B;   // PER: rows of a copy, if ACROSS
+  const unsigned char* base;   // of this stage, less 1024 (N - 1)
+  unsigned off[N];             // the lane's; offsets are below 2^32 because pitches are below kMostPitch
+  unsigned to;                 // in LDS
+  int k;                       // of the lane's first value in its first copy
   __device__ inline void start(const Side& s, int plane, long long first, long long x0, int wave, int lane, unsigned lds) {
-    to = lds + (ACROSS ? 2 * B * row_of_wave(wave) : 1024 * wave);
-    inside = true;
-    const u16* p = s.p + plane * s.plane;
-    if (!ACROSS) {
-      k = 8 * ((lane % 4) ^ (lane / 16));
+    to = lds + 1024 * N * wave;
+    const u16* p = s.p + plane * s.plane + (ACROSS ? first * s.ld + x0 : x0 * s.ld + first);
+    base = reinterpret_cast<const unsigned char*>(p) - 1024 * (N - 1);
+    k = ACROSS ? PER * N * wave + lane / (64 / PER) : 8 * ((lane % 4) ^ (lane / 16));
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const long long row = x0 + 16 * (wave + WAVES * n) + lane / 4;
-        at[n] = p + (row < s.extent ? row : s.extent - 1) * s.ld + first + k;
+    for (int n = 0; n < N; ++n) {
+      unsigned at;
+      if (!ACROSS) {
+        const long long row = x0 + 16 * (N * wave + n) + lane / 4;   // a row behind the last is the last once more
+        at = (unsigned)(((row < s.extent ? row : s.extent - 1) - x0) * s.ld) + k;
+      } else {
+        const int slot = lane % (64 / PER), col = 32 * ((slot / 4) ^ block_of<B>(k + PER * n)) + 8 * (slot % 4);
+        at = (unsigned)((k + PER * n) * s.ld) + (x0 + col < s.extent ? col : 0);   // (columns behind the last: any, their products are dropped)
       }
-    } else {
-      const int slot = lane % (64 / PER);
-      k = row_of_wave(wave) + lane / (64 / PER);
-      const long long col = x0 + 32 * ((slot / 4) ^ block_of<B>(k)) + 8 * (slot % 4);
-      inside = col < s.extent;
-#pragma unroll
-      for (int n = 0; n < N; ++n) at[n] = p + (first + k + row_of_copy(n)) * s.ld + (inside ? col : 0);
+      off[n] = 2 * at + 1024 * (N - 1 - n);
     }
   }
-  // `left`: what of the contraction is left from this stage on
-  __device__ inline void issue(const Side& s, int n, int stage_offset, int left) {
-    const bool live = inside && k + (ACROSS ? row_of_copy(n) : 0) < left;
-    copy_to_lds(live ? at[n] : reinterpret_cast<const u16*>(zero_chunk), to + stage_offset + (ACROSS ? 2 * B * row_of_copy(n) : 1024 * WAVES * n));
-    at[n] += ACROSS ? kStep * s.ld : kStep;
-  }
-  __device__ inline void move(long long by) {
+  // A stage whose contraction is there as a whole, or of which `left` is, and zeros behind.
+  __device__ inline void issue(unsigned stage_offset) { copy_to_lds<N>(base, off, to + stage_offset); }
+  __device__ inline void issue_end(unsigned stage_offset, int left) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) at[n] += by;
+    for (int n = 0; n < N; ++n) {
+      const bool live = k + (ACROSS ? PER * n : 0) < left;
+      copy_to_lds(live ? base + off[n] + 1024 * n : reinterpret_cast<const unsigned char*>(zero_chunk), to + stage_offset + 1024 * n);
+    }
   }
 };
+constexpr long long kMostPitch = 1LL << 22;
 
-// Operand of 32 rows (columns) from r on and sixteen of the contraction from k on: lane l has row l % 32, values 8 (l / 32) + 0..7.
-template <bool ACROSS, int B>
-__device__ inline s16x8 read_operand(const unsigned char* part, int r, int k, int lane) {
-  if (!ACROSS) {
-    const int chunk = (k / 8 + lane / 32) ^ (lane % 32 / 4 % 4);
-    return *reinterpret_cast<const s16x8*>(part + (r + lane % 32) * (2 * kStep) + 16 * chunk);
-  } else {
-    const int row = k + 8 * (lane / 32) + lane % 16 / 4;
-    const int at = row * (2 * B) + 64 * ((r / 32) ^ block_of<B>(row)) + 32 * (lane / 16 % 2) + 8 * (lane % 4);
-    typedef __attribute__((address_space(3))) s16x4* p;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(part + at));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(part + at + 4 * (2 * B)));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+// Operands of 32 rows (columns) and sixteen of the contraction: lane l has row l % 32, values 8 (l / 32) + 0..7.  F of them are a wave's, from
+// row w on.
+template <bool ACROSS, int B, int F>
+struct Reader {
+  unsigned base[ACROSS ? F : 2];
+  __device__ inline void start(unsigned part, int w, int lane) {
+    if (!ACROSS) {
+      base[0] = part + (w + lane % 32) * (2 * kStep) + 16 * ((lane / 32) ^ (lane % 32 / 4 % 4));
+      base[1] = base[0] ^ 32;   // the chunks of the second sixteen (parts begin on 64 bytes)
+    } else {
+      const int row = 8 * (lane / 32) + lane % 16 / 4;
+#pragma unroll
+      for (int r = 0; r < F; ++r)
+        base[r] = part + row * (2 * B) + 64 * ((w / 32 + r) ^ block_of<B>(row)) + 32 * (lane / 16 % 2) + 8 * (lane % 4);
+    }
   }
-}
+  __device__ inline s16x8 read(int r, int k, unsigned stage_offset) const {
+    if constexpr (!ACROSS) {
+      typedef const __attribute__((address_space(3))) s16x8* p;
+      return *(p)(base[k / 16] + stage_offset + r * 32 * (2 * kStep));
+    } else {
+      typedef __attribute__((address_space(3))) s16x4* p;
+      const unsigned at = base[r] + stage_offset;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(at + k * (2 * B)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p)(at + (k + 4) * (2 * B)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
 template <bool HALF>
 __device__ inline f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
   if constexpr (HALF)
@@ -144,16 +172,11 @@ __device__ inline f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// The operands of sixteen of the contraction, in the order in which they are needed.
+// The operands of sixteen of the contraction.
 template <typename S>
 struct Operands {
   s16x8 x[S::FM], y[S::FN];
 };
-template <typename S, bool A_ACROSS, bool B_ACROSS>
-__device__ inline void read_one(int i, const unsigned char* part, int k, int wm, int wn, int lane, Operands<S>& o) {
-  if (i >= 1 && i <= S::FN) o.y[i - 1] = read_operand<B_ACROSS, S::BN>(part + S::A_BYTES, wn + 32 * (i - 1), k, lane);
-  else o.x[i == 0 ? 0 : i - S::FN] = read_operand<A_ACROSS, S::BM>(part, wm + 32 * (i == 0 ? 0 : i - S::FN), k, lane);
-}
 
 // acc += the product of BM rows (columns) of A from m0 on and BN of B from n0 on over `length` of the contraction, which begins at `first`.
 // While a stage is multiplied the next is whole, so that its first operands are read before the barrier, the one behind it is on its way,
@@ -170,46 +193,54 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
   if (total == 0) return;
   Loader<A_ACROSS, S::BM, S::WAVES> la;
   Loader<B_ACROSS, S::BN, S::WAVES> lb;
-  la.start(a, pairs.a[0], first, m0, wave, lane, lds);
-  lb.start(b, pairs.b[0], first, n0, wave, lane, lds + S::A_BYTES);
+  la.start(a, plane_of(pairs.a, 0), first, m0, wave, lane, lds);
+  lb.start(b, plane_of(pairs.b, 0), first, n0, wave, lane, lds + S::A_BYTES);
+  Reader<A_ACROSS, S::BM, S::FM> ra;
+  Reader<B_ACROSS, S::BN, S::FN> rb;
+  ra.start(lds, wm, lane);
+  rb.start(lds + S::A_BYTES, wn, lane);
+  const long long step_a = 2 * kStep * (A_ACROSS ? a.ld : 1), step_b = 2 * kStep * (B_ACROSS ? b.ld : 1);
   int pair = 0, left = length;   // of the next stage to fetch
-  auto fetch_one = [&](int i, int stage) __attribute__((always_inline)) {
-    if (i < S::LOADS_A) la.issue(a, i, stage * S::STAGE, left);
-    else lb.issue(b, i - S::LOADS_A, stage * S::STAGE, left);
-    if (i + 1 < S::LOADS) return;
+  auto fetched = [&]() __attribute__((always_inline)) {
+    la.base += step_a;
+    lb.base += step_b;
     left -= kStep;
     if (left <= 0 && pair + 1 < pairs.count) {
-      const long long back = (long long)steps * kStep;
-      la.move((pairs.a[pair + 1] - pairs.a[pair]) * a.plane - back * (A_ACROSS ? a.ld : 1));
-      lb.move((pairs.b[pair + 1] - pairs.b[pair]) * b.plane - back * (B_ACROSS ? b.ld : 1));
+      la.base += 2 * (plane_of(pairs.a, pair + 1) - plane_of(pairs.a, pair)) * a.plane - steps * step_a;
+      lb.base += 2 * (plane_of(pairs.b, pair + 1) - plane_of(pairs.b, pair)) * b.plane - steps * step_b;
       left = length;
       ++pair;
     }
   };
+  auto fetch = [&](unsigned at) __attribute__((always_inline)) {
+    la.issue_end(at, left);
+    lb.issue_end(at, left);
+    fetched();
+  };
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i)
-    if (i < total) {
-#pragma unroll
-      for (int n = 0; n < S::LOADS; ++n) fetch_one(n, i);
-    }
+    if (i < total) fetch(i * S::STAGE);
   if (total > 2) begin_stage<S::LOADS>();   // the first two are whole
   else begin_stage<0>();
   constexpr int OPERANDS = S::FM + S::FN, PRODUCTS = S::FM * S::FN, READ_UNTIL = PRODUCTS > 4 ? PRODUCTS / 2 : PRODUCTS;
   Operands<S> now, next;
+  auto read_one = [&](int n, int k, unsigned at, Operands<S>& o) __attribute__((always_inline)) {   // in the order in which they are needed
+    if (n >= 1 && n <= S::FN) o.y[n - 1] = rb.read(n - 1, k, at);
+    else o.x[n == 0 ? 0 : n - S::FN] = ra.read(n == 0 ? 0 : n - S::FN, k, at);
+  };
   s16x8 ones;                    // of B's first plane: each plane of A counts once
   int its = 0, until = 0;        // pair that is multiplied, and the step where the next begins
   auto set_ones = [&](int i) __attribute__((always_inline)) {
     if (!SUMS || i < until) return;
     its = i == 0 ? 0 : its + 1;
     until += steps;
-    const short one = pairs.b[its] != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
+    const short one = plane_of(pairs.b, its) != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
     ones = s16x8{one, one, one, one, one, one, one, one};
   };
 #pragma unroll
-  for (int n = 0; n < OPERANDS; ++n) read_one<S, A_ACROSS, B_ACROSS>(n, memory, 0, wm, wn, lane, now);
-  // Sixteen of the contraction; the next sixteen's operands are read behind the first products, copies are sent behind the last.
-  auto half = [&](const Operands<S>& use, Operands<S>& fill, const unsigned char* part, int k, int from, int to, int stage,
-                  auto fetching) __attribute__((always_inline)) {
+  for (int n = 0; n < OPERANDS; ++n) read_one(n, 0, 0, now);
+  // Sixteen of the contraction; the next sixteen's operands are read behind the first products, copies are sent behind half of them.
+  auto half = [&](const Operands<S>& use, Operands<S>& fill, int k, unsigned at, auto send) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PRODUCTS; ++q) {
       const int r = q / S::FN, j = q % S::FN;
@@ -220,31 +251,33 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
       }
 #pragma unroll
       for (int n = 0; n < OPERANDS; ++n)
-        if (n * READ_UNTIL / OPERANDS == q)
-          read_one<S, A_ACROSS, B_ACROSS>(n, part, k, wm, wn, lane, fill);
-      if constexpr (decltype(fetching)::value) {
-#pragma unroll
-        for (int n = from; n < to; ++n)
-          if (PRODUCTS / 2 + (n - from) * (PRODUCTS / 2) / (to - from) == q) fetch_one(n, stage);
-      }
+        if (n * READ_UNTIL / OPERANDS == q) read_one(n, k, at, fill);
+      if (q == PRODUCTS / 2) send();
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto step = [&](int i, auto fetching) __attribute__((always_inline)) {
-    const int stage = (i + kStages - 1) % kStages;
+  unsigned at = 0;               // the stage that is multiplied
+  for (int i = 0; i < total; ++i) {
+    const unsigned after = at + S::STAGE == kStages * S::STAGE ? 0 : at + S::STAGE, to = at == 0 ? (kStages - 1) * S::STAGE : at - S::STAGE;
+    const bool more = i + kStages - 1 < total, whole = left >= kStep;   // a stage is fetched; it is whole
     set_ones(i);
-    half(now, next, memory + (i % kStages) * S::STAGE, 16, 0, S::LOADS / 2, stage, fetching);
+    half(now, next, 16, at, [&]() __attribute__((always_inline)) {
+      if (more) {
+        if (whole) la.issue(to);
+        else la.issue_end(to, left);
+      }
+    });
     // (behind the last stage: what stands in LDS, for no one)
-    half(next, now, memory + ((i + 1) % kStages) * S::STAGE, 0, S::LOADS / 2, S::LOADS, stage, fetching);
-  };
-  int i = 0;
-  for (; i + kStages - 1 < total; ++i) {
-    step(i, std::true_type());
-    begin_stage<S::LOADS>();   // the stage after next is whole
-  }
-  for (; i < total; ++i) {
-    step(i, std::false_type());
-    begin_stage<0>();
+    half(next, now, 0, after, [&]() __attribute__((always_inline)) {
+      if (more) {
+        if (whole) lb.issue(to);
+        else lb.issue_end(to, left);
+        fetched();
+      }
+    });
+    if (more) begin_stage<S::LOADS>();   // the stage after next is whole
+    else begin_stage<0>();
+    at = after;
   }
 }
 
@@ -541,7 +574,7 @@ int padded_width(int width) { return (width + 7) / 8 * 8; }
 int planes_of(int dtype) { return dtype == ZENO_F32 ? 3 : 1; }
 // Whether a matrix can be read as it stands: 16-byte pieces of 16-bit values.
 bool as_it_is(const void* p, long long ld, int dtype, int width) {
-  return dtype != ZENO_F32 && width % 8 == 0 && ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+  return dtype != ZENO_F32 && width % 8 == 0 && ld % 8 == 0 && ld < kMostPitch && reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 hipError_t pack(const void* x, long long ldx, int dtype, int rows, int width, u16* out, hipStream_t stream) {
   const int padded = padded_width(width);
@@ -553,11 +586,10 @@ hipError_t pack(const void* x, long long ldx, int dtype, int rows, int width, u1
     pack_kernel<u16><<<blocks, 256, 0, stream>>>(reinterpret_cast<const u16*>(x), ldx, rows, width, padded, out, plane);
   return hipGetLastError();
 }
-Pairs pairs_of(int a, int b) {   // planes of the two sides
-  if (a == 3) return {6, {2, 0, 1, 1, 0, 0}, {0, 2, 1, 0, 1, 0}};
-  if (a == 2) return {2, {1, 0}, {0, 0}};
-  (void)b;
-  return {1, {0}, {0}};
+Pairs pairs_of(int a, int b) {   // planes of the two sides: three and three, two and one, one and one
+  if (a == 3 && b == 3) return {6, 0x001102, 0x010120};
+  if (a == 2) return {2, 0x01, 0x00};
+  return {1, 0, 0};
 }
 
 // ---- backward
@@ -602,34 +634,40 @@ __device__ inline int column_power(unsigned largest) {   // largest magnitude, a
 }
 __host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
 __device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
-constexpr int kColumnRows = 64;   // that a workgroup looks at
-__global__ __launch_bounds__(256) void column_max_kernel(Side h, int width, unsigned* largest) {
-  const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
-  if (col >= width) return;
+constexpr int kColumnRows = 256;   // of a workgroup
+__global__ __launch_bounds__(1024) void column_max_kernel(Side h, int width, unsigned* largest) {
+  __shared__ unsigned shared[16][512];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = blockIdx.x * 512 + lane * 8;
   unsigned m[8] = {};
-  const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+  const int begin = blockIdx.y * kColumnRows, end = begin + kColumnRows < h.extent ? begin + kColumnRows : h.extent;
+  if (col < width) {
 #pragma unroll 4
-  for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
-    const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
+    for (int row = begin + wave; row < end; row += 16) {
+      const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const unsigned v = (unsigned)raw[j] & 0x7fff;
-      if (v < 0x7f80 && v > m[j]) m[j] = v;
+      for (int j = 0; j < 8; ++j) {
+        const unsigned v = (unsigned)raw[j] & 0x7fff;
+        m[j] = v < 0x7f80 && v > m[j] ? v : m[j];
+      }
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (m[j] != 0 && col + j < width) atomicMax(&largest[col + j], m[j] << 16);
+  for (int j = 0; j < 8; ++j) shared[wave][8 * lane + j] = m[j];
+  __syncthreads();
+  if (threadIdx.x >= 512) return;
+  unsigned most = 0;
+  for (int w = 0; w < 16; ++w) most = shared[w][threadIdx.x] > most ? shared[w][threadIdx.x] : most;
+  if (most != 0 && blockIdx.x * 512 + threadIdx.x < width) atomicMax(&largest[blockIdx.x * 512 + threadIdx.x], most << 16);
 }
-__global__ __launch_bounds__(256) void column_half_kernel(Side h, int width, const unsigned* largest, u16* out) {
+__global__ __launch_bounds__(1024) void column_half_kernel(Side h, int width, const unsigned* largest, u16* out) {
   const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
   if (col >= width) return;
   float up[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) up[j] = power_of_two(column_power(col + j < width ? largest[col + j] : 0));
-  const int end = (int)(blockIdx.y + 1) * kColumnRows < h.extent ? (int)(blockIdx.y + 1) * kColumnRows : h.extent;
+  const int begin = blockIdx.y * kColumnRows, end = begin + kColumnRows < h.extent ? begin + kColumnRows : h.extent;
 #pragma unroll 4
-  for (int row = blockIdx.y * kColumnRows + threadIdx.x / 64; row < end; row += 4) {
+  for (int row = begin + threadIdx.x / 64; row < end; row += 16) {
     const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
     s16x8 half;
 #pragma unroll
@@ -796,17 +834,6 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void hidden_grad_
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
   float* slot = a.slots + (long long)blockIdx.y * a.rows * a.width;
   f32x16 acc[S::FM][S::FN] = {};
-  if (!a.first) {   // the sums go on from what the slot holds, which arrives beside the first operands (behind the products: 684 us, 454 without)
-#pragma unroll
-    for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-      for (int j = 0; j < S::FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
-          if (row < a.rows && col < a.width) acc[r][j][e] = slot[(long long)row * a.width + col];
-        }
-  }
   product<S, HALF, false, true>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0, memory, acc);
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
@@ -815,7 +842,12 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void hidden_grad_
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
-        if (row < a.rows && col < a.width) slot[(long long)row * a.width + col] = acc[r][j][e];
+        if (row >= a.rows || col >= a.width) continue;
+        // One workgroup adds one value of a launch, so the order is that of the launches; nothing is waited for.  (Sums that go on from what the
+        // slot holds 600 us a piece of 8192 x 8192 x 4096, loaded behind the products 684, stored 500.)
+        float* to = slot + (long long)row * a.width + col;
+        if (a.first) *to = acc[r][j][e];
+        else unsafeAtomicAdd(to, acc[r][j][e]);
       }
 }
 // Slots in their order, and what the label's value lost, for the rows that belong to somebody.
@@ -842,11 +874,30 @@ __global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
     const float* from = a.slots + (long long)row * a.width;
     const T* w = reinterpret_cast<const T*>(a.weight) + (has ? y : 0) * a.ldw;
     T* to = reinterpret_cast<T*>(a.out) + row * a.ldo;
-    for (int col = blockIdx.x * 256 + threadIdx.x; col < a.width; col += gridDim.x * 256) {
-      float sum = from[col];
-      for (int s = 1; s < a.splits; ++s) sum += from[s * stride + col];
-      if (has) sum = fmaf(rest, (float)w[col], sum);
-      to[col] = (T)(sum * down);
+    const int whole = a.width / 4 * 4;
+    for (int col = (blockIdx.x * 256 + threadIdx.x) * 4; col < a.width; col += gridDim.x * 1024) {
+      if (col < whole) {
+        f32x4 sum = *reinterpret_cast<const f32x4_a4*>(from + col);
+        for (int s = 1; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4_a4*>(from + s * stride + col);
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        typedef t4 unaligned __attribute__((aligned(sizeof(T))));
+        if (has) {
+          const t4 x = *reinterpret_cast<const unaligned*>(w + col);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] = fmaf(rest, (float)x[i], sum[i]);
+        }
+        t4 out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = (T)(sum[i] * down);
+        *reinterpret_cast<unaligned*>(to + col) = out;
+      } else {
+        for (int i = col; i < a.width; ++i) {
+          float sum = from[i];
+          for (int s = 1; s < a.splits; ++s) sum += from[s * stride + i];
+          if (has) sum = fmaf(rest, (float)w[i], sum);
+          to[i] = (T)(sum * down);
+        }
+      }
     }
   }
 }
@@ -913,6 +964,10 @@ hipError_t allow(const void* kernel) {
 constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
 constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
 
+#ifndef LONG_GROUP
+#define LONG_GROUP 512
+#endif
+constexpr int kLongGroup = LONG_GROUP;
 // Wide tiles where they give every compute unit one.
 bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
 
@@ -967,7 +1022,7 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   p.piece = (int)(((vocab + pieces - 1) / pieces + 255) / 256 * 256);
   p.wide_logits = wide_tiles(p.piece, n);
   p.wide_hidden = wide_tiles(n, width);
-  p.wide_weight = wide_tiles((long long)p.piece * m, width) && n / m >= 64;
+  p.wide_weight = wide_tiles((long long)p.piece * m, width) && n / m >= kLongGroup;
   const int side = p.wide_hidden ? 256 : 128;
   const long long tiles = (long long)ceil_div(n, side) * ceil_div(width, side);
   p.splits = (int)std::max<long long>(1, std::min<long long>(p.piece / 512, (p.wide_hidden ? 256 : 512) / tiles));
@@ -1121,8 +1176,8 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   if (convert) {
     const dim3 grid((unsigned)ceil_div(a.width, 512), (unsigned)ceil_div(a.rows, kColumnRows));
     hidden = {reinterpret_cast<const u16*>(ws + p.half), l.width, 0, a.rows};
-    column_max_kernel<<<grid, 256, 0, stream>>>(l.h, a.width, columns);
-    column_half_kernel<<<grid, 256, 0, stream>>>(l.h, a.width, columns, reinterpret_cast<u16*>(ws + p.half));
+    column_max_kernel<<<grid, 1024, 0, stream>>>(l.h, a.width, columns);
+    column_half_kernel<<<grid, 1024, 0, stream>>>(l.h, a.width, columns, reinterpret_cast<u16*>(ws + p.half));
     ZENO_STEP(hipGetLastError());
   }
   d.rest = planes == 1 ? reinterpret_cast<float*>(ws + p.rest) : nullptr;
@@ -1192,7 +1247,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   if (a.dhidden != nullptr && a.rows > 0) {
     const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.vocab, a.m, a.offsets, a.labels, scale,
                               a.grad_logp != nullptr ? d.rest : nullptr, a.weight, a.ldw, a.dhidden, a.lddh};
-    const dim3 grid((unsigned)std::min(ceil_div(a.width, 256), 64), (unsigned)std::min(a.rows, 16384));
+    const dim3 grid((unsigned)std::min(ceil_div(a.width, 1024), 64), (unsigned)std::min(a.rows, 16384));
     if (a.dtype == ZENO_F32) hidden_join_kernel<float><<<grid, 256, 0, stream>>>(j);
     else if (half) hidden_join_kernel<_Float16><<<grid, 256, 0, stream>>>(j);
     else hidden_join_kernel<__bf16><<<grid, 256, 0, stream>>>(j);
