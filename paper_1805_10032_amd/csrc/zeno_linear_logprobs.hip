@@ -26,7 +26,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
 
 constexpr int kStep = 32;      // of the contraction in a stage
-constexpr int kStages = 4;     // in LDS: one that is multiplied, three on their way
 
 // BM x BN of the product for a workgroup of WM x WN waves.
 template <int BM_, int BN_, int WM_, int WN_>
@@ -35,9 +34,12 @@ struct Tile {
   static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;   // 32 x 32 blocks of a wave
   static constexpr int A_BYTES = BM * kStep * 2, STAGE = (BM + BN) * kStep * 2;
   static constexpr int LOADS_A = A_BYTES / 1024 / WAVES, LOADS_B = BN * kStep * 2 / 1024 / WAVES, LOADS = LOADS_A + LOADS_B;
+  // stages in LDS: one that is multiplied, one that is whole, and what is on its way; with two planes of A in a stage they are longer and fewer
+  template <int PLANES> static constexpr int STAGE_OF = STAGE + (PLANES - 1) * A_BYTES;
+  template <int PLANES> static constexpr int STAGES_OF = PLANES == 1 ? 4 : 3;
   static constexpr int PITCH = BM + 8;                         // of planes of dz on their way out, [32 WN tokens][vocabulary]
-  static constexpr int LDS = kStages * STAGE;
-  static_assert(3 * 32 * WN * PITCH * 2 <= LDS, "dz on its way out");
+  template <int PLANES> static constexpr int LDS = STAGES_OF<PLANES> * STAGE_OF<PLANES>;
+  static_assert(3 * 32 * WN * PITCH * 2 <= LDS<1> && LDS<2> <= 160 * 1024, "dz on its way out; what there is");
 };
 using WideTile = Tile<256, 256, 2, 2>;
 using MidTile = Tile<128, 128, 2, 2>;
@@ -124,12 +126,13 @@ struct Loader {
     }
   }
   // A stage whose contraction is there as a whole, or of which `left` is, and zeros behind.
-  __device__ inline void issue(unsigned stage_offset) { copy_to_lds<N>(base, off, to + stage_offset); }
-  __device__ inline void issue_end(unsigned stage_offset, int left) {
+  // `further`: bytes to another plane.
+  __device__ inline void issue(long long further, unsigned stage_offset) { copy_to_lds<N>(base + further, off, to + stage_offset); }
+  __device__ inline void issue_end(long long further, unsigned stage_offset, int left) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const bool live = k + (ACROSS ? PER * n : 0) < left;
-      copy_to_lds(live ? base + off[n] + 1024 * n : reinterpret_cast<const unsigned char*>(zero_chunk), to + stage_offset + 1024 * n);
+      copy_to_lds(live ? base + further + off[n] + 1024 * n : reinterpret_cast<const unsigned char*>(zero_chunk), to + stage_offset + 1024 * n);
     }
   }
 };
@@ -173,60 +176,74 @@ __device__ inline f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
 }
 
 // The operands of sixteen of the contraction.
-template <typename S>
+template <typename S, int PLANES>
 struct Operands {
-  s16x8 x[S::FM], y[S::FN];
+  s16x8 x[PLANES][S::FM], y[S::FN];
 };
 
 // acc += the product of BM rows (columns) of A from m0 on and BN of B from n0 on over `length` of the contraction, which begins at `first`.
-// While a stage is multiplied the next is whole, so that its first operands are read before the barrier, the one behind it is on its way,
-// and the fourth is requested.  A wave of a wide tile has its SIMD to itself and issues in order: what runs beside the matrix
-// instructions stands between them.
+// While a stage is multiplied the next is whole, so that its first operands are read before the barrier; those behind it are on their way.
+// A wave of a wide tile has its SIMD to itself and issues in order: what runs beside the matrix instructions stands between them.
+// PLANES: 1, pairs of planes one after the other; 2, the first two planes of A in one stage, the second, smaller one first, each times B's first.
 // SUMS: also the sums of A's rows over the contraction, as products with ones; the WN waves that have the same rows take FM / WN blocks of them each.
-template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS, bool SUMS = false>
+template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS, int PLANES, bool SUMS>
 __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
                                unsigned char* memory, f32x16 (&acc)[S::FM][S::FN], f32x16 (&sums)[S::FM / S::WN]) {
+  constexpr int STAGE = S::template STAGE_OF<PLANES>, STAGES = S::template STAGES_OF<PLANES>, LOADS = S::LOADS + (PLANES - 1) * S::LOADS_A;
+  constexpr int OPERANDS = PLANES * S::FM + S::FN, PRODUCTS = PLANES * S::FM * S::FN, READ_UNTIL = PRODUCTS > 8 ? PRODUCTS / 2 : PRODUCTS;
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)memory;
-  const int steps = (length + kStep - 1) / kStep, total = steps * pairs.count;
+  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)memory, lds_b = lds + PLANES * S::A_BYTES;
+  const int steps = (length + kStep - 1) / kStep, total = PLANES == 1 ? steps * pairs.count : steps;
   if (total == 0) return;
   Loader<A_ACROSS, S::BM, S::WAVES> la;
   Loader<B_ACROSS, S::BN, S::WAVES> lb;
-  la.start(a, plane_of(pairs.a, 0), first, m0, wave, lane, lds);
-  lb.start(b, plane_of(pairs.b, 0), first, n0, wave, lane, lds + S::A_BYTES);
+  la.start(a, PLANES == 1 ? plane_of(pairs.a, 0) : 0, first, m0, wave, lane, lds);
+  lb.start(b, PLANES == 1 ? plane_of(pairs.b, 0) : 0, first, n0, wave, lane, lds_b);
   Reader<A_ACROSS, S::BM, S::FM> ra;
   Reader<B_ACROSS, S::BN, S::FN> rb;
   ra.start(lds, wm, lane);
-  rb.start(lds + S::A_BYTES, wn, lane);
+  rb.start(lds_b, wn, lane);
   const long long step_a = 2 * kStep * (A_ACROSS ? a.ld : 1), step_b = 2 * kStep * (B_ACROSS ? b.ld : 1);
   int pair = 0, left = length;   // of the next stage to fetch
   auto fetched = [&]() __attribute__((always_inline)) {
     la.base += step_a;
     lb.base += step_b;
     left -= kStep;
-    if (left <= 0 && pair + 1 < pairs.count) {
+    if (PLANES == 1 && left <= 0 && pair + 1 < pairs.count) {
       la.base += 2 * (plane_of(pairs.a, pair + 1) - plane_of(pairs.a, pair)) * a.plane - steps * step_a;
       lb.base += 2 * (plane_of(pairs.b, pair + 1) - plane_of(pairs.b, pair)) * b.plane - steps * step_b;
       left = length;
       ++pair;
     }
   };
-  auto fetch = [&](unsigned at) __attribute__((always_inline)) {
-    la.issue_end(at, left);
-    lb.issue_end(at, left);
-    fetched();
+  // part 0 .. PLANES - 1: a plane of A, PLANES: B
+  auto send = [&](int part, unsigned at, bool whole) __attribute__((always_inline)) {
+    if (part < PLANES) {
+      if (whole) la.issue(2 * part * a.plane, at + part * S::A_BYTES);
+      else la.issue_end(2 * part * a.plane, at + part * S::A_BYTES, left);
+    } else {
+      if (whole) lb.issue(0, at);
+      else lb.issue_end(0, at, left);
+    }
   };
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i)
-    if (i < total) fetch(i * S::STAGE);
-  if (total > 2) begin_stage<S::LOADS>();   // the first two are whole
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (i < total) {
+#pragma unroll
+      for (int part = 0; part <= PLANES; ++part) send(part, i * STAGE, false);
+      fetched();
+    }
+  if (STAGES == 4 && total > 2) begin_stage<LOADS>();   // the first two are whole
   else begin_stage<0>();
-  constexpr int OPERANDS = S::FM + S::FN, PRODUCTS = S::FM * S::FN, READ_UNTIL = PRODUCTS > 4 ? PRODUCTS / 2 : PRODUCTS;
-  Operands<S> now, next;
-  auto read_one = [&](int n, int k, unsigned at, Operands<S>& o) __attribute__((always_inline)) {   // in the order in which they are needed
-    if (n >= 1 && n <= S::FN) o.y[n - 1] = rb.read(n - 1, k, at);
-    else o.x[n == 0 ? 0 : n - S::FN] = ra.read(n == 0 ? 0 : n - S::FN, k, at);
+  Operands<S, PLANES> now, next;
+  auto read_one = [&](int n, int k, unsigned at, Operands<S, PLANES>& o) __attribute__((always_inline)) {   // in the order in which they are needed
+    if (n >= 1 && n <= S::FN) {
+      o.y[n - 1] = rb.read(n - 1, k, at);
+    } else {
+      const int i = n == 0 ? 0 : n - S::FN, plane = PLANES - 1 - i / S::FM;
+      o.x[plane][i % S::FM] = ra.read(i % S::FM, k, at + plane * S::A_BYTES);
+    }
   };
   s16x8 ones;                    // of B's first plane: each plane of A counts once
   int its = 0, until = 0;        // pair that is multiplied, and the step where the next begins
@@ -234,51 +251,53 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
     if (!SUMS || i < until) return;
     its = i == 0 ? 0 : its + 1;
     until += steps;
-    const short one = plane_of(pairs.b, its) != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
+    const short one = PLANES == 1 && plane_of(pairs.b, its) != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
     ones = s16x8{one, one, one, one, one, one, one, one};
   };
 #pragma unroll
   for (int n = 0; n < OPERANDS; ++n) read_one(n, 0, 0, now);
-  // Sixteen of the contraction; the next sixteen's operands are read behind the first products, copies are sent behind half of them.
-  auto half = [&](const Operands<S>& use, Operands<S>& fill, int k, unsigned at, auto send) __attribute__((always_inline)) {
+  // Sixteen of the contraction; the next sixteen's operands are read behind the first products.
+  auto half = [&](const Operands<S, PLANES>& use, Operands<S, PLANES>& fill, int k, unsigned at, auto beside) __attribute__((always_inline)) {
 #pragma unroll
     for (int q = 0; q < PRODUCTS; ++q) {
-      const int r = q / S::FN, j = q % S::FN;
-      acc[r][j] = multiply<HALF>(use.x[r], use.y[j], acc[r][j]);
+      const int plane = PLANES - 1 - q / (S::FM * S::FN), r = q / S::FN % S::FM, j = q % S::FN;
+      acc[r][j] = multiply<HALF>(use.x[plane][r], use.y[j], acc[r][j]);
       if (SUMS && j == S::FN - 1 && r % S::WN == S::WN - 1) {
         static_assert(S::WN == 2, "two waves have the same rows");
-        sums[r / 2] = multiply<HALF>(wave / S::WM == 0 ? use.x[r - 1] : use.x[r], ones, sums[r / 2]);
+        sums[r / 2] = multiply<HALF>(wave / S::WM == 0 ? use.x[plane][r - 1] : use.x[plane][r], ones, sums[r / 2]);
       }
 #pragma unroll
       for (int n = 0; n < OPERANDS; ++n)
         if (n * READ_UNTIL / OPERANDS == q) read_one(n, k, at, fill);
-      if (q == PRODUCTS / 2) send();
+      beside(q);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   unsigned at = 0;               // the stage that is multiplied
   for (int i = 0; i < total; ++i) {
-    const unsigned after = at + S::STAGE == kStages * S::STAGE ? 0 : at + S::STAGE, to = at == 0 ? (kStages - 1) * S::STAGE : at - S::STAGE;
-    const bool more = i + kStages - 1 < total, whole = left >= kStep;   // a stage is fetched; it is whole
+    const unsigned after = at + STAGE == STAGES * STAGE ? 0 : at + STAGE, to = at == 0 ? (STAGES - 1) * STAGE : at - STAGE;
+    const bool more = i + STAGES - 1 < total, whole = left >= kStep;   // a stage is fetched; it is whole
     set_ones(i);
-    half(now, next, 16, at, [&]() __attribute__((always_inline)) {
-      if (more) {
-        if (whole) la.issue(to);
-        else la.issue_end(to, left);
-      }
+    half(now, next, 16, at, [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+      for (int part = 0; part <= PLANES; ++part)
+        if (q == part * PRODUCTS / (PLANES + 1) && more) {
+          send(part, to, whole);
+          if (part == PLANES) fetched();
+        }
     });
     // (behind the last stage: what stands in LDS, for no one)
-    half(next, now, 0, after, [&]() __attribute__((always_inline)) {
-      if (more) {
-        if (whole) lb.issue(to);
-        else lb.issue_end(to, left);
-        fetched();
-      }
-    });
-    if (more) begin_stage<S::LOADS>();   // the stage after next is whole
+    half(next, now, 0, after, [](int) __attribute__((always_inline)) {});
+    if (STAGES == 4 && more) begin_stage<LOADS>();   // the stage after next is whole
     else begin_stage<0>();
     at = after;
   }
+}
+template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS>
+__device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
+                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN]) {
+  f32x16 none[S::FM / S::WN];
+  product<S, HALF, A_ACROSS, B_ACROSS, 1, false>(a, b, pairs, m0, n0, first, length, memory, acc, none);
 }
 
 // Where a workgroup's tile lies: each of the eight dies, to which workgroups go in turn, takes a run of tiles, in patches of eight rows of tiles.
@@ -294,13 +313,6 @@ __device__ inline Place place_of(unsigned id, unsigned tiles_m, unsigned tiles_n
   p.m = (int)(first + at % patch % rows);
   p.n = (int)(at % patch / rows);
   return p;
-}
-
-template <typename S, bool HALF, bool A_ACROSS, bool B_ACROSS>
-__device__ inline void product(const Side& a, const Side& b, const Pairs& pairs, long long m0, long long n0, long long first, int length,
-                               unsigned char* memory, f32x16 (&acc)[S::FM][S::FN]) {
-  f32x16 none[S::FM / S::WN];
-  product<S, HALF, A_ACROSS, B_ACROSS, false>(a, b, pairs, m0, n0, first, length, memory, acc, none);
 }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -924,7 +936,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_
   const float down = HALF ? a.scale->down : 1.f;
   if (a.dbias != nullptr && t.n == 0) {
     f32x16 sums[S::FM / S::WN] = {};
-    product<S, HALF, true, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, 0, begin, length, memory, acc, sums);
+    product<S, HALF, true, true, HALF ? 2 : 1, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, 0, begin, length, memory, acc, sums);
     if (lane % 32 == 0) {
 #pragma unroll
       for (int r = 0; r < S::FM / S::WN; ++r)
@@ -935,41 +947,50 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_
         }
     }
   } else {
-    product<S, HALF, true, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length, memory, acc);
+    f32x16 none[S::FM / S::WN];
+    product<S, HALF, true, true, HALF ? 2 : 1, false>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length, memory, acc, none);
   }
   if (a.dweight == nullptr) return;
   float* dw = a.dweight + g * a.ldw;
+  // Gradients are read when all layers have theirs: where rows are whole memory lines they go past the caches.
+  const bool past = t.m * S::BM + S::BM <= a.values && t.n * S::BN + S::BN <= a.width && a.width % 32 == 0 && on_line(dw);
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     const int col = col0 + 32 * j;
-    if (col >= a.width) continue;
-    const float back = HALF && a.columns != nullptr ? power_of_two(-column_power(a.columns[col])) : 1.f;
+    const float back = HALF && a.columns != nullptr && col < a.width ? power_of_two(-column_power(a.columns[col])) : 1.f;
+    float* to = dw + (long long)row0 * a.width + col;
+    if (past) {
 #pragma unroll
-    for (int r = 0; r < S::FM; ++r)
+      for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int row = row0 + 32 * r + row_of(e, lane);
-        if (row < a.values) dw[(long long)row * a.width + col] = acc[r][j][e] * down * back;
-      }
+        for (int e = 0; e < 16; ++e) __builtin_nontemporal_store(acc[r][j][e] * down * back, to + (long long)(32 * r + row_of(e, lane)) * a.width);
+      keep_apart();
+    } else if (col < a.width) {
+#pragma unroll
+      for (int r = 0; r < S::FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (row0 + 32 * r + row_of(e, lane) < a.values) to[(long long)(32 * r + row_of(e, lane)) * a.width] = acc[r][j][e] * down * back;
+    }
   }
 }
 
 // ---- plans
 
-template <typename S>
-hipError_t allow(const void* kernel) {
-  return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-}
+hipError_t allow(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds); }
 
 constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
 constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
 
+#ifndef WIDE_FROM
+#define WIDE_FROM 192
+#endif
 #ifndef LONG_GROUP
 #define LONG_GROUP 512
 #endif
 constexpr int kLongGroup = LONG_GROUP;
 // Wide tiles where they give every compute unit one.
-bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
+bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= WIDE_FROM; }
 
 struct Layout {
   size_t at = 0;
@@ -1042,17 +1063,17 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
 template <typename S, bool HALF>
 hipError_t start_stats(const StatArgs& a, hipStream_t stream) {
   const auto kernel = logit_stats_kernel<S, HALF>;
-  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::LDS, stream>>>(a);
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::template LDS<1>, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S, bool HALF, Planes P>
 hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
   const auto kernel = logit_grad_kernel<S, HALF, P>;
-  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::LDS, stream>>>(a);
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::template LDS<1>, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S>
@@ -1063,17 +1084,18 @@ hipError_t start_dz(const DzArgs& a, int dtype, hipStream_t stream) {
 template <typename S, bool HALF>
 hipError_t start_hidden(const HiddenArgs& a, int splits, hipStream_t stream) {
   const auto kernel = hidden_grad_kernel<S, HALF>;
-  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, S::LDS, stream>>>(a);
+  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, S::template LDS<1>, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S, bool HALF>
 hipError_t start_weight(const WeightArgs& a, int m, hipStream_t stream) {
   const auto kernel = head_weight_grad_kernel<S, HALF>;
-  const hipError_t e = allow<S>(reinterpret_cast<const void*>(kernel));
+  constexpr int lds = S::template LDS<(HALF ? 2 : 1)>;
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), lds);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, m), S::THREADS, S::LDS, stream>>>(a);
+  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, m), S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 
