@@ -370,6 +370,76 @@ __device__ inline void logits_of(const Bias<S>& bias, const f32x16 (&acc)[S::FM]
 constexpr float kNear = 0x1p20f;
 
 // ---- forward: for each token and each slice of 32 FM values (max, sum of exp(z - max)) and, for the entropy, the sum of exp(z - max) (z - max)
+// A lane's share of FM blocks of logits of one token, which lane ^ 32 has the other share of, as a slice's sums at `at`; `hit`: the label's place in the
+// slice, of which `inside` values exist.
+template <int FM>
+__device__ inline void leave_stats(const float (&z)[FM][16], int lane, int token, bool live, int hit, int inside, long long at, float2* part_s,
+                                   float* part_u, float* label_logit) {
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int r = 0; r < FM; ++r)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, z[r][e]);
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float from = top == -__builtin_inff() ? 0.f : top;
+  float s, u = 0.f;
+  {
+    const float c = from * kLog2e, off = -fmaf(from, kLog2e, -c), scale = __builtin_amdgcn_exp2f(off);
+    float part[2] = {};
+    if (part_u == nullptr) {
+#pragma unroll
+      for (int r = 0; r < FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) part[e % 2] += __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c));
+    } else {
+#pragma unroll
+      for (int r = 0; r < FM; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {   // (where the exponential is 0, its argument is cut off: 0 * -inf would be NaN)
+          const float d = fmaf(z[r][e], kLog2e, -c), x = __builtin_amdgcn_exp2f(d);
+          part[e % 2] += x;
+          u = fmaf(x, fmaxf(d, -256.f), u);
+        }
+      u = fmaf(off, part[0] + part[1], u) * (scale * kLn2);
+    }
+    s = (part[0] + part[1]) * scale;
+  }
+  const bool far = !(fabsf(from) <= kNear);
+  if (__any(far)) {   // (for these tokens alone: another token's logits do not show)
+    float far_s = 0.f, far_u = 0.f;
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float d = z[r][e] - from, x = exp_fast(d);
+        far_s += x;
+        far_u += x > 0.f ? x * d : 0.f;
+      }
+    s = far ? far_s : s;
+    u = far ? far_u : u;
+  }
+  s += __shfl_xor(s, 32);
+  if (part_u != nullptr) u += __shfl_xor(u, 32);
+  if (live && lane < 32) {
+    part_s[at] = make_float2(top, s);
+    if (part_u != nullptr) part_u[at] = u;
+  }
+  const bool here = hit >= 0 && hit < 32 * FM && hit < inside;
+  if (__any(here)) {
+    float mine_z = 0.f;
+    bool mine = false;
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (hit == 32 * r + row_of(e, lane)) {
+          mine_z = z[r][e];
+          mine = true;
+        }
+    if (here && mine && live) label_logit[token] = mine_z;
+  }
+}
+
 struct StatArgs {
   LogitArgs l;
   int slice0;            // of this launch's vocabulary
@@ -399,71 +469,121 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_
     const int hit = label[j] - v;
     float z[S::FM][16];
     logits_of<S>(bias, acc, j, z);
-    float top = -__builtin_inff();
+    leave_stats<S::FM>(z, lane, token, live, hit, a.l.vocab - v, (long long)slice * a.l.rows + token, a.part, a.part_u, a.label_logit);
+  }
+}
+
+// Few tokens: the weights are what has to be read.  A workgroup takes 32 rows of them, its four waves a share of the contraction each; operands go
+// from memory to the matrix instructions' registers, as they stand: any type, pitch and alignment.  Which values of the contraction an instruction
+// multiplies does not matter as long as both operands agree, so a lane reads 64 bytes of its row in a run.
+struct FewArgs {
+  const void *hidden, *weight;
+  long long ldh, ldw;
+  int rows, vocab, width;
+  const float* bias;
+  const int32_t* labels;
+  float2* part;          // slices of 32 values
+  float *part_u, *label_logit;
+};
+constexpr int kFewRows = 64, kFewWaves = 4;
+template <typename T>
+struct Run {   // a lane's 64 bytes of a row
+  typename Wide<T>::type v[4];
+  __device__ inline void load(const T* p) {
 #pragma unroll
-    for (int r = 0; r < S::FM; ++r)
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * Wide<T>::N);
+  }
+  __device__ inline void load_end(const T* p, int n) {   // the first n, zeros behind
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, z[r][e]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float from = top == -__builtin_inff() ? 0.f : top;
-    float s, u = 0.f;
-    {
-      const float c = from * kLog2e, off = -fmaf(from, kLog2e, -c), scale = __builtin_amdgcn_exp2f(off);
-      float part[2] = {};
-      if (a.part_u == nullptr) {
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < S::FM; ++r)
+      for (int j = 0; j < Wide<T>::N; ++j) v[i][j] = i * Wide<T>::N + j < n ? p[i * Wide<T>::N + j] : (T)0.f;
+  }
+};
+template <typename T>
+__device__ inline f32x16 multiply_run(const Run<T>& a, const Run<T>& b, f32x16 c) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) part[e % 2] += __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c));
-      } else {
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {   // (where the exponential is 0, its argument is cut off: 0 * -inf would be NaN)
-            const float d = fmaf(z[r][e], kLog2e, -c), x = __builtin_amdgcn_exp2f(d);
-            part[e % 2] += x;
-            u = fmaf(x, fmaxf(d, -256.f), u);
-          }
-        u = fmaf(off, part[0] + part[1], u) * (scale * kLn2);
-      }
-      s = (part[0] + part[1]) * scale;
-    }
-    const bool far = !(fabsf(from) <= kNear);
-    if (__any(far)) {   // (for these tokens alone: another token's logits do not show)
-      float far_s = 0.f, far_u = 0.f;
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float d = z[r][e] - from, x = exp_fast(d);
-          far_s += x;
-          far_u += x > 0.f ? x * d : 0.f;
-        }
-      s = far ? far_s : s;
-      u = far ? far_u : u;
-    }
-    s += __shfl_xor(s, 32);
-    if (a.part_u != nullptr) u += __shfl_xor(u, 32);
-    if (live && lane < 32) {
-      const long long at = (long long)slice * a.l.rows + token;
-      a.part[at] = make_float2(top, s);
-      if (a.part_u != nullptr) a.part_u[at] = u;
-    }
-    const bool here = hit >= 0 && hit < 32 * S::FM && hit + v < a.l.vocab;
-    if (__any(here)) {
-      float mine_z = 0.f;
-      bool mine = false;
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (hit == 32 * r + row_of(e, lane)) {
-            mine_z = z[r][e];
-            mine = true;
-          }
-      if (here && mine && live) a.label_logit[token] = mine_z;
+      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i][j], b.v[i][j], c, 0, 0, 0);
+    } else {
+      c = multiply<std::is_same<T, _Float16>::value>(__builtin_bit_cast(s16x8, a.v[i]), __builtin_bit_cast(s16x8, b.v[i]), c);
     }
   }
+  return c;
+}
+template <typename T, int FN>
+__global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
+  __shared__ float shared[kFewWaves][FN][16][64];
+  constexpr int RUN = 64 / (int)sizeof(T), STEP = 2 * RUN;   // of the contraction: a lane's, both halves' of a wave
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * 32;
+  const int steps = (a.width + STEP - 1) / STEP, begin = steps * wave / kFewWaves, end = steps * (wave + 1) / kFewWaves;
+  const int row = v + lane % 32 < a.vocab ? v + lane % 32 : a.vocab - 1;   // (behind the last: the last once more)
+  const T* w = reinterpret_cast<const T*>(a.weight) + row * a.ldw + lane / 32 * RUN;
+  const T* h[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int token = 32 * j + lane % 32;
+    h[j] = reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + lane / 32 * RUN;
+  }
+  f32x16 acc[FN] = {};
+  const int whole = a.width / STEP < end ? a.width / STEP : end;
+  int i = begin;
+  for (; i + 2 <= whole; i += 2) {
+    Run<T> x[2], y[2][FN];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      x[u].load(w + (i + u) * STEP);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) y[u][j].load(h[j] + (i + u) * STEP);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[j] = multiply_run<T>(x[u], y[u][j], acc[j]);
+  }
+  for (; i < end; ++i) {
+    Run<T> x, y[FN];
+    if (i < whole) {
+      x.load(w + i * STEP);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) y[j].load(h[j] + i * STEP);
+    } else {
+      const int n = a.width - i * STEP - lane / 32 * RUN;
+      x.load_end(w + i * STEP, n);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) y[j].load_end(h[j] + i * STEP, n);
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[j] = multiply_run<T>(x, y[j], acc[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < FN; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) shared[wave][j][e][lane] = acc[j][e];
+  __syncthreads();
+  if (wave >= FN) return;   // wave j: the j-th 32 tokens
+  float z[1][16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int at = v + row_of(e, lane);
+    float sum = shared[0][wave][e][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) sum += shared[w][wave][e][lane];
+    z[0][e] = at < a.vocab ? sum + (a.bias != nullptr ? a.bias[at] : 0.f) : -__builtin_inff();
+  }
+  const int token = 32 * wave + lane % 32;
+  const bool live = token < a.rows;
+  const int hit = live && a.labels != nullptr ? a.labels[token] - v : -1;
+  leave_stats<1>(z, lane, token, live, hit, a.vocab - v, (long long)blockIdx.x * a.rows + token, a.part, a.part_u, a.label_logit);
+}
+template <typename T>
+hipError_t start_few(const FewArgs& a, hipStream_t stream) {
+  const unsigned blocks = (unsigned)ceil_div(a.vocab, 32);
+  if (a.rows <= 32) logit_few_kernel<T, 1><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  else logit_few_kernel<T, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 // Slices joined: `tokens` of them a workgroup, the other threads along the slices.
@@ -982,15 +1102,12 @@ hipError_t allow(const void* kernel, int lds) { return hipFuncSetAttribute(kerne
 constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
 constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
 
-#ifndef WIDE_FROM
-#define WIDE_FROM 192
-#endif
-#ifndef LONG_GROUP
-#define LONG_GROUP 512
-#endif
-constexpr int kLongGroup = LONG_GROUP;
-// Wide tiles where they give every compute unit one.
-bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= WIDE_FROM; }
+// Wide tiles of weight gradients: from so many tokens a worker on.  Shorter sums leave the tile's first loads and its 256 KB of stores, which only
+// another workgroup of the compute unit can run beside (100 tokens, 32000 x 1024, 20 workers: 732 us in 128 x 128 tiles, 794 in wide ones; 250 tokens, 50257 x
+// 1600: 139 and 156; 2048 tokens, 8192 x 4096, 4 workers: 1042 and 993).
+constexpr int kLongGroup = 512;
+// Wide tiles where they give most compute units one (250 tokens, 50257 x 1600, 197 tiles: 63 us, 128 x 128 tiles 75; 2000 tokens, 32000 x 1024: 186 and 211).
+bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
 
 struct Layout {
   size_t at = 0;
@@ -1002,7 +1119,7 @@ struct Layout {
 };
 
 struct ForwardPlan {
-  bool wide;
+  bool few, wide;
   int slice;          // values of the vocabulary in a slice
   int piece;          // values that are packed at a time
   int block;          // tokens at a time
@@ -1011,13 +1128,14 @@ struct ForwardPlan {
 ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
   ForwardPlan p;
   p.block = std::min(rows, kRowBlock);
+  p.few = rows <= kFewRows;
   p.wide = wide_tiles(vocab, p.block);
-  p.slice = p.wide ? 32 * WideTile::FM : 32 * MidTile::FM;
+  p.slice = p.few ? 32 : (p.wide ? 32 * WideTile::FM : 32 * MidTile::FM);
   const long long padded = padded_width(width);
   p.piece = (int)std::min<long long>((vocab + 255) / 256 * 256LL, std::max<long long>(256, kPackElements / padded / 256 * 256));
   Layout l;
-  p.hidden = l.take((size_t)planes_of(dtype) * p.block * padded * 2);
-  p.weight = l.take((size_t)planes_of(dtype) * std::min(p.piece, vocab) * padded * 2);
+  p.hidden = l.take(p.few ? 0 : (size_t)planes_of(dtype) * p.block * padded * 2);
+  p.weight = l.take(p.few ? 0 : (size_t)planes_of(dtype) * std::min(p.piece, vocab) * padded * 2);
   const size_t slices = (size_t)ceil_div(vocab, p.slice) + 4;
   p.part = l.take(slices * p.block * 8);
   p.part_u = l.take(slices * p.block * 4);
@@ -1128,11 +1246,28 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
   const ForwardPlan p = forward_plan(a.rows, a.vocab, a.width, a.dtype);
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   const size_t bytes = a.dtype == ZENO_F32 ? 4 : 2;
+  auto join = [&](const StatArgs& s, int t0, int rows, int slices) {
+    const JoinArgs j = {s.part, s.part_u, s.label_logit, a.labels == nullptr ? nullptr : a.labels + t0, slices, rows, a.vocab,
+                        a.logp == nullptr ? nullptr : a.logp + t0, a.entropy == nullptr ? nullptr : a.entropy + t0,
+                        a.stats == nullptr ? nullptr : a.stats + 2 * (size_t)t0};
+    int tokens = 1;   // a workgroup for every compute unit, up to whole memory lines
+    while (tokens < 64 && rows / (2 * tokens) >= 256) tokens *= 2;
+    logit_join_kernel<<<(unsigned)ceil_div(rows, tokens), kJoinThreads, 0, stream>>>(j, tokens);
+    return hipGetLastError();
+  };
+  StatArgs s = {};
+  s.part = reinterpret_cast<float2*>(ws + p.part);
+  s.part_u = a.entropy != nullptr ? reinterpret_cast<float*>(ws + p.part_u) : nullptr;
+  s.label_logit = reinterpret_cast<float*>(ws + p.label);
+  if (p.few) {
+    const FewArgs f = {a.hidden, a.weight, a.ldh, a.ldw, a.rows, a.vocab, a.width, a.bias, a.labels, s.part, s.part_u, s.label_logit};
+    ZENO_STEP(a.dtype == ZENO_F32 ? start_few<float>(f, stream) : a.dtype == ZENO_BF16 ? start_few<__bf16>(f, stream) : start_few<_Float16>(f, stream));
+    return join(s, 0, a.rows, ceil_div(a.vocab, 32));
+  }
   const bool half = a.dtype == ZENO_F16, direct = as_it_is(a.weight, a.ldw, a.dtype, a.width);
   const int piece = direct ? a.vocab : p.piece;
   for (int t0 = 0; t0 < a.rows; t0 += p.block) {
     const int rows = std::min(p.block, a.rows - t0);
-    StatArgs s = {};
     LogitArgs& l = s.l;
     ZENO_STEP(side_of(reinterpret_cast<const unsigned char*>(a.hidden) + (size_t)t0 * a.ldh * bytes, a.ldh, a.dtype, rows, a.width,
                       reinterpret_cast<u16*>(ws + p.hidden), l.h, stream));
@@ -1142,9 +1277,6 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
     l.rows = rows;
     l.bias = a.bias;
     l.labels = a.labels == nullptr ? nullptr : a.labels + t0;
-    s.part = reinterpret_cast<float2*>(ws + p.part);
-    s.part_u = a.entropy != nullptr ? reinterpret_cast<float*>(ws + p.part_u) : nullptr;
-    s.label_logit = reinterpret_cast<float*>(ws + p.label);
     int slices = 0;
     for (int v0 = 0; v0 < a.vocab; v0 += piece) {
       const int values = std::min(piece, a.vocab - v0);
@@ -1159,12 +1291,7 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
       else ZENO_STEP(half ? (start_stats<MidTile, true>(s, stream)) : (start_stats<MidTile, false>(s, stream)));
       slices = s.slice0 + l.tiles_m * 2;
     }
-    const JoinArgs j = {s.part, s.part_u, s.label_logit, l.labels, slices, rows, a.vocab, a.logp == nullptr ? nullptr : a.logp + t0,
-                        a.entropy == nullptr ? nullptr : a.entropy + t0, a.stats == nullptr ? nullptr : a.stats + 2 * (size_t)t0};
-    int tokens = 1;   // a workgroup for every compute unit, up to whole memory lines
-    while (tokens < 64 && rows / (2 * tokens) >= 256) tokens *= 2;
-    logit_join_kernel<<<(unsigned)ceil_div(rows, tokens), kJoinThreads, 0, stream>>>(j, tokens);
-    ZENO_STEP(hipGetLastError());
+    ZENO_STEP(join(s, t0, rows, slices));
   }
   return hipSuccess;
 }
