@@ -474,8 +474,9 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_
 }
 
 // Few tokens: the weights are what has to be read.  A workgroup takes 32 rows of them, its four waves a share of the contraction each; operands go
-// from memory to the matrix instructions' registers, as they stand: any type, pitch and alignment.  Which values of the contraction an instruction
-// multiplies does not matter as long as both operands agree, so a lane reads 64 bytes of its row in a run.
+// from memory to the matrix instructions' registers, as they stand: any type, pitch and alignment.  16 x 16 instructions: four lanes have 64
+// bytes of a row in a run, so a load has sixteen pieces to fetch (32 x 32: 64 pieces of 16 bytes, and 1 x 32000 x 4096 bf16 took 56 us).  Which values of the
+// contraction an instruction multiplies does not matter as long as both operands agree.
 struct FewArgs {
   const void *hidden, *weight;
   long long ldh, ldw;
@@ -487,90 +488,98 @@ struct FewArgs {
 };
 constexpr int kFewRows = 64, kFewWaves = 4;
 template <typename T>
-struct Run {   // a lane's 64 bytes of a row
-  typename Wide<T>::type v[4];
-  __device__ inline void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const typename Wide<T>::unaligned*>(p + i * Wide<T>::N);
-  }
-  __device__ inline void load_end(const T* p, int n) {   // the first n, zeros behind
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < Wide<T>::N; ++j) v[i][j] = i * Wide<T>::N + j < n ? p[i * Wide<T>::N + j] : (T)0.f;
-  }
-};
+using Piece = typename Wide<T>::type;   // 16 bytes of a row
 template <typename T>
-__device__ inline f32x16 multiply_run(const Run<T>& a, const Run<T>& b, f32x16 c) {
+__device__ inline Piece<T> load_piece(const T* p) { return *reinterpret_cast<const typename Wide<T>::unaligned*>(p); }
+template <typename T>
+__device__ inline Piece<T> load_piece_end(const T* p, int n) {   // the first n, zeros behind
+  Piece<T> v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
+  for (int j = 0; j < Wide<T>::N; ++j) v[j] = j < n ? p[j] : (T)0.f;
+  return v;
+}
+template <typename T>
+__device__ inline f32x4 multiply_piece(Piece<T> a, Piece<T> b, f32x4 c) {
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i][j], b.v[i][j], c, 0, 0, 0);
-    } else {
-      c = multiply<std::is_same<T, _Float16>::value>(__builtin_bit_cast(s16x8, a.v[i]), __builtin_bit_cast(s16x8, b.v[i]), c);
-    }
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
   return c;
 }
+// 16 FN tokens
 template <typename T, int FN>
 __global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
-  __shared__ float shared[kFewWaves][FN][16][64];
-  constexpr int RUN = 64 / (int)sizeof(T), STEP = 2 * RUN;   // of the contraction: a lane's, both halves' of a wave
+  __shared__ float shared[kFewWaves][32][16 * FN + 1];
+  constexpr int N = Wide<T>::N, STEP = 8 * N;   // of the contraction: 128 bytes of a row, two pieces a lane
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * 32;
   const int steps = (a.width + STEP - 1) / STEP, begin = steps * wave / kFewWaves, end = steps * (wave + 1) / kFewWaves;
-  const int row = v + lane % 32 < a.vocab ? v + lane % 32 : a.vocab - 1;   // (behind the last: the last once more)
-  const T* w = reinterpret_cast<const T*>(a.weight) + row * a.ldw + lane / 32 * RUN;
-  const T* h[FN];
+  const int from = lane / 16 * N;
+  const T *w[2], *h[FN];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int row = v + 16 * r + lane % 16;   // (behind the last: the last once more)
+    w[r] = reinterpret_cast<const T*>(a.weight) + (row < a.vocab ? row : a.vocab - 1) * a.ldw + from;
+  }
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    const int token = 32 * j + lane % 32;
-    h[j] = reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + lane / 32 * RUN;
+    const int token = 16 * j + lane % 16;
+    h[j] = reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + from;
   }
-  f32x16 acc[FN] = {};
+  f32x4 acc[2][FN] = {};
   const int whole = a.width / STEP < end ? a.width / STEP : end;
   int i = begin;
-  for (; i + 2 <= whole; i += 2) {
-    Run<T> x[2], y[2][FN];
+  constexpr int AHEAD = FN < 4 ? 2 : 1;   // steps whose loads are sent for at once
+  for (; i + AHEAD <= whole; i += AHEAD) {
+    Piece<T> x[2 * AHEAD][2], y[2 * AHEAD][FN];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      x[u].load(w + (i + u) * STEP);
+    for (int u = 0; u < 2 * AHEAD; ++u) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) y[u][j].load(h[j] + (i + u) * STEP);
+      for (int r = 0; r < 2; ++r) x[u][r] = load_piece<T>(w[r] + i * STEP + u * 4 * N);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) y[u][j] = load_piece<T>(h[j] + i * STEP + u * 4 * N);
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2 * AHEAD; ++u)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) acc[j] = multiply_run<T>(x[u], y[u][j], acc[j]);
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[r][j] = multiply_piece<T>(x[u][r], y[u][j], acc[r][j]);
   }
   for (; i < end; ++i) {
-    Run<T> x, y[FN];
-    if (i < whole) {
-      x.load(w + i * STEP);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) y[j].load(h[j] + i * STEP);
-    } else {
-      const int n = a.width - i * STEP - lane / 32 * RUN;
-      x.load_end(w + i * STEP, n);
+    for (int u = 0; u < 2; ++u) {
+      const int at = i * STEP + u * 4 * N, n = a.width - at - from;
+      Piece<T> x[2], y[FN];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) y[j].load_end(h[j] + i * STEP, n);
+      for (int r = 0; r < 2; ++r) x[r] = n >= N ? load_piece<T>(w[r] + at) : load_piece_end<T>(w[r] + at, n);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) y[j] = n >= N ? load_piece<T>(h[j] + at) : load_piece_end<T>(h[j] + at, n);
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[r][j] = multiply_piece<T>(x[r], y[j], acc[r][j]);
     }
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[j] = multiply_run<T>(x, y[j], acc[j]);
   }
 #pragma unroll
-  for (int j = 0; j < FN; ++j)
+  for (int r = 0; r < 2; ++r)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) shared[wave][j][e][lane] = acc[j][e];
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) shared[wave][16 * r + 4 * (lane / 16) + e][16 * j + lane % 16] = acc[r][j][e];
   __syncthreads();
-  if (wave >= FN) return;   // wave j: the j-th 32 tokens
+  if (32 * wave >= 16 * FN) return;   // wave j: the j-th 32 tokens
+  const int here = 32 * wave + lane % 32 < 16 * FN ? 32 * wave + lane % 32 : 16 * FN - 1;
   float z[1][16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    const int at = v + row_of(e, lane);
-    float sum = shared[0][wave][e][lane];
+    const int row = row_of(e, lane), at = v + row;
+    float sum = shared[0][row][here];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) sum += shared[w][wave][e][lane];
+    for (int p = 1; p < kFewWaves; ++p) sum += shared[p][row][here];
     z[0][e] = at < a.vocab ? sum + (a.bias != nullptr ? a.bias[at] : 0.f) : -__builtin_inff();
   }
   const int token = 32 * wave + lane % 32;
@@ -581,8 +590,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
 template <typename T>
 hipError_t start_few(const FewArgs& a, hipStream_t stream) {
   const unsigned blocks = (unsigned)ceil_div(a.vocab, 32);
-  if (a.rows <= 32) logit_few_kernel<T, 1><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
-  else logit_few_kernel<T, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  if (a.rows <= 16) logit_few_kernel<T, 1><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  else if (a.rows <= 32) logit_few_kernel<T, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  else logit_few_kernel<T, 4><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 
