@@ -78,7 +78,7 @@ hipError_t launch_embed_from(const EmbedArgs& a, hipStream_t stream) {
 
 // ---- tokens by (group, id)
 
-constexpr int kSmallSort = 8192;        // tokens that one workgroup sorts in LDS
+constexpr int kSmallSort = 16384;       // tokens that one workgroup sorts in LDS
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSmallBits = 8, kLargeBits = 11;
 constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
@@ -152,29 +152,37 @@ __device__ inline void clear_part(const EmbedGradArgs& a, long long at) {
   if (whole + 4 * quads + threadIdx.x < hi) p[whole + 4 * quads + threadIdx.x] = 0.f;
 }
 
-// Up to kSmallSort tokens: one workgroup, everything in LDS, eight bits of the key a pass; the others clear gradients meanwhile.
+// Up to kSmallSort tokens: one workgroup, eight bits of the key a pass, a wave's consecutive items in registers between the passes; the other
+// workgroups clear gradients meanwhile.
+constexpr int kItems = kSmallSort / kSortThreads;
 __global__ __launch_bounds__(kSortThreads) void embed_sort_small_kernel(EmbedGradArgs a, int passes) {
   if (blockIdx.x > 0) {
     clear_part(a, blockIdx.x - 1);
     return;
   }
-  __shared__ unsigned key[2][kSmallSort];
-  __shared__ unsigned short index[2][kSmallSort];
+  __shared__ unsigned key[kSmallSort];
+  __shared__ unsigned short index[kSmallSort];
   __shared__ unsigned counter[kSortWaves][1 << kSmallBits];
   __shared__ unsigned total[1 << kSmallBits];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  for (int t = tid; t < a.rows; t += kSortThreads) {
-    key[0][t] = token_key(a, t);
-    index[0][t] = (unsigned short)t;
-  }
   const int per = ((a.rows + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;   // a wave's items are consecutive
   const int lo = wave * per < a.rows ? wave * per : a.rows, hi = lo + per < a.rows ? lo + per : a.rows;
+  unsigned k[kItems];
+  unsigned short x[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int t = lo + 64 * i + lane;
+    k[i] = t < hi ? token_key(a, t) : 0;
+    x[i] = (unsigned short)t;
+  }
   for (int pass = 0; pass < passes; ++pass) {
-    const int from = pass % 2, shift = pass * kSmallBits;
+    const int shift = pass * kSmallBits;
     unsigned* mine = counter[wave];
     for (int d = lane; d < 1 << kSmallBits; d += 64) mine[d] = 0;
-    __syncthreads();
-    for (int t = lo + lane; t < hi; t += 64) atomicAdd(&mine[(key[from][t] >> shift) & 255], 1u);
+    lds_order();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (lo + 64 * i + lane < hi) atomicAdd(&mine[(k[i] >> shift) & 255], 1u);
     __syncthreads();
     if (tid < 1 << kSmallBits) {
       unsigned sum = 0;
@@ -205,22 +213,34 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_small_kernel(EmbedGra
     __syncthreads();
     for (int d = lane; d < 1 << kSmallBits; d += 64) mine[d] += total[d];
     lds_order();
-    for (int t0 = lo; t0 < hi; t0 += 64) {
-      const int t = t0 + lane;
-      const bool active = t < hi;
-      const unsigned k = active ? key[from][t] : 0;
-      const unsigned short i = active ? index[from][t] : 0;
-      const unsigned at = place_of<kSmallBits>(mine, (k >> shift) & 255, active, lane);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      if (lo + 64 * i >= hi) break;
+      const bool active = lo + 64 * i + lane < hi;
+      const unsigned at = place_of<kSmallBits>(mine, (k[i] >> shift) & 255, active, lane);
       if (active) {
-        key[1 - from][at] = k;
-        index[1 - from][at] = i;
+        key[at] = k[i];
+        index[at] = x[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int t = lo + 64 * i + lane;
+      if (t < hi) {
+        k[i] = key[t];
+        x[i] = index[t];
       }
     }
     __syncthreads();
   }
-  for (int t = tid; t < a.rows; t += kSortThreads) {
-    a.key[0][t] = key[passes % 2][t];
-    a.index[0][t] = index[passes % 2][t];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int t = lo + 64 * i + lane;
+    if (t < hi) {
+      a.key[0][t] = k[i];
+      a.index[0][t] = x[i];
+    }
   }
 }
 
@@ -228,10 +248,9 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_small_kernel(EmbedGra
 __device__ inline unsigned source_key(const EmbedGradArgs& a, int pass, int t) {
   return pass == 0 ? token_key(a, t) : a.key[(pass - 1) % 2][t];
 }
-__global__ __launch_bounds__(kChunkThreads) void embed_count_kernel(EmbedGradArgs a, int pass, int bits, int chunks, int chunk,
-                                                                   long long fill_from) {
+__global__ __launch_bounds__(kChunkThreads) void embed_count_kernel(EmbedGradArgs a, int pass, int bits, int chunks, int chunk) {
   if ((int)blockIdx.x >= chunks) {
-    clear_part(a, fill_from + blockIdx.x - chunks);
+    clear_part(a, blockIdx.x - chunks);
     return;
   }
   __shared__ unsigned count[1 << kLargeBits];
@@ -245,11 +264,7 @@ __global__ __launch_bounds__(kChunkThreads) void embed_count_kernel(EmbedGradArg
   for (int d = threadIdx.x; d < digits; d += kChunkThreads) a.count[(long long)d * chunks + blockIdx.x] = count[d];
 }
 // One wave a digit: its chunks' counts become what the chunks before hold, and total[d] the digit's.
-__global__ __launch_bounds__(256) void embed_scan_kernel(EmbedGradArgs a, int bits, int chunks, int scans, long long fill_from) {
-  if ((int)blockIdx.x >= scans) {
-    clear_part(a, fill_from + blockIdx.x - scans);
-    return;
-  }
+__global__ __launch_bounds__(256) void embed_scan_kernel(EmbedGradArgs a, int bits, int chunks) {
   const int d = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
   if (d >= 1 << bits) return;
   unsigned before = 0;
@@ -266,12 +281,7 @@ __global__ __launch_bounds__(256) void embed_scan_kernel(EmbedGradArgs a, int bi
   }
   if (lane == 0) a.total[d] = before;
 }
-__global__ __launch_bounds__(kChunkThreads) void embed_scatter_kernel(EmbedGradArgs a, int pass, int bits, int chunks, int chunk,
-                                                                     long long fill_from) {
-  if ((int)blockIdx.x >= chunks) {
-    clear_part(a, fill_from + blockIdx.x - chunks);
-    return;
-  }
+__global__ __launch_bounds__(kChunkThreads) void embed_scatter_kernel(EmbedGradArgs a, int pass, int bits, int chunks, int chunk) {
   __shared__ unsigned counter[kChunkWaves][1 << kLargeBits];
   __shared__ unsigned base[1 << kLargeBits];
   __shared__ unsigned wave_total[kChunkWaves];
@@ -415,44 +425,54 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradArgs a, int la
   else add_to_table<N>(a, now, col, skip, sum);
 }
 
-// Sums that several pieces share, from the piece where one begins: 64 columns a wave, the waves take consecutive pieces' slots.
+// Sums that several pieces share, by the workgroup of the piece where one begins: N columns a lane, the waves take consecutive pieces' slots.
 constexpr int kJoinWaves = 8;
-__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(EmbedGradArgs a, unsigned blocks, int source) {
-  __shared__ float part[kJoinWaves][64];
+template <int N>
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(EmbedGradArgs a, int source) {
+  __shared__ float part[kJoinWaves][64 * N];
   const unsigned* key = a.key[source];
   const unsigned none = (unsigned)a.m * (unsigned)a.vocab;
-  const long long piece = blockIdx.x / blocks, next = (piece + 1) * a.per_piece;
-  if (next >= a.rows) return;
-  const unsigned mine = key[next];
-  if (mine >= none || key[next - 1] != mine) return;
-  const long long begin = piece * a.per_piece;
-  if (key[begin] == mine && begin > 0 && key[begin - 1] == mine) return;   // began before
-  // the last piece that holds it: keys are sorted
-  long long lo = piece + 1, hi = a.pieces;   // piece lo begins with it, piece hi does not
-  while (hi - lo > 1) {
-    const long long mid = (lo + hi) / 2;
-    if (key[mid * a.per_piece] == mine) lo = mid;
-    else hi = mid;
-  }
-  const long long count = lo - piece;        // first slots of pieces piece + 1 .. lo
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const long long col = (long long)(blockIdx.x % blocks) * 64 + lane;
-  const bool live = col < a.width;
-  const long long per = (count + kJoinWaves - 1) / kJoinWaves;
-  const long long from = piece + 1 + (wave * per < count ? wave * per : count);
-  const long long to = from + per < lo + 1 ? from + per : lo + 1;
-  float sum = 0.f;
-  if (live) {
-    if (wave == 0) sum = a.slots[(2 * piece + 1) * a.width + col];
-#pragma unroll 8
-    for (long long p = from; p < to; ++p) sum += a.slots[2 * p * a.width + col];
+  const long long piece = blockIdx.x, begin = piece * a.per_piece, next = begin + a.per_piece;
+  if (next >= a.rows) return;
+  const unsigned mine = key[next], last = key[next - 1], first = key[begin], before = begin > 0 ? key[begin - 1] : none;
+  if (mine >= none || last != mine) return;
+  if (first == mine && before == mine) return;   // began before
+  // the first slots of pieces piece + 1 .. piece + count
+  long long count = 1;
+  for (;;) {
+    const long long p = piece + 1 + count + lane;
+    const unsigned long long has = __ballot(p < a.pieces && key[p * a.per_piece] == mine);
+    const int run = has == ~0ULL ? 64 : __builtin_ctzll(~has);
+    count += run;
+    if (run < 64) break;
   }
-  part[wave][lane] = sum;
-  __syncthreads();
-  if (wave == 0 && live) {
-    float s[1] = {part[0][lane]};
-    for (int w = 1; w < kJoinWaves; ++w) s[0] += part[w][lane];
-    add_to_table<1>(a, mine, col, 0, s);
+  const long long per = (count + kJoinWaves - 1) / kJoinWaves;
+  const long long from = piece + 1 + (wave * per < count ? wave * per : count), end = piece + 1 + count, to = from + per < end ? from + per : end;
+  for (long long unit = lane; unit - lane < (a.width + N - 1) / N; unit += 64) {
+    const bool live = unit * N < a.width;
+    const long long col = unit * N < a.width - N ? unit * N : a.width - N;
+    float sum[N] = {};
+    if (live) {
+      if (wave == 0) load_values<float, N>(a.slots + (2 * piece + 1) * a.width + col, sum);
+#pragma unroll 8
+      for (long long p = from; p < to; ++p) {
+        float v[N];
+        load_values<float, N>(a.slots + 2 * p * a.width + col, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += v[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) part[wave][i * 64 + lane] = sum[i];
+    __syncthreads();
+    if (wave == 0 && live) {
+      for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += part[w][i * 64 + lane];
+      add_to_table<N>(a, mine, col, (int)(unit * N - col), sum);
+    }
+    __syncthreads();
   }
 }
 
@@ -542,32 +562,21 @@ hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream
   if (a.rows <= kSmallSort) {
     embed_sort_small_kernel<<<(unsigned)(1 + fills), kSortThreads, 0, stream>>>(a, p.passes);
   } else {
-    // the gradients are cleared beside the sort's launches, a share in each
-    const int launches = 3 * p.passes;
-    long long done = 0;
-    int launch = 0;
-    auto share = [&] {
-      ++launch;
-      const long long until = fills * launch / launches, n = until - done;
-      done = until;
-      return n;
-    };
     const int scans = ((1 << p.bits) + 3) / 4;
-    for (int pass = 0; pass < p.passes; ++pass) {
-      long long from = done, more = share();
-      embed_count_kernel<<<(unsigned)(p.chunks + more), kChunkThreads, 0, stream>>>(a, pass, p.bits, p.chunks, p.chunk, from);
-      from = done, more = share();
-      embed_scan_kernel<<<(unsigned)(scans + more), 256, 0, stream>>>(a, p.bits, p.chunks, scans, from);
-      from = done, more = share();
-      embed_scatter_kernel<<<(unsigned)(p.chunks + more), kChunkThreads, 0, stream>>>(a, pass, p.bits, p.chunks, p.chunk, from);
+    for (int pass = 0; pass < p.passes; ++pass) {   // the gradients are cleared beside the first launch
+      embed_count_kernel<<<(unsigned)(p.chunks + (pass == 0 ? fills : 0)), kChunkThreads, 0, stream>>>(a, pass, p.bits, p.chunks, p.chunk);
+      embed_scan_kernel<<<scans, 256, 0, stream>>>(a, p.bits, p.chunks);
+      embed_scatter_kernel<<<p.chunks, kChunkThreads, 0, stream>>>(a, pass, p.bits, p.chunks, p.chunk);
     }
     source = (p.passes - 1) % 2;
   }
   if (a.dtype == ZENO_F32) launch_sums<float>(a, source, stream);
   else if (a.dtype == ZENO_BF16) launch_sums<__bf16>(a, source, stream);
   else launch_sums<_Float16>(a, source, stream);
-  const unsigned blocks = (unsigned)((a.width + 63) / 64);
-  if (p.pieces > 1) embed_join_kernel<<<(unsigned)(p.pieces - 1) * blocks, 64 * kJoinWaves, 0, stream>>>(a, blocks, source);
+  if (p.pieces > 1) {
+    if (a.width >= 4) embed_join_kernel<4><<<(unsigned)(p.pieces - 1), 64 * kJoinWaves, 0, stream>>>(a, source);
+    else embed_join_kernel<1><<<(unsigned)(p.pieces - 1), 64 * kJoinWaves, 0, stream>>>(a, source);
+  }
   return hipGetLastError();
 }
 

@@ -486,7 +486,10 @@ struct FewArgs {
   float2* part;          // slices of 32 values
   float *part_u, *label_logit;
 };
-constexpr int kFewRows = 64, kFewWaves = 4;
+// Up to which number of tokens: 16-bit operands are as fast in tiles of 128 tokens from 65 on (32000 x 4096: 64 tokens 74 us here, 65 there 69); float32,
+// which tiles take in six products, from 257 on (1024 columns: 256 tokens 209 us here, 250 there 211; 4096 columns 832 and 939).
+// 32 rows a workgroup for one block of tokens (1 token, 32000 x 4096 bf16: 56 us with the join and the host, 64 rows 63), 64 for more (32 tokens: 82 and 65; 64: 106 and 74).
+constexpr int kFewRows = 64, kFewRowsF32 = 256, kFewWaves = 4;
 template <typename T>
 using Piece = typename Wide<T>::type;   // 16 bytes of a row
 template <typename T>
@@ -510,42 +513,42 @@ __device__ inline f32x4 multiply_piece(Piece<T> a, Piece<T> b, f32x4 c) {
   }
   return c;
 }
-// 16 FN tokens
-template <typename T, int FN>
+// 16 R rows of W, a multiple of 32; 16 FN tokens from 16 FN blockIdx.y on
+template <typename T, int R, int FN>
 __global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
-  __shared__ float shared[kFewWaves][32][16 * FN + 1];
+  __shared__ float shared[kFewWaves][16 * R][16 * FN + 1];
   constexpr int N = Wide<T>::N, STEP = 8 * N;   // of the contraction: 128 bytes of a row, two pieces a lane
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * 32;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
   const int steps = (a.width + STEP - 1) / STEP, begin = steps * wave / kFewWaves, end = steps * (wave + 1) / kFewWaves;
   const int from = lane / 16 * N;
-  const T *w[2], *h[FN];
+  const T *w[R], *h[FN];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < R; ++r) {
     const int row = v + 16 * r + lane % 16;   // (behind the last: the last once more)
     w[r] = reinterpret_cast<const T*>(a.weight) + (row < a.vocab ? row : a.vocab - 1) * a.ldw + from;
   }
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    const int token = 16 * j + lane % 16;
+    const int token = token0 + 16 * j + lane % 16;
     h[j] = reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + from;
   }
-  f32x4 acc[2][FN] = {};
+  f32x4 acc[R][FN] = {};
   const int whole = a.width / STEP < end ? a.width / STEP : end;
   int i = begin;
-  constexpr int AHEAD = FN < 4 ? 2 : 1;   // steps whose loads are sent for at once
+  constexpr int AHEAD = R * FN < 8 ? 2 : 1;   // steps whose loads are sent for at once
   for (; i + AHEAD <= whole; i += AHEAD) {
-    Piece<T> x[2 * AHEAD][2], y[2 * AHEAD][FN];
+    Piece<T> x[2 * AHEAD][R], y[2 * AHEAD][FN];
 #pragma unroll
     for (int u = 0; u < 2 * AHEAD; ++u) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) x[u][r] = load_piece<T>(w[r] + i * STEP + u * 4 * N);
+      for (int r = 0; r < R; ++r) x[u][r] = load_piece<T>(w[r] + i * STEP + u * 4 * N);
 #pragma unroll
       for (int j = 0; j < FN; ++j) y[u][j] = load_piece<T>(h[j] + i * STEP + u * 4 * N);
     }
 #pragma unroll
     for (int u = 0; u < 2 * AHEAD; ++u)
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[r][j] = multiply_piece<T>(x[u][r], y[u][j], acc[r][j]);
   }
@@ -553,46 +556,48 @@ __global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int at = i * STEP + u * 4 * N, n = a.width - at - from;
-      Piece<T> x[2], y[FN];
+      Piece<T> x[R], y[FN];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) x[r] = n >= N ? load_piece<T>(w[r] + at) : load_piece_end<T>(w[r] + at, n);
+      for (int r = 0; r < R; ++r) x[r] = n >= N ? load_piece<T>(w[r] + at) : load_piece_end<T>(w[r] + at, n);
 #pragma unroll
       for (int j = 0; j < FN; ++j) y[j] = n >= N ? load_piece<T>(h[j] + at) : load_piece_end<T>(h[j] + at, n);
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[r][j] = multiply_piece<T>(x[r], y[j], acc[r][j]);
     }
   }
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
+  for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) shared[wave][16 * r + 4 * (lane / 16) + e][16 * j + lane % 16] = acc[r][j][e];
   __syncthreads();
-  if (32 * wave >= 16 * FN) return;   // wave j: the j-th 32 tokens
-  const int here = 32 * wave + lane % 32 < 16 * FN ? 32 * wave + lane % 32 : 16 * FN - 1;
-  float z[1][16];
+  // 32 rows and 32 tokens a wave at a time
+  constexpr int TOKENS = (16 * FN + 31) / 32;
+  for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
+    const int v32 = v + 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, here = t32 < 16 * FN ? t32 : 16 * FN - 1;
+    float z[1][16];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int row = row_of(e, lane), at = v + row;
-    float sum = shared[0][row][here];
+    for (int e = 0; e < 16; ++e) {
+      const int row = v32 - v + row_of(e, lane), at = v + row;
+      float sum = shared[0][row][here];
 #pragma unroll
-    for (int p = 1; p < kFewWaves; ++p) sum += shared[p][row][here];
-    z[0][e] = at < a.vocab ? sum + (a.bias != nullptr ? a.bias[at] : 0.f) : -__builtin_inff();
+      for (int p = 1; p < kFewWaves; ++p) sum += shared[p][row][here];
+      z[0][e] = at < a.vocab ? sum + (a.bias != nullptr ? a.bias[at] : 0.f) : -__builtin_inff();
+    }
+    const int token = token0 + t32;
+    const bool live = t32 < 16 * FN && token < a.rows;
+    const int hit = live && a.labels != nullptr ? a.labels[token] - v32 : -1;
+    leave_stats<1>(z, lane, token, live, hit, a.vocab - v32, (long long)(v32 / 32) * a.rows + token, a.part, a.part_u, a.label_logit);
   }
-  const int token = 32 * wave + lane % 32;
-  const bool live = token < a.rows;
-  const int hit = live && a.labels != nullptr ? a.labels[token] - v : -1;
-  leave_stats<1>(z, lane, token, live, hit, a.vocab - v, (long long)blockIdx.x * a.rows + token, a.part, a.part_u, a.label_logit);
 }
 template <typename T>
 hipError_t start_few(const FewArgs& a, hipStream_t stream) {
-  const unsigned blocks = (unsigned)ceil_div(a.vocab, 32);
-  if (a.rows <= 16) logit_few_kernel<T, 1><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
-  else if (a.rows <= 32) logit_few_kernel<T, 2><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
-  else logit_few_kernel<T, 4><<<blocks, 64 * kFewWaves, 0, stream>>>(a);
+  if (a.rows <= 16) logit_few_kernel<T, 2, 1><<<(unsigned)ceil_div(a.vocab, 32), 64 * kFewWaves, 0, stream>>>(a);
+  else if (a.rows <= 32) logit_few_kernel<T, 4, 2><<<(unsigned)ceil_div(a.vocab, 64), 64 * kFewWaves, 0, stream>>>(a);
+  else logit_few_kernel<T, 4, 4><<<dim3((unsigned)ceil_div(a.vocab, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -1138,7 +1143,7 @@ struct ForwardPlan {
 ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
   ForwardPlan p;
   p.block = std::min(rows, kRowBlock);
-  p.few = rows <= kFewRows;
+  p.few = rows <= (dtype == ZENO_F32 ? kFewRowsF32 : kFewRows);
   p.wide = wide_tiles(vocab, p.block);
   p.slice = p.few ? 32 : (p.wide ? 32 * WideTile::FM : 32 * MidTile::FM);
   const long long padded = padded_width(width);
@@ -1272,7 +1277,7 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
   if (p.few) {
     const FewArgs f = {a.hidden, a.weight, a.ldh, a.ldw, a.rows, a.vocab, a.width, a.bias, a.labels, s.part, s.part_u, s.label_logit};
     ZENO_STEP(a.dtype == ZENO_F32 ? start_few<float>(f, stream) : a.dtype == ZENO_BF16 ? start_few<__bf16>(f, stream) : start_few<_Float16>(f, stream));
-    return join(s, 0, a.rows, ceil_div(a.vocab, 32));
+    return join(s, 0, a.rows, a.rows <= 16 ? ceil_div(a.vocab, 32) : ceil_div(a.vocab, 64) * 2);   // (what the workgroups have left)
   }
   const bool half = a.dtype == ZENO_F16, direct = as_it_is(a.weight, a.ldw, a.dtype, a.width);
   const int piece = direct ? a.vocab : p.piece;

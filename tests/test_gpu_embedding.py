@@ -103,6 +103,9 @@ CASES = [
     (700, 13, 515, [0, 300, 301, 690], "zipf"),
     (2000, 500, 64, [0, 2000], "one"),
     (8192, 300, 24, [100, 3000, 3000, 8000], "zipf"),
+    (16384, 300, 24, [100, 3000, 3000, 16000], "zipf"),
+    (16385, 300, 24, [100, 3000, 3000, 16000], "zipf"),
+    (16384, 70000, 2, [0, 9000, 16384], "zipf"),
     (8193, 300, 24, [100, 3000, 3000, 8000], "zipf"),
     (8200, 3, 5, None, "one"),
     (9000, 10000, 12, None, "distinct"),
