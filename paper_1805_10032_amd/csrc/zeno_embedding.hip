@@ -83,7 +83,6 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kSmallBits = 8, kLargeBits = 11;
 constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
 constexpr int kMaxChunks = 1024;
-constexpr long long kFillFloats = 16384;   // that a workgroup clears
 
 // Key of a token: group * vocab + id; tokens of no group and ids outside the vocabulary come last.
 __device__ inline unsigned token_key(const EmbedGradArgs& a, int t) {
@@ -133,21 +132,22 @@ __device__ inline unsigned place_of(unsigned* counter, unsigned digit, bool acti
   return at + before;
 }
 
-// Clears a workgroup's part of the gradients: piece `at` of all groups' rows, cut at memory lines.
+// Clears piece `at` of all groups' rows, cut at memory lines.  A workgroup clears one piece, so that those that run lie near each other: 2.6 GB at 6.1
+// TB/s beside the sort (pieces dealt to 2048 workgroups 5.1, stores past the caches 5.1 to 5.4).
 __device__ inline void clear_part(const EmbedGradArgs& a, long long at) {
   const long long n = (long long)a.vocab * a.width, per = a.fill_pieces;
   const int g = (int)(at / per);
   const long long c = at % per;
   float* p = a.dtable + g * a.ldg;
   const long long off_line = (long long)((reinterpret_cast<unsigned long long>(p) & 127) / 4);
-  const long long lo = c == 0 ? 0 : c * kFillFloats - off_line;
-  const long long hi = (c + 1) * kFillFloats - off_line < n ? (c + 1) * kFillFloats - off_line : n;
+  const long long lo = c == 0 ? 0 : c * a.fill_floats - off_line;
+  const long long hi = (c + 1) * a.fill_floats - off_line < n ? (c + 1) * a.fill_floats - off_line : n;
   long long whole = lo;
   if (c == 0) whole = off_line == 0 ? 0 : (32 - off_line < hi ? 32 - off_line : hi);
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const long long quads = hi > whole ? (hi - whole) / 4 : 0;
-  for (long long q = threadIdx.x; q < quads; q += blockDim.x) __builtin_nontemporal_store(zero, reinterpret_cast<f32x4*>(p + whole) + q);
-  keep_apart();
+#pragma unroll 4
+  for (long long q = threadIdx.x; q < quads; q += blockDim.x) reinterpret_cast<f32x4*>(p + whole)[q] = zero;
   if (lo + threadIdx.x < whole) p[lo + threadIdx.x] = 0.f;
   if (whole + 4 * quads + threadIdx.x < hi) p[whole + 4 * quads + threadIdx.x] = 0.f;
 }
@@ -395,14 +395,24 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradArgs a, int la
   };
   const T* dy = reinterpret_cast<const T*>(a.dy) + col;
   float v[kAhead][N];
-  unsigned k[kAhead];
-  for (long long t0 = begin; t0 < end; t0 += kAhead) {
+  unsigned k[kAhead], k_next[kAhead];
+  int row[kAhead];   // of the next rows: they are known when these have arrived
+  auto look = [&](long long t0) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const long long t = t0 + i < end ? t0 + i : end - 1;
-      k[i] = t0 + i < end ? key[t] : none;
-      load_values<T, N>(dy + (long long)index[t] * a.lddy, v[i]);
+      k_next[i] = key[t];
+      row[i] = index[t];
     }
+  };
+  look(begin);
+  for (long long t0 = begin; t0 < end; t0 += kAhead) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      k[i] = k_next[i];
+      load_values<T, N>(dy + (long long)row[i] * a.lddy, v[i]);
+    }
+    look(t0 + kAhead);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (t0 + i >= end) break;
@@ -552,8 +562,9 @@ hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream
   a.pieces = p.pieces;
   a.per_piece = p.per_piece;
   const long long n = (long long)a.vocab * a.width;
-  a.fill_pieces = (n + 31 + kFillFloats - 1) / kFillFloats;   // (31: a part's place in its first line)
-  long long fills = a.accumulate ? 0 : a.fill_pieces * a.m;
+  a.fill_floats = a.rows == 0 ? 2048 : 32768;   // of workgroups of 256, 512 and 1024 threads
+  a.fill_pieces = (n + 31 + a.fill_floats - 1) / a.fill_floats;   // (31: a part's place in its first line)
+  const long long fills = a.accumulate ? 0 : a.fill_pieces * a.m;
   if (a.rows == 0) {
     if (fills > 0) embed_clear_kernel<<<(unsigned)fills, 256, 0, stream>>>(a);
     return hipGetLastError();

@@ -283,7 +283,7 @@ struct EmbedGradArgs {
   int* index[2];
   unsigned *count, *total;
   float* slots;
-  long long pieces, per_piece, fill_pieces;
+  long long pieces, per_piece, fill_pieces, fill_floats;
 };
 size_t embedding_workspace_bytes(int rows, int vocab, int width, int m);
 hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream_t stream);
