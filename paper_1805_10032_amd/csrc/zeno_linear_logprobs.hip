@@ -315,7 +315,7 @@ __device__ inline Place place_of(unsigned id, unsigned tiles_m, unsigned tiles_n
   return p;
 }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 __device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // What the logits' kernels share: A = rows of W from the vocabulary's `v0` on, B = h.
@@ -366,9 +366,6 @@ __device__ inline void logits_of(const Bias<S>& bias, const f32x16 (&acc)[S::FM]
 #pragma unroll
     for (int e = 0; e < 16; ++e) z[r][e] = acc[r][j][e] + bias.b[r][e];
 }
-// exp(z - x) as 2^(L z - c) 2^(c - L x), c = L x rounded: one FMA a value, and the second factor once.  Beyond kNear that factor says nothing.
-constexpr float kNear = 0x1p20f;
-
 // ---- forward: for each token and each slice of 32 FM values (max, sum of exp(z - max)) and, for the entropy, the sum of exp(z - max) (z - max)
 // A lane's share of FM blocks of logits of one token, which lane ^ 32 has the other share of, as a slice's sums at `at`; `hit`: the label's place in the
 // slice, of which `inside` values exist.
@@ -382,42 +379,24 @@ __device__ inline void leave_stats(const float (&z)[FM][16], int lane, int token
     for (int e = 0; e < 16; ++e) top = fmaxf(top, z[r][e]);
   top = fmaxf(top, __shfl_xor(top, 32));
   const float from = top == -__builtin_inff() ? 0.f : top;
-  float s, u = 0.f;
-  {
-    const float c = from * kLog2e, off = -fmaf(from, kLog2e, -c), scale = __builtin_amdgcn_exp2f(off);
-    float part[2] = {};
-    if (part_u == nullptr) {
-#pragma unroll
-      for (int r = 0; r < FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) part[e % 2] += __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c));
-    } else {
-#pragma unroll
-      for (int r = 0; r < FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {   // (where the exponential is 0, its argument is cut off: 0 * -inf would be NaN)
-          const float d = fmaf(z[r][e], kLog2e, -c), x = __builtin_amdgcn_exp2f(d);
-          part[e % 2] += x;
-          u = fmaf(x, fmaxf(d, -256.f), u);
-        }
-      u = fmaf(off, part[0] + part[1], u) * (scale * kLn2);
-    }
-    s = (part[0] + part[1]) * scale;
-  }
-  const bool far = !(fabsf(from) <= kNear);
-  if (__any(far)) {   // (for these tokens alone: another token's logits do not show)
-    float far_s = 0.f, far_u = 0.f;
+  // (the largest value's exponential is 1, to the bit: of a token that is nearly certain, what is left counts)
+  float part[2] = {}, u = 0.f;
+  if (part_u == nullptr) {
 #pragma unroll
     for (int r = 0; r < FM; ++r)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = 0; e < 16; ++e) part[e % 2] += exp_fast(z[r][e] - from);
+  } else {
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {   // (where the exponential is 0, its argument is cut off: 0 * -inf would be NaN)
         const float d = z[r][e] - from, x = exp_fast(d);
-        far_s += x;
-        far_u += x > 0.f ? x * d : 0.f;
+        part[e % 2] += x;
+        u = fmaf(x, fmaxf(d, -256.f), u);
       }
-    s = far ? far_s : s;
-    u = far ? far_u : u;
   }
+  float s = part[0] + part[1];
   s += __shfl_xor(s, 32);
   if (part_u != nullptr) u += __shfl_xor(u, 32);
   if (live && lane < 32) {
@@ -478,13 +457,9 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_
 // bytes of a row in a run, so a load has sixteen pieces to fetch (32 x 32: 64 pieces of 16 bytes, and 1 x 32000 x 4096 bf16 took 56 us).  Which values of the
 // contraction an instruction multiplies does not matter as long as both operands agree.
 struct FewArgs {
-  const void *hidden, *weight;
+  const void *hidden, *weight;   // weight: from the vocabulary's v0 on
   long long ldh, ldw;
-  int rows, vocab, width;
-  const float* bias;
-  const int32_t* labels;
-  float2* part;          // slices of 32 values
-  float *part_u, *label_logit;
+  int rows, values, width;       // values: of the vocabulary in this launch
 };
 // Up to which number of tokens: 16-bit operands are as fast in tiles of 128 tokens from 65 on (32000 x 4096: 64 tokens 74 us here, 65 there 69); float32,
 // which tiles take in six products, from 257 on (1024 columns: 256 tokens 209 us here, 250 there 211; 4096 columns 832 and 939).
@@ -513,19 +488,20 @@ __device__ inline f32x4 multiply_piece(Piece<T> a, Piece<T> b, f32x4 c) {
   }
   return c;
 }
-// 16 R rows of W, a multiple of 32; 16 FN tokens from 16 FN blockIdx.y on
+// 16 R rows of W, a multiple of 32, from v on times 16 FN tokens from token0 on: sums[wave][row][token] of the waves' shares.
+template <int R, int FN>
+using FewSums = float[kFewWaves][16 * R][16 * FN + 1];
 template <typename T, int R, int FN>
-__global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
-  __shared__ float shared[kFewWaves][16 * R][16 * FN + 1];
+__device__ inline void few_products(const FewArgs& a, FewSums<R, FN>& shared, int v, int token0) {
   constexpr int N = Wide<T>::N, STEP = 8 * N;   // of the contraction: 128 bytes of a row, two pieces a lane
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int steps = (a.width + STEP - 1) / STEP, begin = steps * wave / kFewWaves, end = steps * (wave + 1) / kFewWaves;
   const int from = lane / 16 * N;
   const T *w[R], *h[FN];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = v + 16 * r + lane % 16;   // (behind the last: the last once more)
-    w[r] = reinterpret_cast<const T*>(a.weight) + (row < a.vocab ? row : a.vocab - 1) * a.ldw + from;
+    w[r] = reinterpret_cast<const T*>(a.weight) + (row < a.values ? row : a.values - 1) * a.ldw + from;
   }
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
@@ -574,30 +550,39 @@ __global__ __launch_bounds__(64 * kFewWaves) void logit_few_kernel(FewArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) shared[wave][16 * r + 4 * (lane / 16) + e][16 * j + lane % 16] = acc[r][j][e];
   __syncthreads();
-  // 32 rows and 32 tokens a wave at a time
+}
+// A wave's 32 rows and 32 tokens: logits as a 32 x 32 block holds them, the vocabulary's from v on.
+template <int R, int FN>
+__device__ inline void few_logits(const FewSums<R, FN>& shared, int row0, int here, int lane, int v, int vocab, const float* bias, float (&z)[1][16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int row = row0 + row_of(e, lane), at = v + row_of(e, lane);
+    float sum = shared[0][row][here];
+#pragma unroll
+    for (int p = 1; p < kFewWaves; ++p) sum += shared[p][row][here];
+    z[0][e] = at < vocab ? sum + (bias != nullptr ? bias[at] : 0.f) : -__builtin_inff();
+  }
+}
+template <typename T, int R, int FN>
+__global__ __launch_bounds__(64 * kFewWaves) void few_stats_kernel(FewArgs a, StatArgs s) {
+  __shared__ FewSums<R, FN> shared;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
+  few_products<T, R, FN>(a, shared, v, token0);
   constexpr int TOKENS = (16 * FN + 31) / 32;
   for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
-    const int v32 = v + 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, here = t32 < 16 * FN ? t32 : 16 * FN - 1;
+    const int row0 = 32 * (block / TOKENS), v32 = v + row0, t32 = 32 * (block % TOKENS) + lane % 32, token = token0 + t32;
     float z[1][16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int row = v32 - v + row_of(e, lane), at = v + row;
-      float sum = shared[0][row][here];
-#pragma unroll
-      for (int p = 1; p < kFewWaves; ++p) sum += shared[p][row][here];
-      z[0][e] = at < a.vocab ? sum + (a.bias != nullptr ? a.bias[at] : 0.f) : -__builtin_inff();
-    }
-    const int token = token0 + t32;
+    few_logits<R, FN>(shared, row0, t32 < 16 * FN ? t32 : 16 * FN - 1, lane, v32, s.l.vocab, s.l.bias, z);
     const bool live = t32 < 16 * FN && token < a.rows;
-    const int hit = live && a.labels != nullptr ? a.labels[token] - v32 : -1;
-    leave_stats<1>(z, lane, token, live, hit, a.vocab - v32, (long long)(v32 / 32) * a.rows + token, a.part, a.part_u, a.label_logit);
+    const int hit = live && s.l.labels != nullptr ? s.l.labels[token] - v32 : -1;
+    leave_stats<1>(z, lane, token, live, hit, s.l.vocab - v32, (long long)(v32 / 32) * a.rows + token, s.part, s.part_u, s.label_logit);
   }
 }
 template <typename T>
-hipError_t start_few(const FewArgs& a, hipStream_t stream) {
-  if (a.rows <= 16) logit_few_kernel<T, 2, 1><<<(unsigned)ceil_div(a.vocab, 32), 64 * kFewWaves, 0, stream>>>(a);
-  else if (a.rows <= 32) logit_few_kernel<T, 4, 2><<<(unsigned)ceil_div(a.vocab, 64), 64 * kFewWaves, 0, stream>>>(a);
-  else logit_few_kernel<T, 4, 4><<<dim3((unsigned)ceil_div(a.vocab, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a);
+hipError_t start_few(const FewArgs& a, const StatArgs& s, hipStream_t stream) {
+  if (a.rows <= 16) few_stats_kernel<T, 2, 1><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, s);
+  else if (a.rows <= 32) few_stats_kernel<T, 4, 2><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, s);
+  else few_stats_kernel<T, 4, 4><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, s);
   return hipGetLastError();
 }
 
@@ -837,6 +822,97 @@ struct DzArgs {
 // Planes of dz.
 enum Planes { kBf16Three, kBf16AndHalf, kHalfTwo };   // three bf16 pieces; one bf16, and two fp16 pieces; two fp16 pieces
 __host__ __device__ constexpr int count_of(Planes p) { return p == kHalfTwo ? 2 : 3; }
+// A token, as far as its gradients need it.
+struct TokenGrad {
+  float M, log_s;        // of its logits
+  float g, q, H;         // gradients of its log probability and of its entropy, its entropy
+  int y;                 // its label, -1: none
+};
+__device__ inline TokenGrad token_grad(const LogitArgs& l, const float* stats, const float* grad_logp, const float* entropy, const float* grad_entropy,
+                                       int token) {
+  TokenGrad t = {-__builtin_inff(), 0.f, 0.f, 0.f, 0.f, -1};   // behind the last: no distribution
+  if (token < l.rows) {
+    t.M = stats[2 * token];
+    t.log_s = stats[2 * token + 1];
+    if (grad_logp != nullptr) {
+      t.y = l.labels[token];
+      t.g = grad_logp[token];
+    }
+    if (grad_entropy != nullptr) {
+      t.q = grad_entropy[token];
+      t.H = entropy[token];
+    }
+  }
+  return t;
+}
+// dz times `up` in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a token that
+// is nearly certain; what it loses in the first plane goes to `rest`.
+template <int FM, Planes P>
+__device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab, float up, float* rest) {
+  const bool empty = t.M == -__builtin_inff() && t.log_s == 0.f;
+  const float g = t.y == -1 ? 0.f : (t.y >= 0 && t.y < vocab ? t.g : __builtin_nanf(""));
+  const float M = empty ? 0.f : t.M, log_s = empty ? __builtin_inff() : t.log_s;   // (empty: every probability is 0)
+  const int hit = t.y - v;
+  const bool here = hit >= 0 && hit < 32 * FM && t.y < vocab;
+  float own = 0.f;
+  if (__any(here)) {
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (hit == 32 * r + row_of(e, lane)) own = z[r][e];
+  }
+  if (with_entropy) {
+    const float base = fmaf(t.q, t.H, g);
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {   // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
+        const float lp = (z[r][e] - M) - log_s;
+        z[r][e] = -exp_fast(lp) * fmaf(t.q, fmaxf(lp, -256.f), base) * up;
+      }
+  } else {
+    const float base = -g * up;        // (up: a power of two)
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[r][e] = exp_fast((z[r][e] - M) - log_s) * base;
+  }
+  if (__any(here)) {
+    const float lp = (own - M) - log_s;
+    float d = -g * expm1f(lp);
+    if (with_entropy) d -= exp_fast(lp) * (t.q * (fmaxf(lp, -256.f) + t.H));
+    d = empty ? 0.f : d * up;
+#pragma unroll
+    for (int r = 0; r < FM; ++r)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (here && hit == 32 * r + row_of(e, lane)) {
+          z[r][e] = d;
+          if (P != kBf16Three) *rest = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
+        }
+  }
+}
+// Four values as their planes.
+template <Planes P>
+__device__ inline void planes_of_dz(const float* from, s16x4 (&out)[count_of(P)]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float d = from[i];
+#pragma unroll
+    for (int plane = 0; plane < count_of(P); ++plane) {
+      if (P == kHalfTwo || (P == kBf16AndHalf && plane > 0)) {
+        const _Float16 x = (_Float16)d;
+        out[plane][i] = __builtin_bit_cast(short, x);
+        d -= (float)x;
+      } else {
+        const __bf16 x = (__bf16)d;
+        out[plane][i] = __builtin_bit_cast(short, x);
+        if (P == kBf16Three) d -= (float)x;
+      }
+    }
+  }
+}
 template <typename S, bool HALF, Planes P>
 __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_kernel(DzArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
@@ -845,83 +921,19 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
   const int wm = (wave % S::WM) * (32 * S::FM), wn = (wave / S::WM) * (32 * S::FN), v = a.l.v0 + t.m * S::BM + wm;
   Bias<S> bias;   // (these arrive beside the operands)
   load_bias<S>(a.l, v, lane, bias);
-  float stat[S::FN][2], grad[S::FN][3];   // max and logarithm of the sum; gradients of logp and entropy, entropy
-  int label[S::FN];
+  TokenGrad token[S::FN];
 #pragma unroll
-  for (int j = 0; j < S::FN; ++j) {
-    const int token = t.n * S::BN + wn + 32 * j + lane % 32;
-    stat[j][0] = -__builtin_inff();
-    stat[j][1] = grad[j][0] = grad[j][1] = grad[j][2] = 0.f;
-    label[j] = -1;
-    if (token < a.l.rows) {
-      stat[j][0] = a.stats[2 * token];
-      stat[j][1] = a.stats[2 * token + 1];
-      if (a.grad_logp != nullptr) {
-        label[j] = a.l.labels[token];
-        grad[j][0] = a.grad_logp[token];
-      }
-      if (a.grad_entropy != nullptr) {
-        grad[j][1] = a.grad_entropy[token];
-        grad[j][2] = a.entropy[token];
-      }
-    }
-  }
+  for (int j = 0; j < S::FN; ++j)
+    token[j] = token_grad(a.l, a.stats, a.grad_logp, a.entropy, a.grad_entropy, t.n * S::BN + wn + 32 * j + lane % 32);
   const float up = P == kBf16Three ? 1.f : a.scale->up;
   f32x16 acc[S::FM][S::FN] = {};
   product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
-    const int token = t.n * S::BN + wn + 32 * j + lane % 32, y = label[j];
-    float M = stat[j][0], log_s = stat[j][1];
-    const bool empty = M == -__builtin_inff() && log_s == 0.f;
-    const float g = y == -1 ? 0.f : (y >= 0 && y < a.l.vocab ? grad[j][0] : __builtin_nanf(""));
-    if (empty) {
-      M = 0.f;
-      log_s = __builtin_inff();   // every probability is 0
-    }
     float z[S::FM][16];
     logits_of<S>(bias, acc, j, z);
-    if (a.grad_entropy != nullptr) {
-      const float q = grad[j][1], base = fmaf(q, grad[j][2], g);
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
-          const float lp = (z[r][e] - M) - log_s;
-          z[r][e] = -exp_fast(lp) * fmaf(q, fmaxf(lp, -256.f), base) * up;
-        }
-    } else {
-      const bool far = empty || !(fabsf(M) <= kNear);
-      const float c = fmaf(log_s, kLog2e, M * kLog2e), plain = -g * up;   // (up: a power of two)
-      const float base = plain * __builtin_amdgcn_exp2f(-fmaf(log_s, kLog2e, fmaf(M, kLog2e, -c)));
-      if (!__any(far)) {
-#pragma unroll
-        for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[r][e] = __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c)) * base;
-      } else {   // (for these tokens alone: another token's logits do not show)
-#pragma unroll
-        for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            z[r][e] = far ? exp_fast((z[r][e] - M) - log_s) * plain : __builtin_amdgcn_exp2f(fmaf(z[r][e], kLog2e, -c)) * base;
-      }
-    }
-    const int hit = y < a.l.vocab ? y - v : -1;
-    if (__any(hit >= 0 && hit < 32 * S::FM)) {
-      const float add = empty ? 0.f : g * up;
-#pragma unroll
-      for (int r = 0; r < S::FM; ++r)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (hit == 32 * r + row_of(e, lane)) {
-            const float d = z[r][e] + add;
-            z[r][e] = d;
-            if (P != kBf16Three) a.rest[token] = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
-          }
-    }
+    logit_grads<S::FM, P>(z, lane, token[j], a.grad_entropy != nullptr, v, a.l.vocab, up, a.rest + (t.n * S::BN + wn + 32 * j + lane % 32));
     // this block of every wave's tokens through LDS, so that rows leave in whole lines
     u16* tile = reinterpret_cast<u16*>(memory);
     constexpr int TOKENS = 32 * S::WN, PLANE = TOKENS * S::PITCH;
@@ -931,22 +943,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         s16x4 out[count_of(P)];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float d = z[r][4 * c + i];
-#pragma unroll
-          for (int plane = 0; plane < count_of(P); ++plane) {
-            if (P == kHalfTwo || (P == kBf16AndHalf && plane > 0)) {
-              const _Float16 x = (_Float16)d;
-              out[plane][i] = __builtin_bit_cast(short, x);
-              d -= (float)x;
-            } else {
-              const __bf16 x = (__bf16)d;
-              out[plane][i] = __builtin_bit_cast(short, x);
-              if (P == kBf16Three) d -= (float)x;
-            }
-          }
-        }
+        planes_of_dz<P>(z[r] + 4 * c, out);
         u16* to = tile + (32 * (wave / S::WM) + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane);
 #pragma unroll
         for (int plane = 0; plane < count_of(P); ++plane) *reinterpret_cast<s16x4*>(to + plane * PLANE) = out[plane];
@@ -962,6 +959,39 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
             *reinterpret_cast<const s16x8*>(tile + plane * PLANE + row * S::PITCH + col);
     }
   }
+}
+
+// The same of few tokens: the logits have to be the forward pass's to the bit, or a nearly certain token's gradient is the difference of two roundings.
+template <typename T, int R, int FN, Planes P>
+__global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(FewArgs a, DzArgs d) {
+  __shared__ FewSums<R, FN> shared;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
+  few_products<T, R, FN>(a, shared, v, token0);
+  const float up = P == kBf16Three ? 1.f : d.scale->up;
+  constexpr int TOKENS = (16 * FN + 31) / 32;
+  for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
+    const int row0 = 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, token = t32 < 16 * FN ? token0 + t32 : a.rows;
+    float z[1][16];
+    few_logits<R, FN>(shared, row0, t32 < 16 * FN ? t32 : 16 * FN - 1, lane, d.l.v0 + v + row0, d.l.vocab, d.l.bias, z);
+    logit_grads<1, P>(z, lane, token_grad(d.l, d.stats, d.grad_logp, d.entropy, d.grad_entropy, token), d.grad_entropy != nullptr, d.l.v0 + v + row0,
+                      d.l.vocab, up, d.rest + token);
+    if (token >= a.rows) continue;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      s16x4 out[count_of(P)];
+      planes_of_dz<P>(z[0] + 4 * c, out);
+#pragma unroll
+      for (int plane = 0; plane < count_of(P); ++plane)
+        *reinterpret_cast<s16x4*>(d.dz + plane * d.plane + token * d.ldz + v + row0 + row_of(4 * c, lane)) = out[plane];
+    }
+  }
+}
+template <typename T, Planes P>
+hipError_t start_few_dz(const FewArgs& a, const DzArgs& d, hipStream_t stream) {
+  if (a.rows <= 16) few_grad_kernel<T, 2, 1, P><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, d);
+  else if (a.rows <= 32) few_grad_kernel<T, 4, 2, P><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, d);
+  else few_grad_kernel<T, 4, 4, P><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, d);
+  return hipGetLastError();
 }
 
 // dh: a piece of the vocabulary, cut into `splits` of `per` values that different workgroups sum, each into its own slot.
@@ -1133,6 +1163,8 @@ struct Layout {
   }
 };
 
+bool few_tokens(int rows, int dtype) { return rows <= (dtype == ZENO_F32 ? kFewRowsF32 : kFewRows); }
+
 struct ForwardPlan {
   bool few, wide;
   int slice;          // values of the vocabulary in a slice
@@ -1143,7 +1175,7 @@ struct ForwardPlan {
 ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
   ForwardPlan p;
   p.block = std::min(rows, kRowBlock);
-  p.few = rows <= (dtype == ZENO_F32 ? kFewRowsF32 : kFewRows);
+  p.few = few_tokens(rows, dtype);
   p.wide = wide_tiles(vocab, p.block);
   p.slice = p.few ? 32 : (p.wide ? 32 * WideTile::FM : 32 * MidTile::FM);
   const long long padded = padded_width(width);
@@ -1160,7 +1192,7 @@ ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
 }
 
 struct BackwardPlan {
-  bool wide_logits, wide_hidden, wide_weight;
+  bool few, wide_logits, wide_hidden, wide_weight;
   int piece;          // values of the vocabulary at a time
   int planes;         // of dz
   int splits;
@@ -1174,6 +1206,7 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
   const long long pieces = (vocab + most - 1) / most;
   p.piece = (int)(((vocab + pieces - 1) / pieces + 255) / 256 * 256);
+  p.few = few_tokens(rows, dtype);
   p.wide_logits = wide_tiles(p.piece, n);
   p.wide_hidden = wide_tiles(n, width);
   p.wide_weight = wide_tiles((long long)p.piece * m, width) && n / m >= kLongGroup;
@@ -1275,8 +1308,11 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
   s.part_u = a.entropy != nullptr ? reinterpret_cast<float*>(ws + p.part_u) : nullptr;
   s.label_logit = reinterpret_cast<float*>(ws + p.label);
   if (p.few) {
-    const FewArgs f = {a.hidden, a.weight, a.ldh, a.ldw, a.rows, a.vocab, a.width, a.bias, a.labels, s.part, s.part_u, s.label_logit};
-    ZENO_STEP(a.dtype == ZENO_F32 ? start_few<float>(f, stream) : a.dtype == ZENO_BF16 ? start_few<__bf16>(f, stream) : start_few<_Float16>(f, stream));
+    const FewArgs f = {a.hidden, a.weight, a.ldh, a.ldw, a.rows, a.vocab, a.width};
+    s.l.vocab = a.vocab;
+    s.l.bias = a.bias;
+    s.l.labels = a.labels;
+    ZENO_STEP(a.dtype == ZENO_F32 ? start_few<float>(f, s, stream) : a.dtype == ZENO_BF16 ? start_few<__bf16>(f, s, stream) : start_few<_Float16>(f, s, stream));
     return join(s, 0, a.rows, a.rows <= 16 ? ceil_div(a.vocab, 32) : ceil_div(a.vocab, 64) * 2);   // (what the workgroups have left)
   }
   const bool half = a.dtype == ZENO_F16, direct = as_it_is(a.weight, a.ldw, a.dtype, a.width);
@@ -1359,13 +1395,20 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const int values = std::min(p.piece, a.vocab - v0);
     if (a.rows > 0) {
-      ZENO_STEP(side_of(reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v0 * a.ldw * bytes, a.ldw, a.dtype, values, a.width,
-                        reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
+      const void* weight = reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v0 * a.ldw * bytes;
+      if (!p.few || a.dhidden != nullptr)
+        ZENO_STEP(side_of(weight, a.ldw, a.dtype, values, a.width, reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
       l.v0 = v0;
-      const int side = p.wide_logits ? 256 : 128;
-      l.tiles_m = ceil_div(values, side);
-      l.tiles_n = ceil_div(a.rows, side);
-      ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<MidTile>(d, a.dtype, stream));
+      if (p.few) {
+        const FewArgs f = {a.hidden, weight, a.ldh, a.ldw, a.rows, values, a.width};
+        ZENO_STEP(a.dtype == ZENO_F32 ? (start_few_dz<float, kBf16Three>(f, d, stream))
+                                      : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16AndHalf>(f, d, stream)));
+      } else {
+        const int side = p.wide_logits ? 256 : 128;
+        l.tiles_m = ceil_div(values, side);
+        l.tiles_n = ceil_div(a.rows, side);
+        ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<MidTile>(d, a.dtype, stream));
+      }
       if (a.dhidden != nullptr) {
         HiddenArgs h = {};
         h.dz = {d.dz, d.ldz, d.plane, a.rows};
