@@ -329,6 +329,30 @@ struct LogitArgs {
 };
 // Row of a wave's 32 x 32 block that element e of a lane holds.
 __device__ inline int row_of(int e, int lane) { return 8 * (e / 4) + 4 * (lane / 32) + e % 4; }
+// The place 16 r + e of a row among FM blocks, if the lane holds it; -1 if it does not.
+template <int FM>
+__device__ inline int place_in(int row, int lane) {
+  const bool mine = row >= 0 && row < 32 * FM && (row / 4 & 1) == lane / 32;
+  return mine ? row / 32 * 16 + row % 32 / 8 * 4 + row % 4 : -1;
+}
+// The value at a place, and another one in it; a place of -1 is none.
+template <int FM>
+__device__ inline float value_at(const float (&z)[FM][16], int place) {
+  float v = 0.f;
+#pragma unroll
+  for (int r = 0; r < FM; ++r)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v = place == 16 * r + e ? z[r][e] : v;
+  return v;
+}
+template <int FM>
+__device__ inline void put_at(float (&z)[FM][16], int place, float v) {
+  asm volatile("" : "+v"(place));   // (or the comparisons of value_at() are kept for here, in registers that there are too few of)
+#pragma unroll
+  for (int r = 0; r < FM; ++r)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[r][e] = place == 16 * r + e ? v : z[r][e];
+}
 
 // The bias of a wave's rows from v on.  What lies behind the vocabulary gets -inf: its products are copies of the last row's, so this makes a NaN of
 // none that is not there.
@@ -403,19 +427,10 @@ __device__ inline void leave_stats(const float (&z)[FM][16], int lane, int token
     part_s[at] = make_float2(top, s);
     if (part_u != nullptr) part_u[at] = u;
   }
-  const bool here = hit >= 0 && hit < 32 * FM && hit < inside;
-  if (__any(here)) {
-    float mine_z = 0.f;
-    bool mine = false;
-#pragma unroll
-    for (int r = 0; r < FM; ++r)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (hit == 32 * r + row_of(e, lane)) {
-          mine_z = z[r][e];
-          mine = true;
-        }
-    if (here && mine && live) label_logit[token] = mine_z;
+  const int place = live && hit < inside ? place_in<FM>(hit, lane) : -1;
+  if (__any(place >= 0)) {
+    const float own = value_at<FM>(z, place);
+    if (place >= 0) label_logit[token] = own;
   }
 }
 
@@ -852,16 +867,9 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
   const bool empty = t.M == -__builtin_inff() && t.log_s == 0.f;
   const float g = t.y == -1 ? 0.f : (t.y >= 0 && t.y < vocab ? t.g : __builtin_nanf(""));
   const float M = empty ? 0.f : t.M, log_s = empty ? __builtin_inff() : t.log_s;   // (empty: every probability is 0)
-  const int hit = t.y - v;
-  const bool here = hit >= 0 && hit < 32 * FM && t.y < vocab;
-  float own = 0.f;
-  if (__any(here)) {
-#pragma unroll
-    for (int r = 0; r < FM; ++r)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (hit == 32 * r + row_of(e, lane)) own = z[r][e];
-  }
+  const int place = t.y < vocab ? place_in<FM>(t.y - v, lane) : -1;
+  const bool any = __any(place >= 0);
+  const float own = any ? value_at<FM>(z, place) : 0.f;
   if (with_entropy) {
     const float base = fmaf(t.q, t.H, g);
 #pragma unroll
@@ -878,19 +886,13 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
 #pragma unroll
       for (int e = 0; e < 16; ++e) z[r][e] = exp_fast((z[r][e] - M) - log_s) * base;
   }
-  if (__any(here)) {
+  if (any) {
     const float lp = (own - M) - log_s;
     float d = -g * expm1f(lp);
     if (with_entropy) d -= exp_fast(lp) * (t.q * (fmaxf(lp, -256.f) + t.H));
     d = empty ? 0.f : d * up;
-#pragma unroll
-    for (int r = 0; r < FM; ++r)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (here && hit == 32 * r + row_of(e, lane)) {
-          z[r][e] = d;
-          if (P != kBf16Three) *rest = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
-        }
+    put_at<FM>(z, place, d);
+    if (P != kBf16Three && place >= 0) *rest = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
   }
 }
 // Four values as their planes.
