@@ -233,3 +233,13 @@ def test_captured(B, rows):
         torch.cuda.synchronize()
         assert torch.equal(out, B.zeno_embedding(ids, table, scale=2.0))
         assert torch.equal(G, B.zeno_embedding_backward(dy, ids, vocab, scale=2.0, groups=groups))
+
+
+def test_lookup_of_a_large_output(B):
+    """160 MB on memory lines, which go past the caches."""
+    table = torch.randn(300, 4096, device="cuda")
+    ids = torch.randint(-1, 300, (20000,), device="cuda", dtype=torch.int32)
+    out = B.zeno_embedding(ids, table, torch.bfloat16, scale=4.0)
+    want = (table[ids.long().clamp(min=0)] * 4.0).bfloat16()
+    want[ids < 0] = 0
+    assert torch.equal(out, want)
