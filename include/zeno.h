@@ -381,9 +381,9 @@ zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* 
 /* Its gradients for gradients g of logp and q of the entropy, the vocabulary in pieces whose logits are formed again:
  *   dz_j = g [j = label] - p_j (g + q (log p_j + H)),   dhidden = dz weight,   dweight_g = sum of dz[t] hidden[t]^T over the rows of group g,
  *   dbias_g = sum of dz[t].
- * In 16-bit types dweight and dbias are taken from dz in two fp16 pieces (off by at most 2^-22 of it or 2^-38 of the largest gradient
- * of the call), and bf16 hidden states are exact in them down to 2^-32 of their column's largest; dhidden, which is rounded itself, is taken from dz rounded
- * to the type, but for the label's value.  In float32 dz is three bf16 pieces.
+ * In 16-bit types a group's dweight and dbias are taken from dz in two fp16 pieces (off by at most 2^-22 of it or 2^-38 of the largest gradient
+ * of the group), and bf16 hidden states are exact in them down to 2^-32 of the largest in their column and group; dhidden, which is rounded itself, is taken from
+ * dz rounded to the type, but for the label's value.  In float32 dz is three bf16 pieces.  One group's values do not show in another's gradients.
  *   stats, entropy  as zeno_linear_logprobs wrote them (entropy only if grad_entropy is given)
  *   labels, grad_logp        DEVICE [rows] or both NULL; a row with label -1 takes no part in g, another label outside 0..vocab-1 gives NaN
  *   grad_entropy             DEVICE [rows] or NULL

@@ -744,35 +744,50 @@ Pairs pairs_of(int a, int b) {   // planes of the two sides: three and three, tw
 struct GradScale {
   float up, down;   // what dz is multiplied by on its way into 16 bits, and the products by on their way out
 };
-// 16-bit types keep dz within 2^14: a power of two of the largest gradient that a token brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
-// p H <= ln V < 21).  float32's pieces have its range.  `clear`: `n` words to set to zero on the way.
-__global__ __launch_bounds__(1024) void grad_scale_kernel(const float* g, const float* q, const int32_t* labels, int rows, int scaled, GradScale* out,
-                                                         unsigned* clear, int n) {
+// 16-bit types keep a worker's dz within 2^14: a power of two of the largest gradient that one of its tokens brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
+// p H <= ln V < 21).  float32's pieces have its range.  One workgroup a worker: another's gradients, or those of nobody, do not show.  `clear`: a worker's n
+// words to set to zero on the way.
+struct ScaleArgs {
+  const float *g, *q;
+  const int32_t *labels, *offsets;
+  int rows, scaled;
+  GradScale* group;      // [m]
+  float* up;             // [rows]
+  unsigned* clear;
+  int n;
+};
+__global__ __launch_bounds__(1024) void grad_scale_kernel(ScaleArgs a) {
   __shared__ float shared[16];
+  __shared__ GradScale all;
+  const int worker = blockIdx.x, begin = group_offset(a.offsets, worker, a.rows), end = group_offset(a.offsets, worker + 1, a.rows);
   float largest = 0.f;
-  for (int i = threadIdx.x; i < n; i += 1024) clear[i] = 0;
-  if (scaled)
-    for (int t = threadIdx.x; t < rows; t += 1024) {
-      float b = g != nullptr && labels[t] != -1 ? fabsf(g[t]) : 0.f;
-      if (q != nullptr) b += 22.f * fabsf(q[t]);
+  for (int i = threadIdx.x; i < a.n; i += 1024) a.clear[(long long)worker * a.n + i] = 0;
+  if (a.scaled)
+    for (int t = begin + threadIdx.x; t < end; t += 1024) {
+      float b = a.g != nullptr && a.labels[t] != -1 ? fabsf(a.g[t]) : 0.f;
+      if (a.q != nullptr) b += 22.f * fabsf(a.q[t]);
       if (b < __builtin_inff()) largest = fmaxf(largest, b);
     }
   largest = wave_max_f(largest);
   if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = largest;
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int w = 1; w < 16; ++w) largest = fmaxf(largest, shared[w]);
-  int up = 0;
-  if (largest > 0.f) {
-    const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126;   // largest < 2^e
-    up = 14 - e;
-    up = up > 100 ? 100 : (up < -100 ? -100 : up);
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 16; ++w) largest = fmaxf(largest, shared[w]);
+    int up = 0;
+    if (largest > 0.f) {
+      const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126;   // largest < 2^e
+      up = 14 - e;
+      up = up > 100 ? 100 : (up < -100 ? -100 : up);
+    }
+    all.up = __uint_as_float((unsigned)(127 + up) << 23);
+    all.down = __uint_as_float((unsigned)(127 - up) << 23);
+    a.group[worker] = all;
   }
-  out->up = __uint_as_float((unsigned)(127 + up) << 23);
-  out->down = __uint_as_float((unsigned)(127 - up) << 23);
+  __syncthreads();
+  for (int t = begin + threadIdx.x; t < end; t += 1024) a.up[t] = all.up;
 }
 
-// bf16 hidden states as fp16, each column times the power of two that brings its largest finite value to 2^14 .. 2^15: exact down to 2^-32
+// bf16 hidden states as fp16, each column of a worker times the power of two that brings its largest finite value to 2^14 .. 2^15: exact down to 2^-32
 // of that value.
 __device__ inline int column_power(unsigned largest) {   // largest magnitude, as float32 bits
   if (largest == 0) return 0;
@@ -782,54 +797,86 @@ __device__ inline int column_power(unsigned largest) {   // largest magnitude, a
 __host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
 __device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
 constexpr int kColumnRows = 256;   // of a workgroup
-__global__ __launch_bounds__(1024) void column_max_kernel(Side h, int width, unsigned* largest) {
+struct ColumnArgs {
+  Side h;
+  int width, m, rows;
+  const int32_t* offsets;
+  unsigned* largest;     // [m][width]
+  u16* out;
+};
+// The worker of a row (of one that belongs to somebody): the last that begins there or before.
+__device__ inline int worker_of(const int32_t* offsets, int m, int row) {
+  if (offsets == nullptr) return 0;
+  int lo = 0, hi = m;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (offsets[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__global__ __launch_bounds__(1024) void column_max_kernel(ColumnArgs a) {
   __shared__ unsigned shared[16][512];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = blockIdx.x * 512 + lane * 8;
-  unsigned m[8] = {};
-  const int begin = blockIdx.y * kColumnRows, end = begin + kColumnRows < h.extent ? begin + kColumnRows : h.extent;
-  if (col < width) {
+  const int from = group_offset(a.offsets, 0, a.rows), until = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
+  const int begin = max((int)blockIdx.y * kColumnRows, from), end = min((int)(blockIdx.y + 1) * kColumnRows, until);
+  if (begin >= end) return;
+  const int first = worker_of(a.offsets, a.m, begin), last = worker_of(a.offsets, a.m, end - 1);
+  for (int g = first; g <= last; ++g) {   // (most often one)
+    const int lo = max(begin, group_offset(a.offsets, g, a.rows)), hi = min(end, group_offset(a.offsets, g + 1, a.rows));
+    unsigned m[8] = {};
+    if (col < a.width) {
 #pragma unroll 4
-    for (int row = begin + wave; row < end; row += 16) {
-      const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
+      for (int row = lo + wave; row < hi; row += 16) {
+        const s16x8 raw = *reinterpret_cast<const s16x8*>(a.h.p + row * a.h.ld + col);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned v = (unsigned)raw[j] & 0x7fff;
-        m[j] = v < 0x7f80 && v > m[j] ? v : m[j];
+        for (int j = 0; j < 8; ++j) {
+          const unsigned v = (unsigned)raw[j] & 0x7fff;
+          m[j] = v < 0x7f80 && v > m[j] ? v : m[j];
+        }
       }
     }
-  }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) shared[wave][8 * lane + j] = m[j];
-  __syncthreads();
-  if (threadIdx.x >= 512) return;
-  unsigned most = 0;
-  for (int w = 0; w < 16; ++w) most = shared[w][threadIdx.x] > most ? shared[w][threadIdx.x] : most;
-  if (most != 0 && blockIdx.x * 512 + threadIdx.x < width) atomicMax(&largest[blockIdx.x * 512 + threadIdx.x], most << 16);
-}
-__global__ __launch_bounds__(1024) void column_half_kernel(Side h, int width, const unsigned* largest, u16* out) {
-  const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
-  if (col >= width) return;
-  float up[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) up[j] = power_of_two(column_power(col + j < width ? largest[col + j] : 0));
-  const int begin = blockIdx.y * kColumnRows, end = begin + kColumnRows < h.extent ? begin + kColumnRows : h.extent;
-#pragma unroll 4
-  for (int row = begin + threadIdx.x / 64; row < end; row += 16) {
-    const s16x8 raw = *reinterpret_cast<const s16x8*>(h.p + row * h.ld + col);
-    s16x8 half;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const short bits = raw[j];
-      half[j] = __builtin_bit_cast(short, (_Float16)(__uint_as_float((unsigned)(u16)bits << 16) * up[j]));
+    for (int j = 0; j < 8; ++j) shared[wave][8 * lane + j] = m[j];
+    __syncthreads();
+    if (threadIdx.x < 512) {
+      unsigned most = 0;
+      for (int w = 0; w < 16; ++w) most = shared[w][threadIdx.x] > most ? shared[w][threadIdx.x] : most;
+      const int c = blockIdx.x * 512 + threadIdx.x;
+      if (most != 0 && c < a.width) atomicMax(&a.largest[(long long)g * a.width + c], most << 16);
     }
-    *reinterpret_cast<s16x8*>(out + (long long)row * padded_stride(width) + col) = half;
+    __syncthreads();
+  }
+}
+__global__ __launch_bounds__(1024) void column_half_kernel(ColumnArgs a) {
+  const int col = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
+  const int from = group_offset(a.offsets, 0, a.rows), until = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
+  const int begin = max((int)blockIdx.y * kColumnRows, from), end = min((int)(blockIdx.y + 1) * kColumnRows, until);
+  if (col >= a.width || begin >= end) return;
+  const int first = worker_of(a.offsets, a.m, begin), last = worker_of(a.offsets, a.m, end - 1);
+  for (int g = first; g <= last; ++g) {
+    const int lo = max(begin, group_offset(a.offsets, g, a.rows)), hi = min(end, group_offset(a.offsets, g + 1, a.rows));
+    float up[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) up[j] = power_of_two(column_power(col + j < a.width ? a.largest[(long long)g * a.width + col + j] : 0));
+#pragma unroll 4
+    for (int row = lo + threadIdx.x / 64; row < hi; row += 16) {
+      const s16x8 raw = *reinterpret_cast<const s16x8*>(a.h.p + row * a.h.ld + col);
+      s16x8 half;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const short bits = raw[j];
+        half[j] = __builtin_bit_cast(short, (_Float16)(__uint_as_float((unsigned)(u16)bits << 16) * up[j]));
+      }
+      *reinterpret_cast<s16x8*>(a.out + (long long)row * padded_stride(a.width) + col) = half;
+    }
   }
 }
 
 struct DzArgs {
   LogitArgs l;
   const float *stats, *grad_logp, *entropy, *grad_entropy;
-  const GradScale* scale;
+  const float* up;       // [rows]
   u16* dz;               // [planes][rows][ldz]
   long long ldz, plane;
   float* rest;           // [rows] what the label's value loses in the first plane, or nullptr
@@ -842,28 +889,30 @@ struct TokenGrad {
   float M, log_s;        // of its logits
   float g, q, H;         // gradients of its log probability and of its entropy, its entropy
   int y;                 // its label, -1: none
+  float up;              // what its dz is multiplied by
 };
-__device__ inline TokenGrad token_grad(const LogitArgs& l, const float* stats, const float* grad_logp, const float* entropy, const float* grad_entropy,
-                                       int token) {
-  TokenGrad t = {-__builtin_inff(), 0.f, 0.f, 0.f, 0.f, -1};   // behind the last: no distribution
-  if (token < l.rows) {
-    t.M = stats[2 * token];
-    t.log_s = stats[2 * token + 1];
-    if (grad_logp != nullptr) {
-      t.y = l.labels[token];
-      t.g = grad_logp[token];
+__device__ inline TokenGrad token_grad(const DzArgs& a, int token) {
+  TokenGrad t = {-__builtin_inff(), 0.f, 0.f, 0.f, 0.f, -1, 0.f};   // behind the last: no distribution
+  if (token < a.l.rows) {
+    t.M = a.stats[2 * token];
+    t.log_s = a.stats[2 * token + 1];
+    t.up = a.up[token];
+    if (a.grad_logp != nullptr) {
+      t.y = a.l.labels[token];
+      t.g = a.grad_logp[token];
     }
-    if (grad_entropy != nullptr) {
-      t.q = grad_entropy[token];
-      t.H = entropy[token];
+    if (a.grad_entropy != nullptr) {
+      t.q = a.grad_entropy[token];
+      t.H = a.entropy[token];
     }
   }
   return t;
 }
-// dz times `up` in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a token that
+// dz, scaled, in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a token that
 // is nearly certain; what it loses in the first plane goes to `rest`.
 template <int FM, Planes P>
-__device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab, float up, float* rest) {
+__device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab, float* rest) {
+  const float up = P == kBf16Three ? 1.f : t.up;       // (a power of two)
   const bool empty = t.M == -__builtin_inff() && t.log_s == 0.f;
   const float g = t.y == -1 ? 0.f : (t.y >= 0 && t.y < vocab ? t.g : __builtin_nanf(""));
   const float M = empty ? 0.f : t.M, log_s = empty ? __builtin_inff() : t.log_s;   // (empty: every probability is 0)
@@ -880,7 +929,7 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
         z[r][e] = -exp_fast(lp) * fmaf(t.q, fmaxf(lp, -256.f), base) * up;
       }
   } else {
-    const float base = -g * up;        // (up: a power of two)
+    const float base = -g * up;
 #pragma unroll
     for (int r = 0; r < FM; ++r)
 #pragma unroll
@@ -926,8 +975,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
   TokenGrad token[S::FN];
 #pragma unroll
   for (int j = 0; j < S::FN; ++j)
-    token[j] = token_grad(a.l, a.stats, a.grad_logp, a.entropy, a.grad_entropy, t.n * S::BN + wn + 32 * j + lane % 32);
-  const float up = P == kBf16Three ? 1.f : a.scale->up;
+    token[j] = token_grad(a, t.n * S::BN + wn + 32 * j + lane % 32);
   f32x16 acc[S::FM][S::FN] = {};
   product<S, HALF, false, false>(a.l.w, a.l.h, a.l.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, 0, a.l.width, memory, acc);
 #pragma unroll
@@ -935,7 +983,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_k
     __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
     float z[S::FM][16];
     logits_of<S>(bias, acc, j, z);
-    logit_grads<S::FM, P>(z, lane, token[j], a.grad_entropy != nullptr, v, a.l.vocab, up, a.rest + (t.n * S::BN + wn + 32 * j + lane % 32));
+    logit_grads<S::FM, P>(z, lane, token[j], a.grad_entropy != nullptr, v, a.l.vocab, a.rest + (t.n * S::BN + wn + 32 * j + lane % 32));
     // this block of every wave's tokens through LDS, so that rows leave in whole lines
     u16* tile = reinterpret_cast<u16*>(memory);
     constexpr int TOKENS = 32 * S::WN, PLANE = TOKENS * S::PITCH;
@@ -969,14 +1017,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(FewArgs a, DzA
   __shared__ FewSums<R, FN> shared;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
   few_products<T, R, FN>(a, shared, v, token0);
-  const float up = P == kBf16Three ? 1.f : d.scale->up;
   constexpr int TOKENS = (16 * FN + 31) / 32;
   for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
     const int row0 = 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, token = t32 < 16 * FN ? token0 + t32 : a.rows;
     float z[1][16];
     few_logits<R, FN>(shared, row0, t32 < 16 * FN ? t32 : 16 * FN - 1, lane, d.l.v0 + v + row0, d.l.vocab, d.l.bias, z);
-    logit_grads<1, P>(z, lane, token_grad(d.l, d.stats, d.grad_logp, d.entropy, d.grad_entropy, token), d.grad_entropy != nullptr, d.l.v0 + v + row0,
-                      d.l.vocab, up, d.rest + token);
+    logit_grads<1, P>(z, lane, token_grad(d, token), d.grad_entropy != nullptr, d.l.v0 + v + row0, d.l.vocab, d.rest + token);
     if (token >= a.rows) continue;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -1034,7 +1080,7 @@ struct HiddenJoinArgs {
   const float* slots;
   int splits, rows, width, vocab, m;
   const int32_t *offsets, *labels;
-  const GradScale* scale;
+  const float* up;       // [rows] or nullptr
   const float* rest;     // or nullptr
   const void* weight;
   long long ldw;
@@ -1045,8 +1091,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
   const int lo = group_offset(a.offsets, 0, a.rows), hi = group_offset(a.offsets, a.offsets == nullptr ? 1 : a.m, a.rows);
   const long long stride = (long long)a.rows * a.width;
-  const float down = a.scale->down;
   for (int row = lo + blockIdx.y; row < hi; row += gridDim.y) {
+    const float down = a.up != nullptr ? 1.f / a.up[row] : 1.f;   // (a power of two: exact)
     const int y = a.rest != nullptr ? a.labels[row] : -1;
     const bool has = y >= 0 && y < a.vocab;
     const float rest = has ? a.rest[row] : 0.f;
@@ -1087,7 +1133,7 @@ struct WeightArgs {
   Pairs pairs;
   int tiles_m, tiles_n, rows, width, values;   // values: of the vocabulary in this piece
   const int32_t* offsets;
-  const GradScale* scale;
+  const GradScale* scale;    // [m]
   const unsigned* columns;   // largest values of the columns of h that have been scaled by column_power(), or nullptr
   float *dweight, *dbias;   // at the piece's first value; each may be nullptr
   long long ldw, ldb;
@@ -1100,7 +1146,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_
   f32x16 acc[S::FM][S::FN] = {};
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, length = end > begin ? end - begin : 0;
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
-  const float down = HALF ? a.scale->down : 1.f;
+  const float down = HALF ? a.scale[g].down : 1.f;
   if (a.dbias != nullptr && t.n == 0) {
     f32x16 sums[S::FM / S::WN] = {};
     product<S, HALF, true, true, HALF ? 2 : 1, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, 0, begin, length, memory, acc, sums);
@@ -1124,7 +1170,7 @@ __global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     const int col = col0 + 32 * j;
-    const float back = HALF && a.columns != nullptr && col < a.width ? power_of_two(-column_power(a.columns[col])) : 1.f;
+    const float back = HALF && a.columns != nullptr && col < a.width ? power_of_two(-column_power(a.columns[(long long)g * a.width + col])) : 1.f;
     float* to = dw + (long long)row0 * a.width + col;
     if (past) {
 #pragma unroll
@@ -1198,7 +1244,7 @@ struct BackwardPlan {
   int piece;          // values of the vocabulary at a time
   int planes;         // of dz
   int splits;
-  size_t hidden, weight, dz, slots, scale, rest, half, columns, bytes;
+  size_t hidden, weight, dz, slots, scale, up, rest, half, columns, bytes;
 };
 BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   BackwardPlan p;
@@ -1220,10 +1266,11 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   p.weight = l.take((size_t)planes_of(dtype) * p.piece * padded * 2);
   p.dz = l.take((size_t)p.planes * n * p.piece * 2);
   p.slots = l.take((size_t)p.splits * n * width * 4);
-  p.scale = l.take(256);
+  p.scale = l.take((size_t)m * sizeof(GradScale));
+  p.up = l.take((size_t)n * 4);
   p.rest = l.take((size_t)n * 4);
   p.half = l.take(dtype == ZENO_BF16 ? (size_t)n * padded * 2 : 0);
-  p.columns = l.take((size_t)width * 4);
+  p.columns = l.take(dtype == ZENO_BF16 ? (size_t)m * width * 4 : 0);
   p.bytes = l.at + 256;
   return p;
 }
@@ -1362,7 +1409,9 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   GradScale* scale = reinterpret_cast<GradScale*>(ws + p.scale);
   const bool convert = a.dtype == ZENO_BF16 && (a.dweight != nullptr || a.dbias != nullptr) && a.rows > 0;
   unsigned* columns = reinterpret_cast<unsigned*>(ws + p.columns);
-  grad_scale_kernel<<<1, 1024, 0, stream>>>(a.grad_logp, a.grad_entropy, a.labels, a.rows, planes == 1 ? 1 : 0, scale, columns, convert ? a.width : 0);
+  float* up = reinterpret_cast<float*>(ws + p.up);
+  const ScaleArgs sc = {a.grad_logp, a.grad_entropy, a.labels, a.offsets, a.rows, planes == 1 ? 1 : 0, scale, up, columns, convert ? a.width : 0};
+  grad_scale_kernel<<<a.m, 1024, 0, stream>>>(sc);
   ZENO_STEP(hipGetLastError());
   DzArgs d = {};
   LogitArgs& l = d.l;
@@ -1378,8 +1427,9 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   if (convert) {
     const dim3 grid((unsigned)ceil_div(a.width, 512), (unsigned)ceil_div(a.rows, kColumnRows));
     hidden = {reinterpret_cast<const u16*>(ws + p.half), l.width, 0, a.rows};
-    column_max_kernel<<<grid, 1024, 0, stream>>>(l.h, a.width, columns);
-    column_half_kernel<<<grid, 1024, 0, stream>>>(l.h, a.width, columns, reinterpret_cast<u16*>(ws + p.half));
+    const ColumnArgs c = {l.h, a.width, a.m, a.rows, a.offsets, columns, reinterpret_cast<u16*>(ws + p.half)};
+    column_max_kernel<<<grid, 1024, 0, stream>>>(c);
+    column_half_kernel<<<grid, 1024, 0, stream>>>(c);
     ZENO_STEP(hipGetLastError());
   }
   d.rest = planes == 1 ? reinterpret_cast<float*>(ws + p.rest) : nullptr;
@@ -1387,7 +1437,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   d.grad_logp = a.grad_logp;
   d.entropy = a.entropy;
   d.grad_entropy = a.grad_entropy;
-  d.scale = scale;
+  d.up = up;
   d.dz = reinterpret_cast<u16*>(ws + p.dz);
   d.ldz = p.piece;
   d.plane = (long long)a.rows * p.piece;
@@ -1454,8 +1504,8 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
     }
   }
   if (a.dhidden != nullptr && a.rows > 0) {
-    const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.vocab, a.m, a.offsets, a.labels, scale,
-                              a.grad_logp != nullptr ? d.rest : nullptr, a.weight, a.ldw, a.dhidden, a.lddh};
+    const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.vocab, a.m, a.offsets, a.labels,
+                              planes == 1 ? up : nullptr, a.grad_logp != nullptr ? d.rest : nullptr, a.weight, a.ldw, a.dhidden, a.lddh};
     const dim3 grid((unsigned)std::min(ceil_div(a.width, 1024), 64), (unsigned)std::min(a.rows, 16384));
     if (a.dtype == ZENO_F32) hidden_join_kernel<float><<<grid, 256, 0, stream>>>(j);
     else if (half) hidden_join_kernel<_Float16><<<grid, 256, 0, stream>>>(j);

@@ -368,3 +368,34 @@ def test_captured(B, ty):
         eager = [torch.full_like(t, float("nan")) for t in out]
         call(eager, [torch.empty_like(x) for x in ws])
         assert all(torch.equal(x, y) for x, y in zip(out, eager))
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("rows,vocab,width", [(40, 300, 64), (600, 700, 136)])
+def test_one_groups_values_do_not_show_in_anothers_gradients(B, rows, vocab, width, ty):
+    """Bit for bit, however large the gradients and hidden states of another group, or of rows that belong to nobody, are."""
+    h, w, b, labels = problem(rows, vocab, width, TYPES[ty], 5)
+    offsets = [3, rows // 3, rows // 3, rows // 2 + 1, rows - 4]
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    g = torch.randn(rows, device="cuda")
+    q = torch.randn(rows, device="cuda")
+
+    def gradients(h, g, q):
+        _, entropy, stats = B.zeno_linear_logprobs(h, w, b, labels, want_entropy=True, want_stats=True)
+        G = torch.full((4, vocab * width + vocab), 3.0, device="cuda")
+        dh = torch.full_like(h, 5.0)
+        B.zeno_linear_logprobs_backward(h, w, b, stats, labels=labels, grad_logp=g, entropy=entropy, grad_entropy=q, groups=off, dhidden=dh,
+                                        dweight=G[:, :vocab * width], dbias=G[:, vocab * width:])
+        return G, dh
+    G, dh = gradients(h, g, q)
+    other = torch.ones(rows, dtype=torch.bool, device="cuda")
+    other[offsets[2]:offsets[3]] = False
+    for factor, gradient in ((2.0 ** 10, 2.0 ** 40), (1.0, float("inf")), (float("nan"), float("nan"))):
+        h2, g2, q2 = h.clone(), g.clone(), q.clone()
+        h2[other] *= factor
+        g2[other] *= gradient
+        q2[other] *= gradient
+        G2, dh2 = gradients(h2, g2, q2)
+        assert torch.equal(G2[2], G[2]), (factor, gradient)
+        assert torch.equal(dh2[~other], dh[~other]), (factor, gradient)
+        assert (G2[1] == 0).all() and torch.equal(dh2[:3], dh[:3]) and torch.equal(dh2[-4:], dh[-4:])
