@@ -28,21 +28,25 @@ typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
 constexpr int kStep = 32;      // of the contraction in a stage
 
 // BM x BN of the product for a workgroup of WM x WN waves.
-template <int BM_, int BN_, int WM_, int WN_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_ = 4>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int FM = BM / WM / 32, FN = BN / WN / 32;   // 32 x 32 blocks of a wave
   static constexpr int A_BYTES = BM * kStep * 2, STAGE = (BM + BN) * kStep * 2;
   static constexpr int LOADS_A = A_BYTES / 1024 / WAVES, LOADS_B = BN * kStep * 2 / 1024 / WAVES, LOADS = LOADS_A + LOADS_B;
-  // stages in LDS: one that is multiplied, one that is whole, and what is on its way; with two planes of A in a stage they are longer and fewer
+  // stages in LDS: one that is multiplied, one that is whole, and what is on its way (of two: what is on its way); with two planes of A in a stage they
+  // are longer and fewer
   template <int PLANES> static constexpr int STAGE_OF = STAGE + (PLANES - 1) * A_BYTES;
-  template <int PLANES> static constexpr int STAGES_OF = PLANES == 1 ? 4 : 3;
+  template <int PLANES> static constexpr int STAGES_OF = PLANES == 1 ? STAGES_ : STAGES_ - 1;
+  static constexpr int GROUPS = BM == 256 ? 1 : (STAGES_ == 4 ? 2 : 3);   // workgroups of a compute unit
   static constexpr int PITCH = BM + 8;                         // of planes of dz on their way out, [32 WN tokens][vocabulary]
+  static constexpr int DZ = 3 * 32 * WN * PITCH * 2;
   template <int PLANES> static constexpr int LDS = STAGES_OF<PLANES> * STAGE_OF<PLANES>;
-  static_assert(3 * 32 * WN * PITCH * 2 <= LDS<1> && LDS<2> <= 160 * 1024, "dz on its way out; what there is");
+  static_assert(GROUPS * DZ <= 160 * 1024 && GROUPS * LDS<2> <= 160 * 1024 && GROUPS * LDS<1> <= 160 * 1024, "what there is");
 };
 using WideTile = Tile<256, 256, 2, 2>;
 using MidTile = Tile<128, 128, 2, 2>;
+using ThirdTile = Tile<128, 128, 2, 2, 3>;   // three workgroups a compute unit
 
 // An operand: planes of 16-bit values, `plane` elements apart, rows ld apart and on 16 bytes.
 struct Side {
@@ -235,7 +239,7 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
       fetched();
     }
   if (STAGES == 4 && total > 2) begin_stage<LOADS>();   // the first two are whole
-  else begin_stage<0>();
+  else if (STAGES > 2) begin_stage<0>();
   Operands<S, PLANES> now, next;
   auto read_one = [&](int n, int k, unsigned at, Operands<S, PLANES>& o) __attribute__((always_inline)) {   // in the order in which they are needed
     if (n >= 1 && n <= S::FN) {
@@ -254,8 +258,6 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
     const short one = PLANES == 1 && plane_of(pairs.b, its) != 0 ? 0 : (HALF ? 0x3c00 : 0x3f80);
     ones = s16x8{one, one, one, one, one, one, one, one};
   };
-#pragma unroll
-  for (int n = 0; n < OPERANDS; ++n) read_one(n, 0, 0, now);
   // Sixteen of the contraction; the next sixteen's operands are read behind the first products.
   auto half = [&](const Operands<S, PLANES>& use, Operands<S, PLANES>& fill, int k, unsigned at, auto beside) __attribute__((always_inline)) {
 #pragma unroll
@@ -268,12 +270,32 @@ __device__ inline void product(const Side& a, const Side& b, const Pairs& pairs,
       }
 #pragma unroll
       for (int n = 0; n < OPERANDS; ++n)
-        if (n * READ_UNTIL / OPERANDS == q) read_one(n, k, at, fill);
+        if (k >= 0 && n * READ_UNTIL / OPERANDS == q) read_one(n, k, at, fill);
       beside(q);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   unsigned at = 0;               // the stage that is multiplied
+  if constexpr (STAGES == 2) {   // the other workgroups of the compute unit run beside what this one waits for
+    for (int i = 0; i < total; ++i) {
+      begin_stage<0>();
+      if (i + 1 < total) {
+        const bool whole = left >= kStep;
+#pragma unroll
+        for (int part = 0; part <= PLANES; ++part) send(part, STAGE - at, whole);
+        fetched();
+      }
+      set_ones(i);
+#pragma unroll
+      for (int n = 0; n < OPERANDS; ++n) read_one(n, 0, at, now);
+      half(now, next, 16, at, [](int) __attribute__((always_inline)) {});
+      half(next, now, -1, at, [](int) __attribute__((always_inline)) {});
+      at = STAGE - at;
+    }
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < OPERANDS; ++n) read_one(n, 0, 0, now);
   for (int i = 0; i < total; ++i) {
     const unsigned after = at + STAGE == STAGES * STAGE ? 0 : at + STAGE, to = at == 0 ? (STAGES - 1) * STAGE : at - STAGE;
     const bool more = i + STAGES - 1 < total, whole = left >= kStep;   // a stage is fetched; it is whole
@@ -442,7 +464,7 @@ struct StatArgs {
   float* label_logit;    // [rows]
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_stats_kernel(StatArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::GROUPS) void logit_stats_kernel(StatArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -965,7 +987,7 @@ __device__ inline void planes_of_dz(const float* from, s16x4 (&out)[count_of(P)]
   }
 }
 template <typename S, bool HALF, Planes P>
-__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void logit_grad_kernel(DzArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::GROUPS) void logit_grad_kernel(DzArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.l.tiles_m, a.l.tiles_n);
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -1051,7 +1073,7 @@ struct HiddenArgs {
   float* slots;          // [splits][rows][width]
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void hidden_grad_kernel(HiddenArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::GROUPS) void hidden_grad_kernel(HiddenArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
   const int begin = blockIdx.y * a.per, length = a.length - begin < a.per ? a.length - begin : a.per;
@@ -1139,7 +1161,7 @@ struct WeightArgs {
   long long ldw, ldb;
 };
 template <typename S, bool HALF>
-__global__ __launch_bounds__(S::THREADS, S::BM == 256 ? 1 : 2) void head_weight_grad_kernel(WeightArgs a) {
+__global__ __launch_bounds__(S::THREADS, S::GROUPS) void head_weight_grad_kernel(WeightArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
   const int g = blockIdx.y, begin = group_offset(a.offsets, g, a.rows), end = group_offset(a.offsets, g + 1, a.rows);
@@ -1278,17 +1300,19 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
 template <typename S, bool HALF>
 hipError_t start_stats(const StatArgs& a, hipStream_t stream) {
   const auto kernel = logit_stats_kernel<S, HALF>;
-  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
+  constexpr int lds = S::template LDS<1>;
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), lds);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::template LDS<1>, stream>>>(a);
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S, bool HALF, Planes P>
 hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
   const auto kernel = logit_grad_kernel<S, HALF, P>;
-  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
+  constexpr int lds = std::max(S::template LDS<1>, S::DZ);
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), lds);
   if (e != hipSuccess) return e;
-  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, S::template LDS<1>, stream>>>(a);
+  kernel<<<(unsigned)a.l.tiles_m * a.l.tiles_n, S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S>
@@ -1299,9 +1323,10 @@ hipError_t start_dz(const DzArgs& a, int dtype, hipStream_t stream) {
 template <typename S, bool HALF>
 hipError_t start_hidden(const HiddenArgs& a, int splits, hipStream_t stream) {
   const auto kernel = hidden_grad_kernel<S, HALF>;
-  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), S::template LDS<1>);
+  constexpr int lds = S::template LDS<1>;
+  const hipError_t e = allow(reinterpret_cast<const void*>(kernel), lds);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, S::template LDS<1>, stream>>>(a);
+  kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 template <typename S, bool HALF>
@@ -1388,7 +1413,7 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
       l.tiles_m = ceil_div(values, side);
       l.tiles_n = ceil_div(rows, side);
       if (p.wide) ZENO_STEP(half ? (start_stats<WideTile, true>(s, stream)) : (start_stats<WideTile, false>(s, stream)));
-      else ZENO_STEP(half ? (start_stats<MidTile, true>(s, stream)) : (start_stats<MidTile, false>(s, stream)));
+      else ZENO_STEP(half ? (start_stats<ThirdTile, true>(s, stream)) : (start_stats<ThirdTile, false>(s, stream)));
       slices = s.slice0 + l.tiles_m * 2;
     }
     ZENO_STEP(join(s, t0, rows, slices));
@@ -1459,7 +1484,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         const int side = p.wide_logits ? 256 : 128;
         l.tiles_m = ceil_div(values, side);
         l.tiles_n = ceil_div(a.rows, side);
-        ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<MidTile>(d, a.dtype, stream));
+        ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<ThirdTile>(d, a.dtype, stream));
       }
       if (a.dhidden != nullptr) {
         HiddenArgs h = {};
@@ -1500,7 +1525,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       w.ldw = a.ldg;
       w.ldb = a.ldb;
       if (p.wide_weight) ZENO_STEP(planes == 1 ? (start_weight<WideTile, true>(w, a.m, stream)) : (start_weight<WideTile, false>(w, a.m, stream)));
-      else ZENO_STEP(planes == 1 ? (start_weight<MidTile, true>(w, a.m, stream)) : (start_weight<MidTile, false>(w, a.m, stream)));
+      else ZENO_STEP(planes == 1 ? (start_weight<ThirdTile, true>(w, a.m, stream)) : (start_weight<ThirdTile, false>(w, a.m, stream)));
     }
   }
   if (a.dhidden != nullptr && a.rows > 0) {
