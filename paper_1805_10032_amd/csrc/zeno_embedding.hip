@@ -31,7 +31,7 @@ __device__ inline void load_values(const T* p, float (&v)[N]) {
 template <typename T, typename O, int N, int ROWS, bool PAST>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int lanes, unsigned blocks, unsigned groups, bool by_row) {
   const int lane = threadIdx.x % lanes, part = threadIdx.x / lanes, parts = 256 / lanes;
-  const unsigned block = by_row ? blockIdx.x % blocks : blockIdx.x / groups, group = by_row ? blockIdx.x / blocks : blockIdx.x % groups;
+  const unsigned at = blockIdx.y * gridDim.x + blockIdx.x, block = by_row ? at % blocks : at / groups, group = by_row ? at / blocks : at % groups;
   const long long unit = (long long)block * lanes + lane;
   if (unit * N >= a.width) return;
   const long long col = unit * N < a.width - N ? unit * N : a.width - N;
@@ -69,9 +69,13 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t stream) {
   const unsigned blocks = (unsigned)((units + lanes - 1) / lanes), groups = (unsigned)((a.rows + rows_a_block - 1) / rows_a_block);
   const bool lines = reinterpret_cast<uintptr_t>(a.out) % 128 == 0 && a.ldo * sizeof(O) % 128 == 0;
   const bool past = lines && a.width * sizeof(O) % 128 == 0 && (long long)a.rows * a.width * (long long)sizeof(O) >= kPastBytes;
-  if (many && past) embed_kernel<T, O, N, 4, true><<<blocks * groups, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
-  else if (many) embed_kernel<T, O, N, 4, false><<<blocks * groups, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
-  else embed_kernel<T, O, N, 1, false><<<blocks * groups, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
+  // (a dimension of a launch ends at 2^32 threads; workgroups behind the last find no row or no column)
+  const long long all = (long long)blocks * groups;
+  const unsigned x = (unsigned)std::min(all, 1LL << 22);
+  const dim3 grid(x, (unsigned)((all + x - 1) / x));
+  if (many && past) embed_kernel<T, O, N, 4, true><<<grid, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
+  else if (many) embed_kernel<T, O, N, 4, false><<<grid, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
+  else embed_kernel<T, O, N, 1, false><<<grid, 256, 0, stream>>>(a, lanes, blocks, groups, lines);
   return hipGetLastError();
 }
 template <typename T, typename O>
@@ -571,7 +575,7 @@ hipError_t launch_embedding_backward(EmbedGradArgs a, void* workspace, hipStream
   a.pieces = p.pieces;
   a.per_piece = p.per_piece;
   const long long n = (long long)a.vocab * a.width;
-  a.fill_floats = a.rows == 0 ? 2048 : 32768;   // of workgroups of 256, 512 and 1024 threads
+  a.fill_floats = a.rows == 0 && n * a.m < 1LL << 33 ? 2048 : 32768;   // of workgroups of 256, 512 and 1024 threads
   a.fill_pieces = (n + 31 + a.fill_floats - 1) / a.fill_floats;   // (31: a part's place in its first line)
   const long long fills = a.accumulate ? 0 : a.fill_pieces * a.m;
   if (a.rows == 0) {
