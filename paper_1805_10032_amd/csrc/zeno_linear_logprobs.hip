@@ -46,7 +46,10 @@ struct Tile {
 };
 using WideTile = Tile<256, 256, 2, 2>;
 using MidTile = Tile<128, 128, 2, 2>;
-using ThirdTile = Tile<128, 128, 2, 2, 3>;   // three workgroups a compute unit
+// Three workgroups a compute unit, a stage less: logits and weight gradients, whose stores and exponentials another workgroup runs beside (20 x 100 tokens'
+// weight gradients, 32000 x 1024: 646 us, with two workgroups 700; 777 x 10007 x 513 float32: logits 108 and 111, weight gradients 83 and 85).  Long sums
+// are faster with two (20 x 100 tokens' dz W 171 and 190).
+using ThirdTile = Tile<128, 128, 2, 2, 3>;
 
 // An operand: planes of 16-bit values, `plane` elements apart, rows ld apart and on 16 bytes.
 struct Side {
@@ -504,15 +507,39 @@ struct FewArgs {
 constexpr int kFewRows = 64, kFewRowsF32 = 256, kFewWaves = 4;
 template <typename T>
 using Piece = typename Wide<T>::type;   // 16 bytes of a row
-template <typename T>
-__device__ inline Piece<T> load_piece(const T* p) { return *reinterpret_cast<const typename Wide<T>::unaligned*>(p); }
-template <typename T>
-__device__ inline Piece<T> load_piece_end(const T* p, int n) {   // the first n, zeros behind
-  Piece<T> v;
+// A lane's pieces of a row.  ODD: rows of 16-bit values may begin between two words.  A load there takes twice as long, so such a piece is shifted together
+// from five whole words (50257 x 1001 fp16, a call for 8, 24 and 40 tokens: 36, 50 and 59 us, as they stand 45, 56 and 70; 1002 columns 29, 34 and 40).  A
+// word that holds a value of the row can be read as a whole.
+template <typename T, bool ODD>
+struct Row {
+  const T* p;                         // if ODD: of the word that the row begins in
+  unsigned shift;                     // bytes of it that are another's
+  __device__ inline void start(const T* from) {
+    shift = ODD ? (unsigned)(reinterpret_cast<unsigned long long>(from) & 2) : 0;
+    p = ODD ? from - shift / 2 : from;
+  }
+  __device__ inline Piece<T> load(int at) const {
+    if constexpr (ODD) {
+      typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+      typedef u32x4 unaligned __attribute__((aligned(4)));
+      const unsigned* words = reinterpret_cast<const unsigned*>(p + at);
+      const u32x4 a = *reinterpret_cast<const unaligned*>(words);
+      const unsigned last = words[3 + shift / 2];   // (the fifth, or the fourth once more)
+      u32x4 v;
 #pragma unroll
-  for (int j = 0; j < Wide<T>::N; ++j) v[j] = j < n ? p[j] : (T)0.f;
-  return v;
-}
+      for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(i < 3 ? a[i + 1] : last, a[i], shift);
+      return __builtin_bit_cast(Piece<T>, v);
+    } else {
+      return *reinterpret_cast<const typename Wide<T>::unaligned*>(p + at);
+    }
+  }
+  __device__ inline Piece<T> load_end(int at, int n) const {   // the first n, zeros behind
+    Piece<T> v;
+#pragma unroll
+    for (int j = 0; j < Wide<T>::N; ++j) v[j] = j < n ? p[at + (int)(ODD ? shift / 2 : 0) + j] : (T)0.f;
+    return v;
+  }
+};
 template <typename T>
 __device__ inline f32x4 multiply_piece(Piece<T> a, Piece<T> b, f32x4 c) {
   if constexpr (sizeof(T) == 4) {
@@ -525,25 +552,27 @@ __device__ inline f32x4 multiply_piece(Piece<T> a, Piece<T> b, f32x4 c) {
   }
   return c;
 }
+// Workgroups a compute unit: what the words of ODD leave registers for (as the compiler places them by itself 37, 52 and 70 us).
+constexpr int few_groups(int blocks, bool odd) { return odd ? (blocks == 4 ? 2 : (blocks == 2 ? 3 : 4)) : 1; }
 // 16 R rows of W, a multiple of 32, from v on times 16 FN tokens from token0 on: sums[wave][row][token] of the waves' shares.
 template <int R, int FN>
 using FewSums = float[kFewWaves][16 * R][16 * FN + 1];
-template <typename T, int R, int FN>
+template <typename T, int R, int FN, bool ODD>
 __device__ inline void few_products(const FewArgs& a, FewSums<R, FN>& shared, int v, int token0) {
   constexpr int N = Wide<T>::N, STEP = 8 * N;   // of the contraction: 128 bytes of a row, two pieces a lane
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int steps = (a.width + STEP - 1) / STEP, begin = steps * wave / kFewWaves, end = steps * (wave + 1) / kFewWaves;
   const int from = lane / 16 * N;
-  const T *w[R], *h[FN];
+  Row<T, ODD> w[R], h[FN];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = v + 16 * r + lane % 16;   // (behind the last: the last once more)
-    w[r] = reinterpret_cast<const T*>(a.weight) + (row < a.values ? row : a.values - 1) * a.ldw + from;
+    w[r].start(reinterpret_cast<const T*>(a.weight) + (row < a.values ? row : a.values - 1) * a.ldw + from);
   }
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
     const int token = token0 + 16 * j + lane % 16;
-    h[j] = reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + from;
+    h[j].start(reinterpret_cast<const T*>(a.hidden) + (token < a.rows ? token : a.rows - 1) * a.ldh + from);
   }
   f32x4 acc[R][FN] = {};
   const int whole = a.width / STEP < end ? a.width / STEP : end;
@@ -554,9 +583,9 @@ __device__ inline void few_products(const FewArgs& a, FewSums<R, FN>& shared, in
 #pragma unroll
     for (int u = 0; u < 2 * AHEAD; ++u) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) x[u][r] = load_piece<T>(w[r] + i * STEP + u * 4 * N);
+      for (int r = 0; r < R; ++r) x[u][r] = w[r].load(i * STEP + u * 4 * N);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) y[u][j] = load_piece<T>(h[j] + i * STEP + u * 4 * N);
+      for (int j = 0; j < FN; ++j) y[u][j] = h[j].load(i * STEP + u * 4 * N);
     }
 #pragma unroll
     for (int u = 0; u < 2 * AHEAD; ++u)
@@ -571,9 +600,9 @@ __device__ inline void few_products(const FewArgs& a, FewSums<R, FN>& shared, in
       const int at = i * STEP + u * 4 * N, n = a.width - at - from;
       Piece<T> x[R], y[FN];
 #pragma unroll
-      for (int r = 0; r < R; ++r) x[r] = n >= N ? load_piece<T>(w[r] + at) : load_piece_end<T>(w[r] + at, n);
+      for (int r = 0; r < R; ++r) x[r] = n >= N ? w[r].load(at) : w[r].load_end(at, n);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) y[j] = n >= N ? load_piece<T>(h[j] + at) : load_piece_end<T>(h[j] + at, n);
+      for (int j = 0; j < FN; ++j) y[j] = n >= N ? h[j].load(at) : h[j].load_end(at, n);
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -600,11 +629,11 @@ __device__ inline void few_logits(const FewSums<R, FN>& shared, int row0, int he
     z[0][e] = at < vocab ? sum + (bias != nullptr ? bias[at] : 0.f) : -__builtin_inff();
   }
 }
-template <typename T, int R, int FN>
-__global__ __launch_bounds__(64 * kFewWaves) void few_stats_kernel(FewArgs a, StatArgs s) {
+template <typename T, int R, int FN, bool ODD>
+__global__ __launch_bounds__(64 * kFewWaves, few_groups(FN, ODD)) void few_stats_kernel(FewArgs a, StatArgs s) {
   __shared__ FewSums<R, FN> shared;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
-  few_products<T, R, FN>(a, shared, v, token0);
+  few_products<T, R, FN, ODD>(a, shared, v, token0);
   constexpr int TOKENS = (16 * FN + 31) / 32;
   for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
     const int row0 = 32 * (block / TOKENS), v32 = v + row0, t32 = 32 * (block % TOKENS) + lane % 32, token = token0 + t32;
@@ -616,11 +645,21 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_stats_kernel(FewArgs a, St
   }
 }
 template <typename T>
+bool between_words(const FewArgs& a) {
+  return ((reinterpret_cast<uintptr_t>(a.hidden) | reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ldh * sizeof(T)) | (uintptr_t)(a.ldw * sizeof(T))) & 3) != 0;
+}
+template <typename T, bool ODD>
 hipError_t start_few(const FewArgs& a, const StatArgs& s, hipStream_t stream) {
-  if (a.rows <= 16) few_stats_kernel<T, 2, 1><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, s);
-  else if (a.rows <= 32) few_stats_kernel<T, 4, 2><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, s);
-  else few_stats_kernel<T, 4, 4><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, s);
+  if (a.rows <= 16) few_stats_kernel<T, 2, 1, ODD><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, s);
+  else if (a.rows <= 32) few_stats_kernel<T, 4, 2, ODD><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, s);
+  else few_stats_kernel<T, 4, 4, ODD><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, s);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t start_few(const FewArgs& a, const StatArgs& s, hipStream_t stream) {
+  if constexpr (sizeof(T) == 2)
+    if (between_words<T>(a)) return start_few<T, true>(a, s, stream);
+  return start_few<T, false>(a, s, stream);
 }
 
 // Slices joined: `tokens` of them a workgroup, the other threads along the slices.
@@ -1034,11 +1073,11 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void logit_grad_kernel(DzArg
 }
 
 // The same of few tokens: the logits have to be the forward pass's to the bit, or a nearly certain token's gradient is the difference of two roundings.
-template <typename T, int R, int FN, Planes P>
-__global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(FewArgs a, DzArgs d) {
+template <typename T, int R, int FN, Planes P, bool ODD>
+__global__ __launch_bounds__(64 * kFewWaves, few_groups(FN, ODD)) void few_grad_kernel(FewArgs a, DzArgs d) {
   __shared__ FewSums<R, FN> shared;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, v = blockIdx.x * (16 * R), token0 = blockIdx.y * (16 * FN);
-  few_products<T, R, FN>(a, shared, v, token0);
+  few_products<T, R, FN, ODD>(a, shared, v, token0);
   constexpr int TOKENS = (16 * FN + 31) / 32;
   for (int block = wave; block < R / 2 * TOKENS; block += kFewWaves) {
     const int row0 = 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, token = t32 < 16 * FN ? token0 + t32 : a.rows;
@@ -1056,12 +1095,18 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(FewArgs a, DzA
     }
   }
 }
+template <typename T, Planes P, bool ODD>
+hipError_t start_few_dz(const FewArgs& a, const DzArgs& d, hipStream_t stream) {
+  if (a.rows <= 16) few_grad_kernel<T, 2, 1, P, ODD><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, d);
+  else if (a.rows <= 32) few_grad_kernel<T, 4, 2, P, ODD><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, d);
+  else few_grad_kernel<T, 4, 4, P, ODD><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, d);
+  return hipGetLastError();
+}
 template <typename T, Planes P>
 hipError_t start_few_dz(const FewArgs& a, const DzArgs& d, hipStream_t stream) {
-  if (a.rows <= 16) few_grad_kernel<T, 2, 1, P><<<(unsigned)ceil_div(a.values, 32), 64 * kFewWaves, 0, stream>>>(a, d);
-  else if (a.rows <= 32) few_grad_kernel<T, 4, 2, P><<<(unsigned)ceil_div(a.values, 64), 64 * kFewWaves, 0, stream>>>(a, d);
-  else few_grad_kernel<T, 4, 4, P><<<dim3((unsigned)ceil_div(a.values, 64), (unsigned)ceil_div(a.rows, 64)), 64 * kFewWaves, 0, stream>>>(a, d);
-  return hipGetLastError();
+  if constexpr (sizeof(T) == 2)
+    if (between_words<T>(a)) return start_few_dz<T, P, true>(a, d, stream);
+  return start_few_dz<T, P, false>(a, d, stream);
 }
 
 // dh: a piece of the vocabulary, cut into `splits` of `per` values that different workgroups sum, each into its own slot.
@@ -1218,9 +1263,9 @@ constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a 
 constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
 
 // Wide tiles of weight gradients: from so many tokens a worker on.  Shorter sums leave the tile's first loads and its 256 KB of stores, which only
-// another workgroup of the compute unit can run beside (100 tokens, 32000 x 1024, 20 workers: 732 us in 128 x 128 tiles, 794 in wide ones; 250 tokens, 50257 x
-// 1600: 139 and 156; 2048 tokens, 8192 x 4096, 4 workers: 1042 and 993).
-constexpr int kLongGroup = 512;
+// another workgroup of the compute unit can run beside (20 x 100 tokens, 32000 x 1024: 646 us in 128 x 128 tiles, 794 in wide ones; logits and weight gradients
+// of 600 tokens, 50257 x 1600: 457 and 491, 4 x 600, 32000 x 1024: 732 and 768, 4 x 1000: 1086 and 1068, 4 x 2048, 8192 x 4096: 1623 and 1606).
+constexpr int kLongGroup = 1024;
 // Wide tiles where they give most compute units one (250 tokens, 50257 x 1600, 197 tiles: 63 us, 128 x 128 tiles 75; 2000 tokens, 32000 x 1024: 186 and 211).
 bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
 
