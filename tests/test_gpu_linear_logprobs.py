@@ -399,3 +399,12 @@ def test_one_groups_values_do_not_show_in_anothers_gradients(B, rows, vocab, wid
         assert torch.equal(G2[2], G[2]), (factor, gradient)
         assert torch.equal(dh2[~other], dh[~other]), (factor, gradient)
         assert (G2[1] == 0).all() and torch.equal(dh2[:3], dh[:3]) and torch.equal(dh2[-4:], dh[-4:])
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("rows,vocab,width,offsets", [
+    (1024, 3, 5, None), (14000, 11, 19, None), (5000, 140, 130, [0, 3, 3, 4990]), (3100, 200, 33, [40, 1600, 3100]), (40000, 3500, 2, None),
+])
+def test_weight_gradients_of_many_tokens_and_few_weights(B, rows, vocab, width, offsets, ty):
+    """A group's tokens in parts, more of them than it has tokens too."""
+    backward(B, rows, vocab, width, ty, offsets, True, seed=9)
