@@ -383,7 +383,8 @@ zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* 
  *   dbias_g = sum of dz[t].
  * In 16-bit types a group's dweight and dbias are taken from dz in two fp16 pieces (off by at most 2^-22 of it or 2^-38 of the largest gradient
  * of the group), and bf16 hidden states are exact in them down to 2^-32 of the largest in their column and group; dhidden, which is rounded itself, is taken from
- * dz rounded to the type, but for the label's value.  In float32 dz is three bf16 pieces.  One group's values do not show in another's gradients.
+ * dz in two pieces of the type: off by at most 2^-16 of it in bf16, 2^-22 in fp16 or 2^-38 of the group's largest gradient.  In float32 dz is three bf16 pieces.
+ * One group's values do not show in another's gradients.
  *   stats, entropy  as zeno_linear_logprobs wrote them (entropy only if grad_entropy is given)
  *   labels, grad_logp        DEVICE [rows] or both NULL; a row with label -1 takes no part in g, another label outside 0..vocab-1 gives NaN
  *   grad_entropy             DEVICE [rows] or NULL

@@ -8,10 +8,11 @@
 // it: with W for dh, with h for dW.
 // Operands are planes of 16 bits: bf16 and fp16 as they are; float32 is a sum of three bf16 pieces, of whose nine products six are taken, those
 // that are left out lie below 2^-24 of the product.
-// dz in 16-bit types.  dh is rounded to the type itself, and takes dz in one plane of it; what the label's value, the largest as a rule, loses there
-// is added behind in float32.  dW and db are float32 and take dz as two fp16 planes, 22 bits, scaled so that the largest gradient comes
-// near fp16's largest: the sum of two bf16 planes has 16 bits, and its error (4e-6 of dW) would be several times that of the float32 sums.  fp16 planes need h in
-// fp16 too: bf16's eight bits fit, once a power of two for each column has brought its range there.
+// dz in 16-bit types.  dh is rounded to the type itself, and takes dz as two planes of it, 16 or 22 bits: dz sums to nothing over the vocabulary, so what the
+// rows of W share cancels, and one plane's roundings, which do not cancel, would stand out by as much (rows that share ten times their spread, peaked tokens:
+// dh five times as far from 64 bits as its own rounding, ten times for the entropy's gradient alone).  dW and db are float32 and take dz as two fp16 planes, 22 bits, scaled
+// so that the largest gradient comes near fp16's largest: the sum of two bf16 planes has 16 bits, and its error (4e-6 of dW) would be several times that of the float32 sums.
+// fp16 planes need h in fp16 too: bf16's eight bits fit, once a power of two for each column has brought its range there.
 #include "zeno_tokens.h"
 #include <algorithm>
 #include <type_traits>
@@ -40,7 +41,8 @@ struct Tile {
   template <int PLANES> static constexpr int STAGES_OF = PLANES == 1 ? STAGES_ : STAGES_ - 1;
   static constexpr int GROUPS = BM == 256 ? 1 : (STAGES_ == 4 ? 2 : 3);   // workgroups of a compute unit
   static constexpr int PITCH = BM + 8;                         // of planes of dz on their way out, [32 WN tokens][vocabulary]
-  static constexpr int DZ = 3 * 32 * WN * PITCH * 2;
+  static constexpr int DZ_PLANES = 3;                          // at a time
+  static constexpr int DZ = DZ_PLANES * 32 * WN * PITCH * 2;
   template <int PLANES> static constexpr int LDS = STAGES_OF<PLANES> * STAGE_OF<PLANES>;
   static_assert(GROUPS * DZ <= 160 * 1024 && GROUPS * LDS<2> <= 160 * 1024 && GROUPS * LDS<1> <= 160 * 1024, "what there is");
 };
@@ -906,11 +908,11 @@ struct DzArgs {
   const float* up;       // [rows]
   u16* dz;               // [planes][rows][ldz]
   long long ldz, plane;
-  float* rest;           // [rows] what the label's value loses in the first plane, or nullptr
 };
 // Planes of dz.
-enum Planes { kBf16Three, kBf16AndHalf, kHalfTwo };   // three bf16 pieces; one bf16, and two fp16 pieces; two fp16 pieces
-__host__ __device__ constexpr int count_of(Planes p) { return p == kHalfTwo ? 2 : 3; }
+enum Planes { kBf16Three, kBf16TwoHalfTwo, kHalfTwo };   // three bf16 pieces; two bf16 pieces, and two fp16 pieces; two fp16 pieces
+__host__ __device__ constexpr int count_of(Planes p) { return p == kHalfTwo ? 2 : (p == kBf16Three ? 3 : 4); }
+__host__ __device__ constexpr int sums_of(Planes p) { return p == kBf16TwoHalfTwo ? 2 : 1; }   // each is dz
 // A token, as far as its gradients need it.
 struct TokenGrad {
   float M, log_s;        // of its logits
@@ -936,9 +938,9 @@ __device__ inline TokenGrad token_grad(const DzArgs& a, int token) {
   return t;
 }
 // dz, scaled, in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a token that
-// is nearly certain; what it loses in the first plane goes to `rest`.
+// is nearly certain.
 template <int FM, Planes P>
-__device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab, float* rest) {
+__device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab) {
   const float up = P == kBf16Three ? 1.f : t.up;       // (a power of two)
   const bool empty = t.M == -__builtin_inff() && t.log_s == 0.f;
   const float g = t.y == -1 ? 0.f : (t.y >= 0 && t.y < vocab ? t.g : __builtin_nanf(""));
@@ -968,25 +970,27 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
     if (with_entropy) d -= exp_fast(lp) * (t.q * (fmaxf(lp, -256.f) + t.H));
     d = empty ? 0.f : d * up;
     put_at<FM>(z, place, d);
-    if (P != kBf16Three && place >= 0) *rest = d - (P == kHalfTwo ? (float)(_Float16)d : (float)(__bf16)d);
   }
 }
-// Four values as their planes.
+// Four values as the planes of sum `sum`.
 template <Planes P>
-__device__ inline void planes_of_dz(const float* from, s16x4 (&out)[count_of(P)]) {
+constexpr int kPlanesOfSum = count_of(P) / sums_of(P);
+template <Planes P>
+__device__ inline void planes_of_dz(const float* from, int sum, s16x4 (&out)[kPlanesOfSum<P>]) {
+  const bool half = P == kHalfTwo || sum == 1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float d = from[i];
 #pragma unroll
-    for (int plane = 0; plane < count_of(P); ++plane) {
-      if (P == kHalfTwo || (P == kBf16AndHalf && plane > 0)) {
+    for (int plane = 0; plane < kPlanesOfSum<P>; ++plane) {
+      if (half) {
         const _Float16 x = (_Float16)d;
         out[plane][i] = __builtin_bit_cast(short, x);
         d -= (float)x;
       } else {
         const __bf16 x = (__bf16)d;
         out[plane][i] = __builtin_bit_cast(short, x);
-        if (P == kBf16Three) d -= (float)x;
+        d -= (float)x;
       }
     }
   }
@@ -1010,30 +1014,34 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void logit_grad_kernel(DzArg
     __builtin_amdgcn_sched_barrier(0);   // (one block of tokens after the other, or all their values want registers at once)
     float z[S::FM][16];
     logits_of<S>(bias, acc, j, z);
-    logit_grads<S::FM, P>(z, lane, token[j], a.grad_entropy != nullptr, v, a.l.vocab, a.rest + (t.n * S::BN + wn + 32 * j + lane % 32));
-    // this block of every wave's tokens through LDS, so that rows leave in whole lines
+    logit_grads<S::FM, P>(z, lane, token[j], a.grad_entropy != nullptr, v, a.l.vocab);
+    // this block of every wave's tokens through LDS, so that rows leave in whole lines; one sum's planes after the other's
     u16* tile = reinterpret_cast<u16*>(memory);
-    constexpr int TOKENS = 32 * S::WN, PLANE = TOKENS * S::PITCH;
-    if (j > 0) __syncthreads();
+    constexpr int TOKENS = 32 * S::WN, PLANE = TOKENS * S::PITCH, COUNT = kPlanesOfSum<P>;
+    static_assert(COUNT <= S::DZ_PLANES, "what there is");
 #pragma unroll
-    for (int r = 0; r < S::FM; ++r)
+    for (int sum = 0; sum < sums_of(P); ++sum) {
+      if (j > 0 || sum > 0) __syncthreads();
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        s16x4 out[count_of(P)];
-        planes_of_dz<P>(z[r] + 4 * c, out);
-        u16* to = tile + (32 * (wave / S::WM) + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane);
+      for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int plane = 0; plane < count_of(P); ++plane) *reinterpret_cast<s16x4*>(to + plane * PLANE) = out[plane];
-      }
-    __syncthreads();
-    constexpr int CHUNKS = S::BM / 8;
+        for (int c = 0; c < 4; ++c) {
+          s16x4 out[COUNT];
+          planes_of_dz<P>(z[r] + 4 * c, sum, out);
+          u16* to = tile + (32 * (wave / S::WM) + lane % 32) * S::PITCH + wm + 32 * r + row_of(4 * c, lane);
+#pragma unroll
+          for (int plane = 0; plane < COUNT; ++plane) *reinterpret_cast<s16x4*>(to + plane * PLANE) = out[plane];
+        }
+      __syncthreads();
+      constexpr int CHUNKS = S::BM / 8;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < count_of(P) * TOKENS * CHUNKS; i += S::THREADS) {
-      const int plane = i / (TOKENS * CHUNKS), row = i / CHUNKS % TOKENS, col = i % CHUNKS * 8;
-      const long long to = (long long)t.n * S::BN + row / 32 * (32 * S::FN) + 32 * j + row % 32;
-      if (to < a.l.rows)
-        *reinterpret_cast<s16x8*>(a.dz + plane * a.plane + to * a.ldz + t.m * S::BM + col) =
-            *reinterpret_cast<const s16x8*>(tile + plane * PLANE + row * S::PITCH + col);
+      for (int i = threadIdx.x; i < COUNT * TOKENS * CHUNKS; i += S::THREADS) {
+        const int plane = i / (TOKENS * CHUNKS), row = i / CHUNKS % TOKENS, col = i % CHUNKS * 8;
+        const long long to = (long long)t.n * S::BN + row / 32 * (32 * S::FN) + 32 * j + row % 32;
+        if (to < a.l.rows)
+          *reinterpret_cast<s16x8*>(a.dz + (sum * COUNT + plane) * a.plane + to * a.ldz + t.m * S::BM + col) =
+              *reinterpret_cast<const s16x8*>(tile + plane * PLANE + row * S::PITCH + col);
+      }
     }
   }
 }
@@ -1049,16 +1057,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_grad_kernel(FewArgs a, DzA
     const int row0 = 32 * (block / TOKENS), t32 = 32 * (block % TOKENS) + lane % 32, token = t32 < 16 * FN ? token0 + t32 : a.rows;
     float z[1][16];
     few_logits<R, FN>(shared, row0, t32 < 16 * FN ? t32 : 16 * FN - 1, lane, d.l.v0 + v + row0, d.l.vocab, d.l.bias, z);
-    logit_grads<1, P>(z, lane, token_grad(d, token), d.grad_entropy != nullptr, d.l.v0 + v + row0, d.l.vocab, d.rest + token);
+    logit_grads<1, P>(z, lane, token_grad(d, token), d.grad_entropy != nullptr, d.l.v0 + v + row0, d.l.vocab);
     if (token >= a.rows) continue;
+    constexpr int COUNT = kPlanesOfSum<P>;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      s16x4 out[count_of(P)];
-      planes_of_dz<P>(z[0] + 4 * c, out);
+    for (int sum = 0; sum < sums_of(P); ++sum)
 #pragma unroll
-      for (int plane = 0; plane < count_of(P); ++plane)
-        *reinterpret_cast<s16x4*>(d.dz + plane * d.plane + token * d.ldz + v + row0 + row_of(4 * c, lane)) = out[plane];
-    }
+      for (int c = 0; c < 4; ++c) {
+        s16x4 out[COUNT];
+        planes_of_dz<P>(z[0] + 4 * c, sum, out);
+#pragma unroll
+        for (int plane = 0; plane < COUNT; ++plane)
+          *reinterpret_cast<s16x4*>(d.dz + (sum * COUNT + plane) * d.plane + token * d.ldz + v + row0 + row_of(4 * c, lane)) = out[plane];
+      }
   }
 }
 template <typename T, Planes P>
@@ -1072,12 +1083,12 @@ hipError_t start_few_dz(const FewArgs& a, const DzArgs& d, hipStream_t stream) {
 // dh: a piece of the vocabulary, cut into `splits` of `per` values that different workgroups sum, each into its own slot.
 struct HiddenArgs {
   Side dz, w;
-  Pairs pairs;
+  Pairs pairs;           // of PLANES 1
   int tiles_m, tiles_n, rows, width, length, per;
   int first;             // the slots hold nothing yet
   float* slots;          // [splits][rows][width]
 };
-template <typename S, bool HALF>
+template <typename S, bool HALF, int PLANES>
 __global__ __launch_bounds__(S::THREADS, S::GROUPS) void hidden_grad_kernel(HiddenArgs a) {
   extern __shared__ __align__(1024) unsigned char memory[];
   const Place t = place_of(blockIdx.x, a.tiles_m, a.tiles_n);
@@ -1085,8 +1096,9 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void hidden_grad_kernel(Hidd
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
   float* slot = a.slots + (long long)blockIdx.y * a.rows * a.width;
-  f32x16 acc[S::FM][S::FN] = {};
-  product<S, HALF, false, true>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0, memory, acc);
+  f32x16 acc[S::FM][S::FN] = {}, none[S::FM / S::WN];
+  product<S, HALF, false, true, PLANES, false>(a.dz, a.w, a.pairs, (long long)t.m * S::BM, (long long)t.n * S::BN, begin, length > 0 ? length : 0,
+                                               memory, acc, none);
 #pragma unroll
   for (int r = 0; r < S::FM; ++r)
 #pragma unroll
@@ -1102,15 +1114,12 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void hidden_grad_kernel(Hidd
         else unsafeAtomicAdd(to, acc[r][j][e]);
       }
 }
-// Slots in their order, and what the label's value lost, for the rows that belong to somebody.
+// Slots in their order, for the rows that belong to somebody.
 struct HiddenJoinArgs {
   const float* slots;
-  int splits, rows, width, vocab, m;
-  const int32_t *offsets, *labels;
+  int splits, rows, width, m;
+  const int32_t* offsets;
   const float* up;       // [rows] or nullptr
-  const float* rest;     // or nullptr
-  const void* weight;
-  long long ldw;
   void* out;
   long long ldo;
 };
@@ -1120,11 +1129,7 @@ __global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
   const long long stride = (long long)a.rows * a.width;
   for (int row = lo + blockIdx.y; row < hi; row += gridDim.y) {
     const float down = a.up != nullptr ? 1.f / a.up[row] : 1.f;   // (a power of two: exact)
-    const int y = a.rest != nullptr ? a.labels[row] : -1;
-    const bool has = y >= 0 && y < a.vocab;
-    const float rest = has ? a.rest[row] : 0.f;
     const float* from = a.slots + (long long)row * a.width;
-    const T* w = reinterpret_cast<const T*>(a.weight) + (has ? y : 0) * a.ldw;
     T* to = reinterpret_cast<T*>(a.out) + row * a.ldo;
     const int whole = a.width / 4 * 4;
     for (int col = (blockIdx.x * 256 + threadIdx.x) * 4; col < a.width; col += gridDim.x * 1024) {
@@ -1133,11 +1138,6 @@ __global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
         for (int s = 1; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4_a4*>(from + s * stride + col);
         typedef T t4 __attribute__((ext_vector_type(4)));
         typedef t4 unaligned __attribute__((aligned(sizeof(T))));
-        if (has) {
-          const t4 x = *reinterpret_cast<const unaligned*>(w + col);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[i] = fmaf(rest, (float)x[i], sum[i]);
-        }
         t4 out;
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = (T)(sum[i] * down);
@@ -1146,7 +1146,6 @@ __global__ __launch_bounds__(256) void hidden_join_kernel(HiddenJoinArgs a) {
         for (int i = col; i < a.width; ++i) {
           float sum = from[i];
           for (int s = 1; s < a.splits; ++s) sum += from[s * stride + i];
-          if (has) sum = fmaf(rest, (float)w[i], sum);
           to[i] = (T)(sum * down);
         }
       }
@@ -1296,12 +1295,12 @@ struct BackwardPlan {
   int piece;          // values of the vocabulary at a time
   int planes;         // of dz
   int splits, parts;
-  size_t hidden, weight, dz, slots, sums, scale, up, rest, half, columns, bytes;
+  size_t hidden, weight, dz, slots, sums, scale, up, half, columns, bytes;
 };
 BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   BackwardPlan p;
   const long long padded = padded_width(width), n = std::max(rows, 1);
-  p.planes = dtype == ZENO_F16 ? 2 : 3;
+  p.planes = count_of(dtype == ZENO_F32 ? kBf16Three : (dtype == ZENO_F16 ? kHalfTwo : kBf16TwoHalfTwo));
   // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles
   const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
   const long long pieces = (vocab + most - 1) / most;
@@ -1325,7 +1324,6 @@ BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   p.sums = l.take(p.parts > 1 ? (size_t)p.parts * m * std::min(p.piece, vocab) * (width + 1LL) * 4 : 0);
   p.scale = l.take((size_t)m * sizeof(GradScale));
   p.up = l.take((size_t)n * 4);
-  p.rest = l.take((size_t)n * 4);
   p.half = l.take(dtype == ZENO_BF16 ? (size_t)n * padded * 2 : 0);
   p.columns = l.take(dtype == ZENO_BF16 ? (size_t)m * width * 4 : 0);
   p.bytes = l.at + 256;
@@ -1353,16 +1351,21 @@ hipError_t start_dz(const DzArgs& a, hipStream_t stream) {
 template <typename S>
 hipError_t start_dz(const DzArgs& a, int dtype, hipStream_t stream) {
   if (dtype == ZENO_F32) return start_dz<S, false, kBf16Three>(a, stream);
-  return dtype == ZENO_F16 ? start_dz<S, true, kHalfTwo>(a, stream) : start_dz<S, false, kBf16AndHalf>(a, stream);
+  return dtype == ZENO_F16 ? start_dz<S, true, kHalfTwo>(a, stream) : start_dz<S, false, kBf16TwoHalfTwo>(a, stream);
 }
-template <typename S, bool HALF>
+template <typename S, bool HALF, int PLANES>
 hipError_t start_hidden(const HiddenArgs& a, int splits, hipStream_t stream) {
-  const auto kernel = hidden_grad_kernel<S, HALF>;
-  constexpr int lds = S::template LDS<1>;
+  const auto kernel = hidden_grad_kernel<S, HALF, PLANES>;
+  constexpr int lds = S::template LDS<PLANES>;
   const hipError_t e = allow(reinterpret_cast<const void*>(kernel), lds);
   if (e != hipSuccess) return e;
   kernel<<<dim3((unsigned)a.tiles_m * a.tiles_n, splits), S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
+}
+template <typename S>
+hipError_t start_hidden(const HiddenArgs& a, int dtype, int splits, hipStream_t stream) {
+  if (dtype == ZENO_F32) return start_hidden<S, false, 1>(a, splits, stream);
+  return dtype == ZENO_F16 ? start_hidden<S, true, 2>(a, splits, stream) : start_hidden<S, false, 2>(a, splits, stream);
 }
 template <typename S, bool HALF>
 hipError_t start_weight(const WeightArgs& a, int m, hipStream_t stream) {
@@ -1492,7 +1495,6 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
     column_half_kernel<<<grid, 1024, 0, stream>>>(c);
     ZENO_STEP(hipGetLastError());
   }
-  d.rest = planes == 1 ? reinterpret_cast<float*>(ws + p.rest) : nullptr;
   d.stats = a.stats;
   d.grad_logp = a.grad_logp;
   d.entropy = a.entropy;
@@ -1502,7 +1504,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   d.ldz = p.piece;
   d.plane = (long long)a.rows * p.piece;
   float* slots = reinterpret_cast<float*>(ws + p.slots);
-  const int fine = a.dtype == ZENO_BF16 ? 1 : 0;   // the first plane that the float32 gradients take
+  const int fine = a.dtype == ZENO_BF16 ? 2 : 0;   // the first plane that the float32 gradients take
   const u16* fine_dz = d.dz + fine * d.plane;
   for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const int values = std::min(p.piece, a.vocab - v0);
@@ -1514,7 +1516,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       if (p.few) {
         const FewArgs f = {a.hidden, weight, a.ldh, a.ldw, a.rows, values, a.width};
         ZENO_STEP(a.dtype == ZENO_F32 ? (start_few_dz<float, kBf16Three>(f, d, stream))
-                                      : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16AndHalf>(f, d, stream)));
+                                      : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16TwoHalfTwo>(f, d, stream)));
       } else {
         const int side = p.wide_logits ? 256 : 128;
         l.tiles_m = ceil_div(values, side);
@@ -1526,7 +1528,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         h.dz = {d.dz, d.ldz, d.plane, a.rows};
         h.w = l.w;
         h.w.extent = l.width;   // (across the contraction: columns)
-        h.pairs = planes == 3 ? pairs_of(3, 3) : pairs_of(1, 1);
+        h.pairs = pairs_of(3, 3);
         const int tile = p.wide_hidden ? 256 : 128;
         h.tiles_m = ceil_div(a.rows, tile);
         h.tiles_n = ceil_div(a.width, tile);
@@ -1536,8 +1538,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         h.per = ceil_div(ceil_div(values, p.splits), kStep) * kStep;
         h.first = v0 == 0;
         h.slots = slots;
-        if (p.wide_hidden) ZENO_STEP(half ? (start_hidden<WideTile, true>(h, p.splits, stream)) : (start_hidden<WideTile, false>(h, p.splits, stream)));
-        else ZENO_STEP(half ? (start_hidden<MidTile, true>(h, p.splits, stream)) : (start_hidden<MidTile, false>(h, p.splits, stream)));
+        ZENO_STEP(p.wide_hidden ? start_hidden<WideTile>(h, a.dtype, p.splits, stream) : start_hidden<MidTile>(h, a.dtype, p.splits, stream));
       }
     }
     if (a.dweight != nullptr || a.dbias != nullptr) {
@@ -1578,8 +1579,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
     }
   }
   if (a.dhidden != nullptr && a.rows > 0) {
-    const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.vocab, a.m, a.offsets, a.labels,
-                              planes == 1 ? up : nullptr, a.grad_logp != nullptr ? d.rest : nullptr, a.weight, a.ldw, a.dhidden, a.lddh};
+    const HiddenJoinArgs j = {slots, p.splits, a.rows, a.width, a.m, a.offsets, planes == 1 ? up : nullptr, a.dhidden, a.lddh};
     const dim3 grid((unsigned)std::min(ceil_div(a.width, 1024), 64), (unsigned)std::min(a.rows, 16384));
     if (a.dtype == ZENO_F32) hidden_join_kernel<float><<<grid, 256, 0, stream>>>(j);
     else if (half) hidden_join_kernel<_Float16><<<grid, 256, 0, stream>>>(j);
