@@ -1244,7 +1244,10 @@ __global__ __launch_bounds__(256) void weight_join_kernel(WeightJoinArgs a) {
 hipError_t allow(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds); }
 
 constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
-constexpr int kRowBlock = 1 << 16;                 // tokens whose slices are kept at a time
+// Tokens whose slices are kept at a time, and how many sums that may be (twelve bytes each): vocabularies beyond 2^18 values take fewer tokens, so that their sums stay
+// below 1.7 GB (2^24 values of 65536 tokens would be 103) and their tiles, 2^18 of them, in a dimension of a launch, which ends at 2^32 threads.
+constexpr int kRowBlock = 1 << 16;
+constexpr long long kSliceSums = 1LL << 27;
 
 // Wide tiles of weight gradients: from so many tokens a worker on.  Shorter sums leave the tile's first loads and its 256 KB of stores, which only
 // another workgroup of the compute unit can run beside (20 x 100 tokens, 32000 x 1024: 646 us in 128 x 128 tiles, 794 in wide ones; logits and weight gradients
@@ -1273,8 +1276,9 @@ struct ForwardPlan {
 };
 ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
   ForwardPlan p;
-  p.block = std::min(rows, kRowBlock);
   p.few = few_tokens(rows, dtype);
+  p.block = std::min(rows, kRowBlock);
+  if (!p.few) p.block = (int)std::min<long long>(p.block, kSliceSums / (ceil_div(vocab, 32 * WideTile::FM) + 4) / 256 * 256);   // (tiles are wide where this is less)
   p.wide = wide_tiles(vocab, p.block);
   p.slice = p.few ? 32 : (p.wide ? 32 * WideTile::FM : 32 * MidTile::FM);
   const long long padded = padded_width(width);

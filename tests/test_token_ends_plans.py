@@ -1,0 +1,21 @@
+"""Workspaces of the log probabilities of a linear layer, on the host: what the largest documented sizes ask for."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    from paper_1805_10032_amd import binding, build
+    if not os.path.exists(binding.LIB_PATH):
+        build.build(verbose=False)
+    return binding.load_library()
+
+
+@pytest.mark.parametrize("dtype", range(3))
+@pytest.mark.parametrize("rows", [65, 257, 65281, 65536, 1 << 22])
+@pytest.mark.parametrize("vocab", [1 << 18, (1 << 24) - 255, 1 << 24])
+def test_sums_of_a_large_vocabulary_are_kept_in_parts(lib, rows, vocab, dtype):
+    """Twelve bytes for each of 2^27 sums; beside them the copies of hidden states and weights (six bytes a value, 64 M of them a plane) and a word a token."""
+    got = lib.zeno_linear_logprobs_workspace_bytes(rows, vocab, 8, dtype)
+    assert 0 < got <= 12 * (1 << 27) + 6 * ((64 << 20) + 8 * 65536) + 4 * 65536 + 4096
+    assert got <= lib.zeno_linear_logprobs_workspace_bytes(1 << 22, vocab, 8, dtype)
