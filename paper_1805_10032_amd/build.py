@@ -56,6 +56,8 @@ def _fresh(obj, src, stamp):
             deps.append(os.path.join(CSRC, "zeno_split.h"))
         if src == "zeno_conv.hip":
             deps.append(os.path.join(CSRC, "zeno_index.h"))
+        if src == "zeno_linear_logprobs.hip":
+            deps.append(os.path.join(CSRC, "zeno_linear_plan.h"))
         if src in TOKEN_SOURCES or src == "zeno_capi.hip":
             deps.append(os.path.join(CSRC, "zeno_tokens.h"))
         return all(os.path.getmtime(d) < t for d in deps)

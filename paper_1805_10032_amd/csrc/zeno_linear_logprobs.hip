@@ -13,6 +13,7 @@
 // dh five times as far from 64 bits as its own rounding, ten times for the entropy's gradient alone).  dW and db are float32 and take dz as two fp16 planes, 22 bits, scaled
 // so that the largest gradient comes near fp16's largest: the sum of two bf16 planes has 16 bits, and its error (4e-6 of dW) would be several times that of the float32 sums.
 // fp16 planes need h in fp16 too: bf16's eight bits fit, once a power of two for each column has brought its range there.
+#include "zeno_linear_plan.h"
 #include "zeno_tokens.h"
 #include <algorithm>
 #include <type_traits>
@@ -503,12 +504,10 @@ struct FewArgs {
   long long ldh, ldw;
   int rows, values, width;       // values: of the vocabulary in this launch
 };
-// Up to which number of tokens: 16-bit operands are as fast in tiles of 128 tokens from 65 on (32000 x 4096: 64 tokens 74 us here, 65 there 69); float32,
-// which tiles take in six products, from 257 on (1024 columns: 256 tokens 209 us here, 250 there 211; 4096 columns 832 and 939).
 // 32 rows a workgroup for one block of tokens (1 token, 32000 x 4096 bf16: 56 us with the join and the host, 64 rows 63), 64 for more (32 tokens: 82 and 65; 64: 106 and 74).
 // (Rows of 16-bit values between two words, shifted together from whole words: 24 tokens, 50257 x 1001 fp16 69 -> 83 us where the weights come from
 // memory, 56 -> 50 where they stand in the caches.)
-constexpr int kFewRows = 64, kFewRowsF32 = 256, kFewWaves = 4;
+constexpr int kFewWaves = 4;
 template <typename T>
 using Piece = typename Wide<T>::type;   // 16 bytes of a row
 template <typename T>
@@ -746,8 +745,6 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* x, long long ldx, in
   }
 }
 
-int padded_width(int width) { return (width + 7) / 8 * 8; }
-int planes_of(int dtype) { return dtype == ZENO_F32 ? 3 : 1; }
 // Whether a matrix can be read as it stands: 16-byte pieces of 16-bit values.
 bool as_it_is(const void* p, long long ld, int dtype, int width) {
   return dtype != ZENO_F32 && width % 8 == 0 && ld % 8 == 0 && ld < kMostPitch && reinterpret_cast<uintptr_t>(p) % 16 == 0;
@@ -773,6 +770,9 @@ Pairs pairs_of(int a, int b) {   // planes of the two sides: three and three, tw
 struct GradScale {
   float up, down;   // what dz is multiplied by on its way into 16 bits, and the products by on their way out
 };
+static_assert(sizeof(GradScale) == kScaleBytes && WideTile::BM == kWideSide && WideTile::WM == 2 && MidTile::BM == kTileSide && ThirdTile::BM == kTileSide &&
+                  ThirdTile::WM == 2,
+              "as the plans have it");
 // 16-bit types keep a worker's dz within 2^14: a power of two of the largest gradient that one of its tokens brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
 // p H <= ln V < 21).  float32's pieces have its range.  One workgroup a worker: another's gradients, or those of nobody, do not show.  `clear`: a worker's n
 // words to set to zero on the way.
@@ -1239,100 +1239,9 @@ __global__ __launch_bounds__(256) void weight_join_kernel(WeightJoinArgs a) {
   }
 }
 
-// ---- plans
+// ---- launches
 
 hipError_t allow(const void* kernel, int lds) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds); }
-
-constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
-// Tokens whose slices are kept at a time, and how many sums that may be (twelve bytes each): vocabularies beyond 2^18 values take fewer tokens, so that their sums stay
-// below 1.7 GB (2^24 values of 65536 tokens would be 103) and their tiles, 2^18 of them, in a dimension of a launch, which ends at 2^32 threads.
-constexpr int kRowBlock = 1 << 16;
-constexpr long long kSliceSums = 1LL << 27;
-
-// Wide tiles of weight gradients: from so many tokens a worker on.  Shorter sums leave the tile's first loads and its 256 KB of stores, which only
-// another workgroup of the compute unit can run beside (20 x 100 tokens, 32000 x 1024: 646 us in 128 x 128 tiles, 794 in wide ones; logits and weight gradients
-// of 600 tokens, 50257 x 1600: 457 and 491, 4 x 600, 32000 x 1024: 732 and 768, 4 x 1000: 1086 and 1068, 4 x 2048, 8192 x 4096: 1623 and 1606).
-constexpr int kLongGroup = 1024;
-// Wide tiles where they give most compute units one (250 tokens, 50257 x 1600, 197 tiles: 63 us, 128 x 128 tiles 75; 2000 tokens, 32000 x 1024: 186 and 211).
-bool wide_tiles(long long m, long long n) { return ((m + 255) / 256) * ((n + 255) / 256) >= 192; }
-
-struct Layout {
-  size_t at = 0;
-  size_t take(size_t bytes) {
-    const size_t here = at;
-    at += align_up(bytes, 256);
-    return here;
-  }
-};
-
-bool few_tokens(int rows, int dtype) { return rows <= (dtype == ZENO_F32 ? kFewRowsF32 : kFewRows); }
-
-struct ForwardPlan {
-  bool few, wide;
-  int slice;          // values of the vocabulary in a slice
-  int piece;          // values that are packed at a time
-  int block;          // tokens at a time
-  size_t hidden, weight, part, part_u, label, bytes;
-};
-ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
-  ForwardPlan p;
-  p.few = few_tokens(rows, dtype);
-  p.block = std::min(rows, kRowBlock);
-  if (!p.few) p.block = (int)std::min<long long>(p.block, kSliceSums / (ceil_div(vocab, 32 * WideTile::FM) + 4) / 256 * 256);   // (tiles are wide where this is less)
-  p.wide = wide_tiles(vocab, p.block);
-  p.slice = p.few ? 32 : (p.wide ? 32 * WideTile::FM : 32 * MidTile::FM);
-  const long long padded = padded_width(width);
-  p.piece = (int)std::min<long long>((vocab + 255) / 256 * 256LL, std::max<long long>(256, kPackElements / padded / 256 * 256));
-  Layout l;
-  p.hidden = l.take(p.few ? 0 : (size_t)planes_of(dtype) * p.block * padded * 2);
-  p.weight = l.take(p.few ? 0 : (size_t)planes_of(dtype) * std::min(p.piece, vocab) * padded * 2);
-  const size_t slices = (size_t)ceil_div(vocab, p.slice) + 4;
-  p.part = l.take(slices * p.block * 8);
-  p.part_u = l.take(slices * p.block * 4);
-  p.label = l.take((size_t)p.block * 4);
-  p.bytes = l.at + 256;
-  return p;
-}
-
-struct BackwardPlan {
-  bool few, wide_logits, wide_hidden, wide_weight;
-  int piece;          // values of the vocabulary at a time
-  int planes;         // of dz
-  int splits, parts;
-  size_t hidden, weight, dz, slots, sums, scale, up, half, columns, bytes;
-};
-BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
-  BackwardPlan p;
-  const long long padded = padded_width(width), n = std::max(rows, 1);
-  p.planes = count_of(dtype == ZENO_F32 ? kBf16Three : (dtype == ZENO_F16 ? kHalfTwo : kBf16TwoHalfTwo));
-  // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles
-  const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
-  const long long pieces = (vocab + most - 1) / most;
-  p.piece = (int)(((vocab + pieces - 1) / pieces + 255) / 256 * 256);
-  p.few = few_tokens(rows, dtype);
-  p.wide_logits = wide_tiles(p.piece, n);
-  p.wide_hidden = wide_tiles(n, width);
-  p.wide_weight = wide_tiles((long long)p.piece * m, width) && n / m >= kLongGroup;
-  const int side = p.wide_hidden ? 256 : 128;
-  const long long tiles = (long long)ceil_div(n, side) * ceil_div(width, side);
-  p.splits = (int)std::max<long long>(1, std::min<long long>(p.piece / 512, (p.wide_hidden ? 256 : 512) / tiles));
-  // Weight gradients of few tiles: a group's tokens in parts, from twice 512 on (logits and weight gradients of 14141 tokens, 11 x 19 bf16: 64 us, in one part
-  // 290; 16384, 1000 x 512 bf16 146 and 363, float32 308 and 1655; 1024, 11 x 19 54 and 60).
-  const long long weights = (long long)ceil_div(p.piece, 128) * ceil_div(width, 128) * m;
-  p.parts = (int)std::max<long long>(1, std::min<long long>(n / m / 512, 512 / weights));
-  Layout l;
-  p.hidden = l.take((size_t)planes_of(dtype) * n * padded * 2);
-  p.weight = l.take((size_t)planes_of(dtype) * p.piece * padded * 2);
-  p.dz = l.take((size_t)p.planes * n * p.piece * 2);
-  p.slots = l.take((size_t)p.splits * n * width * 4);
-  p.sums = l.take(p.parts > 1 ? (size_t)p.parts * m * std::min(p.piece, vocab) * (width + 1LL) * 4 : 0);
-  p.scale = l.take((size_t)m * sizeof(GradScale));
-  p.up = l.take((size_t)n * 4);
-  p.half = l.take(dtype == ZENO_BF16 ? (size_t)n * padded * 2 : 0);
-  p.columns = l.take(dtype == ZENO_BF16 ? (size_t)m * width * 4 : 0);
-  p.bytes = l.at + 256;
-  return p;
-}
 
 template <typename S, bool HALF>
 hipError_t start_stats(const StatArgs& a, hipStream_t stream) {
@@ -1451,7 +1360,7 @@ hipError_t launch_linear_logprobs(const LinearLogprobsArgs& a, void* workspace, 
                         reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
       l.v0 = v0;
       s.slice0 = v0 / p.slice;
-      const int side = p.wide ? 256 : 128;
+      const int side = p.wide ? kWideSide : kTileSide;
       l.tiles_m = ceil_div(values, side);
       l.tiles_n = ceil_div(rows, side);
       if (p.wide) ZENO_STEP(half ? (start_stats<WideTile, true>(s, stream)) : (start_stats<WideTile, false>(s, stream)));
@@ -1522,7 +1431,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         ZENO_STEP(a.dtype == ZENO_F32 ? (start_few_dz<float, kBf16Three>(f, d, stream))
                                       : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16TwoHalfTwo>(f, d, stream)));
       } else {
-        const int side = p.wide_logits ? 256 : 128;
+        const int side = p.wide_logits ? kWideSide : kTileSide;
         l.tiles_m = ceil_div(values, side);
         l.tiles_n = ceil_div(a.rows, side);
         ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<ThirdTile>(d, a.dtype, stream));
@@ -1533,7 +1442,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         h.w = l.w;
         h.w.extent = l.width;   // (across the contraction: columns)
         h.pairs = pairs_of(3, 3);
-        const int tile = p.wide_hidden ? 256 : 128;
+        const int tile = p.wide_hidden ? kWideSide : kTileSide;
         h.tiles_m = ceil_div(a.rows, tile);
         h.tiles_n = ceil_div(a.width, tile);
         h.rows = a.rows;
@@ -1552,7 +1461,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       w.h.extent = l.width;
       w.pairs = pairs_of(p.planes - fine, planes);
       w.columns = convert ? columns : nullptr;
-      const int tile = p.wide_weight ? 256 : 128;
+      const int tile = p.wide_weight ? kWideSide : kTileSide;
       w.tiles_m = ceil_div(values, tile);
       w.tiles_n = a.dweight != nullptr ? ceil_div(a.width, tile) : 1;   // (the first ones take the bias's along)
       w.rows = a.rows;

@@ -19,3 +19,16 @@ def test_sums_of_a_large_vocabulary_are_kept_in_parts(lib, rows, vocab, dtype):
     got = lib.zeno_linear_logprobs_workspace_bytes(rows, vocab, 8, dtype)
     assert 0 < got <= 12 * (1 << 27) + 6 * ((64 << 20) + 8 * 65536) + 4 * 65536 + 4096
     assert got <= lib.zeno_linear_logprobs_workspace_bytes(1 << 22, vocab, 8, dtype)
+
+
+def test_plans(tmp_path):
+    """Which kernels the sizes of the GPU tests take, and that launches and offsets stay in their limits over the documented sizes."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "plan_checks")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-I", os.path.join(root, "include"),
+                    "-I", os.path.join(root, "paper_1805_10032_amd", "csrc"), os.path.join(root, "tests", "sanitize", "plan_checks.cpp"), "-o", exe],
+                   check=True, capture_output=True, text=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "plan checks passed" in res.stdout, res.stdout + res.stderr
