@@ -767,53 +767,45 @@ Pairs pairs_of(int a, int b) {   // planes of the two sides: three and three, tw
 
 // ---- backward
 
-struct GradScale {
-  float up, down;   // what dz is multiplied by on its way into 16 bits, and the products by on their way out
-};
-static_assert(sizeof(GradScale) == kScaleBytes && WideTile::BM == kWideSide && WideTile::WM == 2 && MidTile::BM == kTileSide && ThirdTile::BM == kTileSide &&
+static_assert(WideTile::BM == kWideSide && WideTile::WM == 2 && MidTile::BM == kTileSide && ThirdTile::BM == kTileSide &&
                   ThirdTile::WM == 2,
               "as the plans have it");
-// 16-bit types keep a worker's dz within 2^14: a power of two of the largest gradient that one of its tokens brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
-// p H <= ln V < 21).  float32's pieces have its range.  One workgroup a worker: another's gradients, or those of nobody, do not show.  `clear`: a worker's n
-// words to set to zero on the way.
+// A worker's dz is formed within 2^14, from gradients times a power of two: that of the largest that one of its tokens brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
+// p H <= ln V < 21).  float32's pieces have its range and hold dz itself; 16 bits hold it as it is formed.  Powers from -119 (the largest finite g and q) to 126 are float32's
+// own, and so are their inverses.  One workgroup a worker: another's gradients, or those of nobody, do not show.  `clear`: a worker's n words to set to zero on
+// the way.
 struct ScaleArgs {
   const float *g, *q;
   const int32_t *labels, *offsets;
-  int rows, scaled;
-  GradScale* group;      // [m]
-  float* up;             // [rows]
+  int rows;
+  int* power;            // [m]
+  float* up;             // [rows] 2^power
   unsigned* clear;
   int n;
 };
 __global__ __launch_bounds__(1024) void grad_scale_kernel(ScaleArgs a) {
   __shared__ float shared[16];
-  __shared__ GradScale all;
+  __shared__ int all;
   const int worker = blockIdx.x, begin = group_offset(a.offsets, worker, a.rows), end = group_offset(a.offsets, worker + 1, a.rows);
-  float largest = 0.f;
+  float largest = 0.f;   // a 32nd of it, which no finite gradients take beyond float32
   for (int i = threadIdx.x; i < a.n; i += 1024) a.clear[(long long)worker * a.n + i] = 0;
-  if (a.scaled)
-    for (int t = begin + threadIdx.x; t < end; t += 1024) {
-      float b = a.g != nullptr && a.labels[t] != -1 ? fabsf(a.g[t]) : 0.f;
-      if (a.q != nullptr) b += 22.f * fabsf(a.q[t]);
-      if (b < __builtin_inff()) largest = fmaxf(largest, b);
-    }
+  for (int t = begin + threadIdx.x; t < end; t += 1024) {
+    float b = a.g != nullptr && a.labels[t] != -1 ? fabsf(a.g[t]) * 0.03125f : 0.f;
+    if (a.q != nullptr) b += 0.6875f * fabsf(a.q[t]);
+    if (b < __builtin_inff()) largest = fmaxf(largest, b);
+  }
   largest = wave_max_f(largest);
   if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = largest;
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 16; ++w) largest = fmaxf(largest, shared[w]);
-    int up = 0;
-    if (largest > 0.f) {
-      const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126;   // largest < 2^e
-      up = 14 - e;
-      up = up > 100 ? 100 : (up < -100 ? -100 : up);
-    }
-    all.up = __uint_as_float((unsigned)(127 + up) << 23);
-    all.down = __uint_as_float((unsigned)(127 - up) << 23);
-    a.group[worker] = all;
+    const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126 + 5;   // 32 largest < 2^e
+    all = 14 - e < 126 ? 14 - e : 126;
+    a.power[worker] = all;
   }
   __syncthreads();
-  for (int t = begin + threadIdx.x; t < end; t += 1024) a.up[t] = all.up;
+  const float up = __uint_as_float((unsigned)(127 + all) << 23);
+  for (int t = begin + threadIdx.x; t < end; t += 1024) a.up[t] = up;
 }
 
 // bf16 hidden states as fp16, each column of a worker times the power of two that brings its largest finite value to 2^14 .. 2^15: exact down to 2^-32
@@ -824,7 +816,8 @@ __device__ inline int column_power(unsigned largest) {   // largest magnitude, a
   return up > 126 ? 126 : up;                            // (not below 14 + 127 - 254)
 }
 __host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
-__device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }
+__device__ inline float power_of_two(int k) {   // -126 .. 127
+  return __uint_as_float((unsigned)(127 + k) << 23); }
 constexpr int kColumnRows = 256;   // of a workgroup
 struct ColumnArgs {
   Side h;
@@ -916,32 +909,32 @@ __host__ __device__ constexpr int sums_of(Planes p) { return p == kBf16TwoHalfTw
 // A token, as far as its gradients need it.
 struct TokenGrad {
   float M, log_s;        // of its logits
-  float g, q, H;         // gradients of its log probability and of its entropy, its entropy
+  float g, q, H;         // gradients of its log probability and of its entropy, both times `up`; its entropy
   int y;                 // its label, -1: none
-  float up;              // what its dz is multiplied by
+  float up;              // what its gradients are multiplied by
 };
 __device__ inline TokenGrad token_grad(const DzArgs& a, int token) {
-  TokenGrad t = {-__builtin_inff(), 0.f, 0.f, 0.f, 0.f, -1, 0.f};   // behind the last: no distribution
+  TokenGrad t = {-__builtin_inff(), 0.f, 0.f, 0.f, 0.f, -1, 1.f};   // behind the last: no distribution
   if (token < a.l.rows) {
     t.M = a.stats[2 * token];
     t.log_s = a.stats[2 * token + 1];
     t.up = a.up[token];
     if (a.grad_logp != nullptr) {
       t.y = a.l.labels[token];
-      t.g = a.grad_logp[token];
+      t.g = a.grad_logp[token] * t.up;
     }
     if (a.grad_entropy != nullptr) {
-      t.q = a.grad_entropy[token];
+      t.q = a.grad_entropy[token] * t.up;
       t.H = a.entropy[token];
     }
   }
   return t;
 }
-// dz, scaled, in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a token that
-// is nearly certain.
+// dz, scaled in 16-bit types, in the place of a lane's share of FM blocks of logits from v on.  The label's is -g expm1(log p), which keeps what is left of a
+// token that is nearly certain.
 template <int FM, Planes P>
 __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bool with_entropy, int v, int vocab) {
-  const float up = P == kBf16Three ? 1.f : t.up;       // (a power of two)
+  const float back = P == kBf16Three ? 1.f / t.up : 1.f;   // (a power of two)
   const bool empty = t.M == -__builtin_inff() && t.log_s == 0.f;
   const float g = t.y == -1 ? 0.f : (t.y >= 0 && t.y < vocab ? t.g : __builtin_nanf(""));
   const float M = empty ? 0.f : t.M, log_s = empty ? __builtin_inff() : t.log_s;   // (empty: every probability is 0)
@@ -955,10 +948,10 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
 #pragma unroll
       for (int e = 0; e < 16; ++e) {   // (where p is 0, its logarithm is cut off: 0 * -inf would be NaN)
         const float lp = (z[r][e] - M) - log_s;
-        z[r][e] = -exp_fast(lp) * fmaf(t.q, fmaxf(lp, -256.f), base) * up;
+        z[r][e] = -exp_fast(lp) * fmaf(t.q, fmaxf(lp, -256.f), base) * back;
       }
   } else {
-    const float base = -g * up;
+    const float base = -g * back;
 #pragma unroll
     for (int r = 0; r < FM; ++r)
 #pragma unroll
@@ -968,7 +961,7 @@ __device__ inline void logit_grads(float (&z)[FM][16], int lane, TokenGrad t, bo
     const float lp = (own - M) - log_s;
     float d = -g * expm1f(lp);
     if (with_entropy) d -= exp_fast(lp) * (t.q * (fmaxf(lp, -256.f) + t.H));
-    d = empty ? 0.f : d * up;
+    d = empty ? 0.f : d * back;
     put_at<FM>(z, place, d);
   }
 }
@@ -1159,7 +1152,7 @@ struct WeightArgs {
   Pairs pairs;
   int tiles_m, tiles_n, rows, width, values;   // values: of the vocabulary in this piece
   const int32_t* offsets;
-  const GradScale* scale;    // [m]
+  const int* power;          // [m] of two that dz has been multiplied by, or nullptr
   const unsigned* columns;   // largest values of the columns of h that have been scaled by column_power(), or nullptr
   float *dweight, *dbias;   // at the piece's first value, or in slots; each may be nullptr
   long long ldw, ldb;
@@ -1176,7 +1169,7 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void head_weight_grad_kernel
   f32x16 acc[S::FM][S::FN] = {};
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, length = end > begin ? end - begin : 0;
   const int row0 = t.m * S::BM + (wave % S::WM) * (32 * S::FM), col0 = t.n * S::BN + (wave / S::WM) * (32 * S::FN) + lane % 32;
-  const float down = HALF ? a.scale[g].down : 1.f;
+  const int down = HALF ? -a.power[g] : 0;
   if (a.dbias != nullptr && t.n == 0) {
     f32x16 sums[S::FM / S::WN] = {};
     product<S, HALF, true, true, HALF ? 2 : 1, true>(a.dz, a.h, a.pairs, (long long)t.m * S::BM, 0, begin, length, memory, acc, sums);
@@ -1186,7 +1179,7 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void head_weight_grad_kernel
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int row = row0 + 32 * (S::WN * r + wave / S::WM) + row_of(e, lane);
-          if (row < a.values) a.dbias[g * a.ldb + part * a.slot + row] = sums[r][e] * down;
+          if (row < a.values) a.dbias[g * a.ldb + part * a.slot + row] = ldexpf(sums[r][e], down);
         }
     }
   } else {
@@ -1200,20 +1193,20 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void head_weight_grad_kernel
 #pragma unroll
   for (int j = 0; j < S::FN; ++j) {
     const int col = col0 + 32 * j;
-    const float back = HALF && a.columns != nullptr && col < a.width ? power_of_two(-column_power(a.columns[(long long)g * a.width + col])) : 1.f;
+    const int back = HALF && a.columns != nullptr && col < a.width ? down - column_power(a.columns[(long long)g * a.width + col]) : down;   // (one step: in between it may leave float32's range)
     float* to = dw + (long long)row0 * a.width + col;
     if (past) {
 #pragma unroll
       for (int r = 0; r < S::FM; ++r)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) __builtin_nontemporal_store(acc[r][j][e] * down * back, to + (long long)(32 * r + row_of(e, lane)) * a.width);
+        for (int e = 0; e < 16; ++e) __builtin_nontemporal_store(HALF ? ldexpf(acc[r][j][e], back) : acc[r][j][e], to + (long long)(32 * r + row_of(e, lane)) * a.width);
       keep_apart();
     } else if (col < a.width) {
 #pragma unroll
       for (int r = 0; r < S::FM; ++r)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (row0 + 32 * r + row_of(e, lane) < a.values) to[(long long)(32 * r + row_of(e, lane)) * a.width] = acc[r][j][e] * down * back;
+          if (row0 + 32 * r + row_of(e, lane) < a.values) to[(long long)(32 * r + row_of(e, lane)) * a.width] = HALF ? ldexpf(acc[r][j][e], back) : acc[r][j][e];
     }
   }
 }
@@ -1382,11 +1375,11 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const size_t bytes = a.dtype == ZENO_F32 ? 4 : 2;
   const bool half = a.dtype == ZENO_F16;
   const int planes = planes_of(a.dtype);
-  GradScale* scale = reinterpret_cast<GradScale*>(ws + p.scale);
+  int* power = reinterpret_cast<int*>(ws + p.power);
   const bool convert = a.dtype == ZENO_BF16 && (a.dweight != nullptr || a.dbias != nullptr) && a.rows > 0;
   unsigned* columns = reinterpret_cast<unsigned*>(ws + p.columns);
   float* up = reinterpret_cast<float*>(ws + p.up);
-  const ScaleArgs sc = {a.grad_logp, a.grad_entropy, a.labels, a.offsets, a.rows, planes == 1 ? 1 : 0, scale, up, columns, convert ? a.width : 0};
+  const ScaleArgs sc = {a.grad_logp, a.grad_entropy, a.labels, a.offsets, a.rows, power, up, columns, convert ? a.width : 0};
   grad_scale_kernel<<<a.m, 1024, 0, stream>>>(sc);
   ZENO_STEP(hipGetLastError());
   DzArgs d = {};
@@ -1468,7 +1461,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
       w.width = a.width;
       w.values = values;
       w.offsets = a.offsets;
-      w.scale = scale;
+      w.power = power;
       w.dweight = a.dweight != nullptr ? a.dweight + (long long)v0 * a.width : nullptr;
       w.dbias = a.dbias != nullptr ? a.dbias + v0 : nullptr;
       w.ldw = a.ldg;

@@ -16,7 +16,6 @@ inline long long tiles_along(long long n, long long side) { return (n + side - 1
 inline int padded_width(int width) { return (width + 7) / 8 * 8; }
 inline int planes_of(int dtype) { return dtype == ZENO_F32 ? 3 : 1; }                             // of an operand
 inline int dz_planes_of(int dtype) { return dtype == ZENO_F32 ? 3 : (dtype == ZENO_F16 ? 2 : 4); }
-constexpr size_t kScaleBytes = 8;                  // of a group's scale
 
 constexpr long long kPackElements = 64LL << 20;    // of W that are packed at a time, a plane
 // Tokens whose slices are kept at a time, and how many sums that may be (twelve bytes each): vocabularies beyond 2^18 values take fewer tokens, so that their sums stay
@@ -77,7 +76,7 @@ struct BackwardPlan {
   int piece;          // values of the vocabulary at a time
   int planes;         // of dz
   int splits, parts;
-  size_t hidden, weight, dz, slots, sums, scale, up, half, columns, bytes;
+  size_t hidden, weight, dz, slots, sums, power, up, half, columns, bytes;
 };
 inline BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int m) {
   BackwardPlan p;
@@ -104,7 +103,7 @@ inline BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int
   p.dz = l.take((size_t)p.planes * n * p.piece * 2);
   p.slots = l.take((size_t)p.splits * n * width * 4);
   p.sums = l.take(p.parts > 1 ? (size_t)p.parts * m * std::min(p.piece, vocab) * (width + 1LL) * 4 : 0);
-  p.scale = l.take((size_t)m * kScaleBytes);
+  p.power = l.take((size_t)m * 4);
   p.up = l.take((size_t)n * 4);
   p.half = l.take(dtype == ZENO_BF16 ? (size_t)n * padded * 2 : 0);
   p.columns = l.take(dtype == ZENO_BF16 ? (size_t)m * width * 4 : 0);
