@@ -393,7 +393,8 @@ zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* 
  *   dbias    DEVICE, group g's [vocab] at dbias + g ldb, ldb >= vocab, or NULL
  *   m, offsets  groups (above); rows of no group take no part
  * At least one of the gradients and one of the outputs is given.
- *   workspace  DEVICE, 256-byte aligned, >= zeno_linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, m) */
+ *   workspace  DEVICE, 256-byte aligned, >= zeno_linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, m).  It holds dz of 64 M
+ *            values of tokens and vocabulary at a time, but of 2048 of the vocabulary at least: beyond 32768 rows it grows with them */
 size_t zeno_linear_logprobs_backward_workspace_bytes(int32_t rows, int32_t vocab, int32_t width, int32_t dtype, int32_t m);
 zeno_status_t zeno_linear_logprobs_backward(const void* hidden, int64_t ldh, const void* weight, int64_t ldw, int32_t dtype,
                                             const float* bias, int32_t rows, int32_t vocab, int32_t width, const float* stats,

@@ -1373,7 +1373,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const BackwardPlan p = backward_plan(a.rows, a.vocab, a.width, a.dtype, a.m);
   unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
   const size_t bytes = a.dtype == ZENO_F32 ? 4 : 2;
-  const bool half = a.dtype == ZENO_F16;
+  const bool half = a.dtype == ZENO_F16, direct = as_it_is(a.weight, a.ldw, a.dtype, a.width);
   const int planes = planes_of(a.dtype);
   int* power = reinterpret_cast<int*>(ws + p.power);
   const bool convert = a.dtype == ZENO_BF16 && (a.dweight != nullptr || a.dbias != nullptr) && a.rows > 0;
@@ -1414,24 +1414,30 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const u16* fine_dz = d.dz + fine * d.plane;
   for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
     const int values = std::min(p.piece, a.vocab - v0);
-    if (a.rows > 0) {
-      const void* weight = reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v0 * a.ldw * bytes;
-      if (!p.few || a.dhidden != nullptr)
-        ZENO_STEP(side_of(weight, a.ldw, a.dtype, values, a.width, reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
+    auto weights = [&](int v) { return reinterpret_cast<const unsigned char*>(a.weight) + (size_t)v * a.ldw * bytes; };
+    if (a.rows > 0 && p.few) {
+      const FewArgs f = {a.hidden, weights(v0), a.ldh, a.ldw, a.rows, values, a.width};
       l.v0 = v0;
-      if (p.few) {
-        const FewArgs f = {a.hidden, weight, a.ldh, a.ldw, a.rows, values, a.width};
-        ZENO_STEP(a.dtype == ZENO_F32 ? (start_few_dz<float, kBf16Three>(f, d, stream))
-                                      : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16TwoHalfTwo>(f, d, stream)));
-      } else {
+      ZENO_STEP(a.dtype == ZENO_F32 ? (start_few_dz<float, kBf16Three>(f, d, stream))
+                                    : half ? (start_few_dz<_Float16, kHalfTwo>(f, d, stream)) : (start_few_dz<__bf16, kBf16TwoHalfTwo>(f, d, stream)));
+    }
+    // The weights of the piece: at once where they are read as they stand, or as many as are packed at a time.
+    const bool products = a.rows > 0 && (!p.few || a.dhidden != nullptr);
+    for (int s0 = 0; products && s0 < values; s0 += direct ? p.piece : p.pack) {
+      const int here = std::min(direct ? p.piece : p.pack, values - s0);
+      ZENO_STEP(side_of(weights(v0 + s0), a.ldw, a.dtype, here, a.width, reinterpret_cast<u16*>(ws + p.weight), l.w, stream));
+      if (!p.few) {
+        DzArgs part = d;
+        part.dz = d.dz + s0;
+        part.l.v0 = v0 + s0;
         const int side = p.wide_logits ? kWideSide : kTileSide;
-        l.tiles_m = ceil_div(values, side);
-        l.tiles_n = ceil_div(a.rows, side);
-        ZENO_STEP(p.wide_logits ? start_dz<WideTile>(d, a.dtype, stream) : start_dz<ThirdTile>(d, a.dtype, stream));
+        part.l.tiles_m = ceil_div(here, side);
+        part.l.tiles_n = ceil_div(a.rows, side);
+        ZENO_STEP(p.wide_logits ? start_dz<WideTile>(part, a.dtype, stream) : start_dz<ThirdTile>(part, a.dtype, stream));
       }
       if (a.dhidden != nullptr) {
         HiddenArgs h = {};
-        h.dz = {d.dz, d.ldz, d.plane, a.rows};
+        h.dz = {d.dz + s0, d.ldz, d.plane, a.rows};
         h.w = l.w;
         h.w.extent = l.width;   // (across the contraction: columns)
         h.pairs = pairs_of(3, 3);
@@ -1440,9 +1446,9 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
         h.tiles_n = ceil_div(a.width, tile);
         h.rows = a.rows;
         h.width = a.width;
-        h.length = values;
-        h.per = ceil_div(ceil_div(values, p.splits), kStep) * kStep;
-        h.first = v0 == 0;
+        h.length = here;
+        h.per = ceil_div(ceil_div(here, p.splits), kStep) * kStep;
+        h.first = v0 + s0 == 0;
         h.slots = slots;
         ZENO_STEP(p.wide_hidden ? start_hidden<WideTile>(h, a.dtype, p.splits, stream) : start_hidden<MidTile>(h, a.dtype, p.splits, stream));
       }

@@ -44,6 +44,11 @@ struct PlanLayout {
 constexpr int kFewRows = 64, kFewRowsF32 = 256;
 inline bool few_tokens(int rows, int dtype) { return rows <= (dtype == ZENO_F32 ? kFewRowsF32 : kFewRows); }
 
+// Of so many rows of W, multiples of 256.
+inline int packed_at_a_time(long long values, long long padded) {
+  return (int)std::min<long long>(tiles_along(values, 256) * 256, std::max<long long>(256, kPackElements / padded / 256 * 256));
+}
+
 struct ForwardPlan {
   bool few, wide;
   int slice;          // values of the vocabulary in a slice
@@ -59,7 +64,7 @@ inline ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
   p.wide = enough_wide_tiles(vocab, p.block);
   p.slice = p.few ? kFewSlice : (p.wide ? kWideSide : kTileSide) / 2;
   const long long padded = padded_width(width);
-  p.piece = (int)std::min<long long>((vocab + 255) / 256 * 256LL, std::max<long long>(256, kPackElements / padded / 256 * 256));
+  p.piece = packed_at_a_time(vocab, padded);
   PlanLayout l;
   p.hidden = l.take(p.few ? 0 : (size_t)planes_of(dtype) * p.block * padded * 2);
   p.weight = l.take(p.few ? 0 : (size_t)planes_of(dtype) * std::min(p.piece, vocab) * padded * 2);
@@ -74,6 +79,7 @@ inline ForwardPlan forward_plan(int rows, int vocab, int width, int dtype) {
 struct BackwardPlan {
   bool few, wide_logits, wide_hidden, wide_weight;
   int piece;          // values of the vocabulary at a time
+  int pack;           // values that are packed at a time
   int planes;         // of dz
   int splits, parts;
   size_t hidden, weight, dz, slots, sums, power, up, half, columns, bytes;
@@ -82,10 +88,12 @@ inline BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int
   BackwardPlan p;
   const long long padded = padded_width(width), n = std::max(rows, 1);
   p.planes = dz_planes_of(dtype);
-  // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles
+  // 64 M values of dz at a time: its planes stay near the caches, and a piece still has a thousand tiles.  Of more than 32768 tokens 2048 values each, or every piece's
+  // sums for the hidden states would cost more than its products: dz grows with the tokens then (2^20 tokens in bf16: 17 GB).
   const long long most = std::max<long long>(2048, ((64LL << 20) / n) / 256 * 256);
   const long long pieces = (vocab + most - 1) / most;
   p.piece = (int)(((vocab + pieces - 1) / pieces + 255) / 256 * 256);
+  p.pack = packed_at_a_time(p.piece, padded);
   p.few = few_tokens(rows, dtype);
   p.wide_logits = enough_wide_tiles(p.piece, n);
   p.wide_hidden = enough_wide_tiles(n, width);
@@ -99,7 +107,7 @@ inline BackwardPlan backward_plan(int rows, int vocab, int width, int dtype, int
   p.parts = (int)std::max<long long>(1, std::min<long long>(n / m / 512, 512 / weights));
   PlanLayout l;
   p.hidden = l.take((size_t)planes_of(dtype) * n * padded * 2);
-  p.weight = l.take((size_t)planes_of(dtype) * p.piece * padded * 2);
+  p.weight = l.take((size_t)planes_of(dtype) * p.pack * padded * 2);
   p.dz = l.take((size_t)p.planes * n * p.piece * 2);
   p.slots = l.take((size_t)p.splits * n * width * 4);
   p.sums = l.take(p.parts > 1 ? (size_t)p.parts * m * std::min(p.piece, vocab) * (width + 1LL) * 4 : 0);

@@ -27,6 +27,9 @@ int main() {
     rows = 8200, vocab = 8500, width = 1544, m = 2;
     const BackwardPlan two = backward_plan(rows, vocab, width, dtype, m);
     CHECK(two.wide_weight && two.wide_hidden && two.wide_logits && two.piece < vocab);
+    // tests/test_gpu_linear_logprobs_corners.py
+    rows = 70, vocab = 10000, width = 8191, m = 1;
+    CHECK(backward_plan(rows, vocab, width, dtype, m).pack < backward_plan(rows, vocab, width, dtype, m).piece);
     rows = 2000, vocab = 6400, width = 512, m = 4;
     CHECK(!backward_plan(rows, vocab, width, dtype, m).wide_weight);
   }
@@ -52,6 +55,7 @@ int main() {
             }
             const BackwardPlan b = backward_plan(rows, vocab, width, dtype, m);
             CHECK(b.piece % 256 == 0 && b.splits >= 1 && b.parts >= 1);
+            CHECK(b.pack % 256 == 0 && b.pack <= b.piece && (b.pack == 256 || (long long)b.pack * padded_width(width) <= kPackElements));
             const int s = b.wide_logits ? kWideSide : kTileSide, t = b.wide_weight ? kWideSide : kTileSide;
             CHECK(tiles_along(b.piece, s) * tiles_along(rows, s) <= kMostBlocks);
             CHECK(tiles_along(b.piece, t) * tiles_along(width, t) <= kMostBlocks);

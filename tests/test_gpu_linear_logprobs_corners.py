@@ -2,6 +2,9 @@
 import pytest
 import torch
 
+from _tokens import TYPES
+from test_gpu_linear_logprobs import backward
+
 pytestmark = pytest.mark.gpu
 
 
@@ -31,3 +34,10 @@ def test_the_most_tiles(B, rows, vocab):
     assert logp[5] == 0
     logp[5] = -size
     assert (logp + size).abs().max() <= near and (entropy - size).abs().max() <= near and (stats[:, 0] == 2).all()
+
+
+@pytest.mark.parametrize("ty", TYPES)
+@pytest.mark.parametrize("rows,offsets", [(5, None), (70, [0, 30, 69]), (300, None)])
+def test_weights_that_are_packed_in_pieces(B, rows, offsets, ty):
+    """More weights than are packed at a time in one piece of dz: few tokens, and tiles."""
+    backward(B, rows, 10000, 8191, ty, offsets, False, seed=21)

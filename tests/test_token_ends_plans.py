@@ -32,3 +32,13 @@ def test_plans(tmp_path):
                    check=True, capture_output=True, text=True)
     res = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert res.returncode == 0 and "plan checks passed" in res.stdout, res.stdout + res.stderr
+
+
+@pytest.mark.parametrize("dtype", range(3))
+def test_weights_of_a_few_tokens_are_packed_in_pieces(lib, dtype):
+    """Copies of weights: 64 M of them a plane, in either direction.  Beside them 32 tokens' dz (four planes of 262144 values at most), their copies
+    and the sums of their hidden states' gradients in eight slots."""
+    rows, vocab, width = 32, 1 << 18, 1 << 13
+    got = lib.zeno_linear_logprobs_backward_workspace_bytes(rows, vocab, width, dtype, 1)
+    planes = 3 if dtype == 0 else 1
+    assert got <= 2 * planes * (64 << 20) + 8 * rows * vocab + (8 + 8 * 4) * rows * width + 8 * width + 65536
