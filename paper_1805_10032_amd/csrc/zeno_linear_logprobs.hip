@@ -770,41 +770,53 @@ Pairs pairs_of(int a, int b) {   // planes of the two sides: three and three, tw
 static_assert(WideTile::BM == kWideSide && WideTile::WM == 2 && MidTile::BM == kTileSide && ThirdTile::BM == kTileSide &&
                   ThirdTile::WM == 2,
               "as the plans have it");
-// A worker's dz is formed within 2^14, from gradients times a power of two: that of the largest that one of its tokens brings, |dz| <= |g| + 22 |q| (p |log p| <= 1/e,
-// p H <= ln V < 21).  float32's pieces have its range and hold dz itself; 16 bits hold it as it is formed.  Powers from -119 (the largest finite g and q) to 126 are float32's
-// own, and so are their inverses.  One workgroup a worker: another's gradients, or those of nobody, do not show.  `clear`: a worker's n words to set to zero on
+__device__ inline float power_of_two(int k) { return __uint_as_float((unsigned)(127 + k) << 23); }   // k from -126 to 127
+// dz is formed within 2^14, from gradients times a power of two: that of the largest, |dz| <= |g| + 22 |q| (p |log p| <= 1/e, p H <= ln V < 21).  In 16 bits, which
+// hold dz as it is formed, the largest of a worker; one workgroup a worker: another's gradients, or those of nobody, do not show.  float32's pieces have its range and hold dz
+// itself: a token's own.  Powers from -119 (the largest finite g and q) to 126 are float32's own, and so are their inverses.  `clear`: a worker's n words to set to zero on
 // the way.
 struct ScaleArgs {
   const float *g, *q;
   const int32_t *labels, *offsets;
   int rows;
+  bool own;              // each token its own
   int* power;            // [m]
   float* up;             // [rows] 2^power
   unsigned* clear;
   int n;
 };
+// Of a 32nd of the largest, which no finite gradients take beyond float32.
+__device__ inline int grad_power(float largest) {
+  const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126 + 5;   // 32 largest < 2^e
+  return 14 - e < 126 ? 14 - e : 126;
+}
 __global__ __launch_bounds__(1024) void grad_scale_kernel(ScaleArgs a) {
   __shared__ float shared[16];
   __shared__ int all;
   const int worker = blockIdx.x, begin = group_offset(a.offsets, worker, a.rows), end = group_offset(a.offsets, worker + 1, a.rows);
-  float largest = 0.f;   // a 32nd of it, which no finite gradients take beyond float32
-  for (int i = threadIdx.x; i < a.n; i += 1024) a.clear[(long long)worker * a.n + i] = 0;
-  for (int t = begin + threadIdx.x; t < end; t += 1024) {
+  auto size_of = [&](int t) {
     float b = a.g != nullptr && a.labels[t] != -1 ? fabsf(a.g[t]) * 0.03125f : 0.f;
     if (a.q != nullptr) b += 0.6875f * fabsf(a.q[t]);
-    if (b < __builtin_inff()) largest = fmaxf(largest, b);
+    return b;
+  };
+  float largest = 0.f;
+  for (int i = threadIdx.x; i < a.n; i += 1024) a.clear[(long long)worker * a.n + i] = 0;
+  for (int t = begin + threadIdx.x; t < end; t += 1024) {
+    const float b = size_of(t);
+    if (a.own) a.up[t] = power_of_two(grad_power(b));
+    else if (b < __builtin_inff()) largest = fmaxf(largest, b);
   }
+  if (a.own) return;
   largest = wave_max_f(largest);
   if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = largest;
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 16; ++w) largest = fmaxf(largest, shared[w]);
-    const int e = (int)((__float_as_uint(largest) >> 23) & 255) - 126 + 5;   // 32 largest < 2^e
-    all = 14 - e < 126 ? 14 - e : 126;
+    all = grad_power(largest);
     a.power[worker] = all;
   }
   __syncthreads();
-  const float up = __uint_as_float((unsigned)(127 + all) << 23);
+  const float up = power_of_two(all);
   for (int t = begin + threadIdx.x; t < end; t += 1024) a.up[t] = up;
 }
 
@@ -816,8 +828,6 @@ __device__ inline int column_power(unsigned largest) {   // largest magnitude, a
   return up > 126 ? 126 : up;                            // (not below 14 + 127 - 254)
 }
 __host__ __device__ inline int padded_stride(int width) { return (width + 7) / 8 * 8; }
-__device__ inline float power_of_two(int k) {   // -126 .. 127
-  return __uint_as_float((unsigned)(127 + k) << 23); }
 constexpr int kColumnRows = 256;   // of a workgroup
 struct ColumnArgs {
   Side h;
@@ -1379,7 +1389,7 @@ hipError_t launch_linear_logprobs_backward(const LinearLogprobsGradArgs& a, void
   const bool convert = a.dtype == ZENO_BF16 && (a.dweight != nullptr || a.dbias != nullptr) && a.rows > 0;
   unsigned* columns = reinterpret_cast<unsigned*>(ws + p.columns);
   float* up = reinterpret_cast<float*>(ws + p.up);
-  const ScaleArgs sc = {a.grad_logp, a.grad_entropy, a.labels, a.offsets, a.rows, power, up, columns, convert ? a.width : 0};
+  const ScaleArgs sc = {a.grad_logp, a.grad_entropy, a.labels, a.offsets, a.rows, planes == 3, power, up, columns, convert ? a.width : 0};
   grad_scale_kernel<<<a.m, 1024, 0, stream>>>(sc);
   ZENO_STEP(hipGetLastError());
   DzArgs d = {};

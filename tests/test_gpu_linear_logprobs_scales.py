@@ -87,3 +87,21 @@ def test_gradients_of_the_entropy_near_the_largest_number(B, ty):
     rows, vocab, width = 12, 200, 16
     q = torch.full((rows,), 0.75, device="cuda")
     check(B, rows, vocab, width, ty, [0, 6, 12], [124, -70], None, q)
+
+
+@pytest.mark.parametrize("rows,vocab,width", [(40, 90, 24), (300, 90, 24)])
+def test_small_and_large_gradients_of_one_group_in_float32(B, rows, vocab, width):
+    """A token's gradient does not depend on another's: a power of two scales a row of dhidden exactly, 2^-80 beside 2^80 (all terms and sums of both
+    stay normal but for those below 2^-40 of the largest)."""
+    h, w, b, labels = problem(rows, vocab, width, torch.float32, 23, spread=1.0)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    g = -0.5 - 0.5 * torch.rand(rows, generator=gen, device="cuda")
+    q = 0.1 * torch.rand(rows, generator=gen, device="cuda")
+    _, entropy, stats = B.zeno_linear_logprobs(h, w, b, labels, want_entropy=True, want_stats=True)
+    factor = torch.where(torch.arange(rows, device="cuda") % 2 == 0, 2.0 ** 80, 2.0 ** -80)
+
+    def dhidden(g, q):
+        return B.zeno_linear_logprobs_backward(h, w, b, stats, labels=labels, grad_logp=g, entropy=entropy, grad_entropy=q, want_weight=False,
+                                               want_bias=False)[0]
+    plain, far = dhidden(g, q), dhidden(g * factor, q * factor)
+    assert (far.double() / factor[:, None].double() - plain.double()).abs().max() <= 2.0 ** -40 * vocab
