@@ -385,7 +385,9 @@ zeno_status_t zeno_linear_logprobs(const void* hidden, int64_t ldh, const void* 
  * of the group), and bf16 hidden states are exact in them down to 2^-32 of the largest in their column and group; dhidden, which is rounded itself, is taken from
  * dz in two pieces of the type: off by at most 2^-16 of it in bf16, 2^-22 in fp16 or 2^-38 of the group's largest gradient.  In float32 dz is three bf16 pieces.
  * One group's values do not show in another's gradients.
- *   stats, entropy  as zeno_linear_logprobs wrote them (entropy only if grad_entropy is given)
+ *   stats, entropy  as zeno_linear_logprobs wrote them (entropy only if grad_entropy is given) in a call with as many rows: up to 64 of them (256 in
+ *            float32) another kernel forms the logits than beyond, and where the two calls' logits differ in their last bits, that is all that is left of a
+ *            nearly certain token's gradient
  *   labels, grad_logp        DEVICE [rows] or both NULL; a row with label -1 takes no part in g, another label outside 0..vocab-1 gives NaN
  *   grad_entropy             DEVICE [rows] or NULL
  *   dhidden  DEVICE [rows x width] of `dtype`, rows lddh apart, or NULL; may be hidden itself with lddh = ldh

@@ -50,8 +50,9 @@ struct Tile {
 using WideTile = Tile<256, 256, 2, 2>;
 using MidTile = Tile<128, 128, 2, 2>;
 // Three workgroups a compute unit, a stage less: logits and weight gradients, whose stores and exponentials another workgroup runs beside (20 x 100 tokens'
-// weight gradients, 32000 x 1024: 646 us, with two workgroups 700; 777 x 10007 x 513 float32: logits 108 and 111, weight gradients 83 and 85).  Long sums
-// are faster with two (20 x 100 tokens' dz W 171 and 190).
+// weight gradients, 32000 x 1024: 646 us, with two workgroups 700; 777 x 10007 x 513 float32: logits 108 and 111, weight gradients 83 and 85).  Sums over
+// the vocabulary keep two: with one plane of dz they were faster so (20 x 100 tokens' dz W 171 us, with three 190); with two planes there is little between them (294 and 286,
+// 250 tokens 103 and 100; float32 120 and 110).
 using ThirdTile = Tile<128, 128, 2, 2, 3>;
 
 // An operand: planes of 16-bit values, `plane` elements apart, rows ld apart and on 16 bytes.
@@ -1111,7 +1112,7 @@ __global__ __launch_bounds__(S::THREADS, S::GROUPS) void hidden_grad_kernel(Hidd
         const int row = row0 + 32 * r + row_of(e, lane), col = col0 + 32 * j;
         if (row >= a.rows || col >= a.width) continue;
         // One workgroup adds one value of a launch, so the order is that of the launches; nothing is waited for.  (Sums that go on from what the
-        // slot holds 600 us a piece of 8192 x 8192 x 4096, loaded behind the products 684, stored 500.)
+        // slot holds 600 us a piece of 8192 x 8192 x 4096 with one plane of dz, loaded behind the products 684, stored 500.)
         float* to = slot + (long long)row * a.width + col;
         if (a.first) *to = acc[r][j][e];
         else unsafeAtomicAdd(to, acc[r][j][e]);
